@@ -88,8 +88,8 @@ def work(case):
         return {"bytes": M * K * (3 * s + 6) + gate_in + gate_out + 3 * weights, "flops": 30 * M * K}
     M, V, b = case["M"], case["V"], 2 if case["dtype"] == "bf16" else 4
     if op == "logprobs":
-        return {"bytes": M * V * b + M * (8 + 12 + 8 * case["top"]), "flops": 6 * M * V}
-    return {"bytes": 2 * M * V * b + M * 24, "flops": 8 * M * V}
+        return {"bytes": M * V * b + M * (8 + 16 + 8 * case["top"]), "flops": 6 * M * V}
+    return {"bytes": 2 * M * V * b + M * 28, "flops": 8 * M * V}
 
 
 # ------------------------------------------------------------------------------------------------ inputs
@@ -193,14 +193,17 @@ def prepare(case, seed):
     st["logits"] = x
     if op == "logprobs_bwd":
         T = case["temp"]
-        st["logp"], st["lse"], st["entropy"] = (torch.empty(M, device=_DEV) for _ in range(3))
+        st["logp"], st["peak"], st["log_sum"], st["entropy"] = (torch.empty(M, device=_DEV) for _ in range(4))
         for r in range(0, M, 256):
             z = x[r:r + 256].double() / T
-            lse = torch.logsumexp(z, -1, keepdim=True)
+            peak = z.amax(-1, keepdim=True)
+            log_sum = (z - peak).exp().sum(-1, keepdim=True).log()
+            z = z - peak - log_sum
             tok = st["tokens"][r:r + 256]
-            st["logp"][r:r + 256] = (z - lse).gather(1, tok.clamp_min(0)[:, None])[:, 0] * (tok >= 0)
-            st["lse"][r:r + 256] = lse[:, 0]
-            st["entropy"][r:r + 256] = -((z - lse).exp() * (z - lse)).sum(-1)
+            st["logp"][r:r + 256] = z.gather(1, tok.clamp_min(0)[:, None])[:, 0] * (tok >= 0)
+            st["peak"][r:r + 256] = x[r:r + 256].amax(-1).float()
+            st["log_sum"][r:r + 256] = log_sum[:, 0]
+            st["entropy"][r:r + 256] = -(z.exp() * z).sum(-1)
         st["dlogp"] = torch.randn(M, generator=g, device=_DEV)
         st["dentropy"] = torch.full((M,), -0.01, device=_DEV) if case["entropy"] else None
     return st
@@ -223,8 +226,8 @@ def run(st):
                                           act=st["case"]["act"], alpha=st["alpha"], eps=st["eps"])
         if op == "logprobs":
             return rq.token_logprobs(st["logits"], st["tokens"], temperature=st["case"]["temp"], top=st["case"]["top"])
-        return rq.token_logprobs_backward(st["logits"], st["tokens"], st["logp"], st["lse"], st["entropy"], st["dlogp"],
-                                          st["dentropy"], temperature=st["case"]["temp"])
+        return rq.token_logprobs_backward(st["logits"], st["tokens"], st["logp"], st["peak"], st["log_sum"], st["entropy"],
+                                          st["dlogp"], st["dentropy"], temperature=st["case"]["temp"])
     return {"gemv": _gemv, "join": _join, "join_bwd": _join_bwd, "logprobs": _logprobs, "logprobs_bwd": _logprobs_bwd}[op](st)
 
 
@@ -305,7 +308,8 @@ def _logprobs(st):
     others = e.scatter(1, m.indices, 0.0).sum(-1, keepdim=True)
     log_s = torch.log1p(others)
     logp = torch.where(tok >= 0, (z.gather(1, tok.clamp_min(0)[:, None]) - log_s)[:, 0], torch.zeros_like(log_s[:, 0]))
-    out = {"logp": logp, "entropy": (log_s - (z * e).sum(-1, keepdim=True) / (1 + others))[:, 0], "lse": (m.values / T + log_s)[:, 0]}
+    out = {"logp": logp, "entropy": (log_s - (z * e).sum(-1, keepdim=True) / (1 + others))[:, 0], "peak": m.values[:, 0],
+           "log_sum": log_s[:, 0]}
     if top:
         # one whole number for each logit that orders by value, then by lower place
         bits = (x + 0.0).view(torch.int32)
@@ -317,7 +321,7 @@ def _logprobs(st):
 
 def _logprobs_bwd(st):
     x, tok, T = st["logits"].float(), st["tokens"], st["case"]["temp"]
-    z = x / T - st["lse"][:, None]
+    z = (x - st["peak"][:, None]) / T - st["log_sum"][:, None]
     p = torch.exp(z)
     there = tok >= 0
     dlogp = torch.where(there, st["dlogp"], torch.zeros_like(st["dlogp"]))
@@ -411,7 +415,7 @@ def exact(case, seed):
         p = torch.exp(logp)
         H = -(p * logp).sum(1, keepdim=True)
         if op == "logprobs":
-            row = {"logp": (hot * logp).sum(1), "entropy": H[:, 0], "lse": lse[:, 0]}
+            row = {"logp": (hot * logp).sum(1), "entropy": H[:, 0], "peak": x.amax(1), "log_sum": (lse - x.amax(1, keepdim=True) / T)[:, 0]}
             if case["top"]:
                 best = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :case["top"]]
                 row["top_ids"], row["top_logp"] = best.int(), logp.gather(1, best)
