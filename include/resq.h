@@ -347,6 +347,81 @@ RESQ_API int mxfp4_w16a4_linear(const void* X_bf16, int64_t M, int64_t K, int64_
                        int pattern, void* Y, int out_dtype, int64_t ldy,
                        void* workspace, size_t ws_bytes, void* stream);
 
+/* ---- the weight-only product for a few tokens (Table 1's "W4A16" in its single-token form; the grouping into a call of
+ * its own is this library's) ---------------------------------------------------------------------------------------
+ * Y = X deq(Q(W))^T as *_w4a16_linear, for 1 <= M <= RESQ_GEMV_MAX_TOKENS token rows, as a matrix-vector kernel that
+ * streams the packed weights once (a GEMM tile computes 128 token rows whatever M is).  Same argument rules and output
+ * types; no workspace.  Products of decoded weights and bf16 activations are exact, sums are held in fp32 and added in a
+ * fixed order (bit-identical results run to run; the order depends on M, N and K).  An infinity or NaN in a row of X
+ * makes that row of Y follow IEEE arithmetic (0 x inf = NaN) and leaves the others alone; an MXFP4 weight of 2^128 or more
+ * (scale codes 253 and above) is infinite, as in mxfp4_dequantize. */
+#define RESQ_GEMV_MAX_TOKENS 16
+RESQ_API int hif4_w4a16_gemv(const void* X_bf16, int64_t M, int64_t K, int64_t ldx,
+                    const void* w_codes, const void* w_meta, int64_t N,
+                    void* Y, int out_dtype, int64_t ldy, void* stream);
+RESQ_API int mxfp4_w4a16_gemv(const void* X_bf16, int64_t M, int64_t K, int64_t ldx,
+                     const void* w_codes, const void* w_scale, int64_t N,
+                     void* Y, int out_dtype, int64_t ldy, void* stream);
+
+/* ---- the residual stream between two blocks, and its gradients (no counterpart in the paper) -----------------------
+ * What lies between the output projection of one block and the input projection of the next, in one pass:
+ *     p  = B rp gamma_post,  rp[m] = 1 / sqrt(sum_k B[m,k]^2 / K + eps)     (gamma_post NULL: p = B, no norm)
+ *     H' = H + alpha g p,    g = 1 (gate NULL) | gate (RESQ_GATE_LINEAR) | 1 / (1 + exp(-gate)) (RESQ_GATE_SIGMOID)
+ *     X  = H' r gamma_pre,   r[m]  = 1 / sqrt(sum_k H'[m,k]^2 / K + eps)    (X NULL: H' only)
+ *   H, H_out [M, K]: the residual stream in bf16 or fp32 (`stream_dtype`, a resq_out); B_bf16 [M, K]: the block's output;
+ *   gate_bf16: [M, K] with row pitch ldg, or with ldg = 0 one row [K] for all tokens; gamma_* bf16 [K], 16-byte aligned.
+ *   X_bf16 [M, K] is what *_resq_linear and its relatives take.  1 <= K <= RESQ_JOIN_MAX_K, any K in that range; rows
+ *   start on 16-byte boundaries (ld % 8 == 0 for bf16, % 4 for fp32) and what lies behind column K is neither read nor
+ *   written.  H_out may be H itself; other overlaps are not allowed.  Sums, norms and H' before its one rounding are
+ *   fp32; X is formed from the unrounded H'.  alpha and eps finite, eps >= 0.
+ * Backward: the gradients of these formulas at H_out and B as given (the row factors are formed again from them), with
+ *   dH_out (type of the stream) and / or dX bf16 the gradients of the two outputs (either may be NULL = zero):
+ *     dH [M, K] (type of the stream; may be dH_out itself), dB bf16 [M, K], dgate (bf16 [M, K] with pitch lddg; for a
+ *     channel gate fp32 [K]), dgamma_post fp32 [K], dgamma_pre fp32 [K] (required where the input it belongs to is
+ *     given, dgamma_pre where dX is; otherwise ignored).  Sums over the tokens are fp32 in a fixed order.
+ *   workspace of resq_block_join_backward_workspace_bytes(M, K) bytes, 256-byte aligned, owned by the call until it has
+ *   run (it holds partial sums; no status word). */
+typedef enum { RESQ_GATE_LINEAR = 0, RESQ_GATE_SIGMOID = 1 } resq_gate;
+#define RESQ_JOIN_MAX_K 32768
+RESQ_API int resq_block_join(const void* H, int stream_dtype, const void* B_bf16, int64_t M, int64_t K, int64_t ldh, int64_t ldb,
+                    const void* gate_bf16, int64_t ldg, int gate_act, const void* gamma_post_bf16, const void* gamma_pre_bf16,
+                    float alpha, float eps, void* H_out, int64_t ldho, void* X_bf16, int64_t ldx, void* stream);
+RESQ_API size_t resq_block_join_backward_workspace_bytes(int64_t M, int64_t K);
+RESQ_API int resq_block_join_backward(const void* dH_out, const void* dX_bf16, const void* H_out, int stream_dtype, const void* B_bf16,
+                             int64_t M, int64_t K, int64_t lddho, int64_t lddx, int64_t ldho, int64_t ldb,
+                             const void* gate_bf16, int64_t ldg, int gate_act, const void* gamma_post_bf16,
+                             const void* gamma_pre_bf16, float alpha, float eps, void* dH, int64_t lddh, void* dB_bf16,
+                             int64_t lddb, void* dgate, int64_t lddg, float* dgamma_post, float* dgamma_pre,
+                             void* workspace, size_t ws_bytes, void* stream);
+
+/* ---- log-probabilities of given tokens, with entropy and top alternatives, and the gradient of the logits ----------
+ * What a rollout records and a policy loss reads from the rows of logits that the output projection (any call above that
+ * writes Y) leaves; the paper's rollout and training policies are compared through these values (Section 2).
+ *     peak = max_j logits_j,  log_sum = log sum_j exp((logits_j - peak) / temperature),
+ *     log p_j = (logits_j - peak) / temperature - log_sum,  logp = log p_tok,  entropy = -sum_j p_j log p_j
+ *   (the log-sum-exp of the scaled logits is peak / temperature + log_sum; apart, they keep their digits in rows of very
+ *   large or very low values)
+ *   logits [M, V] bf16 or fp32 (`dtype`, a resq_out), row pitch ld (ld % 8 == 0 for bf16, % 4 for fp32; what lies behind
+ *   column V is not read); tokens int64 [M]; temperature in 1e-6 .. 1e6.  logp, entropy, peak, log_sum fp32 [M], each may
+ *   be NULL.
+ *   top: 0 .. min(V, RESQ_MAX_TOP) largest logits of each row, largest first, equal ones by lower id (-0 equals 0, NaN
+ *   ranks above +inf): top_ids int32 [M, top], top_logp fp32 [M, top].
+ *   - a token outside 0 .. V - 1 names none (prompt, padding): logp 0, and no gradient through logp;
+ *   - a logit of -inf is masked: probability 0, logp -inf; a row of nothing else has peak -inf, log_sum 0, entropy 0,
+ *     logp -inf for every token, and a gradient of zeros; a row with +inf or NaN has NaN for all of them.
+ * Backward: dlogits (type of the logits, row pitch ldd; may be the logits' own buffer with ldd = ld)
+ *     dlogits_j = (1 / temperature) (dlogp (1[j = tok] - p_j) - dentropy p_j (log p_j + entropy))
+ *   from the forward call's logp, peak, log_sum and entropy and the gradients dlogp [M] and dentropy [M] (NULL: none, and entropy
+ *   is not read).  The top alternatives have no gradient.  Both calls read the logits once and need no workspace. */
+#define RESQ_MAX_TOP 32
+#define RESQ_MAX_VOCAB (1 << 28)
+RESQ_API int resq_token_logprobs(const void* logits, int dtype, int64_t M, int64_t V, int64_t ld, const int64_t* tokens,
+                        float temperature, int top, float* logp, float* entropy, float* peak, float* log_sum,
+                        int32_t* top_ids, float* top_logp, void* stream);
+RESQ_API int resq_token_logprobs_backward(const void* logits, int dtype, int64_t M, int64_t V, int64_t ld, const int64_t* tokens,
+                                 float temperature, const float* logp, const float* peak, const float* log_sum,
+                                 const float* entropy, const float* dlogp, const float* dentropy, void* dlogits, int64_t ldd, void* stream);
+
 /* ---- status --------------------------------------------------------------------------------------
  * resq_check synchronizes `stream` and returns the device status word kept at the start of
  * `workspace` (RESQ_OK, or RESQ_ERR_TIMEOUT if a bounded wait expired in the last call that used it). */
@@ -360,7 +435,8 @@ RESQ_API const char* resq_last_error(void);
  * resq_profile_read: synchronizes on the recorded events, adds the device time (ms) and the number of
  * launches per kernel kind into the two arrays of 4 entries (0 = quantizer/residual/mask pass,
  * 1 = top-k select and mask apply, 2 = GEMM, 3 = split-K reduce; either array may be NULL) and
- * clears the records.
+ * clears the records.  (resq_block_join and resq_token_logprobs and their backward calls are counted as launches but
+ * have no kind here.)
  * resq_debug_expire_next_wait(1): test hook for the RESQ_ERR_TIMEOUT path.  The next decode-sized GEMM launch of
  * the process (K-streamed schedule: M > 128 and few output tiles) waits at its end for one partial tile more than
  * its CTAs can deliver, with a poll limit of about a millisecond: the bounded wait runs out, the kernel records

@@ -6,6 +6,7 @@ this module raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Tuple
@@ -24,6 +25,7 @@ STATUS_NAMES = {0: "OK", 1: "ERR_NULL", 2: "ERR_SHAPE", 3: "ERR_ALIGN", 4: "ERR_
 
 # every symbol include/resq.h declares: (name, restype, argtypes)
 _i64, _vp, _ci, _sz = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+_cf = ctypes.c_float
 SYMBOLS = {
     "hif4_codes_bytes": (_sz, [_i64, _i64]),
     "hif4_meta_bytes": (_sz, [_i64, _i64]),
@@ -75,6 +77,14 @@ SYMBOLS = {
     "mxfp4_rht_resq_linear": (_ci, [_vp, _i64, _i64, _i64, ctypes.c_ulonglong, _vp, _vp, _i64, _ci, _vp, _ci, _i64, _vp, _sz, _vp]),
     "hif4_w16a4_linear": (_ci, [_vp, _i64, _i64, _i64, _vp, _i64, _i64, _ci, _vp, _ci, _i64, _vp, _sz, _vp]),
     "mxfp4_w16a4_linear": (_ci, [_vp, _i64, _i64, _i64, _vp, _i64, _i64, _ci, _vp, _ci, _i64, _vp, _sz, _vp]),
+    "hif4_w4a16_gemv": (_ci, [_vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _ci, _i64, _vp]),
+    "mxfp4_w4a16_gemv": (_ci, [_vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _ci, _i64, _vp]),
+    "resq_block_join": (_ci, [_vp, _ci, _vp, _i64, _i64, _i64, _i64, _vp, _i64, _ci, _vp, _vp, _cf, _cf, _vp, _i64, _vp, _i64, _vp]),
+    "resq_block_join_backward_workspace_bytes": (_sz, [_i64, _i64]),
+    "resq_block_join_backward": (_ci, [_vp, _vp, _vp, _ci, _vp, _i64, _i64, _i64, _i64, _i64, _i64, _vp, _i64, _ci, _vp, _vp, _cf, _cf,
+                                       _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "resq_token_logprobs": (_ci, [_vp, _ci, _i64, _i64, _i64, _vp, _cf, _ci, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "resq_token_logprobs_backward": (_ci, [_vp, _ci, _i64, _i64, _i64, _vp, _cf, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
     "resq_check": (_ci, [_vp, _vp]),
     "resq_last_error": (ctypes.c_char_p, []),
     "resq_kernel_launches": (_i64, []),
@@ -503,6 +513,211 @@ def w16a4_linear(X: torch.Tensor, W: torch.Tensor, pattern: int = S_NONE, fmt: s
         OUT_BF16 if Y.dtype == torch.bfloat16 else OUT_F32, Y.stride(0), workspace.data_ptr(), workspace.numel(),
         _stream(stream)))
     return Y
+
+
+# ------------------------------------------------------------------ few-token product, residual stream, log-probabilities
+#
+# These calls run on the device of their first tensor (made current for the call) and on `stream` (default: that device's
+# current stream).  What they allocate belongs to that stream.
+
+GEMV_MAX_TOKENS = 16
+JOIN_MAX_K = 32768
+MAX_TOP = 32
+GATE_LINEAR, GATE_SIGMOID = 0, 1
+_GATES = {"linear": GATE_LINEAR, "sigmoid": GATE_SIGMOID}
+_OUT = {torch.bfloat16: OUT_BF16, torch.float32: OUT_F32}
+
+
+@contextlib.contextmanager
+def _entered(device: torch.device, stream):
+    """The device current and, if a stream is named, that stream current too: the allocator then ties what the call
+    allocates to the stream its kernels run on."""
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
+    with torch.cuda.device(device), torch.cuda.stream(stream):
+        yield
+
+
+def _require(ok: bool, msg: str) -> None:
+    if not ok:
+        raise ValueError(msg)
+
+
+def _rows(t: torch.Tensor, name: str, shape, dtype, device) -> torch.Tensor:
+    """t as a [rows, cols] device matrix of one type with unit inner stride."""
+    if t.dim() != 2 or t.dtype != dtype or t.device != device or tuple(t.shape) != shape or (t.stride(1) != 1 and shape[1] > 1):
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {device} with unit inner stride")
+    return t
+
+
+def _vector(t: torch.Tensor, name: str, n: int, dtype, device) -> torch.Tensor:
+    if t.dim() != 1 or t.numel() != n or t.dtype != dtype or t.device != device or (t.stride(0) != 1 and n > 1):
+        raise ValueError(f"{name} must be a contiguous {dtype} vector of {n} elements on {device}")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Row pitch in elements; a single row has none of its own (any multiple of 8 that covers it will do)."""
+    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+
+
+def w4a16_gemv(X: torch.Tensor, w_codes: torch.Tensor, w_side: torch.Tensor, fmt: str = "hif4",
+               out_dtype: torch.dtype = torch.bfloat16, Y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """*_w4a16_gemv: Y = X deq(Q(W))^T for at most GEMV_MAX_TOKENS token rows, streaming the packed weights once."""
+    fn = _fn(fmt, "hif4_w4a16_gemv", "mxfp4_w4a16_gemv")
+    dev = X.device
+    _require_bf16_matrix(X, "X")
+    M, K = X.shape
+    N = w_codes.shape[0]
+    _packed(w_codes, w_side, N, K, fmt, dev)
+    with _entered(dev, stream):
+        if Y is None:
+            _require(out_dtype in _OUT, "Y must be bf16 or fp32")
+            Y = _out(M, N, out_dtype, dev)
+        _require(Y.dtype in _OUT, "Y must be bf16 or fp32")
+        _rows(Y, "Y", (M, N), Y.dtype, dev)
+        _check(fn(X.data_ptr(), M, K, _ld(X), w_codes.data_ptr(), w_side.data_ptr(), N, Y.data_ptr(), _OUT[Y.dtype], _ld(Y),
+                  _stream(None)))
+    return Y
+
+
+def _packed(codes: torch.Tensor, side: torch.Tensor, N: int, K: int, fmt: str, device) -> None:
+    block, dtype = (64, torch.int32) if fmt == "hif4" else (32, torch.uint8)
+    if codes.dtype != torch.uint8 or codes.shape != (N, K // 2) or not codes.is_contiguous() or codes.device != device or K % 2:
+        raise ValueError(f"w_codes must be contiguous uint8 [N, K/2] on {device} for the activations' K = {K}")
+    if side.dtype not in (dtype, torch.uint32 if dtype == torch.int32 else dtype) or side.shape != (N, K // block) \
+            or not side.is_contiguous() or side.device != device:
+        raise ValueError(f"w_meta / w_scale must be contiguous {dtype} [N, K/{block}] on {device}")
+
+
+def _join_args(H, B, gamma_pre, gamma_post, gate, act):
+    _require(H.dim() == 2 and H.is_cuda and H.dtype in _OUT, "H must be a 2-D CUDA tensor, bf16 or fp32")
+    _require(act in _GATES, f"unknown gate function {act!r}")
+    dev, (M, K) = H.device, H.shape
+    _rows(H, "H", (M, K), H.dtype, dev)
+    _rows(B, "B", (M, K), torch.bfloat16, dev)
+    for name, g in (("gamma_pre", gamma_pre), ("gamma_post", gamma_post)):
+        if g is not None:
+            _vector(g, name, K, torch.bfloat16, dev)
+    ldg = 0
+    if gate is not None and gate.dim() == 1:
+        _vector(gate, "gate", K, torch.bfloat16, dev)
+    elif gate is not None:
+        _rows(gate, "gate", (M, K), torch.bfloat16, dev)
+        ldg = _ld(gate)
+        _require(ldg != 0, "a gate shared by all tokens is given as a vector of K elements")
+    return dev, M, K, ldg
+
+
+def block_join(H: torch.Tensor, B: torch.Tensor, gamma_pre: Optional[torch.Tensor] = None, gamma_post: Optional[torch.Tensor] = None,
+               gate: Optional[torch.Tensor] = None, act: str = "linear", alpha: float = 1.0, eps: float = 1e-6,
+               H_out: Optional[torch.Tensor] = None, X: Optional[torch.Tensor] = None, stream=None):
+    """resq_block_join: H' = H + alpha g(gate) norm(B), X = norm(H') -> (H', X).
+
+    gamma_post None: the branch B is added as it is; gamma_pre None: X is None.  gate: None, [K] (one for all tokens) or
+    [M, K]; act "linear" or "sigmoid".  H_out may be H."""
+    dev, M, K, ldg = _join_args(H, B, gamma_pre, gamma_post, gate, act)
+    with _entered(dev, stream):
+        if H_out is None:
+            H_out = _out(M, K, H.dtype, dev)
+        if gamma_pre is None:
+            _require(X is None, "X needs gamma_pre")
+        elif X is None:
+            X = _out(M, K, torch.bfloat16, dev)
+        _rows(H_out, "H_out", (M, K), H.dtype, dev)
+        if X is not None:
+            _rows(X, "X", (M, K), torch.bfloat16, dev)
+        _check(lib().resq_block_join(H.data_ptr(), _OUT[H.dtype], B.data_ptr(), M, K, _ld(H), _ld(B), _ptr(gate), ldg, _GATES[act],
+                                     _ptr(gamma_post), _ptr(gamma_pre), alpha, eps, H_out.data_ptr(), _ld(H_out), _ptr(X),
+                                     0 if X is None else _ld(X), _stream(None)))
+    return H_out, X
+
+
+def block_join_backward_workspace_bytes(M: int, K: int) -> int:
+    return int(lib().resq_block_join_backward_workspace_bytes(M, K))
+
+
+def block_join_backward(dH_out: Optional[torch.Tensor], dX: Optional[torch.Tensor], H_out: torch.Tensor, B: torch.Tensor,
+                        gamma_pre: Optional[torch.Tensor] = None, gamma_post: Optional[torch.Tensor] = None,
+                        gate: Optional[torch.Tensor] = None, act: str = "linear", alpha: float = 1.0, eps: float = 1e-6,
+                        dH: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """resq_block_join_backward -> dict(dH, dB[, dgate][, dgamma_post][, dgamma_pre]) from the gradients of H' and X (either
+    may be None) and the forward call's H' and inputs.  dgate has the gate's shape, fp32 for a channel gate [K], else bf16;
+    the norms' gradients are fp32.  dH may be dH_out."""
+    dev, M, K, ldg = _join_args(H_out, B, gamma_pre, gamma_post, gate, act)
+    _require(dH_out is not None or dX is not None, "one of dH_out and dX is needed")
+    _require(dX is None or gamma_pre is not None, "dX needs gamma_pre")
+    if dH_out is not None:
+        _rows(dH_out, "dH_out", (M, K), H_out.dtype, dev)
+    if dX is not None:
+        _rows(dX, "dX", (M, K), torch.bfloat16, dev)
+    with _entered(dev, stream):
+        if dH is None:
+            dH = _out(M, K, H_out.dtype, dev)
+        _rows(dH, "dH", (M, K), H_out.dtype, dev)
+        out = {"dH": dH, "dB": _out(M, K, torch.bfloat16, dev)}
+        if dX is not None:
+            out["dgamma_pre"] = torch.empty(K, dtype=torch.float32, device=dev)
+        if gamma_post is not None:
+            out["dgamma_post"] = torch.empty(K, dtype=torch.float32, device=dev)
+        if gate is not None:
+            out["dgate"] = torch.empty(K, dtype=torch.float32, device=dev) if ldg == 0 else _out(M, K, torch.bfloat16, dev)
+        if workspace is None:
+            workspace = alloc_workspace(block_join_backward_workspace_bytes(M, K), dev)
+        _require(workspace.device == dev and workspace.is_contiguous(), f"workspace must be a contiguous tensor on {dev}")
+        dgate = out.get("dgate")
+        _check(lib().resq_block_join_backward(
+            _ptr(dH_out), _ptr(dX), H_out.data_ptr(), _OUT[H_out.dtype], B.data_ptr(), M, K, 0 if dH_out is None else _ld(dH_out),
+            0 if dX is None else _ld(dX), _ld(H_out), _ld(B), _ptr(gate), ldg, _GATES[act], _ptr(gamma_post), _ptr(gamma_pre), alpha,
+            eps, dH.data_ptr(), _ld(dH), out["dB"].data_ptr(), _ld(out["dB"]), _ptr(dgate), _ld(dgate) if ldg else 0,
+            _ptr(out.get("dgamma_post")), _ptr(out.get("dgamma_pre")), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), _stream(None)))
+    return out
+
+
+def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, temperature: float = 1.0, top: int = 0, stream=None):
+    """resq_token_logprobs -> dict(logp, entropy, peak, log_sum[, top_ids, top_logp]) of the rows of logits [M, V] (bf16 or fp32) for
+    tokens int64 [M] (outside 0 .. V - 1: none, logp 0).  top > 0: ids int32 [M, top] and log-probabilities of the largest
+    logits, largest first, equal ones by lower id."""
+    _require(logits.dim() == 2 and logits.is_cuda and logits.dtype in _OUT, "logits must be a 2-D CUDA tensor, bf16 or fp32")
+    dev, (M, V) = logits.device, logits.shape
+    _rows(logits, "logits", (M, V), logits.dtype, dev)
+    _vector(tokens, "tokens", M, torch.int64, dev)
+    with _entered(dev, stream):
+        out = {name: torch.empty(M, dtype=torch.float32, device=dev) for name in ("logp", "entropy", "peak", "log_sum")}
+        if top > 0:
+            out["top_ids"] = torch.empty((M, top), dtype=torch.int32, device=dev)
+            out["top_logp"] = torch.empty((M, top), dtype=torch.float32, device=dev)
+        _check(lib().resq_token_logprobs(logits.data_ptr(), _OUT[logits.dtype], M, V, _ld(logits), tokens.data_ptr(), temperature, top,
+                                         out["logp"].data_ptr(), out["entropy"].data_ptr(), out["peak"].data_ptr(), out["log_sum"].data_ptr(),
+                                         _ptr(out.get("top_ids")), _ptr(out.get("top_logp")), _stream(None)))
+    return out
+
+
+def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, logp: torch.Tensor, peak: torch.Tensor, log_sum: torch.Tensor,
+                            entropy: Optional[torch.Tensor], dlogp: torch.Tensor, dentropy: Optional[torch.Tensor] = None,
+                            temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """resq_token_logprobs_backward: the gradient of the logits from token_logprobs' results and the gradients of logp and
+    (optionally) entropy; dlogits may be the logits tensor itself."""
+    _require(logits.dim() == 2 and logits.is_cuda and logits.dtype in _OUT, "logits must be a 2-D CUDA tensor, bf16 or fp32")
+    dev, (M, V) = logits.device, logits.shape
+    _rows(logits, "logits", (M, V), logits.dtype, dev)
+    _vector(tokens, "tokens", M, torch.int64, dev)
+    for name, t in (("logp", logp), ("peak", peak), ("log_sum", log_sum), ("dlogp", dlogp), ("entropy", entropy), ("dentropy", dentropy)):
+        if t is not None:
+            _vector(t, name, M, torch.float32, dev)
+    _require(all(t is not None for t in (logp, peak, log_sum, dlogp)), "logp, peak, log_sum and dlogp are needed")
+    _require(dentropy is None or entropy is not None, "dentropy needs entropy")
+    with _entered(dev, stream):
+        if dlogits is None:
+            dlogits = _out(M, V, logits.dtype, dev)
+        _rows(dlogits, "dlogits", (M, V), logits.dtype, dev)
+        _check(lib().resq_token_logprobs_backward(
+            logits.data_ptr(), _OUT[logits.dtype], M, V, _ld(logits), tokens.data_ptr(), temperature, logp.data_ptr(), peak.data_ptr(),
+            log_sum.data_ptr(), _ptr(entropy), dlogp.data_ptr(), _ptr(dentropy), dlogits.data_ptr(), _ld(dlogits), _stream(None)))
+    return dlogits
 
 
 def check(workspace: torch.Tensor, stream=None) -> int:

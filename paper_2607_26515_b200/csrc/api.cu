@@ -120,7 +120,7 @@ bool pdl_enabled() {
 
 LaunchScope::LaunchScope(int kind, cudaStream_t stream) : kind_(kind), stream_(stream), rec_(nullptr) {
     g_launches.fetch_add(1, std::memory_order_relaxed);
-    if (!g_profile.load(std::memory_order_relaxed)) return;
+    if (kind >= kNumKinds || !g_profile.load(std::memory_order_relaxed)) return;
     ProfRec* r = new ProfRec{kind, nullptr, nullptr};
     if (cudaEventCreate(&r->start) != cudaSuccess || cudaEventCreate(&r->stop) != cudaSuccess) {
         delete r;

@@ -56,7 +56,8 @@ inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // Diagnostics (api.cu): every kernel launch of the library is counted; when profiling is enabled a
 // pair of CUDA events brackets each launch on its stream so that per-kernel device time can be read.
-enum KernelKind : int { kKindQuant = 0, kKindSelect = 1, kKindGemm = 2, kKindReduce = 3, kNumKinds = 4 };
+enum KernelKind : int { kKindQuant = 0, kKindSelect = 1, kKindGemm = 2, kKindReduce = 3, kNumKinds = 4,
+                        kKindRow = kNumKinds /* row operators: counted as launches, not timed by kind */ };
 struct LaunchScope {
     LaunchScope(int kind, cudaStream_t stream);
     ~LaunchScope();

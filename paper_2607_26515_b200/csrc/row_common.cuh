@@ -1,0 +1,118 @@
+// Shared pieces of the operators that walk rows of plain tensors (block_join.cu, token_logprobs.cu, gemv.cu): host-side
+// argument checks and 8-element vector access.  Internal.
+#pragma once
+#include "common.cuh"
+
+namespace resq {
+
+inline bool is_aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+inline int fail(int status, const char* what, const char* why) {
+    set_last_error("%s: %s", what, why);
+    return status;
+}
+// Rows of bf16 or fp32 values: 16-byte aligned base, rows that start on 16-byte boundaries, ld >= cols.
+inline bool rows_aligned(const void* p, int64_t ld, int64_t cols, int dtype) {
+    return is_aligned(p, 16) && ld >= cols && ld % (dtype == RESQ_OUT_BF16 ? 8 : 4) == 0;
+}
+
+#ifdef __CUDACC__
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Eight consecutive elements as they lie in memory.  `n` < 8 at the ragged end of a row: only those are touched (the
+// row's padding is neither read nor written).
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<__nv_bfloat16> {
+    uint4 q;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int n) {
+        if (n >= 8) {
+            q = *reinterpret_cast<const uint4*>(p);
+            return;
+        }
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        const unsigned short* s = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) w[i / 2] |= (uint32_t)s[i] << (16 * (i & 1));
+        q = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        v[0] = bf16_lo(q.x), v[1] = bf16_hi(q.x), v[2] = bf16_lo(q.y), v[3] = bf16_hi(q.y);
+        v[4] = bf16_lo(q.z), v[5] = bf16_hi(q.z), v[6] = bf16_lo(q.w), v[7] = bf16_hi(q.w);
+    }
+};
+template <>
+struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p, int n) {
+        if (n >= 8) {
+            a = reinterpret_cast<const float4*>(p)[0];
+            b = reinterpret_cast<const float4*>(p)[1];
+            return;
+        }
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+        a = make_float4(v[0], v[1], v[2], v[3]);
+        b = make_float4(v[4], v[5], v[6], v[7]);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    }
+};
+
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8], int n) {
+    if (n >= 8) {
+        *reinterpret_cast<uint4*>(p) =
+            make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = __float2bfloat16_rn(v[i]);
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8], int n) {
+    if (n >= 8) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = v[i];
+}
+
+// Sums of NV values over the block, the same bits in every thread; fixed order.  `buf` holds NV * 32 floats and must not
+// be the buffer of the previous call (two alternate, which saves a barrier).
+template <int NV>
+__device__ __forceinline__ void block_sum(float (&v)[NV], float* buf) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
+    const int nw = (blockDim.x + 31) >> 5;
+    if (nw == 1) return;
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) buf[i * 32 + w] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = lane < nw ? buf[i * 32 + lane] : 0.0f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
+}
+
+#endif  // __CUDACC__
+
+}  // namespace resq
