@@ -6,7 +6,6 @@ this module raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Optional, Tuple
@@ -518,7 +517,8 @@ def w16a4_linear(X: torch.Tensor, W: torch.Tensor, pattern: int = S_NONE, fmt: s
 # ------------------------------------------------------------------ few-token product, residual stream, log-probabilities
 #
 # These calls run on the device of their first tensor (made current for the call) and on `stream` (default: that device's
-# current stream).  What they allocate belongs to that stream.
+# current stream).  What they allocate belongs to that stream.  At one token the call is host time: entering a device and a
+# stream costs three times the launch, so that is done only where they are not the current ones already.
 
 GEMV_MAX_TOKENS = 16
 JOIN_MAX_K = 32768
@@ -526,18 +526,22 @@ MAX_TOP = 32
 GATE_LINEAR, GATE_SIGMOID = 0, 1
 _GATES = {"linear": GATE_LINEAR, "sigmoid": GATE_SIGMOID}
 _OUT = {torch.bfloat16: OUT_BF16, torch.float32: OUT_F32}
+_BF16, _F32 = torch.bfloat16, torch.float32
+# the current stream's handle without a Stream object around it (0.1 instead of 3 us)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
-@contextlib.contextmanager
-def _entered(device: torch.device, stream):
-    """The device current and, if a stream is named, that stream current too: the allocator then ties what the call
-    allocates to the stream its kernels run on."""
+def _run(index: int, stream, body):
+    """body(stream handle) with device `index` current and, if a stream is named, that stream current too: the allocator
+    then ties what the call allocates to the stream its kernels run on."""
+    if stream is None and torch.cuda.current_device() == index:
+        return body(_raw_stream(index))
     if stream is not None and not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device=device)
-    if stream is not None and stream.device != device:
-        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
-    with torch.cuda.device(device), torch.cuda.stream(stream):
-        yield
+        stream = torch.cuda.ExternalStream(int(stream), device=index)
+    if stream is not None and stream.device.index != index:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to cuda:{index}")
+    with torch.cuda.device(index), torch.cuda.stream(stream):
+        return body(_raw_stream(index))
 
 
 def _require(ok: bool, msg: str) -> None:
@@ -545,70 +549,70 @@ def _require(ok: bool, msg: str) -> None:
         raise ValueError(msg)
 
 
-def _rows(t: torch.Tensor, name: str, shape, dtype, device) -> torch.Tensor:
-    """t as a [rows, cols] device matrix of one type with unit inner stride."""
-    if t.dim() != 2 or t.dtype != dtype or t.device != device or tuple(t.shape) != shape or (t.stride(1) != 1 and shape[1] > 1):
-        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {device} with unit inner stride")
-    return t
+def _rows(t: torch.Tensor, name: str, M: int, K: int, dtype, index: int) -> int:
+    """Checks that t is an [M, K] matrix of one type on one device with unit inner stride; its row pitch in elements (a
+    single row has none of its own: any multiple of 8 that covers it will do)."""
+    if t.dtype is not dtype or t.shape != (M, K) or t.get_device() != index or (K > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a {dtype} tensor [{M}, {K}] on cuda:{index} with unit inner stride")
+    return t.stride(0) if M > 1 else (K + 7) // 8 * 8
 
 
-def _vector(t: torch.Tensor, name: str, n: int, dtype, device) -> torch.Tensor:
-    if t.dim() != 1 or t.numel() != n or t.dtype != dtype or t.device != device or (t.stride(0) != 1 and n > 1):
-        raise ValueError(f"{name} must be a contiguous {dtype} vector of {n} elements on {device}")
-    return t
+def _vector(t: torch.Tensor, name: str, n: int, dtype, index: int) -> int:
+    """Checks that t is a contiguous vector of n elements on one device; its address."""
+    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != index or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous {dtype} vector of {n} elements on cuda:{index}")
+    return t.data_ptr()
 
 
-def _ld(t: torch.Tensor) -> int:
-    """Row pitch in elements; a single row has none of its own (any multiple of 8 that covers it will do)."""
-    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+def _new_rows(M: int, K: int, dtype, index: int) -> torch.Tensor:
+    """A matrix whose rows start on 16-byte boundaries."""
+    return torch.empty_strided((M, K), ((K + 7) // 8 * 8, 1), dtype=dtype, device=index)
+
+
+def _first(t: torch.Tensor, name: str):
+    """(M, K, type code, device index) of a call's first tensor."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in _OUT:
+        raise ValueError(f"{name} must be a 2-D CUDA tensor, bf16 or fp32")
+    M, K = t.shape
+    return M, K, _OUT[t.dtype], t.get_device()
 
 
 def w4a16_gemv(X: torch.Tensor, w_codes: torch.Tensor, w_side: torch.Tensor, fmt: str = "hif4",
                out_dtype: torch.dtype = torch.bfloat16, Y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """*_w4a16_gemv: Y = X deq(Q(W))^T for at most GEMV_MAX_TOKENS token rows, streaming the packed weights once."""
     fn = _fn(fmt, "hif4_w4a16_gemv", "mxfp4_w4a16_gemv")
-    dev = X.device
-    _require_bf16_matrix(X, "X")
-    M, K = X.shape
+    M, K, _, index = _first(X, "X")
+    ldx = _rows(X, "X", M, K, _BF16, index)
+    _require(w_codes.dim() == 2, "w_codes must be [N, K/2]")
     N = w_codes.shape[0]
-    _packed(w_codes, w_side, N, K, fmt, dev)
-    with _entered(dev, stream):
-        if Y is None:
-            _require(out_dtype in _OUT, "Y must be bf16 or fp32")
-            Y = _out(M, N, out_dtype, dev)
-        _require(Y.dtype in _OUT, "Y must be bf16 or fp32")
-        _rows(Y, "Y", (M, N), Y.dtype, dev)
-        _check(fn(X.data_ptr(), M, K, _ld(X), w_codes.data_ptr(), w_side.data_ptr(), N, Y.data_ptr(), _OUT[Y.dtype], _ld(Y),
-                  _stream(None)))
-    return Y
+    if w_codes.dtype is not torch.uint8 or w_codes.shape[1] * 2 != K or not w_codes.is_contiguous() or w_codes.get_device() != index:
+        raise ValueError(f"w_codes must be contiguous uint8 [N, K/2] on cuda:{index} for the activations' K = {K}")
+    block, side_type = (64, torch.int32) if fmt == "hif4" else (32, torch.uint8)
+    if w_side.dtype is not side_type or w_side.shape != (N, K // block) or not w_side.is_contiguous() or w_side.get_device() != index:
+        raise ValueError(f"w_meta / w_scale must be contiguous {side_type} [N, K/{block}] on cuda:{index}")
+    out_dtype = out_dtype if Y is None else Y.dtype
+    _require(out_dtype in _OUT, "Y must be bf16 or fp32")
+    if Y is not None:
+        _rows(Y, "Y", M, N, out_dtype, index)
+
+    def body(st):
+        y = _new_rows(M, N, out_dtype, index) if Y is None else Y
+        _check(fn(X.data_ptr(), M, K, ldx, w_codes.data_ptr(), w_side.data_ptr(), N, y.data_ptr(), _OUT[out_dtype],
+                  y.stride(0) if M > 1 else (N + 7) // 8 * 8, st))
+        return y
+
+    return _run(index, stream, body)
 
 
-def _packed(codes: torch.Tensor, side: torch.Tensor, N: int, K: int, fmt: str, device) -> None:
-    block, dtype = (64, torch.int32) if fmt == "hif4" else (32, torch.uint8)
-    if codes.dtype != torch.uint8 or codes.shape != (N, K // 2) or not codes.is_contiguous() or codes.device != device or K % 2:
-        raise ValueError(f"w_codes must be contiguous uint8 [N, K/2] on {device} for the activations' K = {K}")
-    if side.dtype not in (dtype, torch.uint32 if dtype == torch.int32 else dtype) or side.shape != (N, K // block) \
-            or not side.is_contiguous() or side.device != device:
-        raise ValueError(f"w_meta / w_scale must be contiguous {dtype} [N, K/{block}] on {device}")
-
-
-def _join_args(H, B, gamma_pre, gamma_post, gate, act):
-    _require(H.dim() == 2 and H.is_cuda and H.dtype in _OUT, "H must be a 2-D CUDA tensor, bf16 or fp32")
-    _require(act in _GATES, f"unknown gate function {act!r}")
-    dev, (M, K) = H.device, H.shape
-    _rows(H, "H", (M, K), H.dtype, dev)
-    _rows(B, "B", (M, K), torch.bfloat16, dev)
-    for name, g in (("gamma_pre", gamma_pre), ("gamma_post", gamma_post)):
-        if g is not None:
-            _vector(g, name, K, torch.bfloat16, dev)
-    ldg = 0
-    if gate is not None and gate.dim() == 1:
-        _vector(gate, "gate", K, torch.bfloat16, dev)
-    elif gate is not None:
-        _rows(gate, "gate", (M, K), torch.bfloat16, dev)
-        ldg = _ld(gate)
-        _require(ldg != 0, "a gate shared by all tokens is given as a vector of K elements")
-    return dev, M, K, ldg
+def _join_gate(gate, M: int, K: int, index: int):
+    """(address, row pitch) of a gate; the pitch of a channel gate is 0."""
+    if gate is None:
+        return None, 0
+    if gate.dim() == 1:
+        return _vector(gate, "gate", K, _BF16, index), 0
+    ldg = _rows(gate, "gate", M, K, _BF16, index)
+    _require(ldg != 0, "a gate shared by all tokens is given as a vector of K elements")
+    return gate.data_ptr(), ldg
 
 
 def block_join(H: torch.Tensor, B: torch.Tensor, gamma_pre: Optional[torch.Tensor] = None, gamma_post: Optional[torch.Tensor] = None,
@@ -618,21 +622,24 @@ def block_join(H: torch.Tensor, B: torch.Tensor, gamma_pre: Optional[torch.Tenso
 
     gamma_post None: the branch B is added as it is; gamma_pre None: X is None.  gate: None, [K] (one for all tokens) or
     [M, K]; act "linear" or "sigmoid".  H_out may be H."""
-    dev, M, K, ldg = _join_args(H, B, gamma_pre, gamma_post, gate, act)
-    with _entered(dev, stream):
-        if H_out is None:
-            H_out = _out(M, K, H.dtype, dev)
-        if gamma_pre is None:
-            _require(X is None, "X needs gamma_pre")
-        elif X is None:
-            X = _out(M, K, torch.bfloat16, dev)
-        _rows(H_out, "H_out", (M, K), H.dtype, dev)
-        if X is not None:
-            _rows(X, "X", (M, K), torch.bfloat16, dev)
-        _check(lib().resq_block_join(H.data_ptr(), _OUT[H.dtype], B.data_ptr(), M, K, _ld(H), _ld(B), _ptr(gate), ldg, _GATES[act],
-                                     _ptr(gamma_post), _ptr(gamma_pre), alpha, eps, H_out.data_ptr(), _ld(H_out), _ptr(X),
-                                     0 if X is None else _ld(X), _stream(None)))
-    return H_out, X
+    M, K, dtype, index = _first(H, "H")
+    ldh, ldb = _rows(H, "H", M, K, H.dtype, index), _rows(B, "B", M, K, _BF16, index)
+    pre = None if gamma_pre is None else _vector(gamma_pre, "gamma_pre", K, _BF16, index)
+    post = None if gamma_post is None else _vector(gamma_post, "gamma_post", K, _BF16, index)
+    g, ldg = _join_gate(gate, M, K, index)
+    _require(act in _GATES, f"unknown gate function {act!r}")
+    _require(X is None or gamma_pre is not None, "X needs gamma_pre")
+
+    def body(st):
+        h = _new_rows(M, K, H.dtype, index) if H_out is None else H_out
+        x = _new_rows(M, K, _BF16, index) if X is None and gamma_pre is not None else X
+        ldho = _rows(h, "H_out", M, K, H.dtype, index)
+        ldx = 0 if x is None else _rows(x, "X", M, K, _BF16, index)
+        _check(lib().resq_block_join(H.data_ptr(), dtype, B.data_ptr(), M, K, ldh, ldb, g, ldg, _GATES[act], post, pre, alpha, eps,
+                                     h.data_ptr(), ldho, _ptr(x), ldx, st))
+        return h, x
+
+    return _run(index, stream, body)
 
 
 def block_join_backward_workspace_bytes(M: int, K: int) -> int:
@@ -646,54 +653,60 @@ def block_join_backward(dH_out: Optional[torch.Tensor], dX: Optional[torch.Tenso
     """resq_block_join_backward -> dict(dH, dB[, dgate][, dgamma_post][, dgamma_pre]) from the gradients of H' and X (either
     may be None) and the forward call's H' and inputs.  dgate has the gate's shape, fp32 for a channel gate [K], else bf16;
     the norms' gradients are fp32.  dH may be dH_out."""
-    dev, M, K, ldg = _join_args(H_out, B, gamma_pre, gamma_post, gate, act)
+    M, K, dtype, index = _first(H_out, "H_out")
+    ldh, ldb = _rows(H_out, "H_out", M, K, H_out.dtype, index), _rows(B, "B", M, K, _BF16, index)
     _require(dH_out is not None or dX is not None, "one of dH_out and dX is needed")
     _require(dX is None or gamma_pre is not None, "dX needs gamma_pre")
-    if dH_out is not None:
-        _rows(dH_out, "dH_out", (M, K), H_out.dtype, dev)
-    if dX is not None:
-        _rows(dX, "dX", (M, K), torch.bfloat16, dev)
-    with _entered(dev, stream):
-        if dH is None:
-            dH = _out(M, K, H_out.dtype, dev)
-        _rows(dH, "dH", (M, K), H_out.dtype, dev)
-        out = {"dH": dH, "dB": _out(M, K, torch.bfloat16, dev)}
-        if dX is not None:
-            out["dgamma_pre"] = torch.empty(K, dtype=torch.float32, device=dev)
-        if gamma_post is not None:
-            out["dgamma_post"] = torch.empty(K, dtype=torch.float32, device=dev)
-        if gate is not None:
-            out["dgate"] = torch.empty(K, dtype=torch.float32, device=dev) if ldg == 0 else _out(M, K, torch.bfloat16, dev)
-        if workspace is None:
-            workspace = alloc_workspace(block_join_backward_workspace_bytes(M, K), dev)
-        _require(workspace.device == dev and workspace.is_contiguous(), f"workspace must be a contiguous tensor on {dev}")
-        dgate = out.get("dgate")
+    lddho = 0 if dH_out is None else _rows(dH_out, "dH_out", M, K, H_out.dtype, index)
+    lddx = 0 if dX is None else _rows(dX, "dX", M, K, _BF16, index)
+    pre = None if gamma_pre is None else _vector(gamma_pre, "gamma_pre", K, _BF16, index)
+    post = None if gamma_post is None else _vector(gamma_post, "gamma_post", K, _BF16, index)
+    g, ldg = _join_gate(gate, M, K, index)
+    _require(act in _GATES, f"unknown gate function {act!r}")
+    if workspace is not None and (workspace.get_device() != index or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{index}")
+
+    def body(st):
+        out = {"dH": _new_rows(M, K, H_out.dtype, index) if dH is None else dH, "dB": _new_rows(M, K, _BF16, index)}
+        lddh = _rows(out["dH"], "dH", M, K, H_out.dtype, index)
+        ldn = (K + 7) // 8 * 8
+        columns = [n for n, on in (("dgamma_pre", dX is not None), ("dgamma_post", post is not None), ("dgate", g is not None and ldg == 0)) if on]
+        if columns:
+            out.update(zip(columns, torch.empty((len(columns), K), dtype=_F32, device=index).unbind()))
+        if ldg:
+            out["dgate"] = _new_rows(M, K, _BF16, index)
+        ws = alloc_workspace(block_join_backward_workspace_bytes(M, K), index) if workspace is None else workspace
         _check(lib().resq_block_join_backward(
-            _ptr(dH_out), _ptr(dX), H_out.data_ptr(), _OUT[H_out.dtype], B.data_ptr(), M, K, 0 if dH_out is None else _ld(dH_out),
-            0 if dX is None else _ld(dX), _ld(H_out), _ld(B), _ptr(gate), ldg, _GATES[act], _ptr(gamma_post), _ptr(gamma_pre), alpha,
-            eps, dH.data_ptr(), _ld(dH), out["dB"].data_ptr(), _ld(out["dB"]), _ptr(dgate), _ld(dgate) if ldg else 0,
-            _ptr(out.get("dgamma_post")), _ptr(out.get("dgamma_pre")), workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), _stream(None)))
-    return out
+            _ptr(dH_out), _ptr(dX), H_out.data_ptr(), dtype, B.data_ptr(), M, K, lddho, lddx, ldh, ldb, g, ldg, _GATES[act], post, pre,
+            alpha, eps, out["dH"].data_ptr(), lddh, out["dB"].data_ptr(), ldn, _ptr(out.get("dgate")), ldn if ldg else 0,
+            _ptr(out.get("dgamma_post")), _ptr(out.get("dgamma_pre")), ws.data_ptr(), ws.numel() * ws.element_size(), st))
+        return out
+
+    return _run(index, stream, body)
 
 
 def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, temperature: float = 1.0, top: int = 0, stream=None):
-    """resq_token_logprobs -> dict(logp, entropy, peak, log_sum[, top_ids, top_logp]) of the rows of logits [M, V] (bf16 or fp32) for
-    tokens int64 [M] (outside 0 .. V - 1: none, logp 0).  top > 0: ids int32 [M, top] and log-probabilities of the largest
-    logits, largest first, equal ones by lower id."""
-    _require(logits.dim() == 2 and logits.is_cuda and logits.dtype in _OUT, "logits must be a 2-D CUDA tensor, bf16 or fp32")
-    dev, (M, V) = logits.device, logits.shape
-    _rows(logits, "logits", (M, V), logits.dtype, dev)
-    _vector(tokens, "tokens", M, torch.int64, dev)
-    with _entered(dev, stream):
-        out = {name: torch.empty(M, dtype=torch.float32, device=dev) for name in ("logp", "entropy", "peak", "log_sum")}
+    """resq_token_logprobs -> dict(logp, entropy, peak, log_sum[, top_ids, top_logp]) of the rows of logits [M, V] (bf16 or
+    fp32) for tokens int64 [M] (outside 0 .. V - 1: none, logp 0).  top > 0: ids int32 [M, top] and log-probabilities of the
+    largest logits, largest first, equal ones by lower id."""
+    M, V, dtype, index = _first(logits, "logits")
+    ld = _rows(logits, "logits", M, V, logits.dtype, index)
+    tok = _vector(tokens, "tokens", M, torch.int64, index)
+
+    def body(st):
+        values = torch.empty((4, M), dtype=_F32, device=index)
+        logp, entropy, peak, log_sum = values.unbind()
+        out = {"logp": logp, "entropy": entropy, "peak": peak, "log_sum": log_sum}
+        ids = top_logp = None
         if top > 0:
-            out["top_ids"] = torch.empty((M, top), dtype=torch.int32, device=dev)
-            out["top_logp"] = torch.empty((M, top), dtype=torch.float32, device=dev)
-        _check(lib().resq_token_logprobs(logits.data_ptr(), _OUT[logits.dtype], M, V, _ld(logits), tokens.data_ptr(), temperature, top,
-                                         out["logp"].data_ptr(), out["entropy"].data_ptr(), out["peak"].data_ptr(), out["log_sum"].data_ptr(),
-                                         _ptr(out.get("top_ids")), _ptr(out.get("top_logp")), _stream(None)))
-    return out
+            ids = out["top_ids"] = torch.empty((M, top), dtype=torch.int32, device=index)
+            top_logp = out["top_logp"] = torch.empty((M, top), dtype=_F32, device=index)
+        at = values.data_ptr()
+        _check(lib().resq_token_logprobs(logits.data_ptr(), dtype, M, V, ld, tok, temperature, top, at, at + 4 * M, at + 8 * M, at + 12 * M,
+                                         _ptr(ids), _ptr(top_logp), st))
+        return out
+
+    return _run(index, stream, body)
 
 
 def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, logp: torch.Tensor, peak: torch.Tensor, log_sum: torch.Tensor,
@@ -701,23 +714,21 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, logp: to
                             temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """resq_token_logprobs_backward: the gradient of the logits from token_logprobs' results and the gradients of logp and
     (optionally) entropy; dlogits may be the logits tensor itself."""
-    _require(logits.dim() == 2 and logits.is_cuda and logits.dtype in _OUT, "logits must be a 2-D CUDA tensor, bf16 or fp32")
-    dev, (M, V) = logits.device, logits.shape
-    _rows(logits, "logits", (M, V), logits.dtype, dev)
-    _vector(tokens, "tokens", M, torch.int64, dev)
-    for name, t in (("logp", logp), ("peak", peak), ("log_sum", log_sum), ("dlogp", dlogp), ("entropy", entropy), ("dentropy", dentropy)):
-        if t is not None:
-            _vector(t, name, M, torch.float32, dev)
-    _require(all(t is not None for t in (logp, peak, log_sum, dlogp)), "logp, peak, log_sum and dlogp are needed")
+    M, V, dtype, index = _first(logits, "logits")
+    ld = _rows(logits, "logits", M, V, logits.dtype, index)
+    _require(logp is not None and peak is not None and log_sum is not None and dlogp is not None, "logp, peak, log_sum and dlogp are needed")
     _require(dentropy is None or entropy is not None, "dentropy needs entropy")
-    with _entered(dev, stream):
-        if dlogits is None:
-            dlogits = _out(M, V, logits.dtype, dev)
-        _rows(dlogits, "dlogits", (M, V), logits.dtype, dev)
-        _check(lib().resq_token_logprobs_backward(
-            logits.data_ptr(), _OUT[logits.dtype], M, V, _ld(logits), tokens.data_ptr(), temperature, logp.data_ptr(), peak.data_ptr(),
-            log_sum.data_ptr(), _ptr(entropy), dlogp.data_ptr(), _ptr(dentropy), dlogits.data_ptr(), _ld(dlogits), _stream(None)))
-    return dlogits
+    values = [_vector(tokens, "tokens", M, torch.int64, index)]
+    values += [None if t is None else _vector(t, name, M, _F32, index)
+               for name, t in (("logp", logp), ("peak", peak), ("log_sum", log_sum), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy))]
+
+    def body(st):
+        d = _new_rows(M, V, logits.dtype, index) if dlogits is None else dlogits
+        ldd = _rows(d, "dlogits", M, V, logits.dtype, index)
+        _check(lib().resq_token_logprobs_backward(logits.data_ptr(), dtype, M, V, ld, values[0], temperature, *values[1:], d.data_ptr(), ldd, st))
+        return d
+
+    return _run(index, stream, body)
 
 
 def check(workspace: torch.Tensor, stream=None) -> int:
