@@ -349,13 +349,14 @@ RESQ_API int mxfp4_w16a4_linear(const void* X_bf16, int64_t M, int64_t K, int64_
 
 /* ---- the weight-only product for a few tokens (Table 1's "W4A16" in its single-token form; the grouping into a call of
  * its own is this library's) ---------------------------------------------------------------------------------------
- * Y = X deq(Q(W))^T as *_w4a16_linear, for 1 <= M <= RESQ_GEMV_MAX_TOKENS token rows, as a matrix-vector kernel that
+ * Y = X deq(Q(W))^T as *_w4a16_linear, for 1 <= M <= RESQ_GEMV_MAX_TOKENS token rows (K <= RESQ_GEMV_MAX_K), as a kernel that
  * streams the packed weights once (a GEMM tile computes 128 token rows whatever M is).  Same argument rules and output
  * types; no workspace.  Products of decoded weights and bf16 activations are exact, sums are held in fp32 and added in a
  * fixed order (bit-identical results run to run; the order depends on M, N and K).  An infinity or NaN in a row of X
  * makes that row of Y follow IEEE arithmetic (0 x inf = NaN) and leaves the others alone; an MXFP4 weight of 2^128 or more
  * (scale codes 253 and above) is infinite, as in mxfp4_dequantize. */
 #define RESQ_GEMV_MAX_TOKENS 16
+#define RESQ_GEMV_MAX_K 49152
 RESQ_API int hif4_w4a16_gemv(const void* X_bf16, int64_t M, int64_t K, int64_t ldx,
                     const void* w_codes, const void* w_meta, int64_t N,
                     void* Y, int out_dtype, int64_t ldy, void* stream);

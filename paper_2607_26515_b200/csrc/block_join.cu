@@ -151,8 +151,8 @@ __device__ __forceinline__ void row_sum(float (&v)[NV], float* buf, float* xbuf)
             asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote), "f"(v[i]) : "memory");
         }
     }
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         float t = 0.0f;
@@ -245,8 +245,8 @@ __global__ void __launch_bounds__(kMaxThreadsBwd) join_bwd_kernel(const __grid_c
         if (a.gate && a.ldg == 0) store8(out, acc_gate, n);
     }
     if (CS > 1) {  // no CTA leaves while a peer may still write its shared memory
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
 }
 
@@ -291,24 +291,6 @@ int bwd_threads(int64_t K, int cs) { return (int)(((K + 7) / 8 + cs * 32 - 1) / 
 int64_t bwd_groups(int64_t M, int64_t K) {
     const int cs = bwd_cluster(K), per_sm = std::min(16, std::max(1, 1024 / bwd_threads(K, cs)));
     return std::min<int64_t>(M, std::max(1, kSms * per_sm / cs));
-}
-
-template <typename... KArgs, typename... Args>
-cudaError_t launch_clusters(void (*kern)(KArgs...), unsigned grid, unsigned block, int cs, cudaStream_t stream, Args... args) {
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(block);
-    cfg.stream = stream;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)cs;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = pdl_enabled() ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, KArgs(args)...);
 }
 
 int check_join(const char* what, int64_t M, int64_t K, int dtype, const void* B, int64_t ldb, const void* gate, int64_t ldg, int gate_act,
@@ -430,7 +412,7 @@ int resq_block_join_backward(const void* dH_out, const void* dX, const void* H_o
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     {
         LaunchScope scope(kKindRow, st);
-        rc = cuda_fail(launch_clusters(kern, (unsigned)(groups * cs), (unsigned)bwd_threads(K, cs), cs, st, a), "join_bwd_kernel launch");
+        rc = cuda_fail(launch_clusters(kern, (unsigned)(groups * cs), (unsigned)bwd_threads(K, cs), 0, cs, st, a), "join_bwd_kernel launch");
     }
     if (rc || s.ncol == 0) return rc;
     s.part = a.part, s.kp = a.kp, s.P = (int)groups, s.K = (int)K;

@@ -1,76 +1,342 @@
 // *_w4a16_gemv: Y[m, n] = sum_k X[m, k] deq(W)[n, k] for at most RESQ_GEMV_MAX_TOKENS token rows.
 //
-// One warp per weight row: a lane takes eight codes (one 32-bit word) at a time, decodes them to fp32 and multiplies them
-// with the eight activations of every token; the 32 partial sums are added at the end.
+// What it has to do is stream the packed weights (4.5 or 4.25 bits each) once; the arithmetic next to that is the expansion
+// of the codes.  At 6.5 TB/s an SM receives about 41 weights per clock, so an expansion may cost three instructions a weight
+// and the multiplications must cost next to none: they go to the register-operand tensor instruction (m16n8k16, bf16 in, fp32
+// out), whose A fragment is 16 weight rows in exactly the layout a lane can expand in registers, and whose 8 columns are
+// tokens.  (The tensor-memory instruction would need the expanded weights written to shared memory and read back, which is
+// what bounds the decode GEMM.)  The order of k inside a fragment is free as long as both operands use the same one, so
+// a lane owns 32 consecutive k of rows g and g + 8 (one 16-byte load each), and pairs elements i and i + 4 of a 32-bit word:
+// their nibbles lie 16 bits apart, so one mask takes both.
+//
+// Work: a unit is 16 weight rows x 128 k (1 KB of codes).  A CTA (8 warps) owns T row tiles and one of CS slices of K; its
+// T x units are dealt out evenly and contiguously to its warps, which keep kDepth units in flight.  The partial sums of a
+// (tile, warp) go to shared memory and are added in a fixed order, over the CTAs of the cluster where K is sliced.
 #include "common.cuh"
-#include "quant_device.cuh"
 #include "row_common.cuh"
+
+#include <algorithm>
 
 namespace resq {
 namespace {
 
-constexpr int kGemvThreads = 256;
+constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kUnitK = 128, kTileN = 16;
+template <int NT>
+constexpr int kDepthOf = NT == 1 ? 4 : 3;  // units in flight per warp: 16 warps x 4 KB = 64 KB per SM (3 where a second token group takes the registers)
+constexpr int kMaxTiles = 64;   // row tiles per CTA
+constexpr int kXPad = 64;       // bytes behind a token's staged row: neighbouring tokens use the other half of the banks
 
-template <int FMT, int MT>
-__global__ void __launch_bounds__(kGemvThreads) gemv_kernel(const __nv_bfloat16* __restrict__ X, int M, int64_t K, int64_t ldx,
-                                                            const uint8_t* __restrict__ codes, const void* __restrict__ side,
-                                                            int64_t N, void* __restrict__ Y, int out_dtype, int64_t ldy) {
-    pdl_wait();
-    pdl_trigger();
-    const int64_t n = (int64_t)blockIdx.x * (kGemvThreads / 32) + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (n >= N) return;
-    float acc[MT];
+struct GemvArgs {
+    const __nv_bfloat16* X;
+    const uint8_t* codes;
+    const uint8_t* side;
+    void* Y;
+    int64_t ldx, ldy;
+    int M, K, N, out_dtype;
+    int tiles;        // row tiles in all
+    int tiles_cta;    // row tiles per CTA (and cluster)
+    int units_slice;  // units of 128 k per slice
+};
+
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint4 ld_stream_u4(const uint8_t* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+// What a lane needs to expand its 32 codes of one row: HiF4 half a block (four level-2 groups), MXFP4 one whole block.
+template <int FMT>
+struct Scale;
+template <>
+struct Scale<kHiF4> {
+    uint32_t base, e2, e3;
+    // odd: the lane's half of the 64-block
+    __device__ __forceinline__ void set(uint32_t meta, int odd) {
+        base = (meta & 255u) * 0x00200020u + 0x26802680u;  // bf16 bits of S1 / 4 in both halves (s << 5 is (E << 7) | (Mn << 5))
+        e2 = (meta >> (8 + 4 * odd)) & 15u;
+        e3 = (meta >> (16 + 8 * odd)) & 255u;
+    }
+    // (128 + q) c - 128 c is q c exactly (q c has 6 significant bits); the nibble at bits 6:4 reads as 16 q, so c / 16 there
+    __device__ __forceinline__ void expand(uint32_t w, int group, uint32_t (&v)[4]) const {
+        // exponents of the two level-3 groups: bit 2i of e3 to bit 7, bit 2i + 1 to bit 23; bit i of e2 to both
+        const uint32_t m3 = (128u >> (2 * group)) | (0x00400000u >> (2 * group)), m2 = 0x00800080u >> group;
+        const uint32_t c = base + ((e3 * m3) & 0x00800080u) + ((e2 * m2) & 0x00800080u);
+        const uint32_t n = c + 0x83808380u, c16 = c - 0x02000200u, n16 = c + 0x81808180u;  // -128 c, c / 16, -8 c
+        const uint32_t h = w >> 8;
+        v[0] = fma_bf16x2((w & 0x00070007u) | 0x43004300u, c, n) ^ ((w << 12) & 0x80008000u);
+        v[1] = fma_bf16x2((w & 0x00700070u) | 0x43004300u, c16, n16) ^ ((w << 8) & 0x80008000u);
+        v[2] = fma_bf16x2((h & 0x00070007u) | 0x43004300u, c, n) ^ ((w << 4) & 0x80008000u);
+        v[3] = fma_bf16x2((h & 0x00700070u) | 0x43004300u, c16, n16) ^ (w & 0x80008000u);
+    }
+};
+template <>
+struct Scale<kMXFP4> {
+    uint32_t c, c2;
+    // The three magnitude bits of E2M1 at bits 8:6 are the bf16 number value * 2^-126 (0 and 0.5 as subnormals), so one
+    // multiplication by 2^126 2^(sc - 127) gives the weight; where that factor passes 2^127 a second one takes the rest.
+    __device__ __forceinline__ void set(uint32_t sc, int) {
+        c = min(sc + 126u, 254u) * 0x00800080u;
+        c2 = sc > 128u ? (sc == 255u ? 0x7F807F80u : (sc - 1u) * 0x00800080u) : 0x3F803F80u;  // 2^(sc - 128)
+    }
+    __device__ __forceinline__ void expand(uint32_t w, int, uint32_t (&v)[4]) const {
+        v[0] = mul_bf16x2(((w << 6) & 0x01C001C0u) | ((w << 12) & 0x80008000u), c);
+        v[1] = mul_bf16x2(((w << 2) & 0x01C001C0u) | ((w << 8) & 0x80008000u), c);
+        v[2] = mul_bf16x2(((w >> 2) & 0x01C001C0u) | ((w << 4) & 0x80008000u), c);
+        v[3] = mul_bf16x2(((w >> 6) & 0x01C001C0u) | (w & 0x80008000u), c);
+        if (c2 != 0x3F803F80u) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m) acc[m] = 0.0f;
-    for (int64_t k = lane * 8; k < K; k += 256) {
-        const uint32_t c = *reinterpret_cast<const uint32_t*>(codes + n * (K / 2) + k / 2);
-        float w[8];
-        if (FMT == kHiF4)
-            hif4_decode_lane(c, reinterpret_cast<const uint32_t*>(side)[n * (K / kHif4Block) + k / kHif4Block], (int)((k / 8) & 7), w);
-        else
-            mxfp4_decode_lane(c, reinterpret_cast<const uint8_t*>(side)[n * (K / kMxBlock) + k / kMxBlock], w);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if (m >= M) break;
-            Raw8<__nv_bfloat16> r;
-            r.load(X + m * ldx + k, 8);
-            float x[8];
-            r.get(x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[m] = fmaf(x[i], w[i], acc[m]);
+            for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], c2);
         }
     }
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        if (m >= M) break;
-        float v = acc[m];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-        if (lane == 0) {
-            if (out_dtype == RESQ_OUT_BF16) reinterpret_cast<__nv_bfloat16*>(Y)[m * ldy + n] = __float2bfloat16_rn(v);
-            else reinterpret_cast<float*>(Y)[m * ldy + n] = v;
+};
+
+__device__ __forceinline__ uint32_t ld_nc32(const uint8_t* p) {
+    uint32_t v;
+    asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_nc8(const uint8_t* p) {
+    uint32_t v;
+    asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+
+// NT: groups of 8 tokens; CS: CTAs of a cluster, each with its slice of K.
+template <int FMT, int NT, int CS>
+__global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant__ GemvArgs a) {
+    constexpr int kDepth = kDepthOf<NT>;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int rank = CS > 1 ? (int)(blockIdx.x % CS) : 0;
+    const int tile0 = (int)(blockIdx.x / CS) * a.tiles_cta;
+    const int tiles = min(a.tiles_cta, a.tiles - tile0);
+    const int units_all = (a.K + kUnitK - 1) / kUnitK;
+    const int units = max(0, min(a.units_slice, units_all - rank * a.units_slice));
+    const int k0 = rank * a.units_slice * kUnitK;
+    const int xrow = a.units_slice * 256 + kXPad;
+    float* part = reinterpret_cast<float*>(smem + (size_t)a.M * xrow);  // [tile + warp][16 rows][8 NT tokens]
+
+    pdl_wait();
+
+    // ---- the warp's run of (tile, unit) pairs: first loads before the activations are staged
+    const int total = tiles * units;
+    const int first = (int)((int64_t)total * warp / kWarps), last = (int)((int64_t)total * (warp + 1) / kWarps);
+    const int64_t row_codes = a.K / 2, row_side = FMT == kHiF4 ? (int64_t)a.K / 64 * 4 : (int64_t)a.K / 32;
+    constexpr int kSideStep = FMT == kHiF4 ? 8 : 4;  // side bytes per unit
+    uint4 qa[kDepth], qb[kDepth];
+    uint32_t sa[kDepth], sb[kDepth];
+    int lu = units > 0 ? first % units : 0, lt = units > 0 ? first / units : 0;  // load cursor
+    const uint8_t *pa, *pb, *ma, *mb;
+    auto point = [&]() {
+        const int64_t n0 = min((int64_t)(tile0 + lt) * kTileN + g, (int64_t)a.N - 1);
+        const int64_t n1 = min((int64_t)(tile0 + lt) * kTileN + g + 8, (int64_t)a.N - 1);
+        const int64_t kc = (int64_t)k0 / 2 + lu * 64 + t * 16;
+        const int64_t ks = FMT == kHiF4 ? (int64_t)k0 / 16 + lu * 8 + (t >> 1) * 4 : (int64_t)k0 / 32 + lu * 4 + t;
+        pa = a.codes + n0 * row_codes + kc, pb = a.codes + n1 * row_codes + kc;
+        ma = a.side + n0 * row_side + ks, mb = a.side + n1 * row_side + ks;
+    };
+    auto load = [&](int d) {
+        if (k0 + lu * kUnitK + t * 32 < a.K) {  // the last unit of a row may be cut to one, two or three lanes of a quad
+            qa[d] = ld_stream_u4(pa), qb[d] = ld_stream_u4(pb);
+            sa[d] = FMT == kHiF4 ? ld_nc32(ma) : ld_nc8(ma);
+            sb[d] = FMT == kHiF4 ? ld_nc32(mb) : ld_nc8(mb);
+        } else {
+            qa[d] = qb[d] = make_uint4(0u, 0u, 0u, 0u);
+            sa[d] = sb[d] = 0u;
         }
+        if (++lu == units) {
+            lu = 0, ++lt;
+            point();
+        } else {
+            pa += 64, pb += 64, ma += kSideStep, mb += kSideStep;
+        }
+    };
+    if (first < last) point();
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d)
+        if (first + d < last) load(d);
+
+    // ---- activations of this slice: chunks of 8, pairs (i, i + 4) side by side, chunk (lane t, word w) of a unit at
+    // (4 w + t) * 16 bytes, so that the four lanes of a quad read 64 consecutive bytes
+    const int chunks = a.units_slice * 16;
+    for (int i = threadIdx.x; i < a.M * chunks; i += kThreads) {
+        const int m = i / chunks, j = i - m * chunks, k = k0 + j * 8;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (k < a.K) v = *reinterpret_cast<const uint4*>(a.X + m * a.ldx + k);
+        const uint4 p = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410),
+                                   __byte_perm(v.y, v.w, 0x7632));
+        *reinterpret_cast<uint4*>(smem + m * xrow + (j >> 4) * 256 + ((j & 3) * 4 + ((j >> 2) & 3)) * 16) = p;
+    }
+    __syncthreads();
+    pdl_trigger();
+
+    float acc[NT][4];
+#pragma unroll
+    for (int q = 0; q < NT; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[q][i] = 0.0f;
+    const uint8_t* xs[NT];  // the lane's token of each group (columns behind the last token repeat it; they are not stored)
+#pragma unroll
+    for (int q = 0; q < NT; ++q) xs[q] = smem + min(q * 8 + g, a.M - 1) * xrow + t * 16;
+    int cu = units > 0 ? first % units : 0, ct = units > 0 ? first / units : 0;
+    for (int i = first; i < last; i += kDepth) {
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d) {
+            if (i + d >= last) break;
+            const uint4 wa = qa[d], wb = qb[d];
+            Scale<FMT> fa, fb;
+            fa.set(sa[d], t & 1), fb.set(sb[d], t & 1);
+            if (i + d + kDepth < last) load(d);
+            // a chain of 8 instructions from zero, then one rounded addition per sum: the tensor cores cut their sums
+            float c[NT][4];
+#pragma unroll
+            for (int q = 0; q < NT; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) c[q][j] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t va[4], vb[4];
+                fa.expand(w == 0 ? wa.x : w == 1 ? wa.y : w == 2 ? wa.z : wa.w, w, va);
+                fb.expand(w == 0 ? wb.x : w == 1 ? wb.y : w == 2 ? wb.z : wb.w, w, vb);
+#pragma unroll
+                for (int q = 0; q < NT; ++q) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(xs[q] + cu * 256 + w * 64);
+                    mma16816(c[q], va[0], vb[0], va[1], vb[1], x.x, x.y);
+                    mma16816(c[q], va[2], vb[2], va[3], vb[3], x.z, x.w);
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < NT; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[q][j] += c[q][j];
+            if (++cu == units || i + d + 1 == last) {
+                float* out = part + (size_t)(ct + warp) * (kTileN * 8 * NT);
+#pragma unroll
+                for (int q = 0; q < NT; ++q) {
+                    *reinterpret_cast<float2*>(out + g * (8 * NT) + q * 8 + t * 2) = make_float2(acc[q][0], acc[q][1]);
+                    *reinterpret_cast<float2*>(out + (g + 8) * (8 * NT) + q * 8 + t * 2) = make_float2(acc[q][2], acc[q][3]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[q][j] = 0.0f;
+                }
+                if (cu == units) cu = 0, ++ct;
+            }
+        }
+    }
+
+    // ---- sums over warps (and slices) in order.  A tile's part of warp w lies at slot tile + w: both only grow along the run.
+    if (CS > 1) {
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    } else {
+        __syncthreads();
+    }
+    const int rows = tiles * kTileN, outs = rows * a.M;
+    const int per = (outs + CS - 1) / CS;
+    for (int o = rank * per + threadIdx.x; o < min(outs, (rank + 1) * per); o += kThreads) {
+        const int m = o / rows, r = o - m * rows, tile = r / kTileN;
+        const int64_t n = (int64_t)tile0 * kTileN + r;
+        if (n >= a.N) continue;
+        float s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CS; ++c) {
+            const int cunits = CS > 1 ? max(0, min(a.units_slice, units_all - c * a.units_slice)) : units;
+            const int ctotal = tiles * cunits, u0 = tile * cunits, u1 = u0 + cunits;
+            for (int w = 0; w < kWarps; ++w) {
+                const int f = (int)((int64_t)ctotal * w / kWarps), l = (int)((int64_t)ctotal * (w + 1) / kWarps);
+                if (f >= u1 || l <= u0 || f >= l) continue;
+                const float* src = part + (size_t)(tile + w) * (kTileN * 8 * NT) + (r % kTileN) * (8 * NT) + m;
+                if (CS == 1) {
+                    s += *src;
+                } else {
+                    uint32_t remote;
+                    float v;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"((uint32_t)__cvta_generic_to_shared(src)), "r"(c));
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+                    s += v;
+                }
+            }
+        }
+        if (a.out_dtype == RESQ_OUT_BF16) static_cast<__nv_bfloat16*>(a.Y)[m * a.ldy + n] = __float2bfloat16_rn(s);
+        else static_cast<float*>(a.Y)[m * a.ldy + n] = s;
+    }
+    if (CS > 1) {  // no CTA leaves while a peer may still read its shared memory
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
 }
 
-template <int FMT>
-int launch_gemv(const __nv_bfloat16* X, int M, int64_t K, int64_t ldx, const uint8_t* codes, const void* side, int64_t N, void* Y,
-                int out_dtype, int64_t ldy, cudaStream_t stream) {
-    const int64_t grid = (N + kGemvThreads / 32 - 1) / (kGemvThreads / 32);
+// ---- host side -----------------------------------------------------------------------------------
+struct GemvPlan {
+    int cs, tiles_cta, units_slice;
+    size_t smem;
+};
+
+constexpr size_t kSmemMax = 227 * 1024, kSmemTwo = 113 * 1024;  // per CTA: alone on its SM, two on an SM
+
+// Splits the K range over cs CTAs and gives each cluster T row tiles so that the busiest CTA slot finishes first.  Cycles
+// per unit and the fixed costs are rough measurements; only their proportions matter.
+GemvPlan plan_gemv(int M, int64_t N, int64_t K) {
+    const int tiles = (int)((N + kTileN - 1) / kTileN), units = (int)((K + kUnitK - 1) / kUnitK), nt = M > 8 ? 2 : 1;
+    GemvPlan best{0, 0, 0, 0};
+    double best_cost = 0;
+    for (int cs = 1; cs <= 8; cs *= 2) {
+        const int us = (units + cs - 1) / cs;
+        const size_t x = (size_t)M * (us * 256 + kXPad);
+        for (int T = 1; T <= std::min(kMaxTiles, tiles); ++T) {
+            const size_t smem = x + (size_t)(T + kWarps) * kTileN * 8 * nt * sizeof(float);
+            if (smem > kSmemMax) break;
+            const int per_sm = smem <= kSmemTwo ? 2 : 1;
+            const int64_t clusters = (tiles + T - 1) / T, slots = 148 * per_sm / cs;
+            const double waves = (double)((clusters + slots - 1) / slots);
+            const double cost = waves * ((double)((T * us + kWarps - 1) / kWarps) * 450 * per_sm + 2000 + (double)x / 32 + (cs > 1 ? 800 : 0));
+            if (best.cs == 0 || cost < best_cost) best = GemvPlan{cs, T, us, smem}, best_cost = cost;
+        }
+    }
+    return best;
+}
+
+template <int FMT, int NT, int CS>
+int launch_gemv(const GemvArgs& a, const GemvPlan& p, cudaStream_t stream) {
+    auto kern = gemv_kernel<FMT, NT, CS>;
+    int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), (int)kSmemMax, "gemv_kernel shared memory");
+    if (rc) return rc;
+    const unsigned clusters = (unsigned)((a.tiles + p.tiles_cta - 1) / p.tiles_cta);
     LaunchScope scope(kKindGemm, stream);
-    auto kern = M <= 1 ? gemv_kernel<FMT, 1> : M <= 4 ? gemv_kernel<FMT, 4> : gemv_kernel<FMT, RESQ_GEMV_MAX_TOKENS>;
-    return cuda_fail(launch_kernel(kern, dim3((unsigned)grid), dim3(kGemvThreads), 0, stream, X, M, K, ldx, codes, side, N, Y, out_dtype, ldy),
-                     "gemv_kernel launch");
+    return cuda_fail(launch_clusters(kern, clusters * CS, kThreads, p.smem, CS, stream, a), "gemv_kernel launch");
+}
+template <int FMT, int NT>
+int launch_gemv(const GemvArgs& a, const GemvPlan& p, cudaStream_t stream) {
+    switch (p.cs) {
+        case 1: return launch_gemv<FMT, NT, 1>(a, p, stream);
+        case 2: return launch_gemv<FMT, NT, 2>(a, p, stream);
+        case 4: return launch_gemv<FMT, NT, 4>(a, p, stream);
+        default: return launch_gemv<FMT, NT, 8>(a, p, stream);
+    }
 }
 
 int gemv(int fmt, const void* X, int64_t M, int64_t K, int64_t ldx, const void* w_codes, const void* w_side, int64_t N, void* Y,
          int out_dtype, int64_t ldy, void* stream) {
     const int block = fmt == kHiF4 ? kHif4Block : kMxBlock;
     if (!X || !w_codes || !w_side || !Y) return fail(RESQ_ERR_NULL, "gemv", "X, the packed weight and Y must not be NULL");
-    if (M <= 0 || N <= 0 || K <= 0 || K % block != 0 || M > RESQ_GEMV_MAX_TOKENS || N > INT32_MAX || K > INT32_MAX) {
-        set_last_error("gemv: M=%lld N=%lld K=%lld (1 <= M <= %d, K a positive multiple of %d, N and K below 2^31)", (long long)M,
-                       (long long)N, (long long)K, RESQ_GEMV_MAX_TOKENS, block);
+    if (M <= 0 || N <= 0 || K <= 0 || K % block != 0 || M > RESQ_GEMV_MAX_TOKENS || N > INT32_MAX - 65536 || K > RESQ_GEMV_MAX_K) {
+        set_last_error("gemv: M=%lld N=%lld K=%lld (1 <= M <= %d, K a positive multiple of %d up to %d, N below 2^31 - 65536)", (long long)M,
+                       (long long)N, (long long)K, RESQ_GEMV_MAX_TOKENS, block, RESQ_GEMV_MAX_K);
         return RESQ_ERR_SHAPE;
     }
     if (out_dtype != RESQ_OUT_BF16 && out_dtype != RESQ_OUT_F32) {
@@ -81,11 +347,17 @@ int gemv(int fmt, const void* X, int64_t M, int64_t K, int64_t ldx, const void* 
         return fail(RESQ_ERR_ALIGN, "gemv", "X needs a 16-byte aligned base and ldx >= K, ldx % 8 == 0");
     if (!is_aligned(w_codes, 16) || !is_aligned(w_side, 16) || !rows_aligned(Y, ldy, N, out_dtype))
         return fail(RESQ_ERR_ALIGN, "gemv", "Y / weights need 16-byte aligned bases, ldy >= N and 16-byte aligned rows");
-    const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(X);
-    const uint8_t* c = static_cast<const uint8_t*>(w_codes);
+    const GemvPlan p = plan_gemv((int)M, N, K);
+    GemvArgs a;
+    a.X = static_cast<const __nv_bfloat16*>(X);
+    a.codes = static_cast<const uint8_t*>(w_codes);
+    a.side = static_cast<const uint8_t*>(w_side);
+    a.Y = Y;
+    a.ldx = ldx, a.ldy = ldy, a.M = (int)M, a.K = (int)K, a.N = (int)N, a.out_dtype = out_dtype;
+    a.tiles = (int)((N + kTileN - 1) / kTileN), a.tiles_cta = p.tiles_cta, a.units_slice = p.units_slice;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return fmt == kHiF4 ? launch_gemv<kHiF4>(x, (int)M, K, ldx, c, w_side, N, Y, out_dtype, ldy, st)
-                        : launch_gemv<kMXFP4>(x, (int)M, K, ldx, c, w_side, N, Y, out_dtype, ldy, st);
+    if (fmt == kHiF4) return M > 8 ? launch_gemv<kHiF4, 2>(a, p, st) : launch_gemv<kHiF4, 1>(a, p, st);
+    return M > 8 ? launch_gemv<kMXFP4, 2>(a, p, st) : launch_gemv<kMXFP4, 1>(a, p, st);
 }
 
 }  // namespace

@@ -29,7 +29,7 @@ GEMV = dict(X=P, M=4, K=256, ldx=256, codes=P, side=P, N=100, Y=P, out=0, ldy=10
 GEMV_BAD = [
     (NULL, dict(X=None)), (NULL, dict(codes=None)), (NULL, dict(side=None)), (NULL, dict(Y=None)),
     (SHAPE, dict(M=0)), (SHAPE, dict(M=17)), (SHAPE, dict(M=-1)), (SHAPE, dict(N=0)), (SHAPE, dict(K=0)), (SHAPE, dict(K=16)),
-    (SHAPE, dict(N=2 ** 31)), (PATTERN, dict(out=2)), (PATTERN, dict(out=-1)),
+    (SHAPE, dict(N=2 ** 31)), (SHAPE, dict(K=49152 + 64, ldx=49152 + 64)), (PATTERN, dict(out=2)), (PATTERN, dict(out=-1)),
     (ALIGN, dict(X=P + 8)), (ALIGN, dict(ldx=248)), (ALIGN, dict(ldx=260)), (ALIGN, dict(codes=P + 4)), (ALIGN, dict(side=P + 4)),
     (ALIGN, dict(Y=P + 4)), (ALIGN, dict(ldy=96)), (ALIGN, dict(ldy=100)), (ALIGN, dict(out=1, ldy=102)),
 ]
