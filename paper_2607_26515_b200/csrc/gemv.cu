@@ -23,7 +23,7 @@ namespace {
 constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kUnitK = 128, kTileN = 16;
 template <int NT>
-constexpr int kDepthOf = NT == 1 ? 4 : 3;  // units in flight per warp: 16 warps x 4 KB = 64 KB per SM (3 where a second token group takes the registers)
+constexpr int kDepthOf = 3;  // units in flight per warp: 16 warps x 3 KB = 48 KB per SM
 constexpr int kMaxTiles = 64;   // row tiles per CTA
 constexpr int kXPad = 64;       // bytes behind a token's staged row: neighbouring tokens use the other half of the banks
 
@@ -39,20 +39,27 @@ struct GemvArgs {
     int units_slice;  // units of 128 k per slice
 };
 
-__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t r;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-    return r;
-}
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
+__device__ __forceinline__ uint32_t mad(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+// ZERO: the sum starts here
+template <bool ZERO>
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    if (ZERO)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint4 ld_stream_u4(const uint8_t* p) {
     uint4 v;
@@ -61,45 +68,64 @@ __device__ __forceinline__ uint4 ld_stream_u4(const uint8_t* p) {
 }
 
 // What a lane needs to expand its 32 codes of one row: HiF4 half a block (four level-2 groups), MXFP4 one whole block.
+//
+// Both element formats are small floating-point numbers, and their magnitude bits are bf16 numbers as they stand once they
+// sit at the right place: S1P2 (= E1M2) at bits 7:5 is the bf16 number q/4 * 2^-126 (q < 4 as a subnormal), E2M1 at bits
+// 8:6 is value * 2^-126.  So an element is moved into place together with its sign, and one packed multiplication by
+// 2^126 times its scale gives the exact weight (at most 6 significant bits).  A scale for which that factor passes 2^127
+// is applied in two steps.
 template <int FMT>
 struct Scale;
 template <>
 struct Scale<kHiF4> {
     uint32_t base, e2, e3;
+    bool big;
+    __device__ __forceinline__ void clear() {}  // always finite
+    __device__ __forceinline__ bool two_steps() const { return big; }
     // odd: the lane's half of the 64-block
     __device__ __forceinline__ void set(uint32_t meta, int odd) {
-        base = (meta & 255u) * 0x00200020u + 0x26802680u;  // bf16 bits of S1 / 4 in both halves (s << 5 is (E << 7) | (Mn << 5))
-        e2 = (meta >> (8 + 4 * odd)) & 15u;
+        const uint32_t sc = meta & 255u;
+        big = sc >= 192u;  // S1 >= 1: 2^126 S1 2^2 does not fit, 2^-32 of it does
+        // bf16 bits of 2^126 S1 in both halves: s << 5 is (E << 7) | (Mn << 5)
+        base = sc * 0x00200020u + (big ? 0x56805680u : 0x66806680u);
+        e2 = meta >> (8 + 4 * odd);
         e3 = (meta >> (16 + 8 * odd)) & 255u;
     }
-    // (128 + q) c - 128 c is q c exactly (q c has 6 significant bits); the nibble at bits 6:4 reads as 16 q, so c / 16 there
+    // v[i]: elements i (low half) and i + 4.  Element 2j is the low, 2j + 1 the high nibble of byte j; the sign goes to bit 7
+    // of the upper byte, the magnitude to bits 7:5 of the lower byte of a half.
+    template <bool TWO>
     __device__ __forceinline__ void expand(uint32_t w, int group, uint32_t (&v)[4]) const {
-        // exponents of the two level-3 groups: bit 2i of e3 to bit 7, bit 2i + 1 to bit 23; bit i of e2 to both
-        const uint32_t m3 = (128u >> (2 * group)) | (0x00400000u >> (2 * group)), m2 = 0x00800080u >> group;
-        const uint32_t c = base + ((e3 * m3) & 0x00800080u) + ((e2 * m2) & 0x00800080u);
-        const uint32_t n = c + 0x83808380u, c16 = c - 0x02000200u, n16 = c + 0x81808180u;  // -128 c, c / 16, -8 c
-        const uint32_t h = w >> 8;
-        v[0] = fma_bf16x2((w & 0x00070007u) | 0x43004300u, c, n) ^ ((w << 12) & 0x80008000u);
-        v[1] = fma_bf16x2((w & 0x00700070u) | 0x43004300u, c16, n16) ^ ((w << 8) & 0x80008000u);
-        v[2] = fma_bf16x2((h & 0x00070007u) | 0x43004300u, c, n) ^ ((w << 4) & 0x80008000u);
-        v[3] = fma_bf16x2((h & 0x00700070u) | 0x43004300u, c16, n16) ^ (w & 0x80008000u);
+        // exponents of the two level-3 groups: bit 2i of e3 to bit 7, bit 2i + 1 to bit 23; bit i of e2 to both.  Written as
+        // multiply-adds: they run beside the integer pipe, which the element work fills.
+        const uint32_t m3 = (128u >> (2 * group)) | (0x00400000u >> (2 * group));
+        const uint32_t c = mad(e2 & (1u << group), 0x00800080u >> group, mad((e3 * m3) & 0x00800080u, 1u, base));
+        const uint32_t w1 = w << 1, w4 = w << 4, w5 = w << 5;
+        v[0] = mul_bf16x2(__byte_perm(w4, w5, 0x2604) & 0x80E080E0u, c);
+        v[1] = mul_bf16x2(__byte_perm(w, w1, 0x2604) & 0x80E080E0u, c);
+        v[2] = mul_bf16x2(__byte_perm(w4, w5, 0x3715) & 0x80E080E0u, c);
+        v[3] = mul_bf16x2(__byte_perm(w, w1, 0x3715) & 0x80E080E0u, c);
+        if (TWO) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], big ? 0x4F804F80u : 0x3F803F80u);  // 2^32
+        }
     }
 };
 template <>
 struct Scale<kMXFP4> {
     uint32_t c, c2;
-    // The three magnitude bits of E2M1 at bits 8:6 are the bf16 number value * 2^-126 (0 and 0.5 as subnormals), so one
-    // multiplication by 2^126 2^(sc - 127) gives the weight; where that factor passes 2^127 a second one takes the rest.
+    __device__ __forceinline__ void clear() { c = 0u, c2 = 0x3F803F80u; }
+    __device__ __forceinline__ bool two_steps() const { return c2 != 0x3F803F80u; }
     __device__ __forceinline__ void set(uint32_t sc, int) {
         c = min(sc + 126u, 254u) * 0x00800080u;
         c2 = sc > 128u ? (sc == 255u ? 0x7F807F80u : (sc - 1u) * 0x00800080u) : 0x3F803F80u;  // 2^(sc - 128)
     }
+    template <bool TWO>
     __device__ __forceinline__ void expand(uint32_t w, int, uint32_t (&v)[4]) const {
         v[0] = mul_bf16x2(((w << 6) & 0x01C001C0u) | ((w << 12) & 0x80008000u), c);
         v[1] = mul_bf16x2(((w << 2) & 0x01C001C0u) | ((w << 8) & 0x80008000u), c);
         v[2] = mul_bf16x2(((w >> 2) & 0x01C001C0u) | ((w << 4) & 0x80008000u), c);
         v[3] = mul_bf16x2(((w >> 6) & 0x01C001C0u) | (w & 0x80008000u), c);
-        if (c2 != 0x3F803F80u) {
+        if (TWO) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], c2);
         }
@@ -115,6 +141,26 @@ __device__ __forceinline__ uint32_t ld_nc8(const uint8_t* p) {
     uint32_t v;
     asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(v) : "l"(p));
     return v;
+}
+
+// One unit of 16 rows x 128 k: a chain of 8 instructions from zero for each token group.  The caller adds the result to its
+// sums with one rounded addition each (the tensor cores cut their sums instead of rounding them).
+template <int FMT, int NT, bool TWO>
+__device__ __forceinline__ void unit(const uint4& qa, const uint4& qb, const Scale<FMT>& fa, const Scale<FMT>& fb,
+                                     const uint8_t* const (&xs)[NT], float (&c)[NT][4]) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        uint32_t va[4], vb[4];
+        fa.template expand<TWO>(w == 0 ? qa.x : w == 1 ? qa.y : w == 2 ? qa.z : qa.w, w, va);
+        fb.template expand<TWO>(w == 0 ? qb.x : w == 1 ? qb.y : w == 2 ? qb.z : qb.w, w, vb);
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+            const uint4 x = *reinterpret_cast<const uint4*>(xs[q] + w * 64);
+            if (w == 0) mma16816<true>(c[q], va[0], vb[0], va[1], vb[1], x.x, x.y);
+            else mma16816<false>(c[q], va[0], vb[0], va[1], vb[1], x.x, x.y);
+            mma16816<false>(c[q], va[2], vb[2], va[3], vb[3], x.z, x.w);
+        }
+    }
 }
 
 // NT: groups of 8 tokens; CS: CTAs of a cluster, each with its slice of K.
@@ -142,29 +188,39 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant
     uint4 qa[kDepth], qb[kDepth];
     uint32_t sa[kDepth], sb[kDepth];
     int lu = units > 0 ? first % units : 0, lt = units > 0 ? first / units : 0;  // load cursor
-    const uint8_t *pa, *pb, *ma, *mb;
+    // The last unit of K may hold one, two or three blocks of 32: a lane beyond the end reads the start of its row instead
+    // and multiplies it with zeros (its activations are staged as zeros; an MXFP4 scale, which may be infinite, is zeroed).
+    const bool beyond = k0 + (units - 1) * kUnitK + t * 32 >= a.K;
+    const uint8_t *tcodes, *tside;  // the tile's first row; a lane's rows lie at 32-bit offsets from it
+    uint32_t oa, ob, pa, pb;
+    auto cut = [&]() {
+        if (beyond && lu == units - 1) {
+            const uint32_t ra = min(g, a.N - 1 - (tile0 + lt) * kTileN), rb = min(g + 8, a.N - 1 - (tile0 + lt) * kTileN);
+            oa = ra * (uint32_t)row_codes, ob = rb * (uint32_t)row_codes, pa = ra * (uint32_t)row_side, pb = rb * (uint32_t)row_side;
+        }
+    };
     auto point = [&]() {
-        const int64_t n0 = min((int64_t)(tile0 + lt) * kTileN + g, (int64_t)a.N - 1);
-        const int64_t n1 = min((int64_t)(tile0 + lt) * kTileN + g + 8, (int64_t)a.N - 1);
-        const int64_t kc = (int64_t)k0 / 2 + lu * 64 + t * 16;
-        const int64_t ks = FMT == kHiF4 ? (int64_t)k0 / 16 + lu * 8 + (t >> 1) * 4 : (int64_t)k0 / 32 + lu * 4 + t;
-        pa = a.codes + n0 * row_codes + kc, pb = a.codes + n1 * row_codes + kc;
-        ma = a.side + n0 * row_side + ks, mb = a.side + n1 * row_side + ks;
+        const int n0 = (tile0 + lt) * kTileN;
+        if (n0 >= a.N) return;  // behind the last tile: nothing is loaded any more
+        tcodes = a.codes + n0 * row_codes, tside = a.side + n0 * row_side;
+        const uint32_t ra = min(g, a.N - 1 - n0), rb = min(g + 8, a.N - 1 - n0);
+        const uint32_t kc = k0 / 2 + lu * 64 + t * 16, ks = FMT == kHiF4 ? k0 / 16 + lu * 8 + (t >> 1) * 4 : k0 / 32 + lu * 4 + t;
+        oa = ra * (uint32_t)row_codes + kc, ob = rb * (uint32_t)row_codes + kc;
+        pa = ra * (uint32_t)row_side + ks, pb = rb * (uint32_t)row_side + ks;
+        cut();
     };
     auto load = [&](int d) {
-        if (k0 + lu * kUnitK + t * 32 < a.K) {  // the last unit of a row may be cut to one, two or three lanes of a quad
-            qa[d] = ld_stream_u4(pa), qb[d] = ld_stream_u4(pb);
-            sa[d] = FMT == kHiF4 ? ld_nc32(ma) : ld_nc8(ma);
-            sb[d] = FMT == kHiF4 ? ld_nc32(mb) : ld_nc8(mb);
-        } else {
-            qa[d] = qb[d] = make_uint4(0u, 0u, 0u, 0u);
-            sa[d] = sb[d] = 0u;
-        }
-        if (++lu == units) {
-            lu = 0, ++lt;
-            point();
-        } else {
-            pa += 64, pb += 64, ma += kSideStep, mb += kSideStep;
+        qa[d] = ld_stream_u4(tcodes + oa), qb[d] = ld_stream_u4(tcodes + ob);
+        sa[d] = FMT == kHiF4 ? ld_nc32(tside + pa) : ld_nc8(tside + pa);
+        sb[d] = FMT == kHiF4 ? ld_nc32(tside + pb) : ld_nc8(tside + pb);
+        oa += 64, ob += 64, pa += kSideStep, pb += kSideStep;
+        if (++lu >= units - 1) {
+            if (lu >= units) {
+                lu = 0, ++lt;
+                point();
+            } else {
+                cut();
+            }
         }
     };
     if (first < last) point();
@@ -174,14 +230,24 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant
 
     // ---- activations of this slice: chunks of 8, pairs (i, i + 4) side by side, chunk (lane t, word w) of a unit at
     // (4 w + t) * 16 bytes, so that the four lanes of a quad read 64 consecutive bytes
-    const int chunks = a.units_slice * 16;
-    for (int i = threadIdx.x; i < a.M * chunks; i += kThreads) {
-        const int m = i / chunks, j = i - m * chunks, k = k0 + j * 8;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (k < a.K) v = *reinterpret_cast<const uint4*>(a.X + m * a.ldx + k);
-        const uint4 p = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410),
-                                   __byte_perm(v.y, v.w, 0x7632));
-        *reinterpret_cast<uint4*>(smem + m * xrow + (j >> 4) * 256 + ((j & 3) * 4 + ((j >> 2) & 3)) * 16) = p;
+    const int chunks = a.units_slice * 16, staged = a.M * chunks;
+    constexpr int kBatch = 8;  // loads in flight per thread: the staging is latency, not bandwidth
+    for (int i0 = threadIdx.x; i0 < staged; i0 += kThreads * kBatch) {
+        uint4 v[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int i = i0 + b * kThreads, m = i / chunks, k = k0 + (i - m * chunks) * 8;
+            v[b] = make_uint4(0u, 0u, 0u, 0u);
+            if (i < staged && k < a.K) v[b] = *reinterpret_cast<const uint4*>(a.X + m * a.ldx + k);
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int i = i0 + b * kThreads, m = i / chunks, j = i - m * chunks;
+            if (i >= staged) break;
+            *reinterpret_cast<uint4*>(smem + m * xrow + (j >> 4) * 256 + ((j & 3) * 4 + ((j >> 2) & 3)) * 16) =
+                make_uint4(__byte_perm(v[b].x, v[b].z, 0x5410), __byte_perm(v[b].x, v[b].z, 0x7632), __byte_perm(v[b].y, v[b].w, 0x5410),
+                           __byte_perm(v[b].y, v[b].w, 0x7632));
+        }
     }
     __syncthreads();
     pdl_trigger();
@@ -191,40 +257,27 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant
     for (int q = 0; q < NT; ++q)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[q][i] = 0.0f;
+    int cu = units > 0 ? first % units : 0, ct = units > 0 ? first / units : 0;
     const uint8_t* xs[NT];  // the lane's token of each group (columns behind the last token repeat it; they are not stored)
 #pragma unroll
-    for (int q = 0; q < NT; ++q) xs[q] = smem + min(q * 8 + g, a.M - 1) * xrow + t * 16;
-    int cu = units > 0 ? first % units : 0, ct = units > 0 ? first / units : 0;
+    for (int q = 0; q < NT; ++q) xs[q] = smem + min(q * 8 + g, a.M - 1) * xrow + cu * 256 + t * 16;
     for (int i = first; i < last; i += kDepth) {
 #pragma unroll
         for (int d = 0; d < kDepth; ++d) {
             if (i + d >= last) break;
-            const uint4 wa = qa[d], wb = qb[d];
             Scale<FMT> fa, fb;
             fa.set(sa[d], t & 1), fb.set(sb[d], t & 1);
-            if (i + d + kDepth < last) load(d);
-            // a chain of 8 instructions from zero, then one rounded addition per sum: the tensor cores cut their sums
+            if (FMT == kMXFP4 && beyond && cu == units - 1) fa.clear(), fb.clear();
             float c[NT][4];
+            if (__any_sync(0xFFFFFFFFu, fa.two_steps() || fb.two_steps())) unit<FMT, NT, true>(qa[d], qb[d], fa, fb, xs, c);
+            else unit<FMT, NT, false>(qa[d], qb[d], fa, fb, xs, c);
+            if (i + d + kDepth < last) load(d);
 #pragma unroll
-            for (int q = 0; q < NT; ++q)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) c[q][j] = 0.0f;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                uint32_t va[4], vb[4];
-                fa.expand(w == 0 ? wa.x : w == 1 ? wa.y : w == 2 ? wa.z : wa.w, w, va);
-                fb.expand(w == 0 ? wb.x : w == 1 ? wb.y : w == 2 ? wb.z : wb.w, w, vb);
-#pragma unroll
-                for (int q = 0; q < NT; ++q) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(xs[q] + cu * 256 + w * 64);
-                    mma16816(c[q], va[0], vb[0], va[1], vb[1], x.x, x.y);
-                    mma16816(c[q], va[2], vb[2], va[3], vb[3], x.z, x.w);
-                }
-            }
-#pragma unroll
-            for (int q = 0; q < NT; ++q)
+            for (int q = 0; q < NT; ++q) {
+                xs[q] += 256;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[q][j] += c[q][j];
+            }
             if (++cu == units || i + d + 1 == last) {
                 float* out = part + (size_t)(ct + warp) * (kTileN * 8 * NT);
 #pragma unroll
@@ -233,8 +286,9 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant
                     *reinterpret_cast<float2*>(out + (g + 8) * (8 * NT) + q * 8 + t * 2) = make_float2(acc[q][2], acc[q][3]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) acc[q][j] = 0.0f;
+                    xs[q] -= units * 256;
                 }
-                if (cu == units) cu = 0, ++ct;
+                cu = 0, ++ct;
             }
         }
     }
@@ -289,22 +343,26 @@ struct GemvPlan {
 
 constexpr size_t kSmemMax = 227 * 1024, kSmemTwo = 113 * 1024;  // per CTA: alone on its SM, two on an SM
 
+// Clusters of 1, 2, 4, 8 CTAs that are resident at once, one or two CTAs per SM (larger clusters leave SMs of a GPC unused).
+constexpr int kSlots[2][4] = {{148, 74, 33, 15}, {296, 148, 71, 33}};
+
 // Splits the K range over cs CTAs and gives each cluster T row tiles so that the busiest CTA slot finishes first.  Cycles
 // per unit and the fixed costs are rough measurements; only their proportions matter.
 GemvPlan plan_gemv(int M, int64_t N, int64_t K) {
     const int tiles = (int)((N + kTileN - 1) / kTileN), units = (int)((K + kUnitK - 1) / kUnitK), nt = M > 8 ? 2 : 1;
     GemvPlan best{0, 0, 0, 0};
     double best_cost = 0;
-    for (int cs = 1; cs <= 8; cs *= 2) {
+    for (int lg = 0; lg < 4; ++lg) {
+        const int cs = 1 << lg;
         const int us = (units + cs - 1) / cs;
         const size_t x = (size_t)M * (us * 256 + kXPad);
         for (int T = 1; T <= std::min(kMaxTiles, tiles); ++T) {
             const size_t smem = x + (size_t)(T + kWarps) * kTileN * 8 * nt * sizeof(float);
             if (smem > kSmemMax) break;
-            const int per_sm = smem <= kSmemTwo ? 2 : 1;
-            const int64_t clusters = (tiles + T - 1) / T, slots = 148 * per_sm / cs;
+            const bool two = smem <= kSmemTwo;
+            const int64_t clusters = (tiles + T - 1) / T, slots = kSlots[two][lg];
             const double waves = (double)((clusters + slots - 1) / slots);
-            const double cost = waves * ((double)((T * us + kWarps - 1) / kWarps) * 450 * per_sm + 2000 + (double)x / 32 + (cs > 1 ? 800 : 0));
+            const double cost = waves * ((double)((T * us + kWarps - 1) / kWarps) * (two ? 1300 : 800) + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
             if (best.cs == 0 || cost < best_cost) best = GemvPlan{cs, T, us, smem}, best_cost = cost;
         }
     }
