@@ -23,7 +23,7 @@ namespace {
 constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kUnitK = 128, kTileN = 16;
 template <int NT>
-constexpr int kDepthOf = 3;  // units in flight per warp: 16 warps x 3 KB = 48 KB per SM
+constexpr int kDepthOf = 2;  // units in flight per warp beside the one at hand: 16 warps x 2 KB = 32 KB per SM (3 and 4 measured the same)
 constexpr int kMaxTiles = 64;   // row tiles per CTA
 constexpr int kXPad = 64;       // bytes behind a token's staged row: neighbouring tokens use the other half of the banks
 
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant
 
     // ---- the warp's run of (tile, unit) pairs: first loads before the activations are staged
     const int total = tiles * units;
-    const int first = (int)((int64_t)total * warp / kWarps), last = (int)((int64_t)total * (warp + 1) / kWarps);
+    const int first = total * warp / kWarps, last = total * (warp + 1) / kWarps;  // below 64 x 384 x 8
     const int64_t row_codes = a.K / 2, row_side = FMT == kHiF4 ? (int64_t)a.K / 64 * 4 : (int64_t)a.K / 32;
     constexpr int kSideStep = FMT == kHiF4 ? 8 : 4;  // side bytes per unit
     uint4 qa[kDepth], qb[kDepth];
@@ -230,23 +230,25 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant
 
     // ---- activations of this slice: chunks of 8, pairs (i, i + 4) side by side, chunk (lane t, word w) of a unit at
     // (4 w + t) * 16 bytes, so that the four lanes of a quad read 64 consecutive bytes
-    const int chunks = a.units_slice * 16, staged = a.M * chunks;
     constexpr int kBatch = 8;  // loads in flight per thread: the staging is latency, not bandwidth
-    for (int i0 = threadIdx.x; i0 < staged; i0 += kThreads * kBatch) {
-        uint4 v[kBatch];
+    for (int j = threadIdx.x; j < a.units_slice * 16; j += kThreads) {
+        const int k = k0 + j * 8;
+        uint8_t* dst = smem + (j >> 4) * 256 + ((j & 3) * 4 + ((j >> 2) & 3)) * 16;
+        const __nv_bfloat16* src = a.X + k;
+        for (int m0 = 0; m0 < a.M; m0 += kBatch) {
+            uint4 v[kBatch];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            const int i = i0 + b * kThreads, m = i / chunks, k = k0 + (i - m * chunks) * 8;
-            v[b] = make_uint4(0u, 0u, 0u, 0u);
-            if (i < staged && k < a.K) v[b] = *reinterpret_cast<const uint4*>(a.X + m * a.ldx + k);
-        }
+            for (int b = 0; b < kBatch; ++b) {
+                v[b] = make_uint4(0u, 0u, 0u, 0u);
+                if (m0 + b < a.M && k < a.K) v[b] = *reinterpret_cast<const uint4*>(src + (m0 + b) * a.ldx);
+            }
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            const int i = i0 + b * kThreads, m = i / chunks, j = i - m * chunks;
-            if (i >= staged) break;
-            *reinterpret_cast<uint4*>(smem + m * xrow + (j >> 4) * 256 + ((j & 3) * 4 + ((j >> 2) & 3)) * 16) =
-                make_uint4(__byte_perm(v[b].x, v[b].z, 0x5410), __byte_perm(v[b].x, v[b].z, 0x7632), __byte_perm(v[b].y, v[b].w, 0x5410),
-                           __byte_perm(v[b].y, v[b].w, 0x7632));
+            for (int b = 0; b < kBatch; ++b) {
+                if (m0 + b >= a.M) break;
+                *reinterpret_cast<uint4*>(dst + (m0 + b) * xrow) =
+                    make_uint4(__byte_perm(v[b].x, v[b].z, 0x5410), __byte_perm(v[b].x, v[b].z, 0x7632), __byte_perm(v[b].y, v[b].w, 0x5410),
+                               __byte_perm(v[b].y, v[b].w, 0x7632));
+            }
         }
     }
     __syncthreads();
@@ -300,35 +302,35 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant
     } else {
         __syncthreads();
     }
-    const int rows = tiles * kTileN, outs = rows * a.M;
-    const int per = (outs + CS - 1) / CS;
-    for (int o = rank * per + threadIdx.x; o < min(outs, (rank + 1) * per); o += kThreads) {
-        const int m = o / rows, r = o - m * rows, tile = r / kTileN;
-        const int64_t n = (int64_t)tile0 * kTileN + r;
-        if (n >= a.N) continue;
-        float s = 0.0f;
+    const int rows = min(tiles * kTileN, a.N - tile0 * kTileN);
+    for (int m = rank; m < a.M; m += CS)
+        for (int r = threadIdx.x; r < rows; r += kThreads) {
+            const int tile = r / kTileN;
+            const float* slot = part + (size_t)tile * (kTileN * 8 * NT) + (r % kTileN) * (8 * NT) + m;
+            float s = 0.0f;
 #pragma unroll
-        for (int c = 0; c < CS; ++c) {
-            const int cunits = CS > 1 ? max(0, min(a.units_slice, units_all - c * a.units_slice)) : units;
-            const int ctotal = tiles * cunits, u0 = tile * cunits, u1 = u0 + cunits;
-            for (int w = 0; w < kWarps; ++w) {
-                const int f = (int)((int64_t)ctotal * w / kWarps), l = (int)((int64_t)ctotal * (w + 1) / kWarps);
-                if (f >= u1 || l <= u0 || f >= l) continue;
-                const float* src = part + (size_t)(tile + w) * (kTileN * 8 * NT) + (r % kTileN) * (8 * NT) + m;
-                if (CS == 1) {
-                    s += *src;
-                } else {
-                    uint32_t remote;
-                    float v;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"((uint32_t)__cvta_generic_to_shared(src)), "r"(c));
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
-                    s += v;
+            for (int c = 0; c < CS; ++c) {
+                const int cunits = CS > 1 ? max(0, min(a.units_slice, units_all - c * a.units_slice)) : units;
+                const int ctotal = tiles * cunits, u0 = tile * cunits, u1 = u0 + cunits;
+                for (int w = 0; w < kWarps; ++w) {
+                    const int f = ctotal * w / kWarps, l = ctotal * (w + 1) / kWarps;
+                    if (f >= u1 || l <= u0 || f >= l) continue;
+                    const float* src = slot + w * (kTileN * 8 * NT);
+                    if (CS == 1) {
+                        s += *src;
+                    } else {
+                        uint32_t remote;
+                        float v;
+                        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"((uint32_t)__cvta_generic_to_shared(src)), "r"(c));
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+                        s += v;
+                    }
                 }
             }
+            const int64_t o = m * a.ldy + (int64_t)tile0 * kTileN + r;
+            if (a.out_dtype == RESQ_OUT_BF16) static_cast<__nv_bfloat16*>(a.Y)[o] = __float2bfloat16_rn(s);
+            else static_cast<float*>(a.Y)[o] = s;
         }
-        if (a.out_dtype == RESQ_OUT_BF16) static_cast<__nv_bfloat16*>(a.Y)[m * a.ldy + n] = __float2bfloat16_rn(s);
-        else static_cast<float*>(a.Y)[m * a.ldy + n] = s;
-    }
     if (CS > 1) {  // no CTA leaves while a peer may still read its shared memory
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
