@@ -9,9 +9,12 @@
 // a lane owns 32 consecutive k of rows g and g + 8 (one 16-byte load each), and pairs elements i and i + 4 of a 32-bit word:
 // their nibbles lie 16 bits apart, so one mask takes both.
 //
-// Work: a unit is 16 weight rows x 128 k (1 KB of codes).  A CTA (8 warps) owns T row tiles and one of CS slices of K; its
-// T x units are dealt out evenly and contiguously to its warps, which keep kDepth units in flight.  The partial sums of a
-// (tile, warp) go to shared memory and are added in a fixed order, over the CTAs of the cluster where K is sliced.
+// Work: a unit is 16 weight rows x 128 k (1 KB of codes).  A CTA (16 warps, one CTA per SM, so that the activations are staged
+// once) owns T row tiles and one of CS slices of K; its T x units are dealt out evenly and contiguously to its warps.  The codes
+// come by asynchronous copies into a ring of kDepth units per warp, each lane fetching what it will expand itself; loads into
+// registers measured up to 1.6 times slower, because their lines in flight have to fit into what the staged activations leave of
+// the L1.  Tiles that a warp has to itself are written from its registers; the parts of a tile that several warps (or slices)
+// share go to shared memory and are added in a fixed order.
 #include "common.cuh"
 #include "row_common.cuh"
 
@@ -20,11 +23,15 @@
 namespace resq {
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kWarps = 16, kThreads = kWarps * 32;
 constexpr int kUnitK = 128, kTileN = 16;
-template <int NT>
-constexpr int kDepthOf = 2;  // units in flight per warp beside the one at hand: 16 warps x 2 KB = 32 KB per SM (3 and 4 measured the same)
-constexpr int kMaxTiles = 64;   // row tiles per CTA
+constexpr int kDepth = 4;       // units in flight per warp: 64 KB per SM
+constexpr int kChunk = 4;       // scales are fetched for 4 units of a tile at a time (HiF4: 32 bytes a row)
+// words a row of such a chunk: HiF4 8 and one against bank conflicts, MXFP4 4 and one because its rows start on any byte
+template <int FMT>
+constexpr int kSideRow = FMT == kHiF4 ? 9 : 5;
+constexpr int kSideBufs = kDepth + 1;
+constexpr int kMaxTiles = 64;   // row tiles per CTA (int arithmetic on units x warps)
 constexpr int kXPad = 64;       // bytes behind a token's staged row: neighbouring tokens use the other half of the banks
 
 struct GemvArgs {
@@ -61,10 +68,17 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint4 ld_stream_u4(const uint8_t* p) {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// the first `n` bytes of a word (0 to 4), zeros behind them
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, int n) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 // What a lane needs to expand its 32 codes of one row: HiF4 half a block (four level-2 groups), MXFP4 one whole block.
@@ -132,17 +146,6 @@ struct Scale<kMXFP4> {
     }
 };
 
-__device__ __forceinline__ uint32_t ld_nc32(const uint8_t* p) {
-    uint32_t v;
-    asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
-    return v;
-}
-__device__ __forceinline__ uint32_t ld_nc8(const uint8_t* p) {
-    uint32_t v;
-    asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(v) : "l"(p));
-    return v;
-}
-
 // One unit of 16 rows x 128 k: a chain of 8 instructions from zero for each token group.  The caller adds the result to its
 // sums with one rounded addition each (the tensor cores cut their sums instead of rounding them).
 template <int FMT, int NT, bool TWO>
@@ -163,10 +166,24 @@ __device__ __forceinline__ void unit(const uint4& qa, const uint4& qb, const Sca
     }
 }
 
+__device__ __forceinline__ void store_out(const GemvArgs& a, int m, int n, float v) {
+    if (a.out_dtype == RESQ_OUT_BF16) static_cast<__nv_bfloat16*>(a.Y)[m * a.ldy + n] = __float2bfloat16_rn(v);
+    else static_cast<float*>(a.Y)[m * a.ldy + n] = v;
+}
+
+// Slots of 16 x 8 NT partial sums: without slices two per warp (the tile its run starts in and the one it ends in), with slices
+// one per (tile, warp) of a run, at tile + warp (both only grow along the runs).
+template <int FMT>
+__host__ __device__ constexpr size_t ring_bytes() {
+    return (size_t)kWarps * (kDepth * 1024 + kSideBufs * kTileN * kSideRow<FMT> * 4);
+}
+__host__ __device__ inline size_t part_bytes(int cs, int tiles, int nt) {
+    return (size_t)(cs == 1 ? 2 * kWarps : tiles + kWarps) * kTileN * 8 * nt * sizeof(float);
+}
+
 // NT: groups of 8 tokens; CS: CTAs of a cluster, each with its slice of K.
 template <int FMT, int NT, int CS>
-__global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant__ GemvArgs a) {
-    constexpr int kDepth = kDepthOf<NT>;
+__global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant__ GemvArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int rank = CS > 1 ? (int)(blockIdx.x % CS) : 0;
@@ -176,57 +193,79 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant
     const int units = max(0, min(a.units_slice, units_all - rank * a.units_slice));
     const int k0 = rank * a.units_slice * kUnitK;
     const int xrow = a.units_slice * 256 + kXPad;
-    float* part = reinterpret_cast<float*>(smem + (size_t)a.M * xrow);  // [tile + warp][16 rows][8 NT tokens]
+    uint8_t* const ring = smem + (size_t)a.M * xrow + warp * (kDepth * 1024);
+    uint8_t* const sides = smem + (size_t)a.M * xrow + kWarps * (kDepth * 1024) + warp * (kSideBufs * kTileN * kSideRow<FMT> * 4);
+    float* const part = reinterpret_cast<float*>(smem + (size_t)a.M * xrow + ring_bytes<FMT>());
+    constexpr int kSlot = kTileN * 8 * NT;
 
     pdl_wait();
 
-    // ---- the warp's run of (tile, unit) pairs: first loads before the activations are staged
+    // ---- the warp's run of (tile, unit) pairs: first copies before the activations are staged
     const int total = tiles * units;
-    const int first = total * warp / kWarps, last = total * (warp + 1) / kWarps;  // below 64 x 384 x 8
+    const int first = total * warp / kWarps, last = total * (warp + 1) / kWarps;  // below 64 x 384 x 16
     const int64_t row_codes = a.K / 2, row_side = FMT == kHiF4 ? (int64_t)a.K / 64 * 4 : (int64_t)a.K / 32;
-    constexpr int kSideStep = FMT == kHiF4 ? 8 : 4;  // side bytes per unit
-    uint4 qa[kDepth], qb[kDepth];
-    uint32_t sa[kDepth], sb[kDepth];
-    int lu = units > 0 ? first % units : 0, lt = units > 0 ? first / units : 0;  // load cursor
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16, side_at = (uint32_t)__cvta_generic_to_shared(sides);
+    int lu = units > 0 ? first % units : 0, lt = units > 0 ? first / units : 0;  // copy cursor
+    int lstage = 0, lbuf = 0;
+    bool lchunk = true;  // the next copy starts a chunk of scales
     // The last unit of K may hold one, two or three blocks of 32: a lane beyond the end reads the start of its row instead
     // and multiplies it with zeros (its activations are staged as zeros; an MXFP4 scale, which may be infinite, is zeroed).
     const bool beyond = k0 + (units - 1) * kUnitK + t * 32 >= a.K;
-    const uint8_t *tcodes, *tside;  // the tile's first row; a lane's rows lie at 32-bit offsets from it
-    uint32_t oa, ob, pa, pb;
-    auto cut = [&]() {
-        if (beyond && lu == units - 1) {
-            const uint32_t ra = min(g, a.N - 1 - (tile0 + lt) * kTileN), rb = min(g + 8, a.N - 1 - (tile0 + lt) * kTileN);
-            oa = ra * (uint32_t)row_codes, ob = rb * (uint32_t)row_codes, pa = ra * (uint32_t)row_side, pb = rb * (uint32_t)row_side;
-        }
-    };
+    const uint8_t *tcodes = a.codes, *tside = a.side;  // the tile's first row; a lane's rows lie at 32-bit offsets from it
+    uint32_t oa = 0, ob = 0;
     auto point = [&]() {
         const int n0 = (tile0 + lt) * kTileN;
-        if (n0 >= a.N) return;  // behind the last tile: nothing is loaded any more
+        if (n0 >= a.N) return;  // behind the last tile: nothing is copied any more
         tcodes = a.codes + n0 * row_codes, tside = a.side + n0 * row_side;
-        const uint32_t ra = min(g, a.N - 1 - n0), rb = min(g + 8, a.N - 1 - n0);
-        const uint32_t kc = k0 / 2 + lu * 64 + t * 16, ks = FMT == kHiF4 ? k0 / 16 + lu * 8 + (t >> 1) * 4 : k0 / 32 + lu * 4 + t;
-        oa = ra * (uint32_t)row_codes + kc, ob = rb * (uint32_t)row_codes + kc;
-        pa = ra * (uint32_t)row_side + ks, pb = rb * (uint32_t)row_side + ks;
-        cut();
+        const uint32_t kc = beyond && lu == units - 1 ? 0u : (uint32_t)(k0 / 2 + lu * 64 + t * 16);
+        oa = (uint32_t)min(g, a.N - 1 - n0) * (uint32_t)row_codes + kc, ob = (uint32_t)min(g + 8, a.N - 1 - n0) * (uint32_t)row_codes + kc;
     };
-    auto load = [&](int d) {
-        qa[d] = ld_stream_u4(tcodes + oa), qb[d] = ld_stream_u4(tcodes + ob);
-        sa[d] = FMT == kHiF4 ? ld_nc32(tside + pa) : ld_nc8(tside + pa);
-        sb[d] = FMT == kHiF4 ? ld_nc32(tside + pb) : ld_nc8(tside + pb);
-        oa += 64, ob += 64, pa += kSideStep, pb += kSideStep;
-        if (++lu >= units - 1) {
-            if (lu >= units) {
-                lu = 0, ++lt;
-                point();
-            } else {
-                cut();
+    auto copy_sides = [&]() {
+        const int n0 = (tile0 + lt) * kTileN, rows = a.N - 1 - n0;
+        const uint32_t dst = side_at + lbuf * (kTileN * kSideRow<FMT> * 4);
+        if (FMT == kHiF4) {
+            const int b0 = k0 / 64 + (lu / kChunk) * (2 * kChunk), nb = a.K / 64;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = i * 4 + (lane >> 3), b = b0 + (lane & 7);
+                copy4(dst + (r * 9 + (lane & 7)) * 4, tside + (uint32_t)min(r, rows) * (uint32_t)row_side + min(b, nb - 1) * 4, b < nb ? 4 : 0);
             }
+        } else {
+            // whole aligned words over the 16 bytes of a row, of which the first may belong to the row before; the array ends
+            // within a word at the earliest three bytes before a multiple of 4
+            const uint8_t* const end = a.side + a.N * row_side;
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                const int j = i * 32 + lane, r = j / 5;
+                if (j < kTileN * 5) {
+                    const uint8_t* p = tside + (uint32_t)min(r, rows) * (uint32_t)row_side + (k0 / 32 + (lu / kChunk) * (4 * kChunk));
+                    p = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3) + (j - r * 5) * 4;
+                    const int n = (int)max((int64_t)0, min((int64_t)4, (int64_t)(end - p)));
+                    copy4(dst + j * 4, n > 0 ? p : a.side, n);
+                }
+            }
+        }
+        if (++lbuf == kSideBufs) lbuf = 0;
+    };
+    auto copy = [&]() {
+        if (lchunk) copy_sides();
+        copy16(ring_at + lstage * 1024, tcodes + oa);
+        copy16(ring_at + lstage * 1024 + 512, tcodes + ob);
+        if (++lstage == kDepth) lstage = 0;
+        oa += 64, ob += 64;
+        ++lu;
+        lchunk = (lu & (kChunk - 1)) == 0;
+        if (lu >= units - 1) {
+            if (lu == units) lu = 0, ++lt, lchunk = true;
+            point();
         }
     };
     if (first < last) point();
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d)
-        if (first + d < last) load(d);
+    for (int d = 0; d < kDepth; ++d) {
+        if (first + d < last) copy();
+        copies_commit();
+    }
 
     // ---- activations of this slice: chunks of 8, pairs (i, i + 4) side by side, chunk (lane t, word w) of a unit at
     // (4 w + t) * 16 bytes, so that the four lanes of a quad read 64 consecutive bytes
@@ -254,48 +293,87 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant
     __syncthreads();
     pdl_trigger();
 
+    // ---- units in order
     float acc[NT][4];
 #pragma unroll
     for (int q = 0; q < NT; ++q)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[q][i] = 0.0f;
-    int cu = units > 0 ? first % units : 0, ct = units > 0 ? first / units : 0;
+    int cu = units > 0 ? first % units : 0, ct = units > 0 ? first / units : 0, stage = 0, buf = -1;
+    bool whole = cu == 0;  // the run holds the tile's first unit
     const uint8_t* xs[NT];  // the lane's token of each group (columns behind the last token repeat it; they are not stored)
 #pragma unroll
     for (int q = 0; q < NT; ++q) xs[q] = smem + min(q * 8 + g, a.M - 1) * xrow + cu * 256 + t * 16;
-    for (int i = first; i < last; i += kDepth) {
-#pragma unroll
-        for (int d = 0; d < kDepth; ++d) {
-            if (i + d >= last) break;
-            Scale<FMT> fa, fb;
-            fa.set(sa[d], t & 1), fb.set(sb[d], t & 1);
-            if (FMT == kMXFP4 && beyond && cu == units - 1) fa.clear(), fb.clear();
-            float c[NT][4];
-            if (__any_sync(0xFFFFFFFFu, fa.two_steps() || fb.two_steps())) unit<FMT, NT, true>(qa[d], qb[d], fa, fb, xs, c);
-            else unit<FMT, NT, false>(qa[d], qb[d], fa, fb, xs, c);
-            if (i + d + kDepth < last) load(d);
-#pragma unroll
-            for (int q = 0; q < NT; ++q) {
-                xs[q] += 256;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[q][j] += c[q][j];
+    const uint8_t *siderow_a = nullptr, *siderow_b = nullptr;
+    bool chunk = true;
+    for (int i = first; i < last; ++i) {
+        copies_wait<kDepth - 1>();
+        __syncwarp();  // the scales were copied by other lanes
+        if (chunk) {
+            if (++buf == kSideBufs) buf = 0;
+            const uint8_t* s = sides + buf * (kTileN * kSideRow<FMT> * 4);
+            if (FMT == kHiF4) {
+                siderow_a = s + (g * 9 + (t >> 1)) * 4, siderow_b = siderow_a + 8 * 9 * 4;
+            } else {
+                const int n0 = (tile0 + ct) * kTileN, rows = a.N - 1 - n0;
+                siderow_a = s + g * 20 + t + (int)(((n0 + min(g, rows)) * row_side) & 3);
+                siderow_b = s + (g + 8) * 20 + t + (int)(((n0 + min(g + 8, rows)) * row_side) & 3);
             }
-            if (++cu == units || i + d + 1 == last) {
-                float* out = part + (size_t)(ct + warp) * (kTileN * 8 * NT);
+        }
+        const uint4 qa = *reinterpret_cast<const uint4*>(ring + stage * 1024 + lane * 16);
+        const uint4 qb = *reinterpret_cast<const uint4*>(ring + stage * 1024 + lane * 16 + 512);
+        if (++stage == kDepth) stage = 0;
+        const int cc = cu & (kChunk - 1);
+        Scale<FMT> fa, fb;
+        if (FMT == kHiF4) {
+            fa.set(*reinterpret_cast<const uint32_t*>(siderow_a + cc * 8), t & 1);
+            fb.set(*reinterpret_cast<const uint32_t*>(siderow_b + cc * 8), t & 1);
+        } else {
+            fa.set(siderow_a[cc * 4], 0), fb.set(siderow_b[cc * 4], 0);
+            if (beyond && cu == units - 1) fa.clear(), fb.clear();
+        }
+        float c[NT][4];
+        if (__any_sync(0xFFFFFFFFu, fa.two_steps() || fb.two_steps())) unit<FMT, NT, true>(qa, qb, fa, fb, xs, c);
+        else unit<FMT, NT, false>(qa, qb, fa, fb, xs, c);
+        if (i + kDepth < last) copy();
+        copies_commit();
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+            xs[q] += 256;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[q][j] += c[q][j];
+        }
+        ++cu;
+        chunk = (cu & (kChunk - 1)) == 0;
+        if (cu == units || i + 1 == last) {
+            if (CS == 1 && whole && cu == units) {
+                const int n = (tile0 + ct) * kTileN + g;
+#pragma unroll
+                for (int q = 0; q < NT; ++q)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int m = q * 8 + t * 2 + (j & 1);
+                        if (m < a.M && n + (j >> 1) * 8 < a.N) store_out(a, m, n + (j >> 1) * 8, acc[q][j]);
+                    }
+            } else {
+                float* out = part + (size_t)(CS > 1 ? ct + warp : warp * 2 + (i - cu + 1 > first ? 1 : 0)) * kSlot;
 #pragma unroll
                 for (int q = 0; q < NT; ++q) {
                     *reinterpret_cast<float2*>(out + g * (8 * NT) + q * 8 + t * 2) = make_float2(acc[q][0], acc[q][1]);
                     *reinterpret_cast<float2*>(out + (g + 8) * (8 * NT) + q * 8 + t * 2) = make_float2(acc[q][2], acc[q][3]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[q][j] = 0.0f;
-                    xs[q] -= units * 256;
                 }
-                cu = 0, ++ct;
             }
+#pragma unroll
+            for (int q = 0; q < NT; ++q) {
+                xs[q] -= units * 256;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[q][j] = 0.0f;
+            }
+            cu = 0, ++ct, whole = true, chunk = true;
         }
     }
 
-    // ---- sums over warps (and slices) in order.  A tile's part of warp w lies at slot tile + w: both only grow along the run.
+    // ---- tiles that several warps (and slices) share, in order
     if (CS > 1) {
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
@@ -303,34 +381,47 @@ __global__ void __launch_bounds__(kThreads, 2) gemv_kernel(const __grid_constant
         __syncthreads();
     }
     const int rows = min(tiles * kTileN, a.N - tile0 * kTileN);
-    for (int m = rank; m < a.M; m += CS)
-        for (int r = threadIdx.x; r < rows; r += kThreads) {
-            const int tile = r / kTileN;
-            const float* slot = part + (size_t)tile * (kTileN * 8 * NT) + (r % kTileN) * (8 * NT) + m;
-            float s = 0.0f;
+    for (int r = threadIdx.x; r < rows; r += kThreads) {
+        const int tile = r / kTileN;
+        if (CS == 1) {
+            const int u0 = tile * units, u1 = u0 + units;
+            int w0 = kWarps, w1 = -1;
+            for (int w = 0; w < kWarps; ++w) {
+                const int f = total * w / kWarps, l = total * (w + 1) / kWarps;
+                if (f < u1 && l > u0 && f < l) w0 = min(w0, w), w1 = w;
+            }
+            if (w0 >= w1) continue;  // one warp had it
+            const float* src = part + (r % kTileN) * (8 * NT);
+            for (int m = 0; m < a.M; ++m) {
+                float s = 0.0f;
+                for (int w = w0; w <= w1; ++w) {
+                    const int f = total * w / kWarps, l = total * (w + 1) / kWarps;
+                    if (f < l) s += src[(w * 2 + (f < u0 ? 1 : 0)) * kSlot + m];
+                }
+                store_out(a, m, tile0 * kTileN + r, s);
+            }
+        } else {
+            const float* slot = part + (size_t)tile * kSlot + (r % kTileN) * (8 * NT);
+            for (int m = rank; m < a.M; m += CS) {
+                float s = 0.0f;
 #pragma unroll
-            for (int c = 0; c < CS; ++c) {
-                const int cunits = CS > 1 ? max(0, min(a.units_slice, units_all - c * a.units_slice)) : units;
-                const int ctotal = tiles * cunits, u0 = tile * cunits, u1 = u0 + cunits;
-                for (int w = 0; w < kWarps; ++w) {
-                    const int f = ctotal * w / kWarps, l = ctotal * (w + 1) / kWarps;
-                    if (f >= u1 || l <= u0 || f >= l) continue;
-                    const float* src = slot + w * (kTileN * 8 * NT);
-                    if (CS == 1) {
-                        s += *src;
-                    } else {
+                for (int c = 0; c < CS; ++c) {
+                    const int cunits = max(0, min(a.units_slice, units_all - c * a.units_slice));
+                    const int ctotal = tiles * cunits, u0 = tile * cunits, u1 = u0 + cunits;
+                    for (int w = 0; w < kWarps; ++w) {
+                        const int f = ctotal * w / kWarps, l = ctotal * (w + 1) / kWarps;
+                        if (f >= u1 || l <= u0 || f >= l) continue;
                         uint32_t remote;
                         float v;
-                        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"((uint32_t)__cvta_generic_to_shared(src)), "r"(c));
+                        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"((uint32_t)__cvta_generic_to_shared(slot + w * kSlot + m)), "r"(c));
                         asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
                         s += v;
                     }
                 }
+                store_out(a, m, tile0 * kTileN + r, s);
             }
-            const int64_t o = m * a.ldy + (int64_t)tile0 * kTileN + r;
-            if (a.out_dtype == RESQ_OUT_BF16) static_cast<__nv_bfloat16*>(a.Y)[o] = __float2bfloat16_rn(s);
-            else static_cast<float*>(a.Y)[o] = s;
         }
+    }
     if (CS > 1) {  // no CTA leaves while a peer may still read its shared memory
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
@@ -343,28 +434,25 @@ struct GemvPlan {
     size_t smem;
 };
 
-constexpr size_t kSmemMax = 227 * 1024, kSmemTwo = 113 * 1024;  // per CTA: alone on its SM, two on an SM
+constexpr size_t kSmemMax = 227 * 1024;
+// Clusters of 1, 2, 4, 8 CTAs that are resident at once, one CTA per SM (larger clusters leave SMs of a GPC unused).
+constexpr int kSlots[4] = {148, 74, 33, 15};
 
-// Clusters of 1, 2, 4, 8 CTAs that are resident at once, one or two CTAs per SM (larger clusters leave SMs of a GPC unused).
-constexpr int kSlots[2][4] = {{148, 74, 33, 15}, {296, 148, 71, 33}};
-
-// Splits the K range over cs CTAs and gives each cluster T row tiles so that the busiest CTA slot finishes first.  Cycles
-// per unit and the fixed costs are rough measurements; only their proportions matter.
-GemvPlan plan_gemv(int M, int64_t N, int64_t K) {
+// Splits the K range over cs CTAs and gives each cluster T row tiles so that the busiest SM finishes first.  Cycles per unit
+// and the fixed costs are rough measurements; only their proportions matter.
+GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
     const int tiles = (int)((N + kTileN - 1) / kTileN), units = (int)((K + kUnitK - 1) / kUnitK), nt = M > 8 ? 2 : 1;
     GemvPlan best{0, 0, 0, 0};
     double best_cost = 0;
     for (int lg = 0; lg < 4; ++lg) {
-        const int cs = 1 << lg;
-        const int us = (units + cs - 1) / cs;
-        const size_t x = (size_t)M * (us * 256 + kXPad);
+        const int cs = 1 << lg, us = (units + cs - 1) / cs;
+        const size_t x = (size_t)M * (us * 256 + kXPad), ring = fmt == kHiF4 ? ring_bytes<kHiF4>() : ring_bytes<kMXFP4>();
         for (int T = 1; T <= std::min(kMaxTiles, tiles); ++T) {
-            const size_t smem = x + (size_t)(T + kWarps) * kTileN * 8 * nt * sizeof(float);
+            const size_t smem = x + ring + part_bytes(cs, T, nt);
             if (smem > kSmemMax) break;
-            const bool two = smem <= kSmemTwo;
-            const int64_t clusters = (tiles + T - 1) / T, slots = kSlots[two][lg];
-            const double waves = (double)((clusters + slots - 1) / slots);
-            const double cost = waves * ((double)((T * us + kWarps - 1) / kWarps) * (two ? 1300 : 800) + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
+            const int64_t clusters = (tiles + T - 1) / T;
+            const double waves = (double)((clusters + kSlots[lg] - 1) / kSlots[lg]);
+            const double cost = waves * ((double)((T * us + kWarps - 1) / kWarps) * 1200 + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
             if (best.cs == 0 || cost < best_cost) best = GemvPlan{cs, T, us, smem}, best_cost = cost;
         }
     }
@@ -407,17 +495,26 @@ int gemv(int fmt, const void* X, int64_t M, int64_t K, int64_t ldx, const void* 
         return fail(RESQ_ERR_ALIGN, "gemv", "X needs a 16-byte aligned base and ldx >= K, ldx % 8 == 0");
     if (!is_aligned(w_codes, 16) || !is_aligned(w_side, 16) || !rows_aligned(Y, ldy, N, out_dtype))
         return fail(RESQ_ERR_ALIGN, "gemv", "Y / weights need 16-byte aligned bases, ldy >= N and 16-byte aligned rows");
-    const GemvPlan p = plan_gemv((int)M, N, K);
+    // Nine to sixteen tokens of very long rows (K beyond about 24000) do not fit in shared memory even in eight slices: they
+    // take two passes over the weights.
+    GemvPlan p = plan_gemv(fmt, (int)M, N, K);
+    const int64_t step = p.cs ? M : 8;
+    if (!p.cs) p = plan_gemv(fmt, 8, N, K);
     GemvArgs a;
-    a.X = static_cast<const __nv_bfloat16*>(X);
     a.codes = static_cast<const uint8_t*>(w_codes);
     a.side = static_cast<const uint8_t*>(w_side);
-    a.Y = Y;
-    a.ldx = ldx, a.ldy = ldy, a.M = (int)M, a.K = (int)K, a.N = (int)N, a.out_dtype = out_dtype;
+    a.ldx = ldx, a.ldy = ldy, a.K = (int)K, a.N = (int)N, a.out_dtype = out_dtype;
     a.tiles = (int)((N + kTileN - 1) / kTileN), a.tiles_cta = p.tiles_cta, a.units_slice = p.units_slice;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (fmt == kHiF4) return M > 8 ? launch_gemv<kHiF4, 2>(a, p, st) : launch_gemv<kHiF4, 1>(a, p, st);
-    return M > 8 ? launch_gemv<kMXFP4, 2>(a, p, st) : launch_gemv<kMXFP4, 1>(a, p, st);
+    for (int64_t m = 0; m < M; m += step) {
+        a.M = (int)std::min(step, M - m);
+        a.X = static_cast<const __nv_bfloat16*>(X) + m * ldx;
+        a.Y = static_cast<uint8_t*>(Y) + m * ldy * (out_dtype == RESQ_OUT_BF16 ? 2 : 4);
+        const int rc = fmt == kHiF4 ? (a.M > 8 ? launch_gemv<kHiF4, 2>(a, p, st) : launch_gemv<kHiF4, 1>(a, p, st))
+                                    : (a.M > 8 ? launch_gemv<kMXFP4, 2>(a, p, st) : launch_gemv<kMXFP4, 1>(a, p, st));
+        if (rc) return rc;
+    }
+    return RESQ_OK;
 }
 
 }  // namespace

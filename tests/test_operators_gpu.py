@@ -81,7 +81,8 @@ def check_gemv(x, codes, side, fmt, out):
 @pytest.mark.parametrize("out", [BF, F32])
 @pytest.mark.parametrize("fmt", ["hif4", "mxfp4"])
 @pytest.mark.parametrize("M, N, K", [(1, 1, 64), (1, 16, 128), (2, 17, 192), (3, 130, 320), (5, 77, 2048), (8, 250, 704), (9, 33, 448),
-                                     (16, 129, 1152), (1, 2048, 2048), (4, 3584, 1088), (7, 1000, 4160), (16, 64, 18944), (6, 2, 11008)])
+                                     (16, 129, 1152), (1, 2048, 2048), (4, 3584, 1088), (7, 1000, 4160), (16, 64, 18944), (6, 2, 11008),
+                                     (16, 40, 32768), (11, 33, 49152), (8, 16, 49152), (1, 700, 49152)])
 def test_gemv_parity(M, N, K, fmt, out):
     m, g = rq(), gen(M * 1000 + N + K)
     codes, side = m.pack_weight(randn(N, K, BF, g, 0.02), fmt)
