@@ -25,12 +25,13 @@ namespace {
 
 constexpr int kWarps = 16, kThreads = kWarps * 32;
 constexpr int kUnitK = 128, kTileN = 16;
-constexpr int kDepth = 4;       // units in flight per warp: 64 KB per SM
-constexpr int kChunk = 4;       // scales are fetched for 4 units of a tile at a time (HiF4: 32 bytes a row)
-// words a row of such a chunk: HiF4 8 and one against bank conflicts, MXFP4 4 and one because its rows start on any byte
+constexpr int kStep = 2;        // units of a tile per step: 256 k, one wait and one set of copies
+constexpr int kRing = 3;        // steps in flight per warp: 96 KB per SM
+// words per row of a step's scales: HiF4 4 and one against bank conflicts, MXFP4 2 and one because rows start on any byte
 template <int FMT>
-constexpr int kSideRow = FMT == kHiF4 ? 9 : 5;
-constexpr int kSideBufs = kDepth + 1;
+constexpr int kSideRow = FMT == kHiF4 ? 5 : 3;
+template <int FMT>
+constexpr int kSideBytes = kTileN * kSideRow<FMT> * 4;
 constexpr int kMaxTiles = 64;   // row tiles per CTA (int arithmetic on units x warps)
 constexpr int kXPad = 64;       // bytes behind a token's staged row: neighbouring tokens use the other half of the banks
 
@@ -86,24 +87,20 @@ __device__ __forceinline__ void copies_wait() {
 // Both element formats are small floating-point numbers, and their magnitude bits are bf16 numbers as they stand once they
 // sit at the right place: S1P2 (= E1M2) at bits 7:5 is the bf16 number q/4 * 2^-126 (q < 4 as a subnormal), E2M1 at bits
 // 8:6 is value * 2^-126.  So an element is moved into place together with its sign, and one packed multiplication by
-// 2^126 times its scale gives the exact weight (at most 6 significant bits).  A scale for which that factor passes 2^127
-// is applied in two steps.
+// 2^126 times its scale gives the exact weight (at most 6 significant bits).
 template <int FMT>
 struct Scale;
 template <>
 struct Scale<kHiF4> {
+    // 2^126 S1 2^2 may pass the range of bf16, so the weights are formed as w * 2^-16 and the sums take 2^16 at the end; only
+    // products below 2^-110 lose bits by that.
+    static constexpr float kBack = 65536.0f;
     uint32_t base, e2, e3;
-    bool big;
-    __device__ __forceinline__ void clear() {}  // always finite
-    __device__ __forceinline__ bool two_steps() const { return big; }
     // odd: the lane's half of the 64-block
     __device__ __forceinline__ void set(uint32_t meta, int odd) {
-        const uint32_t sc = meta & 255u;
-        big = sc >= 192u;  // S1 >= 1: 2^126 S1 2^2 does not fit, 2^-32 of it does
-        // bf16 bits of 2^126 S1 in both halves: s << 5 is (E << 7) | (Mn << 5)
-        base = sc * 0x00200020u + (big ? 0x56805680u : 0x66806680u);
+        base = (meta & 255u) * 0x00200020u + 0x5E805E80u;  // bf16 bits of 2^110 S1 in both halves (s << 5 is (E << 7) | (Mn << 5))
         e2 = meta >> (8 + 4 * odd);
-        e3 = (meta >> (16 + 8 * odd)) & 255u;
+        e3 = __byte_perm(meta, 0u, odd ? 0x4443 : 0x4442);
     }
     // v[i]: elements i (low half) and i + 4.  Element 2j is the low, 2j + 1 the high nibble of byte j; the sign goes to bit 7
     // of the upper byte, the magnitude to bits 7:5 of the lower byte of a half.
@@ -118,21 +115,17 @@ struct Scale<kHiF4> {
         v[1] = mul_bf16x2(__byte_perm(w, w1, 0x2604) & 0x80E080E0u, c);
         v[2] = mul_bf16x2(__byte_perm(w4, w5, 0x3715) & 0x80E080E0u, c);
         v[3] = mul_bf16x2(__byte_perm(w, w1, 0x3715) & 0x80E080E0u, c);
-        if (TWO) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], big ? 0x4F804F80u : 0x3F803F80u);  // 2^32
-        }
     }
 };
 template <>
 struct Scale<kMXFP4> {
-    uint32_t c, c2;
-    __device__ __forceinline__ void clear() { c = 0u, c2 = 0x3F803F80u; }
-    __device__ __forceinline__ bool two_steps() const { return c2 != 0x3F803F80u; }
-    __device__ __forceinline__ void set(uint32_t sc, int) {
-        c = min(sc + 126u, 254u) * 0x00800080u;
-        c2 = sc > 128u ? (sc == 255u ? 0x7F807F80u : (sc - 1u) * 0x00800080u) : 0x3F803F80u;  // 2^(sc - 128)
+    static constexpr float kBack = 1.0f;
+    uint32_t c, sc;
+    __device__ __forceinline__ void set(uint32_t code, bool none) {
+        sc = none ? 0u : code;
+        c = none ? 0u : min(code + 126u, 254u) * 0x00800080u;  // 2^126 2^(code - 127), at most 2^127
     }
+    // TWO: a scale code above 128 has a second factor 2^(code - 128)
     template <bool TWO>
     __device__ __forceinline__ void expand(uint32_t w, int, uint32_t (&v)[4]) const {
         v[0] = mul_bf16x2(((w << 6) & 0x01C001C0u) | ((w << 12) & 0x80008000u), c);
@@ -140,17 +133,19 @@ struct Scale<kMXFP4> {
         v[2] = mul_bf16x2(((w >> 2) & 0x01C001C0u) | ((w << 4) & 0x80008000u), c);
         v[3] = mul_bf16x2(((w >> 6) & 0x01C001C0u) | (w & 0x80008000u), c);
         if (TWO) {
+            const uint32_t c2 = sc > 128u ? (sc == 255u ? 0x7F807F80u : (sc - 1u) * 0x00800080u) : 0x3F803F80u;
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], c2);
         }
     }
 };
 
-// One unit of 16 rows x 128 k: a chain of 8 instructions from zero for each token group.  The caller adds the result to its
-// sums with one rounded addition each (the tensor cores cut their sums instead of rounding them).
+// One unit of 16 rows x 128 k: a chain of 8 instructions from zero for each token group, then one rounded addition to each sum
+// (the tensor cores cut their sums instead of rounding them).
 template <int FMT, int NT, bool TWO>
 __device__ __forceinline__ void unit(const uint4& qa, const uint4& qb, const Scale<FMT>& fa, const Scale<FMT>& fb,
-                                     const uint8_t* const (&xs)[NT], float (&c)[NT][4]) {
+                                     const uint8_t* const (&xs)[NT], int at, float (&acc)[NT][4]) {
+    float c[NT][4];
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         uint32_t va[4], vb[4];
@@ -158,12 +153,16 @@ __device__ __forceinline__ void unit(const uint4& qa, const uint4& qb, const Sca
         fb.template expand<TWO>(w == 0 ? qb.x : w == 1 ? qb.y : w == 2 ? qb.z : qb.w, w, vb);
 #pragma unroll
         for (int q = 0; q < NT; ++q) {
-            const uint4 x = *reinterpret_cast<const uint4*>(xs[q] + w * 64);
+            const uint4 x = *reinterpret_cast<const uint4*>(xs[q] + at + w * 64);
             if (w == 0) mma16816<true>(c[q], va[0], vb[0], va[1], vb[1], x.x, x.y);
             else mma16816<false>(c[q], va[0], vb[0], va[1], vb[1], x.x, x.y);
             mma16816<false>(c[q], va[2], vb[2], va[3], vb[3], x.z, x.w);
         }
     }
+#pragma unroll
+    for (int q = 0; q < NT; ++q)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[q][j] += c[q][j];
 }
 
 __device__ __forceinline__ void store_out(const GemvArgs& a, int m, int n, float v) {
@@ -175,7 +174,7 @@ __device__ __forceinline__ void store_out(const GemvArgs& a, int m, int n, float
 // one per (tile, warp) of a run, at tile + warp (both only grow along the runs).
 template <int FMT>
 __host__ __device__ constexpr size_t ring_bytes() {
-    return (size_t)kWarps * (kDepth * 1024 + kSideBufs * kTileN * kSideRow<FMT> * 4);
+    return (size_t)kWarps * kRing * (kStep * 1024 + kSideBytes<FMT>);
 }
 __host__ __device__ inline size_t part_bytes(int cs, int tiles, int nt) {
     return (size_t)(cs == 1 ? 2 * kWarps : tiles + kWarps) * kTileN * 8 * nt * sizeof(float);
@@ -193,8 +192,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     const int units = max(0, min(a.units_slice, units_all - rank * a.units_slice));
     const int k0 = rank * a.units_slice * kUnitK;
     const int xrow = a.units_slice * 256 + kXPad;
-    uint8_t* const ring = smem + (size_t)a.M * xrow + warp * (kDepth * 1024);
-    uint8_t* const sides = smem + (size_t)a.M * xrow + kWarps * (kDepth * 1024) + warp * (kSideBufs * kTileN * kSideRow<FMT> * 4);
+    uint8_t* const ring = smem + (size_t)a.M * xrow + warp * (kRing * kStep * 1024);
+    uint8_t* const sides = smem + (size_t)a.M * xrow + kWarps * (kRing * kStep * 1024) + warp * (kRing * kSideBytes<FMT>);
     float* const part = reinterpret_cast<float*>(smem + (size_t)a.M * xrow + ring_bytes<FMT>());
     constexpr int kSlot = kTileN * 8 * NT;
 
@@ -205,67 +204,64 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     const int first = total * warp / kWarps, last = total * (warp + 1) / kWarps;  // below 64 x 384 x 16
     const int64_t row_codes = a.K / 2, row_side = FMT == kHiF4 ? (int64_t)a.K / 64 * 4 : (int64_t)a.K / 32;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16, side_at = (uint32_t)__cvta_generic_to_shared(sides);
-    int lu = units > 0 ? first % units : 0, lt = units > 0 ? first / units : 0;  // copy cursor
-    int lstage = 0, lbuf = 0;
-    bool lchunk = true;  // the next copy starts a chunk of scales
     // The last unit of K may hold one, two or three blocks of 32: a lane beyond the end reads the start of its row instead
     // and multiplies it with zeros (its activations are staged as zeros; an MXFP4 scale, which may be infinite, is zeroed).
     const bool beyond = k0 + (units - 1) * kUnitK + t * 32 >= a.K;
+    auto step_units = [&](int u, int i) { return min(min(kStep - (u & (kStep - 1)), units - u), last - i); };
+    int lu = units > 0 ? first % units : 0, lt = units > 0 ? first / units : 0, li = first, lslot = 0;  // copy cursor
     const uint8_t *tcodes = a.codes, *tside = a.side;  // the tile's first row; a lane's rows lie at 32-bit offsets from it
     uint32_t oa = 0, ob = 0;
+    int rows_left = 0;
     auto point = [&]() {
         const int n0 = (tile0 + lt) * kTileN;
-        if (n0 >= a.N) return;  // behind the last tile: nothing is copied any more
+        rows_left = a.N - 1 - n0;
         tcodes = a.codes + n0 * row_codes, tside = a.side + n0 * row_side;
-        const uint32_t kc = beyond && lu == units - 1 ? 0u : (uint32_t)(k0 / 2 + lu * 64 + t * 16);
-        oa = (uint32_t)min(g, a.N - 1 - n0) * (uint32_t)row_codes + kc, ob = (uint32_t)min(g + 8, a.N - 1 - n0) * (uint32_t)row_codes + kc;
-    };
-    auto copy_sides = [&]() {
-        const int n0 = (tile0 + lt) * kTileN, rows = a.N - 1 - n0;
-        const uint32_t dst = side_at + lbuf * (kTileN * kSideRow<FMT> * 4);
-        if (FMT == kHiF4) {
-            const int b0 = k0 / 64 + (lu / kChunk) * (2 * kChunk), nb = a.K / 64;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = i * 4 + (lane >> 3), b = b0 + (lane & 7);
-                copy4(dst + (r * 9 + (lane & 7)) * 4, tside + (uint32_t)min(r, rows) * (uint32_t)row_side + min(b, nb - 1) * 4, b < nb ? 4 : 0);
-            }
-        } else {
-            // whole aligned words over the 16 bytes of a row, of which the first may belong to the row before; the array ends
-            // within a word at the earliest three bytes before a multiple of 4
-            const uint8_t* const end = a.side + a.N * row_side;
-#pragma unroll
-            for (int i = 0; i < 3; ++i) {
-                const int j = i * 32 + lane, r = j / 5;
-                if (j < kTileN * 5) {
-                    const uint8_t* p = tside + (uint32_t)min(r, rows) * (uint32_t)row_side + (k0 / 32 + (lu / kChunk) * (4 * kChunk));
-                    p = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3) + (j - r * 5) * 4;
-                    const int n = (int)max((int64_t)0, min((int64_t)4, (int64_t)(end - p)));
-                    copy4(dst + j * 4, n > 0 ? p : a.side, n);
-                }
-            }
-        }
-        if (++lbuf == kSideBufs) lbuf = 0;
+        oa = (uint32_t)min(g, rows_left) * (uint32_t)row_codes, ob = (uint32_t)min(g + 8, rows_left) * (uint32_t)row_codes;
     };
     auto copy = [&]() {
-        if (lchunk) copy_sides();
-        copy16(ring_at + lstage * 1024, tcodes + oa);
-        copy16(ring_at + lstage * 1024 + 512, tcodes + ob);
-        if (++lstage == kDepth) lstage = 0;
-        oa += 64, ob += 64;
-        ++lu;
-        lchunk = (lu & (kChunk - 1)) == 0;
-        if (lu >= units - 1) {
-            if (lu == units) lu = 0, ++lt, lchunk = true;
-            point();
+        if (li < last) {
+            const int n = step_units(lu, li), j0 = lu & (kStep - 1);
+#pragma unroll
+            for (int j = 0; j < kStep; ++j) {
+                if (j < j0 || j >= j0 + n) continue;
+                const int u = lu - j0 + j;
+                const uint32_t kc = beyond && u == units - 1 ? 0u : (uint32_t)(k0 / 2 + u * 64 + t * 16);
+                const uint32_t dst = ring_at + (lslot * kStep + j) * 1024;
+                copy16(dst, tcodes + oa + kc);
+                copy16(dst + 512, tcodes + ob + kc);
+            }
+            const uint32_t dst = side_at + lslot * kSideBytes<FMT>;
+            if (FMT == kHiF4) {
+                const int b = k0 / 64 + (lu - j0) * 2 + (lane & 3), nb = a.K / 64;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = i * 8 + (lane >> 2);
+                    copy4(dst + (r * 5 + (lane & 3)) * 4, tside + (uint32_t)min(r, rows_left) * (uint32_t)row_side + min(b, nb - 1) * 4, b < nb ? 4 : 0);
+                }
+            } else {
+                // whole aligned words over the 8 bytes of a row, of which the first may belong to the row before; the array
+                // may end within a word
+                const uint8_t* const end = a.side + a.N * row_side;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int j = i * 32 + lane, r = j / 3;
+                    if (j < kTileN * 3) {
+                        const uint8_t* p = tside + (uint32_t)min(r, rows_left) * (uint32_t)row_side + (k0 / 32 + (lu - j0) * 4);
+                        p = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3) + (j - r * 3) * 4;
+                        const int have = (int)max((int64_t)0, min((int64_t)4, (int64_t)(end - p)));
+                        copy4(dst + j * 4, have > 0 ? p : a.side, have);
+                    }
+                }
+            }
+            if (++lslot == kRing) lslot = 0;
+            li += n, lu += n;
+            if (lu == units && li < last) lu = 0, ++lt, point();
         }
+        copies_commit();
     };
     if (first < last) point();
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d) {
-        if (first + d < last) copy();
-        copies_commit();
-    }
+    for (int d = 0; d < kRing; ++d) copy();
 
     // ---- activations of this slice: chunks of 8, pairs (i, i + 4) side by side, chunk (lane t, word w) of a unit at
     // (4 w + t) * 16 bytes, so that the four lanes of a quad read 64 consecutive bytes
@@ -299,64 +295,74 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     for (int q = 0; q < NT; ++q)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[q][i] = 0.0f;
-    int cu = units > 0 ? first % units : 0, ct = units > 0 ? first / units : 0, stage = 0, buf = -1;
+    int cu = units > 0 ? first % units : 0, ct = units > 0 ? first / units : 0, slot = 0;
     bool whole = cu == 0;  // the run holds the tile's first unit
     const uint8_t* xs[NT];  // the lane's token of each group (columns behind the last token repeat it; they are not stored)
 #pragma unroll
-    for (int q = 0; q < NT; ++q) xs[q] = smem + min(q * 8 + g, a.M - 1) * xrow + cu * 256 + t * 16;
-    const uint8_t *siderow_a = nullptr, *siderow_b = nullptr;
-    bool chunk = true;
-    for (int i = first; i < last; ++i) {
-        copies_wait<kDepth - 1>();
+    for (int q = 0; q < NT; ++q) xs[q] = smem + min(q * 8 + g, a.M - 1) * xrow + t * 16;
+    const uint8_t *side_a = sides + g * (kSideRow<FMT> * 4), *side_b = side_a + 8 * (kSideRow<FMT> * 4);
+    int shift_a = 0, shift_b = 0;  // the byte of its word that a row's MXFP4 scales start on
+    auto tile_sides = [&]() {
+        if (FMT == kMXFP4) {
+            const int n0 = (tile0 + ct) * kTileN, left = a.N - 1 - n0;
+            shift_a = t + (int)(((n0 + min(g, left)) * row_side) & 3), shift_b = t + (int)(((n0 + min(g + 8, left)) * row_side) & 3);
+        } else {
+            shift_a = shift_b = (t >> 1) * 4;
+        }
+    };
+    tile_sides();
+    for (int i = first; i < last;) {
+        const int n = step_units(cu, i), j0 = cu & (kStep - 1);
+        copies_wait<kRing - 1>();
         __syncwarp();  // the scales were copied by other lanes
-        if (chunk) {
-            if (++buf == kSideBufs) buf = 0;
-            const uint8_t* s = sides + buf * (kTileN * kSideRow<FMT> * 4);
+        const uint8_t* codes = ring + slot * (kStep * 1024) + lane * 16;
+        const uint8_t *pa = side_a + slot * kSideBytes<FMT> + shift_a, *pb = side_b + slot * kSideBytes<FMT> + shift_b;
+        const int xat = (cu - j0) * 256;
+        Scale<FMT> fa[kStep], fb[kStep];
+        bool two = false;
+#pragma unroll
+        for (int j = 0; j < kStep; ++j) {
             if (FMT == kHiF4) {
-                siderow_a = s + (g * 9 + (t >> 1)) * 4, siderow_b = siderow_a + 8 * 9 * 4;
+                fa[j].set(*reinterpret_cast<const uint32_t*>(pa + j * 8), t & 1);
+                fb[j].set(*reinterpret_cast<const uint32_t*>(pb + j * 8), t & 1);
             } else {
-                const int n0 = (tile0 + ct) * kTileN, rows = a.N - 1 - n0;
-                siderow_a = s + g * 20 + t + (int)(((n0 + min(g, rows)) * row_side) & 3);
-                siderow_b = s + (g + 8) * 20 + t + (int)(((n0 + min(g + 8, rows)) * row_side) & 3);
+                const bool none = beyond && cu - j0 + j >= units - 1;
+                fa[j].set(pa[j * 4], none), fb[j].set(pb[j * 4], none);
+                two |= max(pa[j * 4], pb[j * 4]) > 128;
             }
         }
-        const uint4 qa = *reinterpret_cast<const uint4*>(ring + stage * 1024 + lane * 16);
-        const uint4 qb = *reinterpret_cast<const uint4*>(ring + stage * 1024 + lane * 16 + 512);
-        if (++stage == kDepth) stage = 0;
-        const int cc = cu & (kChunk - 1);
-        Scale<FMT> fa, fb;
-        if (FMT == kHiF4) {
-            fa.set(*reinterpret_cast<const uint32_t*>(siderow_a + cc * 8), t & 1);
-            fb.set(*reinterpret_cast<const uint32_t*>(siderow_b + cc * 8), t & 1);
+        auto one = [&](int j) {
+            const uint4 qa = *reinterpret_cast<const uint4*>(codes + j * 1024);
+            const uint4 qb = *reinterpret_cast<const uint4*>(codes + j * 1024 + 512);
+            unit<FMT, NT, false>(qa, qb, fa[j], fb[j], xs, xat + j * 256, acc);
+        };
+        if (FMT == kMXFP4 && __any_sync(0xFFFFFFFFu, two)) {
+#pragma unroll 1
+            for (int j = j0; j < j0 + n; ++j) {
+                const uint4 qa = *reinterpret_cast<const uint4*>(codes + j * 1024);
+                const uint4 qb = *reinterpret_cast<const uint4*>(codes + j * 1024 + 512);
+                unit<FMT, NT, true>(qa, qb, j ? fa[1] : fa[0], j ? fb[1] : fb[0], xs, xat + j * 256, acc);
+            }
         } else {
-            fa.set(siderow_a[cc * 4], 0), fb.set(siderow_b[cc * 4], 0);
-            if (beyond && cu == units - 1) fa.clear(), fb.clear();
+            if (j0 == 0) one(0);
+            if (j0 + n == kStep) one(1);
         }
-        float c[NT][4];
-        if (__any_sync(0xFFFFFFFFu, fa.two_steps() || fb.two_steps())) unit<FMT, NT, true>(qa, qb, fa, fb, xs, c);
-        else unit<FMT, NT, false>(qa, qb, fa, fb, xs, c);
-        if (i + kDepth < last) copy();
-        copies_commit();
-#pragma unroll
-        for (int q = 0; q < NT; ++q) {
-            xs[q] += 256;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[q][j] += c[q][j];
-        }
-        ++cu;
-        chunk = (cu & (kChunk - 1)) == 0;
-        if (cu == units || i + 1 == last) {
+        if (++slot == kRing) slot = 0;
+        __syncwarp();  // every lane has read the scales
+        copy();        // into the slot that was just read
+        i += n, cu += n;
+        if (cu == units || i == last) {
             if (CS == 1 && whole && cu == units) {
-                const int n = (tile0 + ct) * kTileN + g;
+                const int row = (tile0 + ct) * kTileN + g;
 #pragma unroll
                 for (int q = 0; q < NT; ++q)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int m = q * 8 + t * 2 + (j & 1);
-                        if (m < a.M && n + (j >> 1) * 8 < a.N) store_out(a, m, n + (j >> 1) * 8, acc[q][j]);
+                        if (m < a.M && row + (j >> 1) * 8 < a.N) store_out(a, m, row + (j >> 1) * 8, acc[q][j] * Scale<FMT>::kBack);
                     }
             } else {
-                float* out = part + (size_t)(CS > 1 ? ct + warp : warp * 2 + (i - cu + 1 > first ? 1 : 0)) * kSlot;
+                float* out = part + (size_t)(CS > 1 ? ct + warp : warp * 2 + (i - cu > first ? 1 : 0)) * kSlot;
 #pragma unroll
                 for (int q = 0; q < NT; ++q) {
                     *reinterpret_cast<float2*>(out + g * (8 * NT) + q * 8 + t * 2) = make_float2(acc[q][0], acc[q][1]);
@@ -364,12 +370,11 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
                 }
             }
 #pragma unroll
-            for (int q = 0; q < NT; ++q) {
-                xs[q] -= units * 256;
+            for (int q = 0; q < NT; ++q)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[q][j] = 0.0f;
-            }
-            cu = 0, ++ct, whole = true, chunk = true;
+            cu = 0, ++ct, whole = true;
+            tile_sides();
         }
     }
 
@@ -398,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
                     const int f = total * w / kWarps, l = total * (w + 1) / kWarps;
                     if (f < l) s += src[(w * 2 + (f < u0 ? 1 : 0)) * kSlot + m];
                 }
-                store_out(a, m, tile0 * kTileN + r, s);
+                store_out(a, m, tile0 * kTileN + r, s * Scale<FMT>::kBack);
             }
         } else {
             const float* slot = part + (size_t)tile * kSlot + (r % kTileN) * (8 * NT);
@@ -418,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
                         s += v;
                     }
                 }
-                store_out(a, m, tile0 * kTileN + r, s);
+                store_out(a, m, tile0 * kTileN + r, s * Scale<FMT>::kBack);
             }
         }
     }
