@@ -9,14 +9,29 @@
 //   log_sum = log1p(s),   entropy = log1p(s) - t / (T (1 + s)),
 // so a log-probability or an entropy near 0 keeps its digits.  The backward pass takes peak and log_sum, not their sum:
 // in a row of very low values the sum would lose log_sum altogether.
+//
+// Forward: one pass over the logits.  A row belongs to a cluster of 1 to 8 CTAs (as many as it takes to fill the device), each
+// with a contiguous slice.  The lanes of a warp share the running maximum, so rescaling is rare; per element that leaves a
+// subtraction, a multiplication, the exponential and two additions.  It is bound by HBM, with the exponentials (16 per clock and
+// SM) at 0.7 of their rate beside it.
+//
+// Top alternatives: every lane remembers its largest logit.  The k-th largest of these is a lower bound of the k-th largest
+// logit, and only the k lanes that reach it can hold anything above it: their elements (a few per cent of the slice) are read
+// again, and the few dozen that pass are ranked.  All comparisons are on (value, lower index) keys, so ties need no care.
 #include "row_common.cuh"
+
+#include <algorithm>
 
 namespace resq {
 namespace {
 
-constexpr int kLpThreads = 256;
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLowest = -3.4028234663852886e38f;  // differences are cut here: 0 * -inf is no term of a sum
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxLpThreads = 1024;
+constexpr int kGroup = 16;        // elements per lane and iteration: two vectors of 8
+constexpr int kMaxCluster = 8;
+constexpr int kCandidates = 1024;  // logits that may pass the bound before the selection falls back to repeated passes
 
 struct LpArgs {
     const void* x;
@@ -29,47 +44,62 @@ struct LpArgs {
     int32_t* top_ids;
     float* top_logp;
     int V, top;
+    int slice;    // vectors of 8 per CTA of a cluster
     float inv_t;  // 1 / T
 };
 
-// Running sums of a set of logits: m its largest value (-inf: the set has no finite term), s the sum of exp((x - m) / T)
-// without one term of value 1, t the sum of exp((x - m) / T) (x - m).
+// Sums of a set of logits: m its largest value (-inf: the set has no finite term), s the sum of exp((x - m) / T) without one
+// term of value 1, t the sum of exp((x - m) / T) (x - m).
 struct Stat {
     float m, s, t;
 };
-__device__ __forceinline__ void stat_add(Stat& a, float x, float c) {
-    if (x == -kInf) return;
-    if (x > a.m) {
-        if (a.m != -kInf) {
-            const float d = fmaxf(a.m - x, kLowest), f = exp2f(d * c);
-            a.t = f * (a.t + d * (a.s + 1.0f));
-            a.s = (a.s + 1.0f) * f;
-        }
-        a.m = x;
-    } else {
-        const float d = fmaxf(x - a.m, kLowest), e = exp2f(d * c);
-        a.s += e;
-        a.t = fmaf(e, d, a.t);
-    }
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float warp_max(float v) {  // NaN is passed over
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
 }
 __device__ __forceinline__ Stat stat_join(const Stat& p, const Stat& q, float c) {
     const bool p_first = p.m >= q.m;
     Stat a = p_first ? p : q;
     const Stat& b = p_first ? q : p;
-    if (b.m == -kInf) return a.m != -kInf ? a : Stat{a.m, p.s + q.s, 0.0f};
-    const float d = fmaxf(b.m - a.m, kLowest), f = exp2f(d * c);
+    if (b.m == -kInf) {
+        a.s += b.s;  // nothing, or the NaN of its logits
+        return a;
+    }
+    const float d = max_nan(b.m - a.m, kLowest), f = ex2(d * c);
     a.s += f * (b.s + 1.0f);
-    a.t += f * (b.t + d * (b.s + 1.0f));
+    a.t += f * b.t + (f * d) * (b.s + 1.0f);
     return a;
 }
 
 __device__ __forceinline__ float load_logit(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float load_logit(const float* p) { return *p; }
 
+// Eight logits of a row from element k on; -inf behind its end.
+template <typename T>
+__device__ __forceinline__ void get_logits(const Raw8<T>& r, int n, float (&v)[8]) {
+    r.get(v);
+    if (n < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i >= n) v[i] = -kInf;
+    }
+}
+
 // Orders logits by value (NaN above +inf, -0 equal to 0), equal values by lower index first.
 __device__ __forceinline__ uint64_t top_key(float x, int j) {
     uint32_t u;
-    if (x != x) u = 0xFFFFFFFFu;
+    if (x != x) u = 0xFFFFFFFEu;  // below the key that stands for no bound
     else {
         const uint32_t b = __float_as_uint(x + 0.0f);
         u = (b & 0x80000000u) ? ~b : b | 0x80000000u;
@@ -77,70 +107,267 @@ __device__ __forceinline__ uint64_t top_key(float x, int j) {
     return ((uint64_t)u << 32) | (uint32_t)~j;
 }
 
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t remote_addr(const void* p, int rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float remote_f32(const float* p, int rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote_addr(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint64_t remote_u64(const uint64_t* p, int rank) {
+    uint64_t v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(remote_addr(p, rank)) : "memory");
+    return v;
+}
+
+// The block's largest key below `last` among vectors v0 .. v1 - 1 of the row, the same in every thread.
 template <typename T>
-__global__ void __launch_bounds__(kLpThreads) logprobs_kernel(const __grid_constant__ LpArgs a) {
-    __shared__ Stat st[kLpThreads / 32];
-    __shared__ uint64_t best[2][kLpThreads / 32];
+__device__ uint64_t next_key(const T* x, int V, int v0, int v1, uint64_t last, uint64_t* buf) {
+    uint64_t b = 0;
+    for (int j = v0 * 8 + threadIdx.x; j < min(v1 * 8, V); j += blockDim.x) {
+        const uint64_t key = top_key(load_logit(x + j), j);
+        if (key < last && key > b) b = key;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const uint64_t q = __shfl_xor_sync(~0u, b, o);
+        b = q > b ? q : b;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = b;
+    __syncthreads();
+    for (int i = 0; i < (int)((blockDim.x + 31) >> 5); ++i) b = buf[i] > b ? buf[i] : b;
+    return b;
+}
+
+// Keys in descending order: those of rank < k go to out[rank].  All keys differ.
+__device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int k, uint64_t* out) {
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const uint64_t mine = keys[i];
+        int r = 0;
+        for (int j = 0; j < n; ++j) r += keys[j] > mine;
+        if (r < k) out[r] = mine;
+    }
+}
+
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kMaxLpThreads) logprobs_kernel(const __grid_constant__ LpArgs a) {
+    __shared__ Stat warp_stat[kMaxLpThreads / 32], cta_stat;
+    __shared__ uint64_t cand[TOP ? kCandidates : 1], best[TOP ? RESQ_MAX_TOP : 1], hot_key[TOP ? 32 : 1];
+    __shared__ uint16_t hot[TOP ? kMaxLpThreads : 1];
+    __shared__ int count[2];
+    uint32_t cs;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(cs));
+    const int rank = cs > 1 ? (int)cluster_rank() : 0;
     pdl_wait();
     pdl_trigger();
-    const int64_t m = blockIdx.x;
-    const T* x = static_cast<const T*>(a.x) + m * a.ld;
-    const float c = a.inv_t * 1.4426950408889634f;
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    Stat s{-kInf, 0.0f, 0.0f};
-    bool bad = false;
-    for (int j = threadIdx.x; j < a.V; j += kLpThreads) {
-        const float v = load_logit(x + j);
-        bad |= !(v < kInf);
-        stat_add(s, v, c);
-    }
-    bad = __syncthreads_or(bad);
+    const int64_t m = blockIdx.x / cs;
+    const T* const x = static_cast<const T*>(a.x) + m * a.ld;
+    const float c = a.inv_t * kLog2e;
+    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, w = tid >> 5, warps = threads >> 5;
+    const int v0 = min(rank * a.slice, (a.V + 7) / 8), v1 = min(v0 + a.slice, (a.V + 7) / 8);
+
+    // ---- one pass
+    float ms = -kInf, s = 0.0f, t = 0.0f;  // the warp's maximum; the lane's sums relative to it
+    bool one = false;                      // the lane holds the maximum's own term, which s leaves out
+    float lane_max = -kInf;
+    int lane_it = 0;
+    Raw8<T> raw[2];
+    auto fetch = [&](int v) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s = stat_join(s, Stat{__shfl_xor_sync(~0u, s.m, o), __shfl_xor_sync(~0u, s.s, o), __shfl_xor_sync(~0u, s.t, o)}, c);
-    if (lane == 0) st[w] = s;
-    __syncthreads();
-    s = st[0];
-    for (int i = 1; i < kLpThreads / 32; ++i) s = stat_join(s, st[i], c);
-    const float log_s = bad ? __int_as_float(0x7FC00000) : log1pf(s.s);
-    const bool empty = s.m == -kInf;
-    if (threadIdx.x == 0) {
-        if (a.logp) {
-            const int64_t tok = a.tokens[m];
-            float v = 0.0f;
-            if (tok >= 0 && tok < a.V) {
-                const float xt = load_logit(x + tok);
-                v = bad ? log_s : xt == -kInf ? -kInf : (xt - s.m) * a.inv_t - log_s;
+        for (int h = 0; h < 2; ++h)
+            if (v + h * threads < v1) raw[h].load(x + (int64_t)(v + h * threads) * 8, a.V - (v + h * threads) * 8);
+    };
+    fetch(v0 + tid);
+    // all lanes of a warp make the same number of iterations
+    for (int vw = v0 + w * 32, it = 0; vw < v1; vw += 2 * threads, ++it) {
+        const int v = vw + lane;
+        float y[kGroup];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float z[8];
+            get_logits(raw[h], v + h * threads < v1 ? a.V - (v + h * threads) * 8 : 0, z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[h * 8 + i] = z[i];
+        }
+        fetch(v + 2 * threads);
+        float top = y[0];
+#pragma unroll
+        for (int i = 1; i < kGroup; ++i) top = fmaxf(top, y[i]);
+        if (TOP && (top > lane_max || it == 0)) lane_max = top, lane_it = it;
+        const float all = warp_max(top);
+        if (all > ms) {  // warp-uniform
+            if (ms != -kInf) {
+                const float d = max_nan(ms - all, kLowest), f = ex2(d * c), held = s + (one ? 1.0f : 0.0f);
+                t = f * t + (f * d) * held;  // f * d first: d may be the lowest number
+                s = f * held;
             }
-            a.logp[m] = v;
-        }
-        if (a.entropy) a.entropy[m] = bad ? log_s : empty ? 0.0f : log_s - s.t * a.inv_t / (1.0f + s.s);
-        if (a.peak) a.peak[m] = bad ? log_s : s.m;
-        if (a.log_sum) a.log_sum[m] = log_s;
-    }
-    uint64_t last = ~0ull;
-    for (int r = 0; r < a.top; ++r) {
-        uint64_t b = 0;
-        for (int j = threadIdx.x; j < a.V; j += kLpThreads) {
-            const uint64_t key = top_key(load_logit(x + j), j);
-            if ((r == 0 || key < last) && key > b) b = key;
-        }
+            ms = all;
+            const unsigned who = __ballot_sync(~0u, top == all);
+            one = lane == __ffs(who) - 1;
+            if (one) {  // its own term stays out: taken out of the group
+                bool done = false;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const uint64_t q = __shfl_xor_sync(~0u, b, o);
-            b = q > b ? q : b;
+                for (int i = 0; i < kGroup; ++i) {
+                    const bool hit = !done && y[i] == all;
+                    done |= hit;
+                    if (hit) y[i] = -kInf;
+                }
+            }
         }
-        if (lane == 0) best[r & 1][w] = b;
-        __syncthreads();
-        b = best[r & 1][0];
-        for (int i = 1; i < kLpThreads / 32; ++i) b = best[r & 1][i] > b ? best[r & 1][i] : b;
-        last = b;
-        if (threadIdx.x == 0) {
-            const int j = (int)~(uint32_t)b;
-            const float v = load_logit(x + j);
-            a.top_ids[m * a.top + r] = j;
-            a.top_logp[m * a.top + r] = bad ? log_s : v == -kInf ? -kInf : (v - s.m) * a.inv_t - log_s;
+        const float ref = fmaxf(ms, kLowest);
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+            const float d = max_nan(y[i] - ref, kLowest), e = ex2(d * c);
+            s += e;
+            t = fmaf(e, d, t);
         }
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o), t += __shfl_xor_sync(~0u, t, o);
+    if (lane == 0) warp_stat[w] = Stat{ms, s, t};
+    if (TOP && tid < 2) count[tid] = 0;
+    __syncthreads();
+    if (w == 0) {
+        Stat q = lane < warps ? warp_stat[lane] : Stat{-kInf, 0.0f, 0.0f};
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            q = stat_join(q, Stat{__shfl_xor_sync(~0u, q.m, o), __shfl_xor_sync(~0u, q.s, o), __shfl_xor_sync(~0u, q.t, o)}, c);
+        if (lane == 0) cta_stat = q;
+    }
+    __syncthreads();
+
+    // ---- this slice's largest keys, in order, into best[]
+    const int have = min(a.V - v0 * 8, (v1 - v0) * 8), k = TOP ? max(0, min(a.top, have)) : 0;
+    if (TOP) {
+        const Stat q = cta_stat;
+        const bool strange = q.m == kInf || q.s != q.s;  // +inf or NaN: by repeated passes, which order them too
+        int found = kCandidates + 1;
+        if (!strange) {
+            // the lane's largest key: the first element of that iteration with the lane's largest value
+            uint64_t key = 0;
+            if (v0 + tid < v1) {
+#pragma unroll
+                for (int h = 1; h >= 0; --h) {
+                    const int v = v0 + (lane_it * 2 + h) * threads + tid;
+                    if (v >= v1) continue;
+                    Raw8<T> r;
+                    float z[8];
+                    r.load(x + (int64_t)v * 8, a.V - v * 8);
+                    get_logits(r, a.V - v * 8, z);
+#pragma unroll
+                    for (int i = 7; i >= 0; --i)
+                        if (z[i] == lane_max) key = top_key(z[i], v * 8 + i);
+                }
+            }
+            // k-th largest lane key by bisection: first the values, then, where equal values leave too many, the places
+            uint64_t bound = 0;
+            int n = threads;
+            for (int bit = 63; bit >= 0 && n != k; --bit) {
+                if (bit == 31 && n <= 2 * RESQ_MAX_TOP) break;  // equal values among the last: few enough
+                if (sizeof(T) == 2 && bit < 48 && bit >= 32) {   // bf16 values end at bit 48 (all ones below in negative ones)
+                    bit = 32;
+                    continue;
+                }
+                const uint64_t trial = bound | (1ull << bit);
+                const int reach = __syncthreads_count(key >= trial);
+                if (reach >= k) bound = trial, n = reach;
+            }
+            if (key != 0 && key >= bound) hot[atomicAdd(&count[0], 1)] = (uint16_t)tid;
+            __syncthreads();
+            // their elements again
+            const int lanes = count[0], per = (v1 - v0 + threads - 1) / threads;
+            for (int i = tid; i < lanes * per; i += threads) {
+                const int v = v0 + (i % per) * threads + hot[i / per];
+                if (v >= v1) continue;
+                Raw8<T> r;
+                float z[8];
+                r.load(x + (int64_t)v * 8, a.V - v * 8);
+                get_logits(r, a.V - v * 8, z);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint64_t q8 = top_key(z[e], v * 8 + e);
+                    if (v * 8 + e < a.V && q8 >= bound) {
+                        const int at = atomicAdd(&count[1], 1);
+                        if (at < kCandidates) cand[at] = q8;
+                    }
+                }
+            }
+            __syncthreads();
+            found = count[1];
+        }
+        if (found <= kCandidates) {
+            rank_keys(cand, found, k, best);
+        } else {
+            uint64_t last = ~0ull;
+            for (int r = 0; r < k; ++r) {
+                last = next_key(x, a.V, v0, v1, last, hot_key);
+                if (tid == 0) best[r] = last;
+            }
+        }
+        if (tid < RESQ_MAX_TOP && tid >= k) best[tid] = 0;
+    }
+
+    // ---- the row's values
+    if (cs > 1) cluster_sync();
+    if (rank == 0) {
+        Stat q = cta_stat;
+        for (int r = 1; r < (int)cs; ++r)
+            q = stat_join(q, Stat{remote_f32(&cta_stat.m, r), remote_f32(&cta_stat.s, r), remote_f32(&cta_stat.t, r)}, c);
+        const bool bad = q.m == kInf || q.s != q.s, empty = q.m == -kInf;
+        const float nan = __int_as_float(0x7FC00000), log_s = bad ? nan : log1pf(q.s);
+        if (tid == 0) {
+            if (a.logp) {
+                const int64_t tok = a.tokens[m];
+                float v = 0.0f;
+                if (tok >= 0 && tok < a.V) {
+                    const float xt = load_logit(x + tok);
+                    v = bad ? nan : xt == -kInf ? -kInf : (xt - q.m) * a.inv_t - log_s;
+                }
+                a.logp[m] = v;
+            }
+            if (a.entropy) a.entropy[m] = bad ? nan : empty ? 0.0f : log_s - q.t * a.inv_t / (1.0f + q.s);
+            if (a.peak) a.peak[m] = bad ? nan : q.m;
+            if (a.log_sum) a.log_sum[m] = log_s;
+        }
+        if (TOP) {
+            __syncthreads();
+            if (cs > 1) {  // the slices' best together
+                for (int i = tid; i < (int)cs * RESQ_MAX_TOP; i += threads) cand[i] = remote_u64(&best[i % RESQ_MAX_TOP], i / RESQ_MAX_TOP);
+                __syncthreads();
+                // slots behind a slice's own count are 0 and rank behind every key
+                for (int i = tid; i < (int)cs * RESQ_MAX_TOP; i += threads) {
+                    const uint64_t mine = cand[i];
+                    int r = 0;
+                    for (int j = 0; j < (int)cs * RESQ_MAX_TOP; ++j) r += cand[j] > mine;
+                    if (mine != 0 && r < a.top) {
+                        const int j = (int)~(uint32_t)mine;
+                        const float v = load_logit(x + j);
+                        a.top_ids[m * a.top + r] = j;
+                        a.top_logp[m * a.top + r] = bad ? nan : v == -kInf ? -kInf : (v - q.m) * a.inv_t - log_s;
+                    }
+                }
+            } else if (tid < a.top) {
+                const int j = (int)~(uint32_t)best[tid];
+                const float v = load_logit(x + j);
+                a.top_ids[m * a.top + tid] = j;
+                a.top_logp[m * a.top + tid] = bad ? nan : v == -kInf ? -kInf : (v - q.m) * a.inv_t - log_s;
+            }
+        }
+    }
+    if (cs > 1) cluster_sync();  // no CTA leaves while rank 0 may still read its shared memory
 }
 
 struct LpBwdArgs {
@@ -159,33 +386,56 @@ struct LpBwdArgs {
     unsigned chunks;  // blocks per row
 };
 
-// dx_j = (1 / T) [dlogp (1[j = tok] - p_j) - dentropy p_j (log p_j + entropy)].  At the token itself 1 - p comes from the
-// forward call's logp (-expm1), which keeps its digits when p is near 1.
+// dx_j = (1 / T) [dlogp (1[j = tok] - p_j) - dentropy p_j (log p_j + entropy)] = -p_j (A + B log2 p_j) but for the token itself,
+// where 1 - p comes from the forward call's logp (-expm1), which keeps its digits when p is near 1.  One read and one write of
+// the row: HBM-bound.
+constexpr int kBwdThreads = 256, kBwdVecs = 4;
 template <typename T>
-__global__ void __launch_bounds__(kLpThreads) logprobs_bwd_kernel(const __grid_constant__ LpBwdArgs a) {
+__global__ void __launch_bounds__(kBwdThreads) logprobs_bwd_kernel(const __grid_constant__ LpBwdArgs a) {
     pdl_wait();
     pdl_trigger();
     const int64_t m = blockIdx.x / a.chunks;
-    const int k = (int)((blockIdx.x % a.chunks) * kLpThreads + threadIdx.x) * 8, n = a.V - k;
-    if (n <= 0) return;
-    const float peak = a.peak[m], log_sum = a.log_sum[m], H = a.dentropy ? a.entropy[m] : 0.0f, de = a.dentropy ? a.dentropy[m] * a.inv_t : 0.0f;
+    const int base = (int)(blockIdx.x % a.chunks) * (kBwdThreads * kBwdVecs * 8) + threadIdx.x * 8;
+    Raw8<T> r[kBwdVecs];
+#pragma unroll
+    for (int h = 0; h < kBwdVecs; ++h) {
+        const int k = base + h * kBwdThreads * 8;
+        if (k < a.V) r[h].load(static_cast<const T*>(a.x) + m * a.ld + k, a.V - k);
+    }
+    const float peak = a.peak[m], log_sum = a.log_sum[m];
+    const float H = a.dentropy ? a.entropy[m] : 0.0f, de = a.dentropy ? a.dentropy[m] * a.inv_t : 0.0f;
     const int64_t tok = a.tokens[m];
     const bool there = tok >= 0 && tok < a.V;
     const float dl = there ? a.dlogp[m] * a.inv_t : 0.0f;
-    Raw8<T> r;
-    float v[8];
-    r.load(static_cast<const T*>(a.x) + m * a.ld + k, n);
-    r.get(v);
+    const float c = a.inv_t * kLog2e, shift = -log_sum * kLog2e, A = -(dl + H * de), B = -de * 0.6931471805599453f;
+    const bool empty = peak == -kInf;
+    const float ref = empty ? 0.0f : peak;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const bool hot = there && k + i == tok;
-        const float z = hot ? a.logp[m] : fmaf(v[i] - peak, a.inv_t, -log_sum);
-        const float p = exp2f(z * 1.4426950408889634f);
-        float g = hot ? -expm1f(z) * dl : -p * dl;
-        if (a.dentropy && p != 0.0f) g -= p * (z + H) * de;
-        v[i] = peak == -kInf ? 0.0f : g;
+    for (int h = 0; h < kBwdVecs; ++h) {
+        const int k = base + h * kBwdThreads * 8, n = a.V - k;
+        if (n <= 0) continue;
+        float v[8];
+        r[h].get(v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float z = max_nan(fmaf(v[i] - ref, c, shift), -1e5f);  // log2 p; 2^-1e5 is 0
+            v[i] = ex2(z) * fmaf(B, z, A);
+        }
+        if (there && tok >= k && tok < k + 8) {
+            const float z = a.logp[m];
+            float g = -expm1f(z) * dl;
+            const float p = expf(z);
+            if (p != 0.0f) g -= p * (z + H) * de;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i == tok) v[i] = g;
+        }
+        if (empty) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        }
+        store8(static_cast<T*>(a.dx) + m * a.ldd + k, v, n);
     }
-    store8(static_cast<T*>(a.dx) + m * a.ldd + k, v, n);
 }
 
 int check_logits(const char* what, const void* x, int dtype, int64_t M, int64_t V, int64_t ld, float temperature) {
@@ -221,11 +471,22 @@ int resq_token_logprobs(const void* logits, int dtype, int64_t M, int64_t V, int
     if (!is_aligned(tokens, 8) || !is_aligned(logp, 4) || !is_aligned(entropy, 4) || !is_aligned(peak, 4) || !is_aligned(log_sum, 4) || !is_aligned(top_ids, 4) ||
         !is_aligned(top_logp, 4))
         return fail(RESQ_ERR_ALIGN, what, "tokens must be 8-byte aligned, the outputs 4-byte aligned");
-    LpArgs a{logits, ld, tokens, logp, entropy, peak, log_sum, top_ids, top_logp, (int)V, top, 1.0f / temperature};
+    // Slices until the device has four CTAs of 256 threads per SM, of at least 512 vectors; with fewer CTAs than SMs they
+    // are made larger instead, so that a lane has one group of its own to read.
+    const int64_t vecs = (V + 7) / 8;
+    int cs = 1;
+    while (cs < kMaxCluster && M * cs < 4 * 148 && vecs / (2 * cs) >= 512) cs *= 2;
+    const int64_t slice = (vecs + cs - 1) / cs;
+    const int64_t most = M * cs <= 148 ? kMaxLpThreads : 256;
+    const unsigned threads = (unsigned)std::min<int64_t>(most, ((slice + 1) / 2 + 31) / 32 * 32);
+    if (M * cs > INT32_MAX) return fail(RESQ_ERR_SHAPE, what, "too many rows for one call");
+    LpArgs a{logits, ld, tokens, logp, entropy, peak, log_sum, top_ids, top_logp, (int)V, top, (int)slice, 1.0f / temperature};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    using bf = __nv_bfloat16;
+    auto kern = dtype == RESQ_OUT_F32 ? (top ? logprobs_kernel<float, true> : logprobs_kernel<float, false>)
+                                      : (top ? logprobs_kernel<bf, true> : logprobs_kernel<bf, false>);
     LaunchScope scope(kKindRow, st);
-    auto kern = dtype == RESQ_OUT_F32 ? logprobs_kernel<float> : logprobs_kernel<__nv_bfloat16>;
-    return cuda_fail(launch_kernel(kern, dim3((unsigned)M), dim3(kLpThreads), 0, st, a), "logprobs_kernel launch");
+    return cuda_fail(launch_clusters(kern, (unsigned)(M * cs), threads, 0, cs, st, a), "logprobs_kernel launch");
 }
 
 int resq_token_logprobs_backward(const void* logits, int dtype, int64_t M, int64_t V, int64_t ld, const int64_t* tokens, float temperature,
@@ -241,13 +502,13 @@ int resq_token_logprobs_backward(const void* logits, int dtype, int64_t M, int64
         !is_aligned(dlogp, 4) ||
         !is_aligned(dentropy, 4))
         return fail(RESQ_ERR_ALIGN, what, "tokens must be 8-byte aligned, the row values 4-byte aligned");
-    const int64_t chunks = (V + kLpThreads * 8 - 1) / (kLpThreads * 8);
+    const int64_t chunks = (V + kBwdThreads * kBwdVecs * 8 - 1) / (kBwdThreads * kBwdVecs * 8);
     if (M * chunks > INT32_MAX) return fail(RESQ_ERR_SHAPE, what, "M x V is too large for one call");
     LpBwdArgs a{logits, dlogits, ld, ldd, tokens, logp, peak, log_sum, entropy, dlogp, dentropy, (int)V, 1.0f / temperature, (unsigned)chunks};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     LaunchScope scope(kKindRow, st);
     auto kern = dtype == RESQ_OUT_F32 ? logprobs_bwd_kernel<float> : logprobs_bwd_kernel<__nv_bfloat16>;
-    return cuda_fail(launch_kernel(kern, dim3((unsigned)(M * chunks)), dim3(kLpThreads), 0, st, a),
+    return cuda_fail(launch_kernel(kern, dim3((unsigned)(M * chunks)), dim3(kBwdThreads), 0, st, a),
                      "logprobs_bwd_kernel launch");
 }
 }

@@ -408,31 +408,54 @@ def test_logprobs_ties_go_to_the_lowest_id(V, dtype):
 @pytest.mark.parametrize("V", [50, 5000, 60001])
 def test_logprobs_masked_rows(V, dtype):
     g = gen(V + 1)
-    x = randn(6, V, dtype, g, 3.0)
+    x = randn(7, V, dtype, g, 3.0)
     inf = float("inf")
+    x[6] = torch.where(torch.rand(V, generator=g, device="cuda") < 0.9, torch.finfo(dtype).min, x[6].float()).to(dtype)
+    x[6, 7] = 1.0
     x[1] = torch.where(torch.rand(V, generator=g, device="cuda") < 0.9, -inf, x[1].float()).to(dtype)
     x[1, 3] = 0.5
     x[2] = -inf
     x[2, V - 1] = -4.0                       # one place left
     x[3] = -inf                              # none left
     x[4] = torch.finfo(dtype).min            # the lowest value is a value
-    tok = torch.tensor([0, 3, 0, 1, 5, -7], device="cuda")
+    tok = torch.tensor([0, 3, 0, 1, 5, -7, 7], device="cuda")
     m = rq()
     got = m.token_logprobs(x, tok, top=32)
-    live = [0, 1, 2, 4, 5]
-    check_logprobs(x[live].contiguous() if V % 8 == 0 else randn(5, V, dtype, g).copy_(x[live]), tok[live], 1.0, 1)
+    live = [0, 1, 2, 4, 5, 6]
+    for top in (1, 20):
+        check_logprobs(randn(6, V, dtype, g).copy_(x[live]), tok[live], 1.0, top)
     assert got["logp"][2] == -inf and got["entropy"][2] == 0 and got["peak"][2] == -4 and got["log_sum"][2] == 0
     assert got["top_ids"][2].tolist() == [V - 1] + list(range(31)) and got["top_logp"][2, 0] == 0 and (got["top_logp"][2, 1:] == -inf).all()
     assert got["logp"][3] == -inf and got["entropy"][3] == 0 and got["peak"][3] == -inf and got["log_sum"][3] == 0
     assert got["top_ids"][3].tolist() == list(range(32)) and (got["top_logp"][3] == -inf).all()
     assert got["logp"][5] == 0               # no token named
-    one = torch.ones(6, device="cuda")
+    one = torch.ones(7, device="cuda")
     d = m.token_logprobs_backward(x, tok, got["logp"], got["peak"], got["log_sum"], got["entropy"], one, one)
     assert d.isfinite().all() and not d[3].any() and not d[1][x[1] == -inf].any()
     # a row of the type's lowest value: every p is 1 / V, and log p + entropy = 0 to (8 + 4 log V + V / 256 + 64) u
     flat = torch.full((V,), -1.0 / V, dtype=F64, device="cuda")
     flat[5] += 1
     close(d[4], flat, (HALF[dtype] + U * (100 + V / 128)) * flat.abs() + U * (100 + V / 128) / V, "lowest")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_logprobs_best_in_few_lanes(dtype):
+    """The largest logits where a division of the row into strides puts them together: more of them than the selection keeps
+    at hand, and whole groups of neighbours; with NaN and +inf among the logits their order is defined too."""
+    m, g = rq(), gen(77)
+    V = 160000
+    for stride in (8 * 256, 8 * 1024, 8 * 32, 16 * 256, 1):
+        x = randn(3, V, dtype, g, 1.0)
+        at = (torch.arange(0, 2000, device="cuda")[:, None] * stride + torch.arange(8, device="cuda")).flatten() % V
+        x[0, at] = (20 + torch.rand(at.numel(), generator=g, device="cuda")).to(dtype)
+        x[1, at] = 20
+        x[2] = torch.arange(V, device="cuda").to(dtype)
+        check_logprobs(x, torch.tensor([5, 6, 7], device="cuda"), 1.0, 32)
+    x = randn(2, 5000, dtype, g, 1.0)
+    x[0, 0] = x[0, 4999] = x[1, 3] = float("nan")
+    x[0, 9] = x[1, 2] = float("inf")
+    ids = m.token_logprobs(x, torch.zeros(2, dtype=torch.int64, device="cuda"), top=3)["top_ids"].tolist()
+    assert ids[0] == [0, 4999, 9] and ids[1][:2] == [3, 2]
 
 
 def test_logprobs_infinity_and_nan_spoil_their_row_only():
