@@ -16,8 +16,8 @@
 // SM) at 0.7 of their rate beside it.
 //
 // Top alternatives: every lane remembers its largest logit.  The k-th largest of these is a lower bound of the k-th largest
-// logit, and only the k lanes that reach it can hold anything above it: their elements (a few per cent of the slice) are read
-// again, and the few dozen that pass are ranked.  All comparisons are on (value, lower index) keys, so ties need no care.
+// logit, and only the lanes that reach it can hold anything above it: their elements (a few per cent of the slice) are read
+// again, and the few dozen that pass are ranked.  Bounds and ranks are on (value, lower index) keys, so ties need no care.
 #include "row_common.cuh"
 
 #include <algorithm>
@@ -28,10 +28,12 @@ namespace {
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLowest = -3.4028234663852886e38f;  // differences are cut here: 0 * -inf is no term of a sum
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kMaxLpThreads = 1024;
-constexpr int kGroup = 16;        // elements per lane and iteration: two vectors of 8
+constexpr int kMaxLpThreads = 512;
+constexpr int kV = 2, kGroup = 8 * kV;  // vectors of 8 per lane and iteration (four need 96 registers: 2 instead of 4 CTAs per SM)
+constexpr int kBuckets = 64;            // sets of lanes whose largest logits bound the k-th largest
 constexpr int kMaxCluster = 8;
-constexpr int kCandidates = 1024;  // logits that may pass the bound before the selection falls back to repeated passes
+constexpr int kCandidates = 2048;  // logits that may pass the bound before the selection falls back to repeated passes
+static_assert(kCandidates >= kMaxLpThreads / kBuckets * RESQ_MAX_TOP * 8, "a row of equal logits");
 
 struct LpArgs {
     const void* x;
@@ -61,6 +63,33 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {  // NaN is passed over
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// Pairs of fp32 values in one instruction.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
 __device__ __forceinline__ float warp_max(float v) {  // NaN is passed over
@@ -165,7 +194,8 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int k, ui
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kMaxLpThreads) logprobs_kernel(const __grid_constant__ LpArgs a) {
     __shared__ Stat warp_stat[kMaxLpThreads / 32], cta_stat;
-    __shared__ uint64_t cand[TOP ? kCandidates : 1], best[TOP ? RESQ_MAX_TOP : 1], hot_key[TOP ? 32 : 1];
+    __shared__ uint64_t cand[TOP ? kCandidates : 1], best[TOP ? RESQ_MAX_TOP : 1];
+    __shared__ __align__(16) uint32_t bucket_order[kBuckets];
     __shared__ uint16_t hot[TOP ? kMaxLpThreads : 1];
     __shared__ int count[2];
     uint32_t cs;
@@ -179,61 +209,124 @@ __global__ void __launch_bounds__(kMaxLpThreads) logprobs_kernel(const __grid_co
     const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, w = tid >> 5, warps = threads >> 5;
     const int v0 = min(rank * a.slice, (a.V + 7) / 8), v1 = min(v0 + a.slice, (a.V + 7) / 8);
 
+    float x_tok = 0.0f;  // thread 0 of the row: asked for before the pass, needed behind it
+    bool named = false;
+    if (a.logp && tid == 0 && rank == 0) {
+        const int64_t tok = a.tokens[m];
+        named = tok >= 0 && tok < a.V;
+        if (named) x_tok = load_logit(x + tok);
+    }
+
     // ---- one pass
-    float ms = -kInf, s = 0.0f, t = 0.0f;  // the warp's maximum; the lane's sums relative to it
-    bool one = false;                      // the lane holds the maximum's own term, which s leaves out
+    float ms = -kInf;                  // the warp's maximum
+    uint64_t s2 = 0, t2 = 0;           // the lane's sums relative to it, in two halves (bits of 0.0f, 0.0f)
+    bool one = false;                  // the lane holds the maximum's own term, which s leaves out
+    bool cut = false;                  // the warp has met a difference of -inf: differences are cut at the lowest number
     float lane_max = -kInf;
     int lane_it = 0;
-    Raw8<T> raw[2];
-    auto fetch = [&](int v) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (v + h * threads < v1) raw[h].load(x + (int64_t)(v + h * threads) * 8, a.V - (v + h * threads) * 8);
-    };
-    fetch(v0 + tid);
-    // all lanes of a warp make the same number of iterations
-    for (int vw = v0 + w * 32, it = 0; vw < v1; vw += 2 * threads, ++it) {
-        const int v = vw + lane;
-        float y[kGroup];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float z[8];
-            get_logits(raw[h], v + h * threads < v1 ? a.V - (v + h * threads) * 8 : 0, z);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[h * 8 + i] = z[i];
-        }
-        fetch(v + 2 * threads);
+    auto take = [&](float (&y)[kGroup], int it) {
         float top = y[0];
 #pragma unroll
-        for (int i = 1; i < kGroup; ++i) top = fmaxf(top, y[i]);
+        for (int i = 1; i + 1 < kGroup; i += 2) top = max3(top, y[i], y[i + 1]);
+        top = fmaxf(top, y[kGroup - 1]);
         if (TOP && (top > lane_max || it == 0)) lane_max = top, lane_it = it;
         const float all = warp_max(top);
         if (all > ms) {  // warp-uniform
             if (ms != -kInf) {
-                const float d = max_nan(ms - all, kLowest), f = ex2(d * c), held = s + (one ? 1.0f : 0.0f);
-                t = f * t + (f * d) * held;  // f * d first: d may be the lowest number
-                s = f * held;
+                const float d = max_nan(ms - all, kLowest), f = ex2(d * c);
+                float sl, sh, tl, th;
+                unpair(s2, sl, sh), unpair(t2, tl, th);
+                const float held = sl + sh + (one ? 1.0f : 0.0f);
+                t2 = pair(f * (tl + th) + (f * d) * held, 0.0f);  // f * d first: d may be the lowest number
+                s2 = pair(f * held, 0.0f);
             }
             ms = all;
             const unsigned who = __ballot_sync(~0u, top == all);
             one = lane == __ffs(who) - 1;
-            if (one) {  // its own term stays out: taken out of the group
+            if (one) {  // its own term stays out: that element becomes one whose term is 0
+                const float none = fabsf(all) < 1e29f ? -1e30f : all > 0.0f ? 0.0f : -kInf;
                 bool done = false;
 #pragma unroll
                 for (int i = 0; i < kGroup; ++i) {
                     const bool hit = !done && y[i] == all;
                     done |= hit;
-                    if (hit) y[i] = -kInf;
+                    if (hit) y[i] = none;
                 }
             }
         }
         const float ref = fmaxf(ms, kLowest);
+        const uint64_t ref2 = pair(-ref, -ref), c2 = pair(c, c);
+        uint64_t gs = 0, gt = 0;
+        // 0 * -inf (a masked logit) shows as NaN in gt: then the group is done again with its differences cut, and so are the
+        // warp's later ones
+        if (!cut) {
 #pragma unroll
-        for (int i = 0; i < kGroup; ++i) {
-            const float d = max_nan(y[i] - ref, kLowest), e = ex2(d * c);
-            s += e;
-            t = fmaf(e, d, t);
+            for (int i = 0; i < kGroup; i += 2) {
+                const uint64_t d = add2(pair(y[i], y[i + 1]), ref2), q = mul2(d, c2);
+                float ql, qh;
+                unpair(q, ql, qh);
+                const uint64_t e = pair(ex2(ql), ex2(qh));
+                gs = add2(gs, e);
+                gt = fma2(e, d, gt);
+            }
+            float tl, th;
+            unpair(gt, tl, th);
+            cut = __any_sync(~0u, !(tl + th <= 0.0f));
         }
+        if (cut) {
+            gs = gt = 0;
+#pragma unroll
+            for (int i = 0; i < kGroup; i += 2) {
+                const float dl = max_nan(y[i] - ref, kLowest), dh = max_nan(y[i + 1] - ref, kLowest);
+                const uint64_t e = pair(ex2(dl * c), ex2(dh * c));
+                gs = add2(gs, e);
+                gt = fma2(e, pair(dl, dh), gt);
+            }
+        }
+        s2 = add2(s2, gs), t2 = add2(t2, gt);
+    };
+    // All lanes of a warp make the same number of iterations: first those whose vectors are all whole, the next one's loads
+    // ahead of the sums, then the one or two at the end of the row or slice.
+    const int step = kV * threads, whole = min(v1, a.V / 8) - (v0 + w * 32 + 31 + (kV - 1) * threads);
+    const int its = whole > 0 ? (whole + step - 1) / step : 0;
+    const T* p = x + (int64_t)(v0 + tid) * 8;
+    Raw8<T> raw[kV];
+    auto fetch = [&]() {
+#pragma unroll
+        for (int h = 0; h < kV; ++h) raw[h].load(p + (int64_t)h * threads * 8, 8);
+        p += (int64_t)step * 8;
+    };
+    if (its > 0) fetch();
+    for (int it = 0; it < its; ++it) {
+        float y[kGroup];
+#pragma unroll
+        for (int h = 0; h < kV; ++h) {
+            float z[8];
+            raw[h].get(z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[h * 8 + i] = z[i];
+        }
+        if (it + 1 < its) fetch();
+        take(y, it);
+    }
+    for (int it = its, vw = v0 + w * 32 + its * step; vw < v1; vw += step, ++it) {
+        float y[kGroup];
+#pragma unroll
+        for (int h = 0; h < kV; ++h) {
+            const int v = vw + lane + h * threads, n = v < v1 ? a.V - v * 8 : 0;
+            float z[8];
+            if (n > 0) raw[h].load(x + (int64_t)v * 8, n);
+            get_logits(raw[h], n, z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[h * 8 + i] = z[i];
+        }
+        take(y, it);
+    }
+    float s, t;
+    {
+        float sl, sh, tl, th;
+        unpair(s2, sl, sh), unpair(t2, tl, th);
+        s = sl + sh, t = tl + th;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o), t += __shfl_xor_sync(~0u, t, o);
@@ -255,65 +348,105 @@ __global__ void __launch_bounds__(kMaxLpThreads) logprobs_kernel(const __grid_co
         const Stat q = cta_stat;
         const bool strange = q.m == kInf || q.s != q.s;  // +inf or NaN: by repeated passes, which order them too
         int found = kCandidates + 1;
-        if (!strange) {
-            // the lane's largest key: the first element of that iteration with the lane's largest value
-            uint64_t key = 0;
-            if (v0 + tid < v1) {
+        if (!strange && k > 0) {
+            // Buckets of neighbouring lanes, ranked by their largest value (cut to make room for the bucket's number: any k
+            // buckets give a valid bound).  Leaders of the first k: their exact keys, the smallest of which is the bound.
+            int per_bucket = 1;  // a power of two; 32 to 64 buckets
+            while (threads > kBuckets * per_bucket) per_bucket *= 2;
+            const int buckets = threads / per_bucket;
+            float bmax = lane_max;
+            for (int o = 1; o < per_bucket; o *= 2) bmax = fmaxf(bmax, __shfl_xor_sync(~0u, bmax, o));
+            const unsigned tied = __ballot_sync(~0u, lane_max == bmax) >> (lane & ~(per_bucket - 1));
+            const bool leader = (lane & (per_bucket - 1)) == __ffs(tied & ((2u << (per_bucket - 1)) - 1u)) - 1;
+            const int mine = tid / per_bucket;
+            const uint32_t order = ((uint32_t)(top_key(bmax, 0) >> 32) & ~(uint32_t)(kBuckets - 1)) | (uint32_t)(kBuckets - 1 - mine);
+            if (leader) bucket_order[mine] = order;
+            __syncthreads();
+            int r = kBuckets;
+            if (leader) {
+                r = 0;
+                for (int j = 0; j < buckets; j += 4) {
+                    const uint4 o = *reinterpret_cast<const uint4*>(bucket_order + j);
+                    r += (o.x > order) + (o.y > order) + (o.z > order) + (o.w > order);
+                }
+            }
+            if (r < k) {
+                uint64_t key = 0;  // a lane without elements: no bound
 #pragma unroll
-                for (int h = 1; h >= 0; --h) {
-                    const int v = v0 + (lane_it * 2 + h) * threads + tid;
+                for (int h = kV - 1; h >= 0; --h) {
+                    const int v = v0 + (lane_it * kV + h) * threads + tid;
                     if (v >= v1) continue;
-                    Raw8<T> r;
+                    Raw8<T> g;
                     float z[8];
-                    r.load(x + (int64_t)v * 8, a.V - v * 8);
-                    get_logits(r, a.V - v * 8, z);
+                    g.load(x + (int64_t)v * 8, a.V - v * 8);
+                    get_logits(g, a.V - v * 8, z);
 #pragma unroll
                     for (int i = 7; i >= 0; --i)
                         if (z[i] == lane_max) key = top_key(z[i], v * 8 + i);
                 }
+                best[r] = key;
             }
-            // k-th largest lane key by bisection: first the values, then, where equal values leave too many, the places
-            uint64_t bound = 0;
-            int n = threads;
-            for (int bit = 63; bit >= 0 && n != k; --bit) {
-                if (bit == 31 && n <= 2 * RESQ_MAX_TOP) break;  // equal values among the last: few enough
-                if (sizeof(T) == 2 && bit < 48 && bit >= 32) {   // bf16 values end at bit 48 (all ones below in negative ones)
-                    bit = 32;
-                    continue;
-                }
-                const uint64_t trial = bound | (1ull << bit);
-                const int reach = __syncthreads_count(key >= trial);
-                if (reach >= k) bound = trial, n = reach;
-            }
-            if (key != 0 && key >= bound) hot[atomicAdd(&count[0], 1)] = (uint16_t)tid;
             __syncthreads();
-            // their elements again
-            const int lanes = count[0], per = (v1 - v0 + threads - 1) / threads;
-            for (int i = tid; i < lanes * per; i += threads) {
-                const int v = v0 + (i % per) * threads + hot[i / per];
-                if (v >= v1) continue;
-                Raw8<T> r;
-                float z[8];
-                r.load(x + (int64_t)v * 8, a.V - v * 8);
-                get_logits(r, a.V - v * 8, z);
+            uint64_t low = lane < k ? best[lane] : ~0ull;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint64_t q8 = top_key(z[e], v * 8 + e);
-                    if (v * 8 + e < a.V && q8 >= bound) {
-                        const int at = atomicAdd(&count[1], 1);
-                        if (at < kCandidates) cand[at] = q8;
+            for (int o = 16; o > 0; o >>= 1) {
+                const uint64_t q8 = __shfl_xor_sync(~0u, low, o);
+                low = q8 < low ? q8 : low;
+            }
+            // lanes that may hold keys from the bound on: all their elements again
+            const uint32_t low_u = (uint32_t)(low >> 32);
+            const float lv = low == 0 ? -kInf : __uint_as_float((low_u & 0x80000000u) ? low_u & 0x7FFFFFFFu : ~low_u);
+            if (v0 + tid < v1 && lane_max >= lv) hot[atomicAdd(&count[0], 1)] = (uint16_t)tid;
+            __syncthreads();
+            const int lanes = count[0], per = (v1 - v0 + threads - 1) / threads;
+            for (int h = w; h < lanes; h += warps) {
+                for (int j = lane; j < per; j += 32) {
+                    const int v = v0 + j * threads + hot[h];
+                    if (v >= v1) continue;
+                    Raw8<T> g;
+                    float z[8];
+                    g.load(x + (int64_t)v * 8, a.V - v * 8);
+                    get_logits(g, a.V - v * 8, z);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (!(z[e] >= lv)) continue;
+                        const uint64_t q8 = top_key(z[e], v * 8 + e);
+                        if (v * 8 + e < a.V && q8 >= low) {
+                            const int at = atomicAdd(&count[1], 1);
+                            if (at < kCandidates) cand[at] = q8;
+                        }
                     }
                 }
             }
             __syncthreads();
             found = count[1];
+            // many equal logits: the k-th largest key itself, by bisection, and the k keys from there on
+            if (found > 128 && found <= kCandidates) {
+                uint64_t bound = 0;
+                int n = found;
+                for (int bit = 63; bit >= 0 && n != k; --bit) {
+                    const uint64_t trial = bound | (1ull << bit);
+                    int reach = 0;
+                    for (int i = 0; i < found; i += threads) reach += __syncthreads_count(i + tid < found && cand[i + tid] >= trial);
+                    if (reach >= k) bound = trial, n = reach;
+                }
+                __syncthreads();
+                if (tid == 0) count[0] = 0;
+                __syncthreads();
+                for (int i = tid; i < found; i += threads)
+                    if (cand[i] >= bound) best[atomicAdd(&count[0], 1)] = cand[i];
+                __syncthreads();
+                if (tid < k) cand[tid] = best[tid];
+                __syncthreads();
+                found = k;
+            }
         }
         if (found <= kCandidates) {
             rank_keys(cand, found, k, best);
         } else {
             uint64_t last = ~0ull;
             for (int r = 0; r < k; ++r) {
-                last = next_key(x, a.V, v0, v1, last, hot_key);
+                last = next_key(x, a.V, v0, v1, last, cand);
                 if (tid == 0) best[r] = last;
             }
         }
@@ -323,47 +456,46 @@ __global__ void __launch_bounds__(kMaxLpThreads) logprobs_kernel(const __grid_co
     // ---- the row's values
     if (cs > 1) cluster_sync();
     if (rank == 0) {
-        Stat q = cta_stat;
-        for (int r = 1; r < (int)cs; ++r)
-            q = stat_join(q, Stat{remote_f32(&cta_stat.m, r), remote_f32(&cta_stat.s, r), remote_f32(&cta_stat.t, r)}, c);
+        if (cs > 1) {
+            if (w == 0) {
+                Stat q{-kInf, 0.0f, 0.0f};
+                if (lane < (int)cs) q = Stat{remote_f32(&cta_stat.m, lane), remote_f32(&cta_stat.s, lane), remote_f32(&cta_stat.t, lane)};
+#pragma unroll
+                for (int o = kMaxCluster / 2; o > 0; o >>= 1)
+                    q = stat_join(q, Stat{__shfl_xor_sync(~0u, q.m, o), __shfl_xor_sync(~0u, q.s, o), __shfl_xor_sync(~0u, q.t, o)}, c);
+                if (lane == 0) warp_stat[0] = q;
+            }
+            if (TOP)
+                for (int i = tid; i < (int)cs * RESQ_MAX_TOP; i += threads) cand[i] = remote_u64(&best[i % RESQ_MAX_TOP], i / RESQ_MAX_TOP);
+            __syncthreads();
+        } else if (TOP) {
+            __syncthreads();
+        }
+        const Stat q = cs > 1 ? warp_stat[0] : cta_stat;
         const bool bad = q.m == kInf || q.s != q.s, empty = q.m == -kInf;
         const float nan = __int_as_float(0x7FC00000), log_s = bad ? nan : log1pf(q.s);
         if (tid == 0) {
-            if (a.logp) {
-                const int64_t tok = a.tokens[m];
-                float v = 0.0f;
-                if (tok >= 0 && tok < a.V) {
-                    const float xt = load_logit(x + tok);
-                    v = bad ? nan : xt == -kInf ? -kInf : (xt - q.m) * a.inv_t - log_s;
-                }
-                a.logp[m] = v;
-            }
+            if (a.logp) a.logp[m] = !named ? 0.0f : bad ? nan : x_tok == -kInf ? -kInf : (x_tok - q.m) * a.inv_t - log_s;
             if (a.entropy) a.entropy[m] = bad ? nan : empty ? 0.0f : log_s - q.t * a.inv_t / (1.0f + q.s);
             if (a.peak) a.peak[m] = bad ? nan : q.m;
             if (a.log_sum) a.log_sum[m] = log_s;
         }
         if (TOP) {
-            __syncthreads();
-            if (cs > 1) {  // the slices' best together
-                for (int i = tid; i < (int)cs * RESQ_MAX_TOP; i += threads) cand[i] = remote_u64(&best[i % RESQ_MAX_TOP], i / RESQ_MAX_TOP);
-                __syncthreads();
-                // slots behind a slice's own count are 0 and rank behind every key
+            auto put = [&](int r, uint64_t key) {
+                const int j = (int)~(uint32_t)key;
+                const float v = load_logit(x + j);
+                a.top_ids[m * a.top + r] = j;
+                a.top_logp[m * a.top + r] = bad ? nan : v == -kInf ? -kInf : (v - q.m) * a.inv_t - log_s;
+            };
+            if (cs > 1) {  // the slices' best together; entries behind a slice's own count are 0 and rank behind every key
                 for (int i = tid; i < (int)cs * RESQ_MAX_TOP; i += threads) {
                     const uint64_t mine = cand[i];
                     int r = 0;
                     for (int j = 0; j < (int)cs * RESQ_MAX_TOP; ++j) r += cand[j] > mine;
-                    if (mine != 0 && r < a.top) {
-                        const int j = (int)~(uint32_t)mine;
-                        const float v = load_logit(x + j);
-                        a.top_ids[m * a.top + r] = j;
-                        a.top_logp[m * a.top + r] = bad ? nan : v == -kInf ? -kInf : (v - q.m) * a.inv_t - log_s;
-                    }
+                    if (mine != 0 && r < a.top) put(r, mine);
                 }
             } else if (tid < a.top) {
-                const int j = (int)~(uint32_t)best[tid];
-                const float v = load_logit(x + j);
-                a.top_ids[m * a.top + tid] = j;
-                a.top_logp[m * a.top + tid] = bad ? nan : v == -kInf ? -kInf : (v - q.m) * a.inv_t - log_s;
+                put(tid, best[tid]);
             }
         }
     }
@@ -472,13 +604,13 @@ int resq_token_logprobs(const void* logits, int dtype, int64_t M, int64_t V, int
         !is_aligned(top_logp, 4))
         return fail(RESQ_ERR_ALIGN, what, "tokens must be 8-byte aligned, the outputs 4-byte aligned");
     // Slices until the device has four CTAs of 256 threads per SM, of at least 512 vectors; with fewer CTAs than SMs they
-    // are made larger instead, so that a lane has one group of its own to read.
+    // are made larger, so that a lane has few groups to read.
     const int64_t vecs = (V + 7) / 8;
     int cs = 1;
     while (cs < kMaxCluster && M * cs < 4 * 148 && vecs / (2 * cs) >= 512) cs *= 2;
     const int64_t slice = (vecs + cs - 1) / cs;
-    const int64_t most = M * cs <= 148 ? kMaxLpThreads : 256;
-    const unsigned threads = (unsigned)std::min<int64_t>(most, ((slice + 1) / 2 + 31) / 32 * 32);
+    const int64_t most = M * cs <= 148 ? kMaxLpThreads : 256, per_lane = kV;
+    const unsigned threads = (unsigned)std::min<int64_t>(most, ((slice + per_lane - 1) / per_lane + 31) / 32 * 32);
     if (M * cs > INT32_MAX) return fail(RESQ_ERR_SHAPE, what, "too many rows for one call");
     LpArgs a{logits, ld, tokens, logp, entropy, peak, log_sum, top_ids, top_logp, (int)V, top, (int)slice, 1.0f / temperature};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
