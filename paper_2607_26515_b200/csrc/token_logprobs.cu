@@ -136,6 +136,11 @@ __device__ __forceinline__ uint64_t top_key(float x, int j) {
     return ((uint64_t)u << 32) | (uint32_t)~j;
 }
 
+__device__ __forceinline__ float key_value(uint64_t key) {  // of a logit that is not NaN
+    const uint32_t u = (uint32_t)(key >> 32);
+    return __uint_as_float((u & 0x80000000u) ? u & 0x7FFFFFFFu : ~u);
+}
+
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -192,7 +197,7 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int k, ui
 }
 
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kMaxLpThreads) logprobs_kernel(const __grid_constant__ LpArgs a) {
+__global__ void __launch_bounds__(kMaxLpThreads, 2) logprobs_kernel(const __grid_constant__ LpArgs a) {
     __shared__ Stat warp_stat[kMaxLpThreads / 32], cta_stat;
     __shared__ uint64_t cand[TOP ? kCandidates : 1], best[TOP ? RESQ_MAX_TOP : 1];
     __shared__ __align__(16) uint32_t bucket_order[kBuckets];
@@ -369,57 +374,72 @@ __global__ void __launch_bounds__(kMaxLpThreads) logprobs_kernel(const __grid_co
                     const uint4 o = *reinterpret_cast<const uint4*>(bucket_order + j);
                     r += (o.x > order) + (o.y > order) + (o.z > order) + (o.w > order);
                 }
+                if (r < k) best[r] = top_key(lane_max, 0) & ~0xFFFFFFFFull;
             }
-            if (r < k) {
-                uint64_t key = 0;  // a lane without elements: no bound
+            // First with the leaders' values alone; a row with too many equal logits goes by their places too, which takes
+            // reading the leaders' groups again.
+            for (int exact = 0; exact < 2; ++exact) {
+                if (exact && r < k) {
+                    uint64_t key = 0;  // a lane without elements: no bound
 #pragma unroll
-                for (int h = kV - 1; h >= 0; --h) {
-                    const int v = v0 + (lane_it * kV + h) * threads + tid;
-                    if (v >= v1) continue;
-                    Raw8<T> g;
-                    float z[8];
-                    g.load(x + (int64_t)v * 8, a.V - v * 8);
-                    get_logits(g, a.V - v * 8, z);
+                    for (int h = kV - 1; h >= 0; --h) {
+                        const int v = v0 + (lane_it * kV + h) * threads + tid;
+                        if (v >= v1) continue;
+                        Raw8<T> g;
+                        float z[8];
+                        g.load(x + (int64_t)v * 8, a.V - v * 8);
+                        get_logits(g, a.V - v * 8, z);
 #pragma unroll
-                    for (int i = 7; i >= 0; --i)
-                        if (z[i] == lane_max) key = top_key(z[i], v * 8 + i);
+                        for (int i = 7; i >= 0; --i)
+                            if (z[i] == lane_max) key = top_key(z[i], v * 8 + i);
+                    }
+                    best[r] = key;
                 }
-                best[r] = key;
-            }
-            __syncthreads();
-            uint64_t low = lane < k ? best[lane] : ~0ull;
+                __syncthreads();
+                uint64_t low = lane < k ? best[lane] : ~0ull;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                const uint64_t q8 = __shfl_xor_sync(~0u, low, o);
-                low = q8 < low ? q8 : low;
-            }
-            // lanes that may hold keys from the bound on: all their elements again
-            const uint32_t low_u = (uint32_t)(low >> 32);
-            const float lv = low == 0 ? -kInf : __uint_as_float((low_u & 0x80000000u) ? low_u & 0x7FFFFFFFu : ~low_u);
-            if (v0 + tid < v1 && lane_max >= lv) hot[atomicAdd(&count[0], 1)] = (uint16_t)tid;
-            __syncthreads();
-            const int lanes = count[0], per = (v1 - v0 + threads - 1) / threads;
-            for (int h = w; h < lanes; h += warps) {
-                for (int j = lane; j < per; j += 32) {
-                    const int v = v0 + j * threads + hot[h];
-                    if (v >= v1) continue;
-                    Raw8<T> g;
-                    float z[8];
-                    g.load(x + (int64_t)v * 8, a.V - v * 8);
-                    get_logits(g, a.V - v * 8, z);
+                for (int o = 16; o > 0; o >>= 1) {
+                    const uint64_t q8 = __shfl_xor_sync(~0u, low, o);
+                    low = q8 < low ? q8 : low;
+                }
+                // lanes that may hold keys from the bound on: all their elements again
+                const float lv = low == 0 ? -kInf : key_value(low);
+                if (v0 + tid < v1 && lane_max >= lv) hot[atomicAdd(&count[0], 1)] = (uint16_t)tid;
+                __syncthreads();
+                const int lanes = count[0], per = (v1 - v0 + threads - 1) / threads, parts = (per + 31) / 32;
+                constexpr int kAhead = 8 / sizeof(T);  // loads in flight per thread: this is latency, not bandwidth
+                for (int i0 = w; i0 < lanes * parts; i0 += warps * kAhead) {
+                    Raw8<T> g[kAhead];
+                    int vs[kAhead];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (!(z[e] >= lv)) continue;
-                        const uint64_t q8 = top_key(z[e], v * 8 + e);
-                        if (v * 8 + e < a.V && q8 >= low) {
-                            const int at = atomicAdd(&count[1], 1);
-                            if (at < kCandidates) cand[at] = q8;
+                    for (int b = 0; b < kAhead; ++b) {
+                        const int i = i0 + b * warps, j = (i % parts) * 32 + lane;
+                        vs[b] = i < lanes * parts && j < per ? v0 + j * threads + hot[i / parts] : v1;
+                        if (vs[b] < v1) g[b].load(x + (int64_t)vs[b] * 8, a.V - vs[b] * 8);
+                    }
+#pragma unroll
+                    for (int b = 0; b < kAhead; ++b) {
+                        const int v = vs[b];
+                        if (v >= v1) continue;
+                        float z[8];
+                        get_logits(g[b], a.V - v * 8, z);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            if (!(z[e] >= lv)) continue;
+                            const uint64_t q8 = top_key(z[e], v * 8 + e);
+                            if (v * 8 + e < a.V && q8 >= low) {
+                                const int at = atomicAdd(&count[1], 1);
+                                if (at < kCandidates) cand[at] = q8;
+                            }
                         }
                     }
                 }
+                __syncthreads();
+                found = count[1];
+                if (found <= kCandidates || exact) break;
+                __syncthreads();
+                if (tid < 2) count[tid] = 0;
             }
-            __syncthreads();
-            found = count[1];
             // many equal logits: the k-th largest key itself, by bisection, and the k keys from there on
             if (found > 128 && found <= kCandidates) {
                 uint64_t bound = 0;
@@ -466,7 +486,7 @@ __global__ void __launch_bounds__(kMaxLpThreads) logprobs_kernel(const __grid_co
                 if (lane == 0) warp_stat[0] = q;
             }
             if (TOP)
-                for (int i = tid; i < (int)cs * RESQ_MAX_TOP; i += threads) cand[i] = remote_u64(&best[i % RESQ_MAX_TOP], i / RESQ_MAX_TOP);
+                for (int i = tid; i < (int)cs * a.top; i += threads) cand[i] = remote_u64(&best[i % a.top], i / a.top);
             __syncthreads();
         } else if (TOP) {
             __syncthreads();
@@ -482,16 +502,15 @@ __global__ void __launch_bounds__(kMaxLpThreads) logprobs_kernel(const __grid_co
         }
         if (TOP) {
             auto put = [&](int r, uint64_t key) {
-                const int j = (int)~(uint32_t)key;
-                const float v = load_logit(x + j);
-                a.top_ids[m * a.top + r] = j;
+                const float v = key_value(key);
+                a.top_ids[m * a.top + r] = (int)~(uint32_t)key;
                 a.top_logp[m * a.top + r] = bad ? nan : v == -kInf ? -kInf : (v - q.m) * a.inv_t - log_s;
             };
             if (cs > 1) {  // the slices' best together; entries behind a slice's own count are 0 and rank behind every key
-                for (int i = tid; i < (int)cs * RESQ_MAX_TOP; i += threads) {
+                for (int i = tid; i < (int)cs * a.top; i += threads) {
                     const uint64_t mine = cand[i];
                     int r = 0;
-                    for (int j = 0; j < (int)cs * RESQ_MAX_TOP; ++j) r += cand[j] > mine;
+                    for (int j = 0; j < (int)cs * a.top; ++j) r += cand[j] > mine;
                     if (mine != 0 && r < a.top) put(r, mine);
                 }
             } else if (tid < a.top) {
@@ -603,13 +622,15 @@ int resq_token_logprobs(const void* logits, int dtype, int64_t M, int64_t V, int
     if (!is_aligned(tokens, 8) || !is_aligned(logp, 4) || !is_aligned(entropy, 4) || !is_aligned(peak, 4) || !is_aligned(log_sum, 4) || !is_aligned(top_ids, 4) ||
         !is_aligned(top_logp, 4))
         return fail(RESQ_ERR_ALIGN, what, "tokens must be 8-byte aligned, the outputs 4-byte aligned");
-    // Slices until the device has four CTAs of 256 threads per SM, of at least 512 vectors; with fewer CTAs than SMs they
-    // are made larger, so that a lane has few groups to read.
+    // Few rows are sliced, up to 256 CTAs and not below 16384 logits a slice: 1 x 131072 takes 5.2 us in eight slices and 9.8
+    // in one, but 512 x 131072 33 us in two and 31 in one, and 8000 logits a slice lose (a cluster's launch costs more than
+    // its CTAs').  Up to two CTAs per SM have 512 threads (250 x 131072: 17.7 against 23.4 us), more have 256 (1000 x 20000:
+    // 15.1 against 23.6 us).
     const int64_t vecs = (V + 7) / 8;
     int cs = 1;
-    while (cs < kMaxCluster && M * cs < 4 * 148 && vecs / (2 * cs) >= 512) cs *= 2;
+    while (cs < kMaxCluster && M * cs * 2 <= 256 && vecs / (2 * cs) >= 2048) cs *= 2;
     const int64_t slice = (vecs + cs - 1) / cs;
-    const int64_t most = M * cs <= 148 ? kMaxLpThreads : 256, per_lane = kV;
+    const int64_t most = M * cs <= 2 * 148 ? kMaxLpThreads : 256, per_lane = kV;
     const unsigned threads = (unsigned)std::min<int64_t>(most, ((slice + per_lane - 1) / per_lane + 31) / 32 * 32);
     if (M * cs > INT32_MAX) return fail(RESQ_ERR_SHAPE, what, "too many rows for one call");
     LpArgs a{logits, ld, tokens, logp, entropy, peak, log_sum, top_ids, top_logp, (int)V, top, (int)slice, 1.0f / temperature};
