@@ -5,9 +5,11 @@
 //   X  = H' r gamma_pre,   r  = 1 / sqrt(mean(H'^2) + eps)
 //
 // Forward: one CTA per row, the row stays in registers between the two row sums, so every tensor crosses HBM once.
-// Backward: persistent CTAs walk rows m = b, b + P, ... (P CTAs or clusters); a thread owns eight columns and keeps their
-// sums over the rows (the gradients of gamma_pre, gamma_post and a channel gate) in registers; at the end each CTA writes its
-// sums as one fp32 partial row and a second kernel adds the P partial rows in a fixed order (bit-identical run to run).
+// Backward: persistent CTAs walk rows m = b, b + P, ... (P CTAs or clusters); a thread owns eight or sixteen columns and keeps
+// their sums over the rows in registers; at the end each CTA writes them as one fp32 partial row and a second kernel adds the P
+// partial rows in a fixed order (bit-identical run to run).  The rows to come are in flight in a ring of asynchronous copies:
+// two row sums with a block barrier each leave a row's loads no time of their own otherwise (8192 x 2048, fp32 stream, channel
+// gate: 122 us without the ring).
 #include "row_common.cuh"
 
 #include <algorithm>
@@ -16,9 +18,8 @@ namespace resq {
 namespace {
 
 constexpr int kMaxThreadsFwd = 1024;  // one row: up to 4 vectors of 8 per thread
-constexpr int kMaxThreadsBwd = 512;   // eight columns per thread; longer rows are split over a cluster of CTAs
-constexpr int kMaxClusterBwd = 8;
-static_assert(kMaxThreadsFwd * 8 * 4 >= RESQ_JOIN_MAX_K && kMaxThreadsBwd * 8 * kMaxClusterBwd >= RESQ_JOIN_MAX_K, "row length");
+constexpr int kMaxThreadsBwd = 512;   // eight or sixteen columns per thread; longer rows are split over a cluster of 2 or 4 CTAs
+static_assert(kMaxThreadsFwd * 8 * 4 >= RESQ_JOIN_MAX_K && kMaxThreadsBwd * 16 * 4 >= RESQ_JOIN_MAX_K, "row length");
 
 struct JoinFwd {
     const void* H;
@@ -37,7 +38,7 @@ __device__ __forceinline__ float sigmoid_of(float g) { return __fdividef(1.0f, 1
 
 template <typename S, int VPT>
 __global__ void __launch_bounds__(kMaxThreadsFwd) join_fwd_kernel(const __grid_constant__ JoinFwd a) {
-    __shared__ float red[2][32];
+    __shared__ __align__(16) float red[2][32];
     pdl_wait();
     pdl_trigger();
     const int64_t m = blockIdx.x;
@@ -65,7 +66,7 @@ __global__ void __launch_bounds__(kMaxThreadsFwd) join_fwd_kernel(const __grid_c
             for (int i = 0; i < 8; ++i) s[0] = fmaf(b[i], b[i], s[0]);
         }
         block_sum<1>(s, red[0]);
-        rp = 1.0f / sqrtf(s[0] / (float)a.K + a.eps);
+        rp = rsqrtf(s[0] / (float)a.K + a.eps);
     }
     float h[VPT][8];
     float s[1] = {0.0f};
@@ -100,7 +101,7 @@ __global__ void __launch_bounds__(kMaxThreadsFwd) join_fwd_kernel(const __grid_c
     if (!a.X) return;
     // X comes from the 32-bit sum, not from its rounding to the stream's type
     block_sum<1>(s, red[1]);
-    const float r = 1.0f / sqrtf(s[0] / (float)a.K + a.eps);
+    const float r = rsqrtf(s[0] / (float)a.K + a.eps);
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         const int k = (threadIdx.x + j * blockDim.x) * 8, n = a.K - k;
@@ -125,13 +126,13 @@ struct JoinBwd {
     const __nv_bfloat16* gamma_pre;
     void* dH;
     __nv_bfloat16* dB;
-    __nv_bfloat16* dgate;        // a gate per token: [M, K]; null with a channel gate or none
-    float* part;                 // [P][ncol][kp]: gamma_pre (if dX), gamma_post (if given), channel gate (if given)
-    int64_t kp;                  // K rounded up to a multiple of 8
-    int ncol;
+    __nv_bfloat16* dgate;        // a gate per token: [M, K]
+    float* col[3];               // column sums: [groups][pitch] partial rows (or, with one group, the results) of gamma_pre,
+                                 // gamma_post, channel gate; null: not asked for
+    int64_t pitch;
     int64_t lddho, lddx, ldh, ldb, ldg, lddh, lddb, lddg;
     int64_t M;
-    int K, sigmoid;
+    int K, sigmoid, depth;
     float alpha, eps;
 };
 
@@ -162,87 +163,265 @@ __device__ __forceinline__ void row_sum(float (&v)[NV], float* buf, float* xbuf)
     }
 }
 
-template <typename S, int CS>
+// Eight columns as four packed pairs of fp32.
+typedef uint64_t Cols[4];
+__device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
+__device__ __forceinline__ uint64_t pair_bf16(uint32_t w) { return pair(bf16_lo(w), bf16_hi(w)); }
+__device__ __forceinline__ void cols_bf16(const uint4& q, Cols& v) {
+    v[0] = pair_bf16(q.x), v[1] = pair_bf16(q.y), v[2] = pair_bf16(q.z), v[3] = pair_bf16(q.w);
+}
+__device__ __forceinline__ float sum2(uint64_t p) {
+    float lo, hi;
+    unpair(p, lo, hi);
+    return lo + hi;
+}
+template <typename T>
+__device__ __forceinline__ void store_cols(T* p, const Cols& v, int n) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpair(v[i], f[2 * i], f[2 * i + 1]);
+    store8(p, f, n);
+}
+__device__ __forceinline__ void copy16(void* dst, const void* src, int bytes) {  // the first `bytes` of 16, zeros behind them
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes)
+                 : "memory");
+}
+
+// One row of a stage in shared memory: its tensors one after the other, each as the CTA's columns lie in memory (whole vectors
+// of 8, zeros behind the last column).
+__host__ __device__ inline int stage_bytes(int stream_size, bool gate, int columns) { return columns * (2 * stream_size + 4 + (gate ? 2 : 0)); }
+constexpr int kMaxDepth = 6;
+
+// POST: the branch is normalised.  GATE: 0 none, 1 channel, 2 per token.  VPT: vectors of 8 columns per thread.  CS: CTAs per row.
+// First come the sums over the row of H'^2, dX gamma_pre H' and B^2; then d = the gradient of H' and v = the gradient of the
+// normalised branch n; then, with a norm on the branch, the sum of v n.  The first sums of the next row and the last one of this
+// row are taken together, so a row costs one barrier.  Without a gate per token the gradients of gamma_post and of the channel
+// gate are the same column sum of d n times a constant of the column.
+template <typename S, bool POST, int GATE, int VPT, int CS>
 __global__ void __launch_bounds__(kMaxThreadsBwd) join_bwd_kernel(const __grid_constant__ JoinBwd a) {
-    __shared__ float red[2][3 * 32];
-    __shared__ float xred[2][3 * CS];
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ __align__(16) float red[2][4 * 32];
+    __shared__ float xred[2][4 * CS];
+    const int threads = blockDim.x, tid = threadIdx.x;
+    const int groups = gridDim.x / CS, rows = (int)a.M;
+    const int columns = VPT * threads * 8, first = (int)(blockIdx.x % CS) * columns;  // this CTA's
+    const int stage_size = stage_bytes(sizeof(S), GATE == 2, columns);
+    int n[VPT];  // columns of the thread's vectors (<= 0: none; such a thread takes part in copies and sums)
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) n[j] = a.K - first - (j * threads + tid) * 8;
+
     pdl_wait();
     pdl_trigger();
-    const int64_t group = blockIdx.x / CS, groups = gridDim.x / CS;
-    const int k = (int)((blockIdx.x % CS) * blockDim.x + threadIdx.x) * 8;
-    const int n = a.K - k;  // <= 0: no column of its own, but it takes part in the sums
-    const float inv_k = 1.0f / (float)a.K;
-    float wpre[8], wpost[8], acc_pre[8], acc_post[8], acc_gate[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) wpre[i] = 0.0f, wpost[i] = 1.0f, acc_pre[i] = acc_post[i] = acc_gate[i] = 0.0f;
-    if (n > 0) {
-        Raw8<__nv_bfloat16> r;
-        if (a.dX) r.load(a.gamma_pre + k, n), r.get(wpre);
-        if (a.gamma_post) r.load(a.gamma_post + k, n), r.get(wpost);
-    }
-    int flip = 0;
-    for (int64_t m = group; m < a.M; m += groups) {
-        float h[8], u[8], d[8], b[8], G[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = u[i] = d[i] = b[i] = 0.0f, G[i] = 1.0f;
-        if (n > 0) {
-            Raw8<S> rs;
-            Raw8<__nv_bfloat16> r;
-            rs.load(static_cast<const S*>(a.H) + m * a.ldh + k, n), rs.get(h);
-            if (a.dHo) rs.load(static_cast<const S*>(a.dHo) + m * a.lddho + k, n), rs.get(d);
-            if (a.dX) r.load(a.dX + m * a.lddx + k, n), r.get(u);
-            r.load(a.B + m * a.ldb + k, n), r.get(b);
-            if (a.gate) r.load(a.gate + m * a.ldg + k, n), r.get(G);
+    // chunks of 16 bytes of one row of one tensor, neighbouring threads neighbouring chunks
+    auto copy_row = [&](uint8_t* dst, const void* src, int size) {
+        const int cols = min(a.K - first, columns), bytes = cols * size, whole = (cols + 7) / 8 * 8 * size;
+        for (int i = tid * 16; i < whole; i += threads * 16) {
+            const int have = min(bytes - i, 16);
+            copy16(dst + i, static_cast<const uint8_t*>(src) + (have > 0 ? i : 0), max(have, 0));
         }
-        float s[3] = {0.0f, 0.0f, 0.0f};  // sum h^2, sum dX gamma_pre h, sum b^2
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            s[0] = fmaf(h[i], h[i], s[0]);
-            s[1] = fmaf(u[i] * wpre[i], h[i], s[1]);
-            s[2] = fmaf(b[i], b[i], s[2]);
+    };
+    auto copy = [&](int m, int stage) {
+        if (m < rows && first < a.K) {
+            uint8_t* dst = ring + (size_t)stage * stage_size;
+            copy_row(dst, static_cast<const S*>(a.H) + (int64_t)m * a.ldh + first, sizeof(S));
+            dst += columns * (int)sizeof(S);
+            if (a.dHo) copy_row(dst, static_cast<const S*>(a.dHo) + (int64_t)m * a.lddho + first, sizeof(S));
+            dst += columns * (int)sizeof(S);
+            if (a.dX) copy_row(dst, a.dX + (int64_t)m * a.lddx + first, 2);
+            dst += columns * 2;
+            copy_row(dst, a.B + (int64_t)m * a.ldb + first, 2);
+            if (GATE == 2) copy_row(dst + columns * 2, a.gate + (int64_t)m * a.ldg + first, 2);
         }
-        row_sum<3, CS>(s, red[flip], xred[flip]);
-        const float r = 1.0f / sqrtf(s[0] * inv_k + a.eps);
-        const float c = s[1] * r * inv_k * r;  // mean(u xhat) r, per unit of h
-        const float rp = a.gamma_post ? 1.0f / sqrtf(s[2] * inv_k + a.eps) : 1.0f;
-        float t[1] = {0.0f};
-        float dg[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (a.dX) {
-                acc_pre[i] = fmaf(u[i], h[i] * r, acc_pre[i]);
-                d[i] = fmaf(r, u[i] * wpre[i] - h[i] * c, d[i]);
-            }
-            const float nb = b[i] * rp;            // normalised branch (or the branch itself)
-            float g = G[i], slope = 1.0f;
-            if (a.gate && a.sigmoid) g = sigmoid_of(g), slope = g * (1.0f - g);
-            const float dp = a.alpha * d[i];
-            dg[i] = dp * nb * wpost[i] * slope;
-            acc_gate[i] += dg[i];
-            acc_post[i] = fmaf(dp * g, nb, acc_post[i]);
-            b[i] = dp * g * wpost[i];              // gradient of the normalised branch
-            h[i] = nb;
-            t[0] = fmaf(b[i], nb, t[0]);
-        }
-        if (a.gamma_post) {
-            row_sum<1, CS>(t, red[1], xred[1]);
-            const float q = t[0] * inv_k;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) b[i] = rp * (b[i] - h[i] * q);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto landed = [&](int pending) {  // all but the newest `pending` copies of this thread have arrived
+        if (pending >= 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        else if (pending == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (pending == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    };
+    auto stream_cols = [&](const uint8_t* p, int j, Cols& v) {
+        const int at = (j * threads + tid) * 8;
+        if (sizeof(S) == 2) {
+            cols_bf16(*reinterpret_cast<const uint4*>(p + at * 2), v);
         } else {
-            flip ^= 1;  // one sum per row: alternate the buffers from row to row
+            const float4 q = *reinterpret_cast<const float4*>(p + at * 4), t = *reinterpret_cast<const float4*>(p + at * 4 + 16);
+            v[0] = pair(q.x, q.y), v[1] = pair(q.z, q.w), v[2] = pair(t.x, t.y), v[3] = pair(t.z, t.w);
         }
-        if (n > 0) {
-            store8(static_cast<S*>(a.dH) + m * a.lddh + k, d, n);
-            store8(a.dB + m * a.lddb + k, b, n);
-            if (a.dgate) store8(a.dgate + m * a.lddg + k, dg, n);
+    };
+    auto half_cols = [&](const uint8_t* p, int j, Cols& v) { cols_bf16(*reinterpret_cast<const uint4*>(p + (j * threads + tid) * 16), v); };
+    const int at_d = columns * (int)sizeof(S), at_x = 2 * at_d, at_b = at_x + columns * 2, at_g = at_b + columns * 2;
+
+    int m = blockIdx.x / CS, ahead = m;  // this row, and the next one to copy
+    for (int d = 0; d < a.depth - 1; ++d, ahead += groups) copy(ahead, d);
+
+    const float inv_k = 1.0f / (float)a.K;
+    uint4 wpre[VPT], wpost[VPT], wgate[VPT];  // bf16, as they lie in memory
+    Cols acc_pre[VPT], acc_post[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        Raw8<__nv_bfloat16> r;
+        const int col = first + (j * threads + tid) * 8;
+        wpre[j] = wpost[j] = wgate[j] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc_pre[j][i] = acc_post[j][i] = 0;
+        if (n[j] <= 0) continue;
+        if (a.dX) r.load(a.gamma_pre + col, n[j]), wpre[j] = r.q;
+        if (POST) r.load(a.gamma_post + col, n[j]), wpost[j] = r.q;
+        if (GATE == 1) r.load(a.gate + col, n[j]), wgate[j] = r.q;
+    }
+    auto gate_of = [&](uint64_t G, uint64_t& slope) {
+        float lo, hi;
+        unpair(G, lo, hi);
+        if (a.sigmoid) {
+            lo = sigmoid_of(lo), hi = sigmoid_of(hi);
+            slope = pair(lo * (1.0f - lo), hi * (1.0f - hi));
+        } else {
+            slope = both(1.0f);
+        }
+        return pair(lo, hi);
+    };
+    // sums of the row in stage p: H'^2, dX gamma_pre H', B^2
+    auto first_sums = [&](const uint8_t* p, float (&s)[4]) {
+        uint64_t sh = 0, su = 0, sb = 0;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            if (n[j] <= 0) continue;
+            Cols h, u, w;
+            stream_cols(p, j, h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sh = fma2(h[i], h[i], sh);
+            if (a.dX) {
+                half_cols(p + at_x, j, u);
+                cols_bf16(wpre[j], w);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) su = fma2(mul2(u[i], w[i]), h[i], su);
+            }
+            if (POST) {
+                half_cols(p + at_b, j, u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sb = fma2(u[i], u[i], sb);
+            }
+        }
+        s[0] = sum2(sh), s[1] = sum2(su), s[2] = sum2(sb);
+    };
+
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    int stage = 0, flip = 0;
+    landed(a.depth - 2);
+    __syncthreads();
+    if (m < rows) first_sums(ring, s);
+    landed(a.depth - 3);
+    row_sum<4, CS>(s, red[0], xred[0]);
+    for (; m < rows; m += groups) {
+        const float r = rsqrtf(s[0] * inv_k + a.eps);
+        const float c = -s[1] * r * inv_k * r * r;  // - mean(u xhat) r, per unit of H'
+        const float rp = POST ? rsqrtf(s[2] * inv_k + a.eps) : 1.0f;
+        // into the stage of the row before, which every thread has left
+        copy(ahead, stage == 0 ? a.depth - 1 : stage - 1);
+        ahead += groups;
+        const uint8_t* p = ring + (size_t)stage * stage_size;
+        Cols v[VPT], nb[VPT];  // gradient of the normalised branch, and that branch
+        uint64_t t2 = 0;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            if (n[j] <= 0) continue;
+            const int col = first + (j * threads + tid) * 8;
+            Cols d, w;
+            if (a.dHo) {
+                stream_cols(p + at_d, j, d);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d[i] = 0;
+            }
+            if (a.dX) {
+                Cols h, u;
+                stream_cols(p, j, h);
+                half_cols(p + at_x, j, u);
+                cols_bf16(wpre[j], w);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint64_t hr = mul2(h[i], both(r)), ur = mul2(u[i], both(r));
+                    acc_pre[j][i] = fma2(u[i], hr, acc_pre[j][i]);
+                    d[i] = fma2(ur, w[i], fma2(both(c), h[i], d[i]));
+                }
+            }
+            store_cols(static_cast<S*>(a.dH) + (int64_t)m * a.lddh + col, d, n[j]);
+            half_cols(p + at_b, j, nb[j]);
+            Cols G, dg;
+            if (GATE == 2) half_cols(p + at_g, j, G);
+            else if (GATE == 1) cols_bf16(wgate[j], G);
+            if (POST) cols_bf16(wpost[j], w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (POST) nb[j][i] = mul2(nb[j][i], both(rp));
+                const uint64_t dn = mul2(d[i], nb[j][i]);
+                uint64_t dp = mul2(d[i], both(a.alpha)), slope = 0;
+                if (GATE != 0) {
+                    const uint64_t g = gate_of(G[i], slope);
+                    dp = mul2(dp, g);
+                    if (GATE == 2) {
+                        dg[i] = mul2(mul2(dn, both(a.alpha)), slope);
+                        if (POST) dg[i] = mul2(dg[i], w[i]), acc_post[j][i] = fma2(dn, g, acc_post[j][i]);
+                    }
+                }
+                if (GATE != 2) acc_post[j][i] = add2(acc_post[j][i], dn);
+                v[j][i] = POST ? mul2(dp, w[i]) : dp;
+                if (POST) t2 = fma2(v[j][i], nb[j][i], t2);
+            }
+            if (GATE == 2) store_cols(a.dgate + (int64_t)m * a.lddg + col, dg, n[j]);
+            if (!POST) store_cols(a.dB + (int64_t)m * a.lddb + col, v[j], n[j]);
+        }
+        if (++stage == a.depth) stage = 0;
+        s[0] = s[1] = s[2] = 0.0f;
+        s[3] = sum2(t2);
+        if (m + groups < rows) first_sums(ring + (size_t)stage * stage_size, s);
+        landed(a.depth - 3);  // the row after the next: visible to all behind the barrier
+        flip ^= 1;
+        row_sum<4, CS>(s, red[flip], xred[flip]);
+        if (POST) {
+            const float q = -s[3] * inv_k;
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+                if (n[j] <= 0) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[j][i] = mul2(both(rp), fma2(both(q), nb[j][i], v[j][i]));
+                store_cols(a.dB + (int64_t)m * a.lddb + first + (j * threads + tid) * 8, v[j], n[j]);
+            }
         }
     }
-    if (n > 0) {
-        float* out = a.part + group * a.ncol * a.kp + k;
-        if (a.dX) store8(out, acc_pre, n), out += a.kp;
-        if (a.gamma_post) store8(out, acc_post, n), out += a.kp;
-        if (a.gate && a.ldg == 0) store8(out, acc_gate, n);
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        if (n[j] <= 0) continue;
+        // a partial row is padded to whole vectors; a result (one group) ends with column K - 1 and starts on any float
+        auto put = [&](int which, const Cols& v) {
+            if (!a.col[which]) return;
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) unpair(v[i], f[2 * i], f[2 * i + 1]);
+            float* p = a.col[which] + (blockIdx.x / CS) * a.pitch + first + (j * threads + tid) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n[j]) p[i] = f[i];
+        };
+        put(0, acc_pre[j]);
+        Cols w, G, x;
+        if (POST) {
+            cols_bf16(wpost[j], w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = both(1.0f);
+        }
+        if (GATE == 1) cols_bf16(wgate[j], G);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint64_t slope = both(1.0f), g = both(1.0f);
+            if (GATE == 1) g = gate_of(G[i], slope);
+            x[i] = mul2(mul2(acc_post[j][i], both(a.alpha)), mul2(slope, w[i]));
+            acc_post[j][i] = mul2(mul2(acc_post[j][i], both(a.alpha)), g);
+        }
+        if (POST) put(1, acc_post[j]);
+        if (GATE == 1) put(2, x);
     }
     if (CS > 1) {  // no CTA leaves while a peer may still write its shared memory
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
@@ -250,31 +429,37 @@ __global__ void __launch_bounds__(kMaxThreadsBwd) join_bwd_kernel(const __grid_c
     }
 }
 
-// Sum of the P partial rows: a block owns 32 columns, each of its eight warps adds a contiguous run of rows, and the eight
-// sums are added in order.
+// Sum of the P partial rows: a block owns 32 columns, each of its 16 warps adds a contiguous run of rows with eight loads in
+// flight, and the 16 sums are added in order.
+constexpr int kSumWarps = 16;
 struct JoinSum {
-    const float* part;
+    const float* part[3];
     float* out[3];
-    int64_t kp;
-    int P, ncol, K;
+    int64_t pitch;
+    int P, K;
 };
-__global__ void __launch_bounds__(256) join_sum_kernel(const __grid_constant__ JoinSum a) {
-    __shared__ float buf[8][32];
+__global__ void __launch_bounds__(kSumWarps * 32) join_sum_kernel(const __grid_constant__ JoinSum a) {
+    __shared__ float buf[kSumWarps][32];
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, col = blockIdx.x * 32 + lane, which = blockIdx.y;
-    const int per = (a.P + 7) / 8, p0 = w * per, p1 = min(a.P, p0 + per);
+    const int per = (a.P + kSumWarps - 1) / kSumWarps, p0 = w * per, p1 = min(a.P, p0 + per);
     float s = 0.0f;
     if (col < a.K) {
-        const float* src = a.part + (int64_t)which * a.kp + col;
-        for (int p = p0; p < p1; ++p) s += src[(int64_t)p * a.ncol * a.kp];
+        const float* src = a.part[which] + col;
+        for (int p = p0; p < p1; p += 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = p + i < p1 ? src[(p + i) * a.pitch] : 0.0f;
+            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
     }
     buf[w][lane] = s;
     __syncthreads();
     if (w == 0 && col < a.K) {
         float t = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t += buf[i][lane];
+        for (int i = 0; i < kSumWarps; ++i) t += buf[i][lane];
         a.out[which][col] = t;
     }
 }
@@ -282,15 +467,59 @@ __global__ void __launch_bounds__(256) join_sum_kernel(const __grid_constant__ J
 // ---- host side -----------------------------------------------------------------------------------
 constexpr int kSms = 148;
 
-int bwd_cluster(int64_t K) {
-    int cs = 1;
-    while ((K + 7) / 8 > (int64_t)cs * kMaxThreadsBwd) cs *= 2;
-    return cs;
+// Split of a row: vectors per thread, CTAs, threads; CTAs per SM (512 threads of 128 registers; each holds at least three rows
+// in shared memory, for which long rows are split further); groups of CTAs that share the rows.
+constexpr int kSmemSm = 224 * 1024, kSmemStatic = 2048;
+struct BwdShape {
+    int vpt, cs, threads, per_sm, depth;
+    int64_t groups;
+};
+BwdShape bwd_shape(int64_t M, int64_t K, int stream_size, bool gate) {
+    const int64_t vecs = (K + 7) / 8;
+    BwdShape s;
+    s.vpt = vecs <= kMaxThreadsBwd ? 1 : 2;
+    int stage = 0;
+    for (s.cs = 1;; s.cs *= 2) {
+        const int64_t per = (int64_t)s.cs * s.vpt * 32;
+        s.threads = (int)((vecs + per - 1) / per * 32);
+        stage = stage_bytes(stream_size, gate, s.vpt * s.threads * 8);
+        if (s.threads <= kMaxThreadsBwd && 3 * stage <= kSmemSm - kSmemStatic) break;
+    }
+    s.per_sm = std::min(kMaxThreadsBwd / s.threads, kSmemSm / (3 * stage + kSmemStatic));
+    s.depth = std::min(kMaxDepth, (kSmemSm / s.per_sm - kSmemStatic) / stage);
+    s.groups = std::min<int64_t>(M, std::max(1, kSms * s.per_sm / s.cs));
+    return s;
 }
-int bwd_threads(int64_t K, int cs) { return (int)(((K + 7) / 8 + cs * 32 - 1) / (cs * 32) * 32); }
-int64_t bwd_groups(int64_t M, int64_t K) {
-    const int cs = bwd_cluster(K), per_sm = std::min(16, std::max(1, 1024 / bwd_threads(K, cs)));
-    return std::min<int64_t>(M, std::max(1, kSms * per_sm / cs));
+int64_t bwd_most_groups(int64_t M, int64_t K) {
+    int64_t g = 0;
+    for (int size = 2; size <= 4; size += 2)
+        for (int gate = 0; gate < 2; ++gate) g = std::max(g, bwd_shape(M, K, size, gate).groups);
+    return g;
+}
+
+template <typename S, bool POST, int GATE, int VPT, int CS>
+int launch_bwd(const BwdShape& s, JoinBwd a, cudaStream_t st) {
+    auto kern = join_bwd_kernel<S, POST, GATE, VPT, CS>;
+    const int smem = s.depth * stage_bytes(sizeof(S), GATE == 2, VPT * s.threads * 8);
+    a.depth = s.depth;
+    const int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem, "join_bwd_kernel shared memory");
+    if (rc) return rc;
+    LaunchScope scope(kKindRow, st);
+    return cuda_fail(launch_clusters(kern, (unsigned)(s.groups * CS), (unsigned)s.threads, (size_t)smem, CS, st, a),
+                     "join_bwd_kernel launch");
+}
+template <typename S, bool POST, int GATE>
+int launch_bwd(const BwdShape& s, const JoinBwd& a, cudaStream_t st) {
+    if (s.vpt == 1) return launch_bwd<S, POST, GATE, 1, 1>(s, a, st);
+    if (s.cs == 1) return launch_bwd<S, POST, GATE, 2, 1>(s, a, st);
+    if (s.cs == 2) return launch_bwd<S, POST, GATE, 2, 2>(s, a, st);
+    return s.cs == 4 ? launch_bwd<S, POST, GATE, 2, 4>(s, a, st) : launch_bwd<S, POST, GATE, 2, 8>(s, a, st);
+}
+template <typename S>
+int launch_bwd(const BwdShape& s, const JoinBwd& a, cudaStream_t st) {
+    const int gate = !a.gate ? 0 : a.ldg == 0 ? 1 : 2;
+    if (a.gamma_post) return gate == 0 ? launch_bwd<S, true, 0>(s, a, st) : gate == 1 ? launch_bwd<S, true, 1>(s, a, st) : launch_bwd<S, true, 2>(s, a, st);
+    return gate == 0 ? launch_bwd<S, false, 0>(s, a, st) : gate == 1 ? launch_bwd<S, false, 1>(s, a, st) : launch_bwd<S, false, 2>(s, a, st);
 }
 
 int check_join(const char* what, int64_t M, int64_t K, int dtype, const void* B, int64_t ldb, const void* gate, int64_t ldg, int gate_act,
@@ -353,7 +582,7 @@ int resq_block_join(const void* H, int stream_dtype, const void* B, int64_t M, i
 
 size_t resq_block_join_backward_workspace_bytes(int64_t M, int64_t K) {
     if (M <= 0 || K <= 0 || K > RESQ_JOIN_MAX_K) return 0;
-    return align_up((size_t)bwd_groups(M, K) * 3 * (size_t)((K + 7) / 8 * 8) * sizeof(float), 256);
+    return align_up((size_t)bwd_most_groups(M, K) * 3 * (size_t)((K + 7) / 8 * 8) * sizeof(float), 256);
 }
 
 int resq_block_join_backward(const void* dH_out, const void* dX, const void* H_out, int stream_dtype, const void* B, int64_t M, int64_t K,
@@ -391,33 +620,26 @@ int resq_block_join_backward(const void* dH_out, const void* dX, const void* H_o
     a.dH = dH;
     a.dB = static_cast<__nv_bfloat16*>(dB);
     a.dgate = gate && ldg != 0 ? static_cast<__nv_bfloat16*>(dgate) : nullptr;
-    a.part = static_cast<float*>(workspace);
-    a.kp = (K + 7) / 8 * 8;
     a.lddho = lddho, a.lddx = lddx, a.ldh = ldho, a.ldb = ldb, a.ldg = ldg, a.lddh = lddh, a.lddb = lddb, a.lddg = lddg;
     a.M = M, a.K = (int)K, a.sigmoid = gate_act == RESQ_GATE_SIGMOID, a.alpha = alpha, a.eps = eps;
+    const BwdShape shape = bwd_shape(M, K, stream_dtype == RESQ_OUT_F32 ? 4 : 2, gate && ldg != 0);
+    float* const results[3] = {dX ? dgamma_pre : nullptr, gamma_post ? dgamma_post : nullptr,
+                               gate && ldg == 0 ? static_cast<float*>(dgate) : nullptr};
+    a.pitch = (K + 7) / 8 * 8;
     JoinSum s;
-    s.ncol = 0;
-    if (dX) s.out[s.ncol++] = dgamma_pre;
-    if (gamma_post) s.out[s.ncol++] = dgamma_post;
-    if (gate && ldg == 0) s.out[s.ncol++] = static_cast<float*>(dgate);
-    a.ncol = s.ncol;
-    const int cs = bwd_cluster(K);
-    const int64_t groups = bwd_groups(M, K);
-    const bool f32 = stream_dtype == RESQ_OUT_F32;
-    using bf = __nv_bfloat16;
-    auto kern = cs == 1   ? (f32 ? join_bwd_kernel<float, 1> : join_bwd_kernel<bf, 1>)
-                : cs == 2 ? (f32 ? join_bwd_kernel<float, 2> : join_bwd_kernel<bf, 2>)
-                : cs == 4 ? (f32 ? join_bwd_kernel<float, 4> : join_bwd_kernel<bf, 4>)
-                          : (f32 ? join_bwd_kernel<float, 8> : join_bwd_kernel<bf, 8>);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    {
-        LaunchScope scope(kKindRow, st);
-        rc = cuda_fail(launch_clusters(kern, (unsigned)(groups * cs), (unsigned)bwd_threads(K, cs), 0, cs, st, a), "join_bwd_kernel launch");
+    int ncol = 0;
+    for (int i = 0; i < 3; ++i) {
+        a.col[i] = results[i];
+        if (!results[i] || shape.groups == 1) continue;  // one group of CTAs: its sums are the results
+        a.col[i] = static_cast<float*>(workspace) + (int64_t)ncol * shape.groups * a.pitch;
+        s.part[ncol] = a.col[i], s.out[ncol++] = results[i];
     }
-    if (rc || s.ncol == 0) return rc;
-    s.part = a.part, s.kp = a.kp, s.P = (int)groups, s.K = (int)K;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    rc = stream_dtype == RESQ_OUT_F32 ? launch_bwd<float>(shape, a, st) : launch_bwd<__nv_bfloat16>(shape, a, st);
+    if (rc || ncol == 0) return rc;
+    s.pitch = a.pitch, s.P = (int)shape.groups, s.K = (int)K;
     LaunchScope scope(kKindRow, st);
-    return cuda_fail(launch_kernel(join_sum_kernel, dim3((unsigned)((K + 31) / 32), (unsigned)s.ncol), dim3(256), 0, st, s),
+    return cuda_fail(launch_kernel(join_sum_kernel, dim3((unsigned)((K + 31) / 32), (unsigned)ncol), dim3(kSumWarps * 32), 0, st, s),
                      "join_sum_kernel launch");
 }
 }

@@ -90,27 +90,78 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8], int n) {
         if (i < n) p[i] = v[i];
 }
 
-// Sums of NV values over the block, the same bits in every thread; fixed order.  `buf` holds NV * 32 floats and must not
-// be the buffer of the previous call (two alternate, which saves a barrier).
+// Pairs of fp32 values in one instruction.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// Sums of NV (1 or 4) values over the block, the same bits in every thread; fixed order.  `buf` holds NV * 32 floats (16-byte
+// aligned) and must not be the buffer of the previous call (two alternate, which saves a barrier).  Four values share their
+// shuffles: after two exchanges a lane carries one of them (6 shuffles instead of 20).
 template <int NV>
 __device__ __forceinline__ void block_sum(float (&v)[NV], float* buf) {
+    static_assert(NV == 1 || NV == 4, "");
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, nw = (blockDim.x + 31) >> 5;
+    float x = v[0];
+    if (NV == 4) {
+        const bool up = lane & 16;
+        const float a = (up ? v[2 % NV] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, up ? v[0] : v[2 % NV], 16);
+        const float b = (up ? v[3 % NV] : v[1 % NV]) + __shfl_xor_sync(0xFFFFFFFFu, up ? v[1 % NV] : v[3 % NV], 16);
+        x = (lane & 8 ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, lane & 8 ? a : b, 8);
+    } else {
+        x += __shfl_xor_sync(0xFFFFFFFFu, x, 16);
+        x += __shfl_xor_sync(0xFFFFFFFFu, x, 8);
+    }
+    x += __shfl_xor_sync(0xFFFFFFFFu, x, 4);
+    x += __shfl_xor_sync(0xFFFFFFFFu, x, 2);
+    x += __shfl_xor_sync(0xFFFFFFFFu, x, 1);
+    if (nw == 1) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
-    const int nw = (blockDim.x + 31) >> 5;
-    if (nw == 1) return;
-    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) buf[i * 32 + w] = v[i];
+        for (int i = 0; i < NV; ++i) v[i] = NV == 1 ? x : __shfl_sync(0xFFFFFFFFu, x, i * 8);
+        return;
+    }
+    if (NV == 1 ? lane == 0 : (lane & 7) == 0) buf[(lane >> 3) * 32 + w] = x;
     __syncthreads();
+    if (nw <= 8) {  // read back whole: less latency than five more shuffles
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = lane < nw ? buf[i * 32 + lane] : 0.0f;
+        for (int i = 0; i < NV; ++i) {
+            const float4 p = *reinterpret_cast<const float4*>(buf + i * 32), q = *reinterpret_cast<const float4*>(buf + i * 32 + 4);
+            v[i] = (((nw > 0 ? p.x : 0.0f) + (nw > 1 ? p.y : 0.0f)) + ((nw > 2 ? p.z : 0.0f) + (nw > 3 ? p.w : 0.0f))) +
+                   (((nw > 4 ? q.x : 0.0f) + (nw > 5 ? q.y : 0.0f)) + ((nw > 6 ? q.z : 0.0f) + (nw > 7 ? q.w : 0.0f)));
+        }
+        return;
+    }
+    if (NV == 4) {  // eight lanes per value
+        float y = 0.0f;
+        for (int j = lane & 7; j < nw; j += 8) y += buf[(lane >> 3) * 32 + j];
+        y += __shfl_xor_sync(0xFFFFFFFFu, y, 4);
+        y += __shfl_xor_sync(0xFFFFFFFFu, y, 2);
+        y += __shfl_xor_sync(0xFFFFFFFFu, y, 1);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+        for (int i = 0; i < NV; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, y, i * 8);
+        return;
+    }
+    v[0] = lane < nw ? buf[lane] : 0.0f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
+    for (int o = 16; o > 0; o >>= 1) v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], o);
 }
 
 // launch_kernel() with clusters of `cs` CTAs.
