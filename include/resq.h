@@ -380,6 +380,7 @@ RESQ_API int mxfp4_w4a16_gemv(const void* X_bf16, int64_t M, int64_t K, int64_t 
  *     dH [M, K] (type of the stream; may be dH_out itself), dB bf16 [M, K], dgate (bf16 [M, K] with pitch lddg; for a
  *     channel gate fp32 [K]), dgamma_post fp32 [K], dgamma_pre fp32 [K] (required where the input it belongs to is
  *     given, dgamma_pre where dX is; otherwise ignored).  Sums over the tokens are fp32 in a fixed order.
+ *   Row pitches below 2^31 elements.
  *   workspace of resq_block_join_backward_workspace_bytes(M, K) bytes, 256-byte aligned, owned by the call until it has
  *   run (it holds partial sums; no status word). */
 typedef enum { RESQ_GATE_LINEAR = 0, RESQ_GATE_SIGMOID = 1 } resq_gate;

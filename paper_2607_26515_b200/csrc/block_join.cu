@@ -29,77 +29,132 @@ struct JoinFwd {
     const __nv_bfloat16* gamma_pre;
     void* H_out;
     __nv_bfloat16* X;
-    int64_t ldh, ldb, ldg, ldho, ldx;
+    int64_t M, ldh, ldb, ldg, ldho, ldx;
     int K, sigmoid;
     float alpha, eps;
 };
 
-__device__ __forceinline__ float sigmoid_of(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
+// 1 / (1 + exp(-g)): two special-function operations, each within 2 ulp; exp overflowing to infinity gives 0.
+__device__ __forceinline__ float sigmoid_of(float g) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return r;
+}
 
-template <typename S, int VPT>
-__global__ void __launch_bounds__(kMaxThreadsFwd) join_fwd_kernel(const __grid_constant__ JoinFwd a) {
+// Eight columns as four packed pairs of fp32.
+typedef uint64_t Cols[4];
+__device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
+__device__ __forceinline__ uint64_t pair_bf16(uint32_t w) { return pair(bf16_lo(w), bf16_hi(w)); }
+__device__ __forceinline__ void cols_bf16(const uint4& q, Cols& v) {
+    v[0] = pair_bf16(q.x), v[1] = pair_bf16(q.y), v[2] = pair_bf16(q.z), v[3] = pair_bf16(q.w);
+}
+__device__ __forceinline__ float sum2(uint64_t p) {
+    float lo, hi;
+    unpair(p, lo, hi);
+    return lo + hi;
+}
+template <typename T>
+__device__ __forceinline__ void store_cols(T* p, const Cols& v, int n) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpair(v[i], f[2 * i], f[2 * i + 1]);
+    store8(p, f, n);
+}
+// G becomes the gate function of G, `slope` its derivative.
+__device__ __forceinline__ void gate_cols(bool sigmoid, Cols& G, Cols& slope) {
+    if (sigmoid) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float lo, hi;
+            unpair(G[i], lo, hi);
+            lo = sigmoid_of(lo), hi = sigmoid_of(hi);
+            G[i] = pair(lo, hi);
+            slope[i] = pair(lo * (1.0f - lo), hi * (1.0f - hi));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) slope[i] = both(1.0f);
+    }
+}
+template <typename S>
+__device__ __forceinline__ void cols_of(const Raw8<S>& r, Cols& v) {
+    float f[8];
+    r.get(f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pair(f[2 * i], f[2 * i + 1]);
+}
+
+// One vector per thread: 32 registers, so that an SM holds 2048 threads and their loads.
+template <typename S, int VPT, bool POST, bool GATE>
+__global__ void __launch_bounds__(kMaxThreadsFwd, VPT == 1 ? 2 : 1) join_fwd_kernel(const __grid_constant__ JoinFwd a) {
     __shared__ __align__(16) float red[2][32];
     pdl_wait();
     pdl_trigger();
-    const int64_t m = blockIdx.x;
-    const S* hrow = static_cast<const S*>(a.H) + m * a.ldh;
-    const __nv_bfloat16* brow = a.B + m * a.ldb;
+    const int64_t m = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;  // several short rows per CTA, a warp each
+    if (m >= a.M) return;
     Raw8<S> rh[VPT];
     Raw8<__nv_bfloat16> rb[VPT], rg[VPT];
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         const int k = (threadIdx.x + j * blockDim.x) * 8, n = a.K - k;
         if (n <= 0) continue;
-        rh[j].load(hrow + k, n);
-        rb[j].load(brow + k, n);
-        if (a.gate) rg[j].load(a.gate + m * a.ldg + k, n);
+        rb[j].load(a.B + m * a.ldb + k, n);
+        rh[j].load(static_cast<const S*>(a.H) + m * a.ldh + k, n);
+        if (GATE) rg[j].load(a.gate + m * a.ldg + k, n);
     }
-    float rp = 1.0f;
-    if (a.gamma_post) {
-        float s[1] = {0.0f};
+    float scale = a.alpha;  // alpha rp
+    if (POST) {
+        uint64_t q = 0;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             if ((int)(threadIdx.x + j * blockDim.x) * 8 >= a.K) continue;
-            float b[8];
-            rb[j].get(b);
+            Cols b;
+            cols_of(rb[j], b);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[0] = fmaf(b[i], b[i], s[0]);
+            for (int i = 0; i < 4; ++i) q = fma2(b[i], b[i], q);
         }
+        float s[1] = {sum2(q)};
         block_sum<1>(s, red[0]);
-        rp = rsqrtf(s[0] / (float)a.K + a.eps);
+        scale *= rsqrtf(s[0] / (float)a.K + a.eps);
     }
-    float h[VPT][8];
-    float s[1] = {0.0f};
+    Cols h[VPT];
+    uint64_t q = 0;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         const int k = (threadIdx.x + j * blockDim.x) * 8, n = a.K - k;
         if (n <= 0) continue;
-        float p[8];
-        rb[j].get(p);
-        if (a.gamma_post) {
+        Cols p;
+        cols_of(rb[j], p);
+        if (POST) {
             Raw8<__nv_bfloat16> r;
-            float w[8];
+            Cols w;
             r.load(a.gamma_post + k, n);
-            r.get(w);
+            cols_of(r, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = p[i] * rp * w[i];
+            for (int i = 0; i < 4; ++i) p[i] = mul2(p[i], w[i]);
         }
-        if (a.gate) {
+        if (GATE) {
             float g[8];
             rg[j].get(g);
+            if (a.sigmoid) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] *= a.sigmoid ? sigmoid_of(g[i]) : g[i];
-        }
-        rh[j].get(h[j]);
+                for (int i = 0; i < 8; ++i) g[i] = sigmoid_of(g[i]);
+            }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            h[j][i] = fmaf(a.alpha, p[i], h[j][i]);
-            if (i < n) s[0] = fmaf(h[j][i], h[j][i], s[0]);
+            for (int i = 0; i < 4; ++i) p[i] = mul2(p[i], pair(g[2 * i], g[2 * i + 1]));
         }
-        store8(static_cast<S*>(a.H_out) + m * a.ldho + k, h[j], n);
+        cols_of(rh[j], h[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // behind the last column both are 0 (a padding gate's sigmoid is not, but B is)
+            h[j][i] = fma2(both(scale), p[i], h[j][i]);
+            q = fma2(h[j][i], h[j][i], q);
+        }
+        store_cols(static_cast<S*>(a.H_out) + m * a.ldho + k, h[j], n);
     }
     if (!a.X) return;
     // X comes from the 32-bit sum, not from its rounding to the stream's type
+    float s[1] = {sum2(q)};
     block_sum<1>(s, red[1]);
     const float r = rsqrtf(s[0] / (float)a.K + a.eps);
 #pragma unroll
@@ -107,13 +162,28 @@ __global__ void __launch_bounds__(kMaxThreadsFwd) join_fwd_kernel(const __grid_c
         const int k = (threadIdx.x + j * blockDim.x) * 8, n = a.K - k;
         if (n <= 0) continue;
         Raw8<__nv_bfloat16> rw;
-        float w[8];
+        Cols w;
         rw.load(a.gamma_pre + k, n);
-        rw.get(w);
+        cols_of(rw, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = h[j][i] * r * w[i];
-        store8(a.X + m * a.ldx + k, w, n);
+        for (int i = 0; i < 4; ++i) w[i] = mul2(mul2(h[j][i], both(r)), w[i]);
+        store_cols(a.X + m * a.ldx + k, w, n);
     }
+}
+
+template <typename S, bool POST, bool GATE>
+cudaError_t launch_fwd(const JoinFwd& a, cudaStream_t st) {
+    const int64_t vecs = (a.K + 7) / 8;
+    const int vpt = vecs <= kMaxThreadsFwd ? 1 : vecs <= 2 * kMaxThreadsFwd ? 2 : 4;
+    const unsigned threads = (unsigned)((vecs + vpt * 32 - 1) / (vpt * 32) * 32);
+    auto kern = vpt == 1 ? join_fwd_kernel<S, 1, POST, GATE> : vpt == 2 ? join_fwd_kernel<S, 2, POST, GATE> : join_fwd_kernel<S, 4, POST, GATE>;
+    const unsigned rows = threads == 32 ? 8 : 1;  // 16384 x 256: 17.4 us with a CTA of one warp per row
+    return launch_kernel(kern, dim3((unsigned)((a.M + rows - 1) / rows)), dim3(threads, rows), 0, st, a);
+}
+template <typename S>
+cudaError_t launch_fwd(const JoinFwd& a, cudaStream_t st) {
+    if (a.gamma_post) return a.gate ? launch_fwd<S, true, true>(a, st) : launch_fwd<S, true, false>(a, st);
+    return a.gate ? launch_fwd<S, false, true>(a, st) : launch_fwd<S, false, false>(a, st);
 }
 
 struct JoinBwd {
@@ -130,9 +200,8 @@ struct JoinBwd {
     float* col[3];               // column sums: [groups][pitch] partial rows (or, with one group, the results) of gamma_pre,
                                  // gamma_post, channel gate; null: not asked for
     int64_t pitch;
-    int64_t lddho, lddx, ldh, ldb, ldg, lddh, lddb, lddg;
-    int64_t M;
-    int K, sigmoid, depth;
+    int lddho, lddx, ldh, ldb, ldg, lddh, lddb, lddg;
+    int M, K, sigmoid, depth;
     float alpha, eps;
 };
 
@@ -163,30 +232,6 @@ __device__ __forceinline__ void row_sum(float (&v)[NV], float* buf, float* xbuf)
     }
 }
 
-// Eight columns as four packed pairs of fp32.
-typedef uint64_t Cols[4];
-__device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
-__device__ __forceinline__ uint64_t pair_bf16(uint32_t w) { return pair(bf16_lo(w), bf16_hi(w)); }
-__device__ __forceinline__ void cols_bf16(const uint4& q, Cols& v) {
-    v[0] = pair_bf16(q.x), v[1] = pair_bf16(q.y), v[2] = pair_bf16(q.z), v[3] = pair_bf16(q.w);
-}
-__device__ __forceinline__ float sum2(uint64_t p) {
-    float lo, hi;
-    unpair(p, lo, hi);
-    return lo + hi;
-}
-template <typename T>
-__device__ __forceinline__ void store_cols(T* p, const Cols& v, int n) {
-    float f[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) unpair(v[i], f[2 * i], f[2 * i + 1]);
-    store8(p, f, n);
-}
-__device__ __forceinline__ void copy16(void* dst, const void* src, int bytes) {  // the first `bytes` of 16, zeros behind them
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes)
-                 : "memory");
-}
-
 // One row of a stage in shared memory: its tensors one after the other, each as the CTA's columns lie in memory (whole vectors
 // of 8, zeros behind the last column).
 __host__ __device__ inline int stage_bytes(int stream_size, bool gate, int columns) { return columns * (2 * stream_size + 4 + (gate ? 2 : 0)); }
@@ -203,34 +248,37 @@ __global__ void __launch_bounds__(kMaxThreadsBwd) join_bwd_kernel(const __grid_c
     __shared__ __align__(16) float red[2][4 * 32];
     __shared__ float xred[2][4 * CS];
     const int threads = blockDim.x, tid = threadIdx.x;
-    const int groups = gridDim.x / CS, rows = (int)a.M;
+    const int groups = gridDim.x / CS, rows = a.M;
     const int columns = VPT * threads * 8, first = (int)(blockIdx.x % CS) * columns;  // this CTA's
     const int stage_size = stage_bytes(sizeof(S), GATE == 2, columns);
+    const int at_d = columns * (int)sizeof(S), at_x = 2 * at_d, at_b = at_x + columns * 2, at_g = at_b + columns * 2;
     int n[VPT];  // columns of the thread's vectors (<= 0: none; such a thread takes part in copies and sums)
 #pragma unroll
     for (int j = 0; j < VPT; ++j) n[j] = a.K - first - (j * threads + tid) * 8;
 
     pdl_wait();
     pdl_trigger();
-    // chunks of 16 bytes of one row of one tensor, neighbouring threads neighbouring chunks
-    auto copy_row = [&](uint8_t* dst, const void* src, int size) {
-        const int cols = min(a.K - first, columns), bytes = cols * size, whole = (cols + 7) / 8 * 8 * size;
-        for (int i = tid * 16; i < whole; i += threads * 16) {
-            const int have = min(bytes - i, 16);
-            copy16(dst + i, static_cast<const uint8_t*>(src) + (have > 0 ? i : 0), max(have, 0));
+    // one row of one tensor: neighbouring threads copy neighbouring chunks of 16 bytes; zeros up to whole vectors
+    const int cols = min(a.K - first, columns);
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + tid * 16;
+    auto copy_row = [&](uint32_t dst, const void* src, int size) {
+        const uint8_t* p = static_cast<const uint8_t*>(src) + tid * 16;
+        int left = cols * size - tid * 16;
+#pragma unroll
+        for (int c = 0; c < VPT * size / 2; ++c) {
+            // behind the last column: the whole of its vector, from the vector's own address (nothing is read there)
+            if (left > -16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(left > 0 ? p : p - 16), "r"(min(max(left, 0), 16)) : "memory");
+            dst += threads * 16, p += threads * 16, left -= threads * 16;
         }
     };
     auto copy = [&](int m, int stage) {
-        if (m < rows && first < a.K) {
-            uint8_t* dst = ring + (size_t)stage * stage_size;
-            copy_row(dst, static_cast<const S*>(a.H) + (int64_t)m * a.ldh + first, sizeof(S));
-            dst += columns * (int)sizeof(S);
-            if (a.dHo) copy_row(dst, static_cast<const S*>(a.dHo) + (int64_t)m * a.lddho + first, sizeof(S));
-            dst += columns * (int)sizeof(S);
-            if (a.dX) copy_row(dst, a.dX + (int64_t)m * a.lddx + first, 2);
-            dst += columns * 2;
-            copy_row(dst, a.B + (int64_t)m * a.ldb + first, 2);
-            if (GATE == 2) copy_row(dst + columns * 2, a.gate + (int64_t)m * a.ldg + first, 2);
+        if (m < rows && cols > 0) {
+            uint32_t dst = ring_at + stage * stage_size;
+            copy_row(dst, static_cast<const S*>(a.H) + first + (int64_t)m * a.ldh, sizeof(S));
+            if (a.dHo) copy_row(dst + at_d, static_cast<const S*>(a.dHo) + first + (int64_t)m * a.lddho, sizeof(S));
+            if (a.dX) copy_row(dst + at_x, a.dX + first + (int64_t)m * a.lddx, 2);
+            copy_row(dst + at_b, a.B + first + (int64_t)m * a.ldb, 2);
+            if (GATE == 2) copy_row(dst + at_g, a.gate + first + (int64_t)m * a.ldg, 2);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -250,37 +298,39 @@ __global__ void __launch_bounds__(kMaxThreadsBwd) join_bwd_kernel(const __grid_c
         }
     };
     auto half_cols = [&](const uint8_t* p, int j, Cols& v) { cols_bf16(*reinterpret_cast<const uint4*>(p + (j * threads + tid) * 16), v); };
-    const int at_d = columns * (int)sizeof(S), at_x = 2 * at_d, at_b = at_x + columns * 2, at_g = at_b + columns * 2;
 
     int m = blockIdx.x / CS, ahead = m;  // this row, and the next one to copy
     for (int d = 0; d < a.depth - 1; ++d, ahead += groups) copy(ahead, d);
 
     const float inv_k = 1.0f / (float)a.K;
-    uint4 wpre[VPT], wpost[VPT], wgate[VPT];  // bf16, as they lie in memory
+    uint4 wpre[VPT];   // gamma_pre, bf16 as it lies in memory
+    Cols scale[VPT];   // alpha gamma_post, times the channel gate's function
     Cols acc_pre[VPT], acc_post[VPT];
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         Raw8<__nv_bfloat16> r;
         const int col = first + (j * threads + tid) * 8;
-        wpre[j] = wpost[j] = wgate[j] = make_uint4(0u, 0u, 0u, 0u);
+        wpre[j] = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc_pre[j][i] = acc_post[j][i] = 0;
+        for (int i = 0; i < 4; ++i) acc_pre[j][i] = acc_post[j][i] = 0, scale[j][i] = both(a.alpha);
         if (n[j] <= 0) continue;
         if (a.dX) r.load(a.gamma_pre + col, n[j]), wpre[j] = r.q;
-        if (POST) r.load(a.gamma_post + col, n[j]), wpost[j] = r.q;
-        if (GATE == 1) r.load(a.gate + col, n[j]), wgate[j] = r.q;
-    }
-    auto gate_of = [&](uint64_t G, uint64_t& slope) {
-        float lo, hi;
-        unpair(G, lo, hi);
-        if (a.sigmoid) {
-            lo = sigmoid_of(lo), hi = sigmoid_of(hi);
-            slope = pair(lo * (1.0f - lo), hi * (1.0f - hi));
-        } else {
-            slope = both(1.0f);
+        Cols w;
+        if (POST) {
+            r.load(a.gamma_post + col, n[j]);
+            cols_of(r, w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) scale[j][i] = mul2(scale[j][i], w[i]);
         }
-        return pair(lo, hi);
-    };
+        if (GATE == 1) {
+            Cols slope;
+            r.load(a.gate + col, n[j]);
+            cols_of(r, w);
+            gate_cols(a.sigmoid, w, slope);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) scale[j][i] = mul2(scale[j][i], w[i]);
+        }
+    }
     // sums of the row in stage p: H'^2, dX gamma_pre H', B^2
     auto first_sums = [&](const uint8_t* p, float (&s)[4]) {
         uint64_t sh = 0, su = 0, sb = 0;
@@ -327,7 +377,7 @@ __global__ void __launch_bounds__(kMaxThreadsBwd) join_bwd_kernel(const __grid_c
         for (int j = 0; j < VPT; ++j) {
             if (n[j] <= 0) continue;
             const int col = first + (j * threads + tid) * 8;
-            Cols d, w;
+            Cols d;
             if (a.dHo) {
                 stream_cols(p + at_d, j, d);
             } else {
@@ -335,38 +385,36 @@ __global__ void __launch_bounds__(kMaxThreadsBwd) join_bwd_kernel(const __grid_c
                 for (int i = 0; i < 4; ++i) d[i] = 0;
             }
             if (a.dX) {
-                Cols h, u;
+                Cols h, u, w;
                 stream_cols(p, j, h);
                 half_cols(p + at_x, j, u);
                 cols_bf16(wpre[j], w);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint64_t hr = mul2(h[i], both(r)), ur = mul2(u[i], both(r));
-                    acc_pre[j][i] = fma2(u[i], hr, acc_pre[j][i]);
+                    const uint64_t ur = mul2(u[i], both(r));
+                    acc_pre[j][i] = fma2(ur, h[i], acc_pre[j][i]);
                     d[i] = fma2(ur, w[i], fma2(both(c), h[i], d[i]));
                 }
             }
             store_cols(static_cast<S*>(a.dH) + (int64_t)m * a.lddh + col, d, n[j]);
             half_cols(p + at_b, j, nb[j]);
             Cols G, dg;
-            if (GATE == 2) half_cols(p + at_g, j, G);
-            else if (GATE == 1) cols_bf16(wgate[j], G);
-            if (POST) cols_bf16(wpost[j], w);
+            if (GATE == 2) {
+                half_cols(p + at_g, j, G);
+                gate_cols(a.sigmoid, G, dg);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (POST) nb[j][i] = mul2(nb[j][i], both(rp));
                 const uint64_t dn = mul2(d[i], nb[j][i]);
-                uint64_t dp = mul2(d[i], both(a.alpha)), slope = 0;
-                if (GATE != 0) {
-                    const uint64_t g = gate_of(G[i], slope);
-                    dp = mul2(dp, g);
-                    if (GATE == 2) {
-                        dg[i] = mul2(mul2(dn, both(a.alpha)), slope);
-                        if (POST) dg[i] = mul2(dg[i], w[i]), acc_post[j][i] = fma2(dn, g, acc_post[j][i]);
-                    }
+                v[j][i] = mul2(d[i], scale[j][i]);
+                if (GATE == 2) {
+                    acc_post[j][i] = fma2(dn, G[i], acc_post[j][i]);
+                    dg[i] = mul2(mul2(dn, scale[j][i]), dg[i]);
+                    v[j][i] = mul2(v[j][i], G[i]);
+                } else {
+                    acc_post[j][i] = add2(acc_post[j][i], dn);
                 }
-                if (GATE != 2) acc_post[j][i] = add2(acc_post[j][i], dn);
-                v[j][i] = POST ? mul2(dp, w[i]) : dp;
                 if (POST) t2 = fma2(v[j][i], nb[j][i], t2);
             }
             if (GATE == 2) store_cols(a.dgate + (int64_t)m * a.lddg + col, dg, n[j]);
@@ -405,20 +453,20 @@ __global__ void __launch_bounds__(kMaxThreadsBwd) join_bwd_kernel(const __grid_c
                 if (i < n[j]) p[i] = f[i];
         };
         put(0, acc_pre[j]);
-        Cols w, G, x;
-        if (POST) {
-            cols_bf16(wpost[j], w);
-        } else {
+        if (!POST && GATE != 1) continue;
+        // acc_post: the column sum of d n (times the gate, if it has one per token)
+        Raw8<__nv_bfloat16> r;
+        const int col = first + (j * threads + tid) * 8;
+        Cols w, G, slope, x;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = both(1.0f);
-        }
-        if (GATE == 1) cols_bf16(wgate[j], G);
+        for (int i = 0; i < 4; ++i) w[i] = G[i] = both(1.0f);
+        if (POST) r.load(a.gamma_post + col, n[j]), cols_of(r, w);
+        if (GATE == 1) r.load(a.gate + col, n[j]), cols_of(r, G), gate_cols(a.sigmoid, G, slope);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            uint64_t slope = both(1.0f), g = both(1.0f);
-            if (GATE == 1) g = gate_of(G[i], slope);
-            x[i] = mul2(mul2(acc_post[j][i], both(a.alpha)), mul2(slope, w[i]));
-            acc_post[j][i] = mul2(mul2(acc_post[j][i], both(a.alpha)), g);
+            const uint64_t sum = mul2(acc_post[j][i], both(a.alpha));
+            if (GATE == 1) x[i] = mul2(mul2(sum, slope[i]), w[i]);
+            acc_post[j][i] = mul2(sum, G[i]);
         }
         if (POST) put(1, acc_post[j]);
         if (GATE == 1) put(2, x);
@@ -429,9 +477,9 @@ __global__ void __launch_bounds__(kMaxThreadsBwd) join_bwd_kernel(const __grid_c
     }
 }
 
-// Sum of the P partial rows: a block owns 32 columns, each of its 16 warps adds a contiguous run of rows with eight loads in
-// flight, and the 16 sums are added in order.
-constexpr int kSumWarps = 16;
+// Sum of the P partial rows: a block owns 32 columns, each of its 32 warps adds a contiguous run of rows with 16 loads in
+// flight, and the 32 sums are added in order.
+constexpr int kSumWarps = 32;
 struct JoinSum {
     const float* part[3];
     float* out[3];
@@ -447,11 +495,15 @@ __global__ void __launch_bounds__(kSumWarps * 32) join_sum_kernel(const __grid_c
     float s = 0.0f;
     if (col < a.K) {
         const float* src = a.part[which] + col;
-        for (int p = p0; p < p1; p += 8) {
-            float v[8];
+        for (int p = p0; p < p1; p += 16) {
+            float v[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = p + i < p1 ? src[(p + i) * a.pitch] : 0.0f;
-            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+            for (int i = 0; i < 16; ++i) v[i] = p + i < p1 ? src[(p + i) * a.pitch] : 0.0f;
+#pragma unroll
+            for (int o = 8; o > 0; o /= 2)
+#pragma unroll
+                for (int i = 0; i < o; ++i) v[i] += v[i + o];
+            s += v[0];
         }
     }
     buf[w][lane] = s;
@@ -566,18 +618,11 @@ int resq_block_join(const void* H, int stream_dtype, const void* B, int64_t M, i
     a.gamma_pre = static_cast<const __nv_bfloat16*>(gamma_pre);
     a.H_out = H_out;
     a.X = static_cast<__nv_bfloat16*>(X);
-    a.ldh = ldh, a.ldb = ldb, a.ldg = ldg, a.ldho = ldho, a.ldx = ldx;
+    a.M = M, a.ldh = ldh, a.ldb = ldb, a.ldg = ldg, a.ldho = ldho, a.ldx = ldx;
     a.K = (int)K, a.sigmoid = gate_act == RESQ_GATE_SIGMOID, a.alpha = alpha, a.eps = eps;
-    const int64_t vecs = (K + 7) / 8;
-    const int vpt = vecs <= kMaxThreadsFwd ? 1 : vecs <= 2 * kMaxThreadsFwd ? 2 : 4;
-    const unsigned threads = (unsigned)((vecs + vpt * 32 - 1) / (vpt * 32) * 32);
-    const bool f32 = stream_dtype == RESQ_OUT_F32;
-    auto kern = vpt == 1   ? (f32 ? join_fwd_kernel<float, 1> : join_fwd_kernel<__nv_bfloat16, 1>)
-                : vpt == 2 ? (f32 ? join_fwd_kernel<float, 2> : join_fwd_kernel<__nv_bfloat16, 2>)
-                           : (f32 ? join_fwd_kernel<float, 4> : join_fwd_kernel<__nv_bfloat16, 4>);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     LaunchScope scope(kKindRow, st);
-    return cuda_fail(launch_kernel(kern, dim3((unsigned)M), dim3(threads), 0, st, a), "join_fwd_kernel launch");
+    return cuda_fail(stream_dtype == RESQ_OUT_F32 ? launch_fwd<float>(a, st) : launch_fwd<__nv_bfloat16>(a, st), "join_fwd_kernel launch");
 }
 
 size_t resq_block_join_backward_workspace_bytes(int64_t M, int64_t K) {
@@ -604,6 +649,8 @@ int resq_block_join_backward(const void* dH_out, const void* dX, const void* H_o
     if (gate && (ldg == 0 ? !is_aligned(dgate, 4) : !rows_aligned(dgate, lddg, K, RESQ_OUT_BF16)))
         return fail(RESQ_ERR_ALIGN, what, "dgate needs a 16-byte aligned base and rows, lddg >= K (a channel gate: fp32 [K])");
     if (gamma_post && !is_aligned(dgamma_post, 4)) return fail(RESQ_ERR_ALIGN, what, "dgamma_post is not aligned");
+    for (int64_t ld : {dH_out ? lddho : 0, dX ? lddx : 0, ldho, ldb, gate ? ldg : 0, lddh, lddb, gate && ldg != 0 ? lddg : 0})
+        if (ld > INT32_MAX) return fail(RESQ_ERR_SHAPE, what, "a row pitch is 2^31 elements or more");
     const size_t need = resq_block_join_backward_workspace_bytes(M, K);
     if (!workspace || !is_aligned(workspace, 256) || ws_bytes < need) {
         set_last_error("workspace: need %zu bytes, 256-byte aligned (have %zu at %p)", need, ws_bytes, workspace);
@@ -620,8 +667,9 @@ int resq_block_join_backward(const void* dH_out, const void* dX, const void* H_o
     a.dH = dH;
     a.dB = static_cast<__nv_bfloat16*>(dB);
     a.dgate = gate && ldg != 0 ? static_cast<__nv_bfloat16*>(dgate) : nullptr;
-    a.lddho = lddho, a.lddx = lddx, a.ldh = ldho, a.ldb = ldb, a.ldg = ldg, a.lddh = lddh, a.lddb = lddb, a.lddg = lddg;
-    a.M = M, a.K = (int)K, a.sigmoid = gate_act == RESQ_GATE_SIGMOID, a.alpha = alpha, a.eps = eps;
+    a.lddho = (int)lddho, a.lddx = (int)lddx, a.ldh = (int)ldho, a.ldb = (int)ldb, a.ldg = (int)ldg;
+    a.lddh = (int)lddh, a.lddb = (int)lddb, a.lddg = (int)lddg;
+    a.M = (int)M, a.K = (int)K, a.sigmoid = gate_act == RESQ_GATE_SIGMOID, a.alpha = alpha, a.eps = eps;
     const BwdShape shape = bwd_shape(M, K, stream_dtype == RESQ_OUT_F32 ? 4 : 2, gate && ldg != 0);
     float* const results[3] = {dX ? dgamma_pre : nullptr, gamma_post ? dgamma_post : nullptr,
                                gate && ldg == 0 ? static_cast<float*>(dgate) : nullptr};

@@ -73,7 +73,7 @@ JOIN_BWD = dict(dH_out=P, dX=P, H_out=P, dtype=0, B=P, M=4, K=100, lddho=104, ld
 JOIN_BWD_BAD = [
     (NULL, dict(dH_out=None, dX=None)), (NULL, dict(H_out=None)), (NULL, dict(B=None)), (NULL, dict(dH=None)), (NULL, dict(dB=None)),
     (NULL, dict(gamma_pre=None)), (NULL, dict(dgamma_pre=None)), (NULL, dict(dgamma_post=None)), (NULL, dict(dgate=None)),
-    (SHAPE, dict(M=0)), (SHAPE, dict(K=-8)), (SHAPE, dict(eps=-1e-9)), (SHAPE, dict(alpha=float("inf"))),
+    (SHAPE, dict(M=0)), (SHAPE, dict(K=-8)), (SHAPE, dict(lddx=2 ** 31)), (SHAPE, dict(lddg=2 ** 32 + 104)), (SHAPE, dict(eps=-1e-9)), (SHAPE, dict(alpha=float("inf"))),
     (PATTERN, dict(dtype=7)), (PATTERN, dict(act=9)),
     (ALIGN, dict(dH_out=P + 2)), (ALIGN, dict(dX=P + 2)), (ALIGN, dict(dH=P + 8)), (ALIGN, dict(dB=P + 8)), (ALIGN, dict(dgate=P + 8)),
     (ALIGN, dict(lddho=96)), (ALIGN, dict(lddx=99)), (ALIGN, dict(lddh=100)), (ALIGN, dict(lddb=0)), (ALIGN, dict(lddg=0)),

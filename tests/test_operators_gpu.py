@@ -214,7 +214,7 @@ def wide(v):
     return [None if t is None else t.double() for t in v]
 
 
-SHAPES = [(1, 1), (1, 8), (3, 5), (2, 64), (5, 257), (4, 1000), (300, 96), (2, 2048), (33, 3584), (3, 5003), (2, 8200), (7, 5130), (2, 18944), (3, 26000), (1, 32768)]
+SHAPES = [(1, 1), (1, 8), (3, 5), (2, 64), (5, 257), (4, 1000), (300, 96), (2, 2048), (33, 3584), (3, 5003), (2, 8200), (7, 5130), (2, 18944), (3, 24577), (3, 26000), (1, 32768)]
 FORMS = [(BF, False, "none", "linear"), (F32, True, "channel", "linear"), (BF, True, "full", "sigmoid"), (F32, False, "channel", "sigmoid"),
          (BF, True, "none", "linear"), (F32, False, "full", "linear")]
 
