@@ -18,8 +18,10 @@ namespace resq {
 namespace {
 
 constexpr int kMaxThreadsFwd = 1024;  // one row: up to 4 vectors of 8 per thread
-constexpr int kMaxThreadsBwd = 512;   // eight or sixteen columns per thread; longer rows are split over a cluster of 2 or 4 CTAs
-static_assert(kMaxThreadsFwd * 8 * 4 >= RESQ_JOIN_MAX_K && kMaxThreadsBwd * 16 * 4 >= RESQ_JOIN_MAX_K, "row length");
+// Backward, threads per SM: 512 of 128 registers; 640 of 96 where a row is split over a cluster (they spill nothing either, but
+// measured slower on short rows: 8192 x 2048, fp32 stream, 69 against 61 us).
+constexpr int bwd_threads(int cs) { return cs == 1 ? 512 : 640; }
+static_assert(kMaxThreadsFwd * 8 * 4 >= RESQ_JOIN_MAX_K && bwd_threads(8) * 8 * 8 >= RESQ_JOIN_MAX_K, "row length");
 
 struct JoinFwd {
     const void* H;
@@ -243,7 +245,7 @@ constexpr int kMaxDepth = 6;
 // row are taken together, so a row costs one barrier.  Without a gate per token the gradients of gamma_post and of the channel
 // gate are the same column sum of d n times a constant of the column.
 template <typename S, bool POST, int GATE, int VPT, int CS>
-__global__ void __launch_bounds__(kMaxThreadsBwd) join_bwd_kernel(const __grid_constant__ JoinBwd a) {
+__global__ void __launch_bounds__(bwd_threads(CS)) join_bwd_kernel(const __grid_constant__ JoinBwd a) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ __align__(16) float red[2][4 * 32];
     __shared__ float xred[2][4 * CS];
@@ -517,9 +519,7 @@ __global__ void __launch_bounds__(kSumWarps * 32) join_sum_kernel(const __grid_c
 }
 
 // ---- host side -----------------------------------------------------------------------------------
-constexpr int kSms = 148;
-
-// Split of a row: vectors per thread, CTAs, threads; CTAs per SM (512 threads of 128 registers; each holds at least three rows
+// Split of a row: vectors per thread, CTAs, threads; CTAs per SM (each holds at least three rows
 // in shared memory, for which long rows are split further); groups of CTAs that share the rows.
 constexpr int kSmemSm = 224 * 1024, kSmemStatic = 2048;
 struct BwdShape {
@@ -529,17 +529,19 @@ struct BwdShape {
 BwdShape bwd_shape(int64_t M, int64_t K, int stream_size, bool gate) {
     const int64_t vecs = (K + 7) / 8;
     BwdShape s;
-    s.vpt = vecs <= kMaxThreadsBwd ? 1 : 2;
     int stage = 0;
-    for (s.cs = 1;; s.cs *= 2) {
+    // one CTA with one vector per thread, then with two, then clusters (2000 x 18944 in four CTAs of one vector: 0.8 of the time of two)
+    for (s.vpt = 1, s.cs = 1;;) {
         const int64_t per = (int64_t)s.cs * s.vpt * 32;
         s.threads = (int)((vecs + per - 1) / per * 32);
         stage = stage_bytes(stream_size, gate, s.vpt * s.threads * 8);
-        if (s.threads <= kMaxThreadsBwd && 3 * stage <= kSmemSm - kSmemStatic) break;
+        if (s.threads <= bwd_threads(s.cs) && 3 * stage <= kSmemSm - kSmemStatic) break;
+        if (s.vpt == 1 && s.cs == 1) s.vpt = 2;
+        else s.vpt = 1, s.cs *= 2;
     }
-    s.per_sm = std::min(kMaxThreadsBwd / s.threads, kSmemSm / (3 * stage + kSmemStatic));
+    s.per_sm = std::min(bwd_threads(s.cs) / s.threads, kSmemSm / (3 * stage + kSmemStatic));
     s.depth = std::min(kMaxDepth, (kSmemSm / s.per_sm - kSmemStatic) / stage);
-    s.groups = std::min<int64_t>(M, std::max(1, kSms * s.per_sm / s.cs));
+    s.groups = std::min<int64_t>(M, resident_clusters(s.cs) * s.per_sm);
     return s;
 }
 int64_t bwd_most_groups(int64_t M, int64_t K) {
@@ -562,10 +564,13 @@ int launch_bwd(const BwdShape& s, JoinBwd a, cudaStream_t st) {
 }
 template <typename S, bool POST, int GATE>
 int launch_bwd(const BwdShape& s, const JoinBwd& a, cudaStream_t st) {
-    if (s.vpt == 1) return launch_bwd<S, POST, GATE, 1, 1>(s, a, st);
-    if (s.cs == 1) return launch_bwd<S, POST, GATE, 2, 1>(s, a, st);
-    if (s.cs == 2) return launch_bwd<S, POST, GATE, 2, 2>(s, a, st);
-    return s.cs == 4 ? launch_bwd<S, POST, GATE, 2, 4>(s, a, st) : launch_bwd<S, POST, GATE, 2, 8>(s, a, st);
+    if (s.vpt == 2) return launch_bwd<S, POST, GATE, 2, 1>(s, a, st);
+    switch (s.cs) {
+        case 1: return launch_bwd<S, POST, GATE, 1, 1>(s, a, st);
+        case 2: return launch_bwd<S, POST, GATE, 1, 2>(s, a, st);
+        case 4: return launch_bwd<S, POST, GATE, 1, 4>(s, a, st);
+        default: return launch_bwd<S, POST, GATE, 1, 8>(s, a, st);
+    }
 }
 template <typename S>
 int launch_bwd(const BwdShape& s, const JoinBwd& a, cudaStream_t st) {

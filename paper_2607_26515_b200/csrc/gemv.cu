@@ -440,9 +440,6 @@ struct GemvPlan {
 };
 
 constexpr size_t kSmemMax = 227 * 1024;
-// Clusters of 1, 2, 4, 8 CTAs that are resident at once, one CTA per SM (larger clusters leave SMs of a GPC unused).
-constexpr int kSlots[4] = {148, 74, 33, 15};
-
 // Splits the K range over cs CTAs and gives each cluster T row tiles so that the busiest SM finishes first.  Cycles per unit
 // and the fixed costs are rough measurements; only their proportions matter.
 GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
@@ -456,7 +453,7 @@ GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
             const size_t smem = x + ring + part_bytes(cs, T, nt);
             if (smem > kSmemMax) break;
             const int64_t clusters = (tiles + T - 1) / T;
-            const double waves = (double)((clusters + kSlots[lg] - 1) / kSlots[lg]);
+            const double waves = (double)((clusters + resident_clusters(cs) - 1) / resident_clusters(cs));
             const double cost = waves * ((double)((T * us + kWarps - 1) / kWarps) * 1200 + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
             if (best.cs == 0 || cost < best_cost) best = GemvPlan{cs, T, us, smem}, best_cost = cost;
         }

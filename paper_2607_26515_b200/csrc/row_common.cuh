@@ -16,6 +16,10 @@ inline bool rows_aligned(const void* p, int64_t ld, int64_t cols, int dtype) {
     return is_aligned(p, 16) && ld >= cols && ld % (dtype == RESQ_OUT_BF16 ? 8 : 4) == 0;
 }
 
+// Clusters of cs CTAs that are resident at once with one CTA per SM, as the occupancy query answers on a B200: larger clusters
+// leave SMs of a GPC unused.
+inline int resident_clusters(int cs) { return cs == 1 ? 148 : cs == 2 ? 74 : cs == 4 ? 33 : 15; }
+
 #ifdef __CUDACC__
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
