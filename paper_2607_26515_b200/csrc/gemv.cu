@@ -266,21 +266,21 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     // ---- activations of this slice: chunks of 8, pairs (i, i + 4) side by side, chunk (lane t, word w) of a unit at
     // (4 w + t) * 16 bytes, so that the four lanes of a quad read 64 consecutive bytes
     constexpr int kBatch = 8;  // loads in flight per thread: the staging is latency, not bandwidth
-    for (int j = threadIdx.x; j < a.units_slice * 16; j += kThreads) {
-        const int k = k0 + j * 8;
-        uint8_t* dst = smem + (j >> 4) * 256 + ((j & 3) * 4 + ((j >> 2) & 3)) * 16;
-        const __nv_bfloat16* src = a.X + k;
-        for (int m0 = 0; m0 < a.M; m0 += kBatch) {
+    const int lg = a.M > 4 ? 3 : a.M > 2 ? 2 : a.M > 1 ? 1 : 0, chunks = a.units_slice * 16;  // 2^lg tokens x 8 / 2^lg chunks
+    for (int m0 = 0; m0 < a.M; m0 += kBatch) {
+        for (int j0 = threadIdx.x; j0 < chunks; j0 += kThreads << (3 - lg)) {
             uint4 v[kBatch];
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
+                const int j = j0 + (b >> lg) * kThreads, m = m0 + (b & ((1 << lg) - 1)), k = k0 + j * 8;
                 v[b] = make_uint4(0u, 0u, 0u, 0u);
-                if (m0 + b < a.M && k < a.K) v[b] = *reinterpret_cast<const uint4*>(src + (m0 + b) * a.ldx);
+                if (m < a.M && j < chunks && k < a.K) v[b] = *reinterpret_cast<const uint4*>(a.X + m * a.ldx + k);
             }
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
-                if (m0 + b >= a.M) break;
-                *reinterpret_cast<uint4*>(dst + (m0 + b) * xrow) =
+                const int j = j0 + (b >> lg) * kThreads, m = m0 + (b & ((1 << lg) - 1));
+                if (m >= a.M || j >= chunks) continue;
+                *reinterpret_cast<uint4*>(smem + m * xrow + (j >> 4) * 256 + ((j & 3) * 4 + ((j >> 2) & 3)) * 16) =
                     make_uint4(__byte_perm(v[b].x, v[b].z, 0x5410), __byte_perm(v[b].x, v[b].z, 0x7632), __byte_perm(v[b].y, v[b].w, 0x5410),
                                __byte_perm(v[b].y, v[b].w, 0x7632));
             }
@@ -379,55 +379,58 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     }
 
     // ---- tiles that several warps (and slices) share, in order
+    __syncthreads();
+    const int rows = min(tiles * kTileN, a.N - tile0 * kTileN);
+    // this CTA's sum for row r of its tiles and token m, from the warps that had a part of it; with slices it replaces the first
+    // part, of which nobody else reads this element
+    for (int r = threadIdx.x; r < rows; r += kThreads) {
+        const int tile = r / kTileN, u0 = tile * units, u1 = u0 + units;
+        int w0 = kWarps, w1 = -1;
+        for (int w = 0; w < kWarps; ++w) {
+            const int f = total * w / kWarps, l = total * (w + 1) / kWarps;
+            if (f < u1 && l > u0 && f < l) w0 = min(w0, w), w1 = w;
+        }
+        if (CS == 1 && w0 >= w1) continue;  // one warp had the tile and has written it
+        float* const src = part + (r % kTileN) * (8 * NT);
+        for (int m = 0; m < a.M; ++m) {
+            float s = 0.0f;
+            for (int w = w0; w <= w1; ++w) {
+                const int f = total * w / kWarps, l = total * (w + 1) / kWarps;
+                if (f < l) s += src[(CS > 1 ? tile + w : w * 2 + (f < u0 ? 1 : 0)) * kSlot + m];
+            }
+            if (CS == 1) store_out(a, m, tile0 * kTileN + r, s * Scale<FMT>::kBack);
+            else if (w1 >= 0) src[(tile + w0) * kSlot + m] = s;
+        }
+    }
     if (CS > 1) {
+        // every slice's sum, in order; a slice without units (the last ones of a short K) has none
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-    } else {
-        __syncthreads();
-    }
-    const int rows = min(tiles * kTileN, a.N - tile0 * kTileN);
-    for (int r = threadIdx.x; r < rows; r += kThreads) {
-        const int tile = r / kTileN;
-        if (CS == 1) {
-            const int u0 = tile * units, u1 = u0 + units;
-            int w0 = kWarps, w1 = -1;
-            for (int w = 0; w < kWarps; ++w) {
-                const int f = total * w / kWarps, l = total * (w + 1) / kWarps;
-                if (f < u1 && l > u0 && f < l) w0 = min(w0, w), w1 = w;
+        for (int r = threadIdx.x; r < rows; r += kThreads) {
+            const int tile = r / kTileN;
+            uint32_t at[CS];
+#pragma unroll
+            for (int c = 0; c < CS; ++c) {
+                const int cunits = max(0, min(a.units_slice, units_all - c * a.units_slice)), ctotal = tiles * cunits;
+                int w0 = 0;  // the first warp of that slice with a part of the tile
+                while (w0 < kWarps - 1 && ctotal * (w0 + 1) / kWarps <= tile * cunits) ++w0;
+                const uint32_t local = (uint32_t)__cvta_generic_to_shared(part + (size_t)(tile + w0) * kSlot + (r % kTileN) * (8 * NT));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at[c]) : "r"(local), "r"(c));
+                if (cunits == 0) at[c] = 0;
             }
-            if (w0 >= w1) continue;  // one warp had it
-            const float* src = part + (r % kTileN) * (8 * NT);
-            for (int m = 0; m < a.M; ++m) {
-                float s = 0.0f;
-                for (int w = w0; w <= w1; ++w) {
-                    const int f = total * w / kWarps, l = total * (w + 1) / kWarps;
-                    if (f < l) s += src[(w * 2 + (f < u0 ? 1 : 0)) * kSlot + m];
-                }
-                store_out(a, m, tile0 * kTileN + r, s * Scale<FMT>::kBack);
-            }
-        } else {
-            const float* slot = part + (size_t)tile * kSlot + (r % kTileN) * (8 * NT);
             for (int m = rank; m < a.M; m += CS) {
-                float s = 0.0f;
+                float v[CS], s = 0.0f;
 #pragma unroll
                 for (int c = 0; c < CS; ++c) {
-                    const int cunits = max(0, min(a.units_slice, units_all - c * a.units_slice));
-                    const int ctotal = tiles * cunits, u0 = tile * cunits, u1 = u0 + cunits;
-                    for (int w = 0; w < kWarps; ++w) {
-                        const int f = ctotal * w / kWarps, l = ctotal * (w + 1) / kWarps;
-                        if (f >= u1 || l <= u0 || f >= l) continue;
-                        uint32_t remote;
-                        float v;
-                        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"((uint32_t)__cvta_generic_to_shared(slot + w * kSlot + m)), "r"(c));
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
-                        s += v;
-                    }
+                    v[c] = 0.0f;
+                    if (at[c]) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[c]) : "r"(at[c] + m * 4));
                 }
+#pragma unroll
+                for (int c = 0; c < CS; ++c) s += v[c];
                 store_out(a, m, tile0 * kTileN + r, s * Scale<FMT>::kBack);
             }
         }
-    }
-    if (CS > 1) {  // no CTA leaves while a peer may still read its shared memory
+        // no CTA leaves while a peer may still read its shared memory
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
