@@ -170,8 +170,12 @@ __device__ __forceinline__ void store_out(const GemvArgs& a, int m, int n, float
     else static_cast<float*>(a.Y)[m * a.ldy + n] = v;
 }
 
-// Slots of 16 x 8 NT partial sums: without slices two per warp (the tile its run starts in and the one it ends in), with slices
+// Slots of 8 NT tokens x 16 rows of partial sums: token pairs at a pitch of 32 floats, a pair's rows turned by four places from
+// pair to pair (a warp's stores from the accumulator layout and its loads of neighbouring rows then meet no bank twice): without slices two per warp (the tile its run starts in and the one it ends in), with slices
 // one per (tile, warp) of a run, at tile + warp (both only grow along the runs).
+__device__ __forceinline__ int part_at(int token, int row) {
+    return (token >> 1) * 32 + ((row + 4 * (token >> 1)) & 15) * 2 + (token & 1);
+}
 template <int FMT>
 __host__ __device__ constexpr size_t ring_bytes() {
     return (size_t)kWarps * kRing * (kStep * 1024 + kSideBytes<FMT>);
@@ -365,8 +369,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
                 float* out = part + (size_t)(CS > 1 ? ct + warp : warp * 2 + (i - cu > first ? 1 : 0)) * kSlot;
 #pragma unroll
                 for (int q = 0; q < NT; ++q) {
-                    *reinterpret_cast<float2*>(out + g * (8 * NT) + q * 8 + t * 2) = make_float2(acc[q][0], acc[q][1]);
-                    *reinterpret_cast<float2*>(out + (g + 8) * (8 * NT) + q * 8 + t * 2) = make_float2(acc[q][2], acc[q][3]);
+                    *reinterpret_cast<float2*>(out + part_at(q * 8 + t * 2, g)) = make_float2(acc[q][0], acc[q][1]);
+                    *reinterpret_cast<float2*>(out + part_at(q * 8 + t * 2, g + 8)) = make_float2(acc[q][2], acc[q][3]);
                 }
             }
 #pragma unroll
@@ -380,55 +384,69 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
 
     // ---- tiles that several warps (and slices) share, in order
     __syncthreads();
-    const int rows = min(tiles * kTileN, a.N - tile0 * kTileN);
-    // this CTA's sum for row r of its tiles and token m, from the warps that had a part of it; with slices it replaces the first
-    // part, of which nobody else reads this element
-    for (int r = threadIdx.x; r < rows; r += kThreads) {
-        const int tile = r / kTileN, u0 = tile * units, u1 = u0 + units;
-        int w0 = kWarps, w1 = -1;
-        for (int w = 0; w < kWarps; ++w) {
-            const int f = total * w / kWarps, l = total * (w + 1) / kWarps;
-            if (f < u1 && l > u0 && f < l) w0 = min(w0, w), w1 = w;
-        }
-        if (CS == 1 && w0 >= w1) continue;  // one warp had the tile and has written it
-        float* const src = part + (r % kTileN) * (8 * NT);
-        for (int m = 0; m < a.M; ++m) {
-            float s = 0.0f;
-            for (int w = w0; w <= w1; ++w) {
-                const int f = total * w / kWarps, l = total * (w + 1) / kWarps;
-                if (f < l) s += src[(CS > 1 ? tile + w : w * 2 + (f < u0 ? 1 : 0)) * kSlot + m];
+    auto first_of = [&](int w) { return total * w / kWarps; };
+    // the parts of the warps from w on whose runs start before unit `end`, four loads at a time
+    auto sum_parts = [&](const float* src, int pitch, int w, int end) {
+        float s = 0.0f;
+        for (; w < kWarps && first_of(w) < end; w += 4) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int f = first_of(w + i);
+                v[i] = w + i < kWarps && f < end && f < first_of(w + i + 1) ? src[(w + i) * pitch] : 0.0f;
             }
-            if (CS == 1) store_out(a, m, tile0 * kTileN + r, s * Scale<FMT>::kBack);
-            else if (w1 >= 0) src[(tile + w0) * kSlot + m] = s;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s += v[i];
+        }
+        return s;
+    };
+    // element o: row o % 16 of tile (o / 16) % tiles, token o / 16 / tiles
+    const int outs = tiles * kTileN * a.M;
+    if (CS == 1) {
+        // A tile is shared if a warp's run starts inside it; the first such warp adds its parts.
+        const int tile = units > 0 ? first / units : 0, u0 = tile * units, u1 = u0 + units;
+        int w0 = warp - 1;
+        while (w0 >= 0 && first_of(w0) == first_of(w0 + 1)) --w0;  // runs without units
+        if (first < last && w0 >= 0 && first > u0 && first_of(w0) <= u0) {
+            for (int m = lane >> 4; m < a.M; m += 2) {
+                const float* src = part + part_at(m, lane & 15);
+                const float s = src[(w0 * 2 + (first_of(w0) < u0 ? 1 : 0)) * kSlot] + sum_parts(src, 2 * kSlot, warp, u1);
+                const int n = (tile0 + tile) * kTileN + (lane & 15);
+                if (n < a.N) store_out(a, m, n, s * Scale<FMT>::kBack);
+            }
+        }
+    } else {
+        // this slice's sum replaces the first warp's part, of which nobody else reads this element
+        for (int o = threadIdx.x; o < outs && units > 0; o += kThreads) {
+            const int m = (o >> 4) / tiles, tile = (o >> 4) - m * tiles, u0 = tile * units, u1 = u0 + units;
+            float* const src = part + part_at(m, o & 15) + tile * kSlot;
+            const int w0 = ((u0 + 1) * kWarps + total - 1) / total - 1;  // the warp that has its first unit
+            src[w0 * kSlot] += sum_parts(src, kSlot, w0 + 1, u1);
         }
     }
     if (CS > 1) {
         // every slice's sum, in order; a slice without units (the last ones of a short K) has none
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-        for (int r = threadIdx.x; r < rows; r += kThreads) {
-            const int tile = r / kTileN;
-            uint32_t at[CS];
+        for (int o = rank * kThreads + threadIdx.x; o < outs; o += CS * kThreads) {
+            const int m = (o >> 4) / tiles, tile = (o >> 4) - m * tiles, n = (tile0 + tile) * kTileN + (o & 15);
+            if (n >= a.N) continue;
+            float v[CS], s = 0.0f;
 #pragma unroll
             for (int c = 0; c < CS; ++c) {
                 const int cunits = max(0, min(a.units_slice, units_all - c * a.units_slice)), ctotal = tiles * cunits;
-                int w0 = 0;  // the first warp of that slice with a part of the tile
-                while (w0 < kWarps - 1 && ctotal * (w0 + 1) / kWarps <= tile * cunits) ++w0;
-                const uint32_t local = (uint32_t)__cvta_generic_to_shared(part + (size_t)(tile + w0) * kSlot + (r % kTileN) * (8 * NT));
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at[c]) : "r"(local), "r"(c));
-                if (cunits == 0) at[c] = 0;
+                v[c] = 0.0f;
+                if (cunits == 0) continue;
+                // the first warp of that slice with a part of the tile: the one that has its first unit
+                const int w0 = ((tile * cunits + 1) * kWarps + ctotal - 1) / ctotal - 1;
+                uint32_t at;
+                const uint32_t local = (uint32_t)__cvta_generic_to_shared(part + (size_t)(tile + w0) * kSlot + part_at(m, o & 15));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(c));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[c]) : "r"(at));
             }
-            for (int m = rank; m < a.M; m += CS) {
-                float v[CS], s = 0.0f;
 #pragma unroll
-                for (int c = 0; c < CS; ++c) {
-                    v[c] = 0.0f;
-                    if (at[c]) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[c]) : "r"(at[c] + m * 4));
-                }
-#pragma unroll
-                for (int c = 0; c < CS; ++c) s += v[c];
-                store_out(a, m, tile0 * kTileN + r, s * Scale<FMT>::kBack);
-            }
+            for (int c = 0; c < CS; ++c) s += v[c];
+            store_out(a, m, n, s * Scale<FMT>::kBack);
         }
         // no CTA leaves while a peer may still read its shared memory
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
