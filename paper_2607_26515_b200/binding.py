@@ -7,6 +7,7 @@ this module raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Tuple
 
@@ -592,13 +593,11 @@ def w4a16_gemv(X: torch.Tensor, w_codes: torch.Tensor, w_side: torch.Tensor, fmt
         raise ValueError(f"w_meta / w_scale must be contiguous {side_type} [N, K/{block}] on cuda:{index}")
     out_dtype = out_dtype if Y is None else Y.dtype
     _require(out_dtype in _OUT, "Y must be bf16 or fp32")
-    if Y is not None:
-        _rows(Y, "Y", M, N, out_dtype, index)
+    ldy = (N + 7) // 8 * 8 if Y is None else _rows(Y, "Y", M, N, out_dtype, index)
 
     def body(st):
         y = _new_rows(M, N, out_dtype, index) if Y is None else Y
-        _check(fn(X.data_ptr(), M, K, ldx, w_codes.data_ptr(), w_side.data_ptr(), N, y.data_ptr(), _OUT[out_dtype],
-                  y.stride(0) if M > 1 else (N + 7) // 8 * 8, st))
+        _check(fn(X.data_ptr(), M, K, ldx, w_codes.data_ptr(), w_side.data_ptr(), N, y.data_ptr(), _OUT[out_dtype], ldy, st))
         return y
 
     return _run(index, stream, body)
@@ -630,11 +629,15 @@ def block_join(H: torch.Tensor, B: torch.Tensor, gamma_pre: Optional[torch.Tenso
     _require(act in _GATES, f"unknown gate function {act!r}")
     _require(X is None or gamma_pre is not None, "X needs gamma_pre")
 
+    ldho = ldx = (K + 7) // 8 * 8
+    if H_out is not None:
+        ldho = _rows(H_out, "H_out", M, K, H.dtype, index)
+    if X is not None:
+        ldx = _rows(X, "X", M, K, _BF16, index)
+
     def body(st):
         h = _new_rows(M, K, H.dtype, index) if H_out is None else H_out
         x = _new_rows(M, K, _BF16, index) if X is None and gamma_pre is not None else X
-        ldho = _rows(h, "H_out", M, K, H.dtype, index)
-        ldx = 0 if x is None else _rows(x, "X", M, K, _BF16, index)
         _check(lib().resq_block_join(H.data_ptr(), dtype, B.data_ptr(), M, K, ldh, ldb, g, ldg, _GATES[act], post, pre, alpha, eps,
                                      h.data_ptr(), ldho, _ptr(x), ldx, st))
         return h, x
@@ -642,6 +645,7 @@ def block_join(H: torch.Tensor, B: torch.Tensor, gamma_pre: Optional[torch.Tenso
     return _run(index, stream, body)
 
 
+@functools.lru_cache(maxsize=1024)
 def block_join_backward_workspace_bytes(M: int, K: int) -> int:
     return int(lib().resq_block_join_backward_workspace_bytes(M, K))
 
@@ -665,11 +669,12 @@ def block_join_backward(dH_out: Optional[torch.Tensor], dX: Optional[torch.Tenso
     _require(act in _GATES, f"unknown gate function {act!r}")
     if workspace is not None and (workspace.get_device() != index or not workspace.is_contiguous()):
         raise ValueError(f"workspace must be a contiguous tensor on cuda:{index}")
+    lddh = ldn = (K + 7) // 8 * 8
+    if dH is not None:
+        lddh = _rows(dH, "dH", M, K, H_out.dtype, index)
 
     def body(st):
         out = {"dH": _new_rows(M, K, H_out.dtype, index) if dH is None else dH, "dB": _new_rows(M, K, _BF16, index)}
-        lddh = _rows(out["dH"], "dH", M, K, H_out.dtype, index)
-        ldn = (K + 7) // 8 * 8
         columns = [n for n, on in (("dgamma_pre", dX is not None), ("dgamma_post", post is not None), ("dgate", g is not None and ldg == 0)) if on]
         if columns:
             out.update(zip(columns, torch.empty((len(columns), K), dtype=_F32, device=index).unbind()))
@@ -722,9 +727,10 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, logp: to
     values += [None if t is None else _vector(t, name, M, _F32, index)
                for name, t in (("logp", logp), ("peak", peak), ("log_sum", log_sum), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy))]
 
+    ldd = (V + 7) // 8 * 8 if dlogits is None else _rows(dlogits, "dlogits", M, V, logits.dtype, index)
+
     def body(st):
         d = _new_rows(M, V, logits.dtype, index) if dlogits is None else dlogits
-        ldd = _rows(d, "dlogits", M, V, logits.dtype, index)
         _check(lib().resq_token_logprobs_backward(logits.data_ptr(), dtype, M, V, ld, values[0], temperature, *values[1:], d.data_ptr(), ldd, st))
         return d
 

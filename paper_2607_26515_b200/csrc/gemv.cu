@@ -470,13 +470,16 @@ GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
     for (int lg = 0; lg < 4; ++lg) {
         const int cs = 1 << lg, us = (units + cs - 1) / cs;
         const size_t x = (size_t)M * (us * 256 + kXPad), ring = fmt == kHiF4 ? ring_bytes<kHiF4>() : ring_bytes<kMXFP4>();
-        for (int T = 1; T <= std::min(kMaxTiles, tiles); ++T) {
-            const size_t smem = x + ring + part_bytes(cs, T, nt);
-            if (smem > kSmemMax) break;
-            const int64_t clusters = (tiles + T - 1) / T;
-            const double waves = (double)((clusters + resident_clusters(cs) - 1) / resident_clusters(cs));
-            const double cost = waves * ((double)((T * us + kWarps - 1) / kWarps) * 1200 + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
-            if (best.cs == 0 || cost < best_cost) best = GemvPlan{cs, T, us, smem}, best_cost = cost;
+        // the fewest waves that shared memory and kMaxTiles allow, and up to three more: the smallest T for each
+        const int slots = resident_clusters(cs);
+        int most = std::min(kMaxTiles, tiles);
+        while (most > 0 && x + ring + part_bytes(cs, most, nt) > kSmemMax) --most;
+        if (most == 0) continue;
+        for (int waves = (tiles + slots * most - 1) / (slots * most), tried = 0; tried < 4; ++waves, ++tried) {
+            const int T = (tiles + slots * waves - 1) / (slots * waves);
+            const double cost = (double)waves * ((double)((T * us + kWarps - 1) / kWarps) * 1200 + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
+            if (best.cs == 0 || cost < best_cost) best = GemvPlan{cs, T, us, x + ring + part_bytes(cs, T, nt)}, best_cost = cost;
+            if (T == 1) break;
         }
     }
     return best;
