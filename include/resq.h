@@ -351,10 +351,11 @@ RESQ_API int mxfp4_w16a4_linear(const void* X_bf16, int64_t M, int64_t K, int64_
  * its own is this library's) ---------------------------------------------------------------------------------------
  * Y = X deq(Q(W))^T as *_w4a16_linear, for 1 <= M <= RESQ_GEMV_MAX_TOKENS token rows (K <= RESQ_GEMV_MAX_K), as a kernel that
  * streams the packed weights once (a GEMM tile computes 128 token rows whatever M is).  Same argument rules and output
- * types; no workspace.  Products of decoded weights and bf16 activations are exact, sums are held in fp32 and added in a
- * fixed order (bit-identical results run to run; the order depends on M, N and K).  An infinity or NaN in a row of X
- * makes that row of Y follow IEEE arithmetic (0 x inf = NaN) and leaves the others alone; an MXFP4 weight of 2^128 or more
- * (scale codes 253 and above) is infinite, as in mxfp4_dequantize. */
+ * types; no workspace.  Products of decoded weights and bf16 activations are exact (HiF4: those of 2^-110 and more in
+ * magnitude), sums are held in fp32 and added in a fixed order (bit-identical results run to run; the order
+ * depends on M, N and K).  An infinity or NaN in a row of X makes that row of Y follow IEEE arithmetic (0 x inf = NaN) and
+ * leaves the others alone; an MXFP4 weight of 2^128 or more (scale codes 253 and above) is infinite, as in
+ * mxfp4_dequantize. */
 #define RESQ_GEMV_MAX_TOKENS 16
 #define RESQ_GEMV_MAX_K 49152
 RESQ_API int hif4_w4a16_gemv(const void* X_bf16, int64_t M, int64_t K, int64_t ldx,
@@ -374,7 +375,8 @@ RESQ_API int mxfp4_w4a16_gemv(const void* X_bf16, int64_t M, int64_t K, int64_t 
  *   X_bf16 [M, K] is what *_resq_linear and its relatives take.  1 <= K <= RESQ_JOIN_MAX_K, any K in that range; rows
  *   start on 16-byte boundaries (ld % 8 == 0 for bf16, % 4 for fp32) and what lies behind column K is neither read nor
  *   written.  H_out may be H itself; other overlaps are not allowed.  Sums, norms and H' before its one rounding are
- *   fp32; X is formed from the unrounded H'.  alpha and eps finite, eps >= 0.
+ *   fp32; X is formed from the unrounded H'.  alpha and eps finite, eps >= 0 (with eps = 0 a row of zeros has the NaN of
+ *   0 / 0; NaN and infinities stay in their row, and in the column sums over the rows).
  * Backward: the gradients of these formulas at H_out and B as given (the row factors are formed again from them), with
  *   dH_out (type of the stream) and / or dX bf16 the gradients of the two outputs (either may be NULL = zero):
  *     dH [M, K] (type of the stream; may be dH_out itself), dB bf16 [M, K], dgate (bf16 [M, K] with pitch lddg; for a
