@@ -23,10 +23,10 @@ namespace resq {
 namespace {
 
 constexpr int kMaxThreadsFwd = 1024;  // one row: up to 4 vectors of 8 per thread
-// Backward, threads per SM: 512 of 128 registers; 640 of 96 where a row is split over a cluster (they spill nothing either, but
-// measured slower on short rows: 8192 x 2048, fp32 stream, 69 against 61 us).
-constexpr int bwd_threads(int cs) { return cs == 1 ? 512 : 640; }
-static_assert(kMaxThreadsFwd * 8 * 4 >= RESQ_JOIN_MAX_K && bwd_threads(8) * 8 * 8 >= RESQ_JOIN_MAX_K, "row length");
+// Backward, threads per SM: 512 of 128 registers, or 640 of 96 for rows that need them (they spill nothing either, but short rows
+// measured slower: 8192 x 2048, fp32 stream, 61 against 57 us; 16384 x 3584, gated, 221 against 212).
+constexpr int kFewThreads = 512, kManyThreads = 640;
+static_assert(kMaxThreadsFwd * 8 * 4 >= RESQ_JOIN_MAX_K && kManyThreads * 8 * 8 >= RESQ_JOIN_MAX_K, "row length");
 
 struct JoinFwd {
     const void* H;
@@ -249,8 +249,8 @@ constexpr int kMaxDepth = 6;
 // normalised branch n; then, with a norm on the branch, the sum of v n.  The first sums of the next row and the last one of this
 // row are taken together, so a row costs one barrier.  Without a gate per token the gradients of gamma_post and of the channel
 // gate are the same column sum of d n times a constant of the column.
-template <typename S, bool POST, int GATE, int VPT, int CS>
-__global__ void __launch_bounds__(bwd_threads(CS)) join_bwd_kernel(const __grid_constant__ JoinBwd a) {
+template <typename S, bool POST, int GATE, int VPT, int CS, int MAX>
+__global__ void __launch_bounds__(MAX) join_bwd_kernel(const __grid_constant__ JoinBwd a) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ __align__(16) float red[2][4 * 32];
     __shared__ float xred[2][4 * CS];
@@ -458,6 +458,10 @@ __global__ void __launch_bounds__(bwd_threads(CS)) join_bwd_kernel(const __grid_
 #pragma unroll
             for (int i = 0; i < 4; ++i) unpair(v[i], f[2 * i], f[2 * i + 1]);
             float* p = a.col[which] + (blockIdx.x / CS) * a.pitch + first + (j * threads + tid) * 8;
+            if (groups > 1) {  // wide stores (single floats at a stride of 8 cost 4 us at 148 x 5003)
+                store8(p, f, 8);
+                return;
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (i < n[j]) p[i] = f[i];
@@ -487,21 +491,22 @@ __global__ void __launch_bounds__(bwd_threads(CS)) join_bwd_kernel(const __grid_
     }
 }
 
-// Sum of the P partial rows: a block owns 32 columns, each of its 32 warps adds a contiguous run of rows with 16 loads in
-// flight, and the 32 sums are added in order.
-constexpr int kSumWarps = 32;
+// Sum of the P partial rows: a block owns 32 columns, each of its warps adds a contiguous run of rows with 16 loads in flight,
+// and the warps' sums are added in order.  Latency: 16 warps for up to 512 rows (148 x 5003: 3 us less than with 32, whose blocks
+// do not all fit on the device at once), 32 for more.
 struct JoinSum {
     const float* part[3];
     float* out[3];
     int64_t pitch;
     int P, K;
 };
-__global__ void __launch_bounds__(kSumWarps * 32) join_sum_kernel(const __grid_constant__ JoinSum a) {
-    __shared__ float buf[kSumWarps][32];
+template <int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) join_sum_kernel(const __grid_constant__ JoinSum a) {
+    __shared__ float buf[WARPS][32];
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, col = blockIdx.x * 32 + lane, which = blockIdx.y;
-    const int per = (a.P + kSumWarps - 1) / kSumWarps, p0 = w * per, p1 = min(a.P, p0 + per);
+    const int per = (a.P + WARPS - 1) / WARPS, p0 = w * per, p1 = min(a.P, p0 + per);
     float s = 0.0f;
     if (col < a.K) {
         const float* src = a.part[which] + col;
@@ -521,7 +526,7 @@ __global__ void __launch_bounds__(kSumWarps * 32) join_sum_kernel(const __grid_c
     if (w == 0 && col < a.K) {
         float t = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kSumWarps; ++i) t += buf[i][lane];
+        for (int i = 0; i < WARPS; ++i) t += buf[i][lane];
         a.out[which][col] = t;
     }
 }
@@ -531,23 +536,26 @@ __global__ void __launch_bounds__(kSumWarps * 32) join_sum_kernel(const __grid_c
 // in shared memory, for which long rows are split further); groups of CTAs that share the rows.
 constexpr int kSmemSm = 224 * 1024, kSmemStatic = 2048;
 struct BwdShape {
-    int vpt, cs, threads, per_sm, depth;
+    int vpt, cs, max, threads, per_sm, depth;
     int64_t groups;
 };
 BwdShape bwd_shape(int64_t M, int64_t K, int stream_size, bool gate) {
     const int64_t vecs = (K + 7) / 8;
     BwdShape s;
     int stage = 0;
-    // one CTA with one vector per thread, then with two, then clusters (2000 x 18944 in four CTAs of one vector: 0.8 of the time of two)
-    for (s.vpt = 1, s.cs = 1;;) {
+    // One CTA with one vector per thread, then with two, then clusters (4736 x 5003, gated: 85 us with one, 109 with two;
+    // 4096 x 8192, channel gate: 96 us with two, 139 in a cluster of two).
+    for (s.vpt = 1, s.cs = 1, s.max = kFewThreads;;) {
         const int64_t per = (int64_t)s.cs * s.vpt * 32;
         s.threads = (int)((vecs + per - 1) / per * 32);
         stage = stage_bytes(stream_size, gate, s.vpt * s.threads * 8);
-        if (s.threads <= bwd_threads(s.cs) && 3 * stage <= kSmemSm - kSmemStatic) break;
-        if (s.vpt == 1 && s.cs == 1) s.vpt = 2;
-        else s.vpt = 1, s.cs *= 2;
+        if (s.threads <= s.max && 3 * stage <= kSmemSm - kSmemStatic) break;
+        if (s.cs > 1) s.cs *= 2;
+        else if (s.vpt == 2) s.vpt = 1, s.cs = 2, s.max = kManyThreads;
+        else if (s.max == kFewThreads) s.max = kManyThreads;
+        else s.vpt = 2, s.max = kFewThreads;
     }
-    s.per_sm = std::min(bwd_threads(s.cs) / s.threads, kSmemSm / (3 * stage + kSmemStatic));
+    s.per_sm = std::min(s.max / s.threads, kSmemSm / (3 * stage + kSmemStatic));
     s.depth = std::min(kMaxDepth, (kSmemSm / s.per_sm - kSmemStatic) / stage);
     s.groups = std::min<int64_t>(M, resident_clusters(s.cs) * s.per_sm);
     return s;
@@ -559,9 +567,9 @@ int64_t bwd_most_groups(int64_t M, int64_t K) {
     return g;
 }
 
-template <typename S, bool POST, int GATE, int VPT, int CS>
+template <typename S, bool POST, int GATE, int VPT, int CS, int MAX>
 int launch_bwd(const BwdShape& s, JoinBwd a, cudaStream_t st) {
-    auto kern = join_bwd_kernel<S, POST, GATE, VPT, CS>;
+    auto kern = join_bwd_kernel<S, POST, GATE, VPT, CS, MAX>;
     const int smem = s.depth * stage_bytes(sizeof(S), GATE == 2, VPT * s.threads * 8);
     a.depth = s.depth;
     const int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem, "join_bwd_kernel shared memory");
@@ -572,12 +580,14 @@ int launch_bwd(const BwdShape& s, JoinBwd a, cudaStream_t st) {
 }
 template <typename S, bool POST, int GATE>
 int launch_bwd(const BwdShape& s, const JoinBwd& a, cudaStream_t st) {
-    if (s.vpt == 2) return launch_bwd<S, POST, GATE, 2, 1>(s, a, st);
+    if (s.vpt == 2) return launch_bwd<S, POST, GATE, 2, 1, kFewThreads>(s, a, st);
     switch (s.cs) {
-        case 1: return launch_bwd<S, POST, GATE, 1, 1>(s, a, st);
-        case 2: return launch_bwd<S, POST, GATE, 1, 2>(s, a, st);
-        case 4: return launch_bwd<S, POST, GATE, 1, 4>(s, a, st);
-        default: return launch_bwd<S, POST, GATE, 1, 8>(s, a, st);
+        case 1:
+            if (s.max == kFewThreads) return launch_bwd<S, POST, GATE, 1, 1, kFewThreads>(s, a, st);
+            return launch_bwd<S, POST, GATE, 1, 1, kManyThreads>(s, a, st);
+        case 2: return launch_bwd<S, POST, GATE, 1, 2, kManyThreads>(s, a, st);
+        case 4: return launch_bwd<S, POST, GATE, 1, 4, kManyThreads>(s, a, st);
+        default: return launch_bwd<S, POST, GATE, 1, 8, kManyThreads>(s, a, st);
     }
 }
 template <typename S>
@@ -700,7 +710,9 @@ int resq_block_join_backward(const void* dH_out, const void* dX, const void* H_o
     if (rc || ncol == 0) return rc;
     s.pitch = a.pitch, s.P = (int)shape.groups, s.K = (int)K;
     LaunchScope scope(kKindRow, st);
-    return cuda_fail(launch_kernel(join_sum_kernel, dim3((unsigned)((K + 31) / 32), (unsigned)ncol), dim3(kSumWarps * 32), 0, st, s),
+    const int warps = s.P > 512 ? 32 : 16;
+    return cuda_fail(launch_kernel(warps == 32 ? join_sum_kernel<32> : join_sum_kernel<16>, dim3((unsigned)((K + 31) / 32), (unsigned)ncol),
+                                   dim3(warps * 32), 0, st, s),
                      "join_sum_kernel launch");
 }
 }
