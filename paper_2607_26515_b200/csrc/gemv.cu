@@ -24,19 +24,19 @@
 #include "row_common.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace resq {
 namespace {
 
 constexpr int kWarps = 16, kThreads = kWarps * 32;
 constexpr int kUnitK = 128, kTileN = 16;
-constexpr int kStep = 2;        // units of a tile per step: 256 k, one wait and one set of copies
-constexpr int kRing = 3;        // steps in flight per warp: 96 KB per SM
-// words per row of a step's scales: HiF4 4 and one against bank conflicts, MXFP4 2 and one because rows start on any byte
-template <int FMT>
-constexpr int kSideRow = FMT == kHiF4 ? 5 : 3;
-template <int FMT>
-constexpr int kSideBytes = kTileN * kSideRow<FMT> * 4;
+// STEP: units of a tile per step (512 or 256 k), which has one wait and one set of copies.  Steps in flight per warp: two of
+// four units (128 KB per SM) or three of two (96 KB, where the staged activations leave no more).
+__host__ __device__ constexpr int ring_steps(int step) { return step == 4 ? 2 : 3; }
+// words per row of a step's scales: HiF4 two per unit and one against bank conflicts, MXFP4 one per unit and one because rows
+// start on any byte
+__host__ __device__ constexpr int side_row(int fmt, int step) { return fmt == kHiF4 ? 2 * step + 1 : step + 1; }
 constexpr int kMaxTiles = 64;   // row tiles per CTA (int arithmetic on units x warps)
 constexpr int kXPad = 64;       // bytes behind a token's staged row: neighbouring tokens use the other half of the banks
 
@@ -182,16 +182,15 @@ __device__ __forceinline__ void store_out(const GemvArgs& a, int m, int n, float
 __device__ __forceinline__ int part_at(int token, int row) {
     return (token >> 1) * 32 + ((row + 4 * (token >> 1)) & 15) * 2 + (token & 1);
 }
-template <int FMT>
-__host__ __device__ constexpr size_t ring_bytes() {
-    return (size_t)kWarps * kRing * (kStep * 1024 + kSideBytes<FMT>);
+__host__ __device__ constexpr size_t ring_bytes(int fmt, int step) {
+    return (size_t)kWarps * ring_steps(step) * (step * 1024 + kTileN * side_row(fmt, step) * 4);
 }
 __host__ __device__ inline size_t part_bytes(int cs, int tiles, int nt) {
     return (size_t)(cs == 1 ? 2 * kWarps : tiles + kWarps) * kTileN * 8 * nt * sizeof(float);
 }
 
 // NT: groups of 8 tokens; CS: CTAs of a cluster, each with its slice of K.
-template <int FMT, int NT, int CS>
+template <int FMT, int NT, int STEP, int CS>
 __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant__ GemvArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -202,9 +201,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     const int units = max(0, min(a.units_slice, units_all - rank * a.units_slice));
     const int k0 = rank * a.units_slice * kUnitK;
     const int xrow = a.units_slice * 256 + kXPad;
-    uint8_t* const ring = smem + (size_t)a.M * xrow + warp * (kRing * kStep * 1024);
-    uint8_t* const sides = smem + (size_t)a.M * xrow + kWarps * (kRing * kStep * 1024) + warp * (kRing * kSideBytes<FMT>);
-    float* const part = reinterpret_cast<float*>(smem + (size_t)a.M * xrow + ring_bytes<FMT>());
+    constexpr int kRing = ring_steps(STEP), kSideRow = side_row(FMT, STEP), kSideBytes = kTileN * kSideRow * 4;
+    uint8_t* const ring = smem + (size_t)a.M * xrow + warp * (kRing * STEP * 1024);
+    uint8_t* const sides = smem + (size_t)a.M * xrow + kWarps * (kRing * STEP * 1024) + warp * (kRing * kSideBytes);
+    float* const part = reinterpret_cast<float*>(smem + (size_t)a.M * xrow + ring_bytes(FMT, STEP));
     constexpr int kSlot = kTileN * 8 * NT;
 
     pdl_wait();
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     // The last unit of K may hold one, two or three blocks of 32: a lane beyond the end reads the start of its row instead
     // and multiplies it with zeros (its activations are staged as zeros; an MXFP4 scale, which may be infinite, is zeroed).
     const bool beyond = k0 + (units - 1) * kUnitK + t * 32 >= a.K;
-    auto step_units = [&](int u, int i) { return min(min(kStep - (u & (kStep - 1)), units - u), last - i); };
+    auto step_units = [&](int u, int i) { return min(min(STEP - (u & (STEP - 1)), units - u), last - i); };
     int lu = units > 0 ? first % units : 0, lt = units > 0 ? first / units : 0, li = first, lslot = 0;  // copy cursor
     const uint8_t *tcodes = a.codes, *tside = a.side;  // the tile's first row; a lane's rows lie at 32-bit offsets from it
     uint32_t oa = 0, ob = 0;
@@ -230,34 +230,35 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     };
     auto copy = [&]() {
         if (li < last) {
-            const int n = step_units(lu, li), j0 = lu & (kStep - 1);
+            const int n = step_units(lu, li), j0 = lu & (STEP - 1);
 #pragma unroll
-            for (int j = 0; j < kStep; ++j) {
+            for (int j = 0; j < STEP; ++j) {
                 if (j < j0 || j >= j0 + n) continue;
                 const int u = lu - j0 + j;
                 const uint32_t kc = beyond && u == units - 1 ? 0u : (uint32_t)(k0 / 2 + u * 64 + t * 16);
-                const uint32_t dst = ring_at + (lslot * kStep + j) * 1024;
+                const uint32_t dst = ring_at + (lslot * STEP + j) * 1024;
                 copy16(dst, tcodes + oa + kc);
                 copy16(dst + 512, tcodes + ob + kc);
             }
-            const uint32_t dst = side_at + lslot * kSideBytes<FMT>;
+            const uint32_t dst = side_at + lslot * kSideBytes;
             if (FMT == kHiF4) {
-                const int b = k0 / 64 + (lu - j0) * 2 + (lane & 3), nb = a.K / 64;
+                constexpr int kWords = 2 * STEP, kRows = 32 / kWords;  // of one copy of the warp
+                const int b = k0 / 64 + (lu - j0) * 2 + lane % kWords, nb = a.K / 64;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int r = i * 8 + (lane >> 2);
-                    copy4(dst + (r * 5 + (lane & 3)) * 4, tside + (uint32_t)min(r, rows_left) * (uint32_t)row_side + min(b, nb - 1) * 4, b < nb ? 4 : 0);
+                for (int i = 0; i < kTileN / kRows; ++i) {
+                    const int r = i * kRows + lane / kWords;
+                    copy4(dst + (r * kSideRow + lane % kWords) * 4, tside + (uint32_t)min(r, rows_left) * (uint32_t)row_side + min(b, nb - 1) * 4, b < nb ? 4 : 0);
                 }
             } else {
-                // whole aligned words over the 8 bytes of a row, of which the first may belong to the row before; the array
+                // whole aligned words over the bytes of a row, of which the first may belong to the row before; the array
                 // may end within a word
                 const uint8_t* const end = a.side + a.N * row_side;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int j = i * 32 + lane, r = j / 3;
-                    if (j < kTileN * 3) {
+                for (int i = 0; i < (kTileN * kSideRow + 31) / 32; ++i) {
+                    const int j = i * 32 + lane, r = j / kSideRow;
+                    if (j < kTileN * kSideRow) {
                         const uint8_t* p = tside + (uint32_t)min(r, rows_left) * (uint32_t)row_side + (k0 / 32 + (lu - j0) * 4);
-                        p = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3) + (j - r * 3) * 4;
+                        p = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3) + (j - r * kSideRow) * 4;
                         const int have = (int)max((int64_t)0, min((int64_t)4, (int64_t)(end - p)));
                         copy4(dst + j * 4, have > 0 ? p : a.side, have);
                     }
@@ -310,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     const uint8_t* xs[NT];  // the lane's token of each group (columns behind the last token repeat it; they are not stored)
 #pragma unroll
     for (int q = 0; q < NT; ++q) xs[q] = smem + min(q * 8 + g, a.M - 1) * xrow + t * 16;
-    const uint8_t *side_a = sides + g * (kSideRow<FMT> * 4), *side_b = side_a + 8 * (kSideRow<FMT> * 4);
+    const uint8_t *side_a = sides + g * (kSideRow * 4), *side_b = side_a + 8 * (kSideRow * 4);
     int shift_a = 0, shift_b = 0;  // the byte of its word that a row's MXFP4 scales start on
     auto tile_sides = [&]() {
         if (FMT == kMXFP4) {
@@ -322,40 +323,40 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     };
     tile_sides();
     for (int i = first; i < last;) {
-        const int n = step_units(cu, i), j0 = cu & (kStep - 1);
+        const int n = step_units(cu, i), j0 = cu & (STEP - 1);
         copies_wait<kRing - 1>();
         __syncwarp();  // the scales were copied by other lanes
-        const uint8_t* codes = ring + slot * (kStep * 1024) + lane * 16;
-        const uint8_t *pa = side_a + slot * kSideBytes<FMT> + shift_a, *pb = side_b + slot * kSideBytes<FMT> + shift_b;
+        const uint8_t* codes = ring + slot * (STEP * 1024) + lane * 16;
+        const uint8_t *pa = side_a + slot * kSideBytes + shift_a, *pb = side_b + slot * kSideBytes + shift_b;
         const int xat = (cu - j0) * 256;
-        Scale<FMT> fa[kStep], fb[kStep];
         bool two = false;
+        if (FMT == kMXFP4) {
 #pragma unroll
-        for (int j = 0; j < kStep; ++j) {
-            if (FMT == kHiF4) {
-                fa[j].set(*reinterpret_cast<const uint32_t*>(pa + j * 8), t & 1);
-                fb[j].set(*reinterpret_cast<const uint32_t*>(pb + j * 8), t & 1);
-            } else {
-                const bool none = beyond && cu - j0 + j >= units - 1;
-                fa[j].set(pa[j * 4], none), fb[j].set(pb[j * 4], none);
-                two |= max(pa[j * 4], pb[j * 4]) > 128;
-            }
+            for (int j = 0; j < STEP; ++j) two |= max(pa[j * 4], pb[j * 4]) > 128;
+            two = __any_sync(0xFFFFFFFFu, two);
         }
-        auto one = [&](int j) {
+        auto one = [&](int j, auto with_second) {
             const uint4 qa = *reinterpret_cast<const uint4*>(codes + j * 1024);
             const uint4 qb = *reinterpret_cast<const uint4*>(codes + j * 1024 + 512);
-            unit<FMT, NT, false>(qa, qb, fa[j], fb[j], xs, xat + j * 256, acc);
-        };
-        if (FMT == kMXFP4 && __any_sync(0xFFFFFFFFu, two)) {
-#pragma unroll 1
-            for (int j = j0; j < j0 + n; ++j) {
-                const uint4 qa = *reinterpret_cast<const uint4*>(codes + j * 1024);
-                const uint4 qb = *reinterpret_cast<const uint4*>(codes + j * 1024 + 512);
-                unit<FMT, NT, true>(qa, qb, j ? fa[1] : fa[0], j ? fb[1] : fb[0], xs, xat + j * 256, acc);
+            Scale<FMT> fa, fb;
+            if (FMT == kHiF4) {
+                fa.set(*reinterpret_cast<const uint32_t*>(pa + j * 8), t & 1);
+                fb.set(*reinterpret_cast<const uint32_t*>(pb + j * 8), t & 1);
+            } else {
+                const bool none = beyond && cu - j0 + j >= units - 1;
+                fa.set(pa[j * 4], none), fb.set(pb[j * 4], none);
             }
+            unit<FMT, NT, decltype(with_second)::value>(qa, qb, fa, fb, xs, xat + j * 256, acc);
+        };
+        if (FMT == kMXFP4 && two) {
+#pragma unroll 1
+            for (int j = j0; j < j0 + n; ++j) one(j, std::true_type());
+        } else if (n == STEP) {
+#pragma unroll
+            for (int j = 0; j < STEP; ++j) one(j, std::false_type());
         } else {
-            if (j0 == 0) one(0);
-            if (j0 + n == kStep) one(1);
+#pragma unroll 1
+            for (int j = j0; j < j0 + n; ++j) one(j, std::false_type());
         }
         if (++slot == kRing) slot = 0;
         __syncwarp();  // every lane has read the scales
@@ -462,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
 
 // ---- host side -----------------------------------------------------------------------------------
 struct GemvPlan {
-    int cs, tiles_cta, units_slice;
+    int cs, tiles_cta, units_slice, step;
     size_t smem;
 };
 
@@ -472,43 +473,51 @@ constexpr size_t kSmemMax = 227 * 1024;
 // and the fixed costs are rough measurements; only their proportions matter.
 GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
     const int tiles = (int)((N + kTileN - 1) / kTileN), units = (int)((K + kUnitK - 1) / kUnitK), nt = M > 8 ? 2 : 1;
-    GemvPlan best{0, 0, 0, 0};
+    GemvPlan best{0, 0, 0, 0, 0};
     double best_cost = 0;
-    for (int lg = 0; lg < 4; ++lg) {
-        const int cs = 1 << lg, us = (units + cs - 1) / cs;
-        const size_t x = (size_t)M * (us * 256 + kXPad), ring = fmt == kHiF4 ? ring_bytes<kHiF4>() : ring_bytes<kMXFP4>();
-        // the fewest waves that shared memory and kMaxTiles allow, and up to three more: the smallest T for each
-        const int slots = resident_clusters(cs);
-        int most = std::min(kMaxTiles, tiles);
-        while (most > 0 && x + ring + part_bytes(cs, most, nt) > kSmemMax) --most;
-        if (most == 0) continue;
-        for (int waves = (tiles + slots * most - 1) / (slots * most), tried = 0; tried < 4; ++waves, ++tried) {
-            const int T = (tiles + slots * waves - 1) / (slots * waves);
-            const double cost = (double)waves * ((double)((T * us + kWarps - 1) / kWarps) * 1200 + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
-            if (best.cs == 0 || cost < best_cost) best = GemvPlan{cs, T, us, x + ring + part_bytes(cs, T, nt)}, best_cost = cost;
-            if (T == 1) break;
+    for (int step = 2; step <= (nt == 1 ? 4 : 2); step += 2) {
+        for (int lg = 0; lg < 4; ++lg) {
+            const int cs = 1 << lg, us = (units + cs - 1) / cs;
+            const size_t x = (size_t)M * (us * 256 + kXPad), ring = ring_bytes(fmt, step);
+            // the fewest waves that shared memory and kMaxTiles allow, and up to three more: the smallest T for each
+            const int slots = resident_clusters(cs);
+            int most = std::min(kMaxTiles, tiles);
+            while (most > 0 && x + ring + part_bytes(cs, most, nt) > kSmemMax) --most;
+            if (most == 0) continue;
+            for (int waves = (tiles + slots * most - 1) / (slots * most), tried = 0; tried < 4; ++waves, ++tried) {
+                const int T = (tiles + slots * waves - 1) / (slots * waves);
+                const double units_warp = (T * us + kWarps - 1) / kWarps;
+                const double cost = (double)waves * (units_warp * (step == 4 ? 1120 : 1200) + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
+                if (best.cs == 0 || cost < best_cost) best = GemvPlan{cs, T, us, step, x + ring + part_bytes(cs, T, nt)}, best_cost = cost;
+                if (T == 1) break;
+            }
         }
     }
     return best;
 }
 
-template <int FMT, int NT, int CS>
+template <int FMT, int NT, int STEP, int CS>
 int launch_gemv(const GemvArgs& a, const GemvPlan& p, cudaStream_t stream) {
-    auto kern = gemv_kernel<FMT, NT, CS>;
+    auto kern = gemv_kernel<FMT, NT, STEP, CS>;
     int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), (int)kSmemMax, "gemv_kernel shared memory");
     if (rc) return rc;
     const unsigned clusters = (unsigned)((a.tiles + p.tiles_cta - 1) / p.tiles_cta);
     LaunchScope scope(kKindGemm, stream);
     return cuda_fail(launch_clusters(kern, clusters * CS, kThreads, p.smem, CS, stream, a), "gemv_kernel launch");
 }
-template <int FMT, int NT>
+template <int FMT, int NT, int STEP>
 int launch_gemv(const GemvArgs& a, const GemvPlan& p, cudaStream_t stream) {
     switch (p.cs) {
-        case 1: return launch_gemv<FMT, NT, 1>(a, p, stream);
-        case 2: return launch_gemv<FMT, NT, 2>(a, p, stream);
-        case 4: return launch_gemv<FMT, NT, 4>(a, p, stream);
-        default: return launch_gemv<FMT, NT, 8>(a, p, stream);
+        case 1: return launch_gemv<FMT, NT, STEP, 1>(a, p, stream);
+        case 2: return launch_gemv<FMT, NT, STEP, 2>(a, p, stream);
+        case 4: return launch_gemv<FMT, NT, STEP, 4>(a, p, stream);
+        default: return launch_gemv<FMT, NT, STEP, 8>(a, p, stream);
     }
+}
+template <int FMT>
+int launch_gemv(const GemvArgs& a, const GemvPlan& p, cudaStream_t stream) {
+    if (a.M > 8) return launch_gemv<FMT, 2, 2>(a, p, stream);
+    return p.step == 4 ? launch_gemv<FMT, 1, 4>(a, p, stream) : launch_gemv<FMT, 1, 2>(a, p, stream);
 }
 
 int gemv(int fmt, const void* X, int64_t M, int64_t K, int64_t ldx, const void* w_codes, const void* w_side, int64_t N, void* Y,
@@ -531,7 +540,7 @@ int gemv(int fmt, const void* X, int64_t M, int64_t K, int64_t ldx, const void* 
     // Nine to sixteen tokens of very long rows (K beyond about 24000) do not fit in shared memory even in eight slices: they
     // take two passes over the weights.
     GemvPlan p = plan_gemv(fmt, (int)M, N, K);
-    const int64_t step = p.cs ? M : 8;
+    const int64_t pass = p.cs ? M : 8;
     if (!p.cs) p = plan_gemv(fmt, 8, N, K);
     GemvArgs a;
     a.codes = static_cast<const uint8_t*>(w_codes);
@@ -539,12 +548,11 @@ int gemv(int fmt, const void* X, int64_t M, int64_t K, int64_t ldx, const void* 
     a.ldx = ldx, a.ldy = ldy, a.K = (int)K, a.N = (int)N, a.out_dtype = out_dtype;
     a.tiles = (int)((N + kTileN - 1) / kTileN), a.tiles_cta = p.tiles_cta, a.units_slice = p.units_slice;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    for (int64_t m = 0; m < M; m += step) {
-        a.M = (int)std::min(step, M - m);
+    for (int64_t m = 0; m < M; m += pass) {
+        a.M = (int)std::min(pass, M - m);
         a.X = static_cast<const __nv_bfloat16*>(X) + m * ldx;
         a.Y = static_cast<uint8_t*>(Y) + m * ldy * (out_dtype == RESQ_OUT_BF16 ? 2 : 4);
-        const int rc = fmt == kHiF4 ? (a.M > 8 ? launch_gemv<kHiF4, 2>(a, p, st) : launch_gemv<kHiF4, 1>(a, p, st))
-                                    : (a.M > 8 ? launch_gemv<kMXFP4, 2>(a, p, st) : launch_gemv<kMXFP4, 1>(a, p, st));
+        const int rc = fmt == kHiF4 ? launch_gemv<kHiF4>(a, p, st) : launch_gemv<kMXFP4>(a, p, st);
         if (rc) return rc;
     }
     return RESQ_OK;
