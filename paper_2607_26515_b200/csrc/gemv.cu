@@ -9,17 +9,18 @@
 // a lane owns 32 consecutive k of rows g and g + 8 (one 16-byte load each), and pairs elements i and i + 4 of a 32-bit word:
 // their nibbles lie 16 bits apart, so one mask takes both.
 //
-// Work: a unit is 16 weight rows x 128 k (1 KB of codes).  A CTA (16 warps, one CTA per SM, so that the activations are staged
+// Work: a unit is 16 weight rows x 128 k (1 KB of codes).  A CTA (12 warps, one CTA per SM, so that the activations are staged
 // once) owns T row tiles and one of CS slices of K; its T x units are dealt out evenly and contiguously to its warps.  The codes
-// come by asynchronous copies into a ring of three steps of two units per warp, each lane fetching what it will expand itself;
-// loads into registers measured up to 1.4 times slower (11 tokens, 3584 -> 100003: 102 against 75 us), because their lines in
-// flight have to fit into what the staged activations leave of the L1.  Tiles that a warp has to itself are written from its
-// registers; the parts of a tile that several warps (or slices) share go to shared memory and are added in a fixed order.
+// come by asynchronous copies into a ring of two steps of up to four units per warp, each lane fetching what it will expand
+// itself; loads into registers measured up to 1.4 times slower (11 tokens, 3584 -> 100003: 102 against 73 us), because their
+// lines in flight have to fit into what the staged activations leave of the L1.  Tiles that a warp has to itself are written from
+// its registers; the parts of a tile that several warps (or slices) share go to shared memory and are added in a fixed order.
+// Twelve warps with four units at a time are faster than sixteen with two (the same case: 65 against 73 us) or eight (68).
 //
-// Measured, weights from HBM: 3584 -> 37888, HiF4, 25 us for one token and 25.4 for eight (3.1 TB/s, 0.47 of the copy rate);
-// 11 tokens 3584 -> 100003 73 us (2.8 TB/s); 2048 -> 2048 4.2 us, of which the launch and the chain load, expand, sum are all.
-// It is bound by instruction issue: about 260 per unit, of which 160 are the expansion (20 per 8 weights); the integer pipe is
-// busy 61 % of the time, the tensor pipe 16 %.
+// Measured, weights from HBM: 3584 -> 37888, HiF4, 23 us for one token and 25 for eight (3.3 TB/s, 0.50 of the copy rate); MXFP4
+// 24.5 us; 11 tokens 3584 -> 100003 65 us (3.1 TB/s); 2048 -> 2048 4.1 us, of which the launch and the chain load, expand, sum
+// are all.  It is bound by the arithmetic of the expansion: without it (the codes taken as they are) 3584 -> 37888 takes 17 us,
+// without the copies 19.5.
 #include "common.cuh"
 #include "row_common.cuh"
 
@@ -29,11 +30,11 @@
 namespace resq {
 namespace {
 
-constexpr int kWarps = 16, kThreads = kWarps * 32;
+constexpr int kWarps = 12, kThreads = kWarps * 32;
 constexpr int kUnitK = 128, kTileN = 16;
-// STEP: units of a tile per step (512 or 256 k), which has one wait and one set of copies.  Steps in flight per warp: two of
-// four units (128 KB per SM) or three of two (96 KB, where the staged activations leave no more).
-__host__ __device__ constexpr int ring_steps(int step) { return step == 4 ? 2 : 3; }
+// STEP: units of a tile per step (512 or 256 k), which has one wait and one set of copies: four, or two where the staged
+// activations leave no room for more.
+constexpr int kRing = 2;        // steps in flight per warp: 96 or 48 KB per SM (three of two units: no faster, and it costs the tiles room)
 // words per row of a step's scales: HiF4 two per unit and one against bank conflicts, MXFP4 one per unit and one because rows
 // start on any byte
 __host__ __device__ constexpr int side_row(int fmt, int step) { return fmt == kHiF4 ? 2 * step + 1 : step + 1; }
@@ -77,6 +78,9 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 // the first `n` bytes of a word (0 to 4), zeros behind them
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, int n) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
@@ -100,21 +104,21 @@ struct Scale<kHiF4> {
     // 2^126 S1 2^2 may pass the range of bf16, so the weights are formed as w * 2^-16 and the sums take 2^16 at the end; only
     // products below 2^-110 lose bits by that.
     static constexpr float kBack = 65536.0f;
-    uint32_t base, e2, e3;
+    uint32_t base, e;  // e: exponents, two bits for every group of four: of words 0 to 3 in bits 0 to 7, of their upper halves in 16 to 23
     // odd: the lane's half of the 64-block
     __device__ __forceinline__ void set(uint32_t meta, int odd) {
         base = (meta & 255u) * 0x00200020u + 0x5E805E80u;  // bf16 bits of 2^110 S1 in both halves (s << 5 is (E << 7) | (Mn << 5))
-        e2 = meta >> (8 + 4 * odd);
-        e3 = __byte_perm(meta, 0u, odd ? 0x4443 : 0x4442);
+        // a level-2 bit counts for both halves of its word, two level-3 bits belong to a word (the lower to its lower half)
+        const uint32_t e3 = __byte_perm(meta, 0u, odd ? 0x4443 : 0x4442), e2 = meta >> (8 + 4 * odd);
+        const uint32_t spread = (e2 & 0x03u) | ((e2 << 2) & 0x30u);
+        e = mad((spread | (spread << 1)) & 0x55u, 0x00010001u, (e3 * 0x8001u) & 0x00550055u);
     }
     // v[i]: elements i (low half) and i + 4.  Element 2j is the low, 2j + 1 the high nibble of byte j; the sign goes to bit 7
     // of the upper byte, the magnitude to bits 7:5 of the lower byte of a half.
     template <bool TWO>
     __device__ __forceinline__ void expand(uint32_t w, int group, uint32_t (&v)[4]) const {
-        // exponents of the two level-3 groups: bit 2i of e3 to bit 7, bit 2i + 1 to bit 23; bit i of e2 to both.  Written as
-        // multiply-adds: they run beside the integer pipe, which the element work fills.
-        const uint32_t m3 = (128u >> (2 * group)) | (0x00400000u >> (2 * group));
-        const uint32_t c = mad(e2 & (1u << group), 0x00800080u >> group, mad((e3 * m3) & 0x00800080u, 1u, base));
+        // both exponents to bit 7 of their half, as a multiply-add: it runs beside the integer pipe, which the element work fills
+        const uint32_t c = mad(e & (0x00030003u << (2 * group)), 128u >> (2 * group), base);
         const uint32_t w1 = w << 1, w4 = w << 4, w5 = w << 5;
         v[0] = mul_bf16x2(__byte_perm(w4, w5, 0x2604) & 0x80E080E0u, c);
         v[1] = mul_bf16x2(__byte_perm(w, w1, 0x2604) & 0x80E080E0u, c);
@@ -133,10 +137,12 @@ struct Scale<kMXFP4> {
     // TWO: a scale code above 128 has a second factor 2^(code - 128)
     template <bool TWO>
     __device__ __forceinline__ void expand(uint32_t w, int, uint32_t (&v)[4]) const {
-        v[0] = mul_bf16x2(((w << 6) & 0x01C001C0u) | ((w << 12) & 0x80008000u), c);
-        v[1] = mul_bf16x2(((w << 2) & 0x01C001C0u) | ((w << 8) & 0x80008000u), c);
-        v[2] = mul_bf16x2(((w >> 2) & 0x01C001C0u) | ((w << 4) & 0x80008000u), c);
-        v[3] = mul_bf16x2(((w >> 6) & 0x01C001C0u) | (w & 0x80008000u), c);
+        // a code times 2^6 + 2^12 has its magnitude at bits 8:6 and its sign at bit 15: one multiply-add instead of two shifts
+        const uint32_t u = w >> 8;
+        v[0] = mul_bf16x2(((w & 0x000F000Fu) * 0x1040u) & 0x81C081C0u, c);
+        v[1] = mul_bf16x2(((w & 0x00F000F0u) * 0x0104u) & 0x81C081C0u, c);
+        v[2] = mul_bf16x2(((u & 0x000F000Fu) * 0x1040u) & 0x81C081C0u, c);
+        v[3] = mul_bf16x2(((u & 0x00F000F0u) * 0x0104u) & 0x81C081C0u, c);
         if (TWO) {
             const uint32_t c2 = sc > 128u ? (sc == 255u ? 0x7F807F80u : (sc - 1u) * 0x00800080u) : 0x3F803F80u;
 #pragma unroll
@@ -183,7 +189,7 @@ __device__ __forceinline__ int part_at(int token, int row) {
     return (token >> 1) * 32 + ((row + 4 * (token >> 1)) & 15) * 2 + (token & 1);
 }
 __host__ __device__ constexpr size_t ring_bytes(int fmt, int step) {
-    return (size_t)kWarps * ring_steps(step) * (step * 1024 + kTileN * side_row(fmt, step) * 4);
+    return (size_t)kWarps * kRing * (step * 1024 + kTileN * side_row(fmt, step) * 4);
 }
 __host__ __device__ inline size_t part_bytes(int cs, int tiles, int nt) {
     return (size_t)(cs == 1 ? 2 * kWarps : tiles + kWarps) * kTileN * 8 * nt * sizeof(float);
@@ -201,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     const int units = max(0, min(a.units_slice, units_all - rank * a.units_slice));
     const int k0 = rank * a.units_slice * kUnitK;
     const int xrow = a.units_slice * 256 + kXPad;
-    constexpr int kRing = ring_steps(STEP), kSideRow = side_row(FMT, STEP), kSideBytes = kTileN * kSideRow * 4;
+    constexpr int kSideRow = side_row(FMT, STEP), kSideBytes = kTileN * kSideRow * 4;
     uint8_t* const ring = smem + (size_t)a.M * xrow + warp * (kRing * STEP * 1024);
     uint8_t* const sides = smem + (size_t)a.M * xrow + kWarps * (kRing * STEP * 1024) + warp * (kRing * kSideBytes);
     float* const part = reinterpret_cast<float*>(smem + (size_t)a.M * xrow + ring_bytes(FMT, STEP));
@@ -211,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
 
     // ---- the warp's run of (tile, unit) pairs: its first copies are under way while the activations are staged
     const int total = tiles * units;
-    const int first = total * warp / kWarps, last = total * (warp + 1) / kWarps;  // below 64 x 384 x 16
+    const int first = total * warp / kWarps, last = total * (warp + 1) / kWarps;  // below 64 x 384 x 12
     const int64_t row_codes = a.K / 2, row_side = FMT == kHiF4 ? (int64_t)a.K / 64 * 4 : (int64_t)a.K / 32;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16, side_at = (uint32_t)__cvta_generic_to_shared(sides);
     // The last unit of K may hold one, two or three blocks of 32: a lane beyond the end reads the start of its row instead
@@ -219,35 +225,49 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     const bool beyond = k0 + (units - 1) * kUnitK + t * 32 >= a.K;
     auto step_units = [&](int u, int i) { return min(min(STEP - (u & (STEP - 1)), units - u), last - i); };
     int lu = units > 0 ? first % units : 0, lt = units > 0 ? first / units : 0, li = first, lslot = 0;  // copy cursor
-    const uint8_t *tcodes = a.codes, *tside = a.side;  // the tile's first row; a lane's rows lie at 32-bit offsets from it
-    uint32_t oa = 0, ob = 0;
+    const uint8_t *pa = a.codes, *pb = a.codes, *tside = a.side;  // the lane's two rows at its first k; the tile's first row
     int rows_left = 0;
+    const uint32_t lane_k = (uint32_t)(k0 / 2 + t * 16);
     auto point = [&]() {
         const int n0 = (tile0 + lt) * kTileN;
         rows_left = a.N - 1 - n0;
-        tcodes = a.codes + n0 * row_codes, tside = a.side + n0 * row_side;
-        oa = (uint32_t)min(g, rows_left) * (uint32_t)row_codes, ob = (uint32_t)min(g + 8, rows_left) * (uint32_t)row_codes;
+        const uint8_t* tcodes = a.codes + n0 * row_codes + lane_k;
+        tside = a.side + n0 * row_side;
+        pa = tcodes + (uint32_t)min(g, rows_left) * (uint32_t)row_codes, pb = tcodes + (uint32_t)min(g + 8, rows_left) * (uint32_t)row_codes;
     };
+    const bool ragged = a.K % kUnitK != 0;
+    const uint32_t lane_side = lane / (2 * STEP) * (uint32_t)row_side + lane % (2 * STEP) * 4;  // HiF4: the lane's first word of scales
+    const uint32_t lane_word = (lane / (2 * STEP) * kSideRow + lane % (2 * STEP)) * 4;
     auto copy = [&]() {
         if (li < last) {
             const int n = step_units(lu, li), j0 = lu & (STEP - 1);
+            const uint32_t to = ring_at + lslot * (STEP * 1024);
+            const uint8_t *ca = pa + (lu - j0) * 64, *cb = pb + (lu - j0) * 64;
+            if (n == STEP && !(ragged && lu + n == units)) {
 #pragma unroll
-            for (int j = 0; j < STEP; ++j) {
-                if (j < j0 || j >= j0 + n) continue;
-                const int u = lu - j0 + j;
-                const uint32_t kc = beyond && u == units - 1 ? 0u : (uint32_t)(k0 / 2 + u * 64 + t * 16);
-                const uint32_t dst = ring_at + (lslot * STEP + j) * 1024;
-                copy16(dst, tcodes + oa + kc);
-                copy16(dst + 512, tcodes + ob + kc);
+                for (int j = 0; j < STEP; ++j) copy16(to + j * 1024, ca + j * 64), copy16(to + j * 1024 + 512, cb + j * 64);
+            } else {
+#pragma unroll 1
+                for (int j = j0; j < j0 + n; ++j) {
+                    const bool out = beyond && lu - j0 + j == units - 1;
+                    copy16(to + j * 1024, out ? pa - lane_k : ca + j * 64);
+                    copy16(to + j * 1024 + 512, out ? pb - lane_k : cb + j * 64);
+                }
             }
             const uint32_t dst = side_at + lslot * kSideBytes;
             if (FMT == kHiF4) {
                 constexpr int kWords = 2 * STEP, kRows = 32 / kWords;  // of one copy of the warp
-                const int b = k0 / 64 + (lu - j0) * 2 + lane % kWords, nb = a.K / 64;
+                const int b0 = k0 / 64 + (lu - j0) * 2, b = b0 + lane % kWords, nb = a.K / 64;
+                if (rows_left >= kTileN - 1 && b0 + kWords <= nb) {
+                    const uint8_t* from = tside + lane_side + b0 * 4;
 #pragma unroll
-                for (int i = 0; i < kTileN / kRows; ++i) {
-                    const int r = i * kRows + lane / kWords;
-                    copy4(dst + (r * kSideRow + lane % kWords) * 4, tside + (uint32_t)min(r, rows_left) * (uint32_t)row_side + min(b, nb - 1) * 4, b < nb ? 4 : 0);
+                    for (int i = 0; i < kTileN / kRows; ++i) copy4(dst + lane_word + i * kRows * kSideRow * 4, from + i * kRows * (uint32_t)row_side);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kTileN / kRows; ++i) {
+                        const uint32_t r = min(i * kRows + lane / kWords, rows_left);
+                        copy4(dst + lane_word + i * kRows * kSideRow * 4, tside + r * (uint32_t)row_side + min(b, nb - 1) * 4, b < nb ? 4 : 0);
+                    }
                 }
             } else {
                 // whole aligned words over the bytes of a row, of which the first may belong to the row before; the array
@@ -327,12 +347,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
         copies_wait<kRing - 1>();
         __syncwarp();  // the scales were copied by other lanes
         const uint8_t* codes = ring + slot * (STEP * 1024) + lane * 16;
-        const uint8_t *pa = side_a + slot * kSideBytes + shift_a, *pb = side_b + slot * kSideBytes + shift_b;
+        const uint8_t *sa = side_a + slot * kSideBytes + shift_a, *sb = side_b + slot * kSideBytes + shift_b;
         const int xat = (cu - j0) * 256;
         bool two = false;
         if (FMT == kMXFP4) {
 #pragma unroll
-            for (int j = 0; j < STEP; ++j) two |= max(pa[j * 4], pb[j * 4]) > 128;
+            for (int j = 0; j < STEP; ++j) two |= max(sa[j * 4], sb[j * 4]) > 128;
             two = __any_sync(0xFFFFFFFFu, two);
         }
         auto one = [&](int j, auto with_second) {
@@ -340,11 +360,11 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
             const uint4 qb = *reinterpret_cast<const uint4*>(codes + j * 1024 + 512);
             Scale<FMT> fa, fb;
             if (FMT == kHiF4) {
-                fa.set(*reinterpret_cast<const uint32_t*>(pa + j * 8), t & 1);
-                fb.set(*reinterpret_cast<const uint32_t*>(pb + j * 8), t & 1);
+                fa.set(*reinterpret_cast<const uint32_t*>(sa + j * 8), t & 1);
+                fb.set(*reinterpret_cast<const uint32_t*>(sb + j * 8), t & 1);
             } else {
                 const bool none = beyond && cu - j0 + j >= units - 1;
-                fa.set(pa[j * 4], none), fb.set(pb[j * 4], none);
+                fa.set(sa[j * 4], none), fb.set(sb[j * 4], none);
             }
             unit<FMT, NT, decltype(with_second)::value>(qa, qb, fa, fb, xs, xat + j * 256, acc);
         };
@@ -475,7 +495,7 @@ GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
     const int tiles = (int)((N + kTileN - 1) / kTileN), units = (int)((K + kUnitK - 1) / kUnitK), nt = M > 8 ? 2 : 1;
     GemvPlan best{0, 0, 0, 0, 0};
     double best_cost = 0;
-    for (int step = 2; step <= (nt == 1 ? 4 : 2); step += 2) {
+    for (int step = 2; step <= 4; step += 2) {
         for (int lg = 0; lg < 4; ++lg) {
             const int cs = 1 << lg, us = (units + cs - 1) / cs;
             const size_t x = (size_t)M * (us * 256 + kXPad), ring = ring_bytes(fmt, step);
@@ -487,7 +507,7 @@ GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
             for (int waves = (tiles + slots * most - 1) / (slots * most), tried = 0; tried < 4; ++waves, ++tried) {
                 const int T = (tiles + slots * waves - 1) / (slots * waves);
                 const double units_warp = (T * us + kWarps - 1) / kWarps;
-                const double cost = (double)waves * (units_warp * (step == 4 ? 1120 : 1200) + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
+                const double cost = (double)waves * (units_warp * (step == 4 ? 1000 : 1080) + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
                 if (best.cs == 0 || cost < best_cost) best = GemvPlan{cs, T, us, step, x + ring + part_bytes(cs, T, nt)}, best_cost = cost;
                 if (T == 1) break;
             }
@@ -516,7 +536,7 @@ int launch_gemv(const GemvArgs& a, const GemvPlan& p, cudaStream_t stream) {
 }
 template <int FMT>
 int launch_gemv(const GemvArgs& a, const GemvPlan& p, cudaStream_t stream) {
-    if (a.M > 8) return launch_gemv<FMT, 2, 2>(a, p, stream);
+    if (a.M > 8) return p.step == 4 ? launch_gemv<FMT, 2, 4>(a, p, stream) : launch_gemv<FMT, 2, 2>(a, p, stream);
     return p.step == 4 ? launch_gemv<FMT, 1, 4>(a, p, stream) : launch_gemv<FMT, 1, 2>(a, p, stream);
 }
 
