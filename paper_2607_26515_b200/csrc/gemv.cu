@@ -81,6 +81,11 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
+template <int BYTES>
+__device__ __forceinline__ void copy_scales(uint32_t dst, const void* src) {
+    static_assert(BYTES == 8 || BYTES == 16);
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
 // the first `n` bytes of a word (0 to 4), zeros behind them
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, int n) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
@@ -236,6 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
         pa = tcodes + (uint32_t)min(g, rows_left) * (uint32_t)row_codes, pb = tcodes + (uint32_t)min(g + 8, rows_left) * (uint32_t)row_codes;
     };
     const bool ragged = a.K % kUnitK != 0;
+    const bool even = FMT == kMXFP4 && (row_side | (k0 / 32)) % (STEP * 4) == 0;  // a step's scales of a row are one aligned piece
     const uint32_t lane_side = lane / (2 * STEP) * (uint32_t)row_side + lane % (2 * STEP) * 4;  // HiF4: the lane's first word of scales
     const uint32_t lane_word = (lane / (2 * STEP) * kSideRow + lane % (2 * STEP)) * 4;
     auto copy = [&]() {
@@ -269,6 +275,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
                         copy4(dst + lane_word + i * kRows * kSideRow * 4, tside + r * (uint32_t)row_side + min(b, nb - 1) * 4, b < nb ? 4 : 0);
                     }
                 }
+            } else if (even) {  // one copy per row
+                const uint8_t* from = tside + (uint32_t)min(lane, rows_left) * (uint32_t)row_side + (k0 / 32 + (lu - j0) * 4);
+                if (lane < kTileN) copy_scales<STEP * 4>(dst + lane * (STEP * 4), from);
             } else {
                 // whole aligned words over the bytes of a row, of which the first may belong to the row before; the array
                 // may end within a word
@@ -331,7 +340,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemv_kernel(const __grid_constant
     const uint8_t* xs[NT];  // the lane's token of each group (columns behind the last token repeat it; they are not stored)
 #pragma unroll
     for (int q = 0; q < NT; ++q) xs[q] = smem + min(q * 8 + g, a.M - 1) * xrow + t * 16;
-    const uint8_t *side_a = sides + g * (kSideRow * 4), *side_b = side_a + 8 * (kSideRow * 4);
+    const int side_pitch = even ? STEP * 4 : kSideRow * 4;
+    const uint8_t *side_a = sides + g * side_pitch, *side_b = side_a + 8 * side_pitch;
     int shift_a = 0, shift_b = 0;  // the byte of its word that a row's MXFP4 scales start on
     auto tile_sides = [&]() {
         if (FMT == kMXFP4) {
