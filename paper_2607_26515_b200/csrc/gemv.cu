@@ -18,7 +18,7 @@
 // Twelve warps with four units at a time are faster than sixteen with two (the same case: 65 against 73 us) or eight (68).
 //
 // Measured, weights from HBM: 3584 -> 37888, HiF4, 23 us for one token and 25 for eight (3.3 TB/s, 0.50 of the copy rate); MXFP4
-// 24.5 us; 11 tokens 3584 -> 100003 65 us (3.1 TB/s); 2048 -> 2048 4.1 us, of which the launch and the chain load, expand, sum
+// 24 us; 11 tokens 3584 -> 100003 65 us (3.1 TB/s); 2048 -> 2048 4.0 us, of which the launch and the chain load, expand, sum
 // are all.  It is bound by the arithmetic of the expansion: without it (the codes taken as they are) 3584 -> 37888 takes 17 us,
 // without the copies 19.5.
 #include "common.cuh"
@@ -499,8 +499,10 @@ struct GemvPlan {
 
 constexpr size_t kSmemMax = 227 * 1024;
 
-// Splits the K range over cs CTAs and gives each cluster T row tiles so that the busiest SM finishes first.  Cycles per unit
-// and the fixed costs are rough measurements; only their proportions matter.
+// Splits the K range over cs CTAs and gives each cluster T row tiles so that the busiest SM finishes first.  Cycles per unit, for
+// staging the activations and for joining the sums are rough measurements (4 tokens 11008 -> 2048: 9.2 us in four slices and
+// 10.3 in one; 16 tokens 3584 -> 3584: 9.9 in two, 11.9 in one; 16 tokens 2048 -> 22016: 21.8 in two, 16.0 in one).
+constexpr double kExchange[4] = {0, 1300, 2300, 4500};
 GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
     const int tiles = (int)((N + kTileN - 1) / kTileN), units = (int)((K + kUnitK - 1) / kUnitK), nt = M > 8 ? 2 : 1;
     GemvPlan best{0, 0, 0, 0, 0};
@@ -509,6 +511,8 @@ GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
         for (int lg = 0; lg < 4; ++lg) {
             const int cs = 1 << lg, us = (units + cs - 1) / cs;
             const size_t x = (size_t)M * (us * 256 + kXPad), ring = ring_bytes(fmt, step);
+            // MXFP4 scales that come word by word
+            const double odd = fmt == kMXFP4 && (K / 32 % (step * 4) || (cs > 1 && us % step)) ? 1.05 : 1.0;
             // the fewest waves that shared memory and kMaxTiles allow, and up to three more: the smallest T for each
             const int slots = resident_clusters(cs);
             int most = std::min(kMaxTiles, tiles);
@@ -517,7 +521,8 @@ GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
             for (int waves = (tiles + slots * most - 1) / (slots * most), tried = 0; tried < 4; ++waves, ++tried) {
                 const int T = (tiles + slots * waves - 1) / (slots * waves);
                 const double units_warp = (T * us + kWarps - 1) / kWarps;
-                const double cost = (double)waves * (units_warp * (step == 4 ? 1000 : 1080) + 3000 + (double)x / 64 + (cs > 1 ? 3000 + 1000 * lg : 0));
+                const double sums = cs == 1 ? 120.0 * M : kExchange[lg] + 2.9 * (T * kTileN * M);
+                const double cost = waves * (units_warp * (step == 4 ? 1000 : 1080) * odd + (step == 4 ? 3700 : 3000) + (double)x / 16 + sums);
                 if (best.cs == 0 || cost < best_cost) best = GemvPlan{cs, T, us, step, x + ring + part_bytes(cs, T, nt)}, best_cost = cost;
                 if (T == 1) break;
             }
