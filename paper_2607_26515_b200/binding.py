@@ -530,12 +530,13 @@ _OUT = {torch.bfloat16: OUT_BF16, torch.float32: OUT_F32}
 _BF16, _F32 = torch.bfloat16, torch.float32
 # the current stream's handle without a Stream object around it (0.1 instead of 3 us)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _run(index: int, stream, body):
     """body(stream handle) with device `index` current and, if a stream is named, that stream current too: the allocator
     then ties what the call allocates to the stream its kernels run on."""
-    if stream is None and torch.cuda.current_device() == index:
+    if stream is None and _current_device() == index:
         return body(_raw_stream(index))
     if stream is not None and not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(stream), device=index)

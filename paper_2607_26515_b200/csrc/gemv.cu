@@ -516,8 +516,8 @@ GemvPlan plan_gemv(int fmt, int M, int64_t N, int64_t K) {
             // the fewest waves that shared memory and kMaxTiles allow, and up to three more: the smallest T for each
             const int slots = resident_clusters(cs);
             int most = std::min(kMaxTiles, tiles);
-            while (most > 0 && x + ring + part_bytes(cs, most, nt) > kSmemMax) --most;
-            if (most == 0) continue;
+            if (x + ring + part_bytes(cs, 1, nt) > kSmemMax) continue;
+            if (cs > 1) most = std::min(most, 1 + (int)((kSmemMax - x - ring - part_bytes(cs, 1, nt)) / (kTileN * 8 * nt * sizeof(float))));
             for (int waves = (tiles + slots * most - 1) / (slots * most), tried = 0; tried < 4; ++waves, ++tried) {
                 const int T = (tiles + slots * waves - 1) / (slots * waves);
                 const double units_warp = (T * us + kWarps - 1) / kWarps;
