@@ -533,17 +533,15 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i:
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _run(index: int, stream, body):
-    """body(stream handle) with device `index` current and, if a stream is named, that stream current too: the allocator
-    then ties what the call allocates to the stream its kernels run on."""
-    if stream is None and _current_device() == index:
-        return body(_raw_stream(index))
+def _elsewhere(index: int, stream, call):
+    """call() with device `index` current and, if a stream is named, that stream current too: the allocator then ties what
+    the call allocates to the stream its kernels run on."""
     if stream is not None and not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(stream), device=index)
     if stream is not None and stream.device.index != index:
         raise ValueError(f"the stream belongs to {stream.device}, the tensors to cuda:{index}")
     with torch.cuda.device(index), torch.cuda.stream(stream):
-        return body(_raw_stream(index))
+        return call()
 
 
 def _require(ok: bool, msg: str) -> None:
@@ -551,9 +549,20 @@ def _require(ok: bool, msg: str) -> None:
         raise ValueError(msg)
 
 
+def _first(t: torch.Tensor, name: str):
+    """(M, K, row pitch in elements, type code, device index) of a call's first tensor: a matrix on a device with unit inner
+    stride (a single row has no pitch of its own: any multiple of 8 that covers it will do)."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in _OUT:
+        raise ValueError(f"{name} must be a 2-D CUDA tensor, bf16 or fp32")
+    M, K = t.shape
+    ld, inner = t.stride()
+    if inner != 1 and K > 1:
+        raise ValueError(f"{name} must have unit inner stride")
+    return M, K, ld if M > 1 else (K + 7) // 8 * 8, _OUT[t.dtype], t.get_device()
+
+
 def _rows(t: torch.Tensor, name: str, M: int, K: int, dtype, index: int) -> int:
-    """Checks that t is an [M, K] matrix of one type on one device with unit inner stride; its row pitch in elements (a
-    single row has none of its own: any multiple of 8 that covers it will do)."""
+    """Checks that t is an [M, K] matrix of one type on one device with unit inner stride; its row pitch as in _first."""
     if t.dtype is not dtype or t.shape != (M, K) or t.get_device() != index or (K > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be a {dtype} tensor [{M}, {K}] on cuda:{index} with unit inner stride")
     return t.stride(0) if M > 1 else (K + 7) // 8 * 8
@@ -576,20 +585,14 @@ def _new(M: int, K: int, dtype, index: int) -> torch.Tensor:
     return torch.empty_strided((M, K), (K, 1), dtype=dtype, device=index)
 
 
-def _first(t: torch.Tensor, name: str):
-    """(M, K, type code, device index) of a call's first tensor."""
-    if t.dim() != 2 or not t.is_cuda or t.dtype not in _OUT:
-        raise ValueError(f"{name} must be a 2-D CUDA tensor, bf16 or fp32")
-    M, K = t.shape
-    return M, K, _OUT[t.dtype], t.get_device()
-
-
 def w4a16_gemv(X: torch.Tensor, w_codes: torch.Tensor, w_side: torch.Tensor, fmt: str = "hif4",
                out_dtype: torch.dtype = torch.bfloat16, Y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """*_w4a16_gemv: Y = X deq(Q(W))^T for at most GEMV_MAX_TOKENS token rows, streaming the packed weights once."""
     fn = _fn(fmt, "hif4_w4a16_gemv", "mxfp4_w4a16_gemv")
-    M, K, _, index = _first(X, "X")
-    ldx = _rows(X, "X", M, K, _BF16, index)
+    M, K, ldx, code, index = _first(X, "X")
+    _require(code == OUT_BF16, "X must be bf16")
+    if stream is not None or _current_device() != index:
+        return _elsewhere(index, stream, lambda: w4a16_gemv(X, w_codes, w_side, fmt, out_dtype, Y))
     _require(w_codes.dim() == 2, "w_codes must be [N, K/2]")
     N = w_codes.shape[0]
     if w_codes.dtype is not torch.uint8 or w_codes.shape[1] * 2 != K or not w_codes.is_contiguous() or w_codes.get_device() != index:
@@ -599,14 +602,12 @@ def w4a16_gemv(X: torch.Tensor, w_codes: torch.Tensor, w_side: torch.Tensor, fmt
         raise ValueError(f"w_meta / w_scale must be contiguous {side_type} [N, K/{block}] on cuda:{index}")
     out_dtype = out_dtype if Y is None else Y.dtype
     _require(out_dtype in _OUT, "Y must be bf16 or fp32")
-    ldy = (N + 7) // 8 * 8 if Y is None else _rows(Y, "Y", M, N, out_dtype, index)
-
-    def body(st):
-        y = _new_rows(M, N, out_dtype, index) if Y is None else Y
-        _check(fn(X.data_ptr(), M, K, ldx, w_codes.data_ptr(), w_side.data_ptr(), N, y.data_ptr(), _OUT[out_dtype], ldy, st))
-        return y
-
-    return _run(index, stream, body)
+    if Y is None:
+        Y, ldy = _new_rows(M, N, out_dtype, index), (N + 7) // 8 * 8
+    else:
+        ldy = _rows(Y, "Y", M, N, out_dtype, index)
+    _check(fn(X.data_ptr(), M, K, ldx, w_codes.data_ptr(), w_side.data_ptr(), N, Y.data_ptr(), _OUT[out_dtype], ldy, _raw_stream(index)))
+    return Y
 
 
 def _join_gate(gate, M: int, K: int, index: int):
@@ -627,8 +628,10 @@ def block_join(H: torch.Tensor, B: torch.Tensor, gamma_pre: Optional[torch.Tenso
 
     gamma_post None: the branch B is added as it is; gamma_pre None: X is None.  gate: None, [K] (one for all tokens) or
     [M, K]; act "linear" or "sigmoid".  H_out may be H."""
-    M, K, dtype, index = _first(H, "H")
-    ldh, ldb = _rows(H, "H", M, K, H.dtype, index), _rows(B, "B", M, K, _BF16, index)
+    M, K, ldh, code, index = _first(H, "H")
+    if stream is not None or _current_device() != index:
+        return _elsewhere(index, stream, lambda: block_join(H, B, gamma_pre, gamma_post, gate, act, alpha, eps, H_out, X))
+    ldb = _rows(B, "B", M, K, _BF16, index)
     pre = None if gamma_pre is None else _vector(gamma_pre, "gamma_pre", K, _BF16, index)
     post = None if gamma_post is None else _vector(gamma_post, "gamma_post", K, _BF16, index)
     g, ldg = _join_gate(gate, M, K, index)
@@ -636,19 +639,17 @@ def block_join(H: torch.Tensor, B: torch.Tensor, gamma_pre: Optional[torch.Tenso
     _require(X is None or gamma_pre is not None, "X needs gamma_pre")
 
     ldho = ldx = (K + 7) // 8 * 8
-    if H_out is not None:
+    if H_out is None:
+        H_out = _new_rows(M, K, H.dtype, index)
+    else:
         ldho = _rows(H_out, "H_out", M, K, H.dtype, index)
     if X is not None:
         ldx = _rows(X, "X", M, K, _BF16, index)
-
-    def body(st):
-        h = _new_rows(M, K, H.dtype, index) if H_out is None else H_out
-        x = _new_rows(M, K, _BF16, index) if X is None and gamma_pre is not None else X
-        _check(lib().resq_block_join(H.data_ptr(), dtype, B.data_ptr(), M, K, ldh, ldb, g, ldg, _GATES[act], post, pre, alpha, eps,
-                                     h.data_ptr(), ldho, _ptr(x), ldx, st))
-        return h, x
-
-    return _run(index, stream, body)
+    elif gamma_pre is not None:
+        X = _new_rows(M, K, _BF16, index)
+    _check(lib().resq_block_join(H.data_ptr(), code, B.data_ptr(), M, K, ldh, ldb, g, ldg, _GATES[act], post, pre, alpha, eps,
+                                 H_out.data_ptr(), ldho, _ptr(X), ldx, _raw_stream(index)))
+    return H_out, X
 
 
 @functools.lru_cache(maxsize=1024)
@@ -663,8 +664,11 @@ def block_join_backward(dH_out: Optional[torch.Tensor], dX: Optional[torch.Tenso
     """resq_block_join_backward -> dict(dH, dB[, dgate][, dgamma_post][, dgamma_pre]) from the gradients of H' and X (either
     may be None) and the forward call's H' and inputs.  dgate has the gate's shape, fp32 for a channel gate [K], else bf16;
     the norms' gradients are fp32.  dH may be dH_out."""
-    M, K, dtype, index = _first(H_out, "H_out")
-    ldh, ldb = _rows(H_out, "H_out", M, K, H_out.dtype, index), _rows(B, "B", M, K, _BF16, index)
+    M, K, ldh, code, index = _first(H_out, "H_out")
+    if stream is not None or _current_device() != index:
+        return _elsewhere(index, stream, lambda: block_join_backward(dH_out, dX, H_out, B, gamma_pre, gamma_post, gate, act, alpha, eps, dH,
+                                                                     workspace))
+    ldb = _rows(B, "B", M, K, _BF16, index)
     _require(dH_out is not None or dX is not None, "one of dH_out and dX is needed")
     _require(dX is None or gamma_pre is not None, "dX needs gamma_pre")
     lddho = 0 if dH_out is None else _rows(dH_out, "dH_out", M, K, H_out.dtype, index)
@@ -679,45 +683,41 @@ def block_join_backward(dH_out: Optional[torch.Tensor], dX: Optional[torch.Tenso
     if dH is not None:
         lddh = _rows(dH, "dH", M, K, H_out.dtype, index)
 
-    def body(st):
-        out = {"dH": _new_rows(M, K, H_out.dtype, index) if dH is None else dH, "dB": _new_rows(M, K, _BF16, index)}
-        columns = [n for n, on in (("dgamma_pre", dX is not None), ("dgamma_post", post is not None), ("dgate", g is not None and ldg == 0)) if on]
-        if columns:
-            out.update(zip(columns, _new(len(columns), K, _F32, index).unbind()))
-        if ldg:
-            out["dgate"] = _new_rows(M, K, _BF16, index)
-        ws = alloc_workspace(block_join_backward_workspace_bytes(M, K), index) if workspace is None else workspace
-        _check(lib().resq_block_join_backward(
-            _ptr(dH_out), _ptr(dX), H_out.data_ptr(), dtype, B.data_ptr(), M, K, lddho, lddx, ldh, ldb, g, ldg, _GATES[act], post, pre,
-            alpha, eps, out["dH"].data_ptr(), lddh, out["dB"].data_ptr(), ldn, _ptr(out.get("dgate")), ldn if ldg else 0,
-            _ptr(out.get("dgamma_post")), _ptr(out.get("dgamma_pre")), ws.data_ptr(), ws.numel() * ws.element_size(), st))
-        return out
-
-    return _run(index, stream, body)
+    out = {"dH": _new_rows(M, K, H_out.dtype, index) if dH is None else dH, "dB": _new_rows(M, K, _BF16, index)}
+    columns = [n for n, on in (("dgamma_pre", dX is not None), ("dgamma_post", post is not None), ("dgate", g is not None and ldg == 0)) if on]
+    if columns:
+        out.update(zip(columns, _new(len(columns), K, _F32, index).unbind()))
+    if ldg:
+        out["dgate"] = _new_rows(M, K, _BF16, index)
+    if workspace is None:
+        workspace = _new(1, max(block_join_backward_workspace_bytes(M, K), 256), torch.uint8, index)
+    _check(lib().resq_block_join_backward(
+        _ptr(dH_out), _ptr(dX), H_out.data_ptr(), code, B.data_ptr(), M, K, lddho, lddx, ldh, ldb, g, ldg, _GATES[act], post, pre,
+        alpha, eps, out["dH"].data_ptr(), lddh, out["dB"].data_ptr(), ldn, _ptr(out.get("dgate")), ldn if ldg else 0,
+        _ptr(out.get("dgamma_post")), _ptr(out.get("dgamma_pre")), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        _raw_stream(index)))
+    return out
 
 
 def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, temperature: float = 1.0, top: int = 0, stream=None):
     """resq_token_logprobs -> dict(logp, entropy, peak, log_sum[, top_ids, top_logp]) of the rows of logits [M, V] (bf16 or
     fp32) for tokens int64 [M] (outside 0 .. V - 1: none, logp 0).  top > 0: ids int32 [M, top] and log-probabilities of the
     largest logits, largest first, equal ones by lower id."""
-    M, V, dtype, index = _first(logits, "logits")
-    ld = _rows(logits, "logits", M, V, logits.dtype, index)
+    M, V, ld, code, index = _first(logits, "logits")
+    if stream is not None or _current_device() != index:
+        return _elsewhere(index, stream, lambda: token_logprobs(logits, tokens, temperature, top))
     tok = _vector(tokens, "tokens", M, torch.int64, index)
-
-    def body(st):
-        values = _new(4, M, _F32, index)
-        logp, entropy, peak, log_sum = values.unbind()
-        out = {"logp": logp, "entropy": entropy, "peak": peak, "log_sum": log_sum}
-        ids = top_logp = None
-        if top > 0:
-            ids = out["top_ids"] = _new(M, top, torch.int32, index)
-            top_logp = out["top_logp"] = _new(M, top, _F32, index)
-        at = values.data_ptr()
-        _check(lib().resq_token_logprobs(logits.data_ptr(), dtype, M, V, ld, tok, temperature, top, at, at + 4 * M, at + 8 * M, at + 12 * M,
-                                         _ptr(ids), _ptr(top_logp), st))
-        return out
-
-    return _run(index, stream, body)
+    values = _new(4, M, _F32, index)
+    logp, entropy, peak, log_sum = values.unbind()
+    out = {"logp": logp, "entropy": entropy, "peak": peak, "log_sum": log_sum}
+    ids = top_logp = None
+    if top > 0:
+        ids = out["top_ids"] = _new(M, top, torch.int32, index)
+        top_logp = out["top_logp"] = _new(M, top, _F32, index)
+    at = values.data_ptr()
+    _check(lib().resq_token_logprobs(logits.data_ptr(), code, M, V, ld, tok, temperature, top, at, at + 4 * M, at + 8 * M, at + 12 * M,
+                                     _ptr(ids), _ptr(top_logp), _raw_stream(index)))
+    return out
 
 
 def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, logp: torch.Tensor, peak: torch.Tensor, log_sum: torch.Tensor,
@@ -725,22 +725,22 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, logp: to
                             temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """resq_token_logprobs_backward: the gradient of the logits from token_logprobs' results and the gradients of logp and
     (optionally) entropy; dlogits may be the logits tensor itself."""
-    M, V, dtype, index = _first(logits, "logits")
-    ld = _rows(logits, "logits", M, V, logits.dtype, index)
+    M, V, ld, code, index = _first(logits, "logits")
+    if stream is not None or _current_device() != index:
+        return _elsewhere(index, stream, lambda: token_logprobs_backward(logits, tokens, logp, peak, log_sum, entropy, dlogp, dentropy,
+                                                                         temperature, dlogits))
     _require(logp is not None and peak is not None and log_sum is not None and dlogp is not None, "logp, peak, log_sum and dlogp are needed")
     _require(dentropy is None or entropy is not None, "dentropy needs entropy")
     values = [_vector(tokens, "tokens", M, torch.int64, index)]
     values += [None if t is None else _vector(t, name, M, _F32, index)
                for name, t in (("logp", logp), ("peak", peak), ("log_sum", log_sum), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy))]
-
-    ldd = (V + 7) // 8 * 8 if dlogits is None else _rows(dlogits, "dlogits", M, V, logits.dtype, index)
-
-    def body(st):
-        d = _new_rows(M, V, logits.dtype, index) if dlogits is None else dlogits
-        _check(lib().resq_token_logprobs_backward(logits.data_ptr(), dtype, M, V, ld, values[0], temperature, *values[1:], d.data_ptr(), ldd, st))
-        return d
-
-    return _run(index, stream, body)
+    if dlogits is None:
+        dlogits, ldd = _new_rows(M, V, logits.dtype, index), (V + 7) // 8 * 8
+    else:
+        ldd = _rows(dlogits, "dlogits", M, V, logits.dtype, index)
+    _check(lib().resq_token_logprobs_backward(logits.data_ptr(), code, M, V, ld, values[0], temperature, *values[1:], dlogits.data_ptr(), ldd,
+                                              _raw_stream(index)))
+    return dlogits
 
 
 def check(workspace: torch.Tensor, stream=None) -> int:
