@@ -170,10 +170,10 @@ __device__ __forceinline__ void block_sum(float (&v)[NV], float* buf) {
 
 // launch_kernel() with clusters of `cs` CTAs.
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_clusters(void (*kern)(KArgs...), unsigned grid, unsigned block, size_t smem, int cs, cudaStream_t stream, Args... args) {
+inline cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, unsigned block, size_t smem, int cs, cudaStream_t stream, Args... args) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
