@@ -174,6 +174,7 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int k, ui
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
         const uint64_t mine = keys[i];
         int r = 0;
+#pragma unroll 4
         for (int j = 0; j < n; ++j) r += keys[j] > mine;
         if (r < k) out[r] = mine;
     }
@@ -403,29 +404,33 @@ __global__ void __launch_bounds__(kMaxLpThreads, 2) logprobs_kernel(const __grid
                 auto pass = [&](const Raw8<T>& g, int v) {
                     float z[8];
                     get_logits(g, a.V - v * 8, z);
+                    unsigned mask = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (z[e] >= lv && v * 8 + e < a.V && top_key(z[e], v * 8 + e) >= low) mask |= 1u << e;
+                    if (mask == 0) return;
+                    int at = atomicAdd(&count[1], __popc(mask));
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        if (!(z[e] >= lv)) continue;
-                        const uint64_t q8 = top_key(z[e], v * 8 + e);
-                        if (v * 8 + e < a.V && q8 >= low) {
-                            const int at = atomicAdd(&count[1], 1);
-                            if (at < kCandidates) cand[at] = q8;
-                        }
+                        if (!(mask >> e & 1)) continue;
+                        if (at < kCandidates) cand[at] = top_key(z[e], v * 8 + e);
+                        ++at;
                     }
                 };
                 // one place in the code takes them all (it runs once per row: its length costs time)
-                const bool any = v0 + tid < v1 && lane_max >= lv, all = any && lane_second >= lv;
+                const int per = (v1 - v0 + threads - 1) / threads;  // vectors of a lane
+                const bool any = v0 + tid < v1 && lane_max >= lv, all = any && per > kV && lane_second >= lv;
                 if (all) hot[atomicAdd(&count[0], 1)] = (uint16_t)tid;
                 __syncthreads();
-                const int lanes = count[0], per = (v1 - v0 + threads - 1) / threads, parts = (per + 31) / 32;
-                // item 0 to kV - 1: the lane's own group; then, of the lanes on the list, 32 vectors per warp and item
+                const int items = count[0] * per;
+                // step 0 to kV - 1: the lane's own group; then the vectors of the lanes on the list, 32 per warp and step
                 auto fetch = [&](int n, Raw8<T>& g) {
                     int v = v1;
                     if (n < kV) {
                         if (any && !all) v = v0 + (lane_it * kV + n) * threads + tid;
                     } else {
-                        const int i = w + (n - kV) * warps, j = (i % parts) * 32 + lane;
-                        if (i < lanes * parts && j < per) v = v0 + j * threads + hot[i / parts];
+                        const int i = (n - kV) * threads + tid;
+                        if (i < items) v = v0 + i % per * threads + hot[i / per];
                     }
                     if (v < v1) g.load(x + (int64_t)v * 8, a.V - v * 8);
                     return v;
@@ -436,7 +441,7 @@ __global__ void __launch_bounds__(kMaxLpThreads, 2) logprobs_kernel(const __grid
 #pragma unroll
                 for (int b = 0; b < kFlight; ++b) at[b] = fetch(b, g[b]);
 #pragma unroll 1
-                for (int n = 0; n < kV || w + (n - kV) * warps < lanes * parts; ++n) {
+                for (int n = 0; n < kV || (n - kV) * threads + w * 32 < items; ++n) {
                     if (at[0] < v1) pass(g[0], at[0]);
 #pragma unroll
                     for (int b = 0; b + 1 < kFlight; ++b) g[b] = g[b + 1], at[b] = at[b + 1];
@@ -638,7 +643,9 @@ int resq_token_logprobs(const void* logits, int dtype, int64_t M, int64_t V, int
     int cs = 1;
     while (cs < kMaxCluster && M * cs * 2 <= 256 && vecs / (2 * cs) >= 2048) cs *= 2;
     const int64_t slice = (vecs + cs - 1) / cs;
-    const int64_t most = M * cs <= 2 * 148 ? kMaxLpThreads : 256, per_lane = kV;
+    // With alternatives rows of up to 64 vectors get a thread for each: the bound wants `top` lanes with logits (4000 x 500, top
+    // 32: 30 against 79 us; 4000 x 1000 would lose, 30 against 27 us for one alternative).
+    const int64_t most = M * cs <= 2 * 148 ? kMaxLpThreads : 256, per_lane = top && slice <= 64 ? 1 : kV;
     const unsigned threads = (unsigned)std::min<int64_t>(most, ((slice + per_lane - 1) / per_lane + 31) / 32 * 32);
     if (M * cs > INT32_MAX) return fail(RESQ_ERR_SHAPE, what, "too many rows for one call");
     LpArgs a{logits, ld, tokens, logp, entropy, peak, log_sum, top_ids, top_logp, (int)V, top, (int)slice, 1.0f / temperature};

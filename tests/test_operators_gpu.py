@@ -662,3 +662,31 @@ def test_captured_and_replayed_with_new_inputs():
     graphs[1].replay()
     torch.cuda.synchronize()
     assert all(torch.equal(outs[0][n], changed[n]) for n in changed) and all(torch.equal(outs[1][n], want[1][n]) for n in want[1])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [19, 150, 300, 512, 520, 1000, 2050, 8200, 131072])
+def test_logprobs_alternatives_that_share_a_lane(V, dtype):
+    """Large logits a fixed distance apart, for the distances at which a division of the row among threads gives several of
+    them to one thread, in one vector, in neighbouring vectors and far apart; rows with fewer vectors than alternatives."""
+    g = gen(V + 9)
+    base = randn(1, V, dtype, g).float()[0]
+    steps = [s for s in (1, 3, 8, 16, 256, 512, 1024, 2048, 4096, 8192) if s < V]
+    x, _ = rows(len(steps) + 1, V, dtype, 8)
+    for i, s in enumerate(steps):
+        row = base.clone()
+        at = torch.arange(i, V, s, device="cuda")[:40]
+        row[at] = 6 + torch.randperm(len(at), generator=g, device="cuda").float() / 64
+        x[i].copy_(row)
+    x[-1].copy_(base)
+    tok = torch.randint(0, V, (len(steps) + 1,), generator=g, device="cuda")
+    for top in (1, 5, 19, 32):
+        if top <= V:
+            check_logprobs(x, tok, 1.0, top)
+
+
+@pytest.mark.parametrize("stream, post, gate, act", [(BF, True, "full", "sigmoid"), (F32, True, "channel", "linear"), (F32, False, "none", "linear")])
+@pytest.mark.parametrize("M, K", [(1, 4099), (160, 4104), (33, 5120), (300, 5121), (700, 250), (2000, 500), (3000, 200), (1100, 1000)])
+def test_join_backward_at_the_bounds_of_its_splits(M, K, stream, post, gate, act):
+    """Row lengths on both sides of the thread counts, and every way to add the partial column sums."""
+    test_join_backward_parity(M, K, stream, post, gate, act)
