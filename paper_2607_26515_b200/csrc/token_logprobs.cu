@@ -637,15 +637,27 @@ int resq_token_logprobs(const void* logits, int dtype, int64_t M, int64_t V, int
         return fail(RESQ_ERR_ALIGN, what, "tokens must be 8-byte aligned, the outputs 4-byte aligned");
     // Few rows are sliced, up to 256 CTAs and not below 16384 logits a slice: 1 x 131072 takes 5.2 us in eight slices and 9.8
     // in one, but 512 x 131072 33 us in two and 31 in one, and 8000 logits a slice lose (a cluster's launch costs more than
-    // its CTAs').  Up to two CTAs per SM have 512 threads (250 x 131072: 17.7 against 23.4 us), more have 256 (1000 x 20000:
-    // 15.1 against 23.6 us).
+    // its CTAs').
     const int64_t vecs = (V + 7) / 8;
     int cs = 1;
     while (cs < kMaxCluster && M * cs * 2 <= 256 && vecs / (2 * cs) >= 2048) cs *= 2;
     const int64_t slice = (vecs + cs - 1) / cs;
+    // An SM holds 1024 of these threads.  Up to eight CTAs per SM share them, so that all rows are under way at once (740 x
+    // 131072, fp32: 59 us with 192 threads, 71 with 256, which leave 148 rows to a second wave); beyond, the number of CTAs
+    // per SM whose waves come out best.
+    const int64_t ctas = M * cs;
+    int per_sm = 2;
+    if (ctas <= 8 * 148) {
+        while (ctas > per_sm * 148) per_sm = per_sm == 6 ? 8 : per_sm + 1;
+    } else {
+        per_sm = 4;
+        auto rows_sm = [&](int n) { return (ctas + 148 * n - 1) / (148 * n) * n; };
+        for (int n = 5; n <= 6; ++n)
+            if (rows_sm(n) < rows_sm(per_sm)) per_sm = n;
+    }
     // With alternatives rows of up to 64 vectors get a thread for each: the bound wants `top` lanes with logits (4000 x 500, top
     // 32: 30 against 79 us; 4000 x 1000 would lose, 30 against 27 us for one alternative).
-    const int64_t most = M * cs <= 2 * 148 ? kMaxLpThreads : 256, per_lane = top && slice <= 64 ? 1 : kV;
+    const int64_t most = 1024 / per_sm / 32 * 32, per_lane = top && slice <= 64 ? 1 : kV;
     const unsigned threads = (unsigned)std::min<int64_t>(most, ((slice + per_lane - 1) / per_lane + 31) / 32 * 32);
     if (M * cs > INT32_MAX) return fail(RESQ_ERR_SHAPE, what, "too many rows for one call");
     LpArgs a{logits, ld, tokens, logp, entropy, peak, log_sum, top_ids, top_logp, (int)V, top, (int)slice, 1.0f / temperature};

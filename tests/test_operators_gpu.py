@@ -690,3 +690,14 @@ def test_logprobs_alternatives_that_share_a_lane(V, dtype):
 def test_join_backward_at_the_bounds_of_its_splits(M, K, stream, post, gate, act):
     """Row lengths on both sides of the thread counts, and every way to add the partial column sums."""
     test_join_backward_parity(M, K, stream, post, gate, act)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("M", [310, 600, 800, 1100, 1300])
+def test_logprobs_every_number_of_rows_per_multiprocessor(M, dtype):
+    """Numbers of rows at which the threads of a row change, rows long enough to have use for all of them."""
+    g = gen(M)
+    x = randn(M, 6007, dtype, g, 2.5, pad=8)
+    tok = torch.randint(0, 6007, (M,), generator=g, device="cuda")
+    for top in (0, 32):
+        check_logprobs(x, tok, 1.0, top)
