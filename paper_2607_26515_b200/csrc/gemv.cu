@@ -33,7 +33,8 @@ namespace {
 constexpr int kWarps = 12, kThreads = kWarps * 32;
 constexpr int kUnitK = 128, kTileN = 16;
 // STEP: units of a tile per step (512 or 256 k), which has one wait and one set of copies: four, or two where the staged
-// activations leave no room for more.
+// activations leave no room for more or a warp's run is too short for them (plan_gemv; one token 2048 -> 2048: 4.0 against 4.1 us,
+// 3584 -> 37888: 26.5 us with two for eight tokens, 25.0 with four).
 constexpr int kRing = 2;        // steps in flight per warp: 96 or 48 KB per SM (three of two units: no faster, and it costs the tiles room)
 // words per row of a step's scales: HiF4 two per unit and one against bank conflicts, MXFP4 one per unit and one because rows
 // start on any byte
