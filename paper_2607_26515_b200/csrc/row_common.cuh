@@ -120,6 +120,8 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 // Sums of NV (1 or 4) values over the block, the same bits in every thread; fixed order.  `buf` holds NV * 32 floats (16-byte
 // aligned) and must not be the buffer of the previous call (two alternate, which saves a barrier).  Four values share their
 // shuffles: after two exchanges a lane carries one of them (6 shuffles instead of 20).
+// It is a barrier of the block for shared memory too, which callers rely on: what a thread has read, written or waited for before
+// it is ordered before what the others do behind it.
 template <int NV>
 __device__ __forceinline__ void block_sum(float (&v)[NV], float* buf) {
     static_assert(NV == 1 || NV == 4, "");
@@ -138,6 +140,7 @@ __device__ __forceinline__ void block_sum(float (&v)[NV], float* buf) {
     x += __shfl_xor_sync(0xFFFFFFFFu, x, 2);
     x += __shfl_xor_sync(0xFFFFFFFFu, x, 1);
     if (nw == 1) {
+        __syncwarp();  // shuffles order no memory
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] = NV == 1 ? x : __shfl_sync(0xFFFFFFFFu, x, i * 8);
         return;

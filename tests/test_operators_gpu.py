@@ -701,3 +701,22 @@ def test_logprobs_every_number_of_rows_per_multiprocessor(M, dtype):
     tok = torch.randint(0, 6007, (M,), generator=g, device="cuda")
     for top in (0, 32):
         check_logprobs(x, tok, 1.0, top)
+
+
+@pytest.mark.parametrize("stream", [BF, F32])
+@pytest.mark.parametrize("K", [9, 64, 250, 256, 264])
+def test_join_backward_rows_do_not_depend_on_the_rows_before(K, stream):
+    """Rows of one or two warps, a dozen of them through the buffers of each block, chunks of which are copied by other lanes than
+    those that read them: each row has the bits that it has in a call in which it is a block's only row."""
+    m = rq()
+    M, part = 30000, 1000
+    v = join_case(M, K, stream, True, "full", K)
+    g = gen(K + 1)
+    dHo, dX = randn(M, K, stream, g, 0.5), randn(M, K, BF, g, 0.5)
+    rest = (v["gamma_pre"], v["gamma_post"])
+    whole = m.block_join_backward(dHo, dX, v["H"], v["B"], *rest, v["gate"], "sigmoid", 0.5)
+    for r in range(0, M, part):
+        at = slice(r, r + part)
+        alone = m.block_join_backward(dHo[at], dX[at], v["H"][at], v["B"][at], *rest, v["gate"][at], "sigmoid", 0.5)
+        for name in ("dH", "dB", "dgate"):
+            assert torch.equal(whole[name][at], alone[name]), (name, r)
