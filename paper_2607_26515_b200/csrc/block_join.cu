@@ -41,13 +41,16 @@ struct JoinFwd {
     float alpha, eps;
 };
 
-// 1 / (1 + exp(-g)): two special-function operations, each within 2 ulp; exp overflowing to infinity gives 0.
-__device__ __forceinline__ float sigmoid_of(float g) {
-    float e, r;
+// e = exp(-g), s = sigmoid(g) = 1 / (1 + e): two special-function operations, each within 2 ulp; e overflowing to infinity gives 0.
+__device__ __forceinline__ float sigmoid_of(float g, float& e) {
+    float s;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-    return r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + e));
+    return s;
 }
+// Its derivative s (1 - s) as e s s: 1 - s has lost 1 % of itself at a gate of 12 and all of it at 17.  e is cut at the largest
+// number, where s is 0.
+__device__ __forceinline__ float sigmoid_slope(float s, float e) { return fminf(e, 3.4028234663852886e38f) * s * s; }
 
 // Eight columns as four packed pairs of fp32.
 typedef uint64_t Cols[4];
@@ -73,11 +76,11 @@ __device__ __forceinline__ void gate_cols(bool sigmoid, Cols& G, Cols& slope) {
     if (sigmoid) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float lo, hi;
+            float lo, hi, el, eh;
             unpair(G[i], lo, hi);
-            lo = sigmoid_of(lo), hi = sigmoid_of(hi);
+            lo = sigmoid_of(lo, el), hi = sigmoid_of(hi, eh);
             G[i] = pair(lo, hi);
-            slope[i] = pair(lo * (1.0f - lo), hi * (1.0f - hi));
+            slope[i] = pair(sigmoid_slope(lo, el), sigmoid_slope(hi, eh));
         }
     } else {
 #pragma unroll
@@ -145,8 +148,9 @@ __global__ void __launch_bounds__(kMaxThreadsFwd, VPT == 1 ? 2 : 1) join_fwd_ker
             float g[8];
             rg[j].get(g);
             if (a.sigmoid) {
+                float e;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = sigmoid_of(g[i]);
+                for (int i = 0; i < 8; ++i) g[i] = sigmoid_of(g[i], e);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) p[i] = mul2(p[i], pair(g[2 * i], g[2 * i + 1]));

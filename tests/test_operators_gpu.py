@@ -720,3 +720,30 @@ def test_join_backward_rows_do_not_depend_on_the_rows_before(K, stream):
         alone = m.block_join_backward(dHo[at], dX[at], v["H"][at], v["B"][at], *rest, v["gate"][at], "sigmoid", 0.5)
         for name in ("dH", "dB", "dgate"):
             assert torch.equal(whole[name][at], alone[name]), (name, r)
+
+
+@pytest.mark.parametrize("M", [1, 5, 400])
+@pytest.mark.parametrize("gate", ["channel", "full"])
+@pytest.mark.parametrize("stream, post", [(BF, True), (F32, False)])
+def test_join_gradient_of_open_and_closed_gates(stream, post, gate, M):
+    """Sigmoid gates from -20 to 20: the slope s (1 - s) keeps its digits on both sides.  Formed from e = exp(-g) it is off by
+    the argument's rounding, 2 |g| u, and a dozen roundings: 52 u of itself at 20, which the 2^-16 = 256 u of every term covers.
+    (In 64 bits 1 - s at 20 is off by 2^-54 / 2^-29, half of u.)"""
+    K = 481
+    v = join_case(M, K, stream, post, gate, M + 7)
+    v["gate"].copy_(torch.linspace(-20, 20, K, device="cuda").expand(v["gate"].shape))
+    g = gen(M + 8)
+    dHo, dX = randn(M, K, stream, g, 0.5), randn(M, K, BF, g, 0.5)
+    back = lambda: rq().block_join_backward(dHo, dX, v["H"], v["B"], v["gamma_pre"], v["gamma_post"], v["gate"], "sigmoid", 0.5, 1e-5)
+    got = back()
+    args = wide([dHo, dX, v["H"], v["B"], v["gamma_pre"], v["gamma_post"], v["gate"]]) + ["sigmoid", 0.5, 1e-5]
+    want, size = join_gradients(*args), join_gradient_sizes(*args)
+    for name in want:
+        chain = U * (M / 148 + 300) if want[name].dim() == 1 else 0.0
+        close(got[name], want[name], (2.0 ** -16 + chain) * size[name] + HALF[got[name].dtype] * want[name].abs(), name)
+    # gates so far out that the slope is 0 in 32 bits, and infinite ones: no gradient, and none of 0 * inf
+    far = torch.tensor([-float("inf"), -3e38, -200.0, 200.0, 3e38, float("inf")], device="cuda", dtype=BF)
+    v["gate"][..., :6] = far
+    got = back()
+    assert all(t.isfinite().all() for t in got.values())
+    assert not got["dgate"][..., :6].any()
