@@ -707,6 +707,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, temperature: floa
     if stream is not None or _current_device() != index:
         return _elsewhere(index, stream, lambda: token_logprobs(logits, tokens, temperature, top))
     tok = _vector(tokens, "tokens", M, torch.int64, index)
+    top = min(max(top, -1), MAX_TOP + 1)  # a C int would keep the low bits of a larger number; the library refuses both ends
     values = _new(4, M, _F32, index)
     logp, entropy, peak, log_sum = values.unbind()
     out = {"logp": logp, "entropy": entropy, "peak": peak, "log_sum": log_sum}

@@ -747,3 +747,13 @@ def test_join_gradient_of_open_and_closed_gates(stream, post, gate, M):
     got = back()
     assert all(t.isfinite().all() for t in got.values())
     assert not got["dgate"][..., :6].any()
+
+
+@pytest.mark.parametrize("top", [33, 10 ** 9, 2 ** 31, 2 ** 32, 2 ** 32 + 5, -1, -2 ** 32])
+def test_logprobs_refuses_numbers_of_alternatives_out_of_range(top):
+    """Those beyond 32 bits too: no call with what their low bits say, and no memory is asked for."""
+    m = rq()
+    x, tok = randn(3, 64, BF, gen(34)), torch.zeros(3, dtype=torch.int64, device="cuda")
+    with pytest.raises(m.ResqError) as e:
+        m.token_logprobs(x, tok, top=top)
+    assert e.value.status == 2
