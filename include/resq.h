@@ -377,6 +377,7 @@ RESQ_API int mxfp4_w4a16_gemv(const void* X_bf16, int64_t M, int64_t K, int64_t 
  *   written.  H_out may be H itself; other overlaps are not allowed.  Sums, norms and H' before its one rounding are
  *   fp32; X is formed from the unrounded H'.  alpha and eps finite, eps >= 0 (with eps = 0 a row of zeros has the NaN of
  *   0 / 0; NaN and infinities stay in their row, and in the column sums over the rows).
+ *   The squares are fp32 too: a row whose sum of them passes its range (values of about 1e19) has a row factor of 0.
  * Backward: the gradients of these formulas at H_out and B as given (the row factors are formed again from them), with
  *   dH_out (type of the stream) and / or dX bf16 the gradients of the two outputs (either may be NULL = zero):
  *     dH [M, K] (type of the stream; may be dH_out itself), dB bf16 [M, K], dgate (bf16 [M, K] with pitch lddg; for a

@@ -757,3 +757,60 @@ def test_logprobs_refuses_numbers_of_alternatives_out_of_range(top):
     with pytest.raises(m.ResqError) as e:
         m.token_logprobs(x, tok, top=top)
     assert e.value.status == 2
+
+
+@pytest.mark.parametrize("stream", [BF, F32])
+def test_join_rows_of_zeros_without_eps(stream):
+    """eps = 0: a row of zeros is 0 / 0, NaN in its own rows and in the column sums, and no other row knows of it."""
+    m = rq()
+    v = join_case(4, 264, stream, True, "full", 11)
+    clean = m.block_join(**v, act="sigmoid", eps=0.0)
+    v["H"][1], v["B"][1] = 0, 0
+    H, X = m.block_join(**v, act="sigmoid", eps=0.0)
+    others = [0, 2, 3]
+    assert H[1].isnan().all() and X[1].isnan().all()
+    assert torch.equal(H[others], clean[0][others]) and torch.equal(X[others], clean[1][others])
+    H[1] = 0
+    g = m.block_join_backward(clean[0], X, H, v["B"], v["gamma_pre"], v["gamma_post"], v["gate"], "sigmoid", 1.0, 0.0)
+    alone = m.block_join_backward(clean[0][2:], X[2:], H[2:], v["B"][2:], v["gamma_pre"], v["gamma_post"], v["gate"][2:], "sigmoid", 1.0, 0.0)
+    for name in ("dH", "dB", "dgate"):
+        assert g[name][1].isnan().all() and torch.equal(g[name][2:], alone[name])
+    assert g["dgamma_pre"].isnan().all() and g["dgamma_post"].isnan().all()
+
+
+@pytest.mark.parametrize("scale_h, scale_b", [(1e15, 1e12), (1e12, 1e15), (1e-12, 1e-12), (1e15, 1e-12)])
+@pytest.mark.parametrize("stream, post, gate, act", FORMS)
+def test_join_rows_of_large_and_small_values(stream, post, gate, act, scale_h, scale_b):
+    """Squares from 1e-24 to 1e30 a term, next to rows of ordinary values (eps is small against none of the norms)."""
+    M, K, alpha, eps = 6, 264, 0.7, 1e-30
+    v = join_case(M, K, stream, post, gate, 12)
+    v["H"][::2] *= scale_h
+    v["B"][::2] *= scale_b
+    H, X = rq().block_join(**v, act=act, alpha=alpha, eps=eps)
+    w = {n: None if t is None else t.double() for n, t in v.items()}
+    h, x = join(w["H"], w["B"], w["gamma_pre"], w["gamma_post"], w["gate"], act, alpha, eps)
+    size = w["H"].abs() + (h - w["H"]).abs()
+    close(H, h, 2.0 ** -16 * size + HALF[stream] * h.abs(), "H")
+    r = 1 / torch.sqrt(h.square().mean(-1, keepdim=True) + eps)
+    close(X, x, 2.0 ** -16 * (size * r * w["gamma_pre"].abs() + x.abs()) + HALF[BF] * x.abs(), "X")
+    g = gen(13)
+    dHo, dX = randn(M, K, stream, g, 0.5), randn(M, K, BF, g, 0.5)
+    dHo[::2] /= scale_h  # of the size of the norm's own gradient
+    got = rq().block_join_backward(dHo, dX, H, v["B"], v["gamma_pre"], v["gamma_post"], v["gate"], act, alpha, eps)
+    args = wide([dHo, dX, H, v["B"], v["gamma_pre"], v["gamma_post"], v["gate"]]) + [act, alpha, eps]
+    want, size = join_gradients(*args), join_gradient_sizes(*args)
+    for name in want:
+        half = HALF[got[name].dtype] * want[name].abs()
+        chain = U * (M / 148 + 300) if want[name].dim() == 1 else 0.0
+        close(got[name], want[name], (2.0 ** -16 + chain) * size[name] + half, name)
+
+
+def test_join_squares_beyond_the_range():
+    """A row whose sum of squares is infinite has r = 0, as the header says: X is 0, and the other rows are as they were."""
+    m = rq()
+    v = join_case(3, 264, F32, False, "none", 14)
+    want = m.block_join(**v)
+    v["H"][1] = 3e19
+    H, X = m.block_join(**v)
+    assert (H[1] == 3e19).all() and not X[1].any()
+    assert torch.equal(H[::2], want[0][::2]) and torch.equal(X[::2], want[1][::2])
