@@ -247,7 +247,8 @@ RESQ_API int mxfp4_wgrad_linear(const void* dY_bf16, const void* X_bf16, int64_t
 /* Weight-only ablation of Table 1 ("W4A16"): Y = X deq(Q(W))^T, the bf16 activations are used as they are
  * (no activation quantizer, no residual term); weights as produced by *_pack_weight.  Same argument rules,
  * output types and error behaviour as *_resq_linear; workspace of resq_w4a16_workspace_bytes(M, N, K) bytes
- * (status word, arrival counters, fp32 partial tiles of a K split), owned by the caller. */
+ * (status word, arrival counters, fp32 partial tiles of a K split), owned by the caller.  (Up to RESQ_GEMV_MAX_TOKENS token
+ * rows: *_w4a16_gemv below is the same product in a third to a half of the time.) */
 RESQ_API size_t resq_w4a16_workspace_bytes(int64_t M, int64_t N, int64_t K);
 RESQ_API int hif4_w4a16_linear(const void* X_bf16, int64_t M, int64_t K, int64_t ldx,
                       const void* w_codes, const void* w_meta, int64_t N,
@@ -439,7 +440,7 @@ RESQ_API const char* resq_last_error(void);
  * stream (this perturbs timing slightly; leave it off when measuring whole-call time).
  * resq_profile_read: synchronizes on the recorded events, adds the device time (ms) and the number of
  * launches per kernel kind into the two arrays of 4 entries (0 = quantizer/residual/mask pass,
- * 1 = top-k select and mask apply, 2 = GEMM, 3 = split-K reduce; either array may be NULL) and
+ * 1 = top-k select and mask apply, 2 = GEMM and *_w4a16_gemv, 3 = split-K reduce; either array may be NULL) and
  * clears the records.  (resq_block_join and resq_token_logprobs and their backward calls are counted as launches but
  * have no kind here.)
  * resq_debug_expire_next_wait(1): test hook for the RESQ_ERR_TIMEOUT path.  The next decode-sized GEMM launch of

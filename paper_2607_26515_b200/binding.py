@@ -405,7 +405,9 @@ def wgrad_linear(dY: torch.Tensor, X: torch.Tensor, fmt: str = "hif4", out_dtype
 def w4a16_linear(X: torch.Tensor, w_codes: torch.Tensor, w_side: torch.Tensor, fmt: str = "hif4",
                  out_dtype: torch.dtype = torch.bfloat16, Y: Optional[torch.Tensor] = None,
                  workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """*_w4a16_linear: Y = X deq(Q(W))^T, activations kept in bf16 (Table 1, W4A16)."""
+    """*_w4a16_linear: Y = X deq(Q(W))^T, activations kept in bf16 (Table 1, W4A16).  Its tile computes 128 rows whatever M is:
+    up to GEMV_MAX_TOKENS rows w4a16_gemv takes a third to a half of its time (3584 -> 37888: 8 rows 25 against 70 us,
+    16 rows 33)."""
     _require_bf16_matrix(X, "X")
     M, K = X.shape
     N = w_codes.shape[0]

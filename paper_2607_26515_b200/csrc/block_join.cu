@@ -9,10 +9,10 @@
 // their sums over the rows in registers; at the end each CTA writes them as one fp32 partial row and a second kernel adds the P
 // partial rows in a fixed order (bit-identical run to run).  The rows to come are in flight in a ring of asynchronous copies:
 // two row sums with a block barrier each leave a row's loads no time of their own otherwise (8192 x 2048, fp32 stream, channel
-// gate: 122 us without the ring, 61 with it).
+// gate: 122 us without the ring, 59 with it).
 //
 // Measured: forward 16384 x 3584, bf16, norm and gate per token, 105 us = 5.6 TB/s (0.86 of the copy rate); backward of the
-// same 215 us = 4.4 TB/s (0.67) and 8192 x 2048, fp32, channel gate, 61 us = 5.0 TB/s (0.76).  The forward pass is bound by HBM.  The
+// same 214 us = 4.4 TB/s (0.67) and 8192 x 2048, fp32, channel gate, 59 us = 5.1 TB/s (0.78).  The forward pass is bound by HBM.  The
 // backward pass keeps a row and its column sums in registers, which leaves 16 warps per SM: between a row's barrier and its
 // loads' arrival in registers there are too few of them to fill the issue slots (about half are empty).
 #include "row_common.cuh"
@@ -24,7 +24,7 @@ namespace {
 
 constexpr int kMaxThreadsFwd = 1024;  // one row: up to 4 vectors of 8 per thread
 // Backward, threads per SM: 512 of 128 registers, or 640 of 96 for rows that need them (they spill nothing either, but short rows
-// measured slower: 8192 x 2048, fp32 stream, 61 against 57 us; 16384 x 3584, gated, 221 against 212).
+// measured slower: 8192 x 2048, fp32 stream, channel gate, 63 against 59 us; 16384 x 3584, gated, 221 against 214).
 constexpr int kFewThreads = 512, kManyThreads = 640;
 static_assert(kMaxThreadsFwd * 8 * 4 >= RESQ_JOIN_MAX_K && kManyThreads * 8 * 8 >= RESQ_JOIN_MAX_K, "row length");
 

@@ -14,14 +14,14 @@
 // with a contiguous slice.  The lanes of a warp share the running maximum, so rescaling is rare; per element that leaves a
 // subtraction, a multiplication, the exponential and two additions.  It is bound by HBM, with the exponentials (16 per clock and
 // SM) at 0.7 of their rate beside it.  Measured: 4096 x 131072, bf16, 184 us = 5.8 TB/s (0.89 of the copy rate); 512 x 131072,
-// fp32, 42 us (0.96); one row of 131072 5.2 us, with 20 alternatives 11.2 (latency: launch, loads, three exchanges in the cluster).
+// fp32, 42 us (0.97); one row of 131072 5.1 us, with 20 alternatives 11.4 (latency: launch, loads, three exchanges in the cluster).
 // Backward: 2048 x 131072, bf16, read and written, 169 us = 6.35 TB/s (0.97).
 //
 // Top alternatives: every lane remembers its largest logit, the group of 16 it was in, and the largest of its other groups.  The
 // k-th largest of the lanes' values (taken over sets of lanes) is a lower bound of the k-th largest logit, and only the lanes
 // that reach it can hold anything above it: that group is read again, or all of the lane's groups if a second one reaches the
 // bound too, and the few dozen logits that pass are ranked.  Bounds and ranks are on (value, lower index) keys, so ties need no
-// care.  (4096 x 131072, top 32: 244 us; 310 when all groups of such lanes were read again, since their sectors
+// care.  (4096 x 131072, top 32: 245 us; 310 when all groups of such lanes were read again, since their sectors
 // come from DRAM.)
 #include "row_common.cuh"
 
