@@ -18,7 +18,7 @@ inline bool rows_aligned(const void* p, int64_t ld, int64_t cols, int dtype) {
 
 // Clusters of cs CTAs that are resident at once with one CTA per SM, as the occupancy query answers on a B200: larger clusters
 // leave SMs of a GPC unused.  Plans only choose splits by it, and the workspace query has to answer without a device: a device with
-// other counts gets the same results at another speed.
+// other counts gets right results at another speed.
 inline int resident_clusters(int cs) { return cs == 1 ? 148 : cs == 2 ? 74 : cs == 4 ? 33 : 15; }
 
 #ifdef __CUDACC__
