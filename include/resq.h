@@ -428,6 +428,83 @@ RESQ_API int resq_token_logprobs_backward(const void* logits, int dtype, int64_t
                                  float temperature, const float* logp, const float* peak, const float* log_sum,
                                  const float* entropy, const float* dlogp, const float* dentropy, void* dlogits, int64_t ldd, void* stream);
 
+/* ---- between the qkv and the output projection of a rollout: rotation, paged cache, attention (no counterpart in the paper) ----
+ * Keys and values live in pages.  Both structs are HOST structs read during the call; their pointers are device pointers.
+ *   cache: k, v bf16, element (page, row, head, d) of each at page * *_page + row * *_row + head * *_head + d; strides in
+ *     elements, multiples of 8 (0 allowed), bases 16-byte aligned; head_dim 64 or 128; page_size a multiple of 8.
+ *   sequences: token rows q_start[b] .. q_start[b + 1] - 1 of the call are the new tokens of sequence b; kv_len[b] counts its
+ *     keys, the new tokens' among them, so its i-th of n new tokens is key (and stands at position) kv_len[b] - n + i;
+ *     page_table[b * ld_table + j] is the page of keys j * page_size ...
+ *   The arrays are read on the device, so a captured call follows what they hold when it runs.  Whatever they hold, nothing is
+ *   read or written out of range: starts are cut to 0 .. T (a sequence whose end lies before its start has no new tokens),
+ *   lengths to 0 .. max_pages * page_size, and a page outside 0 .. pages - 1 is none: nothing is stored there, and its keys and
+ *   values are read as zeros.  Rows behind the last sequence (and before the first) are neither read nor written.
+ *   At most RESQ_MAX_SEQUENCES sequences, RESQ_MAX_GROUP_HEADS query heads per kv head, fewer than 2^31 keys per sequence. */
+#define RESQ_MAX_SEQUENCES 4096
+#define RESQ_MAX_GROUP_HEADS 128
+typedef struct resq_paged_cache {
+    void *k, *v;
+    int64_t pages, page_size, kv_heads, head_dim;
+    int64_t k_page, k_row, k_head, v_page, v_row, v_head;
+} resq_paged_cache;
+typedef struct resq_sequences {
+    const int32_t *q_start, *kv_len, *page_table; /* [count + 1], [count], [count, ld_table] */
+    int64_t count, max_pages, ld_table;
+} resq_sequences;
+
+/* Rotation and append: QKV [T, (Hq + 2 Hkv) D] bf16 or fp32 (`dtype`, a resq_out; what the qkv projection writes: Hq query heads,
+ * Hkv key heads, Hkv value heads), bias_bf16 [(Hq + 2 Hkv) D] or NULL.
+ *     x = QKV + bias;  query and key heads: pair (a, b) of frequency j -> (a cos - b sin, b cos + a sin) of the angle
+ *     position * inv_freq[j];  Q gets the queries, the cache the keys and values of the new tokens
+ *   inv_freq fp64 [rot / 2] (device): any scheme of frequencies; rot <= D, a multiple of 16 (0: no rotation); elements from rot on
+ *   are copied.  Frequency j belongs to elements j and j + rot / 2 of a head, or (pairs != 0) to 2 j and 2 j + 1.  positions int32
+ *   [T] or NULL: where the tokens stand for the rotation, if not at their keys' places (the slots are the keys' all the same).
+ *   Angles are exact to 2^-32 of a turn for any int32 position; everything is fp32 and rounded once.  Q may be the query
+ *   columns of a bf16 QKV itself; other overlaps are not allowed.  A token whose place is negative (kv_len below the number of new
+ *   tokens) or whose page is none is rotated, not stored.  Two sequences must not own the same slot.  No workspace. */
+RESQ_API int resq_rope_append(const void* QKV, int dtype, int64_t T, int64_t ldqkv, int64_t Hq, int64_t Hkv, int64_t D, const void* bias_bf16,
+                     const double* inv_freq, int64_t rot, int pairs, const int32_t* positions, const resq_paged_cache* cache,
+                     const resq_sequences* seqs, void* Q_bf16, int64_t ldq, void* stream);
+
+/* Attention of the new tokens over the cache: query head h of Q [T, Hq D] reads kv head h / (Hq / Hkv); the token at key place i sees
+ * keys 0 .. i (its own and the earlier new ones must be in the cache: resq_rope_append first).
+ *     O_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j - lse_i),  lse_i = log sum_j exp(scale q_i.k_j)
+ *   O bf16 [T, Hq D]; lse fp32 [T, Hq] contiguous, or NULL; scale positive.  A token that sees no key has O = 0 and lse = -inf.
+ *   Scores, sums and O are fp32, the weights are rounded to bf16 for their product with the values.  What lies in masked places
+ *   (keys behind a token, rows of a page behind the last key) has no influence, infinities and NaN included; a score of NaN or +inf
+ *   makes its token's row NaN.  One call serves decoded tokens, drafts and prompts alike, mixed as they come.
+ *   max_new: the largest number of new tokens per sequence as far as the host knows (0: unknown).  It chooses the kernel and the
+ *   size of the workspace, never the result's meaning.  Order of summation is fixed for given lengths (bit-identical run to run).
+ *   O must not overlap Q.  workspace of resq_paged_attention_workspace_bytes() bytes for the same numbers, 256-byte aligned, owned by
+ *   the call until it has run. */
+RESQ_API size_t resq_paged_attention_workspace_bytes(int64_t T, int64_t count, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_new);
+RESQ_API int resq_paged_attention(const void* Q_bf16, int64_t T, int64_t ldq, int64_t Hq, int64_t Hkv, int64_t D, const resq_paged_cache* cache,
+                         const resq_sequences* seqs, int64_t max_new, float scale, void* O_bf16, int64_t ldo, float* lse,
+                         void* workspace, size_t ws_bytes, void* stream);
+
+/* ---- verification of drafted tokens (no counterpart in the paper) ------------------------------------------------------
+ * Rows row_start[b] .. row_start[b + 1] - 1 of the logits [R, V] (bf16 or fp32, layout as in resq_token_logprobs) are the target's
+ * for the positions of sequence b's drafts and one more behind them; drafts int64 [R]: the token proposed at each row's position
+ * (ignored in a sequence's last row; outside 0 .. V - 1: none, the proposals end there).
+ *     p = softmax(logits / temperature),  q = exp((draft_logits - draft_peak) / temperature - draft_log_sum)
+ *     row r's draft x is kept if all before it were and u[r] q(x) < p(x)
+ *     the first row that is not kept gets  argmax_j w_j / noise[b][j],  w = max(p - q, 0), or p where nothing was proposed (or where
+ *     nothing is left of p - q); equal ones: the lowest j
+ *   u fp32 [R] from [0, 1); noise fp32 [count, V] (pitch lde), exponential variates above 0: token j is then drawn with probability
+ *   w_j / sum w, and kept and drawn tokens together follow p.  draft_logits (type of the logits, pitch ldd) with draft_peak and
+ *   draft_log_sum fp32 [R] of the same temperature, as resq_token_logprobs gives them; draft_logits NULL: the drafts were proposed
+ *   with certainty (q(x) = 1).  temperature 0: no random numbers (u, noise and the draft's are not read), a draft is kept if it is
+ *   the largest logit (equal ones: the lowest), which is also what replaces it; log-probabilities are then those of temperature 1.
+ *   accepted int32 [count]: drafts kept; tokens int64 [R]: the kept drafts, the token behind them, then -1; logp fp32 [R]: log p of
+ *   each of these tokens (0 beside -1).  A row of nothing but -inf, or with NaN or +inf, keeps nothing and yields -1.  A sequence
+ *   without rows has accepted 0; rows of no sequence are not written.  Decisions within 2^-14 of a border are made in 64 bits
+ *   (from the row's fp32 peak and log_sum).  workspace of resq_verify_drafts_workspace_bytes(R) bytes, 256-byte aligned. */
+RESQ_API size_t resq_verify_drafts_workspace_bytes(int64_t R);
+RESQ_API int resq_verify_drafts(const void* logits, int dtype, int64_t R, int64_t V, int64_t ld, const int32_t* row_start, int64_t count,
+                       const int64_t* drafts, const float* u, const float* noise, int64_t lde, const void* draft_logits, int64_t ldd,
+                       const float* draft_peak, const float* draft_log_sum, float temperature, int32_t* accepted, int64_t* tokens,
+                       float* logp, void* workspace, size_t ws_bytes, void* stream);
+
 /* ---- status --------------------------------------------------------------------------------------
  * resq_check synchronizes `stream` and returns the device status word kept at the start of
  * `workspace` (RESQ_OK, or RESQ_ERR_TIMEOUT if a bounded wait expired in the last call that used it). */
@@ -441,8 +518,8 @@ RESQ_API const char* resq_last_error(void);
  * resq_profile_read: synchronizes on the recorded events, adds the device time (ms) and the number of
  * launches per kernel kind into the two arrays of 4 entries (0 = quantizer/residual/mask pass,
  * 1 = top-k select and mask apply, 2 = GEMM and *_w4a16_gemv, 3 = split-K reduce; either array may be NULL) and
- * clears the records.  (resq_block_join and resq_token_logprobs and their backward calls are counted as launches but
- * have no kind here.)
+ * clears the records.  (resq_block_join, resq_token_logprobs, resq_rope_append, resq_paged_attention and
+ * resq_verify_drafts are counted as launches but have no kind here.)
  * resq_debug_expire_next_wait(1): test hook for the RESQ_ERR_TIMEOUT path.  The next decode-sized GEMM launch of
  * the process (K-streamed schedule: M > 128 and few output tiles) waits at its end for one partial tile more than
  * its CTAs can deliver, with a poll limit of about a millisecond: the bounded wait runs out, the kernel records

@@ -7,4 +7,6 @@ from .binding import (  # noqa: F401
     debug_expire_next_wait, pack_weight_transposed, dgrad_linear, wgrad_linear, resq_linear_group, resq_group_workspace_bytes, MAX_GROUP,
     w4a16_gemv, block_join, block_join_backward, block_join_backward_workspace_bytes, token_logprobs, token_logprobs_backward,
     GEMV_MAX_TOKENS, JOIN_MAX_K, MAX_TOP,
+    rope_append, paged_attention, paged_attention_workspace_bytes, verify_drafts, verify_drafts_workspace_bytes,
+    MAX_SEQUENCES, MAX_GROUP_HEADS,
 )

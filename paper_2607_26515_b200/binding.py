@@ -85,6 +85,12 @@ SYMBOLS = {
                                        _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
     "resq_token_logprobs": (_ci, [_vp, _ci, _i64, _i64, _i64, _vp, _cf, _ci, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "resq_token_logprobs_backward": (_ci, [_vp, _ci, _i64, _i64, _i64, _vp, _cf, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "resq_rope_append": (_ci, [_vp, _ci, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _i64, _ci, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "resq_paged_attention_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i64, _i64]),
+    "resq_paged_attention": (_ci, [_vp, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _i64, _cf, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "resq_verify_drafts_workspace_bytes": (_sz, [_i64]),
+    "resq_verify_drafts": (_ci, [_vp, _ci, _i64, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _cf, _vp, _vp, _vp, _vp,
+                                 _sz, _vp]),
     "resq_check": (_ci, [_vp, _vp]),
     "resq_last_error": (ctypes.c_char_p, []),
     "resq_kernel_launches": (_i64, []),
@@ -744,6 +750,157 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, logp: to
     _check(lib().resq_token_logprobs_backward(logits.data_ptr(), code, M, V, ld, values[0], temperature, *values[1:], dlogits.data_ptr(), ldd,
                                               _raw_stream(index)))
     return dlogits
+
+
+# ------------------------------------------------------------------ paged cache, attention, verification of drafts
+#
+# As above: on the device of the first tensor, on `stream` or that device's current one.  A cache is a pair of tensors [pages,
+# page_size, kv_heads, head_dim] with any strides that keep 16-byte rows (a transposed view of [pages, kv_heads, page_size,
+# head_dim], or one half of a joint buffer).
+
+MAX_SEQUENCES = 4096
+MAX_GROUP_HEADS = 128
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("pages", _i64), ("page_size", _i64), ("kv_heads", _i64), ("head_dim", _i64), ("k_page", _i64),
+                ("k_row", _i64), ("k_head", _i64), ("v_page", _i64), ("v_row", _i64), ("v_head", _i64)]
+
+
+class _Sequences(ctypes.Structure):
+    _fields_ = [("q_start", _vp), ("kv_len", _vp), ("page_table", _vp), ("count", _i64), ("max_pages", _i64), ("ld_table", _i64)]
+
+
+def _paged(k_cache: torch.Tensor, v_cache: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, index: int):
+    """The two structs of a paged call."""
+    shape = k_cache.shape
+    if (k_cache.dtype is not _BF16 or v_cache.dtype is not _BF16 or len(shape) != 4 or v_cache.shape != shape or k_cache.get_device() != index
+            or v_cache.get_device() != index):
+        raise ValueError(f"k_cache and v_cache must be bf16 tensors of one shape [pages, page_size, kv_heads, head_dim] on cuda:{index}")
+    kp, kr, kh, ki = k_cache.stride()
+    vp, vr, vh, vi = v_cache.stride()
+    _require(ki == 1 and vi == 1, "k_cache and v_cache must have unit inner stride")
+    count = kv_len.shape[0] if kv_len.dim() == 1 else -1
+    at_start, at_len = _vector(q_start, "q_start", count + 1, torch.int32, index), _vector(kv_len, "kv_len", count, torch.int32, index)
+    if (page_table.dtype is not torch.int32 or page_table.dim() != 2 or page_table.shape[0] != count or page_table.get_device() != index
+            or (page_table.shape[1] > 1 and page_table.stride(1) != 1)):
+        raise ValueError(f"page_table must be an int32 tensor [{count}, pages per sequence] on cuda:{index} with unit inner stride")
+    per_seq = page_table.shape[1]
+    return (_PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), *shape, kp, kr, kh, vp, vr, vh),
+            _Sequences(at_start, at_len, page_table.data_ptr(), count, per_seq, page_table.stride(0) if count > 1 else per_seq))
+
+
+def rope_append(qkv: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+                page_table: torch.Tensor, inv_freq: torch.Tensor, bias: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                pairs: bool = False, q: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """resq_rope_append: rows of qkv [T, (Hq + 2 Hkv) D] (bf16 or fp32) plus bias -> the rotated queries q [T, Hq D] bf16 (returned);
+    rotated keys and the values go to their slots of the cache.
+
+    q_start int32 [B + 1], kv_len int32 [B] (keys of each sequence, the new ones among them), page_table int32 [B, pages per
+    sequence].  inv_freq fp64 [rot / 2]; pairs: neighbouring elements turn into each other, not those rot / 2 apart.  q may be
+    qkv[:, :Hq * D] of a bf16 qkv."""
+    T, W, ld, code, index = _first(qkv, "qkv")
+    if stream is not None or _current_device() != index:
+        return _elsewhere(index, stream, lambda: rope_append(qkv, k_cache, v_cache, q_start, kv_len, page_table, inv_freq, bias, positions, pairs, q))
+    cache, seqs = _paged(k_cache, v_cache, q_start, kv_len, page_table, index)
+    Hkv, D = cache.kv_heads, cache.head_dim
+    _require(D > 0 and W % D == 0 and W > 2 * Hkv * D, f"qkv must have (Hq + 2 * {Hkv}) heads of {D} columns")
+    Hq = W // D - 2 * Hkv
+    half = inv_freq.shape[0] if inv_freq.dim() == 1 else -1
+    freq = _vector(inv_freq, "inv_freq", half, torch.float64, index)
+    at_bias = None if bias is None else _vector(bias, "bias", W, _BF16, index)
+    at_pos = None if positions is None else _vector(positions, "positions", T, torch.int32, index)
+    if q is None:
+        q, ldq = _new(T, Hq * D, _BF16, index), Hq * D
+    else:
+        ldq = _rows(q, "q", T, Hq * D, _BF16, index)
+    _check(lib().resq_rope_append(qkv.data_ptr(), code, T, ld, Hq, Hkv, D, at_bias, freq, 2 * half, 1 if pairs else 0, at_pos,
+                                  ctypes.byref(cache), ctypes.byref(seqs), q.data_ptr(), ldq, _raw_stream(index)))
+    return q
+
+
+@functools.lru_cache(maxsize=1024)
+def paged_attention_workspace_bytes(T: int, count: int, Hq: int, Hkv: int, D: int, max_new: int = 0) -> int:
+    return int(lib().resq_paged_attention_workspace_bytes(T, count, Hq, Hkv, D, max_new))
+
+
+def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+                    page_table: torch.Tensor, scale: Optional[float] = None, max_new: Optional[int] = None, lse: bool = False,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """resq_paged_attention: attention of the new tokens' queries q [T, Hq D] over the cache -> out [T, Hq D] bf16, or (out,
+    lse [T, Hq] fp32).
+
+    scale: 1 / sqrt(head_dim) unless given.  max_new: the largest number of new tokens per sequence if the host knows it; it
+    chooses the kernel."""
+    T, W, ldq, code, index = _first(q, "q")
+    if stream is not None or _current_device() != index:
+        return _elsewhere(index, stream, lambda: paged_attention(q, k_cache, v_cache, q_start, kv_len, page_table, scale, max_new, lse, out,
+                                                                 workspace))
+    _require(code == OUT_BF16, "q must be bf16")
+    cache, seqs = _paged(k_cache, v_cache, q_start, kv_len, page_table, index)
+    Hkv, D = cache.kv_heads, cache.head_dim
+    _require(D > 0 and W % D == 0, f"q must have heads of {D} columns")
+    Hq = W // D
+    max_new = 0 if max_new is None else min(max(int(max_new), 0), T)
+    if out is None:
+        out, ldo = _new(T, W, _BF16, index), W
+    else:
+        ldo = _rows(out, "out", T, W, _BF16, index)
+    values = _new(T, Hq, _F32, index) if lse else None
+    if workspace is None:
+        workspace = _new(1, max(paged_attention_workspace_bytes(T, seqs.count, Hq, Hkv, D, max_new), 256), torch.uint8, index)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{index}")
+    _check(lib().resq_paged_attention(q.data_ptr(), T, ldq, Hq, Hkv, D, ctypes.byref(cache), ctypes.byref(seqs), max_new,
+                                      D ** -0.5 if scale is None else scale, out.data_ptr(), ldo, _ptr(values), workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(), _raw_stream(index)))
+    return (out, values) if lse else out
+
+
+@functools.lru_cache(maxsize=1024)
+def verify_drafts_workspace_bytes(R: int) -> int:
+    return int(lib().resq_verify_drafts_workspace_bytes(R))
+
+
+def verify_drafts(logits: torch.Tensor, row_start: torch.Tensor, drafts: torch.Tensor, u: Optional[torch.Tensor] = None,
+                  noise: Optional[torch.Tensor] = None, draft_logits: Optional[torch.Tensor] = None, draft_peak: Optional[torch.Tensor] = None,
+                  draft_log_sum: Optional[torch.Tensor] = None, temperature: float = 1.0, out: Optional[dict] = None,
+                  workspace: Optional[torch.Tensor] = None, stream=None):
+    """resq_verify_drafts -> dict(accepted int32 [B], tokens int64 [R], logp fp32 [R]): of each sequence's rows row_start[b] ..
+    row_start[b + 1] - 1 of the target's logits [R, V] the drafts that are kept, then the token that follows them, then -1.
+
+    drafts int64 [R] (a sequence's last row proposes none); u fp32 [R] uniform, noise fp32 [B, V] exponential.  draft_logits
+    with the draft's peak and log_sum (from token_logprobs at the same temperature), or None for drafts without probabilities.
+    temperature 0: the largest logits, without random numbers.  out: the dict of an earlier call of the same sizes, written anew."""
+    R, V, ld, code, index = _first(logits, "logits")
+    if stream is not None or _current_device() != index:
+        return _elsewhere(index, stream, lambda: verify_drafts(logits, row_start, drafts, u, noise, draft_logits, draft_peak, draft_log_sum,
+                                                               temperature, out, workspace))
+    count = row_start.shape[0] - 1 if row_start.dim() == 1 else -1
+    _require(count >= 1, "row_start must be a vector of at least 2 elements")
+    start, at_drafts = _vector(row_start, "row_start", count + 1, torch.int32, index), _vector(drafts, "drafts", R, torch.int64, index)
+    at_u = at_noise = at_draft = at_peak = at_sum = None
+    lde = ldd = 0
+    if temperature != 0:
+        _require(u is not None and noise is not None, "u and noise are needed to draw tokens")
+        at_u = _vector(u, "u", R, _F32, index)
+        lde, at_noise = _rows(noise, "noise", count, V, _F32, index), noise.data_ptr()
+        if draft_logits is not None:
+            _require(draft_peak is not None and draft_log_sum is not None, "draft_logits needs draft_peak and draft_log_sum")
+            ldd, at_draft = _rows(draft_logits, "draft_logits", R, V, logits.dtype, index), draft_logits.data_ptr()
+            at_peak, at_sum = _vector(draft_peak, "draft_peak", R, _F32, index), _vector(draft_log_sum, "draft_log_sum", R, _F32, index)
+    if out is None:
+        out = {"accepted": torch.empty(count, dtype=torch.int32, device=index), "tokens": torch.empty(R, dtype=torch.int64, device=index),
+               "logp": torch.empty(R, dtype=_F32, device=index)}
+    if workspace is None:
+        workspace = _new(1, verify_drafts_workspace_bytes(R), torch.uint8, index)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{index}")
+    _check(lib().resq_verify_drafts(
+        logits.data_ptr(), code, R, V, ld, start, count, at_drafts, at_u, at_noise, lde, at_draft, ldd, at_peak, at_sum, temperature,
+        _vector(out["accepted"], "accepted", count, torch.int32, index), _vector(out["tokens"], "tokens", R, torch.int64, index),
+        _vector(out["logp"], "logp", R, _F32, index), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(index)))
+    return out
 
 
 def check(workspace: torch.Tensor, stream=None) -> int:

@@ -1,0 +1,490 @@
+// resq_paged_attention: softmax attention of the new tokens of several sequences over their keys and values in a paged cache.
+//
+//   O_i = sum_{j <= pos_i} p_ij v_j,   p_ij = exp(scale q_i.k_j - lse_i),   lse_i = log sum_{j <= pos_i} exp(scale q_i.k_j)
+//
+// One pass over the keys with a running reference m (the largest score so far): p = 2^(s c - m) with c = scale log2(e), the sums
+// l and O multiplied by 2^(m_old - m_new) when m grows, O / l at the end.  P is rounded to bf16 for its product with V (off by at
+// most 2^-8 of each weight, as the output is by its own rounding); scores, sums and O are fp32.
+//
+// attn_rows_kernel (few query rows per kv head: decoded and drafted tokens) is bound by reading the cache once.  The queries of the
+// heads that share a kv head are the rows of one register-operand tensor instruction (m16n8k16), so each key is read once for all of
+// them.  The four warps of a CTA take 16 keys each of a tile of 64, with a ring of asynchronous copies of their own and their own
+// running sums, and meet only when the item is finished: nothing in the loop waits for another warp.
+#include "paged.cuh"
+
+#include <algorithm>
+#include <cmath>
+
+namespace resq {
+
+int check_paged(const char* what, const resq_paged_cache* c, const resq_sequences* s, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+    if (!c || !s || !c->k || !c->v || !s->q_start || !s->kv_len || !s->page_table) return fail(RESQ_ERR_NULL, what, "cache, sequences and their arrays must not be NULL");
+    if (T <= 0 || s->count <= 0 || s->count > kMaxSeqs) {
+        set_last_error("%s: %lld token rows, %lld sequences (1 or more rows, 1 .. %d sequences)", what, (long long)T, (long long)s->count, RESQ_MAX_SEQUENCES);
+        return RESQ_ERR_SHAPE;
+    }
+    if (c->kv_heads != Hkv || c->head_dim != D || Hkv <= 0 || Hq <= 0 || Hq % Hkv || Hq / Hkv > RESQ_MAX_GROUP_HEADS || (D != 64 && D != 128)) {
+        set_last_error("%s: %lld query heads, %lld kv heads of %lld (heads of 64 or 128, 1 .. %d query heads per kv head)", what, (long long)Hq,
+                       (long long)Hkv, (long long)D, RESQ_MAX_GROUP_HEADS);
+        return RESQ_ERR_SHAPE;
+    }
+    if (T > INT32_MAX / Hq || Hkv > INT32_MAX / D / 2) return fail(RESQ_ERR_SHAPE, what, "too many rows or heads for one call");
+    if (c->pages <= 0 || c->pages > INT32_MAX || c->page_size <= 0 || c->page_size % 8 || c->page_size > 65536 || s->max_pages <= 0 ||
+        s->max_pages > (INT32_MAX - 65536) / c->page_size) {
+        set_last_error("%s: %lld pages of %lld, %lld per sequence (pages of a multiple of 8 up to 65536 keys, fewer than 2^31 keys per sequence)", what,
+                       (long long)c->pages, (long long)c->page_size, (long long)s->max_pages);
+        return RESQ_ERR_SHAPE;
+    }
+    const int64_t strides[6] = {c->k_page, c->k_row, c->k_head, c->v_page, c->v_row, c->v_head};
+    for (int64_t v : strides)
+        if (v < 0 || v % 8 || v >= (int64_t)1 << 36) return fail(RESQ_ERR_ALIGN, what, "cache strides must be multiples of 8 elements, below 2^36");
+    if (!is_aligned(c->k, 16) || !is_aligned(c->v, 16)) return fail(RESQ_ERR_ALIGN, what, "the cache must be 16-byte aligned");
+    if (!is_aligned(s->q_start, 4) || !is_aligned(s->kv_len, 4) || !is_aligned(s->page_table, 4) || s->ld_table < s->max_pages)
+        return fail(RESQ_ERR_ALIGN, what, "q_start, kv_len and page_table must be 4-byte aligned, ld_table >= max_pages");
+    return RESQ_OK;
+}
+
+namespace {
+
+constexpr float kInf = __builtin_huge_valf();
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kWarps = 4, kKeys = 64, kWarpKeys = kKeys / kWarps;  // of attn_rows_kernel
+constexpr int kRowsCtasPerSm = 2;
+
+struct AttnArgs {
+    SeqArgs seq;
+    Deal deal;
+    const __nv_bfloat16 *q, *k, *v;
+    int64_t ldq, ldo, k_page, k_row, k_head, v_page, v_row, v_head;
+    __nv_bfloat16* out;
+    float* lse;       // [T, Hq] or null
+    int Hq;
+    float c;          // scale log2(e)
+    int min_chunk;
+    float* part_o;    // [2 ctas][rows][D], unnormalised
+    float2* part_ml;  // [2 ctas][rows]: reference, sum
+    JoinNote* notes;  // [ctas]
+    DeviceStatus* status;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 16 bytes to shared memory; zeros where !there (nothing is read then).
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+template <int D>
+constexpr int rows_stages() { return D == 128 ? 3 : 6; }  // 24 KB of ring per warp
+template <int D, int MT>
+constexpr int rows_smem() { return MT * 16 * D * 2 + kWarps * rows_stages<D>() * kWarpKeys * D * 4 + kWarps * MT * 16 * 8; }
+
+template <int D, int MT>
+__global__ void __launch_bounds__(kWarps * 32, kRowsCtasPerSm) attn_rows_kernel(const __grid_constant__ AttnArgs a) {
+    constexpr int R = MT * 16, CH = D / 8, S = rows_stages<D>(), kStage = kWarpKeys * D * 4, kHalf = kWarpKeys * D * 2;
+    constexpr int KS = D / 16, NT = D / 8;
+    static_assert(S * kStage >= R * D * 4, "the ring holds a warp's sums at the end");
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ int64_t sums[kWarps];
+    __shared__ DealStart found;
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, cta = blockIdx.x;
+    unsigned char* const ring = smem + R * D * 2 + w * S * kStage;
+    float2* const ml = reinterpret_cast<float2*>(smem + R * D * 2 + kWarps * S * kStage);  // [warp][R]
+    const uint32_t q_base = (uint32_t)__cvta_generic_to_shared(smem), ring_base = (uint32_t)__cvta_generic_to_shared(ring);
+    pdl_wait();
+    if (cta == 0 && tid == 0) *a.status = DeviceStatus{RESQ_OK, 0, 0, 0};
+    const Deal& d = a.deal;
+    const DealStart start = deal_start(a.seq, d, cta, gridDim.x, a.min_chunk, sums, &found);
+    DealWalk walk;
+    walk.init(a.seq, d, start);
+    bool first = true;
+    Segment seg;
+    while (walk.next(a.seq, d, seg)) {
+        const int f0 = seg.t * R, rows = min(R, seg.s.n * d.g - f0), k_end = deal_k_end(seg.s, d, seg.t), past = seg.s.kv - seg.s.n;
+        // ---- queries
+        __syncthreads();  // the sums of the segment before have been read
+        for (int i = tid; i < R * CH; i += kWarps * 32) {
+            const int r = i / CH, ch = i % CH;
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (r < rows) {
+                const int tok = (int)div_by((uint32_t)(f0 + r), d.by_g), head = seg.h * d.g + (f0 + r - tok * d.g);
+                v = *reinterpret_cast<const uint4*>(a.q + (int64_t)(seg.s.q0 + tok) * a.ldq + head * D + ch * 8);
+            }
+            *reinterpret_cast<uint4*>(smem + r * D * 2 + ((ch ^ (r & 7)) * 16)) = v;
+        }
+        __syncthreads();
+        int pos[MT][2];  // of the rows this thread holds; rows behind the tile see what the last one does
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                pos[mt][i] = past + (int)div_by((uint32_t)(f0 + min(mt * 16 + i * 8 + lane / 4, rows - 1)), d.by_g);
+        const int first_pos = past + (int)div_by((uint32_t)f0, d.by_g);  // keys up to here are seen by all rows
+
+        const int key_first = seg.u0 * kKeys + w * kWarpKeys;
+        // tiles of this warp that hold a key
+        const int tiles = min(seg.u1 - seg.u0, max(0, (k_end - key_first + kKeys - 1) / kKeys));
+        auto issue = [&](int i) {
+            if (i < tiles) {
+                const int key0 = key_first + i * kKeys;
+                const uint32_t dst = ring_base + (i % S) * kStage;
+                constexpr int kPass = 32 / CH;  // rows per pass of the warp
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    int in_page = 0;
+                    const int page = key0 + half * 8 < k_end ? page_of(a.seq, seg.b, key0 + half * 8, in_page) : -1;
+                    const __nv_bfloat16* kp = a.k + (int64_t)max(page, 0) * a.k_page + seg.h * a.k_head;
+                    const __nv_bfloat16* vp = a.v + (int64_t)max(page, 0) * a.v_page + seg.h * a.v_head;
+#pragma unroll
+                    for (int p = 0; p < 8 / kPass; ++p) {
+                        const int r = p * kPass + lane / CH, ch = lane % CH, rr = half * 8 + r;
+                        const bool there = page >= 0 && key0 + rr < k_end;
+                        const uint32_t at = dst + rr * D * 2 + ((ch ^ (rr & 7)) * 16);
+                        copy16(at, kp + (there ? (int64_t)(in_page + r) * a.k_row + ch * 8 : 0), there);
+                        copy16(at + kHalf, vp + (there ? (int64_t)(in_page + r) * a.v_row + ch * 8 : 0), there);
+                    }
+                }
+            }
+            copy_commit();
+        };
+        float o[MT][NT][4], m[MT][2], l[MT][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.0f;
+            m[mt][0] = m[mt][1] = -kInf, l[mt][0] = l[mt][1] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i) issue(i);
+        for (int i = 0; i < tiles; ++i) {
+            copy_wait<S - 2>();
+            __syncwarp();
+            const uint32_t kb = ring_base + (i % S) * kStage, vb = kb + kHalf;
+            const int key0 = key_first + i * kKeys;
+            float s[MT][2][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) s[mt][n][0] = s[mt][n][1] = s[mt][n][2] = s[mt][n][3] = 0.0f;
+            const int lr = lane & 7, lm = lane >> 3;  // row and matrix of an ldmatrix address
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                uint32_t kf[4];
+                {
+                    const int r = (lm >> 1) * 8 + lr, ch = ks * 2 + (lm & 1);
+                    ldsm4(kf, kb + r * D * 2 + ((ch ^ (r & 7)) * 16));
+                }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    uint32_t qf[4];
+                    const int r = mt * 16 + (lm & 1) * 8 + lr, ch = ks * 2 + (lm >> 1);
+                    ldsm4(qf, q_base + r * D * 2 + ((ch ^ (r & 7)) * 16));
+                    mma(s[mt][0], qf, kf[0], kf[1]);
+                    mma(s[mt][1], qf, kf[2], kf[3]);
+                }
+            }
+            const bool masked = key0 + kWarpKeys - 1 > first_pos;  // some row does not see all of these keys
+            if (masked) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (key0 + n * 8 + (lane & 3) * 2 + (e & 1) > pos[mt][e >> 1]) s[mt][n][e] = -kInf;
+            }
+            uint32_t pf[MT][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                float top[2], ref[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = fmaxf(fmaxf(s[mt][0][2 * e], s[mt][0][2 * e + 1]), fmaxf(s[mt][1][2 * e], s[mt][1][2 * e + 1]));
+                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
+                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 2));
+                    top[e] = fmaxf(m[mt][e], x * a.c);
+                }
+                if (__any_sync(~0u, top[0] > m[mt][0] || top[1] > m[mt][1])) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float f = top[e] > m[mt][e] ? ex2(m[mt][e] - top[e]) : 1.0f;
+                        m[mt][e] = top[e];
+                        l[mt][e] *= f;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) o[mt][n][2 * e] *= f, o[mt][n][2 * e + 1] *= f;
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) ref[e] = m[mt][e] == -kInf ? 0.0f : m[mt][e];
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[mt][n][e] = ex2(fmaf(s[mt][n][e], a.c, -ref[e >> 1]));
+                        l[mt][e >> 1] += s[mt][n][e];
+                    }
+                pf[mt][0] = pack_bf16(s[mt][0][0], s[mt][0][1]);
+                pf[mt][1] = pack_bf16(s[mt][0][2], s[mt][0][3]);
+                pf[mt][2] = pack_bf16(s[mt][1][0], s[mt][1][1]);
+                pf[mt][3] = pack_bf16(s[mt][1][2], s[mt][1][3]);
+            }
+            // A weight of 0 must not meet an infinity or NaN: in a tile with masked keys (those of tokens that came later; keys
+            // from k_end on are zeros here) such values take the way element by element.
+            bool strange = false;
+            if (masked && k_end - 1 > first_pos) {
+                for (int j = lane; j < kWarpKeys * CH; j += 32) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(ring + (i % S) * kStage + kHalf + j * 16);
+                    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) strange |= (x[e] & 0x7F80u) == 0x7F80u || (x[e] & 0x7F800000u) == 0x7F800000u;
+                }
+                strange = __any_sync(~0u, strange);
+            }
+            if (!strange) {
+#pragma unroll
+                for (int n = 0; n < NT; n += 2) {
+                    uint32_t vf[4];
+                    const int r = (lm & 1) * 8 + lr, ch = n + (lm >> 1);
+                    ldsm4_t(vf, vb + r * D * 2 + ((ch ^ (r & 7)) * 16));
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        mma(o[mt][n], pf[mt], vf[0], vf[1]);
+                        mma(o[mt][n + 1], pf[mt], vf[2], vf[3]);
+                    }
+                }
+            } else {
+                for (int j = 0; j < kWarpKeys; ++j) {
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        float p[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float x0 = (j & 8) ? s[mt][1][2 * e] : s[mt][0][2 * e], x1 = (j & 8) ? s[mt][1][2 * e + 1] : s[mt][0][2 * e + 1];
+                            p[e] = __shfl_sync(~0u, (j & 1) ? x1 : x0, (lane & ~3) | ((j & 7) >> 1));
+                        }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const uint32_t v = *reinterpret_cast<const uint32_t*>(ring + (i % S) * kStage + kHalf + j * D * 2 + ((n ^ (j & 7)) * 16) + (lane & 3) * 4);
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                if (key0 + j <= pos[mt][e]) {
+                                    o[mt][n][2 * e] = fmaf(p[e], bf16_lo(v), o[mt][n][2 * e]);
+                                    o[mt][n][2 * e + 1] = fmaf(p[e], bf16_hi(v), o[mt][n][2 * e + 1]);
+                                }
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            issue(i + S - 1);
+        }
+        copy_wait<0>();
+        __syncwarp();
+        // ---- the warps' sums, into their rings
+        float* const mine = reinterpret_cast<float*>(ring);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float x = l[mt][e];
+                x += __shfl_xor_sync(~0u, x, 1);
+                x += __shfl_xor_sync(~0u, x, 2);
+                const int r = mt * 16 + e * 8 + lane / 4;
+                if ((lane & 3) == 0) ml[w * R + r] = make_float2(m[mt][e], x);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    *reinterpret_cast<float2*>(mine + r * D + ((n ^ (r & 7)) * 8) + (lane & 3) * 2) = make_float2(o[mt][n][2 * e], o[mt][n][2 * e + 1]);
+            }
+        __syncthreads();
+        const bool whole = seg.u0 == 0 && seg.u1 == seg.units;
+        const int slot = 2 * cta + (seg.u0 == 0 ? 1 : 0);
+        for (int i = tid; i < rows * NT; i += kWarps * 32) {
+            const int r = i / NT, n = i % NT;
+            float ref = -kInf;
+#pragma unroll
+            for (int x = 0; x < kWarps; ++x) ref = fmaxf(ref, ml[x * R + r].x);
+            float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0.0f;
+#pragma unroll
+            for (int x = 0; x < kWarps; ++x) {
+                const float2 p = ml[x * R + r];
+                const float f = p.x == -kInf ? (p.y == 0.0f ? 0.0f : 1.0f) : ex2(p.x - ref);  // a sum without a reference: NaN scores
+                if (f == 0.0f) continue;  // an underflown share is none, whatever it holds
+                sum = fmaf(f, p.y, sum);
+                const float* src = reinterpret_cast<const float*>(smem + R * D * 2 + x * S * kStage) + r * D + ((n ^ (r & 7)) * 8);
+                const float4 u = *reinterpret_cast<const float4*>(src), v = *reinterpret_cast<const float4*>(src + 4);
+                acc[0] = fmaf(f, u.x, acc[0]), acc[1] = fmaf(f, u.y, acc[1]), acc[2] = fmaf(f, u.z, acc[2]), acc[3] = fmaf(f, u.w, acc[3]);
+                acc[4] = fmaf(f, v.x, acc[4]), acc[5] = fmaf(f, v.y, acc[5]), acc[6] = fmaf(f, v.z, acc[6]), acc[7] = fmaf(f, v.w, acc[7]);
+            }
+            if (whole) {
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] *= inv;
+                const int tok = (int)div_by((uint32_t)(f0 + r), d.by_g), head = seg.h * d.g + (f0 + r - tok * d.g);
+                const int64_t row = seg.s.q0 + tok;
+                store8(a.out + row * a.ldo + head * D + n * 8, acc, 8);
+                if (a.lse && n == 0) a.lse[row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
+            } else {
+                const int64_t at = (int64_t)slot * R + r;
+                store8(a.part_o + at * D + n * 8, acc, 8);
+                if (n == 0) a.part_ml[at] = make_float2(ref, sum);
+            }
+        }
+        if (first && tid == 0) {
+            // the item that this CTA begins inside of: from which CTA to which
+            JoinNote note{0, seg.s.q0, seg.s.n, seg.h, f0, {0, 0, 0}};
+            if (seg.u0 > 0) {
+                const int64_t item = start.unit - seg.u0;
+                const int i0 = (int)(item / start.chunk), i1 = (int)((item + seg.units - 1) / start.chunk);
+                if (i0 == cta - 1) note.parts = i1 - i0 + 1;
+            }
+            a.notes[cta] = note;
+        }
+        first = false;
+    }
+    if (first && tid == 0) a.notes[cta].parts = 0;
+    pdl_trigger();
+}
+
+// Joins the parts of the items that were cut: block (i, y) those of the item whose second CTA is i, rows 8 y .. 8 y + 7, a warp per
+// row, parts in the order of the keys.
+template <int D>
+__global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnArgs a) {
+    constexpr int E = D / 32;
+    const int lane = threadIdx.x & 31, cta = blockIdx.x;
+    pdl_wait();
+    pdl_trigger();
+    const JoinNote note = a.notes[cta];
+    const int r = blockIdx.y * 8 + (threadIdx.x >> 5), R = a.deal.rows, f = note.f0 + r;
+    if (note.parts == 0 || r >= R || f >= note.n * a.deal.g) return;
+    auto slot = [&](int p) { return ((int64_t)(p == 0 ? 2 * (cta - 1) + 1 : 2 * (cta - 1 + p)) * R + r); };
+    float ref = -kInf;
+    for (int p = lane; p < note.parts; p += 32) ref = fmaxf(ref, a.part_ml[slot(p)].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(~0u, ref, o));
+    float acc[E] = {}, sum = 0.0f;
+#pragma unroll 4
+    for (int p = 0; p < note.parts; ++p) {
+        const float2 q = a.part_ml[slot(p)];
+        float x[E];
+        const float* src = a.part_o + slot(p) * D + lane * E;
+        if (E == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(src);
+            x[0] = v.x, x[1] = v.y, x[2 % E] = v.z, x[3 % E] = v.w;
+        } else {
+            const float2 v = *reinterpret_cast<const float2*>(src);
+            x[0] = v.x, x[1] = v.y;
+        }
+        const float w = q.x == -kInf ? (q.y == 0.0f ? 0.0f : 1.0f) : ex2(q.x - ref);
+        if (w != 0.0f) {
+            sum = fmaf(w, q.y, sum);
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(w, x[e], acc[e]);
+        }
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int tok = (int)div_by((uint32_t)f, a.deal.by_g), head = note.h * a.deal.g + (f - tok * a.deal.g);
+    const int64_t row = note.q0 + tok;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * a.ldo + head * D + lane * E);
+#pragma unroll
+    for (int e = 0; e < E; e += 2) dst[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+    if (a.lse && lane == 0) a.lse[row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
+}
+
+// Workspace: notes, then the partial sums of two slots per CTA.
+struct Layout {
+    int ctas, rows;
+    size_t ml, o, bytes;
+};
+Layout layout(int64_t D, int rows, int ctas) {
+    Layout l;
+    l.ctas = ctas, l.rows = rows;
+    l.ml = kWsHeader + align_up((size_t)ctas * sizeof(JoinNote), 256);
+    l.o = l.ml + align_up((size_t)2 * ctas * rows * sizeof(float2), 256);
+    l.bytes = l.o + (size_t)2 * ctas * rows * (size_t)D * 4;
+    return l;
+}
+// Query rows of a tile: the tokens of a sequence times the heads of a group, in one or two tiles of 16.
+int rows_tile(int64_t T, int64_t Hq, int64_t Hkv, int64_t max_new) {
+    const int64_t n = max_new > 0 ? std::min(max_new, T) : T;
+    return n * (Hq / Hkv) <= 16 ? 16 : 32;
+}
+constexpr int kPlanSms = 148;  // the workspace query answers without a device
+
+}  // namespace
+}  // namespace resq
+
+using namespace resq;
+
+extern "C" {
+
+size_t resq_paged_attention_workspace_bytes(int64_t T, int64_t count, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_new) {
+    if (T <= 0 || count <= 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
+    return layout(D, rows_tile(T, Hq, Hkv, max_new), kPlanSms * kRowsCtasPerSm).bytes;
+}
+
+int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int64_t Hkv, int64_t D, const resq_paged_cache* cache,
+                         const resq_sequences* seqs, int64_t max_new, float scale, void* O, int64_t ldo, float* lse, void* workspace, size_t ws_bytes,
+                         void* stream) {
+    const char* what = "paged_attention";
+    if (!Q || !O) return fail(RESQ_ERR_NULL, what, "Q and O must not be NULL");
+    int rc = check_paged(what, cache, seqs, T, Hq, Hkv, D);
+    if (rc) return rc;
+    if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(RESQ_ERR_SHAPE, what, "scale must be positive and finite");
+    if (!rows_aligned(Q, ldq, Hq * D, RESQ_OUT_BF16) || !rows_aligned(O, ldo, Hq * D, RESQ_OUT_BF16) || !is_aligned(lse, 4))
+        return fail(RESQ_ERR_ALIGN, what, "Q and O need 16-byte aligned bases and rows of at least Hq * D elements, lse 4-byte alignment");
+    const Layout l = layout(D, rows_tile(T, Hq, Hkv, max_new), kPlanSms * kRowsCtasPerSm);
+    if (!workspace || !is_aligned(workspace, 256) || ws_bytes < l.bytes) {
+        set_last_error("paged_attention: workspace needs %zu bytes (256-byte aligned), got %zu", l.bytes, ws_bytes);
+        return RESQ_ERR_WORKSPACE;
+    }
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    using bf = __nv_bfloat16;
+    AttnArgs a;
+    a.seq = seq_args(*cache, *seqs, T);
+    a.deal = Deal{l.rows, kKeys, (int)Hkv, (int)(Hq / Hkv), fast_div((uint32_t)(Hq / Hkv))};
+    a.q = static_cast<const bf*>(Q), a.k = static_cast<const bf*>(cache->k), a.v = static_cast<const bf*>(cache->v);
+    a.ldq = ldq, a.ldo = ldo;
+    a.k_page = cache->k_page, a.k_row = cache->k_row, a.k_head = cache->k_head;
+    a.v_page = cache->v_page, a.v_row = cache->v_row, a.v_head = cache->v_head;
+    a.out = static_cast<bf*>(O), a.lse = lse, a.Hq = (int)Hq, a.c = scale * kLog2e, a.min_chunk = 1;
+    a.status = reinterpret_cast<DeviceStatus*>(ws);
+    a.notes = reinterpret_cast<JoinNote*>(ws + kWsHeader);
+    a.part_ml = reinterpret_cast<float2*>(ws + l.ml);
+    a.part_o = reinterpret_cast<float*>(ws + l.o);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    auto kern = D == 128 ? (l.rows == 16 ? attn_rows_kernel<128, 1> : attn_rows_kernel<128, 2>)
+                         : (l.rows == 16 ? attn_rows_kernel<64, 1> : attn_rows_kernel<64, 2>);
+    const int smem = D == 128 ? (l.rows == 16 ? rows_smem<128, 1>() : rows_smem<128, 2>()) : (l.rows == 16 ? rows_smem<64, 1>() : rows_smem<64, 2>());
+    rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem, "attn_rows_kernel shared memory");
+    if (rc) return rc;
+    {
+        LaunchScope scope(kKindRow, st);
+        rc = cuda_fail(launch_kernel(kern, dim3((unsigned)l.ctas), dim3(kWarps * 32), (size_t)smem, st, a), "attn_rows_kernel launch");
+        if (rc) return rc;
+    }
+    LaunchScope scope(kKindRow, st);
+    return cuda_fail(launch_kernel(D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>, dim3((unsigned)l.ctas, (unsigned)(l.rows / 8)), dim3(256), 0, st, a),
+                     "attn_join_kernel launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,297 @@
+// resq_verify_drafts: which drafted tokens a sequence keeps, and the token that takes the place of the first one it does not keep.
+//
+//   row r of a sequence: target p = softmax(logits_r / T), draft x_r proposed with q = exp((draft_logits - draft_peak) / T -
+//   draft_log_sum), or with certainty; x_r is kept while all before it are and u_r q(x_r) < p(x_r)
+//   at the first row that is not kept (the last row proposes nothing): argmax_j w_j / e_j over w = max(p - q, 0), or w = p where
+//   nothing was proposed; e are exponential variates, so token j is drawn with probability w_j / sum w
+//
+// The rows' sums are resq_token_logprobs' kernel, one pass over the logits, which is what the call is bound by.  This file's kernel
+// then needs one row per sequence again (of the logits, the draft's logits and e): a cluster of 1 to 8 CTAs per sequence finds the
+// row and takes the largest w / e of its slices.  Decisions next to a border are made again in 64 bits: a probability within 2^-14
+// of its border, and a drawing whose second largest ratio is that close to its largest.
+#include "row_common.cuh"
+
+#include <algorithm>
+#include <cmath>
+
+namespace resq {
+namespace {
+
+constexpr float kInf = __builtin_huge_valf();
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kThreads = 512;
+constexpr float kNear = 6.103515625e-05f;  // 2^-14: the fast exponentials are within 2^-18 for arguments down to -40
+
+struct VerifyArgs {
+    const void *logits, *draft_logits;
+    int64_t ld, ldd, lde;
+    const int32_t* row_start;
+    const int64_t* drafts;
+    const float *u, *e, *draft_peak, *draft_log_sum;
+    const float *logp, *peak, *log_sum;        // of the target's rows for the drafts
+    const int32_t* best;                       // greedy: the largest logit of every row, and its log-probability
+    const float* best_logp;
+    int32_t* accepted;
+    int64_t* tokens;
+    float* out_logp;
+    int B, R, V, slice;  // slice: vectors of 8 per CTA
+    float inv_t;
+    double inv_t64;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float value(const float* p) { return *p; }
+
+struct Best {
+    float s;     // largest ratio; 0: none
+    int j;       // its lowest place
+    float next;  // the largest of the others
+};
+__device__ __forceinline__ Best join(const Best& p, const Best& q) {
+    const bool p_first = p.s > q.s || (p.s == q.s && p.j < q.j);
+    Best r = p_first ? p : q;
+    r.next = fmaxf(fmaxf(p.next, q.next), p_first ? q.s : p.s);
+    return r;
+}
+struct Best64 {
+    double s;
+    int j;
+};
+__device__ __forceinline__ Best64 join(const Best64& p, const Best64& q) { return p.s > q.s || (p.s == q.s && p.j < q.j) ? p : q; }
+
+__device__ __forceinline__ Best shuffle(const Best& b, int o) {
+    return Best{__shfl_xor_sync(~0u, b.s, o), __shfl_xor_sync(~0u, b.j, o), __shfl_xor_sync(~0u, b.next, o)};
+}
+__device__ __forceinline__ Best64 shuffle(const Best64& b, int o) { return Best64{__shfl_xor_sync(~0u, b.s, o), __shfl_xor_sync(~0u, b.j, o)}; }
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+template <typename W>
+__device__ __forceinline__ W remote(const W* p, int rank) {
+    static_assert(sizeof(W) % 4 == 0, "");
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    W v;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(W) / 4; ++i)
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(dst[i]) : "r"(at + 4 * i) : "memory");
+    return v;
+}
+// The largest over the cluster, the same in all threads.  `warps` and `mine` in shared memory, not used by the call before.
+template <typename W>
+__device__ W cluster_best(W b, W* warps, W* mine, int cs) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) b = join(b, shuffle(b, o));
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = b;
+    __syncthreads();
+    b = warps[0];
+    for (int i = 1; i < (int)(blockDim.x >> 5); ++i) b = join(b, warps[i]);
+    if (cs == 1) return b;
+    if (threadIdx.x == 0) *mine = b;
+    cluster_sync();
+    b = remote(mine, 0);
+    for (int i = 1; i < cs; ++i) b = join(b, remote(mine, i));
+    return b;
+}
+
+template <typename T, bool DRAFT, bool GREEDY>
+__global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant__ VerifyArgs a) {
+    __shared__ Best warp_best[kThreads / 32], cta_best;
+    __shared__ Best64 warp_best64[kThreads / 32], cta_best64;
+    uint32_t cs, rank = 0;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(cs));
+    if (cs > 1) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const int tid = threadIdx.x, lane = tid & 31, b = blockIdx.x / cs;
+    pdl_wait();
+    pdl_trigger();
+    const int r0 = min(max(a.row_start[b], 0), a.R), n = max(min(max(a.row_start[b + 1], 0), a.R) - r0, 0);
+    if (n == 0) {  // the cluster's CTAs alike
+        if (rank == 0 && tid == 0) a.accepted[b] = 0;
+        return;
+    }
+    const float c = a.inv_t * kLog2e;
+    // ---- the first row that is not kept; every warp for itself
+    int kept = 0;
+    bool proposed = false;  // something was proposed at that row
+    for (int i0 = 0;; i0 += 32) {
+        const int i = i0 + lane, r = r0 + i;
+        bool keep = false, some = false;
+        if (i < n - 1) {
+            const int64_t x = a.drafts[r];
+            some = x >= 0 && x < a.V;
+            if (some && GREEDY) keep = x == a.best[r] && a.best_logp[r] > -kInf;  // not of a row of NaN
+            else if (some) {
+                const float logp = a.logp[r], u = a.u[r];
+                float logq = 0.0f, xd = 0.0f;
+                if (DRAFT) {
+                    xd = value(static_cast<const T*>(a.draft_logits) + (int64_t)r * a.ldd + x);
+                    logq = (xd - a.draft_peak[r]) * a.inv_t - a.draft_log_sum[r];
+                }
+                const float ratio = ex2((logp - logq) * kLog2e);
+                keep = u < ratio && logp > -kInf;
+                if (fabsf(u - ratio) <= kNear * ratio) {
+                    const double lp = ((double)value(static_cast<const T*>(a.logits) + (int64_t)r * a.ld + x) - (double)a.peak[r]) * a.inv_t64 - (double)a.log_sum[r];
+                    const double lq = DRAFT ? ((double)xd - (double)a.draft_peak[r]) * a.inv_t64 - (double)a.draft_log_sum[r] : 0.0;
+                    keep = (double)u < exp(lp - lq) && logp > -kInf;
+                }
+            }
+        }
+        const unsigned all = __ballot_sync(~0u, keep), had = __ballot_sync(~0u, some);
+        if (all != ~0u) {
+            const int at = __ffs(~all) - 1;
+            kept = i0 + at;
+            proposed = (had >> at) & 1;
+            break;
+        }
+    }
+    const int r = r0 + kept;
+    // ---- the token at that row
+    int64_t token = -1;
+    float token_logp = 0.0f;
+    if (GREEDY) {
+        const float lp = a.best_logp[r];
+        if (lp == lp && lp > -kInf) token = a.best[r], token_logp = lp;
+    } else {
+        const T* const x = static_cast<const T*>(a.logits) + (int64_t)r * a.ld;
+        const T* const xd = DRAFT ? static_cast<const T*>(a.draft_logits) + (int64_t)r * a.ldd : nullptr;
+        const float* const e = a.e + (int64_t)b * a.lde;
+        const float peak = a.peak[r], log_sum = a.log_sum[r], add = -log_sum * kLog2e;
+        const float dpeak = DRAFT ? a.draft_peak[r] : 0.0f, dadd = DRAFT ? -a.draft_log_sum[r] * kLog2e : 0.0f;
+        const int sure = !DRAFT && proposed ? (int)a.drafts[r] : -1;  // q is 1 there
+        const bool less = DRAFT && proposed;
+        const int v0 = min((int)rank * a.slice, (a.V + 7) / 8), v1 = min(v0 + a.slice, (a.V + 7) / 8);
+        // score(j): w / e in 32 bits, given the three values
+        auto weight = [&](float z, float zd, bool minus) {
+            const float p = ex2(fmaf(z - peak, c, add));
+            return minus ? fmaxf(p - ex2(fmaf(zd - dpeak, c, dadd)), 0.0f) : p;
+        };
+        auto weight64 = [&](float z, float zd, bool minus) {
+            const double p = exp(((double)z - (double)peak) * a.inv_t64 - (double)log_sum);
+            return minus ? fmax(p - exp(((double)zd - (double)dpeak) * a.inv_t64 - (double)a.draft_log_sum[r]), 0.0) : p;
+        };
+        auto visit = [&](bool minus, int skip, auto&& take) {
+            for (int v = v0 + tid; v < v1; v += kThreads) {
+                const int m = min(8, a.V - v * 8);
+                Raw8<T> rz, rd;
+                Raw8<float> re;
+                rz.load(x + (int64_t)v * 8, m);
+                if (DRAFT && minus) rd.load(xd + (int64_t)v * 8, m);
+                re.load(e + (int64_t)v * 8, m);
+                float z[8], zd[8] = {}, ev[8];
+                rz.get(z);
+                if (DRAFT && minus) rd.get(zd);
+                re.get(ev);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < m && v * 8 + i != skip) take(v * 8 + i, z[i], zd[i], ev[i]);
+            }
+        };
+        Best best{0.0f, a.V, 0.0f};
+        bool minus = less;
+        int skip = sure;
+        for (int round = 0; round < 2; ++round) {
+            best = Best{0.0f, a.V, 0.0f};
+            visit(minus, skip, [&](int j, float z, float zd, float ev) {
+                const float s = __fdividef(weight(z, zd, minus), ev);
+                if (s > best.s) best = Best{s, j, best.s};  // in the order of places: equal ones keep the first
+                else best.next = fmaxf(best.next, s);
+            });
+            best = cluster_best(best, warp_best, &cta_best, (int)cs);
+            if (best.j < a.V || (!minus && skip < 0)) break;
+            // nothing is left of p - q (p = q up to rounding): drawn from p
+            minus = false, skip = -1;
+            if (cs > 1) cluster_sync();
+            __syncthreads();
+        }
+        if (best.j < a.V && best.next >= best.s * (1.0f - kNear)) {
+            Best64 b64{0.0, a.V};
+            const float low = best.s * (1.0f - 2.0f * kNear);
+            visit(minus, skip, [&](int j, float z, float zd, float ev) {
+                if (__fdividef(weight(z, zd, minus), ev) >= low) b64 = join(b64, Best64{weight64(z, zd, minus) / (double)ev, j});
+            });
+            best.j = cluster_best(b64, warp_best64, &cta_best64, (int)cs).j;
+        }
+        if (best.j < a.V) token = best.j, token_logp = (value(x + best.j) - peak) * a.inv_t - log_sum;
+        if (cs > 1) cluster_sync();  // a CTA's shared memory stays until the others have read it
+    }
+    if (rank != 0) return;
+    if (tid == 0) a.accepted[b] = kept;
+    for (int i = tid; i < n; i += kThreads) {
+        const bool k = i < kept;
+        a.tokens[r0 + i] = k ? a.drafts[r0 + i] : i == kept ? token : -1;
+        a.out_logp[r0 + i] = k ? (GREEDY ? a.best_logp[r0 + i] : a.logp[r0 + i]) : i == kept ? token_logp : 0.0f;
+    }
+}
+
+struct Layout {
+    size_t logp, peak, log_sum, ids, bytes;
+};
+Layout layout(int64_t R) {
+    const size_t one = align_up((size_t)R * 4, 256);
+    return Layout{kWsHeader, kWsHeader + one, kWsHeader + 2 * one, kWsHeader + 3 * one, kWsHeader + 4 * one};
+}
+
+}  // namespace
+}  // namespace resq
+
+using namespace resq;
+
+extern "C" {
+
+size_t resq_verify_drafts_workspace_bytes(int64_t R) { return R > 0 ? layout(R).bytes : 0; }
+
+int resq_verify_drafts(const void* logits, int dtype, int64_t R, int64_t V, int64_t ld, const int32_t* row_start, int64_t count, const int64_t* drafts,
+                       const float* u, const float* noise, int64_t lde, const void* draft_logits, int64_t ldd, const float* draft_peak,
+                       const float* draft_log_sum, float temperature, int32_t* accepted, int64_t* tokens, float* logp, void* workspace,
+                       size_t ws_bytes, void* stream) {
+    const char* what = "verify_drafts";
+    const bool greedy = temperature == 0.0f, draft = draft_logits != nullptr && !greedy;
+    if (!logits || !row_start || !drafts || !accepted || !tokens || !logp || (!greedy && (!u || !noise)) || (draft && (!draft_peak || !draft_log_sum)))
+        return fail(RESQ_ERR_NULL, what, "logits, row_start, drafts and the outputs must not be NULL, nor u and noise where tokens are drawn, nor a draft's peak and log_sum");
+    if (dtype != RESQ_OUT_BF16 && dtype != RESQ_OUT_F32) return fail(RESQ_ERR_PATTERN, what, "unknown type of the logits");
+    if (R <= 0 || R > INT32_MAX || V <= 0 || V > RESQ_MAX_VOCAB || count <= 0 || count > RESQ_MAX_SEQUENCES) {
+        set_last_error("verify_drafts: %lld rows of %lld, %lld sequences (1 or more, V <= %d, 1 .. %d sequences)", (long long)R, (long long)V, (long long)count,
+                       RESQ_MAX_VOCAB, RESQ_MAX_SEQUENCES);
+        return RESQ_ERR_SHAPE;
+    }
+    if (!greedy && !(temperature >= 1e-6f && temperature <= 1e6f)) return fail(RESQ_ERR_SHAPE, what, "temperature must be 0 or lie in 1e-6 .. 1e6");
+    if (!rows_aligned(logits, ld, V, dtype) || (draft && !rows_aligned(draft_logits, ldd, V, dtype)) || (!greedy && !rows_aligned(noise, lde, V, RESQ_OUT_F32)))
+        return fail(RESQ_ERR_ALIGN, what, "logits, draft_logits and noise need 16-byte aligned bases and rows of at least V elements");
+    if (!is_aligned(row_start, 4) || !is_aligned(drafts, 8) || !is_aligned(u, 4) || !is_aligned(draft_peak, 4) || !is_aligned(draft_log_sum, 4) ||
+        !is_aligned(accepted, 4) || !is_aligned(tokens, 8) || !is_aligned(logp, 4))
+        return fail(RESQ_ERR_ALIGN, what, "drafts and tokens must be 8-byte aligned, the other row values 4-byte aligned");
+    const Layout l = layout(R);
+    if (!workspace || !is_aligned(workspace, 256) || ws_bytes < l.bytes) {
+        set_last_error("verify_drafts: workspace needs %zu bytes (256-byte aligned), got %zu", l.bytes, ws_bytes);
+        return RESQ_ERR_WORKSPACE;
+    }
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    float *wl = reinterpret_cast<float*>(ws + l.logp), *wp = reinterpret_cast<float*>(ws + l.peak), *ws_sum = reinterpret_cast<float*>(ws + l.log_sum);
+    int32_t* ids = reinterpret_cast<int32_t*>(ws + l.ids);
+    int rc = greedy ? resq_token_logprobs(logits, dtype, R, V, ld, nullptr, 1.0f, 1, nullptr, nullptr, nullptr, nullptr, ids, wl, stream)
+                    : resq_token_logprobs(logits, dtype, R, V, ld, drafts, temperature, 0, wl, nullptr, wp, ws_sum, nullptr, nullptr, stream);
+    if (rc) return rc;
+    // Few sequences: their row over a cluster, up to 256 CTAs and not below 8192 logits a CTA (two iterations of its threads).
+    const int64_t vecs = (V + 7) / 8;
+    int cs = 1;
+    while (!greedy && cs < 8 && count * cs * 2 <= 256 && vecs / (2 * cs) >= 1024) cs *= 2;
+    VerifyArgs a{logits, draft ? draft_logits : nullptr, ld, ldd, lde, row_start, drafts, u, noise, draft_peak, draft_log_sum, wl, wp, ws_sum, ids, wl,
+                 accepted, tokens, logp, (int)count, (int)R, (int)V, (int)((vecs + cs - 1) / cs), greedy ? 1.0f : 1.0f / temperature,
+                 greedy ? 1.0 : 1.0 / (double)temperature};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    using bf = __nv_bfloat16;
+    auto kern = dtype == RESQ_OUT_F32 ? (greedy ? verify_kernel<float, false, true> : draft ? verify_kernel<float, true, false> : verify_kernel<float, false, false>)
+                                      : (greedy ? verify_kernel<bf, false, true> : draft ? verify_kernel<bf, true, false> : verify_kernel<bf, false, false>);
+    LaunchScope scope(kKindRow, st);
+    return cuda_fail(launch_clusters(kern, dim3((unsigned)(count * cs)), kThreads, 0, cs, st, a), "verify_kernel launch");
+}
+
+}  // extern "C"
