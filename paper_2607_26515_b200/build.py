@@ -10,7 +10,7 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libresq.so")
 SOURCES = ["api.cu", "quantize.cu", "gemm_hif4.cu", "gemm_pair.cu", "gemm_mxfp4.cu", "gemm_decode.cu", "static_scratch.cu",
            "gemv.cu", "block_join.cu", "token_logprobs.cu",
-           "rope_append.cu", "paged_attention.cu", "verify_drafts.cu"]
+           "rope_append.cu", "paged_attention.cu", "paged_chunk.cu", "verify_drafts.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr",

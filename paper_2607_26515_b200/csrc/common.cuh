@@ -229,6 +229,8 @@ bool gemm_mxfp4_native_supported(int64_t M, int64_t N, int64_t K, bool res);
 int launch_gemm_mxfp4_native(const Mxfp4NativeArgs& g, cudaStream_t stream);
 int make_tmap_2d(CUtensorMap* m, CUtensorMapDataType dt, const void* base, uint64_t inner, uint64_t rows,
                  uint64_t row_stride_bytes, uint32_t box_inner, uint32_t box_rows, CUtensorMapSwizzle sw);
+// bf16 tensor of up to 5 dimensions (innermost first; strides in bytes of dimensions 1 ..), 128-byte swizzle, zeros outside.
+int make_tmap_bf16(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
 int launch_splitk_reduce(const GemmArgs& g, int splits, cudaStream_t stream);
 int gemm_hif4_pick_splits(int64_t M, int64_t N, int64_t K);
 size_t gemm_hif4_scratch_bytes(int64_t M, int64_t N, int64_t K);  // what splitk_partials must hold for this shape

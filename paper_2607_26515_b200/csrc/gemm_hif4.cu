@@ -525,6 +525,25 @@ int make_tmap_2d(CUtensorMap* m, CUtensorMapDataType dt, const void* base, uint6
     return RESQ_OK;
 }
 
+int make_tmap_bf16(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) {
+        set_last_error("cuTensorMapEncodeTiled is not available from the driver");
+        return RESQ_ERR_CUDA;
+    }
+    cuuint64_t d[5], st[5];
+    cuuint32_t bx[5], estr[5] = {1, 1, 1, 1, 1};
+    for (int i = 0; i < rank; ++i) d[i] = dims[i], bx[i] = box[i];
+    for (int i = 0; i + 1 < rank; ++i) st[i] = strides[i];
+    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st, bx, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        set_last_error("cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+        return RESQ_ERR_CUDA;
+    }
+    return RESQ_OK;
+}
+
 int launch_splitk_reduce(const GemmArgs& g, int splits, cudaStream_t stream) {
     if (splits <= 1) return RESQ_OK;
     const int64_t n = (g.N & 3) == 0 ? g.M * g.N / 4 : g.M * g.N;

@@ -45,6 +45,43 @@ inline SeqArgs seq_args(const resq_paged_cache& c, const resq_sequences& s, int6
                    (int)c.pages, fast_div((uint32_t)c.page_size)};
 }
 
+// How attention is dealt out (below): rows and keys per tile, heads.
+struct Deal {
+    int rows, keys, Hkv, g;
+    FastDiv by_g;
+};
+// Where partial results lie: a CTA's first segment, when its item began in an earlier CTA, in slot 2 * cta; one whose item goes on
+// in the next CTA otherwise in slot 2 * cta + 1.  The CTA that begins inside an item says so in its entry of `notes`: the CTAs
+// before it that the item covers, and all of them.
+struct JoinNote {
+    int parts;   // CTAs of the item (0: this CTA does not begin inside an item, or is not the item's second one)
+    int q0, n;   // the item's sequence: first token row, new tokens
+    int h, f0;   // kv head, first row
+    int pad[3];
+};
+struct AttnArgs {
+    SeqArgs seq;
+    Deal deal;
+    const __nv_bfloat16 *q, *k, *v;
+    int64_t ldq, ldo, k_page, k_row, k_head, v_page, v_row, v_head;
+    __nv_bfloat16* out;
+    float* lse;       // [T, Hq] or null
+    int Hq;
+    float c;          // scale log2(e)
+    int min_chunk;
+    float* part_o;    // [2 ctas][rows][D], unnormalised
+    float2* part_ml;  // [2 ctas][rows]: reference, sum
+    JoinNote* notes;  // [ctas]
+    DeviceStatus* status;
+};
+
+// paged_chunk.cu: the tensor-core form for chunks of new tokens.  Rows of its tiles for g query heads per kv head, whether it takes
+// these strides, and its launch (args.deal.rows and .keys as it wants them).
+constexpr int kChunkKeys = 128;
+int attn_chunk_rows(int g);
+bool attn_chunk_supported(const AttnArgs& args);
+int launch_attn_chunk(const AttnArgs& args, int D, int ctas, cudaStream_t stream);
+
 #ifdef __CUDACC__
 
 struct Seq {
@@ -71,10 +108,6 @@ __device__ __forceinline__ int page_of(const SeqArgs& a, int b, int j, int& with
 // writes its rows).  Items are ordered by sequence, kv head, tile; all units in this order are cut into equal ranges, one per CTA,
 // so that ragged lengths need no plan from the host and a captured call follows the lengths on the device.  A CTA's first item may
 // have begun in an earlier CTA and its last one may go on in a later one: those are left as partial results.
-struct Deal {
-    int rows, keys, Hkv, g;
-    FastDiv by_g;
-};
 __device__ __forceinline__ int deal_tiles(const Seq& s, const Deal& d) { return (int)(((int64_t)s.n * d.g + d.rows - 1) / d.rows); }
 __device__ __forceinline__ int deal_k_end(const Seq& s, const Deal& d, int t) {  // keys that tile t sees
     const int64_t f = min((int64_t)(t + 1) * d.rows, (int64_t)s.n * d.g) - 1;
@@ -227,16 +260,6 @@ struct DealWalk {
         ++t;
         return true;
     }
-};
-
-// Where partial results lie: a CTA's first segment, when its item began in an earlier CTA, in slot 2 * cta; one whose item goes on
-// in the next CTA otherwise in slot 2 * cta + 1.  The CTA that begins inside an item says so in its entry of `notes`: the CTAs
-// before it that the item covers, and all of them.
-struct JoinNote {
-    int parts;   // CTAs of the item (0: this CTA does not begin inside an item, or is not the item's second one)
-    int q0, n;   // the item's sequence: first token row, new tokens
-    int h, f0;   // kv head, first row
-    int pad[3];
 };
 
 #endif  // __CUDACC__

@@ -51,22 +51,6 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kWarps = 4, kKeys = 64, kWarpKeys = kKeys / kWarps;  // of attn_rows_kernel
 constexpr int kRowsCtasPerSm = 2;
 
-struct AttnArgs {
-    SeqArgs seq;
-    Deal deal;
-    const __nv_bfloat16 *q, *k, *v;
-    int64_t ldq, ldo, k_page, k_row, k_head, v_page, v_row, v_head;
-    __nv_bfloat16* out;
-    float* lse;       // [T, Hq] or null
-    int Hq;
-    float c;          // scale log2(e)
-    int min_chunk;
-    float* part_o;    // [2 ctas][rows][D], unnormalised
-    float2* part_ml;  // [2 ctas][rows]: reference, sum
-    JoinNote* notes;  // [ctas]
-    DeviceStatus* status;
-};
-
 __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -423,12 +407,19 @@ Layout layout(int64_t D, int rows, int ctas) {
     l.bytes = l.o + (size_t)2 * ctas * rows * (size_t)D * 4;
     return l;
 }
-// Query rows of a tile: the tokens of a sequence times the heads of a group, in one or two tiles of 16.
-int rows_tile(int64_t T, int64_t Hq, int64_t Hkv, int64_t max_new) {
-    const int64_t n = max_new > 0 ? std::min(max_new, T) : T;
-    return n * (Hq / Hkv) <= 16 ? 16 : 32;
-}
+// The kernel and its tiles, from what the host knows of a sequence's query rows per kv head: up to 16 or 32 rows are one or two
+// tiles of the register-operand instruction, more go to the tensor-memory form.
+struct Choice {
+    bool chunk;
+    int rows, ctas;
+};
 constexpr int kPlanSms = 148;  // the workspace query answers without a device
+Choice choose(int64_t T, int64_t Hq, int64_t Hkv, int64_t max_new) {
+    const int64_t n = max_new > 0 ? std::min(max_new, T) : T, rows = n * (Hq / Hkv);
+    const int limit = env_int("RESQ_ATTN_ROWS", 32);
+    if (rows > limit) return Choice{true, attn_chunk_rows((int)(Hq / Hkv)), kPlanSms};
+    return Choice{false, rows <= 16 ? 16 : 32, kPlanSms * kRowsCtasPerSm};
+}
 
 }  // namespace
 }  // namespace resq
@@ -438,8 +429,9 @@ using namespace resq;
 extern "C" {
 
 size_t resq_paged_attention_workspace_bytes(int64_t T, int64_t count, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_new) {
-    if (T <= 0 || count <= 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
-    return layout(D, rows_tile(T, Hq, Hkv, max_new), kPlanSms * kRowsCtasPerSm).bytes;
+    if (T <= 0 || count <= 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv || Hq / Hkv > RESQ_MAX_GROUP_HEADS || (D != 64 && D != 128)) return 0;
+    const Choice c = choose(T, Hq, Hkv, max_new);
+    return layout(D, c.rows, c.ctas).bytes;
 }
 
 int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int64_t Hkv, int64_t D, const resq_paged_cache* cache,
@@ -452,7 +444,8 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
     if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(RESQ_ERR_SHAPE, what, "scale must be positive and finite");
     if (!rows_aligned(Q, ldq, Hq * D, RESQ_OUT_BF16) || !rows_aligned(O, ldo, Hq * D, RESQ_OUT_BF16) || !is_aligned(lse, 4))
         return fail(RESQ_ERR_ALIGN, what, "Q and O need 16-byte aligned bases and rows of at least Hq * D elements, lse 4-byte alignment");
-    const Layout l = layout(D, rows_tile(T, Hq, Hkv, max_new), kPlanSms * kRowsCtasPerSm);
+    Choice ch = choose(T, Hq, Hkv, max_new);
+    Layout l = layout(D, ch.rows, ch.ctas);
     if (!workspace || !is_aligned(workspace, 256) || ws_bytes < l.bytes) {
         set_last_error("paged_attention: workspace needs %zu bytes (256-byte aligned), got %zu", l.bytes, ws_bytes);
         return RESQ_ERR_WORKSPACE;
@@ -461,17 +454,31 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
     using bf = __nv_bfloat16;
     AttnArgs a;
     a.seq = seq_args(*cache, *seqs, T);
-    a.deal = Deal{l.rows, kKeys, (int)Hkv, (int)(Hq / Hkv), fast_div((uint32_t)(Hq / Hkv))};
+    a.deal = Deal{l.rows, ch.chunk ? kChunkKeys : kKeys, (int)Hkv, (int)(Hq / Hkv), fast_div((uint32_t)(Hq / Hkv))};
     a.q = static_cast<const bf*>(Q), a.k = static_cast<const bf*>(cache->k), a.v = static_cast<const bf*>(cache->v);
     a.ldq = ldq, a.ldo = ldo;
     a.k_page = cache->k_page, a.k_row = cache->k_row, a.k_head = cache->k_head;
     a.v_page = cache->v_page, a.v_row = cache->v_row, a.v_head = cache->v_head;
     a.out = static_cast<bf*>(O), a.lse = lse, a.Hq = (int)Hq, a.c = scale * kLog2e, a.min_chunk = 1;
+    if (ch.chunk && !attn_chunk_supported(a)) {  // a stride of 0: no tensor map takes it; this workspace is smaller
+        ch = Choice{false, 32, kPlanSms * kRowsCtasPerSm};
+        l = layout(D, ch.rows, ch.ctas);
+        a.deal.rows = ch.rows, a.deal.keys = kKeys;
+    }
     a.status = reinterpret_cast<DeviceStatus*>(ws);
     a.notes = reinterpret_cast<JoinNote*>(ws + kWsHeader);
     a.part_ml = reinterpret_cast<float2*>(ws + l.ml);
     a.part_o = reinterpret_cast<float*>(ws + l.o);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    auto join = [&] {
+        LaunchScope scope(kKindRow, st);
+        return cuda_fail(launch_kernel(D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>, dim3((unsigned)l.ctas, (unsigned)((l.rows + 7) / 8)), dim3(256), 0, st, a),
+                         "attn_join_kernel launch");
+    };
+    if (ch.chunk) {
+        rc = launch_attn_chunk(a, (int)D, l.ctas, st);
+        return rc ? rc : join();
+    }
     auto kern = D == 128 ? (l.rows == 16 ? attn_rows_kernel<128, 1> : attn_rows_kernel<128, 2>)
                          : (l.rows == 16 ? attn_rows_kernel<64, 1> : attn_rows_kernel<64, 2>);
     const int smem = D == 128 ? (l.rows == 16 ? rows_smem<128, 1>() : rows_smem<128, 2>()) : (l.rows == 16 ? rows_smem<64, 1>() : rows_smem<64, 2>());
@@ -482,9 +489,7 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
         rc = cuda_fail(launch_kernel(kern, dim3((unsigned)l.ctas), dim3(kWarps * 32), (size_t)smem, st, a), "attn_rows_kernel launch");
         if (rc) return rc;
     }
-    LaunchScope scope(kKindRow, st);
-    return cuda_fail(launch_kernel(D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>, dim3((unsigned)l.ctas, (unsigned)(l.rows / 8)), dim3(256), 0, st, a),
-                     "attn_join_kernel launch");
+    return join();
 }
 
 }  // extern "C"

@@ -1,0 +1,552 @@
+// Attention of chunks of new tokens over a paged cache: the tensor-core form of resq_paged_attention (formulas in
+// paged_attention.cu), for sequences with more query rows per kv head than attn_rows_kernel takes.
+//
+// A tile is two halves of up to 128 query rows (tokens times the heads that share a kv head, whole tokens per half), the keys come
+// in tiles of 128.  Scores S = Q K^T of a half fill 128 columns of tensor memory, its softmax warps replace them by the weights P
+// (bf16, in the same columns), which are the A operand of O += P V from there; S and O of both halves are all 512 columns.  While the
+// warps of one half are at their exponentials the tensor cores have the other half's products to do, so the halves take
+// turns, with K and V read into shared memory once for both.
+//
+// Warps: 0-3 and 4-7 softmax of a half (a row per thread, so maxima and sums need no exchange), 8 issues the products, 9 deals out
+// segments and loads (a page's rows per copy, page numbers looked up by its lanes), 10 repairs the value tiles that reach past
+// the first row's last key: rows behind the last key become zeros (0 times what a page holds there may be NaN), and infinities
+// and NaN are taken out and added by those rows that do see them.
+//
+// O is rescaled only when a row's maximum has grown by more than 8 in the exponent of 2 since its reference was set: weights up
+// to 2^8 lose nothing in bf16 or in the fp32 sums, and the final division takes the reference out.
+#include "paged.cuh"
+#include "ptx.cuh"
+
+namespace resq {
+namespace {
+
+constexpr float kInf = __builtin_huge_valf();
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kKeys = kChunkKeys, kHalf = 128;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kFixWarp = 10, kThreads = 384;
+constexpr int kDescs = 4;    // segments described ahead of the slowest reader
+constexpr int kStrange = 4;  // key tiles of a segment that can hold keys of its own tokens (at most 256)
+constexpr float kGrowth = 8.0f;
+
+template <int D>
+constexpr int stages() { return D == 128 ? 5 : 10; }  // 160 KB of key and value tiles
+template <int D>
+constexpr int tile_bytes() { return kKeys * D * 2; }
+
+struct ChunkMaps {
+    CUtensorMap q, k, v;
+};
+struct ChunkArgs {
+    AttnArgs a;
+    int half_rows, half_tokens;  // of a half tile
+    int box;                     // keys per copy: a power of two that divides the page and the tile
+};
+
+struct ChunkSeg {
+    int b, q0, n, h, f0, past, k_end, first_pos;
+    int u0, end, slot;           // key tiles u0 .. end - 1 are to be read; slot: of the partial result, -1: the whole item
+    int rows[2], stop[2];        // per half: rows, key tiles u0 .. stop - 1
+};
+struct ChunkShared {
+    uint64_t desc_full[kDescs], desc_empty[kDescs], strange_full[kDescs];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
+    uint64_t kv_full[10], kv_empty[10], raw_full[10];
+    ChunkSeg seg[kDescs];
+    uint32_t strange[kDescs][kStrange][4];  // a bit per key whose value row holds an infinity or NaN
+    int64_t sums[kThreads / 32];
+    DealStart found;
+    uint32_t tmem;
+    int abort;
+};
+
+__device__ __forceinline__ void chunk_timeout(DeviceStatus* st, int where) {
+    st->where = where;
+    st->block = (int)blockIdx.x;
+    st->code = RESQ_ERR_TIMEOUT;
+}
+// A wait of all lanes with one answer for them all: lanes that gave up apart would part the warp.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    return __all_sync(~0u, ptx::mbar_wait_spin(bar, parity, abort_flag));
+}
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ bool strange_pair(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_constant__ ChunkArgs p, const __grid_constant__ ChunkMaps maps) {
+    constexpr int ST = stages<D>(), TILE = tile_bytes<D>(), CG = D / 64, QH = kHalf * D * 2;  // column groups of 64
+    extern __shared__ unsigned char raw_smem[];
+    unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
+    unsigned char* const q_smem = smem;                // [half][column group][128 rows][128 bytes]
+    unsigned char* const ring = smem + 2 * QH;         // [stage][column group][128 keys][128 bytes]
+    ChunkShared& sh = *reinterpret_cast<ChunkShared*>(ring + ST * TILE);
+    const AttnArgs& a = p.a;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+    volatile int* const abort_flag = &sh.abort;
+
+    if (tid == 0) {
+        for (int i = 0; i < kDescs; ++i) {
+            ptx::mbar_init(&sh.desc_full[i], 1);
+            ptx::mbar_init(&sh.desc_empty[i], 10);  // eight softmax warps, products, repairs
+            ptx::mbar_init(&sh.strange_full[i], 1);
+        }
+        for (int h = 0; h < 2; ++h) {
+            ptx::mbar_init(&sh.q_full[h], 1);
+            ptx::mbar_init(&sh.q_empty[h], 1);
+            ptx::mbar_init(&sh.s_full[h], 1);
+            ptx::mbar_init(&sh.p_full[h], 4);
+            ptx::mbar_init(&sh.o_full[h], 1);
+        }
+        for (int i = 0; i < ST; ++i) {
+            ptx::mbar_init(&sh.kv_full[i], 1);
+            ptx::mbar_init(&sh.kv_empty[i], 1);
+            ptx::mbar_init(&sh.raw_full[i], 1);
+        }
+        ptx::mbar_fence_init();
+        sh.abort = 0;
+    }
+    if (warp == kMmaWarp) ptx::tmem_alloc(&sh.tmem, 512);
+    if (warp == kLoadWarp && lane == 0) {
+        ptx::tma_prefetch_desc(&maps.q);
+        ptx::tma_prefetch_desc(&maps.k);
+        ptx::tma_prefetch_desc(&maps.v);
+    }
+    pdl_wait();
+    if (cta == 0 && tid == 0) *a.status = DeviceStatus{RESQ_OK, 0, 0, 0};
+    ptx::tc_fence_before();
+    const DealStart start = deal_start(a.seq, a.deal, cta, gridDim.x, a.min_chunk, sh.sums, &sh.found);  // orders the block
+    ptx::tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+
+    if (warp == kLoadWarp) {
+        // ------------------------------------------------------------------ segments, queries, keys and values
+        DealWalk walk;
+        walk.init(a.seq, a.deal, start);
+        Segment s;
+        int count = 0, q_uses[2] = {0, 0};
+        uint32_t pos = 0;                // key and value tiles so far
+        uint32_t raw = 0, raw_turn = 0;  // per stage: its tile goes to the repairs; parity of those that did
+        bool ok = true;
+        while (ok && walk.next(a.seq, a.deal, s)) {
+            const int e = count % kDescs;
+            if (!(ok = warp_wait(&sh.desc_empty[e], ((count / kDescs) & 1) ^ 1, abort_flag))) break;
+            ChunkSeg g;
+            g.b = s.b, g.q0 = s.s.q0, g.n = s.s.n, g.h = s.h, g.f0 = s.t * a.deal.rows;
+            g.past = s.s.kv - s.s.n, g.k_end = deal_k_end(s.s, a.deal, s.t);
+            const int tok0 = (int)div_by((uint32_t)g.f0, a.deal.by_g);
+            g.first_pos = g.past + tok0;
+            g.u0 = s.u0, g.end = s.u0;
+            g.slot = s.u0 == 0 && s.u1 == s.units ? -1 : 2 * cta + (s.u0 == 0 ? 1 : 0);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                g.rows[h] = max(0, min(p.half_rows, s.s.n * a.deal.g - g.f0 - h * p.half_rows));
+                const int last = min(tok0 + (h + 1) * p.half_tokens, s.s.n) - 1;  // last token of the half
+                const int k_end = max(0, min(g.past + last + 1, s.s.kv));
+                g.stop[h] = g.rows[h] == 0 ? s.u0 : max(s.u0, min(s.u1, (k_end + kKeys - 1) / kKeys));
+                g.end = max(g.end, g.stop[h]);
+            }
+            if (lane == 0) {
+                if (count == 0) {
+                    JoinNote note{0, g.q0, g.n, g.h, g.f0, {0, 0, 0}};
+                    if (s.u0 > 0) {
+                        const int64_t item = start.unit - s.u0;
+                        const int i0 = (int)(item / start.chunk), i1 = (int)((item + s.units - 1) / start.chunk);
+                        if (i0 == cta - 1) note.parts = i1 - i0 + 1;
+                    }
+                    a.notes[cta] = note;
+                }
+                sh.seg[e] = g;
+                for (int i = 0; i < kStrange * 4; ++i) sh.strange[e][i / 4][i % 4] = 0;
+                ptx::mbar_arrive(&sh.desc_full[e]);
+            }
+            __syncwarp();
+            // one tile of keys or values
+            auto load = [&](int u, const CUtensorMap* m, bool special) {
+                const int st = pos % ST;
+                if (!warp_wait(&sh.kv_empty[st], ((pos / ST) & 1) ^ 1, abort_flag)) return false;
+                ++pos;
+                raw = special ? raw | 1u << st : raw & ~(1u << st);
+                raw_turn ^= (uint32_t)special << st;
+                uint64_t* const bar = special ? &sh.raw_full[st] : &sh.kv_full[st];
+                const int key0 = u * kKeys, pieces = min(kKeys / p.box, (g.k_end - key0 + p.box - 1) / p.box);
+                if (lane == 0) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(pieces * p.box * D * 2));
+                __syncwarp();
+                if (lane < pieces) {
+                    int within = 0;
+                    const int id = page_of(a.seq, g.b, key0 + lane * p.box, within);
+                    const int page = id < 0 ? a.seq.pages : id;  // outside the cache: zeros
+                    unsigned char* const dst = ring + st * TILE + lane * p.box * 128;
+#pragma unroll
+                    for (int c = 0; c < CG; ++c) ptx::tma_load_4d(dst + c * kKeys * 128, m, bar, c * 64, within, g.h, page);
+                }
+                __syncwarp();
+                return true;
+            };
+            auto special = [&](int u) { return u * kKeys + kKeys - 1 > g.first_pos; };
+            if (g.end > g.u0) ok = load(g.u0, &maps.k, false);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (!ok || g.stop[h] <= g.u0) continue;
+                if (!(ok = warp_wait(&sh.q_empty[h], (q_uses[h] & 1) ^ 1, abort_flag))) continue;
+                ++q_uses[h];
+                if (lane == 0) {
+                    ptx::mbar_arrive_expect_tx(&sh.q_full[h], (uint32_t)(p.half_rows * D * 2));
+#pragma unroll
+                    for (int c = 0; c < CG; ++c)
+                        ptx::tma_load_3d(q_smem + h * QH + c * kHalf * 128, &maps.q, &sh.q_full[h], c * 64, g.h * a.deal.g, g.q0 + tok0 + h * p.half_tokens);
+                }
+                __syncwarp();
+            }
+            for (int u = g.u0; ok && u < g.end; ++u) {
+                ok = load(u, &maps.v, special(u));
+                if (ok && u + 1 < g.end) ok = load(u + 1, &maps.k, false);
+            }
+            ++count;
+        }
+        if (lane == 0) {
+            if (count == 0 && ok) a.notes[cta].parts = 0;
+            if (!ok) {
+                chunk_timeout(a.status, 1);
+                // copies in flight write to this CTA's shared memory: wait for them, with a limit
+                for (uint32_t q = pos > ST ? pos - ST : 0; q < pos; ++q) {
+                    const int st = q % ST;
+                    for (int i = 0; i < 4096; ++i) {
+                        if ((raw >> st) & 1 ? ptx::mbar_test_wait(&sh.raw_full[st], ((raw_turn >> st) & 1) ^ 1) : ptx::mbar_test_wait(&sh.kv_full[st], (q / ST) & 1)) break;
+                        __nanosleep(100);
+                    }
+                }
+            } else {
+                // an empty description ends the others' loops
+                const int e = count % kDescs;
+                if (ptx::mbar_wait_spin(&sh.desc_empty[e], ((count / kDescs) & 1) ^ 1, abort_flag)) {
+                    sh.seg[e].b = -1;
+                    ptx::mbar_arrive(&sh.desc_full[e]);
+                } else chunk_timeout(a.status, 2);
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        // ------------------------------------------------------------------ products
+        if (lane == 0) {
+            constexpr uint32_t s_idesc = ptx::idesc_bf16_f32(128, kKeys), o_idesc = ptx::idesc_bf16_f32_bmn(128, D);
+            const uint32_t q_at = ptx::smem_u32(q_smem), ring_at = ptx::smem_u32(ring);
+            uint32_t pos = 0;  // of the segment's first key tile
+            int q_uses[2] = {0, 0}, p_uses[2] = {0, 0};
+            bool ok = true;
+            auto full = [&](uint32_t at) { return ptx::mbar_wait_spin(&sh.kv_full[at % ST], (at / ST) & 1, abort_flag); };
+            auto scores = [&](int h, uint32_t k_pos) {
+                const uint64_t qd = ptx::smem_desc_sw128_kmajor(q_at + h * QH), kd = ptx::smem_desc_sw128_kmajor(ring_at + (k_pos % ST) * TILE);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint64_t off = (uint64_t)(((k / 4) * kHalf * 128 + (k % 4) * 32) >> 4);
+                    ptx::umma_bf16(tmem + h * 128, qd + off, kd + off, s_idesc, k > 0);
+                }
+                ptx::umma_commit(&sh.s_full[h]);
+            };
+            auto values = [&](int h, uint32_t v_pos, bool add) {
+                const uint64_t vd = ptx::smem_desc_sw128_mnmajor(ring_at + (v_pos % ST) * TILE, kKeys * 128);
+#pragma unroll
+                for (int k = 0; k < kKeys / 16; ++k)
+                    ptx::umma_bf16_ta(tmem + 256 + h * D, tmem + h * 128 + k * 8, vd + (uint64_t)((k * 2048) >> 4), o_idesc, add || k > 0);
+            };
+            for (int count = 0; ok; ++count) {
+                const int e = count % kDescs;
+                if (!(ok = ptx::mbar_wait_spin(&sh.desc_full[e], (count / kDescs) & 1, abort_flag))) break;
+                if (sh.seg[e].b < 0) break;
+                const int u0 = sh.seg[e].u0, end = sh.seg[e].end;
+                const int stop[2] = {sh.seg[e].stop[0], sh.seg[e].stop[1]};
+                if (end > u0) {
+                    // tile i of the segment: keys at pos + 2 i, values at pos + 2 i + 1, except that the order of loading puts the next
+                    // keys behind the values
+                    ok = full(pos);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if (ok && stop[h] > u0) {
+                            if (!(ok = ptx::mbar_wait_spin(&sh.q_full[h], q_uses[h] & 1, abort_flag))) continue;
+                            ++q_uses[h];
+                            ptx::tc_fence_after();
+                            scores(h, pos);
+                            if (stop[h] == u0 + 1) ptx::umma_commit(&sh.q_empty[h]);
+                        }
+                    if (!ok) break;
+                    ptx::umma_commit(&sh.kv_empty[pos % ST]);
+                    for (int u = u0; ok && u < end; ++u) {
+                        const uint32_t v_pos = pos + 2 * (u - u0) + 1, k_pos = v_pos + 1;
+                        bool have_v = false, have_k = false;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (!ok || u >= stop[h]) continue;
+                            if (!(ok = ptx::mbar_wait_spin(&sh.p_full[h], p_uses[h] & 1, abort_flag))) continue;
+                            ++p_uses[h];
+                            if (!have_v && !(ok = full(v_pos))) continue;
+                            have_v = true;
+                            ptx::tc_fence_after();
+                            values(h, v_pos, u > u0);
+                            if (u == stop[h] - 1) ptx::umma_commit(&sh.o_full[h]);
+                            else {
+                                if (!have_k && !(ok = full(k_pos))) continue;
+                                have_k = true;
+                                ptx::tc_fence_after();
+                                scores(h, k_pos);
+                                if (u + 1 == stop[h] - 1) ptx::umma_commit(&sh.q_empty[h]);
+                            }
+                        }
+                        if (!ok) break;
+                        ptx::umma_commit(&sh.kv_empty[v_pos % ST]);
+                        if (u + 1 < end) ptx::umma_commit(&sh.kv_empty[k_pos % ST]);
+                    }
+                    pos += 2 * (end - u0);
+                }
+                if (ok) ptx::mbar_arrive(&sh.desc_empty[e]);
+            }
+            if (!ok) chunk_timeout(a.status, 3);
+        }
+    } else if (warp == kFixWarp) {
+        // ------------------------------------------------------------------ repairs of value tiles
+        uint32_t pos = 0, raw_turn = 0;  // parity of the next repaired tile of each stage
+        bool ok = true;
+        for (int count = 0; ok; ++count) {
+            const int e = count % kDescs;
+            if (!(ok = warp_wait(&sh.desc_full[e], (count / kDescs) & 1, abort_flag))) break;
+            const ChunkSeg g = sh.seg[e];
+            if (g.b < 0) break;
+            const int us = max(g.u0, (max(g.first_pos, -1) + 1) / kKeys);  // first tile that reaches past the first row's last key
+            for (int u = us; ok && u < g.end; ++u) {
+                const uint32_t at = pos + 2 * (u - g.u0) + 1;
+                const int st = at % ST;
+                if (!(ok = warp_wait(&sh.raw_full[st], (raw_turn >> st) & 1, abort_flag))) break;
+                raw_turn ^= 1u << st;
+                unsigned char* const tile = ring + st * TILE;
+                const int key0 = u * kKeys, valid = min(kKeys, g.k_end - key0);
+                for (int i = lane; i < (kKeys - valid) * CG * 8; i += 32) {
+                    const int r = valid + i / (CG * 8), c = i % (CG * 8);
+                    *reinterpret_cast<uint4*>(tile + (c / 8) * kKeys * 128 + r * 128 + (c % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                const int lo = max(0, g.first_pos + 1 - key0);
+                for (int i = lane; i < (valid - lo) * CG * 8; i += 32) {
+                    const int r = lo + i / (CG * 8), c = i % (CG * 8);
+                    uint4* const at4 = reinterpret_cast<uint4*>(tile + (c / 8) * kKeys * 128 + r * 128 + (c % 8) * 16);
+                    uint32_t x[4] = {at4->x, at4->y, at4->z, at4->w};
+                    if (strange_pair(x[0]) || strange_pair(x[1]) || strange_pair(x[2]) || strange_pair(x[3])) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if ((x[j] & 0x7F80u) == 0x7F80u) x[j] &= 0xFFFF0000u;
+                            if ((x[j] & 0x7F800000u) == 0x7F800000u) x[j] &= 0xFFFFu;
+                        }
+                        *at4 = make_uint4(x[0], x[1], x[2], x[3]);
+                        if (u - us < kStrange) atomicOr(&sh.strange[e][u - us][r >> 5], 1u << (r & 31));
+                    }
+                }
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sh.kv_full[st]);
+            }
+            pos += 2 * (g.end - g.u0);
+            __syncwarp();
+            if (ok && lane == 0) {
+                ptx::mbar_arrive(&sh.strange_full[e]);
+                ptx::mbar_arrive(&sh.desc_empty[e]);
+            }
+        }
+        if (!ok && lane == 0) chunk_timeout(a.status, 4);
+    } else if (warp < kMmaWarp) {
+        // ------------------------------------------------------------------ softmax: a row per thread
+        const int h = warp >> 2, row = tid & 127;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_at = tmem + lanes + h * 128, o_at = tmem + lanes + 256 + h * D;
+        uint32_t s_uses = 0, o_uses = 0;
+        bool ok = true;
+        for (int count = 0; ok; ++count) {
+            const int e = count % kDescs;
+            if (!(ok = warp_wait(&sh.desc_full[e], (count / kDescs) & 1, abort_flag))) break;
+            const ChunkSeg& g = sh.seg[e];
+            if (g.b < 0) break;
+            const int u0 = g.u0, stop = g.stop[h], rows = g.rows[h];
+            const int f = g.f0 + h * p.half_rows + min(row, max(rows - 1, 0)), tok = (int)div_by((uint32_t)f, a.deal.by_g), pos = g.past + tok;
+            float ref = -kInf;             // reference of the weights, in the exponent of 2
+            uint64_t sum2 = 0, sum3 = 0;   // sums of the weights, in four parts
+            for (int u = u0; u < stop; ++u) {
+                if (!(ok = warp_wait(&sh.s_full[h], s_uses & 1, abort_flag))) break;
+                ++s_uses;
+                ptx::tc_fence_after();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ptx::tmem_ld_32x32(s_at + i * 32, s[i]);
+                ptx::tmem_ld_wait();
+                const int seen = pos - u * kKeys;  // columns up to here
+                if (__any_sync(~0u, seen < kKeys - 1)) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i > seen) s[i / 32][i % 32] = __float_as_uint(-kInf);
+                }
+                float top[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    top[i] = __uint_as_float(s[i][0]);
+#pragma unroll
+                    for (int j = 1; j + 1 < 32; j += 2) top[i] = fmaxf(fmaxf(top[i], __uint_as_float(s[i][j])), __uint_as_float(s[i][j + 1]));
+                    top[i] = fmaxf(top[i], __uint_as_float(s[i][31]));
+                }
+                const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.c;
+                if (u == u0) ref = m;
+                else {
+                    const bool grown = m > ref + kGrowth;
+                    if (__any_sync(~0u, grown)) {  // the products before this tile's scores are done: O is this warp's
+                        const float w = grown ? ex2(ref - m) : 1.0f;
+                        if (grown) ref = m;
+                        const uint64_t w2 = pair(w, w);
+                        sum2 = mul2(sum2, w2), sum3 = mul2(sum3, w2);
+#pragma unroll 1
+                        for (int i = 0; i < D / 32; ++i) {
+                            uint32_t o[32];
+                            ptx::tmem_ld_32x32(o_at + i * 32, o);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * w);
+                            ptx::tmem_st_32x32(o_at + i * 32, o);
+                        }
+                    }
+                }
+                const float r = ref == -kInf ? 0.0f : -ref;
+                const uint64_t c2 = pair(a.c, a.c), r2 = pair(r, r);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        float x, y;
+                        unpair(fma2(pair(__uint_as_float(s[i][j]), __uint_as_float(s[i][j + 1])), c2, r2), x, y);
+                        x = ex2(x), y = ex2(y);
+                        if (j & 2) sum3 = add2(sum3, pair(x, y));
+                        else sum2 = add2(sum2, pair(x, y));
+                        w[j / 2] = pack_bf16(x, y);
+                    }
+                    ptx::tmem_st_32x16(s_at + i * 16, w);
+                }
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sh.p_full[h]);
+            }
+            if (!ok) break;
+            const bool some = stop > u0;
+            if (some) {
+                if (!(ok = warp_wait(&sh.o_full[h], o_uses & 1, abort_flag))) break;
+                ++o_uses;
+                ptx::tc_fence_after();
+            }
+            if (!(ok = warp_wait(&sh.strange_full[e], (count / kDescs) & 1, abort_flag))) break;
+            float sum;
+            {
+                float x, y, z, w;
+                unpair(sum2, x, y), unpair(sum3, z, w);
+                sum = (x + y) + (z + w);
+            }
+            const int slot = g.slot, head = g.h * a.deal.g + (f - tok * a.deal.g);
+            const int64_t out_row = g.q0 + tok, at = (int64_t)max(slot, 0) * a.deal.rows + h * p.half_rows + row;
+            const float inv = slot < 0 ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
+            const int us = max(u0, (max(g.first_pos, -1) + 1) / kKeys);
+            uint32_t any = 0;
+#pragma unroll
+            for (int i = 0; i < kStrange * 4; ++i) any |= sh.strange[e][i / 4][i % 4];
+#pragma unroll 1
+            for (int i = 0; i < D / 32; ++i) {
+                uint32_t o[32];
+                if (some) {
+                    ptx::tmem_ld_32x32(o_at + i * 32, o);
+                    ptx::tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) o[j] = 0;
+                }
+                if (row < rows) {
+                    float v[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(o[j]) * inv;
+                    if (any && some) {  // rare: infinities and NaN of the keys that this row sees
+                        for (int w = 0; w < kStrange * 4; ++w)
+                            for (uint32_t bits = sh.strange[e][w / 4][w % 4]; bits; bits &= bits - 1) {
+                                const int key = (us + w / 4) * kKeys + (w % 4) * 32 + __ffs(bits) - 1;
+                                int within = 0;
+                                const int page = key <= pos ? page_of(a.seq, g.b, key, within) : -1;
+                                if (page < 0) continue;
+                                const __nv_bfloat16* src = a.v + (int64_t)page * a.v_page + (int64_t)within * a.v_row + (int64_t)g.h * a.v_head + i * 32;
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) {
+                                    const float x = __bfloat162float(src[j]);
+                                    if (!(fabsf(x) < kInf)) v[j] += x;
+                                }
+                            }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        float x[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) x[k] = v[j + k];
+                        if (slot < 0) store8(a.out + out_row * a.ldo + head * D + i * 32 + j, x, 8);
+                        else store8(a.part_o + at * D + i * 32 + j, x, 8);
+                    }
+                }
+                __syncwarp();
+            }
+            if (row < rows) {
+                if (slot >= 0) a.part_ml[at] = make_float2(ref, sum);
+                else if (a.lse) a.lse[out_row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
+            }
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&sh.desc_empty[e]);
+        }
+        if (!ok && lane == 0) chunk_timeout(a.status, 5);
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) ptx::tmem_dealloc(tmem, 512);
+    pdl_trigger();
+}
+
+}  // namespace
+
+bool attn_chunk_supported(const AttnArgs& a) {
+    auto ok = [](int64_t stride, int64_t extent) { return extent == 1 || stride > 0; };
+    return ok(a.k_row, a.seq.page) && ok(a.v_row, a.seq.page) && ok(a.k_head, a.deal.Hkv) && ok(a.v_head, a.deal.Hkv) && ok(a.k_page, a.seq.pages) &&
+           ok(a.v_page, a.seq.pages) && (a.seq.T == 1 || a.ldq > 0);
+}
+
+int attn_chunk_rows(int g) { return 2 * (kHalf / g) * g; }
+
+int launch_attn_chunk(const AttnArgs& args, int D, int ctas, cudaStream_t stream) {
+    ChunkArgs p;
+    p.a = args;
+    const int g = args.deal.g;
+    p.half_tokens = kHalf / g;
+    p.half_rows = p.half_tokens * g;
+    p.box = 8;
+    while (p.box < kKeys && args.seq.page % (2 * p.box) == 0) p.box *= 2;
+    ChunkMaps maps;
+    const uint64_t d = (uint64_t)D;
+    auto stride = [](int64_t s, int64_t extent) { return extent == 1 ? (uint64_t)16 : (uint64_t)s * 2; };  // of a single one: any
+    {
+        const uint64_t dims[3] = {d, (uint64_t)args.Hq, (uint64_t)args.seq.T}, strides[2] = {d * 2, args.seq.T == 1 ? d * 2 * args.Hq : (uint64_t)args.ldq * 2};
+        const uint32_t box[3] = {64, (uint32_t)g, (uint32_t)p.half_tokens};
+        int rc = make_tmap_bf16(&maps.q, args.q, 3, dims, strides, box);
+        if (rc) return rc;
+    }
+    const uint64_t dims[4] = {d, (uint64_t)args.seq.page, (uint64_t)args.deal.Hkv, (uint64_t)args.seq.pages};
+    const uint32_t box[4] = {64, (uint32_t)p.box, 1, 1};
+    const uint64_t ks[3] = {stride(args.k_row, args.seq.page), stride(args.k_head, args.deal.Hkv), stride(args.k_page, args.seq.pages)};
+    const uint64_t vs[3] = {stride(args.v_row, args.seq.page), stride(args.v_head, args.deal.Hkv), stride(args.v_page, args.seq.pages)};
+    int rc = make_tmap_bf16(&maps.k, args.k, 4, dims, ks, box);
+    if (rc) return rc;
+    rc = make_tmap_bf16(&maps.v, args.v, 4, dims, vs, box);
+    if (rc) return rc;
+    auto kern = D == 128 ? attn_chunk_kernel<128> : attn_chunk_kernel<64>;
+    const int smem = 1024 + 2 * kHalf * D * 2 + (D == 128 ? stages<128>() * tile_bytes<128>() : stages<64>() * tile_bytes<64>()) + (int)sizeof(ChunkShared);
+    rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem, "attn_chunk_kernel shared memory");
+    if (rc) return rc;
+    LaunchScope scope(kKindRow, stream);
+    return cuda_fail(launch_kernel(kern, dim3((unsigned)ctas), dim3(kThreads), (size_t)smem, stream, p, maps), "attn_chunk_kernel launch");
+}
+
+}  // namespace resq
