@@ -48,6 +48,7 @@ inline SeqArgs seq_args(const resq_paged_cache& c, const resq_sequences& s, int6
 // How attention is dealt out (below): rows and keys per tile, heads.
 struct Deal {
     int rows, keys, Hkv, g;
+    int extra;  // what an item costs besides its keys, in units
     FastDiv by_g;
 };
 // Where partial results lie: a CTA's first segment, when its item began in an earlier CTA, in slot 2 * cta; one whose item goes on
@@ -77,7 +78,7 @@ struct AttnArgs {
 
 // paged_chunk.cu: the tensor-core form for chunks of new tokens.  Rows of its tiles for g query heads per kv head, whether it takes
 // these strides, and its launch (args.deal.rows and .keys as it wants them).
-constexpr int kChunkKeys = 128;
+constexpr int kChunkKeys = 128, kChunkExtra = 3;
 int attn_chunk_rows(int g);
 bool attn_chunk_supported(const AttnArgs& args);
 int launch_attn_chunk(const AttnArgs& args, int D, int ctas, cudaStream_t stream);
@@ -104,8 +105,8 @@ __device__ __forceinline__ int page_of(const SeqArgs& a, int b, int j, int& with
 
 // ---- how attention is dealt out ------------------------------------------------------------------------------------------------
 // The queries of a sequence that share a kv head are rows f = token * g + head, cut into tiles of `rows`; an item is one tile, and
-// its units are tiles of `keys` keys up to the last one that its last token sees (one at least: an item without keys still
-// writes its rows).  Items are ordered by sequence, kv head, tile; all units in this order are cut into equal ranges, one per CTA,
+// its units are `extra` ones for its beginning and end, then tiles of `keys` keys up to the last one that its last token sees (one
+// at least: an item without keys still writes its rows).  Items are ordered by sequence, kv head, tile; all units in this order are cut into equal ranges, one per CTA,
 // so that ragged lengths need no plan from the host and a captured call follows the lengths on the device.  A CTA's first item may
 // have begun in an earlier CTA and its last one may go on in a later one: those are left as partial results.
 __device__ __forceinline__ int deal_tiles(const Seq& s, const Deal& d) { return (int)(((int64_t)s.n * d.g + d.rows - 1) / d.rows); }
@@ -114,7 +115,7 @@ __device__ __forceinline__ int deal_k_end(const Seq& s, const Deal& d, int t) { 
     const int last = (int)div_by((uint32_t)f, d.by_g);
     return max(0, min(s.kv - s.n + last + 1, s.kv));
 }
-__device__ __forceinline__ int deal_units(const Seq& s, const Deal& d, int t) { return max(1, (deal_k_end(s, d, t) + d.keys - 1) / d.keys); }
+__device__ __forceinline__ int deal_units(const Seq& s, const Deal& d, int t) { return max(1, (deal_k_end(s, d, t) + d.keys - 1) / d.keys) + d.extra; }
 
 // Where a CTA's range begins, and how long it is.
 struct DealStart {
@@ -200,6 +201,7 @@ __device__ __forceinline__ DealStart deal_start(const SeqArgs& a, const Deal& d,
 struct Segment {
     int b, h, t;        // sequence, kv head, tile
     int u0, u1, units;  // units u0 .. u1 - 1 of the item's `units`
+    int k0, k1;         // their tiles of keys, k0 .. k1 - 1
     Seq s;
 };
 // Walks a CTA's range item by item; one warp at a time, all lanes alike.
@@ -256,6 +258,7 @@ struct DealWalk {
         out.u0 = u;
         out.u1 = (int)min((int64_t)out.units, u + left);
         left -= out.u1 - u;
+        out.k0 = max(out.u0 - d.extra, 0), out.k1 = max(out.u1 - d.extra, 0);
         u = 0;
         ++t;
         return true;

@@ -125,9 +125,9 @@ __global__ void __launch_bounds__(kWarps * 32, kRowsCtasPerSm) attn_rows_kernel(
                 pos[mt][i] = past + (int)div_by((uint32_t)(f0 + min(mt * 16 + i * 8 + lane / 4, rows - 1)), d.by_g);
         const int first_pos = past + (int)div_by((uint32_t)f0, d.by_g);  // keys up to here are seen by all rows
 
-        const int key_first = seg.u0 * kKeys + w * kWarpKeys;
+        const int key_first = seg.k0 * kKeys + w * kWarpKeys;
         // tiles of this warp that hold a key
-        const int tiles = min(seg.u1 - seg.u0, max(0, (k_end - key_first + kKeys - 1) / kKeys));
+        const int tiles = min(seg.k1 - seg.k0, max(0, (k_end - key_first + kKeys - 1) / kKeys));
         auto issue = [&](int i) {
             if (i < tiles) {
                 const int key0 = key_first + i * kKeys;
@@ -454,7 +454,7 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
     using bf = __nv_bfloat16;
     AttnArgs a;
     a.seq = seq_args(*cache, *seqs, T);
-    a.deal = Deal{l.rows, ch.chunk ? kChunkKeys : kKeys, (int)Hkv, (int)(Hq / Hkv), fast_div((uint32_t)(Hq / Hkv))};
+    a.deal = Deal{l.rows, ch.chunk ? kChunkKeys : kKeys, (int)Hkv, (int)(Hq / Hkv), ch.chunk ? env_int("RESQ_ATTN_EXTRA", kChunkExtra) : 0, fast_div((uint32_t)(Hq / Hkv))};
     a.q = static_cast<const bf*>(Q), a.k = static_cast<const bf*>(cache->k), a.v = static_cast<const bf*>(cache->v);
     a.ldq = ldq, a.ldo = ldo;
     a.k_page = cache->k_page, a.k_row = cache->k_row, a.k_head = cache->k_head;
@@ -463,7 +463,7 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
     if (ch.chunk && !attn_chunk_supported(a)) {  // a stride of 0: no tensor map takes it; this workspace is smaller
         ch = Choice{false, 32, kPlanSms * kRowsCtasPerSm};
         l = layout(D, ch.rows, ch.ctas);
-        a.deal.rows = ch.rows, a.deal.keys = kKeys;
+        a.deal.rows = ch.rows, a.deal.keys = kKeys, a.deal.extra = 0;
     }
     a.status = reinterpret_cast<DeviceStatus*>(ws);
     a.notes = reinterpret_cast<JoinNote*>(ws + kWsHeader);

@@ -17,16 +17,20 @@
 #include "paged.cuh"
 #include "ptx.cuh"
 
+
 namespace resq {
 namespace {
 
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kKeys = kChunkKeys, kHalf = 128;
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kFixWarp = 10, kThreads = 384;
+constexpr int kMmaWarp = 8, kLoadWarp = 10, kFixWarp = 11, kThreads = 384;  // products: warps 8 and 9
 constexpr int kDescs = 4;    // segments described ahead of the slowest reader
 constexpr int kStrange = 4;  // key tiles of a segment that can hold keys of its own tokens (at most 256)
-constexpr float kGrowth = 8.0f;
+constexpr float kGrowth = 20.0f;
+// Registers per thread: 168 at the launch; the eight softmax warps take what the other four give up.
+constexpr int kSoftmaxRegs = 200, kOtherRegs = 104;
+static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * 168, "");
 
 template <int D>
 constexpr int stages() { return D == 128 ? 5 : 10; }  // 160 KB of key and value tiles
@@ -49,7 +53,7 @@ struct ChunkSeg {
 };
 struct ChunkShared {
     uint64_t desc_full[kDescs], desc_empty[kDescs], strange_full[kDescs];
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2];
     uint64_t kv_full[10], kv_empty[10], raw_full[10];
     ChunkSeg seg[kDescs];
     uint32_t strange[kDescs][kStrange][4];  // a bit per key whose value row holds an infinity or NaN
@@ -59,12 +63,15 @@ struct ChunkShared {
     int abort;
 };
 
+static_assert(2 * kHalf * 128 * 2 + stages<128>() * tile_bytes<128>() + sizeof(ChunkShared) <= 232448, "227 KB");
+
 __device__ __forceinline__ void chunk_timeout(DeviceStatus* st, int where) {
     st->where = where;
     st->block = (int)blockIdx.x;
     st->code = RESQ_ERR_TIMEOUT;
 }
-// A wait of all lanes with one answer for them all: lanes that gave up apart would part the warp.
+// A wait of all lanes with one answer for them all: lanes that gave up apart would part the warp.  It does not let the warp sleep:
+// every role's answer is on the way of the next product.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
     return __all_sync(~0u, ptx::mbar_wait_spin(bar, parity, abort_flag));
 }
@@ -73,13 +80,30 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {  // NaN if one of them is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+template <int N>
+__device__ __forceinline__ void more_registers() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void fewer_registers() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
 __device__ __forceinline__ bool strange_pair(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_constant__ ChunkArgs p, const __grid_constant__ ChunkMaps maps) {
     constexpr int ST = stages<D>(), TILE = tile_bytes<D>(), CG = D / 64, QH = kHalf * D * 2;  // column groups of 64
-    extern __shared__ unsigned char raw_smem[];
-    unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char* const q_smem = smem;                // [half][column group][128 rows][128 bytes]
     unsigned char* const ring = smem + 2 * QH;         // [stage][column group][128 keys][128 bytes]
     ChunkShared& sh = *reinterpret_cast<ChunkShared*>(ring + ST * TILE);
@@ -90,19 +114,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
     if (tid == 0) {
         for (int i = 0; i < kDescs; ++i) {
             ptx::mbar_init(&sh.desc_full[i], 1);
-            ptx::mbar_init(&sh.desc_empty[i], 10);  // eight softmax warps, products, repairs
+            ptx::mbar_init(&sh.desc_empty[i], 11);  // eight softmax warps, products of two halves, repairs
             ptx::mbar_init(&sh.strange_full[i], 1);
         }
         for (int h = 0; h < 2; ++h) {
             ptx::mbar_init(&sh.q_full[h], 1);
             ptx::mbar_init(&sh.q_empty[h], 1);
             ptx::mbar_init(&sh.s_full[h], 1);
-            ptx::mbar_init(&sh.p_full[h], 4);
+            ptx::mbar_init(&sh.p_full[h][0], 4);  // the weights of the first 64 keys, of the others
+            ptx::mbar_init(&sh.p_full[h][1], 4);
             ptx::mbar_init(&sh.o_full[h], 1);
         }
         for (int i = 0; i < ST; ++i) {
             ptx::mbar_init(&sh.kv_full[i], 1);
-            ptx::mbar_init(&sh.kv_empty[i], 1);
+            ptx::mbar_init(&sh.kv_empty[i], 2);  // the products of both halves
             ptx::mbar_init(&sh.raw_full[i], 1);
         }
         ptx::mbar_fence_init();
@@ -121,6 +146,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
     ptx::tc_fence_after();
     const uint32_t tmem = sh.tmem;
 
+    // (The four warps of a group change their registers together, before they part.)
+    if (warp >= kMmaWarp) {
+    fewer_registers<kOtherRegs>();
     if (warp == kLoadWarp) {
         // ------------------------------------------------------------------ segments, queries, keys and values
         DealWalk walk;
@@ -138,14 +166,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             g.past = s.s.kv - s.s.n, g.k_end = deal_k_end(s.s, a.deal, s.t);
             const int tok0 = (int)div_by((uint32_t)g.f0, a.deal.by_g);
             g.first_pos = g.past + tok0;
-            g.u0 = s.u0, g.end = s.u0;
+            g.u0 = s.k0, g.end = s.k0;
             g.slot = s.u0 == 0 && s.u1 == s.units ? -1 : 2 * cta + (s.u0 == 0 ? 1 : 0);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 g.rows[h] = max(0, min(p.half_rows, s.s.n * a.deal.g - g.f0 - h * p.half_rows));
                 const int last = min(tok0 + (h + 1) * p.half_tokens, s.s.n) - 1;  // last token of the half
                 const int k_end = max(0, min(g.past + last + 1, s.s.kv));
-                g.stop[h] = g.rows[h] == 0 ? s.u0 : max(s.u0, min(s.u1, (k_end + kKeys - 1) / kKeys));
+                g.stop[h] = g.rows[h] == 0 ? s.k0 : max(s.k0, min(s.k1, (k_end + kKeys - 1) / kKeys));
                 g.end = max(g.end, g.stop[h]);
             }
             if (lane == 0) {
@@ -163,6 +191,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 ptx::mbar_arrive(&sh.desc_full[e]);
             }
             __syncwarp();
+            // where this lane's piece of key tile u lies; asked for a tile ahead, since the answer takes as long as a copy
+            int page = 0, within = 0, next_page = 0, next_within = 0;
+            auto look = [&](int u) {
+                const int key = u * kKeys + lane * p.box;
+                if (lane * p.box < kKeys && key < g.k_end) {
+                    next_page = page_of(a.seq, g.b, key, next_within);
+                    if (next_page < 0) next_page = a.seq.pages;  // outside the cache: zeros
+                }
+            };
             // one tile of keys or values
             auto load = [&](int u, const CUtensorMap* m, bool special) {
                 const int st = pos % ST;
@@ -171,13 +208,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 raw = special ? raw | 1u << st : raw & ~(1u << st);
                 raw_turn ^= (uint32_t)special << st;
                 uint64_t* const bar = special ? &sh.raw_full[st] : &sh.kv_full[st];
-                const int key0 = u * kKeys, pieces = min(kKeys / p.box, (g.k_end - key0 + p.box - 1) / p.box);
+                const int pieces = min(kKeys / p.box, (g.k_end - u * kKeys + p.box - 1) / p.box);
                 if (lane == 0) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(pieces * p.box * D * 2));
                 __syncwarp();
                 if (lane < pieces) {
-                    int within = 0;
-                    const int id = page_of(a.seq, g.b, key0 + lane * p.box, within);
-                    const int page = id < 0 ? a.seq.pages : id;  // outside the cache: zeros
                     unsigned char* const dst = ring + st * TILE + lane * p.box * 128;
 #pragma unroll
                     for (int c = 0; c < CG; ++c) ptx::tma_load_4d(dst + c * kKeys * 128, m, bar, c * 64, within, g.h, page);
@@ -186,7 +220,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 return true;
             };
             auto special = [&](int u) { return u * kKeys + kKeys - 1 > g.first_pos; };
-            if (g.end > g.u0) ok = load(g.u0, &maps.k, false);
+            if (g.end > g.u0) {
+                look(g.u0);
+                page = next_page, within = next_within;
+                look(g.u0 + 1);
+                ok = load(g.u0, &maps.k, false);
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (!ok || g.stop[h] <= g.u0) continue;
@@ -202,7 +241,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             }
             for (int u = g.u0; ok && u < g.end; ++u) {
                 ok = load(u, &maps.v, special(u));
-                if (ok && u + 1 < g.end) ok = load(u + 1, &maps.k, false);
+                if (!ok || u + 1 == g.end) continue;
+                page = next_page, within = next_within;
+                look(u + 2);
+                ok = load(u + 1, &maps.k, false);
             }
             ++count;
         }
@@ -227,78 +269,80 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 } else chunk_timeout(a.status, 2);
             }
         }
-    } else if (warp == kMmaWarp) {
-        // ------------------------------------------------------------------ products
+    } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+        // ------------------------------------------------------------------ products of a half
+        // Few products are taken ahead of their execution: a thread that waits leaves the tensor cores idle unless another one has
+        // products for them.  So each half has a thread of its own.
         if (lane == 0) {
+            const int h = warp - kMmaWarp;
             constexpr uint32_t s_idesc = ptx::idesc_bf16_f32(128, kKeys), o_idesc = ptx::idesc_bf16_f32_bmn(128, D);
-            const uint32_t q_at = ptx::smem_u32(q_smem), ring_at = ptx::smem_u32(ring);
-            uint32_t pos = 0;  // of the segment's first key tile
-            int q_uses[2] = {0, 0}, p_uses[2] = {0, 0};
+            const uint64_t q_desc = ptx::smem_desc_sw128_kmajor(ptx::smem_u32(q_smem) + h * QH);
+            const uint64_t k_desc = ptx::smem_desc_sw128_kmajor(ptx::smem_u32(ring)), v_desc = ptx::smem_desc_sw128_mnmajor(ptx::smem_u32(ring), kKeys * 128);
+            const uint32_t s_at = tmem + h * 128, o_at = tmem + 256 + h * D;
+            uint32_t pos = 0;  // of the segment's first key tile; tile i's values are at pos + 2 i + 1, tile i + 1's keys behind them
+            uint32_t q_uses = 0, p_uses = 0;
             bool ok = true;
-            auto full = [&](uint32_t at) { return ptx::mbar_wait_spin(&sh.kv_full[at % ST], (at / ST) & 1, abort_flag); };
-            auto scores = [&](int h, uint32_t k_pos) {
-                const uint64_t qd = ptx::smem_desc_sw128_kmajor(q_at + h * QH), kd = ptx::smem_desc_sw128_kmajor(ring_at + (k_pos % ST) * TILE);
+            auto wait = [&](uint64_t* bar, uint32_t parity) { return ptx::mbar_wait_spin(bar, parity, abort_flag); };
+            auto full = [&](uint32_t at) { return wait(&sh.kv_full[at % ST], (at / ST) & 1); };
+            auto scores = [&](uint32_t k_pos) {
+                const uint64_t kd = k_desc + (uint64_t)((k_pos % ST) * (TILE >> 4));
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint64_t off = (uint64_t)(((k / 4) * kHalf * 128 + (k % 4) * 32) >> 4);
-                    ptx::umma_bf16(tmem + h * 128, qd + off, kd + off, s_idesc, k > 0);
+                    ptx::umma_bf16(s_at, q_desc + off, kd + off, s_idesc, k > 0);
                 }
                 ptx::umma_commit(&sh.s_full[h]);
             };
-            auto values = [&](int h, uint32_t v_pos, bool add) {
-                const uint64_t vd = ptx::smem_desc_sw128_mnmajor(ring_at + (v_pos % ST) * TILE, kKeys * 128);
+            auto values = [&](uint32_t v_pos, int part, bool add) {  // keys 64 part .. + 63 of the tile
+                const uint64_t vd = v_desc + (uint64_t)((v_pos % ST) * (TILE >> 4));
 #pragma unroll
-                for (int k = 0; k < kKeys / 16; ++k)
-                    ptx::umma_bf16_ta(tmem + 256 + h * D, tmem + h * 128 + k * 8, vd + (uint64_t)((k * 2048) >> 4), o_idesc, add || k > 0);
+                for (int k = part * 4; k < part * 4 + 4; ++k)
+                    ptx::umma_bf16_ta(o_at, s_at + k * 8, vd + (uint64_t)((k * 2048) >> 4), o_idesc, add || k > part * 4);
+            };
+            // a tile this half has no use for: given back once it is there (before, the arrival could count for the buffer's turn before)
+            auto skip = [&](uint32_t at) {
+                if (!full(at)) return false;
+                ptx::mbar_arrive(&sh.kv_empty[at % ST]);
+                return true;
             };
             for (int count = 0; ok; ++count) {
                 const int e = count % kDescs;
-                if (!(ok = ptx::mbar_wait_spin(&sh.desc_full[e], (count / kDescs) & 1, abort_flag))) break;
+                if (!(ok = wait(&sh.desc_full[e], (count / kDescs) & 1))) break;
                 if (sh.seg[e].b < 0) break;
-                const int u0 = sh.seg[e].u0, end = sh.seg[e].end;
-                const int stop[2] = {sh.seg[e].stop[0], sh.seg[e].stop[1]};
-                if (end > u0) {
-                    // tile i of the segment: keys at pos + 2 i, values at pos + 2 i + 1, except that the order of loading puts the next
-                    // keys behind the values
-                    ok = full(pos);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        if (ok && stop[h] > u0) {
-                            if (!(ok = ptx::mbar_wait_spin(&sh.q_full[h], q_uses[h] & 1, abort_flag))) continue;
-                            ++q_uses[h];
-                            ptx::tc_fence_after();
-                            scores(h, pos);
-                            if (stop[h] == u0 + 1) ptx::umma_commit(&sh.q_empty[h]);
-                        }
-                    if (!ok) break;
+                const int tiles = sh.seg[e].end - sh.seg[e].u0, mine = sh.seg[e].stop[h] - sh.seg[e].u0;
+                if (mine > 0) {
+                    if (!(ok = full(pos) && wait(&sh.q_full[h], q_uses & 1))) break;
+                    ++q_uses;
+                    ptx::tc_fence_after();
+                    scores(pos);
+                    if (mine == 1) ptx::umma_commit(&sh.q_empty[h]);
                     ptx::umma_commit(&sh.kv_empty[pos % ST]);
-                    for (int u = u0; ok && u < end; ++u) {
-                        const uint32_t v_pos = pos + 2 * (u - u0) + 1, k_pos = v_pos + 1;
-                        bool have_v = false, have_k = false;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            if (!ok || u >= stop[h]) continue;
-                            if (!(ok = ptx::mbar_wait_spin(&sh.p_full[h], p_uses[h] & 1, abort_flag))) continue;
-                            ++p_uses[h];
-                            if (!have_v && !(ok = full(v_pos))) continue;
-                            have_v = true;
-                            ptx::tc_fence_after();
-                            values(h, v_pos, u > u0);
-                            if (u == stop[h] - 1) ptx::umma_commit(&sh.o_full[h]);
-                            else {
-                                if (!have_k && !(ok = full(k_pos))) continue;
-                                have_k = true;
-                                ptx::tc_fence_after();
-                                scores(h, k_pos);
-                                if (u + 1 == stop[h] - 1) ptx::umma_commit(&sh.q_empty[h]);
-                            }
-                        }
-                        if (!ok) break;
+                } else if (tiles > 0 && !(ok = skip(pos))) break;
+                for (int i = 0; ok && i < mine; ++i) {
+                    const uint32_t v_pos = pos + 2 * i + 1, k_pos = v_pos + 1;
+                    // the tiles first: they are there by then, and asking costs time that the weights would wait for
+                    if (!(ok = full(v_pos) && (i + 1 == mine || full(k_pos)))) break;
+                    if (!(ok = wait(&sh.p_full[h][0], p_uses & 1))) break;
+                    ptx::tc_fence_after();
+                    values(v_pos, 0, i > 0);
+                    if (!(ok = wait(&sh.p_full[h][1], p_uses & 1))) break;
+                    ++p_uses;
+                    ptx::tc_fence_after();
+                    values(v_pos, 1, true);
+                    if (i + 1 < mine) {
+                        scores(k_pos);
+                        if (i + 2 == mine) ptx::umma_commit(&sh.q_empty[h]);
                         ptx::umma_commit(&sh.kv_empty[v_pos % ST]);
-                        if (u + 1 < end) ptx::umma_commit(&sh.kv_empty[k_pos % ST]);
+                        ptx::umma_commit(&sh.kv_empty[k_pos % ST]);
+                    } else {
+                        ptx::umma_commit(&sh.o_full[h]);
+                        ptx::umma_commit(&sh.kv_empty[v_pos % ST]);
+                        if (i + 1 < tiles) ok = skip(k_pos);
                     }
-                    pos += 2 * (end - u0);
                 }
+                // (the keys of the first tile left over were given back above)
+                for (int i = max(mine, 0); ok && i < tiles; ++i) ok = skip(pos + 2 * i + 1) && (i + 1 == tiles || skip(pos + 2 * i + 2));
+                pos += 2 * tiles;
                 if (ok) ptx::mbar_arrive(&sh.desc_empty[e]);
             }
             if (!ok) chunk_timeout(a.status, 3);
@@ -325,19 +369,27 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     *reinterpret_cast<uint4*>(tile + (c / 8) * kKeys * 128 + r * 128 + (c % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
                 const int lo = max(0, g.first_pos + 1 - key0);
-                for (int i = lane; i < (valid - lo) * CG * 8; i += 32) {
-                    const int r = lo + i / (CG * 8), c = i % (CG * 8);
-                    uint4* const at4 = reinterpret_cast<uint4*>(tile + (c / 8) * kKeys * 128 + r * 128 + (c % 8) * 16);
-                    uint32_t x[4] = {at4->x, at4->y, at4->z, at4->w};
-                    if (strange_pair(x[0]) || strange_pair(x[1]) || strange_pair(x[2]) || strange_pair(x[3])) {
+                const int chunks = (valid - lo) * CG * 8;
+                for (int base = lane; base < chunks; base += 32 * 8) {
+                    uint4 x[8];
+                    auto place = [&](int n) {
+                        const int i = base + n * 32, r = lo + i / (CG * 8), c = i % (CG * 8);
+                        return reinterpret_cast<uint4*>(tile + (c / 8) * kKeys * 128 + r * 128 + (c % 8) * 16);
+                    };
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if ((x[j] & 0x7F80u) == 0x7F80u) x[j] &= 0xFFFF0000u;
-                            if ((x[j] & 0x7F800000u) == 0x7F800000u) x[j] &= 0xFFFFu;
+                    for (int n = 0; n < 8; ++n) x[n] = base + n * 32 < chunks ? *place(n) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                    for (int n = 0; n < 8; ++n)
+                        if (strange_pair(x[n].x) || strange_pair(x[n].y) || strange_pair(x[n].z) || strange_pair(x[n].w)) {
+                            const int r = lo + (base + n * 32) / (CG * 8);
+                            auto clean = [](uint32_t v) {
+                                if ((v & 0x7F80u) == 0x7F80u) v &= 0xFFFF0000u;
+                                if ((v & 0x7F800000u) == 0x7F800000u) v &= 0xFFFFu;
+                                return v;
+                            };
+                            *place(n) = make_uint4(clean(x[n].x), clean(x[n].y), clean(x[n].z), clean(x[n].w));
+                            if (u - us < kStrange) atomicOr(&sh.strange[e][u - us][r >> 5], 1u << (r & 31));
                         }
-                        *at4 = make_uint4(x[0], x[1], x[2], x[3]);
-                        if (u - us < kStrange) atomicOr(&sh.strange[e][u - us][r >> 5], 1u << (r & 31));
-                    }
                 }
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
@@ -351,7 +403,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             }
         }
         if (!ok && lane == 0) chunk_timeout(a.status, 4);
-    } else if (warp < kMmaWarp) {
+    }
+    } else {
+        more_registers<kSoftmaxRegs>();
         // ------------------------------------------------------------------ softmax: a row per thread
         const int h = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_at = tmem + lanes + h * 128, o_at = tmem + lanes + 256 + h * D;
@@ -383,51 +437,66 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 float top[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    top[i] = __uint_as_float(s[i][0]);
+                    top[i] = max3(__uint_as_float(s[i][0]), __uint_as_float(s[i][1]), __uint_as_float(s[i][2]));
 #pragma unroll
-                    for (int j = 1; j + 1 < 32; j += 2) top[i] = fmaxf(fmaxf(top[i], __uint_as_float(s[i][j])), __uint_as_float(s[i][j + 1]));
-                    top[i] = fmaxf(top[i], __uint_as_float(s[i][31]));
+                    for (int j = 3; j + 1 < 32; j += 2) top[i] = max3(top[i], __uint_as_float(s[i][j]), __uint_as_float(s[i][j + 1]));
+                    top[i] = max_nan(top[i], __uint_as_float(s[i][31]));
                 }
-                const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.c;
+                // a score of NaN or +inf makes the row NaN by way of its reference
+                float m = max3(max_nan(top[0], top[1]), top[2], top[3]) * a.c;
+                if (m == kInf) m = __int_as_float(0x7FFFFFFF);
                 if (u == u0) ref = m;
-                else {
-                    const bool grown = m > ref + kGrowth;
-                    if (__any_sync(~0u, grown)) {  // the products before this tile's scores are done: O is this warp's
-                        const float w = grown ? ex2(ref - m) : 1.0f;
-                        if (grown) ref = m;
-                        const uint64_t w2 = pair(w, w);
-                        sum2 = mul2(sum2, w2), sum3 = mul2(sum3, w2);
-#pragma unroll 1
-                        for (int i = 0; i < D / 32; ++i) {
-                            uint32_t o[32];
-                            ptx::tmem_ld_32x32(o_at + i * 32, o);
-                            ptx::tmem_ld_wait();
+                bool again = false;
+                auto weights = [&](int part, uint32_t (&w)[32], uint64_t& a2, uint64_t& b2) {  // of keys 64 part .. + 63, and their sums
+                    const float r = ref == -kInf ? 0.0f : -ref;
+                    const uint64_t c2 = pair(a.c, a.c), r2 = pair(r, r);
+                    a2 = b2 = 0;
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * w);
-                            ptx::tmem_st_32x32(o_at + i * 32, o);
-                        }
-                    }
-                }
-                const float r = ref == -kInf ? 0.0f : -ref;
-                const uint64_t c2 = pair(a.c, a.c), r2 = pair(r, r);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
+                    for (int i = 0; i < 64; i += 2) {
+                        const uint32_t* const v = &s[part * 2 + i / 32][i % 32];
                         float x, y;
-                        unpair(fma2(pair(__uint_as_float(s[i][j]), __uint_as_float(s[i][j + 1])), c2, r2), x, y);
+                        unpair(fma2(pair(__uint_as_float(v[0]), __uint_as_float(v[1])), c2, r2), x, y);
                         x = ex2(x), y = ex2(y);
-                        if (j & 2) sum3 = add2(sum3, pair(x, y));
-                        else sum2 = add2(sum2, pair(x, y));
-                        w[j / 2] = pack_bf16(x, y);
+                        if (i & 2) b2 = add2(b2, pair(x, y));
+                        else a2 = add2(a2, pair(x, y));
+                        w[i / 2] = pack_bf16(x, y);
                     }
-                    ptx::tmem_st_32x16(s_at + i * 16, w);
+                };
+                auto deliver = [&](int part, const uint32_t (&w)[32]) {
+                    ptx::tmem_st_32x32(s_at + part * 32, w);
+                    ptx::tmem_st_wait();
+                    ptx::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sh.p_full[h][part]);
+                };
+                uint32_t w[32];
+                uint64_t a2, b2;
+                // The weights by the reference as it is; the maximum is wanted only to see that it will do, and comes meanwhile.
+                for (;;) {
+                    weights(0, w, a2, b2);
+                    const bool grown = row < rows && !(m <= ref + kGrowth) && !again;  // (rows behind the last hold anything)
+                    if (!__any_sync(~0u, grown)) break;
+                    // the products before this tile's scores are done: O is this warp's
+                    const float f2 = grown ? ex2(ref - m) : 1.0f;
+                    if (grown) ref = m;
+                    again = true;  // (a reference of NaN stays below nothing)
+                    sum2 = mul2(sum2, pair(f2, f2)), sum3 = mul2(sum3, pair(f2, f2));
+                    if (u == u0) continue;
+#pragma unroll 1
+                    for (int i = 0; i < D / 16; ++i) {
+                        uint32_t o[16];
+                        ptx::tmem_ld_32x16(o_at + i * 16, o);
+                        ptx::tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f2);
+                        ptx::tmem_st_32x16(o_at + i * 16, o);
+                    }
                 }
-                ptx::tmem_st_wait();
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&sh.p_full[h]);
+                sum2 = add2(sum2, a2), sum3 = add2(sum3, b2);
+                deliver(0, w);
+                weights(1, w, a2, b2);
+                sum2 = add2(sum2, a2), sum3 = add2(sum3, b2);
+                deliver(1, w);
             }
             if (!ok) break;
             const bool some = stop > u0;
@@ -460,7 +529,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
 #pragma unroll
                     for (int j = 0; j < 32; ++j) o[j] = 0;
                 }
-                if (row < rows) {
+                if (row < rows && (some || slot < 0)) {
+                    const int col = i * 32;
                     float v[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(o[j]) * inv;
@@ -471,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                                 int within = 0;
                                 const int page = key <= pos ? page_of(a.seq, g.b, key, within) : -1;
                                 if (page < 0) continue;
-                                const __nv_bfloat16* src = a.v + (int64_t)page * a.v_page + (int64_t)within * a.v_row + (int64_t)g.h * a.v_head + i * 32;
+                                const __nv_bfloat16* src = a.v + (int64_t)page * a.v_page + (int64_t)within * a.v_row + (int64_t)g.h * a.v_head + col;
 #pragma unroll
                                 for (int j = 0; j < 32; ++j) {
                                     const float x = __bfloat162float(src[j]);
@@ -484,8 +554,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                         float x[8];
 #pragma unroll
                         for (int k = 0; k < 8; ++k) x[k] = v[j + k];
-                        if (slot < 0) store8(a.out + out_row * a.ldo + head * D + i * 32 + j, x, 8);
-                        else store8(a.part_o + at * D + i * 32 + j, x, 8);
+                        if (slot < 0) store8(a.out + out_row * a.ldo + head * D + col + j, x, 8);
+                        else store8(a.part_o + at * D + col + j, x, 8);
                     }
                 }
                 __syncwarp();
@@ -542,7 +612,7 @@ int launch_attn_chunk(const AttnArgs& args, int D, int ctas, cudaStream_t stream
     rc = make_tmap_bf16(&maps.v, args.v, 4, dims, vs, box);
     if (rc) return rc;
     auto kern = D == 128 ? attn_chunk_kernel<128> : attn_chunk_kernel<64>;
-    const int smem = 1024 + 2 * kHalf * D * 2 + (D == 128 ? stages<128>() * tile_bytes<128>() : stages<64>() * tile_bytes<64>()) + (int)sizeof(ChunkShared);
+    const int smem = 2 * kHalf * D * 2 + (D == 128 ? stages<128>() * tile_bytes<128>() : stages<64>() * tile_bytes<64>()) + (int)sizeof(ChunkShared);
     rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem, "attn_chunk_kernel shared memory");
     if (rc) return rc;
     LaunchScope scope(kKindRow, stream);
