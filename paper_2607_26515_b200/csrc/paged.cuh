@@ -70,7 +70,7 @@ struct AttnArgs {
     int Hq;
     float c;          // scale log2(e)
     int min_chunk;
-    float* part_o;    // [2 ctas][rows][D], unnormalised
+    float* part_o;    // [2 ctas][rows][D] (attn_chunk_kernel: [2 ctas][D][rows]), unnormalised
     float2* part_ml;  // [2 ctas][rows]: reference, sum
     JoinNote* notes;  // [ctas]
     DeviceStatus* status;

@@ -349,49 +349,131 @@ __global__ void __launch_bounds__(kWarps * 32, kRowsCtasPerSm) attn_rows_kernel(
     pdl_trigger();
 }
 
-// Joins the parts of the items that were cut: block (i, y) those of the item whose second CTA is i, rows 8 y .. 8 y + 7, a warp per
-// row, parts in the order of the keys.
+// What the parts of an item weigh: by lane, parts `lane`, `lane` + 32, ... of row r; the largest reference is the same in all lanes.
+__device__ __forceinline__ int64_t join_slot(int cta, int p, int R, int r) { return (int64_t)(p == 0 ? 2 * (cta - 1) + 1 : 2 * (cta - 1 + p)) * R + r; }
+__device__ __forceinline__ float join_weight(float2 q, float ref) {  // (a sum without a reference is one of NaN scores)
+    return q.x == -kInf ? (q.y == 0.0f ? 0.0f : 1.0f) : ex2(q.x - ref);
+}
+__device__ __forceinline__ void join_place(const AttnArgs& a, const JoinNote& note, int f, int64_t& row, int& head) {
+    const int tok = (int)div_by((uint32_t)f, a.deal.by_g);
+    head = note.h * a.deal.g + (f - tok * a.deal.g);
+    row = note.q0 + tok;
+}
+
+// Joins the parts of the items that attn_rows_kernel had to cut, in a fixed order: block (i, y) those of the item whose second CTA
+// is i, its rows y, y + grid.y, ...  The eight warps share a row's parts (a long sequence by itself is cut into as many as the
+// device has CTAs), with eight loads of a warp in flight.
 template <int D>
 __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnArgs a) {
-    constexpr int E = D / 32;
-    const int lane = threadIdx.x & 31, cta = blockIdx.x;
+    constexpr int E = D / 32, W = 8, kDeep = 8;
+    __shared__ float2 warp_ml[W];
+    __shared__ float warp_o[W][D];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, cta = blockIdx.x;
     pdl_wait();
     pdl_trigger();
     const JoinNote note = a.notes[cta];
-    const int r = blockIdx.y * 8 + (threadIdx.x >> 5), R = a.deal.rows, f = note.f0 + r;
+    if (note.parts == 0) return;
+    const int R = a.deal.rows, rows = min(R, note.n * a.deal.g - note.f0);
+    const int per = (note.parts + W - 1) / W, p0 = min(w * per, note.parts), p1 = min(p0 + per, note.parts);
+    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+        float ref = -kInf, sum = 0.0f, acc[E] = {};
+        for (int p = p0 + lane; p < p1; p += 32) ref = fmaxf(ref, a.part_ml[join_slot(cta, p, R, r)].x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(~0u, ref, o));
+        for (int b = p0; b < p1; b += kDeep) {
+            float2 q[kDeep];
+            float x[kDeep][E];
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                q[i] = make_float2(-kInf, 0.0f);
+                if (b + i >= p1) continue;
+                const int64_t at = join_slot(cta, b + i, R, r);
+                q[i] = a.part_ml[at];
+                if (E == 4) {
+                    const float4 v = *reinterpret_cast<const float4*>(a.part_o + at * D + lane * E);
+                    x[i][0] = v.x, x[i][1] = v.y, x[i][2 % E] = v.z, x[i][3 % E] = v.w;
+                } else {
+                    const float2 v = *reinterpret_cast<const float2*>(a.part_o + at * D + lane * E);
+                    x[i][0] = v.x, x[i][1] = v.y;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                const float f = join_weight(q[i], ref);
+                if (f == 0.0f) continue;
+                sum = fmaf(f, q[i].y, sum);
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = fmaf(f, x[i][e], acc[e]);
+            }
+        }
+        if (lane == 0) warp_ml[w] = make_float2(ref, sum);
+#pragma unroll
+        for (int e = 0; e < E; ++e) warp_o[w][lane * E + e] = acc[e];
+        __syncthreads();
+        if (w == 0) {
+            ref = -kInf;
+#pragma unroll
+            for (int i = 0; i < W; ++i) ref = fmaxf(ref, warp_ml[i].x);
+            sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float f = join_weight(warp_ml[i], ref);
+                if (f == 0.0f) continue;
+                sum = fmaf(f, warp_ml[i].y, sum);
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = fmaf(f, warp_o[i][lane * E + e], acc[e]);
+            }
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            int64_t row;
+            int head;
+            join_place(a, note, note.f0 + r, row, head);
+            uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * a.ldo + head * D + lane * E);
+#pragma unroll
+            for (int e = 0; e < E; e += 2) dst[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+            if (a.lse && lane == 0) a.lse[row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
+        }
+        __syncthreads();
+    }
+}
+
+// The same for attn_chunk_kernel, whose parts lie with the rows of a column side by side: block (i, y) rows 32 y .. + 31 of the item,
+// a row per lane, 16 columns per warp.
+template <int D>
+__global__ void __launch_bounds__(D * 2) attn_join_tiles_kernel(const __grid_constant__ AttnArgs a) {
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, cta = blockIdx.x;
+    pdl_wait();
+    pdl_trigger();
+    const JoinNote note = a.notes[cta];
+    const int R = a.deal.rows, r = blockIdx.y * 32 + lane, f = note.f0 + r;
     if (note.parts == 0 || r >= R || f >= note.n * a.deal.g) return;
-    auto slot = [&](int p) { return ((int64_t)(p == 0 ? 2 * (cta - 1) + 1 : 2 * (cta - 1 + p)) * R + r); };
-    float ref = -kInf;
-    for (int p = lane; p < note.parts; p += 32) ref = fmaxf(ref, a.part_ml[slot(p)].x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(~0u, ref, o));
-    float acc[E] = {}, sum = 0.0f;
-#pragma unroll 4
+    float ref = -kInf, sum = 0.0f, acc[16] = {};
+    for (int p = 0; p < note.parts; ++p) ref = fmaxf(ref, a.part_ml[join_slot(cta, p, R, r)].x);
     for (int p = 0; p < note.parts; ++p) {
-        const float2 q = a.part_ml[slot(p)];
-        float x[E];
-        const float* src = a.part_o + slot(p) * D + lane * E;
-        if (E == 4) {
-            const float4 v = *reinterpret_cast<const float4*>(src);
-            x[0] = v.x, x[1] = v.y, x[2 % E] = v.z, x[3 % E] = v.w;
-        } else {
-            const float2 v = *reinterpret_cast<const float2*>(src);
-            x[0] = v.x, x[1] = v.y;
-        }
-        const float w = q.x == -kInf ? (q.y == 0.0f ? 0.0f : 1.0f) : ex2(q.x - ref);
-        if (w != 0.0f) {
-            sum = fmaf(w, q.y, sum);
+        const int64_t at = join_slot(cta, p, R, r);
+        const float2 q = a.part_ml[at];
+        const float* const src = a.part_o + ((at - r) / R * D + w * 16) * R + r;
+        float x[16];
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = fmaf(w, x[e], acc[e]);
-        }
+        for (int i = 0; i < 16; ++i) x[i] = src[i * R];
+        const float weight = join_weight(q, ref);
+        if (weight == 0.0f) continue;
+        sum = fmaf(weight, q.y, sum);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] = fmaf(weight, x[i], acc[i]);
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const int tok = (int)div_by((uint32_t)f, a.deal.by_g), head = note.h * a.deal.g + (f - tok * a.deal.g);
-    const int64_t row = note.q0 + tok;
-    uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * a.ldo + head * D + lane * E);
+    int64_t row;
+    int head;
+    join_place(a, note, f, row, head);
 #pragma unroll
-    for (int e = 0; e < E; e += 2) dst[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
-    if (a.lse && lane == 0) a.lse[row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
+    for (int i = 0; i < 16; ++i) acc[i] *= inv;
+    const float lo[8] = {acc[0], acc[1], acc[2], acc[3], acc[4], acc[5], acc[6], acc[7]}, hi[8] = {acc[8], acc[9], acc[10], acc[11], acc[12], acc[13], acc[14], acc[15]};
+    __nv_bfloat16* const dst = a.out + row * a.ldo + head * D + w * 16;
+    store8(dst, lo, 8);
+    store8(dst + 8, hi, 8);
+    if (a.lse && w == 0) a.lse[row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
 }
 
 // Workspace: notes, then the partial sums of two slots per CTA.
@@ -470,14 +552,13 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
     a.part_ml = reinterpret_cast<float2*>(ws + l.ml);
     a.part_o = reinterpret_cast<float*>(ws + l.o);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    auto join = [&] {
-        LaunchScope scope(kKindRow, st);
-        return cuda_fail(launch_kernel(D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>, dim3((unsigned)l.ctas, (unsigned)((l.rows + 7) / 8)), dim3(256), 0, st, a),
-                         "attn_join_kernel launch");
-    };
     if (ch.chunk) {
         rc = launch_attn_chunk(a, (int)D, l.ctas, st);
-        return rc ? rc : join();
+        if (rc) return rc;
+        LaunchScope scope(kKindRow, st);
+        return cuda_fail(launch_kernel(D == 128 ? attn_join_tiles_kernel<128> : attn_join_tiles_kernel<64>, dim3((unsigned)l.ctas, (unsigned)((l.rows + 31) / 32)),
+                                       dim3((unsigned)(2 * D)), 0, st, a),
+                         "attn_join_tiles_kernel launch");
     }
     auto kern = D == 128 ? (l.rows == 16 ? attn_rows_kernel<128, 1> : attn_rows_kernel<128, 2>)
                          : (l.rows == 16 ? attn_rows_kernel<64, 1> : attn_rows_kernel<64, 2>);
@@ -489,7 +570,9 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
         rc = cuda_fail(launch_kernel(kern, dim3((unsigned)l.ctas), dim3(kWarps * 32), (size_t)smem, st, a), "attn_rows_kernel launch");
         if (rc) return rc;
     }
-    return join();
+    LaunchScope scope(kKindRow, st);
+    return cuda_fail(launch_kernel(D == 128 ? attn_join_kernel<128> : attn_join_kernel<64>, dim3((unsigned)l.ctas, 8), dim3(256), 0, st, a),
+                     "attn_join_kernel launch");
 }
 
 }  // extern "C"

@@ -44,18 +44,21 @@ struct ChunkArgs {
     AttnArgs a;
     int half_rows, half_tokens;  // of a half tile
     int box;                     // keys per copy: a power of two that divides the page and the tile
+    int wide;                    // rows of the output start on 32-byte boundaries
 };
 
 struct ChunkSeg {
     int b, q0, n, h, f0, past, k_end, first_pos;
     int u0, end, slot;           // key tiles u0 .. end - 1 are to be read; slot: of the partial result, -1: the whole item
     int rows[2], stop[2];        // per half: rows, key tiles u0 .. stop - 1
+    int split;                   // rows for one half only: both work on them, on every second key tile each
 };
 struct ChunkShared {
     uint64_t desc_full[kDescs], desc_empty[kDescs], strange_full[kDescs];
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], merge_full, merge_free;
     uint64_t kv_full[10], kv_empty[10], raw_full[10];
     ChunkSeg seg[kDescs];
+    float2 other[kHalf];                    // of a split segment's second half: reference and sum of each row
     uint32_t strange[kDescs][kStrange][4];  // a bit per key whose value row holds an infinity or NaN
     int64_t sums[kThreads / 32];
     DealStart found;
@@ -119,12 +122,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         }
         for (int h = 0; h < 2; ++h) {
             ptx::mbar_init(&sh.q_full[h], 1);
-            ptx::mbar_init(&sh.q_empty[h], 1);
+            ptx::mbar_init(&sh.q_empty[h], h == 0 ? 2 : 1);  // the first half's queries: the products of both halves
             ptx::mbar_init(&sh.s_full[h], 1);
             ptx::mbar_init(&sh.p_full[h][0], 4);  // the weights of the first 64 keys, of the others
             ptx::mbar_init(&sh.p_full[h][1], 4);
             ptx::mbar_init(&sh.o_full[h], 1);
         }
+        ptx::mbar_init(&sh.merge_full, 4);
+        ptx::mbar_init(&sh.merge_free, 4);
         for (int i = 0; i < ST; ++i) {
             ptx::mbar_init(&sh.kv_full[i], 1);
             ptx::mbar_init(&sh.kv_empty[i], 2);  // the products of both halves
@@ -176,6 +181,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 g.stop[h] = g.rows[h] == 0 ? s.k0 : max(s.k0, min(s.k1, (k_end + kKeys - 1) / kKeys));
                 g.end = max(g.end, g.stop[h]);
             }
+            g.split = g.rows[1] == 0;
+            if (g.split) g.stop[1] = g.stop[0];
             if (lane == 0) {
                 if (count == 0) {
                     JoinNote note{0, g.q0, g.n, g.h, g.f0, {0, 0, 0}};
@@ -231,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 if (!ok || g.stop[h] <= g.u0) continue;
                 if (!(ok = warp_wait(&sh.q_empty[h], (q_uses[h] & 1) ^ 1, abort_flag))) continue;
                 ++q_uses[h];
-                if (lane == 0) {
+                if (lane == 0 && (h == 0 || !g.split)) {  // (a split segment's second half has no queries, but uses their room at its end)
                     ptx::mbar_arrive_expect_tx(&sh.q_full[h], (uint32_t)(p.half_rows * D * 2));
 #pragma unroll
                     for (int c = 0; c < CG; ++c)
@@ -276,15 +283,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         if (lane == 0) {
             const int h = warp - kMmaWarp;
             constexpr uint32_t s_idesc = ptx::idesc_bf16_f32(128, kKeys), o_idesc = ptx::idesc_bf16_f32_bmn(128, D);
-            const uint64_t q_desc = ptx::smem_desc_sw128_kmajor(ptx::smem_u32(q_smem) + h * QH);
+            const uint64_t q_desc = ptx::smem_desc_sw128_kmajor(ptx::smem_u32(q_smem));
             const uint64_t k_desc = ptx::smem_desc_sw128_kmajor(ptx::smem_u32(ring)), v_desc = ptx::smem_desc_sw128_mnmajor(ptx::smem_u32(ring), kKeys * 128);
             const uint32_t s_at = tmem + h * 128, o_at = tmem + 256 + h * D;
             uint32_t pos = 0;  // of the segment's first key tile; tile i's values are at pos + 2 i + 1, tile i + 1's keys behind them
-            uint32_t q_uses = 0, p_uses = 0;
+            uint32_t q_uses[2] = {0, 0}, p_uses = 0;
             bool ok = true;
             auto wait = [&](uint64_t* bar, uint32_t parity) { return ptx::mbar_wait_spin(bar, parity, abort_flag); };
             auto full = [&](uint32_t at) { return wait(&sh.kv_full[at % ST], (at / ST) & 1); };
-            auto scores = [&](uint32_t k_pos) {
+            auto scores = [&](uint64_t q_desc, uint32_t k_pos) {
                 const uint64_t kd = k_desc + (uint64_t)((k_pos % ST) * (TILE >> 4));
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
@@ -299,49 +306,73 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 for (int k = part * 4; k < part * 4 + 4; ++k)
                     ptx::umma_bf16_ta(o_at, s_at + k * 8, vd + (uint64_t)((k * 2048) >> 4), o_idesc, add || k > part * 4);
             };
-            // a tile this half has no use for: given back once it is there (before, the arrival could count for the buffer's turn before)
-            auto skip = [&](uint32_t at) {
-                if (!full(at)) return false;
-                ptx::mbar_arrive(&sh.kv_empty[at % ST]);
+            // tiles this half has no use for: given back once they are there (before, the arrival could count for the buffer's turn before)
+            auto skip = [&](uint32_t from, uint32_t to) {
+                for (; from < to; ++from) {
+                    if (!full(from)) return false;
+                    ptx::mbar_arrive(&sh.kv_empty[from % ST]);
+                }
                 return true;
             };
             for (int count = 0; ok; ++count) {
                 const int e = count % kDescs;
                 if (!(ok = wait(&sh.desc_full[e], (count / kDescs) & 1))) break;
                 if (sh.seg[e].b < 0) break;
-                const int tiles = sh.seg[e].end - sh.seg[e].u0, mine = sh.seg[e].stop[h] - sh.seg[e].u0;
-                if (mine > 0) {
-                    if (!(ok = full(pos) && wait(&sh.q_full[h], q_uses & 1))) break;
-                    ++q_uses;
+                const int u0 = sh.seg[e].u0, tiles = sh.seg[e].end - u0, split = sh.seg[e].split;
+                const int step = split ? 2 : 1, first = split ? h : 0, end = sh.seg[e].stop[h] - u0;  // tiles first, first + step .. below end
+                const int from = split ? 0 : h;                                                        // whose queries
+                const uint64_t qd = q_desc + (uint64_t)(from * (QH >> 4));
+                // the other half's queries, and room that is not used
+                if (h == 1 && (!split || first >= end) && sh.seg[e].stop[0] > u0) {
+                    if (!(ok = wait(&sh.q_full[0], q_uses[0] & 1))) break;
+                    ptx::mbar_arrive(&sh.q_empty[0]);
+                    if (split) ptx::mbar_arrive(&sh.q_empty[1]);
+                }
+                uint32_t done = pos;  // tiles up to here are given back, or will be when the products with them are done
+                if (first < end) {
+                    const uint32_t at = pos + 2 * first;
+                    if (!(ok = skip(done, at) && full(at) && wait(&sh.q_full[from], q_uses[from] & 1))) break;
                     ptx::tc_fence_after();
-                    scores(pos);
-                    if (mine == 1) ptx::umma_commit(&sh.q_empty[h]);
-                    ptx::umma_commit(&sh.kv_empty[pos % ST]);
-                } else if (tiles > 0 && !(ok = skip(pos))) break;
-                for (int i = 0; ok && i < mine; ++i) {
-                    const uint32_t v_pos = pos + 2 * i + 1, k_pos = v_pos + 1;
-                    // the tiles first: they are there by then, and asking costs time that the weights would wait for
-                    if (!(ok = full(v_pos) && (i + 1 == mine || full(k_pos)))) break;
+                    scores(qd, at);
+                    if (first + step >= end) ptx::umma_commit(&sh.q_empty[from]);
+                    ptx::umma_commit(&sh.kv_empty[at % ST]);
+                    done = at + 1;
+                }
+                for (int i = first; ok && i < end; i += step) {
+                    const uint32_t v_pos = pos + 2 * i + 1, k_pos = v_pos + 2 * step - 1;
+                    const bool more = i + step < end;
+                    // The tiles first: they are there by then, and asking costs time that the weights would wait for.  (The next keys of a
+                    // split segment are four tiles on, which may have to wait for the room of these values.)
+                    if (!(ok = full(v_pos) && (!more || split || full(k_pos)))) break;
                     if (!(ok = wait(&sh.p_full[h][0], p_uses & 1))) break;
                     ptx::tc_fence_after();
-                    values(v_pos, 0, i > 0);
+                    values(v_pos, 0, i > first);
                     if (!(ok = wait(&sh.p_full[h][1], p_uses & 1))) break;
                     ++p_uses;
                     ptx::tc_fence_after();
                     values(v_pos, 1, true);
-                    if (i + 1 < mine) {
-                        scores(k_pos);
-                        if (i + 2 == mine) ptx::umma_commit(&sh.q_empty[h]);
+                    if (more && !split) {
+                        scores(qd, k_pos);
+                        if (i + 2 * step >= end) ptx::umma_commit(&sh.q_empty[from]);
                         ptx::umma_commit(&sh.kv_empty[v_pos % ST]);
                         ptx::umma_commit(&sh.kv_empty[k_pos % ST]);
-                    } else {
-                        ptx::umma_commit(&sh.o_full[h]);
-                        ptx::umma_commit(&sh.kv_empty[v_pos % ST]);
-                        if (i + 1 < tiles) ok = skip(k_pos);
+                        done = k_pos + 1;
+                        continue;
                     }
+                    if (!more) ptx::umma_commit(&sh.o_full[h]);
+                    ptx::umma_commit(&sh.kv_empty[v_pos % ST]);
+                    done = v_pos + 1;
+                    if (!more) break;
+                    if (!(ok = skip(done, k_pos) && full(k_pos))) break;
+                    ptx::tc_fence_after();
+                    scores(qd, k_pos);
+                    if (i + 2 * step >= end) ptx::umma_commit(&sh.q_empty[from]);
+                    ptx::umma_commit(&sh.kv_empty[k_pos % ST]);
+                    done = k_pos + 1;
                 }
-                // (the keys of the first tile left over were given back above)
-                for (int i = max(mine, 0); ok && i < tiles; ++i) ok = skip(pos + 2 * i + 1) && (i + 1 == tiles || skip(pos + 2 * i + 2));
+                ok = ok && skip(done, pos + 2 * tiles);
+                if (sh.seg[e].stop[0] > u0) ++q_uses[0];
+                if (!split && sh.seg[e].stop[1] > u0) ++q_uses[1];
                 pos += 2 * tiles;
                 if (ok) ptx::mbar_arrive(&sh.desc_empty[e]);
             }
@@ -416,11 +447,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             if (!(ok = warp_wait(&sh.desc_full[e], (count / kDescs) & 1, abort_flag))) break;
             const ChunkSeg& g = sh.seg[e];
             if (g.b < 0) break;
-            const int u0 = g.u0, stop = g.stop[h], rows = g.rows[h];
-            const int f = g.f0 + h * p.half_rows + min(row, max(rows - 1, 0)), tok = (int)div_by((uint32_t)f, a.deal.by_g), pos = g.past + tok;
+            const int split = g.split, u0 = g.u0 + (split ? h : 0), stop = g.stop[h], rows = g.rows[split ? 0 : h], step = split ? 2 : 1;
+            const int half_row = (split ? 0 : h * p.half_rows) + row;  // in the tile
+            const int f = g.f0 + half_row - row + min(row, max(rows - 1, 0)), tok = (int)div_by((uint32_t)f, a.deal.by_g), pos = g.past + tok;
             float ref = -kInf;             // reference of the weights, in the exponent of 2
             uint64_t sum2 = 0, sum3 = 0;   // sums of the weights, in four parts
-            for (int u = u0; u < stop; ++u) {
+            for (int u = u0; u < stop; u += step) {
                 if (!(ok = warp_wait(&sh.s_full[h], s_uses & 1, abort_flag))) break;
                 ++s_uses;
                 ptx::tc_fence_after();
@@ -512,16 +544,60 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 unpair(sum2, x, y), unpair(sum3, z, w);
                 sum = (x + y) + (z + w);
             }
+            // A split segment: the second half's sums go through the room of the second half's queries, half of the columns at a time
+            // ([column][row], a row per thread), and the first half joins them to its own.
+            const bool merge = split && g.u0 + 1 < stop, any_row = (warp & 3) * 32 < rows;  // of the warp
+            float* const room = reinterpret_cast<float*>(q_smem + QH) + row;
+            if (merge && h == 1) {
+                sh.other[row] = make_float2(ref, sum);
+#pragma unroll 1
+                for (int r = 0; r < 2; ++r) {
+#pragma unroll 1
+                    for (int i = 0; any_row && i < D / 64; ++i) {
+                        uint32_t o[32];
+                        ptx::tmem_ld_32x32(o_at + r * (D / 2) + i * 32, o);
+                        ptx::tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) room[(i * 32 + j) * kHalf] = __uint_as_float(o[j]);
+                    }
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sh.merge_full);
+                    if (!(ok = warp_wait(&sh.merge_free, r, abort_flag))) break;
+                }
+                if (!ok) break;
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (warp == 4 && lane == 0) ptx::mbar_arrive(&sh.q_empty[1]);
+            }
+            float f_own = 1.0f, f_other = 0.0f;
+            const bool writes = !split || h == 0;
+            if (merge && h == 0) {
+                if (!(ok = warp_wait(&sh.merge_full, 0, abort_flag))) break;
+                const float2 q = sh.other[row];
+                // (a reference of -inf with a sum that is not 0 is one of NaN scores)
+                const float top = max_nan(ref, q.x);
+                f_own = ref == top || ref == -kInf ? 1.0f : ex2(ref - top), f_other = q.x == top || q.x == -kInf ? 1.0f : ex2(q.x - top);
+                sum = sum * f_own + q.y * f_other;
+                ref = top;
+            }
             const int slot = g.slot, head = g.h * a.deal.g + (f - tok * a.deal.g);
-            const int64_t out_row = g.q0 + tok, at = (int64_t)max(slot, 0) * a.deal.rows + h * p.half_rows + row;
+            const int64_t out_row = g.q0 + tok, at = (int64_t)max(slot, 0) * a.deal.rows + half_row;
             const float inv = slot < 0 ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
-            const int us = max(u0, (max(g.first_pos, -1) + 1) / kKeys);
+            f_own *= inv, f_other *= inv;
+            const int us = max(g.u0, (max(g.first_pos, -1) + 1) / kKeys);
             uint32_t any = 0;
 #pragma unroll
             for (int i = 0; i < kStrange * 4; ++i) any |= sh.strange[e][i / 4][i % 4];
 #pragma unroll 1
-            for (int i = 0; i < D / 32; ++i) {
+            for (int i = 0; writes && i < D / 32; ++i) {
                 uint32_t o[32];
+                if (merge && i == D / 64) {  // on to the second half of the columns
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sh.merge_free);
+                    if (!(ok = warp_wait(&sh.merge_full, 1, abort_flag))) break;
+                }
+                if (!any_row) continue;
                 if (some) {
                     ptx::tmem_ld_32x32(o_at + i * 32, o);
                     ptx::tmem_ld_wait();
@@ -533,7 +609,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     const int col = i * 32;
                     float v[32];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(o[j]) * inv;
+                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(o[j]) * f_own;
+                    if (merge) {
+                        const float* const x = room + (i % (D / 64)) * 32 * kHalf;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(x[j * kHalf], f_other, v[j]);
+                    }
                     if (any && some) {  // rare: infinities and NaN of the keys that this row sees
                         for (int w = 0; w < kStrange * 4; ++w)
                             for (uint32_t bits = sh.strange[e][w / 4][w % 4]; bits; bits &= bits - 1) {
@@ -549,18 +630,33 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                                 }
                             }
                     }
+                    if (slot >= 0) {  // [column][row]: the lanes' rows lie side by side
+                        float* const dst = a.part_o + ((int64_t)slot * D + i * 32) * a.deal.rows + half_row;
 #pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        float x[8];
+                        for (int j = 0; j < 32; ++j) dst[j * a.deal.rows] = v[j];
+                    } else {
+                        __nv_bfloat16* const dst = a.out + out_row * a.ldo + head * D + i * 32;
+                        uint32_t x[16];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) x[k] = v[j + k];
-                        if (slot < 0) store8(a.out + out_row * a.ldo + head * D + col + j, x, 8);
-                        else store8(a.part_o + at * D + col + j, x, 8);
+                        for (int j = 0; j < 16; ++j) x[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+                        if (p.wide) {  // whole sectors
+                            ptx::st_global_v8(dst, x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]);
+                            ptx::st_global_v8(dst + 16, x[8], x[9], x[10], x[11], x[12], x[13], x[14], x[15]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 16; j += 4) reinterpret_cast<uint4*>(dst)[j / 4] = make_uint4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+                        }
                     }
                 }
                 __syncwarp();
             }
-            if (row < rows) {
+            if (!ok) break;
+            if (merge && h == 0) {
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sh.merge_free);
+            }
+            if (writes && row < rows) {
                 if (slot >= 0) a.part_ml[at] = make_float2(ref, sum);
                 else if (a.lse) a.lse[out_row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
             }
@@ -592,6 +688,7 @@ int launch_attn_chunk(const AttnArgs& args, int D, int ctas, cudaStream_t stream
     const int g = args.deal.g;
     p.half_tokens = kHalf / g;
     p.half_rows = p.half_tokens * g;
+    p.wide = reinterpret_cast<uintptr_t>(args.out) % 32 == 0 && args.ldo % 16 == 0;
     p.box = 8;
     while (p.box < kKeys && args.seq.page % (2 * p.box) == 0) p.box *= 2;
     ChunkMaps maps;
