@@ -78,7 +78,7 @@ struct AttnArgs {
 
 // paged_chunk.cu: the tensor-core form for chunks of new tokens.  Rows of its tiles for g query heads per kv head, whether it takes
 // these strides, and its launch (args.deal.rows and .keys as it wants them).
-constexpr int kChunkKeys = 128, kChunkExtra = 3;
+constexpr int kChunkKeys = 128, kChunkExtra = 6;
 int attn_chunk_rows(int g);
 bool attn_chunk_supported(const AttnArgs& args);
 int launch_attn_chunk(const AttnArgs& args, int D, int ctas, cudaStream_t stream);

@@ -360,12 +360,54 @@ __device__ __forceinline__ void join_place(const AttnArgs& a, const JoinNote& no
     row = note.q0 + tok;
 }
 
+// A row's parts p0 .. p1 - 1 by one warp, kDeep loads in flight: reference, sum and this lane's columns.
+template <int D, int E, int kDeep>
+__device__ __forceinline__ void join_parts(const AttnArgs& a, int cta, int p0, int p1, int R, int r, float& ref, float& sum, float (&acc)[E]) {
+    const int lane = threadIdx.x & 31;
+    ref = -kInf, sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+    for (int b = p0; b < p1; b += kDeep) {
+        float2 q[kDeep];
+        float x[kDeep][E];
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            q[i] = make_float2(-kInf, 0.0f);
+            if (b + i >= p1) continue;
+            const int64_t at = join_slot(cta, b + i, R, r);
+            q[i] = a.part_ml[at];
+            if (E == 4) {
+                const float4 v = *reinterpret_cast<const float4*>(a.part_o + at * D + lane * E);
+                x[i][0] = v.x, x[i][1] = v.y, x[i][2 % E] = v.z, x[i][3 % E] = v.w;
+            } else {
+                const float2 v = *reinterpret_cast<const float2*>(a.part_o + at * D + lane * E);
+                x[i][0] = v.x, x[i][1] = v.y;
+            }
+        }
+        float top = ref;
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) top = fmaxf(top, q[i].x);
+        const float f0 = join_weight(make_float2(ref, sum), top);
+        ref = top, sum *= f0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] *= f0;
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            const float f = join_weight(q[i], ref);
+            if (f == 0.0f) continue;
+            sum = fmaf(f, q[i].y, sum);
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(f, x[i][e], acc[e]);
+        }
+    }
+}
+
 // Joins the parts of the items that attn_rows_kernel had to cut, in a fixed order: block (i, y) those of the item whose second CTA
-// is i, its rows y, y + grid.y, ...  The eight warps share a row's parts (a long sequence by itself is cut into as many as the
-// device has CTAs), with eight loads of a warp in flight.
+// is i, rows 8 y .. 8 y + 7, a warp per row.  An item of many parts (a long sequence by itself is cut into as many as the device
+// has CTAs) has its rows one by one, y, y + grid.y, ..., and the eight warps share a row's parts.
 template <int D>
 __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnArgs a) {
-    constexpr int E = D / 32, W = 8, kDeep = 8;
+    constexpr int E = D / 32, W = 8, kDeep = 4;
     __shared__ float2 warp_ml[W];
     __shared__ float warp_o[W][D];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, cta = blockIdx.x;
@@ -374,47 +416,35 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
     const JoinNote note = a.notes[cta];
     if (note.parts == 0) return;
     const int R = a.deal.rows, rows = min(R, note.n * a.deal.g - note.f0);
+    float ref, sum, acc[E];
+    auto write = [&](int r) {
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        int64_t row;
+        int head;
+        join_place(a, note, note.f0 + r, row, head);
+        uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * a.ldo + head * D + lane * E);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) dst[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+        if (a.lse && lane == 0) a.lse[row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
+    };
+    if (note.parts <= 2 * kDeep) {
+        const int r = blockIdx.y * W + w;
+        if (r >= rows) return;
+        join_parts<D, E, kDeep>(a, cta, 0, note.parts, R, r, ref, sum, acc);
+        write(r);
+        return;
+    }
     const int per = (note.parts + W - 1) / W, p0 = min(w * per, note.parts), p1 = min(p0 + per, note.parts);
     for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-        float ref = -kInf, sum = 0.0f, acc[E] = {};
-        for (int p = p0 + lane; p < p1; p += 32) ref = fmaxf(ref, a.part_ml[join_slot(cta, p, R, r)].x);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(~0u, ref, o));
-        for (int b = p0; b < p1; b += kDeep) {
-            float2 q[kDeep];
-            float x[kDeep][E];
-#pragma unroll
-            for (int i = 0; i < kDeep; ++i) {
-                q[i] = make_float2(-kInf, 0.0f);
-                if (b + i >= p1) continue;
-                const int64_t at = join_slot(cta, b + i, R, r);
-                q[i] = a.part_ml[at];
-                if (E == 4) {
-                    const float4 v = *reinterpret_cast<const float4*>(a.part_o + at * D + lane * E);
-                    x[i][0] = v.x, x[i][1] = v.y, x[i][2 % E] = v.z, x[i][3 % E] = v.w;
-                } else {
-                    const float2 v = *reinterpret_cast<const float2*>(a.part_o + at * D + lane * E);
-                    x[i][0] = v.x, x[i][1] = v.y;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kDeep; ++i) {
-                const float f = join_weight(q[i], ref);
-                if (f == 0.0f) continue;
-                sum = fmaf(f, q[i].y, sum);
-#pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] = fmaf(f, x[i][e], acc[e]);
-            }
-        }
+        join_parts<D, E, kDeep>(a, cta, p0, p1, R, r, ref, sum, acc);
         if (lane == 0) warp_ml[w] = make_float2(ref, sum);
 #pragma unroll
         for (int e = 0; e < E; ++e) warp_o[w][lane * E + e] = acc[e];
         __syncthreads();
         if (w == 0) {
-            ref = -kInf;
+            ref = -kInf, sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < W; ++i) ref = fmaxf(ref, warp_ml[i].x);
-            sum = 0.0f;
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[e] = 0.0f;
 #pragma unroll
@@ -425,14 +455,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
 #pragma unroll
                 for (int e = 0; e < E; ++e) acc[e] = fmaf(f, warp_o[i][lane * E + e], acc[e]);
             }
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            int64_t row;
-            int head;
-            join_place(a, note, note.f0 + r, row, head);
-            uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * a.ldo + head * D + lane * E);
-#pragma unroll
-            for (int e = 0; e < E; e += 2) dst[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
-            if (a.lse && lane == 0) a.lse[row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
+            write(r);
         }
         __syncthreads();
     }
@@ -449,19 +472,35 @@ __global__ void __launch_bounds__(D * 2) attn_join_tiles_kernel(const __grid_con
     const int R = a.deal.rows, r = blockIdx.y * 32 + lane, f = note.f0 + r;
     if (note.parts == 0 || r >= R || f >= note.n * a.deal.g) return;
     float ref = -kInf, sum = 0.0f, acc[16] = {};
-    for (int p = 0; p < note.parts; ++p) ref = fmaxf(ref, a.part_ml[join_slot(cta, p, R, r)].x);
-    for (int p = 0; p < note.parts; ++p) {
-        const int64_t at = join_slot(cta, p, R, r);
-        const float2 q = a.part_ml[at];
-        const float* const src = a.part_o + ((at - r) / R * D + w * 16) * R + r;
-        float x[16];
+    constexpr int kDeep = 3;
+    for (int b = 0; b < note.parts; b += kDeep) {
+        float2 q[kDeep];
+        float x[kDeep][16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = src[i * R];
-        const float weight = join_weight(q, ref);
-        if (weight == 0.0f) continue;
-        sum = fmaf(weight, q.y, sum);
+        for (int k = 0; k < kDeep; ++k) {
+            q[k] = make_float2(-kInf, 0.0f);
+            if (b + k >= note.parts) continue;
+            const int64_t at = join_slot(cta, b + k, R, r);
+            q[k] = a.part_ml[at];
+            const float* const src = a.part_o + ((at - r) * D + (int64_t)w * 16 * R) + r;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] = fmaf(weight, x[i], acc[i]);
+            for (int i = 0; i < 16; ++i) x[k][i] = src[i * R];
+        }
+        float top = ref;
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) top = fmaxf(top, q[k].x);
+        const float f0 = join_weight(make_float2(ref, sum), top);
+        ref = top, sum *= f0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] *= f0;
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            const float weight = join_weight(q[k], ref);
+            if (weight == 0.0f) continue;
+            sum = fmaf(weight, q[k].y, sum);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[i] = fmaf(weight, x[k][i], acc[i]);
+        }
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     int64_t row;

@@ -235,10 +235,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (!ok || g.stop[h] <= g.u0) continue;
+                // (a split segment's second half has no queries of its own; where it has keys, its sums use their room at the end)
+                if (!ok || g.stop[h] <= g.u0 + (h == 1 && g.split)) continue;
                 if (!(ok = warp_wait(&sh.q_empty[h], (q_uses[h] & 1) ^ 1, abort_flag))) continue;
                 ++q_uses[h];
-                if (lane == 0 && (h == 0 || !g.split)) {  // (a split segment's second half has no queries, but uses their room at its end)
+                if (lane == 0 && (h == 0 || !g.split)) {
                     ptx::mbar_arrive_expect_tx(&sh.q_full[h], (uint32_t)(p.half_rows * D * 2));
 #pragma unroll
                     for (int c = 0; c < CG; ++c)
@@ -322,11 +323,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 const int step = split ? 2 : 1, first = split ? h : 0, end = sh.seg[e].stop[h] - u0;  // tiles first, first + step .. below end
                 const int from = split ? 0 : h;                                                        // whose queries
                 const uint64_t qd = q_desc + (uint64_t)(from * (QH >> 4));
-                // the other half's queries, and room that is not used
+                // the other half's queries
                 if (h == 1 && (!split || first >= end) && sh.seg[e].stop[0] > u0) {
                     if (!(ok = wait(&sh.q_full[0], q_uses[0] & 1))) break;
                     ptx::mbar_arrive(&sh.q_empty[0]);
-                    if (split) ptx::mbar_arrive(&sh.q_empty[1]);
                 }
                 uint32_t done = pos;  // tiles up to here are given back, or will be when the products with them are done
                 if (first < end) {

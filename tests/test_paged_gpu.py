@@ -246,6 +246,26 @@ def test_attention_offsets_beyond_32_bits():
         hold(out, lse, q, p, D ** -0.5)
 
 
+@pytest.mark.parametrize("Hq, Hkv, D", [(14, 2, 64), (16, 2, 128), (4, 4, 128)])
+def test_attention_many_short_chunks_one_after_the_other(Hq, Hkv, D):
+    """CTAs that go through several items of one tile or a few, with rows for one half of a tile or both: their parts hand buffers
+    and barriers on from item to item.  Every run has to end in time and with the same bits."""
+    m = rq()
+    g = torch.Generator().manual_seed(D + Hq)
+    n = torch.randint(1, 20, (300,), generator=g).tolist()
+    past = torch.randint(0, 600, (300,), generator=g).tolist()
+    past = [p if i % 3 else p * 5 for i, p in enumerate(past)]
+    p = Paged([(a if i % 7 else 2 * a, b) for i, (a, b) in enumerate(zip(n, past))], Hkv, D, 16, seed=D)
+    q = p.queries(Hq)
+    ws = m.alloc_workspace(m.paged_attention_workspace_bytes(p.T, 300, Hq, Hkv, D, 0))
+    first, lse = m.paged_attention(q, *p.args(), lse=True, workspace=ws)
+    hold(first, lse, q, p, D ** -0.5)
+    for _ in range(100):
+        out = m.paged_attention(q, *p.args(), workspace=ws)
+        assert m.check(ws) == 0, m.last_error()
+        assert torch.equal(out, first)
+
+
 def test_attention_is_the_same_from_run_to_run():
     p = Paged([(1, 5000), (5, 300), (90, 800)], 2, 128, 16)
     q = p.queries(16)
