@@ -593,6 +593,10 @@ def _new(M: int, K: int, dtype, index: int) -> torch.Tensor:
     return torch.empty_strided((M, K), (K, 1), dtype=dtype, device=index)
 
 
+def _new_vector(n: int, dtype, index: int) -> torch.Tensor:
+    return torch.empty_strided((n,), (1,), dtype=dtype, device=index)
+
+
 def w4a16_gemv(X: torch.Tensor, w_codes: torch.Tensor, w_side: torch.Tensor, fmt: str = "hif4",
                out_dtype: torch.dtype = torch.bfloat16, Y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """*_w4a16_gemv: Y = X deq(Q(W))^T for at most GEMV_MAX_TOKENS token rows, streaming the packed weights once."""
@@ -890,8 +894,7 @@ def verify_drafts(logits: torch.Tensor, row_start: torch.Tensor, drafts: torch.T
             ldd, at_draft = _rows(draft_logits, "draft_logits", R, V, logits.dtype, index), draft_logits.data_ptr()
             at_peak, at_sum = _vector(draft_peak, "draft_peak", R, _F32, index), _vector(draft_log_sum, "draft_log_sum", R, _F32, index)
     if out is None:
-        out = {"accepted": torch.empty(count, dtype=torch.int32, device=index), "tokens": torch.empty(R, dtype=torch.int64, device=index),
-               "logp": torch.empty(R, dtype=_F32, device=index)}
+        out = {"accepted": _new_vector(count, torch.int32, index), "tokens": _new_vector(R, torch.int64, index), "logp": _new_vector(R, _F32, index)}
     if workspace is None:
         workspace = _new(1, verify_drafts_workspace_bytes(R), torch.uint8, index)
     elif workspace.get_device() != index or not workspace.is_contiguous():

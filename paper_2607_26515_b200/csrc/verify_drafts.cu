@@ -19,7 +19,7 @@ namespace {
 
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
 constexpr float kNear = 6.103515625e-05f;  // 2^-14: the fast exponentials are within 2^-18 for arguments down to -40
 
 struct VerifyArgs {
@@ -42,6 +42,21 @@ struct VerifyArgs {
 __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {  // NaN is passed over
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float warp_max(float v) {  // NaN is passed over
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float rcp(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 __device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
@@ -97,13 +112,13 @@ __device__ W cluster_best(W b, W* warps, W* mine, int cs) {
     if (cs == 1) return b;
     if (threadIdx.x == 0) *mine = b;
     cluster_sync();
-    b = remote(mine, 0);
-    for (int i = 1; i < cs; ++i) b = join(b, remote(mine, i));
+    b = remote(mine, threadIdx.x & (cs - 1));  // cs is a power of two
+    for (int o = 1; o < cs; o <<= 1) b = join(b, shuffle(b, o));
     return b;
 }
 
 template <typename T, bool DRAFT, bool GREEDY>
-__global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant__ VerifyArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_constant__ VerifyArgs a) {
     __shared__ Best warp_best[kThreads / 32], cta_best;
     __shared__ Best64 warp_best64[kThreads / 32], cta_best64;
     uint32_t cs, rank = 0;
@@ -177,21 +192,38 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
             const double p = exp(((double)z - (double)peak) * a.inv_t64 - (double)log_sum);
             return minus ? fmax(p - exp(((double)zd - (double)dpeak) * a.inv_t64 - (double)a.draft_log_sum[r]), 0.0) : p;
         };
+        // take(j, ratios, logits, draft's logits, e) for eight of this thread's places after the other, the next ones' loads ahead; all
+        // lanes of a warp the same number of times.  Places behind the row's end and the one to be left out have a logit of -inf, that
+        // is a ratio of 0.
         auto visit = [&](bool minus, int skip, auto&& take) {
-            for (int v = v0 + tid; v < v1; v += kThreads) {
-                const int m = min(8, a.V - v * 8);
-                Raw8<T> rz, rd;
-                Raw8<float> re;
+            Raw8<T> rz, rd;
+            Raw8<float> re;
+            const int whole = min(v1, a.V / 8);
+            auto fetch = [&](int v, int m) {
                 rz.load(x + (int64_t)v * 8, m);
                 if (DRAFT && minus) rd.load(xd + (int64_t)v * 8, m);
                 re.load(e + (int64_t)v * 8, m);
-                float z[8], zd[8] = {}, ev[8];
+            };
+            auto step = [&](int v, int m, int next) {
+                float z[8], zd[8] = {}, ev[8], s[8];
                 rz.get(z);
                 if (DRAFT && minus) rd.get(zd);
                 re.get(ev);
+                if (next < whole) fetch(next, 8);
+                if (m < 8 || skip >> 3 == v) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < m && v * 8 + i != skip) take(v * 8 + i, z[i], zd[i], ev[i]);
+                    for (int i = 0; i < 8; ++i)
+                        if (i >= m || v * 8 + i == skip) z[i] = -kInf, ev[i] = 1.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] = weight(z[i], zd[i], minus) * rcp(ev[i]);
+                take(v * 8, s, z, zd, ev);
+            };
+            if (v0 + tid < whole) fetch(v0 + tid, 8);
+            for (int vw = v0 + (tid & ~31); vw < whole; vw += kThreads) step(vw + lane, vw + lane < whole ? 8 : 0, vw + lane + kThreads);
+            if (whole < v1 && tid < 32) {  // the ragged end of the row
+                if (lane == 0) fetch(whole, a.V - whole * 8);
+                step(whole, lane == 0 ? a.V - whole * 8 : 0, whole);
             }
         };
         Best best{0.0f, a.V, 0.0f};
@@ -199,10 +231,18 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
         int skip = sure;
         for (int round = 0; round < 2; ++round) {
             best = Best{0.0f, a.V, 0.0f};
-            visit(minus, skip, [&](int j, float z, float zd, float ev) {
-                const float s = __fdividef(weight(z, zd, minus), ev);
-                if (s > best.s) best = Best{s, j, best.s};  // in the order of places: equal ones keep the first
-                else best.next = fmaxf(best.next, s);
+            // most are far below the largest that the warp has seen, and are not looked at one by one
+            float seen = 0.0f;
+            visit(minus, skip, [&](int j, const float (&s)[8], const float (&)[8], const float (&)[8], const float (&)[8]) {
+                const float all = warp_max(max3(max3(s[0], s[1], s[2]), max3(s[3], s[4], s[5]), fmaxf(s[6], s[7])));
+                if (!(all >= seen * (1.0f - 2.0f * kNear))) return;  // warp-uniform
+                seen = fmaxf(seen, all);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    best.next = fmaxf(best.next, fminf(s[i], best.s));
+                    best.j = s[i] > best.s ? j + i : best.j;  // in the order of places: equal ones keep the first
+                    best.s = fmaxf(best.s, s[i]);
+                }
             });
             best = cluster_best(best, warp_best, &cta_best, (int)cs);
             if (best.j < a.V || (!minus && skip < 0)) break;
@@ -214,8 +254,10 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
         if (best.j < a.V && best.next >= best.s * (1.0f - kNear)) {
             Best64 b64{0.0, a.V};
             const float low = best.s * (1.0f - 2.0f * kNear);
-            visit(minus, skip, [&](int j, float z, float zd, float ev) {
-                if (__fdividef(weight(z, zd, minus), ev) >= low) b64 = join(b64, Best64{weight64(z, zd, minus) / (double)ev, j});
+            visit(minus, skip, [&](int j, const float (&s)[8], const float (&z)[8], const float (&zd)[8], const float (&ev)[8]) {
+#pragma unroll 1
+                for (int i = 0; i < 8; ++i)
+                    if (s[i] >= low) b64 = join(b64, Best64{weight64(z[i], zd[i], minus) / (double)ev[i], j + i});
             });
             best.j = cluster_best(b64, warp_best64, &cta_best64, (int)cs).j;
         }
@@ -276,13 +318,21 @@ int resq_verify_drafts(const void* logits, int dtype, int64_t R, int64_t V, int6
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     float *wl = reinterpret_cast<float*>(ws + l.logp), *wp = reinterpret_cast<float*>(ws + l.peak), *ws_sum = reinterpret_cast<float*>(ws + l.log_sum);
     int32_t* ids = reinterpret_cast<int32_t*>(ws + l.ids);
-    int rc = greedy ? resq_token_logprobs(logits, dtype, R, V, ld, nullptr, 1.0f, 1, nullptr, nullptr, nullptr, nullptr, ids, wl, stream)
-                    : resq_token_logprobs(logits, dtype, R, V, ld, drafts, temperature, 0, wl, nullptr, wp, ws_sum, nullptr, nullptr, stream);
-    if (rc) return rc;
-    // Few sequences: their row over a cluster, up to 256 CTAs and not below 8192 logits a CTA (two iterations of its threads).
     const int64_t vecs = (V + 7) / 8;
+    // A few hundred rows leave SMs with one row less than others: cut in two or four the SMs' shares come out within 1.2 of each
+    // other (320 x 131072: two slices, 28.0 us against 28.3 with cold caches; the whole call 47.4 against 51.1).
+    int slices = 0;
+    if (R > 128 && R < 148 * 8) {
+        slices = 1;
+        while (slices < 4 && vecs / (2 * slices) >= 2048 && (R * slices + 147) / 148 * 148 > R * slices * 6 / 5) slices *= 2;
+    }
+    int rc = greedy ? token_logprobs_sliced(logits, dtype, R, V, ld, nullptr, 1.0f, 1, nullptr, nullptr, nullptr, nullptr, ids, wl, slices, stream)
+                    : token_logprobs_sliced(logits, dtype, R, V, ld, drafts, temperature, 0, wl, nullptr, wp, ws_sum, nullptr, nullptr, slices, stream);
+    if (rc) return rc;
+    // Few sequences: their row over a cluster, up to 592 CTAs (four per SM) and not below 4096 logits a CTA (two iterations of its
+    // threads).
     int cs = 1;
-    while (!greedy && cs < 8 && count * cs * 2 <= 256 && vecs / (2 * cs) >= 1024) cs *= 2;
+    while (!greedy && cs < 8 && count * cs * 2 <= 592 && vecs / (2 * cs) >= 512) cs *= 2;
     VerifyArgs a{logits, draft ? draft_logits : nullptr, ld, ldd, lde, row_start, drafts, u, noise, draft_peak, draft_log_sum, wl, wp, ws_sum, ids, wl,
                  accepted, tokens, logp, (int)count, (int)R, (int)V, (int)((vecs + cs - 1) / cs), greedy ? 1.0f : 1.0f / temperature,
                  greedy ? 1.0 : 1.0 / (double)temperature};
