@@ -265,6 +265,17 @@ struct DealWalk {
     }
 };
 
+// The note of a CTA whose first segment is `seg`: the item that it begins inside of, if it is that item's second CTA.
+__device__ __forceinline__ JoinNote join_note(const Segment& seg, const DealStart& start, int cta, int f0) {
+    JoinNote note{0, seg.s.q0, seg.s.n, seg.h, f0, {0, 0, 0}};
+    if (seg.u0 > 0) {
+        const int64_t item = start.unit - seg.u0;
+        const int i0 = (int)(item / start.chunk), i1 = (int)((item + seg.units - 1) / start.chunk);
+        if (i0 == cta - 1) note.parts = i1 - i0 + 1;
+    }
+    return note;
+}
+
 #endif  // __CUDACC__
 
 }  // namespace resq

@@ -333,16 +333,234 @@ __global__ void __launch_bounds__(kWarps * 32, kRowsCtasPerSm) attn_rows_kernel(
                 if (n == 0) a.part_ml[at] = make_float2(ref, sum);
             }
         }
-        if (first && tid == 0) {
-            // the item that this CTA begins inside of: from which CTA to which
-            JoinNote note{0, seg.s.q0, seg.s.n, seg.h, f0, {0, 0, 0}};
-            if (seg.u0 > 0) {
-                const int64_t item = start.unit - seg.u0;
-                const int i0 = (int)(item / start.chunk), i1 = (int)((item + seg.units - 1) / start.chunk);
-                if (i0 == cta - 1) note.parts = i1 - i0 + 1;
+        if (first && tid == 0) a.notes[cta] = join_note(seg, start, cta, f0);
+        first = false;
+    }
+    if (first && tid == 0) a.notes[cta].parts = 0;
+    pdl_trigger();
+}
+
+// The form for 33 to 64 query rows per kv head (drafted tokens): the four warps share each tile of 64 keys and take 16 rows each, so
+// that a warp's sums fit its registers (keys apart, as above, would take 256 of them) and nothing is to be joined at the end; the
+// price is a barrier per tile and four reads of it from shared memory.
+template <int D>
+constexpr int wide_stages() { return D == 128 ? 3 : 6; }
+template <int D>
+constexpr int wide_smem() { return 64 * D * 2 + wide_stages<D>() * kKeys * D * 4; }
+
+template <int D>
+__global__ void __launch_bounds__(kWarps * 32, kRowsCtasPerSm) attn_wide_kernel(const __grid_constant__ AttnArgs a) {
+    constexpr int R = 64, CH = D / 8, S = wide_stages<D>(), kHalf = kKeys * D * 2, kStage = 2 * kHalf, KS = D / 16, NT = D / 8;
+    constexpr int kTiles = 3;  // key tiles that can hold keys of the item's own tokens
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ int64_t sums[kWarps];
+    __shared__ DealStart found;
+    __shared__ uint32_t strange[kTiles][2];  // a bit per key whose value row holds an infinity or NaN
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, cta = blockIdx.x;
+    unsigned char* const ring = smem + R * D * 2;
+    const uint32_t q_base = (uint32_t)__cvta_generic_to_shared(smem), ring_base = q_base + R * D * 2;
+    pdl_wait();
+    if (cta == 0 && tid == 0) *a.status = DeviceStatus{RESQ_OK, 0, 0, 0};
+    const Deal& d = a.deal;
+    const DealStart start = deal_start(a.seq, d, cta, gridDim.x, a.min_chunk, sums, &found);
+    DealWalk walk;
+    walk.init(a.seq, d, start);
+    bool first = true;
+    Segment seg;
+    const int lr = lane & 7, lm = lane >> 3;  // row and matrix of an ldmatrix address
+    while (walk.next(a.seq, d, seg)) {
+        const int f0 = seg.t * R, rows = min(R, seg.s.n * d.g - f0), k_end = deal_k_end(seg.s, d, seg.t), past = seg.s.kv - seg.s.n;
+        const int key_first = seg.k0 * kKeys, tiles = min(seg.k1 - seg.k0, max(0, (k_end - key_first + kKeys - 1) / kKeys));
+        const int first_pos = past + (int)div_by((uint32_t)f0, d.by_g);  // keys up to here are seen by all rows
+        const int first_cut = max(seg.k0, (max(first_pos, -1) + 1) / kKeys);  // the first tile with a key that some row does not see
+        __syncthreads();  // the segment before has read its buffers
+        if (tid < kTiles * 2) strange[tid / 2][tid % 2] = 0;
+        auto issue = [&](int i) {
+            if (i < tiles) {
+                const int key0 = key_first + i * kKeys;
+                const uint32_t dst = ring_base + (i % S) * kStage;
+                // lanes 0-7 look up the pages of eight keys each
+                int in_page = 0;
+                const int key = key0 + (lane & 7) * 8, found_page = key < k_end ? page_of(a.seq, seg.b, key, in_page) : -1;
+                constexpr int kPass = 128 / CH;  // rows per pass of the block: 8 or 16
+#pragma unroll
+                for (int p = 0; p < kKeys / kPass; ++p) {
+                    const int r = p * kPass + tid / CH, ch = tid % CH, group = r / 8;  // the same group for all lanes of a warp
+                    const int page = __shfl_sync(~0u, found_page, group), row = __shfl_sync(~0u, in_page, group) + r % 8;
+                    const bool there = page >= 0 && key0 + r < k_end;
+                    const uint32_t at = dst + r * D * 2 + ((ch ^ (r & 7)) * 16);
+                    const int64_t pg = there ? page : 0, rw = there ? row : 0;
+                    copy16(at, a.k + pg * a.k_page + rw * a.k_row + seg.h * a.k_head + (there ? ch * 8 : 0), there);
+                    copy16(at + kHalf, a.v + pg * a.v_page + rw * a.v_row + seg.h * a.v_head + (there ? ch * 8 : 0), there);
+                }
             }
-            a.notes[cta] = note;
+            copy_commit();
+        };
+        // ---- queries with the first tile
+        for (int i = tid; i < R * CH; i += kWarps * 32) {
+            const int r = i / CH, ch = i % CH;
+            const bool there = r < rows;
+            const int tok = (int)div_by((uint32_t)(f0 + (there ? r : 0)), d.by_g), head = seg.h * d.g + (f0 + (there ? r : 0) - tok * d.g);
+            copy16(q_base + r * D * 2 + ((ch ^ (r & 7)) * 16), a.q + (int64_t)(seg.s.q0 + tok) * a.ldq + head * D + ch * 8, there);
         }
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i) issue(i);
+        int pos[2];  // of the rows this thread holds; rows behind the tile see what the last one does
+#pragma unroll
+        for (int i = 0; i < 2; ++i) pos[i] = past + (int)div_by((uint32_t)(f0 + min(w * 16 + i * 8 + lane / 4, rows - 1)), d.by_g);
+        float o[NT][4], m[2] = {-kInf, -kInf}, l[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
+        uint32_t qf[KS][4];
+        for (int i = 0; i < tiles; ++i) {
+            copy_wait<S - 2>();
+            __syncthreads();  // the tile is there, and all have done with the one before, whose room the next copies take
+            issue(i + S - 1);
+            if (i == 0) {
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const int r = w * 16 + (lm & 1) * 8 + lr, ch = ks * 2 + (lm >> 1);
+                    ldsm4(qf[ks], q_base + r * D * 2 + ((ch ^ (r & 7)) * 16));
+                }
+            }
+            const uint32_t kb = ring_base + (i % S) * kStage, vb = kb + kHalf;
+            const int key0 = key_first + i * kKeys;
+            const bool masked = seg.k0 + i >= first_cut;
+            if (masked && k_end - 1 > first_pos) {
+                // A weight of 0 must not meet an infinity or NaN: keys that some row does not see give theirs up, and the rows that do
+                // see them get them at the end.  (Keys from k_end on are zeros here.)
+                const int lo = max(0, first_pos + 1 - key0), n = min(kKeys, k_end - key0) - lo;
+                for (int j = tid; j < n * CH; j += kWarps * 32) {
+                    uint4* const at = reinterpret_cast<uint4*>(ring + (i % S) * kStage + kHalf + (lo + j / CH) * D * 2 + j % CH * 16);
+                    uint32_t x[4] = {at->x, at->y, at->z, at->w};
+                    bool bad = false;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if ((x[e] & 0x7F80u) == 0x7F80u) x[e] &= 0xFFFF0000u, bad = true;
+                        if ((x[e] & 0x7F800000u) == 0x7F800000u) x[e] &= 0xFFFFu, bad = true;
+                    }
+                    if (bad) {
+                        *at = make_uint4(x[0], x[1], x[2], x[3]);
+                        const int t = min(seg.k0 + i - first_cut, kTiles - 1), r = lo + j / CH;
+                        atomicOr(&strange[t][r / 32], 1u << (r & 31));
+                    }
+                }
+                __syncthreads();
+            }
+            float s[8][4];
+#pragma unroll
+            for (int n = 0; n < 8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int n = 0; n < 8; n += 2) {
+                    uint32_t kf[4];
+                    const int r = n * 8 + (lm >> 1) * 8 + lr, ch = ks * 2 + (lm & 1);
+                    ldsm4(kf, kb + r * D * 2 + ((ch ^ (r & 7)) * 16));
+                    mma(s[n], qf[ks], kf[0], kf[1]);
+                    mma(s[n + 1], qf[ks], kf[2], kf[3]);
+                }
+            if (masked) {
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key0 + n * 8 + (lane & 3) * 2 + (e & 1) > pos[e >> 1]) s[n][e] = -kInf;
+            }
+            float top[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float x = fmaxf(s[0][2 * e], s[0][2 * e + 1]);
+#pragma unroll
+                for (int n = 1; n < 8; ++n) x = fmaxf(x, fmaxf(s[n][2 * e], s[n][2 * e + 1]));
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 2));
+                top[e] = fmaxf(m[e], x * a.c);
+            }
+            if (__any_sync(~0u, top[0] > m[0] || top[1] > m[1])) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float f = top[e] > m[e] ? ex2(m[e] - top[e]) : 1.0f;
+                    m[e] = top[e];
+                    l[e] *= f;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) o[n][2 * e] *= f, o[n][2 * e + 1] *= f;
+                }
+            }
+            const float ref[2] = {m[0] == -kInf ? 0.0f : m[0], m[1] == -kInf ? 0.0f : m[1]};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {  // 16 keys at a time: their weights, and their product with the values
+                uint32_t pf[4];
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    float* const x = s[2 * k + n];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = ex2(fmaf(x[e], a.c, -ref[e >> 1]));
+                        l[e >> 1] += x[e];
+                    }
+                    pf[2 * n] = pack_bf16(x[0], x[1]), pf[2 * n + 1] = pack_bf16(x[2], x[3]);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; n += 2) {
+                    uint32_t vf[4];
+                    const int r = k * 16 + (lm & 1) * 8 + lr, ch = n + (lm >> 1);
+                    ldsm4_t(vf, vb + r * D * 2 + ((ch ^ (r & 7)) * 16));
+                    mma(o[n], pf, vf[0], vf[1]);
+                    mma(o[n + 1], pf, vf[2], vf[3]);
+                }
+            }
+        }
+        copy_wait<0>();
+        const bool whole = seg.u0 == 0 && seg.u1 == seg.units;
+        const int slot = 2 * cta + (seg.u0 == 0 ? 1 : 0);
+        uint32_t any = 0;
+        if (tiles > 0) {
+#pragma unroll
+            for (int t = 0; t < kTiles * 2; ++t) any |= strange[t / 2][t % 2];
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float sum = l[e];
+            sum += __shfl_xor_sync(~0u, sum, 1);
+            sum += __shfl_xor_sync(~0u, sum, 2);
+            const int r = w * 16 + e * 8 + lane / 4;
+            if (r >= rows) continue;
+            const float inv = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n][2 * e] *= inv, o[n][2 * e + 1] *= inv;
+            if (any) {  // rare
+                for (int t = 0; t < kTiles * 2; ++t)
+                    for (uint32_t bits = strange[t / 2][t % 2]; bits; bits &= bits - 1) {
+                        const int key = (first_cut + t / 2) * kKeys + t % 2 * 32 + __ffs(bits) - 1;
+                        int in_page = 0;
+                        const int page = key <= pos[e] ? page_of(a.seq, seg.b, key, in_page) : -1;
+                        if (page < 0) continue;
+                        const __nv_bfloat16* src = a.v + (int64_t)page * a.v_page + (int64_t)in_page * a.v_row + (int64_t)seg.h * a.v_head + (lane & 3) * 2;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const float x = __bfloat162float(src[n * 8]), y = __bfloat162float(src[n * 8 + 1]);
+                            if (!(fabsf(x) < kInf)) o[n][2 * e] += x;
+                            if (!(fabsf(y) < kInf)) o[n][2 * e + 1] += y;
+                        }
+                    }
+            }
+            if (whole) {
+                const int tok = (int)div_by((uint32_t)(f0 + r), d.by_g), head = seg.h * d.g + (f0 + r - tok * d.g);
+                const int64_t row = seg.s.q0 + tok;
+                uint32_t* const dst = reinterpret_cast<uint32_t*>(a.out + row * a.ldo + head * D + (lane & 3) * 2);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) dst[n * 4] = pack_bf16(o[n][2 * e], o[n][2 * e + 1]);
+                if (a.lse && (lane & 3) == 0) a.lse[row * a.Hq + head] = sum == 0.0f ? -kInf : (m[e] + log2f(sum)) * kLn2;
+            } else {
+                const int64_t at = (int64_t)slot * R + r;
+                float* const dst = a.part_o + at * D + (lane & 3) * 2;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) *reinterpret_cast<float2*>(dst + n * 8) = make_float2(o[n][2 * e], o[n][2 * e + 1]);
+                if ((lane & 3) == 0) a.part_ml[at] = make_float2(m[e], sum);
+            }
+        }
+        if (first && tid == 0) a.notes[cta] = join_note(seg, start, cta, f0);
         first = false;
     }
     if (first && tid == 0) a.notes[cta].parts = 0;
@@ -537,9 +755,9 @@ struct Choice {
 constexpr int kPlanSms = 148;  // the workspace query answers without a device
 Choice choose(int64_t T, int64_t Hq, int64_t Hkv, int64_t max_new) {
     const int64_t n = max_new > 0 ? std::min(max_new, T) : T, rows = n * (Hq / Hkv);
-    const int limit = env_int("RESQ_ATTN_ROWS", 32);
+    const int limit = env_int("RESQ_ATTN_ROWS", 64);
     if (rows > limit) return Choice{true, attn_chunk_rows((int)(Hq / Hkv)), kPlanSms};
-    return Choice{false, rows <= 16 ? 16 : 32, kPlanSms * kRowsCtasPerSm};
+    return Choice{false, rows <= 16 ? 16 : rows <= 32 ? 32 : 64, kPlanSms * kRowsCtasPerSm};
 }
 
 }  // namespace
@@ -599,9 +817,10 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
                                        dim3((unsigned)(2 * D)), 0, st, a),
                          "attn_join_tiles_kernel launch");
     }
-    auto kern = D == 128 ? (l.rows == 16 ? attn_rows_kernel<128, 1> : attn_rows_kernel<128, 2>)
-                         : (l.rows == 16 ? attn_rows_kernel<64, 1> : attn_rows_kernel<64, 2>);
-    const int smem = D == 128 ? (l.rows == 16 ? rows_smem<128, 1>() : rows_smem<128, 2>()) : (l.rows == 16 ? rows_smem<64, 1>() : rows_smem<64, 2>());
+    auto kern = D == 128 ? (l.rows == 16 ? attn_rows_kernel<128, 1> : l.rows == 32 ? attn_rows_kernel<128, 2> : attn_wide_kernel<128>)
+                         : (l.rows == 16 ? attn_rows_kernel<64, 1> : l.rows == 32 ? attn_rows_kernel<64, 2> : attn_wide_kernel<64>);
+    const int smem = D == 128 ? (l.rows == 16 ? rows_smem<128, 1>() : l.rows == 32 ? rows_smem<128, 2>() : wide_smem<128>())
+                              : (l.rows == 16 ? rows_smem<64, 1>() : l.rows == 32 ? rows_smem<64, 2>() : wide_smem<64>());
     rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem, "attn_rows_kernel shared memory");
     if (rc) return rc;
     {

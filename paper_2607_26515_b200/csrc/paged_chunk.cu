@@ -184,15 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             g.split = g.rows[1] == 0;
             if (g.split) g.stop[1] = g.stop[0];
             if (lane == 0) {
-                if (count == 0) {
-                    JoinNote note{0, g.q0, g.n, g.h, g.f0, {0, 0, 0}};
-                    if (s.u0 > 0) {
-                        const int64_t item = start.unit - s.u0;
-                        const int i0 = (int)(item / start.chunk), i1 = (int)((item + s.units - 1) / start.chunk);
-                        if (i0 == cta - 1) note.parts = i1 - i0 + 1;
-                    }
-                    a.notes[cta] = note;
-                }
+                if (count == 0) a.notes[cta] = join_note(s, start, cta, g.f0);
                 sh.seg[e] = g;
                 for (int i = 0; i < kStrange * 4; ++i) sh.strange[e][i / 4][i % 4] = 0;
                 ptx::mbar_arrive(&sh.desc_full[e]);

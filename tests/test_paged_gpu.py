@@ -200,7 +200,7 @@ def test_attention_wild_arrays(n):
     hold(out, None, q, p, 64 ** -0.5)
 
 
-@pytest.mark.parametrize("n, past", [(4, 100), (3, 61), (60, 40), (200, 500), (300, 0)])
+@pytest.mark.parametrize("n, past", [(4, 100), (3, 61), (8, 120), (16, 100), (21, 50), (60, 40), (200, 500), (300, 0)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_attention_strange_values_behind_a_token(n, past, D):
     """NaN and infinities in the keys and values of later tokens of the same chunk do not reach the earlier ones."""
