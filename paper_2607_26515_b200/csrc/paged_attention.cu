@@ -625,7 +625,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs& a, int cta, int p0, i
 // has CTAs) has its rows one by one, y, y + grid.y, ..., and the eight warps share a row's parts.
 template <int D>
 __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnArgs a) {
-    constexpr int E = D / 32, W = 8, kDeep = 4;
+    constexpr int E = D / 32, W = 8, kDeep = 8;
     __shared__ float2 warp_ml[W];
     __shared__ float warp_o[W][D];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, cta = blockIdx.x;
@@ -645,7 +645,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
         for (int e = 0; e < E; e += 2) dst[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
         if (a.lse && lane == 0) a.lse[row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
     };
-    if (note.parts <= 2 * kDeep) {
+    if (note.parts <= 3 * kDeep) {
         const int r = blockIdx.y * W + w;
         if (r >= rows) return;
         join_parts<D, E, kDeep>(a, cta, 0, note.parts, R, r, ref, sum, acc);
@@ -690,7 +690,7 @@ __global__ void __launch_bounds__(D * 2) attn_join_tiles_kernel(const __grid_con
     const int R = a.deal.rows, r = blockIdx.y * 32 + lane, f = note.f0 + r;
     if (note.parts == 0 || r >= R || f >= note.n * a.deal.g) return;
     float ref = -kInf, sum = 0.0f, acc[16] = {};
-    constexpr int kDeep = 3;
+    constexpr int kDeep = 4;
     for (int b = 0; b < note.parts; b += kDeep) {
         float2 q[kDeep];
         float x[kDeep][16];
@@ -798,7 +798,9 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
     a.ldq = ldq, a.ldo = ldo;
     a.k_page = cache->k_page, a.k_row = cache->k_row, a.k_head = cache->k_head;
     a.v_page = cache->v_page, a.v_row = cache->v_row, a.v_head = cache->v_head;
-    a.out = static_cast<bf*>(O), a.lse = lse, a.Hq = (int)Hq, a.c = scale * kLog2e, a.min_chunk = 1;
+    // Tiles a CTA takes at least: with up to 32 rows a part costs less than the tile it saves (one decoded token at 4000 keys: 12.1 us with
+    // one, 13.3 with two); with more, joining does (40 rows at 4000 keys: 20.6 us with one, 15.9 with three, 18.7 with four).
+    a.out = static_cast<bf*>(O), a.lse = lse, a.Hq = (int)Hq, a.c = scale * kLog2e, a.min_chunk = ch.rows == 64 ? 3 : 1;
     if (ch.chunk && !attn_chunk_supported(a)) {  // a stride of 0: no tensor map takes it; this workspace is smaller
         ch = Choice{false, 32, kPlanSms * kRowsCtasPerSm};
         l = layout(D, ch.rows, ch.ctas);
