@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -766,32 +767,31 @@ MAX_SEQUENCES = 4096
 MAX_GROUP_HEADS = 128
 
 
-class _PagedCache(ctypes.Structure):
-    _fields_ = [("k", _vp), ("v", _vp), ("pages", _i64), ("page_size", _i64), ("kv_heads", _i64), ("head_dim", _i64), ("k_page", _i64),
-                ("k_row", _i64), ("k_head", _i64), ("v_page", _i64), ("v_row", _i64), ("v_head", _i64)]
-
-
-class _Sequences(ctypes.Structure):
-    _fields_ = [("q_start", _vp), ("kv_len", _vp), ("page_table", _vp), ("count", _i64), ("max_pages", _i64), ("ld_table", _i64)]
+# The structs resq_paged_cache and resq_sequences, packed (a quarter of the time of filling a ctypes.Structure): addresses of k and v,
+# then pages, page_size, kv_heads, head_dim and the strides of k and of v; addresses of q_start, kv_len and page_table, then count,
+# max_pages and ld_table.
+_PAGED_CACHE, _SEQUENCES = struct.Struct("2Q10q"), struct.Struct("3Q3q")
 
 
 def _paged(k_cache: torch.Tensor, v_cache: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, index: int):
-    """The two structs of a paged call."""
+    """The two structs of a paged call, and its kv_heads, head_dim and number of sequences."""
     shape = k_cache.shape
     if (k_cache.dtype is not _BF16 or v_cache.dtype is not _BF16 or len(shape) != 4 or v_cache.shape != shape or k_cache.get_device() != index
             or v_cache.get_device() != index):
         raise ValueError(f"k_cache and v_cache must be bf16 tensors of one shape [pages, page_size, kv_heads, head_dim] on cuda:{index}")
     kp, kr, kh, ki = k_cache.stride()
     vp, vr, vh, vi = v_cache.stride()
-    _require(ki == 1 and vi == 1, "k_cache and v_cache must have unit inner stride")
-    count = kv_len.shape[0] if kv_len.dim() == 1 else -1
+    if ki != 1 or vi != 1:
+        raise ValueError("k_cache and v_cache must have unit inner stride")
+    table = page_table.shape
+    if page_table.dtype is not torch.int32 or len(table) != 2 or page_table.get_device() != index or (table[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError(f"page_table must be an int32 tensor [sequences, pages per sequence] on cuda:{index} with unit inner stride")
+    count, per_seq = table
     at_start, at_len = _vector(q_start, "q_start", count + 1, torch.int32, index), _vector(kv_len, "kv_len", count, torch.int32, index)
-    if (page_table.dtype is not torch.int32 or page_table.dim() != 2 or page_table.shape[0] != count or page_table.get_device() != index
-            or (page_table.shape[1] > 1 and page_table.stride(1) != 1)):
-        raise ValueError(f"page_table must be an int32 tensor [{count}, pages per sequence] on cuda:{index} with unit inner stride")
-    per_seq = page_table.shape[1]
-    return (_PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), *shape, kp, kr, kh, vp, vr, vh),
-            _Sequences(at_start, at_len, page_table.data_ptr(), count, per_seq, page_table.stride(0) if count > 1 else per_seq))
+    pages, page, heads, dim = shape
+    return (_PAGED_CACHE.pack(k_cache.data_ptr(), v_cache.data_ptr(), pages, page, heads, dim, kp, kr, kh, vp, vr, vh),
+            _SEQUENCES.pack(at_start, at_len, page_table.data_ptr(), count, per_seq, page_table.stride(0) if count > 1 else per_seq),
+            heads, dim, count)
 
 
 def rope_append(qkv: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
@@ -806,8 +806,7 @@ def rope_append(qkv: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
     T, W, ld, code, index = _first(qkv, "qkv")
     if stream is not None or _current_device() != index:
         return _elsewhere(index, stream, lambda: rope_append(qkv, k_cache, v_cache, q_start, kv_len, page_table, inv_freq, bias, positions, pairs, q))
-    cache, seqs = _paged(k_cache, v_cache, q_start, kv_len, page_table, index)
-    Hkv, D = cache.kv_heads, cache.head_dim
+    cache, seqs, Hkv, D, _ = _paged(k_cache, v_cache, q_start, kv_len, page_table, index)
     _require(D > 0 and W % D == 0 and W > 2 * Hkv * D, f"qkv must have (Hq + 2 * {Hkv}) heads of {D} columns")
     Hq = W // D - 2 * Hkv
     half = inv_freq.shape[0] if inv_freq.dim() == 1 else -1
@@ -819,7 +818,7 @@ def rope_append(qkv: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
     else:
         ldq = _rows(q, "q", T, Hq * D, _BF16, index)
     _check(lib().resq_rope_append(qkv.data_ptr(), code, T, ld, Hq, Hkv, D, at_bias, freq, 2 * half, 1 if pairs else 0, at_pos,
-                                  ctypes.byref(cache), ctypes.byref(seqs), q.data_ptr(), ldq, _raw_stream(index)))
+                                  cache, seqs, q.data_ptr(), ldq, _raw_stream(index)))
     return q
 
 
@@ -841,8 +840,7 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
         return _elsewhere(index, stream, lambda: paged_attention(q, k_cache, v_cache, q_start, kv_len, page_table, scale, max_new, lse, out,
                                                                  workspace))
     _require(code == OUT_BF16, "q must be bf16")
-    cache, seqs = _paged(k_cache, v_cache, q_start, kv_len, page_table, index)
-    Hkv, D = cache.kv_heads, cache.head_dim
+    cache, seqs, Hkv, D, count = _paged(k_cache, v_cache, q_start, kv_len, page_table, index)
     _require(D > 0 and W % D == 0, f"q must have heads of {D} columns")
     Hq = W // D
     max_new = 0 if max_new is None else min(max(int(max_new), 0), T)
@@ -852,10 +850,10 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
         ldo = _rows(out, "out", T, W, _BF16, index)
     values = _new(T, Hq, _F32, index) if lse else None
     if workspace is None:
-        workspace = _new(1, max(paged_attention_workspace_bytes(T, seqs.count, Hq, Hkv, D, max_new), 256), torch.uint8, index)
+        workspace = _new(1, max(paged_attention_workspace_bytes(T, count, Hq, Hkv, D, max_new), 256), torch.uint8, index)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on cuda:{index}")
-    _check(lib().resq_paged_attention(q.data_ptr(), T, ldq, Hq, Hkv, D, ctypes.byref(cache), ctypes.byref(seqs), max_new,
+    _check(lib().resq_paged_attention(q.data_ptr(), T, ldq, Hq, Hkv, D, cache, seqs, max_new,
                                       D ** -0.5 if scale is None else scale, out.data_ptr(), ldo, _ptr(values), workspace.data_ptr(),
                                       workspace.numel() * workspace.element_size(), _raw_stream(index)))
     return (out, values) if lse else out

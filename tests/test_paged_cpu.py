@@ -51,8 +51,15 @@ ATTN_BAD = PAGED_BAD + [
 ]
 
 
+class _PagedCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v")] + [(n, ctypes.c_int64) for n in CACHE if n not in ("k", "v")]
+
+
+class _Sequences(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q_start", "kv_len", "page_table")] + [(n, ctypes.c_int64) for n in ("count", "max_pages", "ld_table")]
+
+
 def call(fn, args, changes):
-    from paper_2607_26515_b200.binding import _PagedCache, _Sequences
     got, held = [], []
     for name, value in args.items():
         if name in ("cache", "seqs"):
@@ -111,6 +118,12 @@ def test_workspace_queries(lib):
     # one more byte is enough, one less is not
     n = q(5, 3, 16, 2, 128, 1)
     assert call(lib.resq_paged_attention, ATTN, dict(ws_bytes=n - 1)) == WORKSPACE
+
+
+def test_packed_structs_have_the_layout_of_the_header():
+    from paper_2607_26515_b200 import binding
+    cache, seqs = _PagedCache(*range(1, 13)), _Sequences(*range(21, 27))
+    assert bytes(cache) == binding._PAGED_CACHE.pack(*range(1, 13)) and bytes(seqs) == binding._SEQUENCES.pack(*range(21, 27))
 
 
 def test_binding_refuses_on_the_cpu():
