@@ -153,13 +153,21 @@ __device__ __forceinline__ int64_t deal_head_units(const Seq& s, const Deal& d) 
 __device__ __forceinline__ DealStart deal_start(const SeqArgs& a, const Deal& d, int cta, int ctas, int min_chunk, int64_t* sums, DealStart* found) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, nw = blockDim.x >> 5;
     const int per = (a.B + (int)blockDim.x - 1) / (int)blockDim.x;
+    // visit(i, units of a head): this thread's sequences in order, four loads in flight
+    auto each = [&](auto&& visit) {
+        for (int i0 = 0; i0 < per; i0 += 4) {
+            Seq s[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[i] = Seq{0, 0, 0};
+                if (i0 + i < per && tid * per + i0 + i < a.B) s[i] = load_seq(a, tid * per + i0 + i);
+            }
+#pragma unroll 1
+            for (int i = 0; i < 4 && i0 + i < per; ++i) visit(tid * per + i0 + i, deal_head_units(i == 0 ? s[0] : i == 1 ? s[1] : i == 2 ? s[2] : s[3], d));
+        }
+    };
     int64_t mine = 0;
-    for (int i = 0; i < per; ++i) {
-        const int b = tid * per + i;
-        Seq s{0, 0, 0};
-        if (b < a.B) s = load_seq(a, b);
-        mine += deal_head_units(s, d) * d.Hkv;
-    }
+    each([&](int, int64_t per_head) { mine += per_head * d.Hkv; });
     int64_t upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -181,17 +189,13 @@ __device__ __forceinline__ DealStart deal_start(const SeqArgs& a, const Deal& d,
     if (__any_sync(~0u, owner)) {
         int64_t at = upto - mine;
         bool open = owner;
-        for (int i = 0; i < per; ++i) {
-            const int b = tid * per + i;
-            Seq s{0, 0, 0};
-            if (b < a.B) s = load_seq(a, b);
-            const int64_t per_head = deal_head_units(s, d);
+        each([&](int b, int64_t per_head) {
             if (open && unit < at + per_head * d.Hkv) {
                 *found = DealStart{unit, min(chunk, total - unit), chunk, at, per_head, b};
                 open = false;
             }
             at += per_head * d.Hkv;
-        }
+        });
     }
     __syncthreads();
     return *found;

@@ -755,8 +755,7 @@ struct Choice {
 constexpr int kPlanSms = 148;  // the workspace query answers without a device
 Choice choose(int64_t T, int64_t Hq, int64_t Hkv, int64_t max_new) {
     const int64_t n = max_new > 0 ? std::min(max_new, T) : T, rows = n * (Hq / Hkv);
-    const int limit = env_int("RESQ_ATTN_ROWS", 64);
-    if (rows > limit) return Choice{true, attn_chunk_rows((int)(Hq / Hkv)), kPlanSms};
+    if (rows > 64) return Choice{true, attn_chunk_rows((int)(Hq / Hkv)), kPlanSms};
     return Choice{false, rows <= 16 ? 16 : rows <= 32 ? 32 : 64, kPlanSms * kRowsCtasPerSm};
 }
 
@@ -793,7 +792,7 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
     using bf = __nv_bfloat16;
     AttnArgs a;
     a.seq = seq_args(*cache, *seqs, T);
-    a.deal = Deal{l.rows, ch.chunk ? kChunkKeys : kKeys, (int)Hkv, (int)(Hq / Hkv), ch.chunk ? env_int("RESQ_ATTN_EXTRA", kChunkExtra) : 0, fast_div((uint32_t)(Hq / Hkv))};
+    a.deal = Deal{l.rows, ch.chunk ? kChunkKeys : kKeys, (int)Hkv, (int)(Hq / Hkv), ch.chunk ? kChunkExtra : 0, fast_div((uint32_t)(Hq / Hkv))};
     a.q = static_cast<const bf*>(Q), a.k = static_cast<const bf*>(cache->k), a.v = static_cast<const bf*>(cache->v);
     a.ldq = ldq, a.ldo = ldo;
     a.k_page = cache->k_page, a.k_row = cache->k_row, a.k_head = cache->k_head;

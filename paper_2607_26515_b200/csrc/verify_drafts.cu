@@ -34,6 +34,7 @@ struct VerifyArgs {
     int32_t* accepted;
     int64_t* tokens;
     float* out_logp;
+    DeviceStatus* status;
     int B, R, V, slice;  // slice: vectors of 8 per CTA
     float inv_t;
     double inv_t64;
@@ -127,6 +128,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
     const int tid = threadIdx.x, lane = tid & 31, b = blockIdx.x / cs;
     pdl_wait();
     pdl_trigger();
+    if (blockIdx.x == 0 && tid == 0) *a.status = DeviceStatus{RESQ_OK, 0, 0, 0};
     const int r0 = min(max(a.row_start[b], 0), a.R), n = max(min(max(a.row_start[b + 1], 0), a.R) - r0, 0);
     if (n == 0) {  // the cluster's CTAs alike
         if (rank == 0 && tid == 0) a.accepted[b] = 0;
@@ -334,7 +336,7 @@ int resq_verify_drafts(const void* logits, int dtype, int64_t R, int64_t V, int6
     int cs = 1;
     while (!greedy && cs < 8 && count * cs * 2 <= 592 && vecs / (2 * cs) >= 512) cs *= 2;
     VerifyArgs a{logits, draft ? draft_logits : nullptr, ld, ldd, lde, row_start, drafts, u, noise, draft_peak, draft_log_sum, wl, wp, ws_sum, ids, wl,
-                 accepted, tokens, logp, (int)count, (int)R, (int)V, (int)((vecs + cs - 1) / cs), greedy ? 1.0f : 1.0f / temperature,
+                 accepted, tokens, logp, reinterpret_cast<DeviceStatus*>(ws), (int)count, (int)R, (int)V, (int)((vecs + cs - 1) / cs), greedy ? 1.0f : 1.0f / temperature,
                  greedy ? 1.0 : 1.0 / (double)temperature};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     using bf = __nv_bfloat16;
