@@ -45,12 +45,18 @@ inline SeqArgs seq_args(const resq_paged_cache& c, const resq_sequences& s, int6
                    (int)c.pages, fast_div((uint32_t)c.page_size)};
 }
 
-// How attention is dealt out (below): rows and keys per tile, heads.
+// How attention is dealt out (below): rows and keys (a power of two) per tile, heads.
 struct Deal {
     int rows, keys, Hkv, g;
     int extra;  // what an item costs besides its keys, in units
-    FastDiv by_g;
+    int key_bits;
+    FastDiv by_g, by_rows;
 };
+inline Deal make_deal(int rows, int keys, int Hkv, int g, int extra) {
+    Deal d{rows, keys, Hkv, g, extra, 0, fast_div((uint32_t)g), fast_div((uint32_t)rows)};
+    while ((1 << d.key_bits) < keys) ++d.key_bits;
+    return d;
+}
 // Where partial results lie: a CTA's first segment, when its item began in an earlier CTA, in slot 2 * cta; one whose item goes on
 // in the next CTA otherwise in slot 2 * cta + 1.  The CTA that begins inside an item says so in its entry of `notes`: the CTAs
 // before it that the item covers, and all of them.
@@ -109,13 +115,13 @@ __device__ __forceinline__ int page_of(const SeqArgs& a, int b, int j, int& with
 // at least: an item without keys still writes its rows).  Items are ordered by sequence, kv head, tile; all units in this order are cut into equal ranges, one per CTA,
 // so that ragged lengths need no plan from the host and a captured call follows the lengths on the device.  A CTA's first item may
 // have begun in an earlier CTA and its last one may go on in a later one: those are left as partial results.
-__device__ __forceinline__ int deal_tiles(const Seq& s, const Deal& d) { return (int)(((int64_t)s.n * d.g + d.rows - 1) / d.rows); }
+__device__ __forceinline__ int deal_tiles(const Seq& s, const Deal& d) { return (int)div_by((uint32_t)max(s.n * d.g - 1, 0), d.by_rows) + (s.n > 0); }
 __device__ __forceinline__ int deal_k_end(const Seq& s, const Deal& d, int t) {  // keys that tile t sees
-    const int64_t f = min((int64_t)(t + 1) * d.rows, (int64_t)s.n * d.g) - 1;
-    const int last = (int)div_by((uint32_t)f, d.by_g);
+    const uint32_t f = min((uint32_t)(t + 1) * (uint32_t)d.rows, (uint32_t)(s.n * d.g)) - 1u;  // n g < 2^31, and the last tile ends below 2^32
+    const int last = (int)div_by(f, d.by_g);
     return max(0, min(s.kv - s.n + last + 1, s.kv));
 }
-__device__ __forceinline__ int deal_units(const Seq& s, const Deal& d, int t) { return max(1, (deal_k_end(s, d, t) + d.keys - 1) / d.keys) + d.extra; }
+__device__ __forceinline__ int deal_units(const Seq& s, const Deal& d, int t) { return max(1, (deal_k_end(s, d, t) + d.keys - 1) >> d.key_bits) + d.extra; }
 
 // Where a CTA's range begins, and how long it is.
 struct DealStart {
@@ -213,13 +219,14 @@ struct DealWalk {
     DealStart at;
     int64_t left;  // units still to hand out
     int b, h, t, u;
-    Seq s;
+    Seq s, ahead;  // of sequence b, and of the next one, asked for early
     int tiles;
     __device__ __forceinline__ void init(const SeqArgs& a, const Deal& d, const DealStart& start) {
         at = start, left = start.units;
         if (left <= 0) return;
         b = start.b;
         s = load_seq(a, b);
+        ahead = load_seq(a, min(b + 1, a.B - 1));
         tiles = deal_tiles(s, d);
         int64_t off = start.unit - start.before;
         h = (int)(off / start.per_head);
@@ -253,7 +260,8 @@ struct DealWalk {
             if (tiles == 0 || ++h == d.Hkv) {
                 h = 0;
                 if (++b >= a.B) return false;
-                s = load_seq(a, b);
+                s = ahead;
+                ahead = load_seq(a, min(b + 1, a.B - 1));
                 tiles = deal_tiles(s, d);
             }
         }

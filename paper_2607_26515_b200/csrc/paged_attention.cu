@@ -105,18 +105,14 @@ __global__ void __launch_bounds__(kWarps * 32, kRowsCtasPerSm) attn_rows_kernel(
     Segment seg;
     while (walk.next(a.seq, d, seg)) {
         const int f0 = seg.t * R, rows = min(R, seg.s.n * d.g - f0), k_end = deal_k_end(seg.s, d, seg.t), past = seg.s.kv - seg.s.n;
-        // ---- queries
         __syncthreads();  // the sums of the segment before have been read
+        // ---- queries, on their way with the first keys
         for (int i = tid; i < R * CH; i += kWarps * 32) {
             const int r = i / CH, ch = i % CH;
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (r < rows) {
-                const int tok = (int)div_by((uint32_t)(f0 + r), d.by_g), head = seg.h * d.g + (f0 + r - tok * d.g);
-                v = *reinterpret_cast<const uint4*>(a.q + (int64_t)(seg.s.q0 + tok) * a.ldq + head * D + ch * 8);
-            }
-            *reinterpret_cast<uint4*>(smem + r * D * 2 + ((ch ^ (r & 7)) * 16)) = v;
+            const bool there = r < rows;
+            const int f = f0 + (there ? r : 0), tok = (int)div_by((uint32_t)f, d.by_g), head = seg.h * d.g + (f - tok * d.g);
+            copy16(q_base + r * D * 2 + ((ch ^ (r & 7)) * 16), a.q + (int64_t)(seg.s.q0 + tok) * a.ldq + head * D + ch * 8, there);
         }
-        __syncthreads();
         int pos[MT][2];  // of the rows this thread holds; rows behind the tile see what the last one does
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -160,6 +156,8 @@ __global__ void __launch_bounds__(kWarps * 32, kRowsCtasPerSm) attn_rows_kernel(
         }
 #pragma unroll
         for (int i = 0; i < S - 1; ++i) issue(i);
+        copy_wait<S - 2>();
+        __syncthreads();  // the queries, whoever brought them
         for (int i = 0; i < tiles; ++i) {
             copy_wait<S - 2>();
             __syncwarp();
@@ -792,7 +790,7 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
     using bf = __nv_bfloat16;
     AttnArgs a;
     a.seq = seq_args(*cache, *seqs, T);
-    a.deal = Deal{l.rows, ch.chunk ? kChunkKeys : kKeys, (int)Hkv, (int)(Hq / Hkv), ch.chunk ? kChunkExtra : 0, fast_div((uint32_t)(Hq / Hkv))};
+    a.deal = make_deal(l.rows, ch.chunk ? kChunkKeys : kKeys, (int)Hkv, (int)(Hq / Hkv), ch.chunk ? kChunkExtra : 0);
     a.q = static_cast<const bf*>(Q), a.k = static_cast<const bf*>(cache->k), a.v = static_cast<const bf*>(cache->v);
     a.ldq = ldq, a.ldo = ldo;
     a.k_page = cache->k_page, a.k_row = cache->k_row, a.k_head = cache->k_head;
@@ -803,7 +801,7 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
     if (ch.chunk && !attn_chunk_supported(a)) {  // a stride of 0: no tensor map takes it; this workspace is smaller
         ch = Choice{false, 32, kPlanSms * kRowsCtasPerSm};
         l = layout(D, ch.rows, ch.ctas);
-        a.deal.rows = ch.rows, a.deal.keys = kKeys, a.deal.extra = 0;
+        a.deal = make_deal(l.rows, kKeys, (int)Hkv, (int)(Hq / Hkv), 0);
     }
     a.status = reinterpret_cast<DeviceStatus*>(ws);
     a.notes = reinterpret_cast<JoinNote*>(ws + kWsHeader);
