@@ -475,6 +475,7 @@ RESQ_API int resq_rope_append(const void* QKV, int dtype, int64_t T, int64_t ldq
  *   makes its token's row NaN.  One call serves decoded tokens, drafts and prompts alike, mixed as they come.
  *   max_new: the largest number of new tokens per sequence as far as the host knows (0: unknown).  It chooses the kernel and the
  *   size of the workspace, never the result's meaning.  Order of summation is fixed for given lengths (bit-identical run to run).
+ *   Device-side waits (long chunks) are bounded and reported by resq_check on the workspace, as for the linear layer.
  *   O must not overlap Q.  workspace of resq_paged_attention_workspace_bytes() bytes for the same numbers, 256-byte aligned, owned by
  *   the call until it has run. */
 RESQ_API size_t resq_paged_attention_workspace_bytes(int64_t T, int64_t count, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_new);

@@ -4,19 +4,26 @@
 // A tile is two halves of up to 128 query rows (tokens times the heads that share a kv head, whole tokens per half), the keys come
 // in tiles of 128.  Scores S = Q K^T of a half fill 128 columns of tensor memory, its softmax warps replace them by the weights P
 // (bf16, in the same columns), which are the A operand of O += P V from there; S and O of both halves are all 512 columns.  While the
-// warps of one half are at their exponentials the tensor cores have the other half's products to do, so the halves take
-// turns, with K and V read into shared memory once for both.
+// warps of one half are at their exponentials the tensor cores have the other half's products to do, with K and V read into
+// shared memory once for both.  An item with rows for one half only is worked on by both halves, on every second key tile each,
+// and their sums are joined at its end.
 //
-// Warps: 0-3 and 4-7 softmax of a half (a row per thread, so maxima and sums need no exchange), 8 issues the products, 9 deals out
-// segments and loads (a page's rows per copy, page numbers looked up by its lanes), 10 repairs the value tiles that reach past
-// the first row's last key: rows behind the last key become zeros (0 times what a page holds there may be NaN), and infinities
-// and NaN are taken out and added by those rows that do see them.
+// Warps: 0-3 and 4-7 softmax of a half (a row per thread, so maxima and sums need no exchange), 8 and 9 issue a half's products, 10
+// deals out segments and loads (a page's rows per copy, page numbers looked up by its lanes), 11 repairs the value tiles that reach
+// past the first row's last key: rows behind the last key become zeros (0 times what a page holds there may be NaN), and
+// infinities and NaN are taken out and added by those rows that do see them.
 //
-// O is rescaled only when a row's maximum has grown by more than 8 in the exponent of 2 since its reference was set: weights up
-// to 2^8 lose nothing in bf16 or in the fp32 sums, and the final division takes the reference out.
+// O is rescaled only when a row's maximum has grown by more than 20 in the exponent of 2 since its reference was set: weights up
+// to 2^20 lose nothing in bf16 or in the fp32 sums, and the final division takes the reference out.
+//
+// Measured: 8192 tokens from the beginning, 28 heads on 4 of 128, 571 us = 843 TFLOP/s (0.51 of the burst rate of a library product);
+// 512 tokens behind 31500 keys, 16 heads on 2, two sequences, 300 us = 876 TFLOP/s.  The products alone, with the weights left
+// as they lie, take 379 and 214 us: S = Q K^T is bound by the reads of both operands from shared memory (115 cycles an
+// instruction instead of 64).  The rest is the way from scores to weights: 512 cycles for a half's scores out of tensor memory and
+// their maxima, 1024 for its 16384 exponentials (16 a clock), 600 of hand-overs, of which the other half hides the part that its
+// own phase allows.
 #include "paged.cuh"
 #include "ptx.cuh"
-
 
 namespace resq {
 namespace {
@@ -153,280 +160,284 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
 
     // (The four warps of a group change their registers together, before they part.)
     if (warp >= kMmaWarp) {
-    fewer_registers<kOtherRegs>();
-    if (warp == kLoadWarp) {
-        // ------------------------------------------------------------------ segments, queries, keys and values
-        DealWalk walk;
-        walk.init(a.seq, a.deal, start);
-        Segment s;
-        int count = 0, q_uses[2] = {0, 0};
-        uint32_t pos = 0;                // key and value tiles so far
-        uint32_t raw = 0, raw_turn = 0;  // per stage: its tile goes to the repairs; parity of those that did
-        bool ok = true;
-        while (ok && walk.next(a.seq, a.deal, s)) {
-            const int e = count % kDescs;
-            if (!(ok = warp_wait(&sh.desc_empty[e], ((count / kDescs) & 1) ^ 1, abort_flag))) break;
-            ChunkSeg g;
-            g.b = s.b, g.q0 = s.s.q0, g.n = s.s.n, g.h = s.h, g.f0 = s.t * a.deal.rows;
-            g.past = s.s.kv - s.s.n, g.k_end = deal_k_end(s.s, a.deal, s.t);
-            const int tok0 = (int)div_by((uint32_t)g.f0, a.deal.by_g);
-            g.first_pos = g.past + tok0;
-            g.u0 = s.k0, g.end = s.k0;
-            g.slot = s.u0 == 0 && s.u1 == s.units ? -1 : 2 * cta + (s.u0 == 0 ? 1 : 0);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                g.rows[h] = max(0, min(p.half_rows, s.s.n * a.deal.g - g.f0 - h * p.half_rows));
-                const int last = min(tok0 + (h + 1) * p.half_tokens, s.s.n) - 1;  // last token of the half
-                const int k_end = max(0, min(g.past + last + 1, s.s.kv));
-                g.stop[h] = g.rows[h] == 0 ? s.k0 : max(s.k0, min(s.k1, (k_end + kKeys - 1) / kKeys));
-                g.end = max(g.end, g.stop[h]);
-            }
-            g.split = g.rows[1] == 0;
-            if (g.split) g.stop[1] = g.stop[0];
-            if (lane == 0) {
-                if (count == 0) a.notes[cta] = join_note(s, start, cta, g.f0);
-                sh.seg[e] = g;
-                for (int i = 0; i < kStrange * 4; ++i) sh.strange[e][i / 4][i % 4] = 0;
-                ptx::mbar_arrive(&sh.desc_full[e]);
-            }
-            __syncwarp();
-            // where this lane's piece of key tile u lies; asked for a tile ahead, since the answer takes as long as a copy
-            int page = 0, within = 0, next_page = 0, next_within = 0;
-            auto look = [&](int u) {
-                const int key = u * kKeys + lane * p.box;
-                if (lane * p.box < kKeys && key < g.k_end) {
-                    next_page = page_of(a.seq, g.b, key, next_within);
-                    if (next_page < 0) next_page = a.seq.pages;  // outside the cache: zeros
-                }
-            };
-            // one tile of keys or values
-            auto load = [&](int u, const CUtensorMap* m, bool special) {
-                const int st = pos % ST;
-                if (!warp_wait(&sh.kv_empty[st], ((pos / ST) & 1) ^ 1, abort_flag)) return false;
-                ++pos;
-                raw = special ? raw | 1u << st : raw & ~(1u << st);
-                raw_turn ^= (uint32_t)special << st;
-                uint64_t* const bar = special ? &sh.raw_full[st] : &sh.kv_full[st];
-                const int pieces = min(kKeys / p.box, (g.k_end - u * kKeys + p.box - 1) / p.box);
-                if (lane == 0) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(pieces * p.box * D * 2));
-                __syncwarp();
-                if (lane < pieces) {
-                    unsigned char* const dst = ring + st * TILE + lane * p.box * 128;
-#pragma unroll
-                    for (int c = 0; c < CG; ++c) ptx::tma_load_4d(dst + c * kKeys * 128, m, bar, c * 64, within, g.h, page);
-                }
-                __syncwarp();
-                return true;
-            };
-            auto special = [&](int u) { return u * kKeys + kKeys - 1 > g.first_pos; };
-            if (g.end > g.u0) {
-                look(g.u0);
-                page = next_page, within = next_within;
-                look(g.u0 + 1);
-                ok = load(g.u0, &maps.k, false);
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                // (a split segment's second half has no queries of its own; where it has keys, its sums use their room at the end)
-                if (!ok || g.stop[h] <= g.u0 + (h == 1 && g.split)) continue;
-                if (!(ok = warp_wait(&sh.q_empty[h], (q_uses[h] & 1) ^ 1, abort_flag))) continue;
-                ++q_uses[h];
-                if (lane == 0 && (h == 0 || !g.split)) {
-                    ptx::mbar_arrive_expect_tx(&sh.q_full[h], (uint32_t)(p.half_rows * D * 2));
-#pragma unroll
-                    for (int c = 0; c < CG; ++c)
-                        ptx::tma_load_3d(q_smem + h * QH + c * kHalf * 128, &maps.q, &sh.q_full[h], c * 64, g.h * a.deal.g, g.q0 + tok0 + h * p.half_tokens);
-                }
-                __syncwarp();
-            }
-            for (int u = g.u0; ok && u < g.end; ++u) {
-                ok = load(u, &maps.v, special(u));
-                if (!ok || u + 1 == g.end) continue;
-                page = next_page, within = next_within;
-                look(u + 2);
-                ok = load(u + 1, &maps.k, false);
-            }
-            ++count;
-        }
-        if (lane == 0) {
-            if (count == 0 && ok) a.notes[cta].parts = 0;
-            if (!ok) {
-                chunk_timeout(a.status, 1);
-                // copies in flight write to this CTA's shared memory: wait for them, with a limit
-                for (uint32_t q = pos > ST ? pos - ST : 0; q < pos; ++q) {
-                    const int st = q % ST;
-                    for (int i = 0; i < 4096; ++i) {
-                        if ((raw >> st) & 1 ? ptx::mbar_test_wait(&sh.raw_full[st], ((raw_turn >> st) & 1) ^ 1) : ptx::mbar_test_wait(&sh.kv_full[st], (q / ST) & 1)) break;
-                        __nanosleep(100);
-                    }
-                }
-            } else {
-                // an empty description ends the others' loops
-                const int e = count % kDescs;
-                if (ptx::mbar_wait_spin(&sh.desc_empty[e], ((count / kDescs) & 1) ^ 1, abort_flag)) {
-                    sh.seg[e].b = -1;
-                    ptx::mbar_arrive(&sh.desc_full[e]);
-                } else chunk_timeout(a.status, 2);
-            }
-        }
-    } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
-        // ------------------------------------------------------------------ products of a half
-        // Few products are taken ahead of their execution: a thread that waits leaves the tensor cores idle unless another one has
-        // products for them.  So each half has a thread of its own.
-        if (lane == 0) {
-            const int h = warp - kMmaWarp;
-            constexpr uint32_t s_idesc = ptx::idesc_bf16_f32(128, kKeys), o_idesc = ptx::idesc_bf16_f32_bmn(128, D);
-            const uint64_t q_desc = ptx::smem_desc_sw128_kmajor(ptx::smem_u32(q_smem));
-            const uint64_t k_desc = ptx::smem_desc_sw128_kmajor(ptx::smem_u32(ring)), v_desc = ptx::smem_desc_sw128_mnmajor(ptx::smem_u32(ring), kKeys * 128);
-            const uint32_t s_at = tmem + h * 128, o_at = tmem + 256 + h * D;
-            uint32_t pos = 0;  // of the segment's first key tile; tile i's values are at pos + 2 i + 1, tile i + 1's keys behind them
-            uint32_t q_uses[2] = {0, 0}, p_uses = 0;
+        fewer_registers<kOtherRegs>();
+        if (warp == kLoadWarp) {
+            // ------------------------------------------------------------------ segments, queries, keys and values
+            DealWalk walk;
+            walk.init(a.seq, a.deal, start);
+            Segment s;
+            int count = 0, q_uses[2] = {0, 0}, q_loads[2] = {0, 0};
+            uint32_t pos = 0;                // key and value tiles so far
+            uint32_t raw = 0, raw_turn = 0;  // per stage: its tile goes to the repairs; parity of those that did
             bool ok = true;
-            auto wait = [&](uint64_t* bar, uint32_t parity) { return ptx::mbar_wait_spin(bar, parity, abort_flag); };
-            auto full = [&](uint32_t at) { return wait(&sh.kv_full[at % ST], (at / ST) & 1); };
-            auto scores = [&](uint64_t q_desc, uint32_t k_pos) {
-                const uint64_t kd = k_desc + (uint64_t)((k_pos % ST) * (TILE >> 4));
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint64_t off = (uint64_t)(((k / 4) * kHalf * 128 + (k % 4) * 32) >> 4);
-                    ptx::umma_bf16(s_at, q_desc + off, kd + off, s_idesc, k > 0);
-                }
-                ptx::umma_commit(&sh.s_full[h]);
-            };
-            auto values = [&](uint32_t v_pos, int part, bool add) {  // keys 64 part .. + 63 of the tile
-                const uint64_t vd = v_desc + (uint64_t)((v_pos % ST) * (TILE >> 4));
-#pragma unroll
-                for (int k = part * 4; k < part * 4 + 4; ++k)
-                    ptx::umma_bf16_ta(o_at, s_at + k * 8, vd + (uint64_t)((k * 2048) >> 4), o_idesc, add || k > part * 4);
-            };
-            // tiles this half has no use for: given back once they are there (before, the arrival could count for the buffer's turn before)
-            auto skip = [&](uint32_t from, uint32_t to) {
-                for (; from < to; ++from) {
-                    if (!full(from)) return false;
-                    ptx::mbar_arrive(&sh.kv_empty[from % ST]);
-                }
-                return true;
-            };
-            for (int count = 0; ok; ++count) {
+            while (ok && walk.next(a.seq, a.deal, s)) {
                 const int e = count % kDescs;
-                if (!(ok = wait(&sh.desc_full[e], (count / kDescs) & 1))) break;
-                if (sh.seg[e].b < 0) break;
-                const int u0 = sh.seg[e].u0, tiles = sh.seg[e].end - u0, split = sh.seg[e].split;
-                const int step = split ? 2 : 1, first = split ? h : 0, end = sh.seg[e].stop[h] - u0;  // tiles first, first + step .. below end
-                const int from = split ? 0 : h;                                                        // whose queries
-                const uint64_t qd = q_desc + (uint64_t)(from * (QH >> 4));
-                // the other half's queries
-                if (h == 1 && (!split || first >= end) && sh.seg[e].stop[0] > u0) {
-                    if (!(ok = wait(&sh.q_full[0], q_uses[0] & 1))) break;
-                    ptx::mbar_arrive(&sh.q_empty[0]);
+                if (!(ok = warp_wait(&sh.desc_empty[e], ((count / kDescs) & 1) ^ 1, abort_flag))) break;
+                ChunkSeg g;
+                g.b = s.b, g.q0 = s.s.q0, g.n = s.s.n, g.h = s.h, g.f0 = s.t * a.deal.rows;
+                g.past = s.s.kv - s.s.n, g.k_end = deal_k_end(s.s, a.deal, s.t);
+                const int tok0 = (int)div_by((uint32_t)g.f0, a.deal.by_g);
+                g.first_pos = g.past + tok0;
+                g.u0 = s.k0, g.end = s.k0;
+                g.slot = s.u0 == 0 && s.u1 == s.units ? -1 : 2 * cta + (s.u0 == 0 ? 1 : 0);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    g.rows[h] = max(0, min(p.half_rows, s.s.n * a.deal.g - g.f0 - h * p.half_rows));
+                    const int last = min(tok0 + (h + 1) * p.half_tokens, s.s.n) - 1;  // last token of the half
+                    const int k_end = max(0, min(g.past + last + 1, s.s.kv));
+                    g.stop[h] = g.rows[h] == 0 ? s.k0 : max(s.k0, min(s.k1, (k_end + kKeys - 1) / kKeys));
+                    g.end = max(g.end, g.stop[h]);
                 }
-                uint32_t done = pos;  // tiles up to here are given back, or will be when the products with them are done
-                if (first < end) {
-                    const uint32_t at = pos + 2 * first;
-                    if (!(ok = skip(done, at) && full(at) && wait(&sh.q_full[from], q_uses[from] & 1))) break;
-                    ptx::tc_fence_after();
-                    scores(qd, at);
-                    if (first + step >= end) ptx::umma_commit(&sh.q_empty[from]);
-                    ptx::umma_commit(&sh.kv_empty[at % ST]);
-                    done = at + 1;
+                g.split = g.rows[1] == 0;
+                if (g.split) g.stop[1] = g.stop[0];
+                if (lane == 0) {
+                    if (count == 0) a.notes[cta] = join_note(s, start, cta, g.f0);
+                    sh.seg[e] = g;
+                    for (int i = 0; i < kStrange * 4; ++i) sh.strange[e][i / 4][i % 4] = 0;
+                    ptx::mbar_arrive(&sh.desc_full[e]);
                 }
-                for (int i = first; ok && i < end; i += step) {
-                    const uint32_t v_pos = pos + 2 * i + 1, k_pos = v_pos + 2 * step - 1;
-                    const bool more = i + step < end;
-                    // The tiles first: they are there by then, and asking costs time that the weights would wait for.  (The next keys of a
-                    // split segment are four tiles on, which may have to wait for the room of these values.)
-                    if (!(ok = full(v_pos) && (!more || split || full(k_pos)))) break;
-                    if (!(ok = wait(&sh.p_full[h][0], p_uses & 1))) break;
-                    ptx::tc_fence_after();
-                    values(v_pos, 0, i > first);
-                    if (!(ok = wait(&sh.p_full[h][1], p_uses & 1))) break;
-                    ++p_uses;
-                    ptx::tc_fence_after();
-                    values(v_pos, 1, true);
-                    if (more && !split) {
+                __syncwarp();
+                // where this lane's piece of key tile u lies; asked for a tile ahead, since the answer takes as long as a copy
+                int page = 0, within = 0, next_page = 0, next_within = 0;
+                auto look = [&](int u) {
+                    const int key = u * kKeys + lane * p.box;
+                    if (lane * p.box < kKeys && key < g.k_end) {
+                        next_page = page_of(a.seq, g.b, key, next_within);
+                        if (next_page < 0) next_page = a.seq.pages;  // outside the cache: zeros
+                    }
+                };
+                // one tile of keys or values
+                auto load = [&](int u, const CUtensorMap* m, bool special) {
+                    const int st = pos % ST;
+                    if (!warp_wait(&sh.kv_empty[st], ((pos / ST) & 1) ^ 1, abort_flag)) return false;
+                    ++pos;
+                    raw = special ? raw | 1u << st : raw & ~(1u << st);
+                    raw_turn ^= (uint32_t)special << st;
+                    uint64_t* const bar = special ? &sh.raw_full[st] : &sh.kv_full[st];
+                    const int pieces = min(kKeys / p.box, (g.k_end - u * kKeys + p.box - 1) / p.box);
+                    if (lane == 0) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(pieces * p.box * D * 2));
+                    __syncwarp();
+                    if (lane < pieces) {
+                        unsigned char* const dst = ring + st * TILE + lane * p.box * 128;
+#pragma unroll
+                        for (int c = 0; c < CG; ++c) ptx::tma_load_4d(dst + c * kKeys * 128, m, bar, c * 64, within, g.h, page);
+                    }
+                    __syncwarp();
+                    return true;
+                };
+                auto special = [&](int u) { return u * kKeys + kKeys - 1 > g.first_pos; };
+                if (g.end > g.u0) {
+                    look(g.u0);
+                    page = next_page, within = next_within;
+                    look(g.u0 + 1);
+                    ok = load(g.u0, &maps.k, false);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    // (a split segment's second half has no queries of its own; where it has keys, its sums use their room at the end)
+                    if (!ok || g.stop[h] <= g.u0 + (h == 1 && g.split)) continue;
+                    if (!(ok = warp_wait(&sh.q_empty[h], (q_uses[h] & 1) ^ 1, abort_flag))) continue;
+                    ++q_uses[h];
+                    if (h == 1 && g.split) continue;
+                    ++q_loads[h];
+                    if (lane == 0) {
+                        ptx::mbar_arrive_expect_tx(&sh.q_full[h], (uint32_t)(p.half_rows * D * 2));
+#pragma unroll
+                        for (int c = 0; c < CG; ++c)
+                            ptx::tma_load_3d(q_smem + h * QH + c * kHalf * 128, &maps.q, &sh.q_full[h], c * 64, g.h * a.deal.g, g.q0 + tok0 + h * p.half_tokens);
+                    }
+                    __syncwarp();
+                }
+                for (int u = g.u0; ok && u < g.end; ++u) {
+                    ok = load(u, &maps.v, special(u));
+                    if (!ok || u + 1 == g.end) continue;
+                    page = next_page, within = next_within;
+                    look(u + 2);
+                    ok = load(u + 1, &maps.k, false);
+                }
+                ++count;
+            }
+            if (lane == 0) {
+                if (count == 0 && ok) a.notes[cta].parts = 0;
+                if (!ok) {
+                    chunk_timeout(a.status, 1);
+                    // copies in flight write to this CTA's shared memory: wait for them, with a limit
+                    for (int h = 0; h < 2; ++h)
+                        for (int i = 0; q_loads[h] > 0 && i < 4096 && !ptx::mbar_test_wait(&sh.q_full[h], (q_loads[h] - 1) & 1); ++i) __nanosleep(100);
+                    for (uint32_t q = pos > ST ? pos - ST : 0; q < pos; ++q) {
+                        const int st = q % ST;
+                        for (int i = 0; i < 4096; ++i) {
+                            if ((raw >> st) & 1 ? ptx::mbar_test_wait(&sh.raw_full[st], ((raw_turn >> st) & 1) ^ 1) : ptx::mbar_test_wait(&sh.kv_full[st], (q / ST) & 1)) break;
+                            __nanosleep(100);
+                        }
+                    }
+                } else {
+                    // an empty description ends the others' loops
+                    const int e = count % kDescs;
+                    if (ptx::mbar_wait_spin(&sh.desc_empty[e], ((count / kDescs) & 1) ^ 1, abort_flag)) {
+                        sh.seg[e].b = -1;
+                        ptx::mbar_arrive(&sh.desc_full[e]);
+                    } else chunk_timeout(a.status, 2);
+                }
+            }
+        } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+            // ------------------------------------------------------------------ products of a half
+            // Few products are taken ahead of their execution: a thread that waits leaves the tensor cores idle unless another one has
+            // products for them.  So each half has a thread of its own.
+            if (lane == 0) {
+                const int h = warp - kMmaWarp;
+                constexpr uint32_t s_idesc = ptx::idesc_bf16_f32(128, kKeys), o_idesc = ptx::idesc_bf16_f32_bmn(128, D);
+                const uint64_t q_desc = ptx::smem_desc_sw128_kmajor(ptx::smem_u32(q_smem));
+                const uint64_t k_desc = ptx::smem_desc_sw128_kmajor(ptx::smem_u32(ring)), v_desc = ptx::smem_desc_sw128_mnmajor(ptx::smem_u32(ring), kKeys * 128);
+                const uint32_t s_at = tmem + h * 128, o_at = tmem + 256 + h * D;
+                uint32_t pos = 0;  // of the segment's first key tile; tile i's values are at pos + 2 i + 1, tile i + 1's keys behind them
+                uint32_t q_uses[2] = {0, 0}, p_uses = 0;
+                bool ok = true;
+                auto wait = [&](uint64_t* bar, uint32_t parity) { return ptx::mbar_wait_spin(bar, parity, abort_flag); };
+                auto full = [&](uint32_t at) { return wait(&sh.kv_full[at % ST], (at / ST) & 1); };
+                auto scores = [&](uint64_t q_desc, uint32_t k_pos) {
+                    const uint64_t kd = k_desc + (uint64_t)((k_pos % ST) * (TILE >> 4));
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint64_t off = (uint64_t)(((k / 4) * kHalf * 128 + (k % 4) * 32) >> 4);
+                        ptx::umma_bf16(s_at, q_desc + off, kd + off, s_idesc, k > 0);
+                    }
+                    ptx::umma_commit(&sh.s_full[h]);
+                };
+                auto values = [&](uint32_t v_pos, int part, bool add) {  // keys 64 part .. + 63 of the tile
+                    const uint64_t vd = v_desc + (uint64_t)((v_pos % ST) * (TILE >> 4));
+#pragma unroll
+                    for (int k = part * 4; k < part * 4 + 4; ++k)
+                        ptx::umma_bf16_ta(o_at, s_at + k * 8, vd + (uint64_t)((k * 2048) >> 4), o_idesc, add || k > part * 4);
+                };
+                // tiles this half has no use for: given back once they are there (before, the arrival could count for the buffer's turn before)
+                auto skip = [&](uint32_t from, uint32_t to) {
+                    for (; from < to; ++from) {
+                        if (!full(from)) return false;
+                        ptx::mbar_arrive(&sh.kv_empty[from % ST]);
+                    }
+                    return true;
+                };
+                for (int count = 0; ok; ++count) {
+                    const int e = count % kDescs;
+                    if (!(ok = wait(&sh.desc_full[e], (count / kDescs) & 1))) break;
+                    if (sh.seg[e].b < 0) break;
+                    const int u0 = sh.seg[e].u0, tiles = sh.seg[e].end - u0, split = sh.seg[e].split;
+                    const int step = split ? 2 : 1, first = split ? h : 0, end = sh.seg[e].stop[h] - u0;  // tiles first, first + step .. below end
+                    const int from = split ? 0 : h;                                                        // whose queries
+                    const uint64_t qd = q_desc + (uint64_t)(from * (QH >> 4));
+                    // the other half's queries
+                    if (h == 1 && (!split || first >= end) && sh.seg[e].stop[0] > u0) {
+                        if (!(ok = wait(&sh.q_full[0], q_uses[0] & 1))) break;
+                        ptx::mbar_arrive(&sh.q_empty[0]);
+                    }
+                    uint32_t done = pos;  // tiles up to here are given back, or will be when the products with them are done
+                    if (first < end) {
+                        const uint32_t at = pos + 2 * first;
+                        if (!(ok = skip(done, at) && full(at) && wait(&sh.q_full[from], q_uses[from] & 1))) break;
+                        ptx::tc_fence_after();
+                        scores(qd, at);
+                        if (first + step >= end) ptx::umma_commit(&sh.q_empty[from]);
+                        ptx::umma_commit(&sh.kv_empty[at % ST]);
+                        done = at + 1;
+                    }
+                    for (int i = first; ok && i < end; i += step) {
+                        const uint32_t v_pos = pos + 2 * i + 1, k_pos = v_pos + 2 * step - 1;
+                        const bool more = i + step < end;
+                        // The tiles first: they are there by then, and asking costs time that the weights would wait for.  (The next keys of a
+                        // split segment are four tiles on, which may have to wait for the room of these values.)
+                        if (!(ok = full(v_pos) && (!more || split || full(k_pos)))) break;
+                        if (!(ok = wait(&sh.p_full[h][0], p_uses & 1))) break;
+                        ptx::tc_fence_after();
+                        values(v_pos, 0, i > first);
+                        if (!(ok = wait(&sh.p_full[h][1], p_uses & 1))) break;
+                        ++p_uses;
+                        ptx::tc_fence_after();
+                        values(v_pos, 1, true);
+                        if (more && !split) {
+                            scores(qd, k_pos);
+                            if (i + 2 * step >= end) ptx::umma_commit(&sh.q_empty[from]);
+                            ptx::umma_commit(&sh.kv_empty[v_pos % ST]);
+                            ptx::umma_commit(&sh.kv_empty[k_pos % ST]);
+                            done = k_pos + 1;
+                            continue;
+                        }
+                        if (!more) ptx::umma_commit(&sh.o_full[h]);
+                        ptx::umma_commit(&sh.kv_empty[v_pos % ST]);
+                        done = v_pos + 1;
+                        if (!more) break;
+                        if (!(ok = skip(done, k_pos) && full(k_pos))) break;
+                        ptx::tc_fence_after();
                         scores(qd, k_pos);
                         if (i + 2 * step >= end) ptx::umma_commit(&sh.q_empty[from]);
-                        ptx::umma_commit(&sh.kv_empty[v_pos % ST]);
                         ptx::umma_commit(&sh.kv_empty[k_pos % ST]);
                         done = k_pos + 1;
-                        continue;
                     }
-                    if (!more) ptx::umma_commit(&sh.o_full[h]);
-                    ptx::umma_commit(&sh.kv_empty[v_pos % ST]);
-                    done = v_pos + 1;
-                    if (!more) break;
-                    if (!(ok = skip(done, k_pos) && full(k_pos))) break;
-                    ptx::tc_fence_after();
-                    scores(qd, k_pos);
-                    if (i + 2 * step >= end) ptx::umma_commit(&sh.q_empty[from]);
-                    ptx::umma_commit(&sh.kv_empty[k_pos % ST]);
-                    done = k_pos + 1;
+                    ok = ok && skip(done, pos + 2 * tiles);
+                    if (sh.seg[e].stop[0] > u0) ++q_uses[0];
+                    if (!split && sh.seg[e].stop[1] > u0) ++q_uses[1];
+                    pos += 2 * tiles;
+                    if (ok) ptx::mbar_arrive(&sh.desc_empty[e]);
                 }
-                ok = ok && skip(done, pos + 2 * tiles);
-                if (sh.seg[e].stop[0] > u0) ++q_uses[0];
-                if (!split && sh.seg[e].stop[1] > u0) ++q_uses[1];
-                pos += 2 * tiles;
-                if (ok) ptx::mbar_arrive(&sh.desc_empty[e]);
+                if (!ok) chunk_timeout(a.status, 3);
             }
-            if (!ok) chunk_timeout(a.status, 3);
-        }
-    } else if (warp == kFixWarp) {
-        // ------------------------------------------------------------------ repairs of value tiles
-        uint32_t pos = 0, raw_turn = 0;  // parity of the next repaired tile of each stage
-        bool ok = true;
-        for (int count = 0; ok; ++count) {
-            const int e = count % kDescs;
-            if (!(ok = warp_wait(&sh.desc_full[e], (count / kDescs) & 1, abort_flag))) break;
-            const ChunkSeg g = sh.seg[e];
-            if (g.b < 0) break;
-            const int us = max(g.u0, (max(g.first_pos, -1) + 1) / kKeys);  // first tile that reaches past the first row's last key
-            for (int u = us; ok && u < g.end; ++u) {
-                const uint32_t at = pos + 2 * (u - g.u0) + 1;
-                const int st = at % ST;
-                if (!(ok = warp_wait(&sh.raw_full[st], (raw_turn >> st) & 1, abort_flag))) break;
-                raw_turn ^= 1u << st;
-                unsigned char* const tile = ring + st * TILE;
-                const int key0 = u * kKeys, valid = min(kKeys, g.k_end - key0);
-                for (int i = lane; i < (kKeys - valid) * CG * 8; i += 32) {
-                    const int r = valid + i / (CG * 8), c = i % (CG * 8);
-                    *reinterpret_cast<uint4*>(tile + (c / 8) * kKeys * 128 + r * 128 + (c % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                }
-                const int lo = max(0, g.first_pos + 1 - key0);
-                const int chunks = (valid - lo) * CG * 8;
-                for (int base = lane; base < chunks; base += 32 * 8) {
-                    uint4 x[8];
-                    auto place = [&](int n) {
-                        const int i = base + n * 32, r = lo + i / (CG * 8), c = i % (CG * 8);
-                        return reinterpret_cast<uint4*>(tile + (c / 8) * kKeys * 128 + r * 128 + (c % 8) * 16);
-                    };
+        } else if (warp == kFixWarp) {
+            // ------------------------------------------------------------------ repairs of value tiles
+            uint32_t pos = 0, raw_turn = 0;  // parity of the next repaired tile of each stage
+            bool ok = true;
+            for (int count = 0; ok; ++count) {
+                const int e = count % kDescs;
+                if (!(ok = warp_wait(&sh.desc_full[e], (count / kDescs) & 1, abort_flag))) break;
+                const ChunkSeg g = sh.seg[e];
+                if (g.b < 0) break;
+                const int us = max(g.u0, (max(g.first_pos, -1) + 1) / kKeys);  // first tile that reaches past the first row's last key
+                for (int u = us; ok && u < g.end; ++u) {
+                    const uint32_t at = pos + 2 * (u - g.u0) + 1;
+                    const int st = at % ST;
+                    if (!(ok = warp_wait(&sh.raw_full[st], (raw_turn >> st) & 1, abort_flag))) break;
+                    raw_turn ^= 1u << st;
+                    unsigned char* const tile = ring + st * TILE;
+                    const int key0 = u * kKeys, valid = min(kKeys, g.k_end - key0);
+                    for (int i = lane; i < (kKeys - valid) * CG * 8; i += 32) {
+                        const int r = valid + i / (CG * 8), c = i % (CG * 8);
+                        *reinterpret_cast<uint4*>(tile + (c / 8) * kKeys * 128 + r * 128 + (c % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    const int lo = max(0, g.first_pos + 1 - key0);
+                    const int chunks = (valid - lo) * CG * 8;
+                    for (int base = lane; base < chunks; base += 32 * 8) {
+                        uint4 x[8];
+                        auto place = [&](int n) {
+                            const int i = base + n * 32, r = lo + i / (CG * 8), c = i % (CG * 8);
+                            return reinterpret_cast<uint4*>(tile + (c / 8) * kKeys * 128 + r * 128 + (c % 8) * 16);
+                        };
 #pragma unroll
-                    for (int n = 0; n < 8; ++n) x[n] = base + n * 32 < chunks ? *place(n) : make_uint4(0u, 0u, 0u, 0u);
+                        for (int n = 0; n < 8; ++n) x[n] = base + n * 32 < chunks ? *place(n) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                    for (int n = 0; n < 8; ++n)
-                        if (strange_pair(x[n].x) || strange_pair(x[n].y) || strange_pair(x[n].z) || strange_pair(x[n].w)) {
-                            const int r = lo + (base + n * 32) / (CG * 8);
-                            auto clean = [](uint32_t v) {
-                                if ((v & 0x7F80u) == 0x7F80u) v &= 0xFFFF0000u;
-                                if ((v & 0x7F800000u) == 0x7F800000u) v &= 0xFFFFu;
-                                return v;
-                            };
-                            *place(n) = make_uint4(clean(x[n].x), clean(x[n].y), clean(x[n].z), clean(x[n].w));
-                            if (u - us < kStrange) atomicOr(&sh.strange[e][u - us][r >> 5], 1u << (r & 31));
-                        }
+                        for (int n = 0; n < 8; ++n)
+                            if (strange_pair(x[n].x) || strange_pair(x[n].y) || strange_pair(x[n].z) || strange_pair(x[n].w)) {
+                                const int r = lo + (base + n * 32) / (CG * 8);
+                                auto clean = [](uint32_t v) {
+                                    if ((v & 0x7F80u) == 0x7F80u) v &= 0xFFFF0000u;
+                                    if ((v & 0x7F800000u) == 0x7F800000u) v &= 0xFFFFu;
+                                    return v;
+                                };
+                                *place(n) = make_uint4(clean(x[n].x), clean(x[n].y), clean(x[n].z), clean(x[n].w));
+                                if (u - us < kStrange) atomicOr(&sh.strange[e][u - us][r >> 5], 1u << (r & 31));
+                            }
+                    }
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&sh.kv_full[st]);
                 }
-                ptx::fence_proxy_async_smem();
+                pos += 2 * (g.end - g.u0);
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&sh.kv_full[st]);
+                if (ok && lane == 0) {
+                    ptx::mbar_arrive(&sh.strange_full[e]);
+                    ptx::mbar_arrive(&sh.desc_empty[e]);
+                }
             }
-            pos += 2 * (g.end - g.u0);
-            __syncwarp();
-            if (ok && lane == 0) {
-                ptx::mbar_arrive(&sh.strange_full[e]);
-                ptx::mbar_arrive(&sh.desc_empty[e]);
-            }
+            if (!ok && lane == 0) chunk_timeout(a.status, 4);
         }
-        if (!ok && lane == 0) chunk_timeout(a.status, 4);
-    }
     } else {
         more_registers<kSoftmaxRegs>();
         // ------------------------------------------------------------------ softmax: a row per thread
@@ -503,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     // the products before this tile's scores are done: O is this warp's
                     const float f2 = grown ? ex2(ref - m) : 1.0f;
                     if (grown) ref = m;
-                    again = true;  // (a reference of NaN stays below nothing)
+                    again = true;  // once: a reference of NaN would never do
                     sum2 = mul2(sum2, pair(f2, f2)), sum3 = mul2(sum3, pair(f2, f2));
                     if (u == u0) continue;
 #pragma unroll 1

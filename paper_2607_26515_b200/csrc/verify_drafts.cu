@@ -7,7 +7,8 @@
 //
 // The rows' sums are resq_token_logprobs' kernel, one pass over the logits, which is what the call is bound by.  This file's kernel
 // then needs one row per sequence again (of the logits, the draft's logits and e): a cluster of 1 to 8 CTAs per sequence finds the
-// row and takes the largest w / e of its slices.  Decisions next to a border are made again in 64 bits: a probability within 2^-14
+// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 47.5 us (rows 26, this kernel 21: its
+// 290 instructions per eight places are half of the issue slots); one such sequence 13.4 us, latency of both.  Decisions next to a border are made again in 64 bits: a probability within 2^-14
 // of its border, and a drawing whose second largest ratio is that close to its largest.
 #include "row_common.cuh"
 

@@ -155,6 +155,29 @@ def test_attention_many_sequences():
     check([(1, (i * 37) % 90) for i in range(4096)], 2, 1, 64, 8, seed=4)
 
 
+@pytest.mark.parametrize("lens", [[(1, 100)], [(1, 0)], [(1, 300), (1, 5), (1, 1000)], [(2, 129), (1, 0)], [(40, 77)]])
+@pytest.mark.parametrize("Hq, Hkv, D", [(128, 1, 64), (100, 1, 128), (130, 2, 64)])
+def test_attention_large_groups(lens, Hq, Hkv, D):
+    """More than 64 query heads per kv head: a single token fills half a tile."""
+    check(lens, Hq, Hkv, D, 16, seed=Hq)
+
+
+@pytest.mark.parametrize("n", [1, 12, 200])
+def test_attention_heads_that_share_their_keys_in_memory(n):
+    """A stride of 0, which tensor maps do not take."""
+    p = Paged([(n, 70), (n, 3)], 1, 64, 16)
+    wide = [c.expand(-1, -1, 3, -1) for c in (p.k, p.v)]
+    q = p.queries(9)
+    out = rq().paged_attention(q, *wide, p.q_start, p.kv_len, p.table)
+    p.k, p.v = wide
+    hold(out, None, q, p, 64 ** -0.5)
+
+
+@pytest.mark.parametrize("page", [40, 48, 136, 512])
+def test_attention_other_pages(page):
+    check([(3, 500), (70, 300), (130, 137)], 8, 2, 128, page, seed=page)
+
+
 def test_attention_strided_rows():
     check([(5, 100), (1, 30)], 6, 2, 128, 16, pad=4 * 128)
     p = Paged([(5, 100), (40, 30)], 2, 128, 16)
