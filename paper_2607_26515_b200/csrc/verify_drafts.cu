@@ -7,9 +7,11 @@
 //
 // The rows' sums are resq_token_logprobs' kernel, one pass over the logits, which is what the call is bound by.  This file's kernel
 // then needs one row per sequence again (of the logits, the draft's logits and e): a cluster of 1 to 8 CTAs per sequence finds the
-// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 47.5 us (rows 26, this kernel 21: its
-// 290 instructions per eight places are half of the issue slots); one such sequence 13.4 us, latency of both.  Decisions next to a border are made again in 64 bits: a probability within 2^-14
-// of its border, and a drawing whose second largest ratio is that close to its largest.
+// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 47.5 us (rows 26, this kernel
+// 21: its 290 instructions per eight places are half of the issue slots); one such sequence 13.4 us, latency of both.
+//
+// Decisions next to a border are made again in 64 bits: a probability next to its border, and a drawing whose second largest ratio is
+// next to its largest.  How near that is follows from what 32 bits can be off by (below).
 #include "row_common.cuh"
 
 #include <algorithm>
@@ -21,7 +23,12 @@ namespace {
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 256;
-constexpr float kNear = 6.103515625e-05f;  // 2^-14: the fast exponentials are within 2^-18 for arguments down to -40
+// A fast exponential is within 2^-22 and its argument x within 2^-23 |x|.  Weights down to 2^-126 count, so each of p and q is within
+// 2^-16 of itself, and mostly within 2^-19 (arguments of -10).  p - q is off by that part of p: within 2^-10 of itself where a
+// hundredth of p is left (where less is left, the fp32 log_sums, off by 2^-22, decide too).
+constexpr float kNear = 6.103515625e-05f, kNearLess = 9.765625e-04f;  // 2^-14; of p - q 2^-10
+// log p and log q are off by at most 2^-22 of themselves (three roundings each), which matters where both are far below 0.
+constexpr float kNearLog = 2.384185791015625e-07f;
 
 struct VerifyArgs {
     const void *logits, *draft_logits;
@@ -155,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
                 }
                 const float ratio = ex2((logp - logq) * kLog2e);
                 keep = u < ratio && logp > -kInf;
-                if (fabsf(u - ratio) <= kNear * ratio) {
+                if (fabsf(u - ratio) <= (kNear + kNearLog * (fabsf(logp) + fabsf(logq))) * ratio) {
                     const double lp = ((double)value(static_cast<const T*>(a.logits) + (int64_t)r * a.ld + x) - (double)a.peak[r]) * a.inv_t64 - (double)a.log_sum[r];
                     const double lq = DRAFT ? ((double)xd - (double)a.draft_peak[r]) * a.inv_t64 - (double)a.draft_log_sum[r] : 0.0;
                     keep = (double)u < exp(lp - lq) && logp > -kInf;
@@ -232,13 +239,14 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
         Best best{0.0f, a.V, 0.0f};
         bool minus = less;
         int skip = sure;
+        const float near = less ? kNearLess : kNear, window = 1.0f - 2.0f * near;
         for (int round = 0; round < 2; ++round) {
             best = Best{0.0f, a.V, 0.0f};
             // most are far below the largest that the warp has seen, and are not looked at one by one
             float seen = 0.0f;
             visit(minus, skip, [&](int j, const float (&s)[8], const float (&)[8], const float (&)[8], const float (&)[8]) {
                 const float all = warp_max(max3(max3(s[0], s[1], s[2]), max3(s[3], s[4], s[5]), fmaxf(s[6], s[7])));
-                if (!(all >= seen * (1.0f - 2.0f * kNear))) return;  // warp-uniform
+                if (!(all >= seen * window)) return;  // warp-uniform
                 seen = fmaxf(seen, all);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -254,9 +262,9 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
             if (cs > 1) cluster_sync();
             __syncthreads();
         }
-        if (best.j < a.V && best.next >= best.s * (1.0f - kNear)) {
+        if (best.j < a.V && best.next >= best.s * (1.0f - near)) {
             Best64 b64{0.0, a.V};
-            const float low = best.s * (1.0f - 2.0f * kNear);
+            const float low = best.s * window;
             visit(minus, skip, [&](int j, const float (&s)[8], const float (&z)[8], const float (&zd)[8], const float (&ev)[8]) {
 #pragma unroll 1
                 for (int i = 0; i < 8; ++i)

@@ -161,6 +161,53 @@ def test_verify_near_a_border_decides_in_64_bits():
     assert want[1] == [7] * 32
 
 
+@pytest.mark.parametrize("V", [200, 1000])
+def test_verify_draws_where_the_draft_is_close_to_the_target(V):
+    """p - q keeps less than a hundredth of p, so the ratios lose digits: thousands of draws, each the one that 64 bits make from the
+    same fp32 peaks and log_sums.  (Their own error in 64 bits is 1e-15 of p, far below the asserted distance of the two largest.)"""
+    B = 4096
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = (torch.randn((2 * B, V), generator=g, device="cuda") * 2)
+    d = x + 0.005 * torch.randn((2 * B, V), generator=g, device="cuda")
+    noise = torch.empty((B, V), device="cuda").exponential_(generator=g).clamp_min(1e-30)
+    none = torch.full((2 * B,), -1, dtype=torch.int64, device="cuda")
+    of_x, of_d = rq().token_logprobs(x, none), rq().token_logprobs(d, none)
+    p = ((x.double() - of_x["peak"].double()[:, None]) - of_x["log_sum"].double()[:, None]).exp()
+    q = ((d.double() - of_d["peak"].double()[:, None]) - of_d["log_sum"].double()[:, None]).exp()
+    drafts = (q / p).argmax(-1)  # refused: u is next to 1
+    got = rq().verify_drafts(x, torch.arange(0, 2 * B + 1, 2, dtype=torch.int32, device="cuda"), drafts,
+                             torch.full((2 * B,), 1 - 2.0 ** -20, device="cuda"), noise, d, of_d["peak"], of_d["log_sum"])
+    assert not got["accepted"].any()
+    ratio = (p - q).clamp_min(0)[::2] / noise.double()
+    two = ratio.topk(2, dim=-1)
+    assert (two.values[:, 0] > two.values[:, 1] * (1 + 1e-10)).all()
+    assert torch.equal(got["tokens"][::2], two.indices[:, 0])
+
+
+@pytest.mark.parametrize("T", [1e-3, 1e-4, 1e-5])
+def test_verify_far_drafts_by_64_bits(T):
+    """log p and log q of -1000 and below, where fp32 keeps too few digits of their difference: u next to the ratio."""
+    V = 64
+    for seed in range(32):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        x = torch.randn((2, V), generator=g, device="cuda") * 2
+        d = torch.randn((2, V), generator=g, device="cuda") * 2
+        none = torch.full((2,), -1, dtype=torch.int64, device="cuda")
+        of_d, of_x = rq().token_logprobs(d, none, T), rq().token_logprobs(x, none, T)
+        x[0, 5] = of_x["peak"][0] - 1.5
+        d[0, 5] = x[0, 5] - of_x["peak"][0] + of_d["peak"][0] + 0.4 * T
+        lp = (x[0, 5].double() - of_x["peak"][0].double()) / T - of_x["log_sum"][0].double()
+        lq = (d[0, 5].double() - of_d["peak"][0].double()) / T - of_d["log_sum"][0].double()
+        ratio = float((lp - lq).exp())
+        for step, kept in ((-2e-6, 1), (2e-6, 0)):
+            u = torch.full((2,), ratio * (1 + step), device="cuda")
+            if float(u[0]) >= 1:
+                continue
+            got = rq().verify_drafts(x, torch.tensor([0, 2], dtype=torch.int32, device="cuda"), torch.full((2,), 5, device="cuda"), u,
+                                     torch.ones((1, V), device="cuda"), d, of_d["peak"], of_d["log_sum"], T)
+            assert got["accepted"].tolist() == [kept]
+
+
 def test_verify_draws_from_the_target():
     """Kept and drawn first tokens together follow p: 40000 sequences of one draft over 12 tokens; each share within 5 of its
     standard deviations sqrt(p (1 - p) / n)."""
