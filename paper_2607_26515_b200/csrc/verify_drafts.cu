@@ -193,19 +193,24 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
         const int sure = !DRAFT && proposed ? (int)a.drafts[r] : -1;  // q is 1 there
         const bool less = DRAFT && proposed;
         const int v0 = min((int)rank * a.slice, (a.V + 7) / 8), v1 = min(v0 + a.slice, (a.V + 7) / 8);
-        // score(j): w / e in 32 bits, given the three values
-        auto weight = [&](float z, float zd, bool minus) {
-            const float p = ex2(fmaf(z - peak, c, add));
-            return minus ? fmaxf(p - ex2(fmaf(zd - dpeak, c, dadd)), 0.0f) : p;
+        const uint64_t c2 = pair(c, c), peak2 = pair(-peak, -peak), add2c = pair(add, add), dpeak2 = pair(-dpeak, -dpeak), dadd2 = pair(dadd, dadd);
+        const uint64_t minus1 = pair(-1.0f, -1.0f);
+        auto weights = [&](uint64_t z, uint64_t zd, bool minus) {  // of two places; below 0 where p < q
+            float l, h;
+            unpair(fma2(add2(z, peak2), c2, add2c), l, h);
+            const uint64_t p = pair(ex2(l), ex2(h));
+            if (!DRAFT || !minus) return p;
+            unpair(fma2(add2(zd, dpeak2), c2, dadd2), l, h);
+            return fma2(pair(ex2(l), ex2(h)), minus1, p);
         };
         auto weight64 = [&](float z, float zd, bool minus) {
             const double p = exp(((double)z - (double)peak) * a.inv_t64 - (double)log_sum);
             return minus ? fmax(p - exp(((double)zd - (double)dpeak) * a.inv_t64 - (double)a.draft_log_sum[r]), 0.0) : p;
         };
-        // take(j, ratios, logits, draft's logits, e) for eight of this thread's places after the other, the next ones' loads ahead; all
-        // lanes of a warp the same number of times.  Places behind the row's end and the one to be left out have a logit of -inf, that
-        // is a ratio of 0.
-        auto visit = [&](bool minus, int skip, auto&& take) {
+        // take(j, weights, logits, draft's logits, e) for eight of this thread's places after the other, the next ones' loads ahead;
+        // all lanes of a warp the same number of times, and only where a ratio of the warp reaches `floor` (w >= floor e, without a
+        // division).  Places behind the row's end and the one to be left out have a logit of -inf.
+        auto visit = [&](bool minus, int skip, const float& floor, auto&& take) {
             Raw8<T> rz, rd;
             Raw8<float> re;
             const int whole = min(v1, a.V / 8);
@@ -215,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
                 re.load(e + (int64_t)v * 8, m);
             };
             auto step = [&](int v, int m, int next) {
-                float z[8], zd[8] = {}, ev[8], s[8];
+                float z[8], zd[8] = {}, ev[8], w[8];
                 rz.get(z);
                 if (DRAFT && minus) rd.get(zd);
                 re.get(ev);
@@ -225,9 +230,15 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
                     for (int i = 0; i < 8; ++i)
                         if (i >= m || v * 8 + i == skip) z[i] = -kInf, ev[i] = 1.0f;
                 }
+                const uint64_t floor2 = pair(-floor, -floor);
+                float t[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s[i] = weight(z[i], zd[i], minus) * rcp(ev[i]);
-                take(v * 8, s, z, zd, ev);
+                for (int i = 0; i < 8; i += 2) {
+                    const uint64_t w2 = weights(pair(z[i], z[i + 1]), pair(zd[i], zd[i + 1]), minus);
+                    unpair(w2, w[i], w[i + 1]);
+                    unpair(fma2(pair(ev[i], ev[i + 1]), floor2, w2), t[i], t[i + 1]);
+                }
+                if (__any_sync(~0u, max3(max3(t[0], t[1], t[2]), max3(t[3], t[4], t[5]), fmaxf(t[6], t[7])) >= 0.0f)) take(v * 8, w, z, zd, ev);
             };
             if (v0 + tid < whole) fetch(v0 + tid, 8);
             for (int vw = v0 + (tid & ~31); vw < whole; vw += kThreads) step(vw + lane, vw + lane < whole ? 8 : 0, vw + lane + kThreads);
@@ -243,17 +254,17 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
         for (int round = 0; round < 2; ++round) {
             best = Best{0.0f, a.V, 0.0f};
             // most are far below the largest that the warp has seen, and are not looked at one by one
-            float seen = 0.0f;
-            visit(minus, skip, [&](int j, const float (&s)[8], const float (&)[8], const float (&)[8], const float (&)[8]) {
-                const float all = warp_max(max3(max3(s[0], s[1], s[2]), max3(s[3], s[4], s[5]), fmaxf(s[6], s[7])));
-                if (!(all >= seen * window)) return;  // warp-uniform
-                seen = fmaxf(seen, all);
+            float seen = 0.0f, floor = 0.0f;
+            visit(minus, skip, floor, [&](int j, const float (&w)[8], const float (&)[8], const float (&)[8], const float (&ev)[8]) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    best.next = fmaxf(best.next, fminf(s[i], best.s));
-                    best.j = s[i] > best.s ? j + i : best.j;  // in the order of places: equal ones keep the first
-                    best.s = fmaxf(best.s, s[i]);
+                    const float s = w[i] * rcp(ev[i]);
+                    best.next = fmaxf(best.next, fminf(s, best.s));
+                    best.j = s > best.s ? j + i : best.j;  // in the order of places: equal ones keep the first
+                    best.s = fmaxf(best.s, s);
                 }
+                seen = fmaxf(seen, warp_max(best.s));
+                floor = fminf(seen, 1e38f) * window;
             });
             best = cluster_best(best, warp_best, &cta_best, (int)cs);
             if (best.j < a.V || (!minus && skip < 0)) break;
@@ -264,11 +275,11 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
         }
         if (best.j < a.V && best.next >= best.s * (1.0f - near)) {
             Best64 b64{0.0, a.V};
-            const float low = best.s * window;
-            visit(minus, skip, [&](int j, const float (&s)[8], const float (&z)[8], const float (&zd)[8], const float (&ev)[8]) {
+            const float low = fminf(best.s, 1e38f) * window;
+            visit(minus, skip, low, [&](int j, const float (&w)[8], const float (&z)[8], const float (&zd)[8], const float (&ev)[8]) {
 #pragma unroll 1
                 for (int i = 0; i < 8; ++i)
-                    if (s[i] >= low) b64 = join(b64, Best64{weight64(z[i], zd[i], minus) / (double)ev[i], j + i});
+                    if (w[i] >= low * ev[i]) b64 = join(b64, Best64{weight64(z[i], zd[i], minus) / (double)ev[i], j + i});
             });
             best.j = cluster_best(b64, warp_best64, &cta_best64, (int)cs).j;
         }
