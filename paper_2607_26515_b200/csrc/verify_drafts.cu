@@ -7,8 +7,9 @@
 //
 // The rows' sums are resq_token_logprobs' kernel, one pass over the logits, which is what the call is bound by.  This file's kernel
 // then needs one row per sequence again (of the logits, the draft's logits and e): a cluster of 1 to 8 CTAs per sequence finds the
-// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 47.5 us (rows 26, this kernel
-// 21: its 290 instructions per eight places are half of the issue slots); one such sequence 13.4 us, latency of both.
+// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 43.1 us (rows and
+// both launches 27.6, the deciding row 2, the drawing 13.5 for 67 MB, 10.2 of them at the copy rate); one such sequence 13.8 us, latency of
+// both.
 //
 // Decisions next to a border are made again in 64 bits: a probability next to its border, and a drawing whose second largest ratio is
 // next to its largest.  How near that is follows from what 32 bits can be off by (below).
@@ -22,7 +23,7 @@ namespace {
 
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;  // at most
 // A fast exponential is within 2^-22 and its argument x within 2^-23 |x|.  Weights down to 2^-126 count, so each of p and q is within
 // 2^-16 of itself, and mostly within 2^-19 (arguments of -10).  p - q is off by that part of p: within 2^-10 of itself where a
 // hundredth of p is left (where less is left, the fp32 log_sums, off by 2^-22, decide too).
@@ -127,13 +128,13 @@ __device__ W cluster_best(W b, W* warps, W* mine, int cs) {
 }
 
 template <typename T, bool DRAFT, bool GREEDY>
-__global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_constant__ VerifyArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_constant__ VerifyArgs a) {
     __shared__ Best warp_best[kThreads / 32], cta_best;
     __shared__ Best64 warp_best64[kThreads / 32], cta_best64;
     uint32_t cs, rank = 0;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(cs));
     if (cs > 1) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    const int tid = threadIdx.x, lane = tid & 31, b = blockIdx.x / cs;
+    const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x, b = blockIdx.x / cs;
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0 && tid == 0) *a.status = DeviceStatus{RESQ_OK, 0, 0, 0};
@@ -241,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
                 if (__any_sync(~0u, max3(max3(t[0], t[1], t[2]), max3(t[3], t[4], t[5]), fmaxf(t[6], t[7])) >= 0.0f)) take(v * 8, w, z, zd, ev);
             };
             if (v0 + tid < whole) fetch(v0 + tid, 8);
-            for (int vw = v0 + (tid & ~31); vw < whole; vw += kThreads) step(vw + lane, vw + lane < whole ? 8 : 0, vw + lane + kThreads);
+            for (int vw = v0 + (tid & ~31); vw < whole; vw += threads) step(vw + lane, vw + lane < whole ? 8 : 0, vw + lane + threads);
             if (whole < v1 && tid < 32) {  // the ragged end of the row
                 if (lane == 0) fetch(whole, a.V - whole * 8);
                 step(whole, lane == 0 ? a.V - whole * 8 : 0, whole);
@@ -288,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
     }
     if (rank != 0) return;
     if (tid == 0) a.accepted[b] = kept;
-    for (int i = tid; i < n; i += kThreads) {
+    for (int i = tid; i < n; i += threads) {
         const bool k = i < kept;
         a.tokens[r0 + i] = k ? a.drafts[r0 + i] : i == kept ? token : -1;
         a.out_logp[r0 + i] = k ? (GREEDY ? a.best_logp[r0 + i] : a.logp[r0 + i]) : i == kept ? token_logp : 0.0f;
@@ -351,19 +352,29 @@ int resq_verify_drafts(const void* logits, int dtype, int64_t R, int64_t V, int6
     int rc = greedy ? token_logprobs_sliced(logits, dtype, R, V, ld, nullptr, 1.0f, 1, nullptr, nullptr, nullptr, nullptr, ids, wl, slices, stream)
                     : token_logprobs_sliced(logits, dtype, R, V, ld, drafts, temperature, 0, wl, nullptr, wp, ws_sum, nullptr, nullptr, slices, stream);
     if (rc) return rc;
-    // Few sequences: their row over a cluster, up to 592 CTAs (four per SM) and not below 4096 logits a CTA (two iterations of its
-    // threads).
+    // Few sequences: their row over a cluster, not below 4096 logits a CTA.  The 1024 threads that an SM holds are shared by the CTAs
+    // it gets, and the clusters are as large as it takes to keep most of them busy on the average: 64 sequences of 131072 take 43.1
+    // us by four CTAs of 512 threads each, 47.2 by eight of 256 (clusters of eight leave SMs of a GPC over) and 50.9 by four of
+    // 256; 100 sequences 50.3 by four of 320, 53.2 by two of 512.  Short rows get no more threads than vectors.
     int cs = 1;
-    while (!greedy && cs < 8 && count * cs * 2 <= 592 && vecs / (2 * cs) >= 512) cs *= 2;
+    unsigned threads = 128;
+    int64_t busy = 0;
+    for (int n = 1; n <= (greedy ? 1 : 8) && (n == 1 || (count * n <= 148 * 8 && vecs / n >= 512)); n *= 2) {
+        const int64_t per_sm = std::min<int64_t>(8, (count * n + 147) / 148), most = std::min<int64_t>(kThreads, 1024 / per_sm / 32 * 32);
+        if (n > 1 && count * n * most * 100 < busy * 106) continue;
+        busy = std::max(busy, count * n * most), cs = n;
+        if (!greedy) threads = (unsigned)std::min<int64_t>(most, std::max<int64_t>(64, ((vecs + n - 1) / n + 31) / 32 * 32));
+    }
+    const int64_t slice = (vecs + cs - 1) / cs;
     VerifyArgs a{logits, draft ? draft_logits : nullptr, ld, ldd, lde, row_start, drafts, u, noise, draft_peak, draft_log_sum, wl, wp, ws_sum, ids, wl,
-                 accepted, tokens, logp, reinterpret_cast<DeviceStatus*>(ws), (int)count, (int)R, (int)V, (int)((vecs + cs - 1) / cs), greedy ? 1.0f : 1.0f / temperature,
+                 accepted, tokens, logp, reinterpret_cast<DeviceStatus*>(ws), (int)count, (int)R, (int)V, (int)slice, greedy ? 1.0f : 1.0f / temperature,
                  greedy ? 1.0 : 1.0 / (double)temperature};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     using bf = __nv_bfloat16;
     auto kern = dtype == RESQ_OUT_F32 ? (greedy ? verify_kernel<float, false, true> : draft ? verify_kernel<float, true, false> : verify_kernel<float, false, false>)
                                       : (greedy ? verify_kernel<bf, false, true> : draft ? verify_kernel<bf, true, false> : verify_kernel<bf, false, false>);
     LaunchScope scope(kKindRow, st);
-    return cuda_fail(launch_clusters(kern, dim3((unsigned)(count * cs)), kThreads, 0, cs, st, a), "verify_kernel launch");
+    return cuda_fail(launch_clusters(kern, dim3((unsigned)(count * cs)), threads, 0, cs, st, a), "verify_kernel launch");
 }
 
 }  // extern "C"
