@@ -85,6 +85,14 @@ __device__ __forceinline__ void copy_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// A share of a row's keys has a reference and a sum (and a product).  One without weights is none: its product may not even be
+// written.  Any other counts, also where its weight is 0 beside a far larger reference: what it holds may be NaN or infinite, and
+// which keys share a part must not decide whether a row is.
+__device__ __forceinline__ bool no_share(float2 q) { return q.x == -kInf && q.y == 0.0f; }
+__device__ __forceinline__ float join_weight(float2 q, float ref) {
+    return q.x == -kInf ? (q.y == 0.0f ? 0.0f : 1.0f) : ex2(q.x - ref);  // a sum without a reference is one of NaN scores
+}
+
 template <int D>
 constexpr int rows_stages() { return D == 128 ? 3 : 6; }  // 24 KB of ring per warp
 template <int D, int MT>
@@ -316,8 +324,8 @@ __global__ void __launch_bounds__(kWarps * 32, kRowsCtasPerSm) attn_rows_kernel(
 #pragma unroll
             for (int x = 0; x < kWarps; ++x) {
                 const float2 p = ml[x * R + r];
-                const float f = p.x == -kInf ? (p.y == 0.0f ? 0.0f : 1.0f) : ex2(p.x - ref);  // a sum without a reference: NaN scores
-                if (f == 0.0f) continue;  // an underflown share is none, whatever it holds
+                if (no_share(p)) continue;
+                const float f = join_weight(p, ref);
                 sum = fmaf(f, p.y, sum);
                 const float* src = reinterpret_cast<const float*>(smem + R * D * 2 + x * S * kStage) + r * D + ((n ^ (r & 7)) * 8);
                 const float4 u = *reinterpret_cast<const float4*>(src), v = *reinterpret_cast<const float4*>(src + 4);
@@ -572,11 +580,8 @@ __global__ void __launch_bounds__(kWarps * 32, kRowsCtasPerSm) attn_wide_kernel(
     pdl_trigger();
 }
 
-// What the parts of an item weigh: by lane, parts `lane`, `lane` + 32, ... of row r; the largest reference is the same in all lanes.
+// Where part p of an item lies whose second CTA is `cta`, row r.
 __device__ __forceinline__ int64_t join_slot(int cta, int p, int R, int r) { return (int64_t)(p == 0 ? 2 * (cta - 1) + 1 : 2 * (cta - 1 + p)) * R + r; }
-__device__ __forceinline__ float join_weight(float2 q, float ref) {  // (a sum without a reference is one of NaN scores)
-    return q.x == -kInf ? (q.y == 0.0f ? 0.0f : 1.0f) : ex2(q.x - ref);
-}
 __device__ __forceinline__ void join_place(const AttnArgs& a, const JoinNote& note, int f, int64_t& row, int& head) {
     const int tok = (int)div_by((uint32_t)f, a.deal.by_g);
     head = note.h * a.deal.g + (f - tok * a.deal.g);
@@ -616,8 +621,8 @@ __device__ __forceinline__ void join_parts(const AttnArgs& a, int cta, int p0, i
         for (int e = 0; e < E; ++e) acc[e] *= f0;
 #pragma unroll
         for (int i = 0; i < kDeep; ++i) {
+            if (no_share(q[i])) continue;
             const float f = join_weight(q[i], ref);
-            if (f == 0.0f) continue;
             sum = fmaf(f, q[i].y, sum);
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[e] = fmaf(f, x[i][e], acc[e]);
@@ -672,8 +677,8 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
             for (int e = 0; e < E; ++e) acc[e] = 0.0f;
 #pragma unroll
             for (int i = 0; i < W; ++i) {
+                if (no_share(warp_ml[i])) continue;
                 const float f = join_weight(warp_ml[i], ref);
-                if (f == 0.0f) continue;
                 sum = fmaf(f, warp_ml[i].y, sum);
 #pragma unroll
                 for (int e = 0; e < E; ++e) acc[e] = fmaf(f, warp_o[i][lane * E + e], acc[e]);
@@ -718,8 +723,8 @@ __global__ void __launch_bounds__(D * 2) attn_join_tiles_kernel(const __grid_con
         for (int i = 0; i < 16; ++i) acc[i] *= f0;
 #pragma unroll
         for (int k = 0; k < kDeep; ++k) {
+            if (no_share(q[k])) continue;
             const float weight = join_weight(q[k], ref);
-            if (weight == 0.0f) continue;
             sum = fmaf(weight, q[k].y, sum);
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[i] = fmaf(weight, x[k][i], acc[i]);
