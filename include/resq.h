@@ -498,8 +498,8 @@ RESQ_API int resq_paged_attention(const void* Q_bf16, int64_t T, int64_t ldq, in
  *   the largest logit (equal ones: the lowest), which is also what replaces it; log-probabilities are then those of temperature 1.
  *   accepted int32 [count]: drafts kept; tokens int64 [R]: the kept drafts, the token behind them, then -1; logp fp32 [R]: log p of
  *   each of these tokens (0 beside -1).  A row of nothing but -inf, or with NaN or +inf, keeps nothing and yields -1.  A sequence
- *   without rows has accepted 0; rows of no sequence are not written.  Decisions near a border (2^-14, of p - q 2^-10) are
- *   made in 64 bits from the rows' fp32 peaks and log_sums.  workspace of resq_verify_drafts_workspace_bytes(R) bytes, 256-byte aligned. */
+ *   without rows has accepted 0; rows of no sequence are not written.  Decisions that 32 bits leave open are made in 64 bits from
+ *   the rows' fp32 peaks and log_sums: u next to its border, ratios next to each other, little or nothing left of p - q.  workspace of resq_verify_drafts_workspace_bytes(R) bytes, 256-byte aligned. */
 RESQ_API size_t resq_verify_drafts_workspace_bytes(int64_t R);
 RESQ_API int resq_verify_drafts(const void* logits, int dtype, int64_t R, int64_t V, int64_t ld, const int32_t* row_start, int64_t count,
                        const int64_t* drafts, const float* u, const float* noise, int64_t lde, const void* draft_logits, int64_t ldd,

@@ -7,12 +7,12 @@
 //
 // The rows' sums are resq_token_logprobs' kernel, one pass over the logits, which is what the call is bound by.  This file's kernel
 // then needs one row per sequence again (of the logits, the draft's logits and e): a cluster of 1 to 8 CTAs per sequence finds the
-// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 43.1 us (rows and
-// both launches 27.6, the deciding row 2, the drawing 13.5 for 67 MB, 10.2 of them at the copy rate); one such sequence 13.8 us, latency of
+// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 42.7 us (rows and
+// both launches 27.6, the deciding row 2, the drawing 13 for 67 MB, 10.2 of them at the copy rate); one such sequence 13.6 us, latency of
 // both.
 //
-// Decisions next to a border are made again in 64 bits: a probability next to its border, and a drawing whose second largest ratio is
-// next to its largest.  How near that is follows from what 32 bits can be off by (below).
+// Decisions that 32 bits leave open are made in 64 bits: a probability next to its border, and a drawing where another ratio may be
+// the largest, or where nothing may be left of p - q.  What 32 bits can be off by is below.
 #include "row_common.cuh"
 
 #include <algorithm>
@@ -24,12 +24,18 @@ namespace {
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 512;  // at most
-// A fast exponential is within 2^-22 and its argument x within 2^-23 |x|.  Weights down to 2^-126 count, so each of p and q is within
-// 2^-16 of itself, and mostly within 2^-19 (arguments of -10).  p - q is off by that part of p: within 2^-10 of itself where a
-// hundredth of p is left (where less is left, the fp32 log_sums, off by 2^-22, decide too).
-constexpr float kNear = 6.103515625e-05f, kNearLess = 9.765625e-04f;  // 2^-14; of p - q 2^-10
-// log p and log q are off by at most 2^-22 of themselves (three roundings each), which matters where both are far below 0.
-constexpr float kNearLog = 2.384185791015625e-07f;
+// The argument of an exponential of 2 is a sum of two terms of one sign with six roundings of 2^-24 at most on the way of each, and
+// weights down to 2^-126 count: it is off by 6 * 127 * 2^-24 = 4.6e-5 at most, and a fast exponential and log_sum / ln 2 add
+// 1.3e-6.  kSlack, 2^-14 in the exponent, is above that: 2^(y + kSlack) is an upper bound of p, 2^(y - kSlack) a lower one.
+constexpr float kSlack = 6.103515625e-05f;
+// Ratios p / e, off by less than 2^-14.5 of themselves each: the largest is the largest if the next one is this far below.
+constexpr float kNear = 6.103515625e-05f;
+// Ratios (p - q) / e have no such bound, since little may be left of p.  The pass takes upper bounds of p - q, leaves out what lies
+// more than kWide below the largest, and the largest's lower bound then says whether another one reaches it (or one left out may).
+// Where more than 1/370 of p is left it is mostly clear; with less the row is read again.
+constexpr float kWide = 0.0625f, kFold = 1.9073486328125e-06f;  // 2^-19: what the quotients and their bounds are rounded by, several times over
+// log p and log q are off by at most 7 * 2^-24 of themselves and of each other, which matters where both are far below 0.
+constexpr float kNearLog = 4.76837158203125e-07f;  // 2^-21
 
 struct VerifyArgs {
     const void *logits, *draft_logits;
@@ -127,6 +133,30 @@ __device__ W cluster_best(W b, W* warps, W* mine, int cs) {
     return b;
 }
 
+// This thread's largest ratio in 64 bits, among the places from j0 to j1 - 1 of row r whose ratio in 32 bits reaches `low`.  Rare:
+// kept out of the pass, whose registers it would take.
+template <typename T, bool DRAFT>
+__device__ __noinline__ Best64 best64(const VerifyArgs& a, int r, int b, int j0, int j1, bool minus, int skip, float low) {
+    const T* const x = static_cast<const T*>(a.logits) + (int64_t)r * a.ld;
+    const T* const xd = DRAFT ? static_cast<const T*>(a.draft_logits) + (int64_t)r * a.ldd : nullptr;
+    const float* const e = a.e + (int64_t)b * a.lde;
+    const float c = a.inv_t * kLog2e, peak = a.peak[r], log_sum = a.log_sum[r];
+    const float dpeak = DRAFT && minus ? a.draft_peak[r] : 0.0f, dlog_sum = DRAFT && minus ? a.draft_log_sum[r] : 0.0f;
+    const float add = -log_sum * kLog2e + kSlack, dadd = -dlog_sum * kLog2e - kSlack;
+    Best64 best{0.0, a.V};
+#pragma unroll 4
+    for (int j = j0 + (int)threadIdx.x; j < j1; j += (int)blockDim.x) {
+        const float z = value(x + j), zd = DRAFT && minus ? value(xd + j) : 0.0f, ev = e[j];
+        float w = ex2(fmaf(z - peak, c, add));
+        if (DRAFT && minus) w -= ex2(fmaf(zd - dpeak, c, dadd));
+        if (!(w >= low * ev) || j == skip) continue;
+        double w64 = exp(((double)z - (double)peak) * a.inv_t64 - (double)log_sum);
+        if (DRAFT && minus) w64 -= exp(((double)zd - (double)dpeak) * a.inv_t64 - (double)dlog_sum);
+        if (w64 > 0.0) best = join(best, Best64{w64 / (double)ev, j});
+    }
+    return best;
+}
+
 template <typename T, bool DRAFT, bool GREEDY>
 __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_constant__ VerifyArgs a) {
     __shared__ Best warp_best[kThreads / 32], cta_best;
@@ -189,57 +219,53 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
         const T* const x = static_cast<const T*>(a.logits) + (int64_t)r * a.ld;
         const T* const xd = DRAFT ? static_cast<const T*>(a.draft_logits) + (int64_t)r * a.ldd : nullptr;
         const float* const e = a.e + (int64_t)b * a.lde;
-        const float peak = a.peak[r], log_sum = a.log_sum[r], add = -log_sum * kLog2e;
-        const float dpeak = DRAFT ? a.draft_peak[r] : 0.0f, dadd = DRAFT ? -a.draft_log_sum[r] * kLog2e : 0.0f;
-        const int sure = !DRAFT && proposed ? (int)a.drafts[r] : -1;  // q is 1 there
         const bool less = DRAFT && proposed;
+        const float peak = a.peak[r], log_sum = a.log_sum[r], add = -log_sum * kLog2e + (less ? kSlack : 0.0f);
+        const float dpeak = DRAFT ? a.draft_peak[r] : 0.0f, dadd = DRAFT ? -a.draft_log_sum[r] * kLog2e - kSlack : 0.0f;
+        const int sure = !DRAFT && proposed ? (int)a.drafts[r] : -1;  // q is 1 there
         const int v0 = min((int)rank * a.slice, (a.V + 7) / 8), v1 = min(v0 + a.slice, (a.V + 7) / 8);
         const uint64_t c2 = pair(c, c), peak2 = pair(-peak, -peak), add2c = pair(add, add), dpeak2 = pair(-dpeak, -dpeak), dadd2 = pair(dadd, dadd);
         const uint64_t minus1 = pair(-1.0f, -1.0f);
-        auto weights = [&](uint64_t z, uint64_t zd, bool minus) {  // of two places; below 0 where p < q
+        auto weights = [&](uint64_t z, uint64_t zd) {  // of two places; of p - q upper bounds, below 0 where p < q
             float l, h;
             unpair(fma2(add2(z, peak2), c2, add2c), l, h);
             const uint64_t p = pair(ex2(l), ex2(h));
-            if (!DRAFT || !minus) return p;
+            if (!less) return p;
             unpair(fma2(add2(zd, dpeak2), c2, dadd2), l, h);
             return fma2(pair(ex2(l), ex2(h)), minus1, p);
         };
-        auto weight64 = [&](float z, float zd, bool minus) {
-            const double p = exp(((double)z - (double)peak) * a.inv_t64 - (double)log_sum);
-            return minus ? fmax(p - exp(((double)zd - (double)dpeak) * a.inv_t64 - (double)a.draft_log_sum[r]), 0.0) : p;
-        };
-        // take(j, weights, logits, draft's logits, e) for eight of this thread's places after the other, the next ones' loads ahead;
-        // all lanes of a warp the same number of times, and only where a ratio of the warp reaches `floor` (w >= floor e, without a
-        // division).  Places behind the row's end and the one to be left out have a logit of -inf.
-        auto visit = [&](bool minus, int skip, const float& floor, auto&& take) {
+        // take(j, weights, e) for eight of this thread's places after the other, the next ones' loads ahead; all lanes of a warp the
+        // same number of times, and only where a ratio of the warp reaches `floor` (w >= floor e, without a division).  Places
+        // behind the row's end and the one to be left out have a logit of -inf.
+        auto visit = [&](const float& floor, auto&& take) {
             Raw8<T> rz, rd;
             Raw8<float> re;
             const int whole = min(v1, a.V / 8);
             auto fetch = [&](int v, int m) {
                 rz.load(x + (int64_t)v * 8, m);
-                if (DRAFT && minus) rd.load(xd + (int64_t)v * 8, m);
+                if (less) rd.load(xd + (int64_t)v * 8, m);
                 re.load(e + (int64_t)v * 8, m);
             };
             auto step = [&](int v, int m, int next) {
                 float z[8], zd[8] = {}, ev[8], w[8];
                 rz.get(z);
-                if (DRAFT && minus) rd.get(zd);
+                if (less) rd.get(zd);
                 re.get(ev);
                 if (next < whole) fetch(next, 8);
-                if (m < 8 || skip >> 3 == v) {
+                if (m < 8 || sure >> 3 == v) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        if (i >= m || v * 8 + i == skip) z[i] = -kInf, ev[i] = 1.0f;
+                        if (i >= m || v * 8 + i == sure) z[i] = -kInf, ev[i] = 1.0f;
                 }
                 const uint64_t floor2 = pair(-floor, -floor);
                 float t[8];
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) {
-                    const uint64_t w2 = weights(pair(z[i], z[i + 1]), pair(zd[i], zd[i + 1]), minus);
+                    const uint64_t w2 = weights(pair(z[i], z[i + 1]), pair(zd[i], zd[i + 1]));
                     unpair(w2, w[i], w[i + 1]);
                     unpair(fma2(pair(ev[i], ev[i + 1]), floor2, w2), t[i], t[i + 1]);
                 }
-                if (__any_sync(~0u, max3(max3(t[0], t[1], t[2]), max3(t[3], t[4], t[5]), fmaxf(t[6], t[7])) >= 0.0f)) take(v * 8, w, z, zd, ev);
+                if (__any_sync(~0u, max3(max3(t[0], t[1], t[2]), max3(t[3], t[4], t[5]), fmaxf(t[6], t[7])) >= 0.0f)) take(v * 8, w, ev);
             };
             if (v0 + tid < whole) fetch(v0 + tid, 8);
             for (int vw = v0 + (tid & ~31); vw < whole; vw += threads) step(vw + lane, vw + lane < whole ? 8 : 0, vw + lane + threads);
@@ -249,40 +275,38 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
             }
         };
         Best best{0.0f, a.V, 0.0f};
-        bool minus = less;
-        int skip = sure;
-        const float near = less ? kNearLess : kNear, window = 1.0f - 2.0f * near;
-        for (int round = 0; round < 2; ++round) {
-            best = Best{0.0f, a.V, 0.0f};
-            // most are far below the largest that the warp has seen, and are not looked at one by one
-            float seen = 0.0f, floor = 0.0f;
-            visit(minus, skip, floor, [&](int j, const float (&w)[8], const float (&)[8], const float (&)[8], const float (&ev)[8]) {
+        const float window = 1.0f - (less ? kWide : 2.0f * kNear);
+        // most are far below the largest that the warp has seen, and are not looked at one by one
+        float seen = 0.0f, floor = 0.0f;
+        visit(floor, [&](int j, const float (&w)[8], const float (&ev)[8]) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float s = w[i] * rcp(ev[i]);
-                    best.next = fmaxf(best.next, fminf(s, best.s));
-                    best.j = s > best.s ? j + i : best.j;  // in the order of places: equal ones keep the first
-                    best.s = fmaxf(best.s, s);
-                }
-                seen = fmaxf(seen, warp_max(best.s));
-                floor = fminf(seen, 1e38f) * window;
-            });
-            best = cluster_best(best, warp_best, &cta_best, (int)cs);
-            if (best.j < a.V || (!minus && skip < 0)) break;
-            // nothing is left of p - q (p = q up to rounding): drawn from p
-            minus = false, skip = -1;
+            for (int i = 0; i < 8; ++i) {
+                const float s = w[i] * rcp(ev[i]);
+                best.next = fmaxf(best.next, fminf(s, best.s));
+                best.j = s > best.s ? j + i : best.j;  // in the order of places: equal ones keep the first
+                best.s = fmaxf(best.s, s);
+            }
+            seen = fmaxf(seen, warp_max(best.s));
+            floor = fminf(seen, 1e38f) * window;
+        });
+        best = cluster_best(best, warp_best, &cta_best, (int)cs);
+        const int j0 = v0 * 8, j1 = min(v1 * 8, a.V);
+        if (best.j < a.V) {
+            // any place that reaches `low` may be the largest
+            float low = fminf(best.s, 1e38f) * window;
+            bool open = best.next >= best.s * (1.0f - kNear);
+            if (less) {
+                const float least = ex2(fmaf(value(x + best.j) - peak, c, add) - 2.0f * kSlack) - ex2(fmaf(value(xd + best.j) - dpeak, c, dadd) + 2.0f * kSlack);
+                const float reach = least > 0.0f ? fminf(least * rcp(e[best.j]), 1e38f) * (1.0f - kFold) : 0.0f;
+                open = best.next >= reach || low > reach;
+                low = reach;
+            }
+            if (open) best.j = cluster_best(best64<T, DRAFT>(a, r, b, j0, j1, less, sure, low), warp_best64, &cta_best64, (int)cs).j;
+        }
+        if (best.j == a.V && (less || sure >= 0)) {  // nothing is left of p - q (p = q up to rounding): drawn from p
             if (cs > 1) cluster_sync();
             __syncthreads();
-        }
-        if (best.j < a.V && best.next >= best.s * (1.0f - near)) {
-            Best64 b64{0.0, a.V};
-            const float low = fminf(best.s, 1e38f) * window;
-            visit(minus, skip, low, [&](int j, const float (&w)[8], const float (&z)[8], const float (&zd)[8], const float (&ev)[8]) {
-#pragma unroll 1
-                for (int i = 0; i < 8; ++i)
-                    if (w[i] >= low * ev[i]) b64 = join(b64, Best64{weight64(z[i], zd[i], minus) / (double)ev[i], j + i});
-            });
-            best.j = cluster_best(b64, warp_best64, &cta_best64, (int)cs).j;
+            best.j = cluster_best(best64<T, DRAFT>(a, r, b, j0, j1, false, -1, 0.0f), warp_best64, &cta_best64, (int)cs).j;
         }
         if (best.j < a.V) token = best.j, token_logp = (value(x + best.j) - peak) * a.inv_t - log_sum;
         if (cs > 1) cluster_sync();  // a CTA's shared memory stays until the others have read it
