@@ -436,9 +436,10 @@ RESQ_API int resq_token_logprobs_backward(const void* logits, int dtype, int64_t
  *     keys, the new tokens' among them, so its i-th of n new tokens is key (and stands at position) kv_len[b] - n + i;
  *     page_table[b * ld_table + j] is the page of keys j * page_size ...
  *   The arrays are read on the device, so a captured call follows what they hold when it runs.  Whatever they hold, nothing is
- *   read or written out of range: starts are cut to 0 .. T (a sequence whose end lies before its start has no new tokens),
- *   lengths to 0 .. max_pages * page_size, and a page outside 0 .. pages - 1 is none: nothing is stored there, and its keys and
- *   values are read as zeros.  Rows behind the last sequence (and before the first) are neither read nor written.
+ *   read or written out of range: starts are cut to 0 .. T (a sequence whose end lies before its start has no new tokens; they need
+ *   not be in order, but a row belongs to one sequence at most), lengths to 0 .. max_pages * page_size, and a page outside 0 .. pages - 1
+ *   is none: nothing is stored there, and its keys and values are read as zeros.  Rows of no sequence, such as those behind the last
+ *   one, have no influence and are not written (they may be loaded).
  *   At most RESQ_MAX_SEQUENCES sequences, RESQ_MAX_GROUP_HEADS query heads per kv head, fewer than 2^31 keys per sequence. */
 #define RESQ_MAX_SEQUENCES 4096
 #define RESQ_MAX_GROUP_HEADS 128

@@ -49,13 +49,13 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
     const int nt = (int)min((int64_t)a.tokens, a.seq.T - t0);
     pdl_wait();
     pdl_trigger();
-    // ---- whose token it is: a warp looks for each token's sequence, 32 starts at a time
+    // ---- whose token it is: a warp looks for each token's sequence, among starts in order by 32 at a time
     if (w < nt) {
         const int tok = (int)t0 + w;
         int lo = 0, hi = a.seq.B;  // the last b in lo .. hi with q_start[b] <= tok
         while (hi > lo) {
             const int step = (hi - lo + 31) / 32, b = min(lo + 1 + lane * step, hi);
-            // Starts out of order would make the answers disagree: only their first run counts.
+            // Starts out of order make the answers disagree: only their first run counts here.
             const unsigned upto = __ballot_sync(~0u, a.seq.q_start[b] <= tok);
             const int n = upto == ~0u ? 32 : __ffs(~upto) - 1;
             const int at = n == 0 ? lo : min(lo + 1 + (n - 1) * step, hi);
@@ -66,16 +66,29 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
             }
             lo = at;
         }
+        Seq s{0, 0, 0};
+        if (lo < a.seq.B) s = load_seq(a.seq, lo);
+        // Starts out of order, or a row of no sequence: all of them are asked, eight loads of a lane in flight.
+        if (tok < s.q0 || tok - s.q0 >= s.n) {
+            lo = a.seq.B;
+            for (int b0 = 0; b0 < a.seq.B && lo == a.seq.B; b0 += 128) {
+                Seq each[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) each[k] = load_seq(a.seq, min(b0 + k * 32 + lane, a.seq.B - 1));
+#pragma unroll
+                for (int k = 3; k >= 0; --k) {
+                    const unsigned here = __ballot_sync(~0u, tok >= each[k].q0 && tok - each[k].q0 < each[k].n);
+                    if (here) lo = min(b0 + k * 32 + __ffs(here) - 1, a.seq.B - 1);
+                }
+            }
+            if (lo < a.seq.B) s = load_seq(a.seq, lo);
+        }
         Place p{0, 0, -1, 0};
         if (lo < a.seq.B) {
-            const Seq s = load_seq(a.seq, lo);
-            const int i = tok - s.q0;
-            if (i >= 0 && i < s.n) {
-                const int slot = s.kv - s.n + i;
-                p.there = 1;
-                p.pos = a.positions ? a.positions[tok] : slot;
-                if (slot >= 0) p.page = page_of(a.seq, lo, slot, p.row);
-            }
+            const int i = tok - s.q0, slot = s.kv - s.n + i;
+            p.there = 1;
+            p.pos = a.positions ? a.positions[tok] : slot;
+            if (slot >= 0) p.page = page_of(a.seq, lo, slot, p.row);
         }
         if (lane == 0) place[w] = p;
     }

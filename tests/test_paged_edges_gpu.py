@@ -3,7 +3,8 @@ attention as in test_paged_gpu.py)."""
 import pytest
 import torch
 
-from test_paged_gpu import BF, NAN, Paged, rq
+import paged_formulas as formulas
+from test_paged_gpu import BF, HALF_BF, NAN, U, Paged, freqs, ints, rq
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +50,39 @@ def test_attention_a_visible_strange_value_is_never_lost(n, keys, high, value):
         strange = ~torch.isfinite(out.view(n, 8, 128))
         assert strange[:, :4, 5].all() and int(strange.sum()) == 4 * n, hint
         assert torch.isfinite(lse).all()
+
+
+# ------------------------------------------------------------------------------------------------ starts out of order
+
+@pytest.mark.parametrize("starts, T", [([4, 9, 2, 4], 12), ([20, 3, 3, 0, 2, -4], 12), ([50, 60, 0, 9, 10, 40, 44], 70), ([5, 2 ** 31 - 1, -3, 2, 1, -2 ** 31], 9)])
+def test_append_starts_out_of_order(starts, T):
+    """Every sequence has the rows from its start to its end, wherever the others lie; the lists give each row to one sequence at most."""
+    B = len(starts) - 1
+    p = Paged([(2, 30)] * B, 2, 64, 8)
+    p.table = torch.cat([p.table, p.table.new_full((B, 10), -1)], 1)
+    p.k.nan_to_num_(0.5)
+    p.v.nan_to_num_(0.25)
+    qkv = torch.randn((T, 8 * 64), generator=p.g, device="cuda").to(BF)
+    q_start = ints(starts)
+    want = formulas.rope_append(qkv, None, p.k, p.v, starts, p.kv, p.table, freqs(64), False)
+    owned = sum(max(min(max(b, 0), T) - min(max(a, 0), T), 0) for a, b in zip(starts, starts[1:]))
+    there = ~torch.isnan(want[0])
+    assert int(there[:, 0].sum()) == owned > 0
+    q = torch.full((T, 4 * 64), 3.0, dtype=BF, device="cuda")
+    rq().rope_append(qkv, p.k, p.v, q_start, p.kv_len, p.table, freqs(64), q=q)
+    tol = lambda w: HALF_BF * w.abs() + 16 * U * 2 * float(qkv.abs().max())
+    assert ((q.double() - want[0]).abs() <= tol(want[0]))[there].all() and (q[~there] == 3).all()
+    assert ((p.k.double() - want[1]).abs() <= tol(want[1])).all() and ((p.v.double() - want[2]).abs() <= tol(want[2])).all()
+
+
+@pytest.mark.parametrize("B", [1, 40, 4096])
+def test_append_rows_behind_many_sequences(B):
+    """Rows of no sequence are looked for in all of them, and stay as they were."""
+    p = Paged([(i % 2, 3) for i in range(B)] if B > 1 else [(1, 3)], 1, 64, 8)
+    T = p.T + 21
+    qkv = torch.randn((T, 4 * 64), generator=p.g, device="cuda").to(BF)
+    q = torch.full((T, 2 * 64), 3.0, dtype=BF, device="cuda")
+    rq().rope_append(qkv, *p.args(), freqs(64), q=q)
+    want = formulas.rope_append(qkv, None, p.k, p.v, p.starts, p.kv, p.table, freqs(64), False)[0]
+    assert (q[p.T:] == 3).all()
+    assert ((q.double() - want).abs()[:p.T] <= HALF_BF * want[:p.T].abs() + 16 * U * 2 * float(qkv.abs().max())).all()
