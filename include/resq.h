@@ -460,7 +460,8 @@ typedef struct resq_sequences {
  *   inv_freq fp64 [rot / 2] (device): any scheme of frequencies; rot <= D, a multiple of 16 (0: no rotation); elements from rot on
  *   are copied.  Frequency j belongs to elements j and j + rot / 2 of a head, or (pairs != 0) to 2 j and 2 j + 1.  positions int32
  *   [T] or NULL: where the tokens stand for the rotation, if not at their keys' places (the slots are the keys' all the same).
- *   Angles are exact to 2^-32 of a turn for any int32 position; everything is fp32 and rounded once.  Q may be the query
+ *   Angles are right to 2^-32 of a turn for any int32 position and go to fp32 sines and cosines (2^-26 of a turn); the rest is
+ *   fp32 and rounded once.  Q may be the query
  *   columns of a bf16 QKV itself; other overlaps are not allowed.  A token whose place is negative (kv_len below the number of new
  *   tokens) or whose page is none is rotated, not stored.  Two sequences must not own the same slot.  No workspace. */
 RESQ_API int resq_rope_append(const void* QKV, int dtype, int64_t T, int64_t ldqkv, int64_t Hq, int64_t Hkv, int64_t D, const void* bias_bf16,

@@ -4,8 +4,9 @@
 //   a' = a cos - b sin,  b' = b cos + a sin;  values and elements from `rot` on are copied
 //
 // Angles.  pos inv_freq in fp32 is off by 0.03 rad half a million tokens into a sequence.  inv_freq / 2 pi is turned into a 64-bit
-// fraction of a turn instead (fp64, once per angle), and pos times that fraction modulo 2^64 is the angle without any further
-// error; its top 32 bits, as a signed number of half turns, go to sincospi: 2^-32 of a turn in all.
+// fraction of a turn instead (once per angle; a product of fp64 numbers keeps 53 bits, too few times a position of 2^31, so its
+// second half and that of 1 / 2 pi are added), within 2 2^-64, and pos times that fraction modulo 2^64 is the angle within 2^-32 of a
+// turn.  Its top 32 bits, as a signed number of half turns, go to sincospi in fp32: 2^-26 of a turn, or 1.6 2^-24 rad, at every position.
 //
 // Bound by HBM: every element is read and written once.  A block takes one to eight tokens; its threads first compute the tokens'
 // sines and cosines (two each for eight tokens of 128-wide heads, shared by all heads), with their first elements already on the
@@ -117,9 +118,10 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
     // ---- sines and cosines
     for (int i = tid; i < nt * half; i += kThreads) {
         const int tok = i / half, j = i - tok * half;
-        const double f = a.inv_freq[j] * 0.15915494309189533577;  // 1 / 2 pi
-        const double frac = f - floor(f);
-        const unsigned long long turn = (unsigned long long)(frac * 18446744073709551616.0) * (unsigned long long)(long long)place[tok].pos;
+        const double inv = a.inv_freq[j], mag = fabs(inv), k2Pi = 0.15915494309189535, kLow2Pi = -9.839338337591243e-18;  // 1 / 2 pi
+        const double f = mag * k2Pi, low = fma(mag, k2Pi, -f) + mag * kLow2Pi, k64 = 18446744073709551616.0;
+        const unsigned long long part = (unsigned long long)((f - floor(f)) * k64) + (unsigned long long)(long long)(low * k64);
+        const unsigned long long turn = (inv < 0.0 ? 0ull - part : part) * (unsigned long long)(long long)place[tok].pos;
         sincospif((float)(int)(unsigned)(turn >> 32) * 4.656612873077393e-10f, &sn[tok][j], &cs[tok][j]);  // 2^-31: in half turns
     }
     __syncthreads();

@@ -1,10 +1,12 @@
 """What the operators on a paged cache do at their edges, against their definitions in 64 bits (paged_formulas.py; tolerances of
 attention as in test_paged_gpu.py)."""
+from fractions import Fraction
+
 import pytest
 import torch
 
 import paged_formulas as formulas
-from test_paged_gpu import BF, HALF_BF, NAN, U, Paged, freqs, ints, rq
+from test_paged_gpu import BF, F32, F64, HALF_BF, NAN, U, Paged, freqs, gen, ints, rq
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +88,35 @@ def test_append_rows_behind_many_sequences(B):
     want = formulas.rope_append(qkv, None, p.k, p.v, p.starts, p.kv, p.table, freqs(64), False)[0]
     assert (q[p.T:] == 3).all()
     assert ((q.double() - want).abs()[:p.T] <= HALF_BF * want[:p.T].abs() + 16 * U * 2 * float(qkv.abs().max())).all()
+
+
+# ------------------------------------------------------------------------------------------------ angles
+
+# 1 / (2 pi) to 84 digits
+INV_2PI = Fraction(159154943091895335768883763372514362034459645740456448747667344058896797634226535090, 10 ** 84)
+
+
+def test_append_angles_of_any_position_and_frequency():
+    """A pair (sin, cos) of its own angle turns into (0, 1): what is left in the first place is the error of the angle, of its sine and
+    cosine.  Tolerance: the angle 2 pi (2^-32 + 2^-26) (fixed point; fp32 number of half turns), sine and cosine one unit in the last
+    place each (2^-24 (|sin| + |cos|) <= 1.42 * 2^-24), a rounded product 2^-25 and the output's rounding."""
+    g = gen(0)
+    f = torch.cat([freqs(128)[:20], torch.rand(14, generator=g, dtype=F64, device="cuda"), torch.rand(10, generator=g, dtype=F64, device="cuda") * 100,
+                   -torch.rand(10, generator=g, dtype=F64, device="cuda"), -torch.rand(4, generator=g, dtype=F64, device="cuda") * 50,
+                   torch.rand(3, generator=g, dtype=F64, device="cuda") * 1e-9, -torch.rand(3, generator=g, dtype=F64, device="cuda") * 1e-9])
+    pos = [0, 1, -1, 2, 77, 8191, 131071, 900001, 2 ** 24 + 1, 2 ** 30 - 1, -2 ** 30 - 5, 2 ** 31 - 1, -2 ** 31, -2 ** 31 + 1]
+    pos += torch.randint(-2 ** 31, 2 ** 31, (40,), generator=g, device="cuda").tolist()
+    T, tau = len(pos), 6.283185307179586476925
+    exact = [Fraction(x) * INV_2PI for x in f.tolist()]
+    turn = torch.tensor([[float((p * e + Fraction(1, 2)) % 1 - Fraction(1, 2)) for e in exact] for p in pos], dtype=F64, device="cuda")
+    s, c = (turn * tau).sin(), (turn * tau).cos()
+    qkv = torch.zeros((T, 3 * 128), dtype=F32, device="cuda")
+    qkv[:, :64], qkv[:, 64:128] = s, c
+    a, b = qkv[:, :64].double(), qkv[:, 64:128].double()
+    p = Paged([(T, 0)], 1, 128, 8)
+    q = rq().rope_append(qkv, *p.args(), f, positions=ints(pos)).double()
+    want = a * c - b * s
+    err = (q[:, :64] - want).abs()
+    tol = tau * (2.0 ** -32 + 2.0 ** -26) + 1.42 * 2.0 ** -24 + 2.0 ** -25 + HALF_BF * want.abs()
+    assert (err <= tol).all(), f"{int((err > tol).sum())} of {err.numel()} off, worst {float((err / tol).max())} of the tolerance"
+    assert ((q[:, 64:] - 1).abs() <= HALF_BF + 1e-6).all()
