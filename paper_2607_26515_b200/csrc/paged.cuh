@@ -6,6 +6,7 @@
 namespace resq {
 
 constexpr int64_t kMaxSeqs = RESQ_MAX_SEQUENCES;
+constexpr float kLn2 = 0.6931471805599453f;
 
 // n / d for 0 <= n < 2^31 by one multiplication (Granlund and Montgomery: m = ceil(2^(32 + s) / d), s = ceil(log2 d) - 1 bits of
 // shift are enough for 31-bit n; d = 1 is apart).
@@ -85,11 +86,19 @@ struct AttnArgs {
 // paged_chunk.cu: the tensor-core form for chunks of new tokens.  Rows of its tiles for g query heads per kv head, whether it takes
 // these strides, and its launch (args.deal.rows and .keys as it wants them).
 constexpr int kChunkKeys = 128, kChunkExtra = 6;
+constexpr float kChunkGrowth = 20.0f;  // its references lie this far above the maximum that they were set by, in the exponent of 2
 int attn_chunk_rows(int g);
 bool attn_chunk_supported(const AttnArgs& args);
 int launch_attn_chunk(const AttnArgs& args, int D, int ctas, cudaStream_t stream);
 
 #ifdef __CUDACC__
+
+// Log of a row's sum relative to such a reference.  The 20 are taken out of both first (exactly): the sum of the two would round to
+// the digits of a number of 20.
+__device__ __forceinline__ float chunk_lse(float ref, float sum) {
+    return sum == 0.0f ? -__builtin_huge_valf() : ((ref - kChunkGrowth) + log2f(sum * 1048576.0f)) * kLn2;
+}
+static_assert(kChunkGrowth == 20.0f, "2^20 above");
 
 struct Seq {
     int q0, n, kv;  // first token row, new tokens, keys (the new tokens' among them)

@@ -54,7 +54,7 @@ int check_paged(const char* what, const resq_paged_cache* c, const resq_sequence
 namespace {
 
 constexpr float kInf = __builtin_huge_valf();
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWarps = 4, kKeys = 64, kWarpKeys = kKeys / kWarps;  // of attn_rows_kernel
 constexpr int kRowsCtasPerSm = 2;
 
@@ -740,7 +740,7 @@ __global__ void __launch_bounds__(D * 2) attn_join_tiles_kernel(const __grid_con
     __nv_bfloat16* const dst = a.out + row * a.ldo + head * D + w * 16;
     store8(dst, lo, 8);
     store8(dst + 8, hi, 8);
-    if (a.lse && w == 0) a.lse[row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
+    if (a.lse && w == 0) a.lse[row * a.Hq + head] = chunk_lse(ref, sum);
 }
 
 // Workspace: notes, then the partial sums of two slots per CTA.

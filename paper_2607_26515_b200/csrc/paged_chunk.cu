@@ -13,8 +13,9 @@
 // past the first row's last key: rows behind the last key become zeros (0 times what a page holds there may be NaN), and
 // infinities and NaN are taken out and added by those rows that do see them.
 //
-// O is rescaled only when a row's maximum has grown by more than 20 in the exponent of 2 since its reference was set: weights up
-// to 2^20 lose nothing in bf16 or in the fp32 sums, and the final division takes the reference out.
+// O is rescaled only when a row's maximum has grown by more than 20 in the exponent of 2 since its reference was set.  The reference
+// lies those 20 above the maximum that it was set by: weights are at most 1, so that sums with large values overflow no sooner than
+// they have to, lose nothing in bf16 or fp32 by being 2^-20, and the final division takes the reference out.
 //
 // Measured: 8192 tokens from the beginning, 28 heads on 4 of 128, 571 us = 843 TFLOP/s (0.51 of the burst rate of a library product);
 // 512 tokens behind 31500 keys, 16 heads on 2, two sequences, 300 us = 876 TFLOP/s.  The products alone, with the weights left
@@ -29,12 +30,10 @@ namespace resq {
 namespace {
 
 constexpr float kInf = __builtin_huge_valf();
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kKeys = kChunkKeys, kHalf = 128;
 constexpr int kMmaWarp = 8, kLoadWarp = 10, kFixWarp = 11, kThreads = 384;  // products: warps 8 and 9
 constexpr int kDescs = 4;    // segments described ahead of the slowest reader
 constexpr int kStrange = 4;  // key tiles of a segment that can hold keys of its own tokens (at most 256)
-constexpr float kGrowth = 20.0f;
 // Registers per thread: 168 at the launch; the eight softmax warps take what the other four give up.
 constexpr int kSoftmaxRegs = 200, kOtherRegs = 104;
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * 168, "");
@@ -477,8 +476,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     for (int j = 3; j + 1 < 32; j += 2) top[i] = max3(top[i], __uint_as_float(s[i][j]), __uint_as_float(s[i][j + 1]));
                     top[i] = max_nan(top[i], __uint_as_float(s[i][31]));
                 }
-                // a score of NaN or +inf makes the row NaN by way of its reference
-                float m = max3(max_nan(top[0], top[1]), top[2], top[3]) * a.c;
+                // what the reference would be; a score of NaN or +inf makes the row NaN by way of it
+                float m = fmaf(max3(max_nan(top[0], top[1]), top[2], top[3]), a.c, kChunkGrowth);
                 if (m == kInf) m = __int_as_float(0x7FFFFFFF);
                 if (u == u0) ref = m;
                 bool again = false;
@@ -509,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 // The weights by the reference as it is; the maximum is wanted only to see that it will do, and comes meanwhile.
                 for (;;) {
                     weights(0, w, a2, b2);
-                    const bool grown = row < rows && !(m <= ref + kGrowth) && !again;  // (rows behind the last hold anything)
+                    const bool grown = row < rows && !(m <= ref + kChunkGrowth) && !again;  // (rows behind the last hold anything)
                     if (!__any_sync(~0u, grown)) break;
                     // the products before this tile's scores are done: O is this warp's
                     const float f2 = grown ? ex2(ref - m) : 1.0f;
@@ -661,7 +660,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             }
             if (writes && row < rows) {
                 if (slot >= 0) a.part_ml[at] = make_float2(ref, sum);
-                else if (a.lse) a.lse[out_row * a.Hq + head] = sum == 0.0f ? -kInf : (ref + log2f(sum)) * kLn2;
+                else if (a.lse) a.lse[out_row * a.Hq + head] = chunk_lse(ref, sum);
             }
             ptx::tc_fence_before();
             __syncwarp();

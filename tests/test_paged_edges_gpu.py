@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paged_formulas as formulas
-from test_paged_gpu import BF, F32, F64, HALF_BF, NAN, U, Paged, freqs, gen, ints, rq
+from test_paged_gpu import BF, F32, F64, HALF_BF, NAN, U, Paged, freqs, gen, hold, ints, rq
 
 pytestmark = pytest.mark.gpu
 
@@ -52,6 +52,21 @@ def test_attention_a_visible_strange_value_is_never_lost(n, keys, high, value):
         strange = ~torch.isfinite(out.view(n, 8, 128))
         assert strange[:, :4, 5].all() and int(strange.sum()) == 4 * n, hint
         assert torch.isfinite(lse).all()
+
+
+# ------------------------------------------------------------------------------------------------ values near the ends of their type
+
+@pytest.mark.parametrize("size", [1e34, 1e-25])
+@pytest.mark.parametrize("n, keys", [(1, 3000), (12, 3000), (100, 1000), (300, 5000)])
+def test_attention_values_of_any_size(n, keys, size):
+    """Scores that rise by 13 (19 in the exponent of 2) behind the first keys; sums of weights up to 1 times these values are within
+    fp32, of weights up to 2^19 they would not be."""
+    p, q = far_scores(n, keys, keys - n - 40)
+    p.k.mul_(0.13)
+    p.v.nan_to_num_(0.0).mul_(size)
+    for hint in (n, None):
+        out, lse = rq().paged_attention(q, *p.args(), scale=1.0, max_new=hint, lse=True)
+        hold(out, lse, q, p, 1.0, f"hint {hint}")
 
 
 # ------------------------------------------------------------------------------------------------ starts out of order
