@@ -21,10 +21,6 @@ inline bool rows_aligned(const void* p, int64_t ld, int64_t cols, int dtype) {
 // other counts gets right results at another speed.
 inline int resident_clusters(int cs) { return cs == 1 ? 148 : cs == 2 ? 74 : cs == 4 ? 33 : 15; }
 
-// resq_token_logprobs with rows cut into `slices` (1, 2, 4 or 8; 0: as that call cuts them).  token_logprobs.cu.
-int token_logprobs_sliced(const void* logits, int dtype, int64_t M, int64_t V, int64_t ld, const int64_t* tokens, float temperature, int top,
-                          float* logp, float* entropy, float* peak, float* log_sum, int32_t* top_ids, float* top_logp, int slices, void* stream);
-
 #ifdef __CUDACC__
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }

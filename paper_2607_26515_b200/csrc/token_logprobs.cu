@@ -619,8 +619,10 @@ int check_logits(const char* what, const void* x, int dtype, int64_t M, int64_t 
 
 using namespace resq;
 
-int resq::token_logprobs_sliced(const void* logits, int dtype, int64_t M, int64_t V, int64_t ld, const int64_t* tokens, float temperature, int top,
-                               float* logp, float* entropy, float* peak, float* log_sum, int32_t* top_ids, float* top_logp, int slices, void* stream) {
+extern "C" {
+
+int resq_token_logprobs(const void* logits, int dtype, int64_t M, int64_t V, int64_t ld, const int64_t* tokens, float temperature, int top,
+                        float* logp, float* entropy, float* peak, float* log_sum, int32_t* top_ids, float* top_logp, void* stream) {
     const char* what = "token_logprobs";
     int rc = check_logits(what, logits, dtype, M, V, ld, temperature);
     if (rc) return rc;
@@ -638,8 +640,7 @@ int resq::token_logprobs_sliced(const void* logits, int dtype, int64_t M, int64_
     // its CTAs').
     const int64_t vecs = (V + 7) / 8;
     int cs = 1;
-    if (slices > 0) cs = slices;
-    else while (cs < kMaxCluster && M * cs * 2 <= 256 && vecs / (2 * cs) >= 2048) cs *= 2;
+    while (cs < kMaxCluster && M * cs * 2 <= 256 && vecs / (2 * cs) >= 2048) cs *= 2;
     const int64_t slice = (vecs + cs - 1) / cs;
     // An SM holds 1024 of these threads.  Up to eight CTAs per SM share them, so that all rows are under way at once (740 x
     // 131072, fp32: 59 us with 192 threads, 71 with 256, which leave 148 rows to a second wave); beyond, the number of CTAs
@@ -666,13 +667,6 @@ int resq::token_logprobs_sliced(const void* logits, int dtype, int64_t M, int64_
                                       : (top ? logprobs_kernel<bf, true> : logprobs_kernel<bf, false>);
     LaunchScope scope(kKindRow, st);
     return cuda_fail(launch_clusters(kern, (unsigned)(M * cs), threads, 0, cs, st, a), "logprobs_kernel launch");
-}
-
-extern "C" {
-
-int resq_token_logprobs(const void* logits, int dtype, int64_t M, int64_t V, int64_t ld, const int64_t* tokens, float temperature, int top,
-                        float* logp, float* entropy, float* peak, float* log_sum, int32_t* top_ids, float* top_logp, void* stream) {
-    return resq::token_logprobs_sliced(logits, dtype, M, V, ld, tokens, temperature, top, logp, entropy, peak, log_sum, top_ids, top_logp, 0, stream);
 }
 
 int resq_token_logprobs_backward(const void* logits, int dtype, int64_t M, int64_t V, int64_t ld, const int64_t* tokens, float temperature,

@@ -7,8 +7,8 @@
 //
 // The rows' sums are resq_token_logprobs' kernel, one pass over the logits, which is what the call is bound by.  This file's kernel
 // then needs one row per sequence again (of the logits, the draft's logits and e): a cluster of 1 to 8 CTAs per sequence finds the
-// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 42.7 us (rows and
-// both launches 27.6, the deciding row 2, the drawing 13 for 67 MB, 10.2 of them at the copy rate); one such sequence 13.6 us, latency of
+// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 43.9 us (rows and
+// both launches 28.8, the deciding row 2, the drawing 13 for 67 MB, 10.2 of them at the copy rate); one such sequence 13.6 us, latency of
 // both.
 //
 // Decisions that 32 bits leave open are made in 64 bits: a probability next to its border, and a drawing where another ratio may be
@@ -366,15 +366,10 @@ int resq_verify_drafts(const void* logits, int dtype, int64_t R, int64_t V, int6
     float *wl = reinterpret_cast<float*>(ws + l.logp), *wp = reinterpret_cast<float*>(ws + l.peak), *ws_sum = reinterpret_cast<float*>(ws + l.log_sum);
     int32_t* ids = reinterpret_cast<int32_t*>(ws + l.ids);
     const int64_t vecs = (V + 7) / 8;
-    // A few hundred rows leave SMs with one row less than others: cut in two or four the SMs' shares come out within 1.2 of each
-    // other (320 x 131072: two slices, 28.0 us against 28.3 with cold caches; the whole call 47.4 against 51.1).
-    int slices = 0;
-    if (R > 128 && R < 148 * 8) {
-        slices = 1;
-        while (slices < 4 && vecs / (2 * slices) >= 2048 && (R * slices + 147) / 148 * 148 > R * slices * 6 / 5) slices *= 2;
-    }
-    int rc = greedy ? token_logprobs_sliced(logits, dtype, R, V, ld, nullptr, 1.0f, 1, nullptr, nullptr, nullptr, nullptr, ids, wl, slices, stream)
-                    : token_logprobs_sliced(logits, dtype, R, V, ld, drafts, temperature, 0, wl, nullptr, wp, ws_sum, nullptr, nullptr, slices, stream);
+    // (Rows cut into two or four slices so that the SMs' shares are even gain 1 to 4 us at 150 and 160 rows of 131072 and lose 8 at 180 and
+    // 300: 33.2 against 24.7 us for the largest logit, bf16, at 180, 48.6 against 40.0 for fp32 rows to draw from.)
+    int rc = greedy ? resq_token_logprobs(logits, dtype, R, V, ld, nullptr, 1.0f, 1, nullptr, nullptr, nullptr, nullptr, ids, wl, stream)
+                    : resq_token_logprobs(logits, dtype, R, V, ld, drafts, temperature, 0, wl, nullptr, wp, ws_sum, nullptr, nullptr, stream);
     if (rc) return rc;
     // Few sequences: their row over a cluster, not below 4096 logits a CTA.  The 1024 threads that an SM holds are shared by the CTAs
     // it gets, and the clusters are as large as it takes to keep most of them busy on the average: 64 sequences of 131072 take 43.1
