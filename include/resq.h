@@ -529,7 +529,9 @@ RESQ_API const char* resq_last_error(void);
  * its CTAs can deliver, with a poll limit of about a millisecond: the bounded wait runs out, the kernel records
  * RESQ_ERR_TIMEOUT in the status word, leaves through its normal exit (tensor memory freed, no output for the
  * tiles it was summing) and the context stays usable; resq_check then returns RESQ_ERR_TIMEOUT and the next call
- * on the same workspace is an ordinary one.  Nothing faults or hangs.  (0 withdraws an unconsumed request.) */
+ * on the same workspace is an ordinary one.  Nothing faults or hangs.  (2) does the same to the next resq_paged_attention
+ * launch of the form for long chunks, in which every role then gives up in turn and the rows' outputs mean nothing; 3 to both.
+ * (0 withdraws unconsumed requests.) */
 RESQ_API int64_t resq_kernel_launches(void);
 RESQ_API int resq_debug_expire_next_wait(int on);
 RESQ_API int resq_profile_enable(int on);

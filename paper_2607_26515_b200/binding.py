@@ -919,9 +919,10 @@ def kernel_launches() -> int:
     return int(lib().resq_kernel_launches())
 
 
-def debug_expire_next_wait(on: bool = True) -> None:
-    """resq_debug_expire_next_wait: the next decode-sized GEMM launch lets its bounded wait run out (test hook)."""
-    _check(lib().resq_debug_expire_next_wait(1 if on else 0))
+def debug_expire_next_wait(on: bool = True, attention: bool = False) -> None:
+    """resq_debug_expire_next_wait: the next decode-sized GEMM launch, or the next attention of long chunks, lets its bounded wait
+    run out (test hook)."""
+    _check(lib().resq_debug_expire_next_wait((2 if attention else 1) if on else 0))
 
 
 def profile_enable(on: bool) -> None:

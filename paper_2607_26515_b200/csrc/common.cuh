@@ -194,6 +194,7 @@ bool gemm_decode_supported(const GemmArgs* g, int count);
 int launch_gemm_decode(const GemmArgs* g, int count, cudaStream_t stream);
 // Test hook behind resq_debug_expire_next_wait (gemm_pair.cu).
 void debug_expire_next_wait(int on);
+bool take_expire_request(int kind);  // 1: decode-sized GEMM, 2: attention of chunks; withdraws the request that it finds
 // Whether launch_gemm_hif4 takes the keep flags of the block-wise selection for this shape (see GemmArgs::blk_flags).
 bool gemm_block_lists_supported(int64_t M, int64_t N, int64_t K);
 // Whether launch_gemm_hif4 takes the compressed 2:4 residual for this shape (the CTA-pair kernel runs it).

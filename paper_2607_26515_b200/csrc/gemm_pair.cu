@@ -875,7 +875,7 @@ gemm_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constan
     }
 }
 
-std::atomic<int> g_expire_next_wait{0};
+std::atomic<int> g_expire_next_wait{0};  // bits: the kinds of launches whose next one is to run out
 
 constexpr int kStreamKTN = 256;    // tile width of the K-streamed schedule (two accumulators fit in tensor memory)
 constexpr int kStreamKMaxPairs = 74;
@@ -1001,7 +1001,7 @@ void common_params(PairParams<NP>& p, const GemmArgs& g, bool streamk) {
     p.sk_flags = g.sk_flags;
     p.sk_poll_limit = 1 << 20;
     p.sk_extra = 0;
-    if (streamk && g_expire_next_wait.exchange(0)) {  // test hook: this launch's wait for the segments cannot be met
+    if (streamk && take_expire_request(1)) {  // test hook: this launch's wait for the segments cannot be met
         p.sk_poll_limit = 1 << 12;
         p.sk_extra = 1;
     }
@@ -1331,7 +1331,10 @@ int dispatch_pair(const GemmArgs& g, int tn, int splits, cudaStream_t stream) {
 
 }  // namespace
 
-void debug_expire_next_wait(int on) { g_expire_next_wait.store(on ? 1 : 0); }
+void debug_expire_next_wait(int on) { g_expire_next_wait.store(on & 3); }
+bool take_expire_request(int kind) {
+    return (g_expire_next_wait.load(std::memory_order_relaxed) & kind) && (g_expire_next_wait.fetch_and(~kind) & kind);
+}
 
 size_t gemm_pair_streamk_scratch_bytes() {
     return (size_t)2 * kStreamKMaxPairs * (2 * kBM) * kStreamKTN * sizeof(float);

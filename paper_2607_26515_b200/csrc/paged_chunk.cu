@@ -51,6 +51,7 @@ struct ChunkArgs {
     int half_rows, half_tokens;  // of a half tile
     int box;                     // keys per copy: a power of two that divides the page and the tile
     int wide;                    // rows of the output start on 32-byte boundaries
+    int expire;                  // test hook: the repairs wait for what does not come
 };
 
 struct ChunkSeg {
@@ -61,7 +62,7 @@ struct ChunkSeg {
 };
 struct ChunkShared {
     uint64_t desc_full[kDescs], desc_empty[kDescs], strange_full[kDescs];
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], merge_full, merge_free;
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], merge_full, merge_free, done[2], never;
     uint64_t kv_full[10], kv_empty[10], raw_full[10];
     ChunkSeg seg[kDescs];
     float2 other[kHalf];                    // of a split segment's second half: reference and sum of each row
@@ -83,6 +84,10 @@ __device__ __forceinline__ void chunk_timeout(DeviceStatus* st, int where) {
 // every role's answer is on the way of the next product.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
     return __all_sync(~0u, ptx::mbar_wait_spin(bar, parity, abort_flag));
+}
+// Waits for what is under way in any case, without a look at the others: 0.4 ms at most.
+__device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
+    for (int i = 0; i < 4096 && !ptx::mbar_test_wait(bar, parity); ++i) __nanosleep(100);
 }
 __device__ __forceinline__ float ex2(float x) {
     float r;
@@ -133,9 +138,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             ptx::mbar_init(&sh.p_full[h][0], 4);  // the weights of the first 64 keys, of the others
             ptx::mbar_init(&sh.p_full[h][1], 4);
             ptx::mbar_init(&sh.o_full[h], 1);
+            ptx::mbar_init(&sh.done[h], 1);
         }
         ptx::mbar_init(&sh.merge_full, 4);
         ptx::mbar_init(&sh.merge_free, 4);
+        ptx::mbar_init(&sh.never, 1);
         for (int i = 0; i < ST; ++i) {
             ptx::mbar_init(&sh.kv_full[i], 1);
             ptx::mbar_init(&sh.kv_empty[i], 2);  // the products of both halves
@@ -260,16 +267,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 if (count == 0 && ok) a.notes[cta].parts = 0;
                 if (!ok) {
                     chunk_timeout(a.status, 1);
-                    // copies in flight write to this CTA's shared memory: wait for them, with a limit
-                    for (int h = 0; h < 2; ++h)
-                        for (int i = 0; q_loads[h] > 0 && i < 4096 && !ptx::mbar_test_wait(&sh.q_full[h], (q_loads[h] - 1) & 1); ++i) __nanosleep(100);
-                    for (uint32_t q = pos > ST ? pos - ST : 0; q < pos; ++q) {
-                        const int st = q % ST;
-                        for (int i = 0; i < 4096; ++i) {
-                            if ((raw >> st) & 1 ? ptx::mbar_test_wait(&sh.raw_full[st], ((raw_turn >> st) & 1) ^ 1) : ptx::mbar_test_wait(&sh.kv_full[st], (q / ST) & 1)) break;
-                            __nanosleep(100);
-                        }
-                    }
                 } else {
                     // an empty description ends the others' loops
                     const int e = count % kDescs;
@@ -277,6 +274,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                         sh.seg[e].b = -1;
                         ptx::mbar_arrive(&sh.desc_full[e]);
                     } else chunk_timeout(a.status, 2);
+                }
+                // Copies in flight write to this CTA's shared memory: whoever has given up, they are waited for, with a limit.
+                for (int h = 0; h < 2; ++h)
+                    if (q_loads[h] > 0) drain(&sh.q_full[h], (q_loads[h] - 1) & 1);
+                for (uint32_t q = pos > ST ? pos - ST : 0; q < pos; ++q) {
+                    const int st = q % ST;
+                    if ((raw >> st) & 1) drain(&sh.raw_full[st], ((raw_turn >> st) & 1) ^ 1);
+                    else drain(&sh.kv_full[st], (q / ST) & 1);
                 }
             }
         } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
@@ -383,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         } else if (warp == kFixWarp) {
             // ------------------------------------------------------------------ repairs of value tiles
             uint32_t pos = 0, raw_turn = 0;  // parity of the next repaired tile of each stage
-            bool ok = true;
+            bool ok = !p.expire || __all_sync(~0u, ptx::mbar_wait_spin(&sh.never, 0, abort_flag, 1u << 12));
             for (int count = 0; ok; ++count) {
                 const int e = count % kDescs;
                 if (!(ok = warp_wait(&sh.desc_full[e], (count / kDescs) & 1, abort_flag))) break;
@@ -668,6 +673,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         }
         if (!ok && lane == 0) chunk_timeout(a.status, 5);
     }
+    // Products in flight read shared memory, write tensor memory and report to barriers.  (In the products' own branch this costs its
+    // loop 3 % of a prefill.)
+    if ((warp == kMmaWarp || warp == kMmaWarp + 1) && lane == 0) {
+        ptx::umma_commit(&sh.done[warp - kMmaWarp]);
+        drain(&sh.done[warp - kMmaWarp], 0);
+    }
     ptx::tc_fence_before();
     __syncthreads();
     if (warp == kMmaWarp) ptx::tmem_dealloc(tmem, 512);
@@ -691,6 +702,7 @@ int launch_attn_chunk(const AttnArgs& args, int D, int ctas, cudaStream_t stream
     p.half_tokens = kHalf / g;
     p.half_rows = p.half_tokens * g;
     p.wide = reinterpret_cast<uintptr_t>(args.out) % 32 == 0 && args.ldo % 16 == 0;
+    p.expire = take_expire_request(2);
     p.box = 8;
     while (p.box < kKeys && args.seq.page % (2 * p.box) == 0) p.box *= 2;
     ChunkMaps maps;

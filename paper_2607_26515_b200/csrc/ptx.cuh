@@ -78,8 +78,8 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
 // Bounded wait that never suspends the thread: for the single-thread roles (TMA producers, MMA issuer), whose
 // reaction time is on the critical path of the pipeline.  About 2^24 polls of ~25 cycles bound it to a fraction
 // of a second.
-__device__ __forceinline__ bool mbar_wait_spin(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    for (uint32_t i = 0; i < (1u << 24); ++i) {
+__device__ __forceinline__ bool mbar_wait_spin(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint32_t polls = 1u << 24) {
+    for (uint32_t i = 0; i < polls; ++i) {
         if (mbar_test_wait(bar, parity)) return true;
         if ((i & 1023u) == 1023u && *abort_flag) return false;
     }

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paged_formulas as formulas
-from test_paged_gpu import BF, F32, F64, HALF_BF, NAN, U, Paged, freqs, gen, hold, ints, rq
+from test_paged_gpu import BF, F32, F64, HALF_BF, I32, NAN, U, Paged, freqs, gen, hold, ints, rq
 
 pytestmark = pytest.mark.gpu
 
@@ -135,3 +135,48 @@ def test_append_angles_of_any_position_and_frequency():
     tol = tau * (2.0 ** -32 + 2.0 ** -26) + 1.42 * 2.0 ** -24 + 2.0 ** -25 + HALF_BF * want.abs()
     assert (err <= tol).all(), f"{int((err > tol).sum())} of {err.numel()} off, worst {float((err / tol).max())} of the tolerance"
     assert ((q[:, 64:] - 1).abs() <= HALF_BF + 1e-6).all()
+
+
+# ------------------------------------------------------------------------------------------------ waits
+
+TIMEOUT = 7
+
+
+@pytest.mark.parametrize("lens, Hq, Hkv, D", [([(100, 900), (300, 40)], 4, 2, 128), ([(40, 700)], 8, 2, 64), ([(1, 9000)], 128, 1, 64),
+                                              ([(17, 30)] * 60, 16, 2, 128), ([(2000, 0)], 8, 2, 128), ([(3, 129)], 100, 1, 128)])
+def test_attention_bounded_waits_expire_and_the_context_stays_usable(lens, Hq, Hkv, D):
+    """The test hook makes the repairs of value tiles wait for a barrier that nothing arrives at: they give up after 4096 polls, the
+    other roles find no tile and give up behind them, copies and products under way are waited for, tensor memory is freed
+    (the next call would not get it otherwise), the status is recorded, and the next call on the same workspace is an ordinary one."""
+    m = rq()
+    p = Paged(lens, Hkv, D, 16)
+    q = p.queries(Hq)
+    ws = m.alloc_workspace(m.paged_attention_workspace_bytes(p.T, len(lens), Hq, Hkv, D, 0))
+    around = torch.full((p.T + 2, Hq * D), 3.0, dtype=BF, device="cuda")
+    for i in range(4):
+        m.debug_expire_next_wait(True, attention=True)
+        m.paged_attention(q, *p.args(), workspace=ws, out=around[1:p.T + 1])
+        assert m.check(ws) == TIMEOUT and "gave up" in m.last_error()
+        torch.cuda.synchronize()
+        assert (around[0] == 3).all() and (around[-1] == 3).all()
+        out, lse = m.paged_attention(q, *p.args(), workspace=ws, lse=True)
+        assert m.check(ws) == 0, m.last_error()
+        hold(out, lse, q, p, D ** -0.5)
+
+
+def test_attention_requests_to_expire_are_their_own():
+    """A request for attention is not taken by calls of few rows or by other kernels, and can be withdrawn."""
+    m = rq()
+    p = Paged([(1, 90), (1, 5)], 2, 128, 16)
+    q = p.queries(4)
+    ws = m.alloc_workspace(m.paged_attention_workspace_bytes(2, 2, 4, 2, 128, 1))
+    m.debug_expire_next_wait(True, attention=True)
+    m.paged_attention(q, *p.args(), workspace=ws, max_new=1)
+    assert m.check(ws) == 0
+    m.debug_expire_next_wait(False)
+    p = Paged([(90, 90)], 2, 128, 16)
+    q = p.queries(4)
+    ws = m.alloc_workspace(m.paged_attention_workspace_bytes(90, 1, 4, 2, 128, 0))
+    out, lse = m.paged_attention(q, *p.args(), workspace=ws, lse=True)
+    assert m.check(ws) == 0
+    hold(out, lse, q, p, 128 ** -0.5)
