@@ -82,9 +82,11 @@ __device__ __forceinline__ void chunk_timeout(DeviceStatus* st, int where) {
 }
 // A wait of all lanes with one answer for them all: lanes that gave up apart would part the warp.  It does not let the warp sleep:
 // every role's answer is on the way of the next product.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    return __all_sync(~0u, ptx::mbar_wait_spin(bar, parity, abort_flag));
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint32_t polls = 1u << 24) {
+    return __all_sync(~0u, ptx::mbar_wait_spin(bar, parity, abort_flag, polls));
 }
+// Polls of a wait that may take as long as `tiles` key tiles do: 250 are 6000 cycles, twice what a tile takes.
+__device__ __forceinline__ uint32_t long_wait(int tiles) { return (1u << 24) + 250u * (uint32_t)tiles; }
 // Waits for what is under way in any case, without a look at the others: 0.4 ms at most.
 __device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
     for (int i = 0; i < 4096 && !ptx::mbar_test_wait(bar, parity); ++i) __nanosleep(100);
@@ -388,17 +390,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         } else if (warp == kFixWarp) {
             // ------------------------------------------------------------------ repairs of value tiles
             uint32_t pos = 0, raw_turn = 0;  // parity of the next repaired tile of each stage
-            bool ok = !p.expire || __all_sync(~0u, ptx::mbar_wait_spin(&sh.never, 0, abort_flag, 1u << 12));
+            uint32_t polls = long_wait(0);  // this warp waits for the end of the segment that the others are at
+            bool ok = !p.expire || warp_wait(&sh.never, 0, abort_flag, 1u << 12);
             for (int count = 0; ok; ++count) {
                 const int e = count % kDescs;
-                if (!(ok = warp_wait(&sh.desc_full[e], (count / kDescs) & 1, abort_flag))) break;
+                if (!(ok = warp_wait(&sh.desc_full[e], (count / kDescs) & 1, abort_flag, polls))) break;
                 const ChunkSeg g = sh.seg[e];
                 if (g.b < 0) break;
+                polls = long_wait(g.end - g.u0);
                 const int us = max(g.u0, (max(g.first_pos, -1) + 1) / kKeys);  // first tile that reaches past the first row's last key
                 for (int u = us; ok && u < g.end; ++u) {
                     const uint32_t at = pos + 2 * (u - g.u0) + 1;
                     const int st = at % ST;
-                    if (!(ok = warp_wait(&sh.raw_full[st], (raw_turn >> st) & 1, abort_flag))) break;
+                    if (!(ok = warp_wait(&sh.raw_full[st], (raw_turn >> st) & 1, abort_flag, polls))) break;
                     raw_turn ^= 1u << st;
                     unsigned char* const tile = ring + st * TILE;
                     const int key0 = u * kKeys, valid = min(kKeys, g.k_end - key0);

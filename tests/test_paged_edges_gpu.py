@@ -1,5 +1,6 @@
 """What the operators on a paged cache do at their edges, against their definitions in 64 bits (paged_formulas.py; tolerances of
 attention as in test_paged_gpu.py)."""
+import math
 from fractions import Fraction
 
 import pytest
@@ -180,3 +181,20 @@ def test_attention_requests_to_expire_are_their_own():
     out, lse = m.paged_attention(q, *p.args(), workspace=ws, lse=True)
     assert m.check(ws) == 0
     hold(out, lse, q, p, 128 ** -0.5)
+
+
+def test_attention_waits_as_long_as_the_keys_take():
+    """Nearly 2^31 keys (one page, over and over): each CTA goes through its share for most of a second, at whose end a repair is
+    due.  Scores of 0 and values of powers of 2 make every sum exact: 2^-20 times up to 2^26 keys, in steps of 16 at least."""
+    m = rq()
+    page, pages, Hkv, D = 8192, 262135, 8, 64
+    k = torch.zeros((1, page, Hkv, D), dtype=BF, device="cuda")
+    value = 2.0 ** (torch.arange(Hkv * D, device="cuda") % 7 - 3.0) * (1 - 2 * (torch.arange(Hkv * D, device="cuda") % 2))
+    v = value.view(1, 1, Hkv, D).expand(1, page, Hkv, D).to(BF).contiguous()
+    q = torch.ones((1, 128 * Hkv * D), dtype=BF, device="cuda")
+    ws = m.alloc_workspace(m.paged_attention_workspace_bytes(1, 1, 128 * Hkv, Hkv, D, 1))
+    out, lse = m.paged_attention(q, k, v, ints([0, 1]), ints([page * pages]), torch.zeros((1, pages), dtype=I32, device="cuda"), lse=True, max_new=1,
+                                 workspace=ws)
+    assert m.check(ws) == 0, m.last_error()
+    assert torch.equal(out.view(Hkv, 128, D), value.view(Hkv, 1, D).expand(Hkv, 128, D).to(BF))
+    assert ((lse - math.log(page * pages)).abs() <= 64 * U * math.log(page * pages)).all()
