@@ -431,7 +431,8 @@ RESQ_API int resq_token_logprobs_backward(const void* logits, int dtype, int64_t
 /* ---- between the qkv and the output projection of a rollout: rotation, paged cache, attention (no counterpart in the paper) ----
  * Keys and values live in pages.  Both structs are HOST structs read during the call; their pointers are device pointers.
  *   cache: k, v bf16, element (page, row, head, d) of each at page * *_page + row * *_row + head * *_head + d; strides in
- *     elements, multiples of 8 (0 allowed), bases 16-byte aligned; head_dim 64 or 128; page_size a multiple of 8.
+ *     elements, multiples of 8 (0 allowed; a cache that is written to has them D apart at least), bases 16-byte aligned; head_dim 64 or
+ *     128; page_size a multiple of 8.
  *   sequences: token rows q_start[b] .. q_start[b + 1] - 1 of the call are the new tokens of sequence b; kv_len[b] counts its
  *     keys, the new tokens' among them, so its i-th of n new tokens is key (and stands at position) kv_len[b] - n + i;
  *     page_table[b * ld_table + j] is the page of keys j * page_size ...

@@ -197,6 +197,12 @@ extern "C" int resq_rope_append(const void* QKV, int dtype, int64_t T, int64_t l
     if (dtype != RESQ_OUT_BF16 && dtype != RESQ_OUT_F32) return fail(RESQ_ERR_PATTERN, what, "unknown type of QKV");
     int rc = check_paged(what, cache, seqs, T, Hq, Hkv, D);
     if (rc) return rc;
+    // Slots that share memory would be written by several threads: slots of one kind lie D apart or more.
+    auto apart = [&](int64_t page, int64_t row, int64_t head) {
+        return (cache->pages == 1 || page >= D) && (cache->page_size == 1 || row >= D) && (Hkv == 1 || head >= D);
+    };
+    if (!apart(cache->k_page, cache->k_row, cache->k_head) || !apart(cache->v_page, cache->v_row, cache->v_head))
+        return fail(RESQ_ERR_ALIGN, what, "pages, rows and heads of a cache that is written to must not share memory");
     if (rot < 0 || rot > D || rot % 16) return fail(RESQ_ERR_SHAPE, what, "rot must be a multiple of 16 up to the head's width");
     if ((Hq + 2 * Hkv) * D > INT32_MAX / 8) return fail(RESQ_ERR_SHAPE, what, "too many heads");
     if (!rows_aligned(QKV, ldqkv, (Hq + 2 * Hkv) * D, dtype) || !rows_aligned(Q, ldq, Hq * D, RESQ_OUT_BF16))
