@@ -472,7 +472,7 @@ RESQ_API int resq_rope_append(const void* QKV, int dtype, int64_t T, int64_t ldq
 /* Attention of the new tokens over the cache: query head h of Q [T, Hq D] reads kv head h / (Hq / Hkv); the token at key place i sees
  * keys 0 .. i (its own and the earlier new ones must be in the cache: resq_rope_append first).
  *     O_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j - lse_i),  lse_i = log sum_j exp(scale q_i.k_j)
- *   O bf16 [T, Hq D]; lse fp32 [T, Hq] contiguous, or NULL; scale positive.  A token that sees no key has O = 0 and lse = -inf.
+ *   O bf16 [T, Hq D]; lse fp32 [T, Hq] contiguous, or NULL; scale positive, below 2.3e38.  A token that sees no key has O = 0 and lse = -inf.
  *   Scores, sums and O are fp32 (finite while a row's number of keys times its largest |v| is below 3e38), the weights, at most 1, are
  *   rounded to bf16 for their product with the values.  What lies in masked places
  *   (keys behind a token, rows of a page behind the last key) has no influence, infinities and NaN included; a score of NaN or +inf

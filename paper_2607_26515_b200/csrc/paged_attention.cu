@@ -789,7 +789,7 @@ int resq_paged_attention(const void* Q, int64_t T, int64_t ldq, int64_t Hq, int6
     if (!Q || !O) return fail(RESQ_ERR_NULL, what, "Q and O must not be NULL");
     int rc = check_paged(what, cache, seqs, T, Hq, Hkv, D);
     if (rc) return rc;
-    if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(RESQ_ERR_SHAPE, what, "scale must be positive and finite");
+    if (!(scale > 0.0f) || !std::isfinite(scale * kLog2e)) return fail(RESQ_ERR_SHAPE, what, "scale must be positive and below 2.3e38");
     if (!rows_aligned(Q, ldq, Hq * D, RESQ_OUT_BF16) || !rows_aligned(O, ldo, Hq * D, RESQ_OUT_BF16) || !is_aligned(lse, 4))
         return fail(RESQ_ERR_ALIGN, what, "Q and O need 16-byte aligned bases and rows of at least Hq * D elements, lse 4-byte alignment");
     Choice ch = choose(T, Hq, Hkv, max_new);
