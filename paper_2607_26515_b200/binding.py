@@ -884,6 +884,7 @@ def verify_drafts(logits: torch.Tensor, row_start: torch.Tensor, drafts: torch.T
     at_u = at_noise = at_draft = at_peak = at_sum = None
     lde = ldd = 0
     if temperature != 0:
+        _require(1e-6 <= temperature <= 1e6, "temperature must be 0 or lie in 1e-6 .. 1e6")  # (one of 1e-50 would arrive as 0)
         _require(u is not None and noise is not None, "u and noise are needed to draw tokens")
         at_u = _vector(u, "u", R, _F32, index)
         lde, at_noise = _rows(noise, "noise", count, V, _F32, index), noise.data_ptr()

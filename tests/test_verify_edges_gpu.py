@@ -2,7 +2,6 @@
 import pytest
 import torch
 
-import paged_formulas as formulas
 from test_verify_gpu import BF, F32, F64, INF, NAN, problem, rows, rq
 
 pytestmark = pytest.mark.gpu
@@ -94,3 +93,11 @@ def test_verify_draws_where_hardly_anything_is_left_at_other_temperatures(T):
     x.copy_(torch.randn((2 * B, V), generator=g, device="cuda") * 2)
     d.copy_(x + 5e-5 * T * torch.randn((2 * B, V), generator=g, device="cuda"))
     hold_drawn(*refused(x, d, V, T), least=B // 2)
+
+
+@pytest.mark.parametrize("T", [1e-50, -1e-50, 9e-7, -1.0, 1.1e6, NAN, INF])
+def test_verify_refuses_temperatures_that_are_none(T):
+    """Numbers too small for fp32 among them: they are not temperature 0."""
+    a = problem([2, 3], 40, F32, "sure", seed=1)
+    with pytest.raises(ValueError, match="temperature"):
+        rq().verify_drafts(**{**a, "temperature": T})
