@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import paged_formulas as formulas
 from test_verify_gpu import BF, F32, F64, INF, NAN, problem, rows, rq
 
 pytestmark = pytest.mark.gpu
@@ -101,3 +102,53 @@ def test_verify_refuses_temperatures_that_are_none(T):
     a = problem([2, 3], 40, F32, "sure", seed=1)
     with pytest.raises(ValueError, match="temperature"):
         rq().verify_drafts(**{**a, "temperature": T})
+
+
+# ------------------------------------------------------------------------------------------------ borders of the other tests' problems
+
+def distance(a):
+    """How near the decisions of a call are to their borders: the smallest |u q - p| / p of the drafts that are looked at, and the
+    smallest relative distance of the two largest ratios of the places that are drawn."""
+    x, T, V = a["logits"].double(), a["temperature"], a["logits"].shape[1]
+    start, drafts = a["row_start"].tolist(), a["drafts"].tolist()
+    accepted = formulas.verify(a["logits"], start, a["drafts"], a["u"], a["noise"], a.get("draft_logits"), a.get("draft_peak"),
+                               a.get("draft_log_sum"), T)[0]
+    near, tie = INF, INF
+    for b, kept in enumerate(accepted):
+        n = start[b + 1] - start[b]
+        for i in range(min(kept + 1, n)):
+            r = start[b] + i
+            p = torch.softmax(x[r] / T, 0)
+            if "draft_logits" in a:
+                q = torch.exp((a["draft_logits"][r].double() - a["draft_peak"][r].double()) / T - a["draft_log_sum"][r].double())
+            else:
+                q = torch.zeros_like(p)
+                q[drafts[r]] = 1.0
+            if i < n - 1:
+                near = min(near, abs(float(a["u"][r]) * float(q[drafts[r]] / p[drafts[r]]) - 1))
+            if i == kept:
+                w = torch.relu(p - q) if i < n - 1 else p
+                s = w / a["noise"][b].double()
+                if V > 1 and float(s.max()) > 0:
+                    two = s.topk(2).values
+                    tie = min(tie, float(1 - two[1] / two[0]))
+    return near, tie
+
+
+@pytest.mark.parametrize("kind", ["logits", "sure"])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("counts, V", [([1], 1), ([2], 3), ([5], 131072), ([1, 4, 2, 8, 1, 3], 50001), ([3] * 40, 999), ([2, 70, 1, 33, 34], 77),
+                                       ([5] * 20, 20000), ([6] * 300, 64), ([2], 262144)])
+def test_verify_problems_are_clear(counts, V, kind, dtype):
+    """Every decision of the problems that test_verify compares whole numbers of is further than 1e-5 from its border."""
+    near, tie = distance(problem(counts, V, dtype, kind, seed=V + len(counts)))
+    assert near > 1e-5 and tie > 1e-5, (near, tie)
+
+
+@pytest.mark.parametrize("kind", ["logits", "sure"])
+def test_verify_other_problems_are_clear(kind):
+    for T in (0.3, 0.7, 1.7):
+        near, tie = distance(problem([4] * 12, 5001, F32, kind, seed=int(T * 10), T=T, pad=8))
+        assert near > 1e-5 and tie > 1e-5, (T, near, tie)
+    near, tie = distance(problem([5] * 60, 300, F32, kind, seed=9, likely=(5.0, 9.0) if kind == "sure" else (1.0, 5.0)))
+    assert near > 1e-5 and tie > 1e-5, (near, tie)
