@@ -472,11 +472,13 @@ RESQ_API int resq_rope_append(const void* QKV, int dtype, int64_t T, int64_t ldq
 /* Attention of the new tokens over the cache: query head h of Q [T, Hq D] reads kv head h / (Hq / Hkv); the token at key place i sees
  * keys 0 .. i (its own and the earlier new ones must be in the cache: resq_rope_append first).
  *     O_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j - lse_i),  lse_i = log sum_j exp(scale q_i.k_j)
- *   O bf16 [T, Hq D]; lse fp32 [T, Hq] contiguous, or NULL; scale positive, below 2.3e38.  A token that sees no key has O = 0 and lse = -inf.
+ *   O bf16 [T, Hq D]; lse fp32 [T, Hq] contiguous, or NULL; scale positive, below 2.3e38.  A token that sees no key, or only
+ *   scores of -inf, has O = 0 and lse = -inf.
  *   Scores, sums and O are fp32 (finite while a row's number of keys times its largest |v| is below 3e38), the weights, at most 1, are
- *   rounded to bf16 for their product with the values.  What lies in masked places
- *   (keys behind a token, rows of a page behind the last key) has no influence, infinities and NaN included; a score of NaN or +inf
- *   makes its token's row NaN.  One call serves decoded tokens, drafts and prompts alike, mixed as they come.
+ *   rounded to bf16 for their product with the values.  What lies in masked places (keys behind a token, rows of a page behind the
+ *   last key) has no influence, infinities and NaN included; a score of NaN or +inf makes its token's row NaN, and an infinity or NaN
+ *   among the values that a token sees makes its column of the row one, however little above 0 it weighs.  One call serves decoded
+ *   tokens, drafts and prompts alike, mixed as they come.
  *   max_new: the largest number of new tokens per sequence as far as the host knows (0: unknown).  It chooses the kernel and the
  *   size of the workspace, never the result's meaning.  Order of summation is fixed for given lengths (bit-identical run to run).
  *   Device-side waits (long chunks) are bounded and reported by resq_check on the workspace, as for the linear layer.
@@ -503,7 +505,8 @@ RESQ_API int resq_paged_attention(const void* Q_bf16, int64_t T, int64_t ldq, in
  *   accepted int32 [count]: drafts kept; tokens int64 [R]: the kept drafts, the token behind them, then -1; logp fp32 [R]: log p of
  *   each of these tokens (0 beside -1).  A row of nothing but -inf, or with NaN or +inf, keeps nothing and yields -1.  A sequence
  *   without rows has accepted 0; rows of no sequence are not written.  Decisions that 32 bits leave open are made in 64 bits from
- *   the rows' fp32 peaks and log_sums: u next to its border, ratios next to each other, little or nothing left of p - q.  workspace of resq_verify_drafts_workspace_bytes(R) bytes, 256-byte aligned. */
+ *   the rows' fp32 peaks and log_sums: u next to its border, ratios next to each other, little or nothing left of p - q.
+ *   workspace of resq_verify_drafts_workspace_bytes(R) bytes, 256-byte aligned. */
 RESQ_API size_t resq_verify_drafts_workspace_bytes(int64_t R);
 RESQ_API int resq_verify_drafts(const void* logits, int dtype, int64_t R, int64_t V, int64_t ld, const int32_t* row_start, int64_t count,
                        const int64_t* drafts, const float* u, const float* noise, int64_t lde, const void* draft_logits, int64_t ldd,

@@ -3,18 +3,21 @@
 //   O_i = sum_{j <= pos_i} p_ij v_j,   p_ij = exp(scale q_i.k_j - lse_i),   lse_i = log sum_{j <= pos_i} exp(scale q_i.k_j)
 //
 // One pass over the keys with a running reference m (the largest score so far): p = 2^(s c - m) with c = scale log2(e), the sums
-// l and O multiplied by 2^(m_old - m_new) when m grows, O / l at the end.  P is rounded to bf16 for its product with V (off by at
-// most 2^-8 of each weight, as the output is by its own rounding); scores, sums and O are fp32.
+// l and O multiplied by 2^(m_old - m_new) when m grows, O / l at the end.  P is rounded to bf16 for its product with V, since the
+// instruction takes both operands in the type that V has (off by at most 2^-8 of each weight, as the output is by its own rounding); l is
+// of the weights before that, which lse needs.  Scores, sums and O are fp32.
 //
 // Three kernels, by the query rows that share a kv head (tokens times heads of a group):
 //   attn_rows_kernel, up to 32 (decoded tokens): bound by reading the cache once.  The queries are the rows of one register-operand
 //     tensor instruction (m16n8k16), so each key is read once for all of them.  The four warps of a CTA take 16 keys each of a tile of
 //     64, with a ring of asynchronous copies of their own and their own running sums, and meet only when the item is finished:
 //     nothing in the loop waits for another warp.  64 sequences of 2000 to 12000 keys, 28 heads on 4 of 128: 176 us = 6.0 TB/s (0.92 of the
-//     copy rate); one sequence of 4000 keys 11.6 us, latency (lengths, page numbers, keys, sums, and the join of 63 parts).
-//   attn_wide_kernel, up to 64 (drafted tokens): bound by that instruction, which does 512 products of a row, a key and a channel
-//     per clock and SM, an eighth of what tensor memory allows.  24 sequences of up to 9000 keys, 2 to 6 tokens, 16 heads on 2: 40 us
-//     for 91 MB; the chunk kernel takes 44, and 31 instead of 23 for 64 sequences of 100 to 600 keys (larger fixed parts).
+//     copy rate); one sequence of 4000 keys 11.5 us, latency (lengths, page numbers, keys, sums, and the join of 63 parts).
+//   attn_wide_kernel, up to 64 (drafted tokens): bound by latencies.  That instruction does 1024 products of a row, a key and a
+//     channel per clock and SM, a quarter of what tensor memory allows, and is busy 39 % of the time, as issue slots and DRAM are 35 %:
+//     products, maxima, exponentials and products follow one another in a warp, and rows that do not exist are multiplied too.  24
+//     sequences of up to 9000 keys, 2 to 6 tokens, 16 heads on 2: 39.6 us for 91 MB; the chunk kernel takes 44, and 31 instead of 23
+//     for 64 sequences of 100 to 600 keys (larger fixed parts).
 //   attn_chunk_kernel (paged_chunk.cu), beyond.
 // Work is dealt out over the keys of all items evenly (paged.cuh), and what was cut is joined by a second kernel.
 #include "paged.cuh"

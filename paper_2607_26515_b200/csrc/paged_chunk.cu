@@ -17,8 +17,8 @@
 // lies those 20 above the maximum that it was set by: weights are at most 1, so that sums with large values overflow no sooner than
 // they have to, lose nothing in bf16 or fp32 by being 2^-20, and the final division takes the reference out.
 //
-// Measured: 8192 tokens from the beginning, 28 heads on 4 of 128, 571 us = 843 TFLOP/s (0.51 of the burst rate of a library product);
-// 512 tokens behind 31500 keys, 16 heads on 2, two sequences, 300 us = 876 TFLOP/s.  The products alone, with the weights left
+// Measured: 8192 tokens from the beginning, 28 heads on 4 of 128, 562 us = 856 TFLOP/s (0.52 of the burst rate of a library product);
+// 512 tokens behind 31500 keys, 16 heads on 2, two sequences, 299 us = 880 TFLOP/s.  The products alone, with the weights left
 // as they lie, take 379 and 214 us: S = Q K^T is bound by the reads of both operands from shared memory (115 cycles an
 // instruction instead of 64).  The rest is the way from scores to weights: 512 cycles for a half's scores out of tensor memory and
 // their maxima, 1024 for its 16384 exponentials (16 a clock), 600 of hand-overs, of which the other half hides the part that its

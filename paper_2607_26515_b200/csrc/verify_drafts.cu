@@ -7,8 +7,8 @@
 //
 // The rows' sums are resq_token_logprobs' kernel, one pass over the logits, which is what the call is bound by.  This file's kernel
 // then needs one row per sequence again (of the logits, the draft's logits and e): a cluster of 1 to 8 CTAs per sequence finds the
-// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 43.9 us (rows and
-// both launches 28.8, the deciding row 2, the drawing 13 for 67 MB, 10.2 of them at the copy rate); one such sequence 13.6 us, latency of
+// row and takes the largest w / e of its slices.  Measured: 64 sequences of 5 rows of 131072, bf16, 43.8 us (rows and
+// both launches 28.7, the deciding row 2, the drawing 13 for 67 MB, 10.2 of them at the copy rate); one such sequence 13.6 us, latency of
 // both.
 //
 // Decisions that 32 bits leave open are made in 64 bits: a probability next to its border, and a drawing where another ratio may be
@@ -372,9 +372,10 @@ int resq_verify_drafts(const void* logits, int dtype, int64_t R, int64_t V, int6
                     : resq_token_logprobs(logits, dtype, R, V, ld, drafts, temperature, 0, wl, nullptr, wp, ws_sum, nullptr, nullptr, stream);
     if (rc) return rc;
     // Few sequences: their row over a cluster, not below 4096 logits a CTA.  The 1024 threads that an SM holds are shared by the CTAs
-    // it gets, and the clusters are as large as it takes to keep most of them busy on the average: 64 sequences of 131072 take 43.1
-    // us by four CTAs of 512 threads each, 47.2 by eight of 256 (clusters of eight leave SMs of a GPC over) and 50.9 by four of
-    // 256; 100 sequences 50.3 by four of 320, 53.2 by two of 512.  Short rows get no more threads than vectors.
+    // it gets, and the clusters are as large as it takes to keep most of them busy on the average: 64 sequences of 131072 take 43.4
+    // us by four CTAs of 512 threads each, 49.9 by eight of 256 (clusters of eight leave SMs of a GPC over) and 51.0 by four of
+    // 256; 100 sequences 54.6 by four of 320, 56.6 by two of 512; one sequence 13.6 by eight of 512, 13.3 by eight of 256.  Short
+    // rows get no more threads than vectors.
     int cs = 1;
     unsigned threads = 128;
     int64_t busy = 0;
