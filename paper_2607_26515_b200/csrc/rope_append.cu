@@ -44,14 +44,43 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_constant__ RopeArgs a) {
     constexpr int C = D / 16;  // threads' shares per head
     __shared__ Place place[kMaxTokens];
+    __shared__ int owner[kMaxTokens];
     __shared__ __align__(16) float cs[kMaxTokens][D / 2], sn[kMaxTokens][D / 2];
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const int64_t t0 = (int64_t)blockIdx.x * a.tokens;
     const int nt = (int)min((int64_t)a.tokens, a.seq.T - t0);
     pdl_wait();
     pdl_trigger();
-    // ---- whose token it is: a warp looks for each token's sequence, among starts in order by 32 at a time
-    if (w < nt) {
+    // ---- whose token it is: up to 128 sequences are all asked, by a warp per token
+    const bool few = a.seq.B <= 128;
+    bool lost = false;
+    auto place_of = [&](int b) {  // of token t0 + w, if it is sequence b's
+        Place p{0, 0, -1, 0};
+        if (b >= a.seq.B) return p;
+        const Seq s = load_seq(a.seq, b);
+        const int tok = (int)t0 + w, i = tok - s.q0;
+        if (i < 0 || i >= s.n) return p;
+        const int slot = s.kv - s.n + i;
+        p.there = 1;
+        p.pos = a.positions ? a.positions[tok] : slot;
+        if (slot >= 0) p.page = page_of(a.seq, b, slot, p.row);
+        return p;
+    };
+    if (w < nt && few) {
+        int from[4], to[4], b = a.seq.B;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            from[k] = to[k] = 0;
+            if (k * 32 + lane < a.seq.B) from[k] = a.seq.q_start[k * 32 + lane], to[k] = a.seq.q_start[k * 32 + lane + 1];
+        }
+#pragma unroll
+        for (int k = 3; k >= 0; --k) {
+            const unsigned here = __ballot_sync(~0u, t0 + w >= from[k] && t0 + w < to[k]);
+            if (here) b = k * 32 + __ffs(here) - 1;
+        }
+        const Place p = place_of(b);
+        if (lane == 0) place[w] = p;
+    } else if (w < nt) {  // more are searched, 32 starts at a time
         const int tok = (int)t0 + w;
         int lo = 0, hi = a.seq.B;  // the last b in lo .. hi with q_start[b] <= tok
         while (hi > lo) {
@@ -67,33 +96,35 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
             }
             lo = at;
         }
-        Seq s{0, 0, 0};
-        if (lo < a.seq.B) s = load_seq(a.seq, lo);
-        // Starts out of order, or a row of no sequence: all of them are asked, eight loads of a lane in flight.
-        if (tok < s.q0 || tok - s.q0 >= s.n) {
-            lo = a.seq.B;
-            for (int b0 = 0; b0 < a.seq.B && lo == a.seq.B; b0 += 128) {
-                Seq each[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) each[k] = load_seq(a.seq, min(b0 + k * 32 + lane, a.seq.B - 1));
-#pragma unroll
-                for (int k = 3; k >= 0; --k) {
-                    const unsigned here = __ballot_sync(~0u, tok >= each[k].q0 && tok - each[k].q0 < each[k].n);
-                    if (here) lo = min(b0 + k * 32 + __ffs(here) - 1, a.seq.B - 1);
-                }
-            }
-            if (lo < a.seq.B) s = load_seq(a.seq, lo);
-        }
-        Place p{0, 0, -1, 0};
-        if (lo < a.seq.B) {
-            const int i = tok - s.q0, slot = s.kv - s.n + i;
-            p.there = 1;
-            p.pos = a.positions ? a.positions[tok] : slot;
-            if (slot >= 0) p.page = page_of(a.seq, lo, slot, p.row);
-        }
+        const Place p = place_of(lo);
+        lost = !p.there;
         if (lane == 0) place[w] = p;
     }
-    __syncthreads();
+    // Starts out of order, or rows of no sequence (a padded batch has them): then all are asked, once for the block's tokens (1.5 us of 8 at
+    // 256 sequences and 4096 tokens, nearly all of them padding).
+    if (few) __syncthreads();
+    else if (__syncthreads_or(lost)) {
+        if (tid < kMaxTokens) owner[tid] = a.seq.B;
+        __syncthreads();
+        for (int b0 = tid; b0 < a.seq.B; b0 += 4 * kThreads) {
+            int from[4], to[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int b = min(b0 + k * kThreads, a.seq.B - 1);
+                from[k] = a.seq.q_start[b], to[k] = a.seq.q_start[b + 1];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                for (int64_t t = max((int64_t)from[k] - t0, (int64_t)0); t < nt && t0 + t < to[k]; ++t)
+                    atomicMin(&owner[t], min(b0 + k * kThreads, a.seq.B - 1));
+        }
+        __syncthreads();
+        if (lost) {
+            const Place p = place_of(owner[w]);
+            if (lane == 0) place[w] = p;
+        }
+        __syncthreads();
+    }
     const int heads = a.Hq + 2 * a.Hkv, per_token = heads * C, items = nt * per_token;
     const int half = a.rot / 2, turning = a.rot / 16;
     // the two runs of 8 elements of a share, within its head

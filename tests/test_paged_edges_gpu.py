@@ -72,7 +72,13 @@ def test_attention_values_of_any_size(n, keys, size):
 
 # ------------------------------------------------------------------------------------------------ starts out of order
 
-@pytest.mark.parametrize("starts, T", [([4, 9, 2, 4], 12), ([20, 3, 3, 0, 2, -4], 12), ([50, 60, 0, 9, 10, 40, 44], 70), ([5, 2 ** 31 - 1, -3, 2, 1, -2 ** 31], 9)])
+def backwards(n):
+    """n sequences of two rows from the last to the first, and between them n - 1 without rows."""
+    return [x for i in range(n - 1, -1, -1) for x in (2 * i, 2 * i + 2)]
+
+
+@pytest.mark.parametrize("starts, T", [([4, 9, 2, 4], 12), ([20, 3, 3, 0, 2, -4], 12), ([50, 60, 0, 9, 10, 40, 44], 70), ([5, 2 ** 31 - 1, -3, 2, 1, -2 ** 31], 9),
+                                       (backwards(64), 140), (backwards(65), 130), (backwards(700), 1409)])
 def test_append_starts_out_of_order(starts, T):
     """Every sequence has the rows from its start to its end, wherever the others lie; the lists give each row to one sequence at most."""
     B = len(starts) - 1
@@ -93,7 +99,7 @@ def test_append_starts_out_of_order(starts, T):
     assert ((p.k.double() - want[1]).abs() <= tol(want[1])).all() and ((p.v.double() - want[2]).abs() <= tol(want[2])).all()
 
 
-@pytest.mark.parametrize("B", [1, 40, 4096])
+@pytest.mark.parametrize("B", [1, 40, 128, 129, 300, 4096])
 def test_append_rows_behind_many_sequences(B):
     """Rows of no sequence are looked for in all of them, and stay as they were."""
     p = Paged([(i % 2, 3) for i in range(B)] if B > 1 else [(1, 3)], 1, 64, 8)
