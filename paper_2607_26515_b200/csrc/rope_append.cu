@@ -11,7 +11,7 @@
 // Bound by HBM: every element is read and written once.  A block takes one to eight tokens; its threads first compute the tokens'
 // sines and cosines (two each for eight tokens of 128-wide heads, shared by all heads), with their first elements already on the
 // way, then take 16 elements each: the two runs of 8 that turn into each other.  Measured: 16384 tokens of 28 + 2 x 4 heads of 128, bf16 with
-// bias, 54.9 us = 5.5 TB/s (0.84 of the copy rate); one token 2.8 us.
+// bias, 54.5 us = 5.5 TB/s (0.85 of the copy rate); one token 2.9 us.
 #include "paged.cuh"
 
 #include <algorithm>
